@@ -52,12 +52,12 @@ enum { MIXFP4_MODE_MIX = 0,        /* Alg. 1: per-block E2M1/E1M2 by lower MSE *
        MIXFP4_MODE_FOUR_SIX = 3    /* the {E2M1(6), E2M1(4)} candidate set of Sec. 2.4 ("4/6"):
                                       per block the lower-MSE of s8 from B/6 or B/4 (B/4 on a
                                       tie), E2M1 codes, T = 0 (plain NVFP4 bits, so both GEMMs
-                                      take it); mixfp4_quantize and mixfp4_quantize_noalloc only */ };
+                                      take it); mixfp4_quantize, mixfp4_quantize_noalloc, mixfp4_kv_append only */ };
 
 enum { MIXFP4_SCALE_COMPUTE = 0,   /* compute s32 = fl32(max|x| / 2688), write *tensor_scale */
        MIXFP4_SCALE_GIVEN = 1      /* read s32 from *tensor_scale */ };
 
-enum { MIXFP4_DTYPE_BF16 = 0, MIXFP4_DTYPE_F32 = 1 /* output of mixfp4_fake_quantize only */ };
+enum { MIXFP4_DTYPE_BF16 = 0, MIXFP4_DTYPE_F32 = 1 /* mixfp4_fake_quantize's output, mixfp4_kv_append's input, mixfp4_kv_gather's output */ };
 
 /* Candidate formats of mixfp4_fake_quantize (bit c of `candidates`). */
 enum { MIXFP4_CAND_E2M1_6 = 1,   /* E2M1, block max mapped to 6 (Algorithm 1's E2M1) */
@@ -443,6 +443,182 @@ int mixfp4_gemm_native_fewrows(const uint8_t* a_codes, const uint8_t* a_scales, 
 int mixfp4_quantize_noalloc(const void* x, int dtype, int64_t rows, int64_t K, int64_t ldx,
                             uint8_t* codes, uint8_t* scales, float* tensor_scale, int mode,
                             void* stream);
+
+/*
+ * mixfp4_kv_cache -- one layer's paged cache of keys and values, the state of
+ * the attention between the linear layers (no counterpart in the paper, which
+ * leaves attention in BF16; a MixFP4 cache stores each head's row as
+ * Algorithm 1's codes and scale bytes, Sec. 3.2, blocks along head_dim, under
+ * one given tensor scale for all keys and one for all values).
+ *
+ * Element d of token position o of page p, head h is at
+ *   p * page_stride + o * token_stride + h * head_stride + d
+ * of k and of v (d / 2 for codes, low nibble first): pages may hold
+ * [token][head][d] or [head][token][d], and k and v may be slices of one
+ * buffer.  A MixFP4 cache's scale bytes are addressed likewise by the scale
+ * strides (block d / 16).  A slot is p * page_size + o.
+ *
+ * dtype        MIXFP4_CACHE_BF16 or MIXFP4_CACHE_MIXFP4.
+ * page_size    tokens of a page, >= 1.    heads  key heads, >= 1.
+ * head_dim     a multiple of 16, 16 .. 256.    pages  >= 0.
+ * k, v         device, bf16 (32-byte aligned, strides multiples of 16 elements)
+ *              or uint8 codes (8-byte aligned, strides multiples of 8 bytes).
+ * k_scales, v_scales   device, uint8; MixFP4 only.  Where head_dim % 64 == 0 they are
+ *              aligned to head_dim / 16 bytes, strides too.
+ * k_ts, v_ts   device, one float each: the tensor scales; MixFP4 only.
+ * Strides are >= 0; places of different elements must not coincide.
+ */
+enum { MIXFP4_CACHE_BF16 = 0, MIXFP4_CACHE_MIXFP4 = 1 };
+
+typedef struct {
+  int32_t dtype;
+  int32_t page_size;
+  int32_t heads;
+  int32_t head_dim;
+  int64_t pages;
+  void* k;
+  void* v;
+  int64_t page_stride, token_stride, head_stride;
+  uint8_t* k_scales;
+  uint8_t* v_scales;
+  int64_t scale_page_stride, scale_token_stride, scale_head_stride;
+  const float* k_ts;
+  const float* v_ts;
+} mixfp4_kv_cache;
+
+/*
+ * mixfp4_kv_append -- the new tokens' keys and values into a mixfp4_kv_cache,
+ * queries and keys rotated to their positions on the way:
+ *   (a, b) -> (fl32(fl32(a c) - fl32(b s)), fl32(fl32(b c) + fl32(a s)))
+ * for the pairs (i, i + rot_dim / 2), or with `interleaved` (2i, 2i + 1), of a
+ * head's first rot_dim elements, with (c, s) = entries i and rot_dim / 2 + i of
+ * row positions[t] of cos_sin.  Rotated queries, and keys and values for a
+ * bf16 cache, are rounded to bf16 (nearest even); for a MixFP4 cache
+ * Algorithm 1 runs on the fp32 rows as in mixfp4_quantize with
+ * MIXFP4_SCALE_GIVEN (values past the scale's range saturate).
+ *
+ * q, k, v      device, `dtype` MIXFP4_DTYPE_BF16 or MIXFP4_DTYPE_F32 (what the
+ *              linear layer returns): element d of head h of token t at
+ *              t * token stride + h * head stride + d; 32-byte aligned, strides
+ *              multiples of 16 elements.  q = NULL: no queries (q_heads 0).
+ * T            tokens, >= 0.
+ * positions    device, int64 [T]; cos_sin  device, float [max_positions][rot_dim],
+ *              32-byte aligned; both unused with rot_dim = 0 (no rotation).
+ *              rot_dim is even, 0 .. head_dim.
+ * slots        device, int64 [T]: where token t goes.  A slot outside the cache (-1
+ *              for a padding token) keeps nothing.  Slots of one call differ.
+ * q_out        device, bf16 [T][q_heads][head_dim], 32-byte aligned.       (output)
+ * mode         MIXFP4_MODE_* of a MixFP4 cache's blocks.
+ * A token whose position is outside the table keeps nothing, and its rotated
+ * query is NaN.
+ */
+int mixfp4_kv_append(const void* q, int64_t q_token_stride, int64_t q_head_stride, int64_t q_heads, const void* k,
+                     int64_t k_token_stride, int64_t k_head_stride, const void* v, int64_t v_token_stride,
+                     int64_t v_head_stride, int dtype, int64_t T, const int64_t* positions, const float* cos_sin,
+                     int64_t max_positions, int64_t rot_dim, int interleaved, const mixfp4_kv_cache* cache,
+                     const int64_t* slots, void* q_out, int mode, void* stream);
+
+/*
+ * mixfp4_kv_gather -- rows of a mixfp4_kv_cache as values, in the order of
+ * `slots` (a cached prefix for the attention of a longer prompt, or a
+ * sequence's rows to keep elsewhere).  A MixFP4 row is decoded as
+ * mixfp4_dequantize does, then rounded to out_dtype.
+ *
+ * slots        device, int64 [T]; a slot outside the cache gives zeros.
+ * k_out, v_out device, [T][heads][head_dim] of out_dtype (MIXFP4_DTYPE_BF16 or
+ *              MIXFP4_DTYPE_F32), 32-byte aligned.                        (output)
+ */
+int mixfp4_kv_gather(const mixfp4_kv_cache* cache, const int64_t* slots, int64_t T, void* k_out, void* v_out,
+                     int out_dtype, void* stream);
+
+/*
+ * mixfp4_paged_attention -- attention of one new token per sequence over a
+ * mixfp4_kv_cache: for query head h of sequence b, with the key head
+ * h / (q_heads / heads) and j over the sequence's tokens that are seen,
+ *   s_j = scale * q . k_j,   out = sum_j exp(s_j - lse) v_j,   lse = log sum_j exp(s_j).
+ * Products are exact, sums and the softmax in fp32 (the weights enter the
+ * second product as two bf16 parts, or for a MixFP4 cache as f16 of 11 bits),
+ * and out is rounded to bf16.  A sequence that sees no token gives out = 0 and
+ * lse = -inf.  The tokens' axis is cut over the GPU and joined, in an order
+ * that depends on the arguments alone.
+ *
+ * q            device, bf16: element d of head h of sequence b at
+ *              b * q_stride + h * q_head_stride + d; 16-byte aligned, strides
+ *              multiples of 8.
+ * B, q_heads   B >= 0; q_heads a multiple of the cache's heads.
+ * block_table  device, int32 [B][table_stride]: the pages of each sequence in
+ *              order, table_pages of them at most.  Entries past a sequence's length
+ *              are not read; a token on a page outside the cache is not seen.
+ * lengths      device, int32 [B]: tokens of each sequence in the cache, the new one
+ *              included; at most table_pages * page_size are looked at, and less
+ *              than 1 is none.
+ * window       0: every token is seen; else the last `window` ones.
+ * out          device, bf16 [B][q_heads][head_dim], 16-byte aligned.       (output)
+ * lse          device, float [B][q_heads], or NULL.                        (output)
+ * workspace    device, 256-byte aligned, at least the bytes
+ *              mixfp4_paged_attention_workspace reports; free for reuse once the
+ *              call's work on `stream` is done.
+ */
+int mixfp4_paged_attention(const void* q, int64_t q_stride, int64_t q_head_stride, int64_t B, int64_t q_heads,
+                           const mixfp4_kv_cache* cache, const int32_t* block_table, int64_t table_stride,
+                           int64_t table_pages, const int32_t* lengths, float scale, int64_t window, void* out,
+                           float* lse, void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
+ * mixfp4_paged_attention_workspace -- bytes of workspace mixfp4_paged_attention
+ * takes for B sequences of q_heads on the current device.
+ *
+ * bytes        host, one int64.                                          (output)
+ */
+int mixfp4_paged_attention_workspace(const mixfp4_kv_cache* cache, int64_t B, int64_t q_heads, int64_t* bytes);
+
+/*
+ * mixfp4_lora -- low-rank adapters of many requests at once beside a shared
+ * projection (mixfp4_linear; no counterpart in the paper): for the tokens t of
+ * segment i, with its adapter j = ids[i],
+ *   u_t = A_j x_t,   out_t = base_t + scaling_j B_j u_t.
+ * Products are exact, u and all sums fp32.  A segment whose id is outside
+ * 0 .. adapters - 1 (-1) has no adapter: u = 0, out = base.
+ *
+ * x, dtype     device, bf16 (MIXFP4_DTYPE_BF16) [T][ldx]; 16-byte aligned, ldx % 8 == 0.
+ * K, N         K % 16 == 0; N needs no padding; both at most 2^24.
+ * a, b         device, bf16 [adapters][R][K] and [adapters][N][R], 16-byte aligned.
+ *              R % 8 == 0, 8 .. 128 (smaller ranks: zeros).
+ * scaling      device, float [adapters].    adapters  0 .. 65535.
+ * starts       device, int32 [segments + 1], not decreasing, starts[0] = 0 and
+ *              starts[segments] = T; a segment may be empty.  Tokens outside every
+ *              segment are neither read nor written.
+ * ids          device, int32 [segments].    segments  at most 2^20.
+ * base         device, float [T][ld_base], or NULL for zeros; may be out.
+ * out          device, float [T][ld_out] (16-byte alignment and strides % 4 == 0
+ *              enable vector stores).                                    (output)
+ * u            device, float [T][R], 16-byte aligned: what the backward pass
+ *              needs.                                                    (output)
+ */
+int mixfp4_lora(const void* x, int dtype, int64_t T, int64_t K, int64_t ldx, const void* a, const void* b,
+                const float* scaling, int64_t adapters, int64_t R, int64_t N, const int32_t* starts,
+                const int32_t* ids, int64_t segments, const float* base, int64_t ld_base, float* out, int64_t ld_out,
+                float* u, void* stream);
+
+/*
+ * mixfp4_lora_backward -- the gradients of mixfp4_lora, given that of its
+ * output: with v_t = scaling_j B_j^T dy_t,
+ *   dx_t = base_t + A_j^T v_t,   da_j = sum_t v_t x_t^T,   db_j = scaling_j sum_t dy_t u_t^T,
+ * the sums over the tokens of all segments with adapter j (zeros where there are
+ * none).  base is the input gradient of the projection itself, or NULL.
+ *
+ * dy           device, bf16 [T][ldy]; 16-byte aligned, ldy % 8 == 0; N % 16 == 0.
+ * u            device, float [T][R], as mixfp4_lora wrote it.
+ * dx           device, float [T][ld_dx]; may be base.                    (output)
+ * da, db       device, float [adapters][R][K] and [adapters][N][R].      (output)
+ * v            device, float [T][R], 16-byte aligned: scratch memory.
+ * Other arguments, alignment and errors: as mixfp4_lora.
+ */
+int mixfp4_lora_backward(const void* dy, int64_t ldy, const void* x, int64_t ldx, int dtype, int64_t T, int64_t K,
+                         const float* u, const void* a, const void* b, const float* scaling, int64_t adapters,
+                         int64_t R, int64_t N, const int32_t* starts, const int32_t* ids, int64_t segments,
+                         const float* base, int64_t ld_base, float* dx, int64_t ld_dx, float* da, float* db, float* v,
+                         void* stream);
 
 /* Human-readable name of a mixfp4_status value (static string). */
 const char* mixfp4_status_string(int status);

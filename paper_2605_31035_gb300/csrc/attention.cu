@@ -1,0 +1,721 @@
+// Attention of one new token per sequence over the paged cache
+// (mixfp4_paged_attention).
+//
+// The cache's rows are read once and met by few queries (q_heads / heads of
+// them per key head), so the kernel is bound by HBM: 4 G flops per element
+// read, with G = 4 a twentieth of what the tensor cores do meanwhile.  What
+// matters is that enough bytes are in flight and that nothing else stands in
+// their way:
+//
+//   * Each warp streams 16 tokens at a time into a ring of its own with 16-byte
+//     cp.async (rows of a page are 32 to 512 bytes apart from each other, at
+//     places the block table gives), and every thread reads back only what it
+//     copied itself: no barrier stands between load and use, and 64-bit
+//     addresses are formed once per row.
+//   * Tokens are the rows of m16n8k16 products and query heads their 8 columns,
+//     so no query row is padded to 16.  S = K Q^T takes K's rows as they lie
+//     (four dimensions per thread and step, Q permuted alike); O^T = V^T P^T
+//     takes V's as token pairs, put together by byte permutes, and P^T out of
+//     S's registers by an 8 x 8 transpose.  m16n8k16 moves these operands from
+//     registers; a tcgen05.mma would want them in shared memory in a layout that
+//     a paged row does not have.
+//   * The weights P keep 16 bits of mantissa in two bf16 parts (one product
+//     each) on a bf16 cache.  On a MixFP4 cache a row's values times its block
+//     scales are exact in f16, Q is scaled per head by a power of two into f16
+//     (exact but for elements 2^-29 below the largest), and P takes 11 bits: the
+//     4-bit rows themselves hold 3.
+//   * Sequences differ in length, so the axis (sequence, key head, token) is cut
+//     into equal shares of 64-token units, one per CTA; where a CTA's share ends
+//     inside a row's tokens, both sides leave a partial result (m, l, O) in the
+//     workspace, and a second small kernel, launched early, joins them in order.
+#include <cuda_runtime.h>
+#include <atomic>
+#include <cstdint>
+
+#include "decode.cuh"
+#include "host_util.cuh"
+#include "kernels.cuh"
+#include "kvcache.cuh"
+#include "ptx.cuh"
+
+namespace mixfp4 {
+namespace {
+
+constexpr int kWarps = 4;
+constexpr int kThreads = kWarps * 32;
+constexpr int kUnit = 64;  // tokens of a unit of work
+constexpr unsigned kAll = 0xFFFFFFFFu;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr int kFp4Exp = 14;  // a MixFP4 cache's weights are 2^14 p: f16 then reaches down to 2^-38 of the largest
+
+struct AttnArgs {
+  const uint16_t* q;
+  int64_t q_stride, q_head_stride;
+  int B, q_heads, group, chunks;  // group = q_heads / heads; chunks of 8 NT query heads per key head
+  mixfp4_kv_cache c;
+  int page_shift;  // log2 page_size, or -1
+  const int32_t* table;
+  int64_t table_stride;
+  int64_t max_tokens;
+  const int32_t* lengths;
+  float scale;
+  int64_t window;
+  uint16_t* out;
+  float* lse;
+  float* part;    // [2 grid][8 NT][DT], the partial results
+  float2* stat;   // [2 grid][8 NT] (m, l)
+  int4* split;    // [grid]: a row that goes on in later CTAs: (sequence, head chunk, last CTA, 0); x < 0: none
+};
+
+template <int DT, int NT, bool kFp4>
+struct Cfg {
+  static constexpr int kHeads = 8 * NT;
+  static constexpr int kVBytes = kFp4 ? (DT == 64 ? 4 : 8) : 16;       // a thread's piece of a V row
+  static constexpr int kVDims = kFp4 ? 2 * kVBytes : 8;
+  static constexpr int kVPieces = DT / (8 * kVDims);
+  static constexpr int kKBytes = kFp4 ? 8 : 16;                        // and of a K row
+  static constexpr int kKDims = kFp4 ? 16 : 8;
+  static constexpr int kKPieces = DT / (4 * kKDims);
+  static constexpr int kKTile = 2 * kKPieces * 32 * kKBytes, kVTile = 4 * kVPieces * 32 * kVBytes;
+  static constexpr int kScaleTile = kFp4 ? 32 * 16 : 0;                // 16 scale bytes a row at most
+  static constexpr int kStage = kKTile + kVTile + kScaleTile;
+  static constexpr int kBudget = (DT == 256 && !kFp4) ? 200 * 1024 : 98 * 1024;
+  static constexpr int kStages = kBudget / (kWarps * kStage) < 8 ? kBudget / (kWarps * kStage) : 8;
+  static constexpr int kRing = kWarps * kStages * kStage;
+  static constexpr int kMerge = kWarps * kHeads * (DT + 4) * 4;
+  static constexpr int kSmem = kRing > kMerge ? kRing : kMerge;
+};
+
+template <int kBytes>
+__device__ __forceinline__ void cp_async(uint32_t dst, const void* src, bool take) {
+  const int n = take ? kBytes : 0;
+  if constexpr (kBytes == 16)
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+  else
+    asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(dst), "l"(src), "n"(kBytes), "r"(n) : "memory");
+}
+__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int n>
+__device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(n) : "memory"); }
+
+__device__ __forceinline__ uint4 lds128(uint32_t a) {
+  uint4 v;
+  asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
+  return v;
+}
+__device__ __forceinline__ uint2 lds64(uint32_t a) {
+  uint2 v;
+  asm volatile("ld.shared.v2.b32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a) : "memory");
+  return v;
+}
+__device__ __forceinline__ uint32_t lds32(uint32_t a) {
+  uint32_t v;
+  asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
+  return v;
+}
+__device__ __forceinline__ uint32_t lds8(uint32_t a) {
+  uint32_t v;
+  asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
+  return v;
+}
+__device__ __forceinline__ void sts8(uint32_t a, uint32_t v) {
+  asm volatile("st.shared.u8 [%0], %1;" ::"r"(a), "r"(v) : "memory");
+}
+
+template <bool kF16>
+__device__ __forceinline__ void mma16816(float d[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                         uint32_t b1) {
+  if constexpr (kF16)
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+  else
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// The transpose of an 8 x 8 matrix of 16-bit elements, thread (g, t) = (lane / 4, lane % 4) holding row g, columns 2t, 2t + 1.
+__device__ __forceinline__ uint32_t transpose8(uint32_t v) {
+  uint32_t d;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(v));
+  return d;
+}
+__device__ __forceinline__ uint32_t bf16x2(float lo, float hi) {
+  uint32_t d;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+  return d;
+}
+__device__ __forceinline__ uint32_t f16x2(float lo, float hi) {
+  uint32_t d;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+  return d;
+}
+__device__ __forceinline__ float bf_lo(uint32_t v) { return __uint_as_float(v << 16); }
+__device__ __forceinline__ float bf_hi(uint32_t v) { return __uint_as_float(v & 0xFFFF0000u); }
+
+// Tokens [first, end) of sequence b that are seen.
+__device__ __forceinline__ int2 seen(const AttnArgs& p, int b) {
+  int64_t n = p.lengths[b];
+  n = n < p.max_tokens ? n : p.max_tokens;
+  n = n > 0 ? n : 0;
+  const int64_t lo = p.window > 0 && n > p.window ? n - p.window : 0;
+  return make_int2((int)lo, (int)n);
+}
+__device__ __forceinline__ int units(int2 r) { return (r.y - r.x + kUnit - 1) / kUnit; }
+
+// One output element pair of a finished row.
+__device__ __forceinline__ void store_out(const AttnArgs& p, int b, int h, int d, float x, float y) {
+  *reinterpret_cast<uint32_t*>(p.out + ((int64_t)b * p.q_heads + h) * p.c.head_dim + d) = bf16x2(x, y);
+}
+
+template <int DT, int NT, bool kFp4>
+__global__ void __launch_bounds__(kThreads) paged_attention_kernel(const AttnArgs p) {
+  using C = Cfg<DT, NT, kFp4>;
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ int sh_b;
+  __shared__ int64_t sh_before, sh_scan[kWarps];
+  griddep_launch_dependents();
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
+  const int D = p.c.head_dim;
+  const int rows = p.c.heads * p.chunks;  // rows of work of a sequence
+
+  // This CTA's share [pos, end) of all units, and the sequence it starts in.
+  const int strip = (p.B + kThreads - 1) / kThreads;
+  int64_t mine = 0;
+  for (int b = tid * strip; b < min(p.B, (tid + 1) * strip); ++b) mine += units(seen(p, b));
+  int64_t before = mine;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const int64_t v = __shfl_up_sync(kAll, before, d);
+    if (lane >= d) before += v;
+  }
+  if (lane == 31) sh_scan[warp] = before;
+  __syncthreads();
+  int64_t total = 0;
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) {
+    if (w < warp) before += sh_scan[w];
+    total += sh_scan[w];
+  }
+  before -= mine;
+  const int64_t all = total * rows;
+  const int64_t grid = all < (int64_t)gridDim.x ? all : (int64_t)gridDim.x;  // CTAs with a share
+  for (int b = blockIdx.x; b < p.B; b += gridDim.x) {  // sequences that see nothing
+    const int2 r = seen(p, b);
+    if (r.y > r.x) continue;
+    for (int i = tid; i < p.q_heads * D / 2; i += kThreads)
+      reinterpret_cast<uint32_t*>(p.out)[(int64_t)b * p.q_heads * D / 2 + i] = 0u;
+    if (p.lse)
+      for (int h = tid; h < p.q_heads; h += kThreads) p.lse[(int64_t)b * p.q_heads + h] = -INFINITY;
+  }
+  if (tid == 0) p.split[blockIdx.x] = make_int4(-1, 0, 0, 0);
+  if ((int64_t)blockIdx.x >= grid) return;
+  int64_t pos = all * blockIdx.x / grid;
+  const int64_t end = all * (blockIdx.x + 1) / grid;
+  if (pos >= before * rows && pos < (before + mine) * rows) {
+    int b = tid * strip;
+    int64_t at = before;
+    for (const int to = min(p.B, b + strip) - 1; b < to; ++b) {
+      const int u = units(seen(p, b));
+      if (pos < (at + u) * rows) break;
+      at += u;
+    }
+    sh_b = b;
+    sh_before = at;
+  }
+  __syncthreads();
+  int b = sh_b;
+  int64_t base = sh_before * rows;  // first unit of sequence b
+
+  const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem) + warp * C::kStages * C::kStage;
+  const float kts = kFp4 ? *p.c.k_ts : 1.0f, vts = kFp4 ? *p.c.v_ts : 1.0f;
+
+  while (pos < end && b < p.B) {
+    const int2 range = seen(p, b);
+    const int u = units(range);
+    if (u == 0 || pos >= base + (int64_t)u * rows) {  // the next sequence (this one may have no unit)
+      base += (int64_t)u * rows;
+      ++b;
+      continue;
+    }
+    const int row = (int)((pos - base) / u);
+    const int k0 = (int)((pos - base) - (int64_t)row * u);
+    const int cnt = (int)min((int64_t)(u - k0), end - pos);
+    const int head = row / p.chunks, h0 = head * p.group + (row - head * p.chunks) * C::kHeads;
+    const int nh = min(C::kHeads, (head + 1) * p.group - h0);  // query heads of this row
+    const int tok0 = range.x + k0 * kUnit, tok1 = min(range.y, tok0 + cnt * kUnit);
+
+    // ---- the queries: B fragments, thread (g, t) holding head g's dimensions of its K pieces
+    uint32_t qf[NT][DT / 16][2];
+    float fs[NT][2];  // factor of the scores of heads 2t, 2t + 1 (of the 8 NT)
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      const int h = 8 * n + g;
+      const uint16_t* q = p.q + (int64_t)b * p.q_stride + (int64_t)(h0 + h) * p.q_head_stride;
+      float top = 0.0f;
+#pragma unroll
+      for (int i = 0; i < C::kKPieces; ++i) {
+        const int d = (t + 4 * i) * C::kKDims;
+#pragma unroll
+        for (int s = 0; s < C::kKDims / 8; ++s) {
+          uint4 w = make_uint4(0, 0, 0, 0);
+          if (h < nh && d < D) w = *reinterpret_cast<const uint4*>(q + d + 8 * s);
+          const int st = (i * C::kKDims / 8 + s) * 2;
+          qf[n][st][0] = w.x, qf[n][st][1] = w.y, qf[n][st + 1][0] = w.z, qf[n][st + 1][1] = w.w;
+          if (kFp4) {
+            const uint32_t v[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) top = max3f(top, fabsf(bf_lo(v[j])), fabsf(bf_hi(v[j])));
+          }
+        }
+      }
+      float back = 1.0f;
+      if (kFp4) {  // q times 2^(14 - exponent of the head's largest) as f16
+        top = fmaxf(top, __shfl_xor_sync(kAll, top, 1));
+        top = fmaxf(top, __shfl_xor_sync(kAll, top, 2));
+        int e = (int)(__float_as_uint(top) >> 23);
+        e = min(max(e, 15), 253);
+        const float up = __uint_as_float((uint32_t)(268 - e) << 23);
+        back = __uint_as_float((uint32_t)(e - 14) << 23);
+#pragma unroll
+        for (int s = 0; s < DT / 16; ++s)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) qf[n][s][j] = f16x2(bf_lo(qf[n][s][j]) * up, bf_hi(qf[n][s][j]) * up);
+      }
+      const float f = p.scale * kLog2e * (kFp4 ? 0.5f * kts : 1.0f);  // the decoded rows are twice the values
+#pragma unroll
+      for (int j = 0; j < 2; ++j) fs[n][j] = f * (kFp4 ? __shfl_sync(kAll, back, (2 * t + j) * 4) : 1.0f);
+    }
+
+    // ---- the ring: this warp's tiles are 16 tokens at tok0 + 16 (warp + kWarps i)
+    const int tiles_all = (tok1 - tok0 + 15) / 16;
+    const int tiles = tiles_all > warp ? (tiles_all - warp + kWarps - 1) / kWarps : 0;
+    const int32_t* table = p.table + (int64_t)b * p.table_stride;
+    const uint8_t* kb = static_cast<const uint8_t*>(p.c.k) + (int64_t)head * p.c.head_stride * (kFp4 ? 1 : 2);
+    const uint8_t* vb = static_cast<const uint8_t*>(p.c.v) + (int64_t)head * p.c.head_stride * (kFp4 ? 1 : 2);
+    const uint8_t* sb = nullptr;
+    if (kFp4) sb = (lane < 16 ? p.c.k_scales : p.c.v_scales) + (int64_t)head * p.c.scale_head_stride;
+
+    // Lane l looks after token l % 16 of a tile: its page, asked for a tile ahead.
+    auto tile_token = [&](int i) { return tok0 + 16 * (warp + kWarps * i) + (lane & 15); };
+    auto page_of = [&](int tok) { return p.page_shift >= 0 ? tok >> p.page_shift : tok / p.c.page_size; };
+    auto ask = [&](int i) -> int {
+      const int tok = tile_token(i);
+      return i < tiles && tok < tok1 ? table[page_of(tok)] : -1;
+    };
+    int asked = ask(0);
+    auto issue = [&](int i) -> uint32_t {
+      const int page = asked;
+      asked = ask(i + 1);
+      const bool ok = page >= 0 && page < p.c.pages;
+      const int tok = tile_token(i);
+      const int off = tok - page_of(tok) * p.c.page_size;
+      int64_t at = ok ? (int64_t)page * p.c.page_stride + (int64_t)off * p.c.token_stride : 0;
+      if (!kFp4) at *= 2;
+      const uint32_t there = __ballot_sync(kAll, ok) & 0xFFFFu;
+      const uint32_t dst = ring + (i % C::kStages) * C::kStage;
+      const uint32_t kd = dst + lane * C::kKBytes, vd = dst + C::kKTile + lane * C::kVBytes;
+#pragma unroll
+      for (int r = 0; r < 2; ++r) {
+        const int64_t ra = __shfl_sync(kAll, at, g + 8 * r);
+        const bool take = (there >> (g + 8 * r)) & 1u;
+#pragma unroll
+        for (int k = 0; k < C::kKPieces; ++k) {
+          const int c = t + 4 * k;
+          cp_async<C::kKBytes>(kd + (r * C::kKPieces + k) * 32 * C::kKBytes, kb + ra + c * C::kKBytes,
+                               take && c * C::kKDims < D);
+        }
+      }
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int tr = 2 * t + (r & 1) + 8 * (r >> 1);
+        const int64_t ra = __shfl_sync(kAll, at, tr);
+        const bool take = (there >> tr) & 1u;
+#pragma unroll
+        for (int k = 0; k < C::kVPieces; ++k) {
+          const int c = g + 8 * k;
+          cp_async<C::kVBytes>(vd + (r * C::kVPieces + k) * 32 * C::kVBytes, vb + ra + c * C::kVBytes,
+                               take && c * C::kVDims < D);
+        }
+      }
+      if (kFp4) {
+        const int64_t sa = ok ? (int64_t)page * p.c.scale_page_stride + (int64_t)off * p.c.scale_token_stride : 0;
+        const uint32_t sd = dst + C::kKTile + C::kVTile + lane * 16;
+        if (D == 128) {
+          cp_async<8>(sd, sb + sa, ok);
+        } else if (D == 256) {
+          cp_async<16>(sd, sb + sa, ok);
+        } else if (D % 64 == 0) {
+          for (int k = 0; k < D / 16; k += 4) cp_async<4>(sd + k, sb + sa + k, ok);
+        } else {  // rows of an odd number of scale bytes
+          for (int k = 0; k < D / 16; ++k) sts8(sd + k, ok ? sb[sa + k] : 0u);
+        }
+      }
+      return there;
+    };
+
+    uint32_t there[C::kStages];  // which of a tile's tokens there are; there[0]: the tile to be used next
+#pragma unroll
+    for (int i = 0; i < C::kStages; ++i) there[i] = 0;
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < C::kStages - 1; ++i) {
+      if (i < tiles) there[i] = issue(i);
+      cp_commit();
+    }
+
+    float o[NT][DT / 16][4];
+    float m[NT][2], l[NT][2];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      m[n][0] = m[n][1] = -INFINITY;
+      l[n][0] = l[n][1] = 0.0f;
+#pragma unroll
+      for (int i = 0; i < DT / 16; ++i) o[n][i][0] = o[n][i][1] = o[n][i][2] = o[n][i][3] = 0.0f;
+    }
+
+    for (int i = 0; i < tiles; ++i) {
+      __syncwarp();  // the stage about to be filled again has been read by every lane
+      if (i + C::kStages - 1 < tiles) there[C::kStages - 1] = issue(i + C::kStages - 1);
+      cp_commit();
+      cp_wait<C::kStages - 1>();
+      __syncwarp();
+      const uint32_t src = ring + (i % C::kStages) * C::kStage;
+      const uint32_t ks = src + lane * C::kKBytes, vs = src + C::kKTile + lane * C::kVBytes;
+      const uint32_t ss = src + C::kKTile + C::kVTile;
+
+      // ---- scores of 16 tokens x 8 NT heads
+      float s[NT][4];
+#pragma unroll
+      for (int n = 0; n < NT; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.0f;
+#pragma unroll
+      for (int k = 0; k < C::kKPieces; ++k) {
+        uint32_t w[2][C::kKDims / 2];  // rows g and g + 8
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          const uint32_t a = ks + (r * C::kKPieces + k) * 32 * C::kKBytes;
+          if constexpr (kFp4) {
+            const uint2 v = lds64(a);
+            // beyond D the codes are zeros and the scale bytes whatever lay there
+            const uint32_t sc = (t + 4 * k) * 16 < D ? lds8(ss + (g + 8 * r) * 16 + t + 4 * k) : 0u;
+            const bool one = sc >> 7;
+            const uint32_t s2 = cvt_f16x2_from_e4m3x2((uint16_t)((sc & 0x7Fu) * 0x0101u));
+            const uint32_t ll = one ? kLutE1M2Lo : kLutE2M1Lo, lh = one ? kLutE1M2Hi : kLutE2M1Hi;
+            decode8(v.x, ll, lh, s2, w[r]);
+            decode8(v.y, ll, lh, s2, w[r] + 4);
+          } else {
+            const uint4 v = lds128(a);
+            w[r][0] = v.x, w[r][1] = v.y, w[r][2] = v.z, w[r][3] = v.w;
+          }
+        }
+#pragma unroll
+        for (int st = 0; st < C::kKDims / 4; ++st)
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+            mma16816<kFp4>(s[n], w[0][2 * st], w[1][2 * st], w[0][2 * st + 1], w[1][2 * st + 1],
+                           qf[n][k * C::kKDims / 4 + st][0], qf[n][k * C::kKDims / 4 + st][1]);
+      }
+      const bool ok0 = (there[0] >> g) & 1u, ok1 = (there[0] >> (g + 8)) & 1u;
+
+      // ---- softmax: running maximum and weights, thread (g, t) for tokens g, g + 8 and heads 2t, 2t + 1
+      uint32_t ph[NT][2], pl[NT][2];
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        float mn[2], cor[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          s[n][j] = ok0 ? s[n][j] * fs[n][j] : -INFINITY;
+          s[n][2 + j] = ok1 ? s[n][2 + j] * fs[n][j] : -INFINITY;
+          float v = fmaxf(s[n][j], s[n][2 + j]);
+          v = fmaxf(v, __shfl_xor_sync(kAll, v, 4));
+          v = fmaxf(v, __shfl_xor_sync(kAll, v, 8));
+          v = fmaxf(v, __shfl_xor_sync(kAll, v, 16));
+          mn[j] = fmaxf(m[n][j], v);
+        }
+        const bool moved = mn[0] > m[n][0] || mn[1] > m[n][1];
+        if (__any_sync(kAll, moved)) {
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            cor[j] = mn[j] == -INFINITY ? 1.0f : exp2f(m[n][j] - mn[j]);
+            l[n][j] *= cor[j];
+            m[n][j] = mn[j];
+          }
+#pragma unroll
+          for (int k = 0; k < DT / 16; ++k) {
+            o[n][k][0] *= cor[0], o[n][k][1] *= cor[1], o[n][k][2] *= cor[0], o[n][k][3] *= cor[1];
+          }
+        }
+        float w[4];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const float top = m[n][j] == -INFINITY ? 0.0f : m[n][j];
+          w[j] = exp2f(s[n][j] - top + (kFp4 ? (float)kFp4Exp : 0.0f));
+          w[2 + j] = exp2f(s[n][2 + j] - top + (kFp4 ? (float)kFp4Exp : 0.0f));
+          l[n][j] += w[j] + w[2 + j];
+        }
+        if (kFp4) {
+          ph[n][0] = transpose8(f16x2(w[0], w[1]));
+          ph[n][1] = transpose8(f16x2(w[2], w[3]));
+        } else {
+          const uint32_t a = bf16x2(w[0], w[1]), c = bf16x2(w[2], w[3]);
+          ph[n][0] = transpose8(a);
+          ph[n][1] = transpose8(c);
+          pl[n][0] = transpose8(bf16x2(w[0] - bf_lo(a), w[1] - bf_hi(a)));
+          pl[n][1] = transpose8(bf16x2(w[2] - bf_lo(c), w[3] - bf_hi(c)));
+        }
+      }
+
+      // ---- O^T += V^T P^T: rows g and g + 8 of product (k, j) are dimensions 2j, 2j + 1 of the thread's piece k
+#pragma unroll
+      for (int k = 0; k < C::kVPieces; ++k) {
+        uint32_t w[4][C::kVDims / 2];  // tokens 2t, 2t + 1, 2t + 8, 2t + 9
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const uint32_t a = vs + (r * C::kVPieces + k) * 32 * C::kVBytes;
+          if constexpr (kFp4) {
+            const int tr = 2 * t + (r & 1) + 8 * (r >> 1);
+            const int d = (g + 8 * k) * C::kVDims;
+            const uint32_t sc = d < D ? lds8(ss + (16 + tr) * 16 + d / 16) : 0u;
+            const bool one = sc >> 7;
+            const uint32_t s2 = cvt_f16x2_from_e4m3x2((uint16_t)((sc & 0x7Fu) * 0x0101u));
+            const uint32_t ll = one ? kLutE1M2Lo : kLutE2M1Lo, lh = one ? kLutE1M2Hi : kLutE2M1Hi;
+            if constexpr (C::kVBytes == 8) {
+              const uint2 v = lds64(a);
+              decode8(v.x, ll, lh, s2, w[r]);
+              decode8(v.y, ll, lh, s2, w[r] + 4);
+            } else {
+              decode8(lds32(a), ll, lh, s2, w[r]);
+            }
+          } else {
+            const uint4 v = lds128(a);
+            w[r][0] = v.x, w[r][1] = v.y, w[r][2] = v.z, w[r][3] = v.w;
+          }
+        }
+#pragma unroll
+        for (int j = 0; j < C::kVDims / 2; ++j) {
+          const uint32_t a0 = prmt(w[0][j], w[1][j], 0x5410u), a1 = prmt(w[0][j], w[1][j], 0x7632u);
+          const uint32_t a2 = prmt(w[2][j], w[3][j], 0x5410u), a3 = prmt(w[2][j], w[3][j], 0x7632u);
+#pragma unroll
+          for (int n = 0; n < NT; ++n) {
+            float* acc = o[n][k * C::kVDims / 2 + j];
+            mma16816<kFp4>(acc, a0, a1, a2, a3, ph[n][0], ph[n][1]);
+            if (!kFp4) mma16816<kFp4>(acc, a0, a1, a2, a3, pl[n][0], pl[n][1]);
+          }
+        }
+      }
+#pragma unroll
+      for (int k = 0; k + 1 < C::kStages; ++k) there[k] = there[k + 1];
+    }
+    cp_wait<0>();
+
+    // ---- the warps' results joined in shared memory (the ring is drained)
+    __syncthreads();
+    float* mo = reinterpret_cast<float*>(smem);                              // [warp][head][DT]
+    float* ms = mo + kWarps * C::kHeads * DT;                                // [warp][head] m, then l
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        float v = l[n][j];
+        v += __shfl_xor_sync(kAll, v, 4);
+        v += __shfl_xor_sync(kAll, v, 8);
+        v += __shfl_xor_sync(kAll, v, 16);
+        const int h = 8 * n + 2 * t + j;
+        if (g == 0) {
+          ms[(warp * C::kHeads + h) * 2] = m[n][j];
+          ms[(warp * C::kHeads + h) * 2 + 1] = v;
+        }
+        float* to = mo + (warp * C::kHeads + h) * DT;
+#pragma unroll
+        for (int k = 0; k < C::kVPieces; ++k)
+#pragma unroll
+          for (int i = 0; i < C::kVDims / 2; ++i) {
+            const int d = (g + 8 * k) * C::kVDims + 2 * i;
+            const float* acc = o[n][k * C::kVDims / 2 + i];
+            *reinterpret_cast<float2*>(to + d) = make_float2(acc[j], acc[2 + j]);
+          }
+      }
+    }
+    __syncthreads();
+    const bool first = k0 == 0, last = k0 + cnt == u;
+    const int64_t slot = 2 * (int64_t)blockIdx.x + (first ? 1 : 0);
+    for (int i = tid; i < nh * (DT / 2); i += kThreads) {
+      const int h = i / (DT / 2), d = (i - h * (DT / 2)) * 2;
+      float M = -INFINITY, L = 0.0f;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) M = fmaxf(M, ms[(w * C::kHeads + h) * 2]);
+      float x = 0.0f, y = 0.0f;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) {
+        const float f = M == -INFINITY ? 0.0f : exp2f(ms[(w * C::kHeads + h) * 2] - M);
+        const float2 v = *reinterpret_cast<const float2*>(mo + (w * C::kHeads + h) * DT + d);
+        L += f * ms[(w * C::kHeads + h) * 2 + 1];
+        x += f * v.x;
+        y += f * v.y;
+      }
+      if (first && last) {
+        const float f = L > 0.0f ? (kFp4 ? 0.5f * vts : 1.0f) / L : 0.0f;
+        if (d < D) store_out(p, b, h0 + h, d, x * f, y * f);
+        if (d == 0 && p.lse)
+          p.lse[(int64_t)b * p.q_heads + h0 + h] =
+              L > 0.0f ? (M + log2f(L) - (kFp4 ? (float)kFp4Exp : 0.0f)) * kLn2 : -INFINITY;
+      } else {
+        *reinterpret_cast<float2*>(p.part + (slot * C::kHeads + h) * DT + d) = make_float2(x, y);
+        if (d == 0) p.stat[slot * C::kHeads + h] = make_float2(M, L);
+      }
+    }
+    if (tid == 0 && first && !last) {
+      const int64_t x = base + (int64_t)(row + 1) * u;  // behind the row's last unit
+      p.split[blockIdx.x] = make_int4(b, row, (int)((x * grid - 1) / all), 0);
+    }
+    __syncthreads();
+    pos += cnt;
+  }
+}
+
+// Joins the parts of the row that CTA blockIdx.x of the first kernel began and
+// did not finish, for one query head of it: 32 lanes over the dimensions, the
+// parts shared out to the four warps.
+template <int DT, int NT, bool kFp4>
+__global__ void __launch_bounds__(kThreads) paged_attention_join_kernel(const AttnArgs p) {
+  constexpr int kHeads = 8 * NT, kV = DT / 32;
+  __shared__ float red[kWarps][DT + 2];
+  griddep_wait();
+  const int4 s = p.split[blockIdx.x];
+  if (s.x < 0) return;
+  const int h = blockIdx.y, head = s.y / p.chunks, h0 = head * p.group + (s.y - head * p.chunks) * kHeads;
+  if (h0 + h >= (head + 1) * p.group) return;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int parts = s.z - (int)blockIdx.x + 1;
+  auto slot = [&](int i) { return (2 * ((int64_t)blockIdx.x + i) + (i == 0 ? 1 : 0)) * kHeads + h; };
+  float M = -INFINITY;
+  for (int i = lane; i < parts; i += 32) M = fmaxf(M, p.stat[slot(i)].x);
+#pragma unroll
+  for (int d = 16; d; d >>= 1) M = fmaxf(M, __shfl_xor_sync(kAll, M, d));
+  float acc[kV], L = 0.0f;
+#pragma unroll
+  for (int j = 0; j < kV; ++j) acc[j] = 0.0f;
+  if (M != -INFINITY) {
+#pragma unroll 4
+    for (int i = warp; i < parts; i += kWarps) {
+      const float2 st = p.stat[slot(i)];
+      const float f = exp2f(st.x - M);
+      L += f * st.y;
+      const float* o = p.part + slot(i) * DT + lane;
+#pragma unroll
+      for (int j = 0; j < kV; ++j) acc[j] += f * o[32 * j];
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < kV; ++j) red[warp][lane + 32 * j] = acc[j];
+  if (lane == 0) red[warp][DT] = L;
+  __syncthreads();
+  L = red[0][DT] + red[1][DT] + red[2][DT] + red[3][DT];
+  const float f = L > 0.0f ? (kFp4 ? 0.5f * *p.c.v_ts : 1.0f) / L : 0.0f;
+  for (int d = 2 * threadIdx.x; d < p.c.head_dim; d += 2 * kThreads) {
+    const float x = red[0][d] + red[1][d] + red[2][d] + red[3][d];
+    const float y = red[0][d + 1] + red[1][d + 1] + red[2][d + 1] + red[3][d + 1];
+    store_out(p, s.x, h0 + h, d, x * f, y * f);
+  }
+  if (threadIdx.x == 0 && p.lse)
+    p.lse[(int64_t)s.x * p.q_heads + h0 + h] =
+        L > 0.0f ? (M + log2f(L) - (kFp4 ? (float)kFp4Exp : 0.0f)) * kLn2 : -INFINITY;
+}
+
+inline bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
+inline int launch_status() { return cudaGetLastError() == cudaSuccess ? MIXFP4_OK : MIXFP4_ERR_CUDA; }
+
+inline int padded_dim(int D) { return D <= 64 ? 64 : (D <= 128 ? 128 : 256); }
+inline int padded_heads(int64_t group) { return group <= 8 ? 8 : 16; }
+// CTAs of the first kernel: as many as the device holds at once, two to an SM
+// where two rings fit.
+inline int grid_of(const mixfp4_kv_cache* c) {
+  return num_sms() * (padded_dim(c->head_dim) == 256 && c->dtype == MIXFP4_CACHE_BF16 ? 1 : 2);
+}
+
+template <int DT, int NT, bool kFp4>
+int launch(const AttnArgs& p, int grid, cudaStream_t s) {
+  using C = Cfg<DT, NT, kFp4>;
+  static std::atomic<uint64_t> done{0};
+  auto* kernel = paged_attention_kernel<DT, NT, kFp4>;
+  if (!set_dynamic_smem_once(reinterpret_cast<const void*>(kernel), C::kSmem, done)) return MIXFP4_ERR_CUDA;
+  kernel<<<grid, kThreads, C::kSmem, s>>>(p);
+  if (int st = launch_status()) return st;
+  const dim3 jg((unsigned)grid, (unsigned)(p.group < C::kHeads ? p.group : C::kHeads));
+  return launch_pdl(paged_attention_join_kernel<DT, NT, kFp4>, jg, dim3(kThreads), 0, s, p) == cudaSuccess
+             ? MIXFP4_OK
+             : MIXFP4_ERR_CUDA;
+}
+
+template <int DT, bool kFp4>
+int launch_heads(const AttnArgs& p, int grid, cudaStream_t s) {
+  return padded_heads(p.group) == 8 ? launch<DT, 1, kFp4>(p, grid, s) : launch<DT, 2, kFp4>(p, grid, s);
+}
+
+template <bool kFp4>
+int launch_dim(const AttnArgs& p, int grid, cudaStream_t s) {
+  switch (padded_dim(p.c.head_dim)) {
+    case 64: return launch_heads<64, kFp4>(p, grid, s);
+    case 128: return launch_heads<128, kFp4>(p, grid, s);
+    default: return launch_heads<256, kFp4>(p, grid, s);
+  }
+}
+
+}  // namespace
+}  // namespace mixfp4
+
+extern "C" {
+
+int mixfp4_paged_attention_workspace(const mixfp4_kv_cache* cache, int64_t B, int64_t q_heads, int64_t* bytes) {
+  using namespace mixfp4;
+  if (int st = check_kv_cache(cache)) return st;
+  if (!bytes) return MIXFP4_ERR_NULL;
+  if (B < 0 || q_heads < 0 || q_heads % cache->heads != 0) return MIXFP4_ERR_SHAPE;
+  *bytes = 0;
+  if (B == 0 || q_heads == 0) return MIXFP4_OK;
+  const int64_t grid = grid_of(cache), heads = padded_heads(q_heads / cache->heads);
+  *bytes = grid * 16 + 2 * grid * heads * 8 + 2 * grid * heads * padded_dim(cache->head_dim) * 4;
+  return MIXFP4_OK;
+}
+
+int mixfp4_paged_attention(const void* q, int64_t q_stride, int64_t q_head_stride, int64_t B, int64_t q_heads,
+                           const mixfp4_kv_cache* cache, const int32_t* block_table, int64_t table_stride,
+                           int64_t table_pages, const int32_t* lengths, float scale, int64_t window, void* out,
+                           float* lse, void* workspace, int64_t workspace_bytes, void* stream) {
+  using namespace mixfp4;
+  int64_t need = 0;
+  if (int st = mixfp4_paged_attention_workspace(cache, B, q_heads, &need)) return st;
+  if (B > INT32_MAX || q_heads > INT32_MAX || q_stride < 0 || q_head_stride < 0 || table_stride < 0 ||
+      table_pages < 0 || table_stride < table_pages || table_pages > (INT32_MAX - 4096) / cache->page_size || window < 0 ||
+      workspace_bytes < need)
+    return MIXFP4_ERR_SHAPE;
+  if (B == 0 || q_heads == 0) return MIXFP4_OK;
+  if (!q || !out || !lengths || !workspace || (table_pages > 0 && !block_table)) return MIXFP4_ERR_NULL;
+  if (!aligned(q, 16) || q_stride % 8 || q_head_stride % 8 || !aligned(block_table, 4) || !aligned(lengths, 4) ||
+      !aligned(out, 16) || !aligned(lse, 4) || !aligned(workspace, 256))
+    return MIXFP4_ERR_ALIGN;
+  const int grid = grid_of(cache);
+  const int64_t heads = padded_heads(q_heads / cache->heads);
+  AttnArgs p = {};
+  p.q = static_cast<const uint16_t*>(q);
+  p.q_stride = q_stride, p.q_head_stride = q_head_stride;
+  p.B = (int)B, p.q_heads = (int)q_heads, p.group = (int)(q_heads / cache->heads);
+  p.chunks = (int)((p.group + heads - 1) / heads);
+  p.c = *cache;
+  p.page_shift = -1;
+  for (int i = 0; i < 31; ++i)
+    if (cache->page_size == 1 << i) p.page_shift = i;
+  p.table = block_table, p.table_stride = table_stride;
+  p.max_tokens = table_pages * cache->page_size;
+  p.lengths = lengths;
+  p.scale = scale, p.window = window;
+  p.out = static_cast<uint16_t*>(out), p.lse = lse;
+  uint8_t* w = static_cast<uint8_t*>(workspace);
+  p.split = reinterpret_cast<int4*>(w);
+  p.stat = reinterpret_cast<float2*>(w + (int64_t)grid * 16);
+  p.part = reinterpret_cast<float*>(w + (int64_t)grid * 16 + 2 * (int64_t)grid * heads * 8);
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  return cache->dtype == MIXFP4_CACHE_MIXFP4 ? launch_dim<true>(p, grid, s) : launch_dim<false>(p, grid, s);
+}
+
+}  // extern "C"

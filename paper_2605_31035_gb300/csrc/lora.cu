@@ -1,0 +1,654 @@
+// Low-rank adapters of many requests beside a shared projection
+// (mixfp4_lora, mixfp4_lora_backward).  Tokens lie request by request; a
+// request's tokens use its adapter (A [R][K], B [N][R], scaling s):
+//
+//   u = x A^T             shrink   y  = base + s u B^T     expand
+//   v = s dy B            shrink   dx = base + v A         expand
+//   dA = sum_t v^T x      grad     dB = s sum_t dy^T u     grad
+//
+// R is small, so every product is bound by reading its tall operand (x, dy) or
+// by reading and writing its wide result (y, dx) once: 2 R flops per element of
+// 2 to 8 bytes.  All three kernels feed m16n8k16 products from registers, which
+// global loads fill directly: which 16 contraction indices a step covers, and
+// which column a result register holds, is free, so each thread takes 8 or 16
+// bytes that lie together.  A matrix that lies the other way round is put
+// together from row pairs by byte permutes.
+//
+// u and v are fp32.  Where they enter a product they are cut into three bf16
+// parts (24 bits), one product each, so nothing but the inputs' own bf16 is
+// rounded below fp32; sums are fp32, each warp's tensor-core chain a share of
+// the whole.  The order of every sum depends on the arguments alone (no
+// atomics).
+#include <cuda_runtime.h>
+#include <atomic>
+#include <cstdint>
+
+#include "host_util.cuh"
+#include "kernels.cuh"
+#include "ptx.cuh"
+
+namespace mixfp4 {
+namespace {
+
+constexpr unsigned kAll = 0xFFFFFFFFu;
+constexpr int kWarps = 8;
+constexpr int kThreads = kWarps * 32;
+
+__device__ __forceinline__ void mma_bf16(float d[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                         uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t bf16x2(float lo, float hi) {
+  uint32_t d;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+  return d;
+}
+// A pair of fp32 as three pairs of bf16 whose sum it is (to 24 bits).
+__device__ __forceinline__ void split3(float lo, float hi, uint32_t w[3]) {
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    w[i] = bf16x2(lo, hi);
+    lo = __fsub_rn(lo, __uint_as_float(w[i] << 16));
+    hi = __fsub_rn(hi, __uint_as_float(w[i] & 0xFFFF0000u));
+  }
+}
+
+__device__ __forceinline__ uint32_t smem_addr(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+// A float of the same shared variable in CTA `rank` of the cluster (after a cluster barrier).
+__device__ __forceinline__ float peer_load(uint32_t addr, uint32_t rank) {
+  float v;
+  asm volatile("{ .reg .b32 r; mapa.shared::cluster.u32 r, %1, %2; ld.shared::cluster.f32 %0, [r]; }"
+               : "=f"(v) : "r"(addr), "r"(rank) : "memory");
+  return v;
+}
+__device__ __forceinline__ void cluster_barrier() {
+  asm volatile("barrier.cluster.arrive.aligned;\n barrier.cluster.wait.aligned;" ::: "memory");
+}
+
+struct Segments {
+  const int32_t* starts;  // [count + 1]
+  const int32_t* ids;     // [count]
+  int count, adapters;
+  int64_t tokens;
+};
+
+__device__ __forceinline__ int2 bounds(const Segments& s, int i) {
+  const int T = (int)s.tokens;
+  const int a = min(max(s.starts[i], 0), T), b = min(max(s.starts[i + 1], 0), T);
+  return make_int2(a, max(a, b));
+}
+__device__ __forceinline__ int adapter_of(const Segments& s, int i) {
+  const int a = s.ids[i];
+  return a >= 0 && a < s.adapters ? a : -1;
+}
+
+struct Tile {
+  int t0, t1, adapter;
+};
+
+// The `index`-th tile of at most kTile tokens, counted through the segments in
+// order (t0 = t1: there is none).  All threads of the CTA call this.
+template <int kTile>
+__device__ __forceinline__ Tile find_tile(const Segments& s, int index) {
+  __shared__ int scan[kWarps];
+  __shared__ int found[3];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int strip = (s.count + kThreads - 1) / kThreads;
+  const int lo = min(s.count, tid * strip), hi = min(s.count, lo + strip);
+  int mine = 0;
+  for (int i = lo; i < hi; ++i) {
+    const int2 r = bounds(s, i);
+    mine += (r.y - r.x + kTile - 1) / kTile;
+  }
+  int before = mine;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const int v = __shfl_up_sync(kAll, before, d);
+    if (lane >= d) before += v;
+  }
+  if (lane == 31) scan[warp] = before;
+  if (tid == 0) found[0] = found[1] = 0, found[2] = -1;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w)
+    if (w < warp) before += scan[w];
+  before -= mine;
+  if (index >= before && index < before + mine) {
+    int at = before;
+    for (int i = lo; i < hi; ++i) {
+      const int2 r = bounds(s, i);
+      const int n = (r.y - r.x + kTile - 1) / kTile;
+      if (index < at + n) {
+        found[0] = r.x + (index - at) * kTile;
+        found[1] = min(r.y, found[0] + kTile);
+        found[2] = adapter_of(s, i);
+        break;
+      }
+      at += n;
+    }
+  }
+  __syncthreads();
+  return Tile{found[0], found[1], found[2]};
+}
+
+// ---- shrink: out[t][r] = factor_a sum_k in[t][k] W_a[r][k], k < kdim -------------------------------
+// Ranks are the rows of the products (RT tiles of 16), tokens their columns
+// (TT / 8 tiles of 8).  A step covers 32 k: thread (g, t) holds k 8t .. 8t + 7
+// of its rows.  Warps take steps in turn, the CTAs of a cluster shares of k;
+// both are summed in order through shared memory.
+struct ShrinkArgs {
+  const uint16_t* in;  // [tokens][ld]
+  int64_t ld;
+  const uint16_t* w;   // [adapters][R][kdim], or kTrans: [adapters][kdim][R]
+  const float* factor; // [adapters] or NULL
+  float* out;          // [tokens][R]
+  int64_t kdim;
+  int R, splits;
+  Segments seg;
+};
+
+template <int RT, int TT, bool kTrans>
+__global__ void __launch_bounds__(kThreads) lora_shrink_kernel(const ShrinkArgs p) {
+  extern __shared__ float part[];  // [warps][16 RT][TT], then the CTA's sum in the first
+  constexpr int kOut = 16 * RT * TT;
+  griddep_wait();  // `in` may be what the kernel before it on the stream writes
+  griddep_launch_dependents();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
+  const int split = (int)(blockIdx.x % p.splits);
+  const Tile tile = find_tile<TT>(p.seg, (int)(blockIdx.x / p.splits));
+  if (tile.t0 >= tile.t1) return;  // the whole cluster alike
+  const int r0 = blockIdx.y * 16 * RT;
+  if (tile.adapter < 0) {
+    if (split == 0)
+      for (int i = threadIdx.x; i < kOut; i += kThreads) {
+        const int tok = tile.t0 + i / (16 * RT), r = r0 + i % (16 * RT);
+        if (tok < tile.t1 && r < p.R) p.out[(int64_t)tok * p.R + r] = 0.0f;
+      }
+    return;
+  }
+  const uint16_t* w = p.w + (int64_t)tile.adapter * p.R * p.kdim;
+  const int64_t steps = (p.kdim + 31) / 32;
+  const int64_t s0 = steps * split / p.splits, s1 = steps * (split + 1) / p.splits;
+
+  float acc[RT][TT / 8][4];
+#pragma unroll
+  for (int i = 0; i < RT; ++i)
+#pragma unroll
+    for (int n = 0; n < TT / 8; ++n) acc[i][n][0] = acc[i][n][1] = acc[i][n][2] = acc[i][n][3] = 0.0f;
+
+  const uint4 zero = make_uint4(0, 0, 0, 0);
+#pragma unroll 2
+  for (int64_t s = s0 + warp; s < s1; s += kWarps) {
+    const int64_t k = s * 32 + 8 * t;
+    const bool in_k = k < p.kdim;
+    uint4 x[TT / 8];
+#pragma unroll
+    for (int n = 0; n < TT / 8; ++n) {
+      const int tok = tile.t0 + 8 * n + g;
+      x[n] = in_k && tok < tile.t1 ? *reinterpret_cast<const uint4*>(p.in + (int64_t)tok * p.ld + k) : zero;
+    }
+    if (!kTrans) {
+      uint4 a[RT][2];
+#pragma unroll
+      for (int i = 0; i < RT; ++i)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int r = r0 + 16 * i + 8 * h + g;
+          a[i][h] = in_k && r < p.R ? *reinterpret_cast<const uint4*>(w + (int64_t)r * p.kdim + k) : zero;
+        }
+#pragma unroll
+      for (int i = 0; i < RT; ++i)
+#pragma unroll
+        for (int n = 0; n < TT / 8; ++n) {
+          mma_bf16(acc[i][n], a[i][0].x, a[i][1].x, a[i][0].y, a[i][1].y, x[n].x, x[n].y);
+          mma_bf16(acc[i][n], a[i][0].z, a[i][1].z, a[i][0].w, a[i][1].w, x[n].z, x[n].w);
+        }
+    } else {
+      // Rows k .. k + 7 at the thread's ranks 2 RT g ..: words of rank pairs, permuted to k pairs.
+      uint32_t a[8][RT];
+      const int r = r0 + 2 * RT * g;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const uint16_t* src = w + (k + j) * p.R + r;
+        const bool ok = in_k && r < p.R;
+        if constexpr (RT == 4) {
+          const uint4 v = ok ? *reinterpret_cast<const uint4*>(src) : zero;
+          a[j][0] = v.x, a[j][1] = v.y, a[j][2] = v.z, a[j][3] = v.w;
+        } else if constexpr (RT == 2) {
+          const uint2 v = ok ? *reinterpret_cast<const uint2*>(src) : make_uint2(0, 0);
+          a[j][0] = v.x, a[j][1] = v.y;
+        } else {
+          a[j][0] = ok ? *reinterpret_cast<const uint32_t*>(src) : 0u;
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < RT; ++i)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const uint32_t a0 = prmt(a[4 * h][i], a[4 * h + 1][i], 0x5410u);
+          const uint32_t a1 = prmt(a[4 * h][i], a[4 * h + 1][i], 0x7632u);
+          const uint32_t a2 = prmt(a[4 * h + 2][i], a[4 * h + 3][i], 0x5410u);
+          const uint32_t a3 = prmt(a[4 * h + 2][i], a[4 * h + 3][i], 0x7632u);
+#pragma unroll
+          for (int n = 0; n < TT / 8; ++n)
+            mma_bf16(acc[i][n], a0, a1, a2, a3, h ? x[n].z : x[n].x, h ? x[n].w : x[n].y);
+        }
+    }
+  }
+
+  // Rank (row) and token (column) of every result register.
+#pragma unroll
+  for (int i = 0; i < RT; ++i)
+#pragma unroll
+    for (int n = 0; n < TT / 8; ++n)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int r = kTrans ? 2 * RT * g + 2 * i + (e >> 1) : 16 * i + g + 8 * (e >> 1);
+        part[(warp * TT + 8 * n + 2 * t + (e & 1)) * (16 * RT) + r] = acc[i][n][e];
+      }
+  __syncthreads();
+  for (int i = threadIdx.x; i < kOut; i += kThreads) {
+    float v = part[i];
+#pragma unroll
+    for (int q = 1; q < kWarps; ++q) v += part[q * kOut + i];
+    part[i] = v;
+  }
+  if (p.splits > 1) cluster_barrier();
+  else __syncthreads();
+  const float f = p.factor ? p.factor[tile.adapter] : 1.0f;
+  for (int i = split * kThreads + threadIdx.x; i < kOut; i += p.splits * kThreads) {
+    const int tok = tile.t0 + i / (16 * RT), r = r0 + i % (16 * RT);
+    float v = 0.0f;
+    for (int q = 0; q < p.splits; ++q) v += p.splits > 1 ? peer_load(smem_addr(part + i), q) : part[i];
+    if (tok < tile.t1 && r < p.R) p.out[(int64_t)tok * p.R + r] = f * v;
+  }
+  if (p.splits > 1) cluster_barrier();  // no CTA leaves while others read its sum
+}
+
+// ---- expand: out[t][n] = base[t][n] + factor_a sum_r u[t][r] W_a[n][r] -----------------------------
+// Tokens are the rows of the products (16), features their columns: product j
+// of a warp's 64 features has column c at feature 8 c + j, so that thread
+// (g, t) ends with features 16 t .. 16 t + 15 of tokens g and g + 8.  A step
+// covers 16 ranks, thread t holding 4 t .. 4 t + 3.
+struct ExpandArgs {
+  const float* u;      // [tokens][R]
+  const uint16_t* w;   // [adapters][N][R], or kTrans: [adapters][R][N]
+  const float* factor; // [adapters] or NULL
+  const float* base;   // [tokens][ld_base] or NULL
+  int64_t ld_base;
+  float* out;          // [tokens][ld_out]
+  int64_t ld_out;
+  int64_t N;
+  int R, vec;
+  Segments seg;
+};
+
+template <int TT, bool kTrans>
+__global__ void __launch_bounds__(kThreads) lora_expand_kernel(const ExpandArgs p) {
+  griddep_launch_dependents();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
+  const Tile tile = find_tile<TT>(p.seg, (int)blockIdx.x);
+  griddep_wait();
+  const int64_t n0 = ((int64_t)blockIdx.y * kWarps + warp) * 64;
+  if (tile.t0 >= tile.t1 || n0 >= p.N) return;
+  const uint16_t* w = p.w + (int64_t)max(tile.adapter, 0) * p.R * p.N;
+  const float f = tile.adapter < 0 ? 0.0f : (p.factor ? p.factor[tile.adapter] : 1.0f);
+  const int64_t nt = n0 + 16 * t;  // this thread's results
+  for (int m = tile.t0; m < tile.t1; m += 16) {
+    float acc[8][4];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.0f;
+    const int ta = m + g, tb = m + g + 8;
+    const bool oka = ta < tile.t1, okb = tb < tile.t1;
+    if (tile.adapter >= 0)
+      for (int r0 = 0; r0 < p.R; r0 += 16) {
+        const int r = r0 + 4 * t;
+        const bool in_r = r < p.R;
+        const float4 z = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        const float4 ua = in_r && oka ? *reinterpret_cast<const float4*>(p.u + (int64_t)ta * p.R + r) : z;
+        const float4 ub = in_r && okb ? *reinterpret_cast<const float4*>(p.u + (int64_t)tb * p.R + r) : z;
+        uint32_t a0[3], a1[3], a2[3], a3[3];
+        split3(ua.x, ua.y, a0);
+        split3(ub.x, ub.y, a1);
+        split3(ua.z, ua.w, a2);
+        split3(ub.z, ub.w, a3);
+        uint32_t b[8][2];
+        if (!kTrans) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const int64_t n = n0 + 8 * g + j;
+            const uint2 v = in_r && n < p.N ? *reinterpret_cast<const uint2*>(w + n * p.R + r) : make_uint2(0, 0);
+            b[j][0] = v.x, b[j][1] = v.y;
+          }
+        } else {
+          uint32_t q[4][4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int64_t n = n0 + 8 * g;
+            const uint4 v = in_r && n < p.N ? *reinterpret_cast<const uint4*>(w + (int64_t)(r + i) * p.N + n)
+                                            : make_uint4(0, 0, 0, 0);
+            q[i][0] = v.x, q[i][1] = v.y, q[i][2] = v.z, q[i][3] = v.w;
+          }
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            b[2 * i][0] = prmt(q[0][i], q[1][i], 0x5410u), b[2 * i + 1][0] = prmt(q[0][i], q[1][i], 0x7632u);
+            b[2 * i][1] = prmt(q[2][i], q[3][i], 0x5410u), b[2 * i + 1][1] = prmt(q[2][i], q[3][i], 0x7632u);
+          }
+        }
+#pragma unroll
+        for (int i = 2; i >= 0; --i)  // the small parts first
+#pragma unroll
+          for (int j = 0; j < 8; ++j) mma_bf16(acc[j], a0[i], a1[i], a2[i], a3[i], b[j][0], b[j][1]);
+      }
+    // acc[j]: (token g, features 16 t + j and 16 t + 8 + j), then token g + 8
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      if (!(h ? okb : oka)) continue;
+      const int64_t tok = h ? tb : ta;
+      float* o = p.out + tok * p.ld_out + nt;
+      const float* s = p.base ? p.base + tok * p.ld_base + nt : nullptr;
+      if (p.vec && nt + 16 <= p.N) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int c = 2 * h + (q >> 1), j = 4 * (q & 1);
+          float4 v = s ? *reinterpret_cast<const float4*>(s + 4 * q) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+          v.x = fmaf(f, acc[j][c], v.x), v.y = fmaf(f, acc[j + 1][c], v.y);
+          v.z = fmaf(f, acc[j + 2][c], v.z), v.w = fmaf(f, acc[j + 3][c], v.w);
+          *reinterpret_cast<float4*>(o + 4 * q) = v;
+        }
+      } else {
+#pragma unroll
+        for (int q = 0; q < 16; ++q)
+          if (nt + q < p.N) o[q] = fmaf(f, acc[q & 7][2 * h + (q >> 3)], s ? s[q] : 0.0f);
+      }
+    }
+  }
+}
+
+// ---- grad: dW_a[r][n] = factor_a sum_t c[t][r] z[t][n] over adapter a's tokens ----------------------
+// Ranks are the rows of the products (RT tiles of 16, thread g holding ranks
+// 2 RT g ..), features their columns as in expand, tokens the contraction (16
+// a step).  The tokens of an adapter are one list through its segments; the
+// CTA's warps take its steps in turn and are summed in order.
+struct GradArgs {
+  const float* c[2];       // v, u: [tokens][R]
+  const uint16_t* z[2];    // x, dy: [tokens][ld]
+  int64_t ld[2];
+  const float* factor[2];  // NULL, scaling
+  float* out[2];           // dA [adapters][R][K], dB [adapters][N][R]
+  int64_t dim[2];          // K, N
+  int blocks[2];           // 64-feature blocks of each
+  int R;
+  Segments seg;
+};
+
+template <int RT>
+__global__ void __launch_bounds__(kThreads) lora_grad_kernel(const GradArgs p) {
+  extern __shared__ float part[];  // [warps][64 features][16 RT]
+  constexpr int kOut = 16 * RT * 64;
+  __shared__ int ends[kThreads + 1], first[kThreads], count[kWarps + 1];
+  griddep_wait();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
+  const int which = (int)blockIdx.x >= p.blocks[0];
+  const int64_t n0 = (int64_t)((int)blockIdx.x - (which ? p.blocks[0] : 0)) * 64;
+  const int adapter = blockIdx.y, r0 = blockIdx.z * 16 * RT;
+  const float* c = p.c[which];
+  const uint16_t* z = p.z[which];
+  const int64_t ld = p.ld[which], N = p.dim[which];
+
+  float acc[RT][8][4];
+#pragma unroll
+  for (int i = 0; i < RT; ++i)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) acc[i][j][0] = acc[i][j][1] = acc[i][j][2] = acc[i][j][3] = 0.0f;
+
+  for (int s0 = 0; s0 < p.seg.count; s0 += kThreads) {
+    // This batch's segments of the adapter, in order: first tokens and running ends of their lengths.
+    const int i = s0 + (int)threadIdx.x;
+    int2 r = make_int2(0, 0);
+    if (i < p.seg.count && adapter_of(p.seg, i) == adapter) r = bounds(p.seg, i);
+    const int len = r.y - r.x;
+    const uint32_t some = __ballot_sync(kAll, len > 0);
+    int sum = len;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int v = __shfl_up_sync(kAll, sum, d);
+      if (lane >= d) sum += v;
+    }
+    __syncthreads();  // the batch before has been used
+    if (lane == 31) count[warp] = sum, first[warp] = __popc(some);
+    __syncthreads();
+    int at = __popc(some & ((1u << lane) - 1u)), off = sum, lists = 0, total = 0;
+    for (int q = 0; q < kWarps; ++q) {
+      if (q < warp) at += first[q], off += count[q];
+      lists += first[q], total += count[q];
+    }
+    __syncthreads();
+    if (len > 0) first[at] = r.x - (off - len), ends[at] = off;  // token = index + first
+    __syncthreads();
+    if (total == 0) continue;
+    int top = 1;
+    while (top < lists) top <<= 1;
+
+    for (int step = warp; step * 16 < total; step += kWarps) {
+      // Lane l finds token l % 16 of the step: the first list whose end lies beyond it.
+      const int want = step * 16 + (lane & 15);
+      int lo = 0;
+      for (int h = top >> 1; h; h >>= 1)
+        if (lo + h <= lists - 1 && ends[lo + h - 1] <= want) lo += h;
+      const int tok = want < total ? want + first[lo] : -1;
+      uint32_t cw[RT][2][2][3];  // [tile][row half][token pair][part]
+      uint4 zw[4];
+      float cv[4][2 * RT];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int64_t tk = __shfl_sync(kAll, tok, 2 * t + (q & 1) + 8 * (q >> 1));
+        zw[q] = tk >= 0 && n0 + 8 * g < N ? *reinterpret_cast<const uint4*>(z + tk * ld + n0 + 8 * g)
+                                          : make_uint4(0, 0, 0, 0);
+        const int rr = r0 + 2 * RT * g;
+#pragma unroll
+        for (int h = 0; h < RT; ++h) {
+          const float2 v = tk >= 0 && rr < p.R ? *reinterpret_cast<const float2*>(c + tk * p.R + rr + 2 * h)
+                                               : make_float2(0.0f, 0.0f);
+          cv[q][2 * h] = v.x, cv[q][2 * h + 1] = v.y;
+        }
+      }
+#pragma unroll
+      for (int h = 0; h < RT; ++h)
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+#pragma unroll
+          for (int q = 0; q < 2; ++q) split3(cv[2 * q][2 * h + e], cv[2 * q + 1][2 * h + e], cw[h][e][q]);
+      const uint32_t zz[4][4] = {{zw[0].x, zw[0].y, zw[0].z, zw[0].w},
+                                 {zw[1].x, zw[1].y, zw[1].z, zw[1].w},
+                                 {zw[2].x, zw[2].y, zw[2].z, zw[2].w},
+                                 {zw[3].x, zw[3].y, zw[3].z, zw[3].w}};
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const uint32_t sel = j & 1 ? 0x7632u : 0x5410u;
+        const uint32_t b0 = prmt(zz[0][j / 2], zz[1][j / 2], sel), b1 = prmt(zz[2][j / 2], zz[3][j / 2], sel);
+#pragma unroll
+        for (int h = 0; h < RT; ++h)
+#pragma unroll
+          for (int q = 2; q >= 0; --q)
+            mma_bf16(acc[h][j], cw[h][0][0][q], cw[h][1][0][q], cw[h][0][1][q], cw[h][1][1][q], b0, b1);
+      }
+    }
+  }
+
+  // acc[h][j]: ranks 2 RT g + 2 h (+ 1 for registers 2, 3), features 16 t + j (+ 8 for registers 1, 3)
+#pragma unroll
+  for (int h = 0; h < RT; ++h)
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        part[(warp * 64 + 16 * t + j + 8 * (e & 1)) * (16 * RT) + 2 * RT * g + 2 * h + (e >> 1)] = acc[h][j][e];
+  __syncthreads();
+  const float f = p.factor[which] ? p.factor[which][adapter] : 1.0f;
+  for (int i = threadIdx.x; i < kOut; i += kThreads) {
+    // dA: features run fastest; dB: ranks do
+    const int n = which ? i / (16 * RT) : i % 64, r = which ? i % (16 * RT) : i / 64;
+    float v = 0.0f;
+#pragma unroll
+    for (int q = 0; q < kWarps; ++q) v += part[(q * 64 + n) * (16 * RT) + r];
+    if (n0 + n < N && r0 + r < p.R) {
+      const int64_t to = which ? ((int64_t)adapter * N + n0 + n) * p.R + r0 + r
+                               : ((int64_t)adapter * p.R + r0 + r) * N + n0 + n;
+      p.out[which][to] = f * v;
+    }
+  }
+}
+
+inline bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
+
+template <int RT, int TT, bool kTrans>
+int launch_shrink(const ShrinkArgs& p, bool dependent, cudaStream_t s) {
+  const int smem = kWarps * 16 * RT * TT * 4;
+  auto* kernel = lora_shrink_kernel<RT, TT, kTrans>;
+  static std::atomic<uint64_t> done{0};
+  if (smem > 48 * 1024 && !set_dynamic_smem_once(reinterpret_cast<const void*>(kernel), smem, done))
+    return MIXFP4_ERR_CUDA;
+  const int64_t tiles = p.seg.tokens / TT + p.seg.count;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = (unsigned)p.splits, attr[0].val.clusterDim.y = 1, attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(tiles * p.splits), (unsigned)((p.R + 16 * RT - 1) / (16 * RT)));
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cfg.attrs = attr;
+  cfg.numAttrs = dependent ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, kernel, p) == cudaSuccess ? MIXFP4_OK : MIXFP4_ERR_CUDA;
+}
+
+template <bool kTrans>
+int shrink(ShrinkArgs p, bool dependent, cudaStream_t s) {
+  const bool few = p.seg.tokens <= 8 * (int64_t)p.seg.count;
+  const int64_t tiles = p.seg.tokens / (few ? 8 : 32) + p.seg.count;
+  const int rt = p.R <= 16 ? 1 : (p.R <= 32 ? 2 : 4);
+  const int64_t ctas = tiles * ((p.R + 16 * rt - 1) / (16 * rt));
+  p.splits = 1;
+  while (p.splits < 8 && ctas * p.splits < 2 * num_sms() && p.kdim / (p.splits * 2) >= 32 * kWarps) p.splits *= 2;
+  if (few)
+    return rt == 1   ? launch_shrink<1, 8, kTrans>(p, dependent, s)
+           : rt == 2 ? launch_shrink<2, 8, kTrans>(p, dependent, s)
+                     : launch_shrink<4, 8, kTrans>(p, dependent, s);
+  return rt == 1   ? launch_shrink<1, 32, kTrans>(p, dependent, s)
+         : rt == 2 ? launch_shrink<2, 32, kTrans>(p, dependent, s)
+                   : launch_shrink<4, 32, kTrans>(p, dependent, s);
+}
+
+template <bool kTrans>
+int expand(const ExpandArgs& p, cudaStream_t s) {
+  const bool few = p.seg.tokens <= 16 * (int64_t)p.seg.count;
+  const int64_t tiles = p.seg.tokens / (few ? 16 : 64) + p.seg.count;
+  const dim3 grid((unsigned)tiles, (unsigned)((p.N + 64 * kWarps - 1) / (64 * kWarps)));
+  const cudaError_t e = few ? launch_pdl(lora_expand_kernel<16, kTrans>, grid, dim3(kThreads), 0, s, p)
+                            : launch_pdl(lora_expand_kernel<64, kTrans>, grid, dim3(kThreads), 0, s, p);
+  return e == cudaSuccess ? MIXFP4_OK : MIXFP4_ERR_CUDA;
+}
+
+template <int RT>
+int launch_grad(const GradArgs& p, cudaStream_t s) {
+  const int smem = kWarps * 16 * RT * 64 * 4;
+  auto* kernel = lora_grad_kernel<RT>;
+  static std::atomic<uint64_t> done{0};
+  if (smem > 48 * 1024 && !set_dynamic_smem_once(reinterpret_cast<const void*>(kernel), smem, done))
+    return MIXFP4_ERR_CUDA;
+  const dim3 grid((unsigned)(p.blocks[0] + p.blocks[1]), (unsigned)p.seg.adapters,
+                  (unsigned)((p.R + 16 * RT - 1) / (16 * RT)));
+  return launch_pdl(kernel, grid, dim3(kThreads), smem, s, p) == cudaSuccess ? MIXFP4_OK : MIXFP4_ERR_CUDA;
+}
+
+// The arguments both entry points share.
+int check_lora(int64_t T, int64_t K, int64_t N, int64_t R, int64_t adapters, const void* a, const void* b,
+               const float* scaling, const int32_t* starts, const int32_t* ids, int64_t segments) {
+  if (T < 0 || T > INT32_MAX - 4096 || K < 0 || K % 16 != 0 || N < 0 || R < 8 || R > 128 || R % 8 != 0 ||
+      adapters < 0 || adapters > 65535 || segments < 0 || segments > (1 << 20) || N > ((int64_t)1 << 24) ||
+      K > ((int64_t)1 << 24))
+    return MIXFP4_ERR_SHAPE;
+  if (!starts || (segments > 0 && !ids) || (adapters > 0 && ((K > 0 && !a) || (N > 0 && !b) || !scaling)))
+    return MIXFP4_ERR_NULL;
+  if (!aligned(a, 16) || !aligned(b, 16) || !aligned(scaling, 4) || !aligned(starts, 4) || !aligned(ids, 4))
+    return MIXFP4_ERR_ALIGN;
+  return MIXFP4_OK;
+}
+
+inline bool vec_ok(const float* p, int64_t ld) { return aligned(p, 16) && ld % 4 == 0; }
+
+}  // namespace
+}  // namespace mixfp4
+
+extern "C" {
+
+int mixfp4_lora(const void* x, int dtype, int64_t T, int64_t K, int64_t ldx, const void* a, const void* b,
+                const float* scaling, int64_t adapters, int64_t R, int64_t N, const int32_t* starts,
+                const int32_t* ids, int64_t segments, const float* base, int64_t ld_base, float* out, int64_t ld_out,
+                float* u, void* stream) {
+  using namespace mixfp4;
+  if (dtype != MIXFP4_DTYPE_BF16) return MIXFP4_ERR_DTYPE;
+  if (int st = check_lora(T, K, N, R, adapters, a, b, scaling, starts, ids, segments)) return st;
+  if (ldx < K || ld_out < N || (base && ld_base < N)) return MIXFP4_ERR_SHAPE;
+  if (T == 0 || segments == 0) return MIXFP4_OK;
+  if ((K > 0 && !x) || (N > 0 && !out) || !u) return MIXFP4_ERR_NULL;
+  if (!aligned(x, 16) || ldx % 8 || !aligned(u, 16) || !aligned(out, 4) || !aligned(base, 4)) return MIXFP4_ERR_ALIGN;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  const Segments seg{starts, ids, (int)segments, (int)adapters, T};
+  const ShrinkArgs sp{static_cast<const uint16_t*>(x), ldx, static_cast<const uint16_t*>(a), nullptr, u, K,
+                      (int)R, 1, seg};
+  if (int st = shrink<false>(sp, false, s)) return st;
+  if (N == 0) return MIXFP4_OK;
+  const ExpandArgs ep{u, static_cast<const uint16_t*>(b), scaling, base, ld_base, out, ld_out, N, (int)R,
+                      vec_ok(out, ld_out) && (!base || vec_ok(base, ld_base)), seg};
+  return expand<false>(ep, s);
+}
+
+int mixfp4_lora_backward(const void* dy, int64_t ldy, const void* x, int64_t ldx, int dtype, int64_t T, int64_t K,
+                         const float* u, const void* a, const void* b, const float* scaling, int64_t adapters,
+                         int64_t R, int64_t N, const int32_t* starts, const int32_t* ids, int64_t segments,
+                         const float* base, int64_t ld_base, float* dx, int64_t ld_dx, float* da, float* db, float* v,
+                         void* stream) {
+  using namespace mixfp4;
+  if (dtype != MIXFP4_DTYPE_BF16) return MIXFP4_ERR_DTYPE;
+  if (int st = check_lora(T, K, N, R, adapters, a, b, scaling, starts, ids, segments)) return st;
+  if (N % 16 != 0 || ldx < K || ldy < N || ld_dx < K || (base && ld_base < K)) return MIXFP4_ERR_SHAPE;
+  const bool tokens = T > 0 && segments > 0;
+  if (tokens && ((K > 0 && (!x || !dx)) || (N > 0 && !dy) || !u || !v)) return MIXFP4_ERR_NULL;
+  if (adapters > 0 && ((K > 0 && !da) || (N > 0 && !db))) return MIXFP4_ERR_NULL;
+  if (!aligned(x, 16) || ldx % 8 || !aligned(dy, 16) || ldy % 8 || !aligned(u, 16) || !aligned(v, 16) ||
+      !aligned(dx, 4) || !aligned(base, 4) || !aligned(da, 4) || !aligned(db, 4))
+    return MIXFP4_ERR_ALIGN;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  const Segments seg{starts, ids, (int)segments, (int)adapters, T};
+  if (tokens) {
+    const ShrinkArgs sp{static_cast<const uint16_t*>(dy), ldy, static_cast<const uint16_t*>(b), scaling, v, N,
+                        (int)R, 1, seg};
+    if (int st = shrink<true>(sp, false, s)) return st;
+    if (K > 0) {
+      const ExpandArgs ep{v, static_cast<const uint16_t*>(a), nullptr, base, ld_base, dx, ld_dx, K, (int)R,
+                          vec_ok(dx, ld_dx) && (!base || vec_ok(base, ld_base)), seg};
+      if (int st = expand<true>(ep, s)) return st;
+    }
+  }
+  GradArgs gp = {};
+  gp.c[0] = v, gp.c[1] = u;
+  gp.z[0] = static_cast<const uint16_t*>(x), gp.z[1] = static_cast<const uint16_t*>(dy);
+  gp.ld[0] = ldx, gp.ld[1] = ldy;
+  gp.factor[1] = scaling;
+  gp.out[0] = da, gp.out[1] = db;
+  gp.dim[0] = K, gp.dim[1] = N;
+  gp.blocks[0] = (int)((K + 63) / 64), gp.blocks[1] = (int)((N + 63) / 64);
+  gp.R = (int)R;
+  gp.seg = seg;
+  if (!tokens) gp.seg.count = 0;
+  if (adapters == 0 || gp.blocks[0] + gp.blocks[1] == 0) return MIXFP4_OK;
+  return R <= 16 ? launch_grad<1>(gp, s) : launch_grad<2>(gp, s);
+}
+
+}  // extern "C"

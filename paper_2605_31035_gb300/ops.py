@@ -16,6 +16,7 @@ import torch
 MODE_MIX, MODE_E2M1_ONLY, MODE_E1M2_ONLY, MODE_FOUR_SIX = 0, 1, 2, 3
 SCALE_COMPUTE, SCALE_GIVEN = 0, 1
 DTYPE_BF16, DTYPE_F32 = 0, 1
+CACHE_BF16, CACHE_MIXFP4 = 0, 1
 # Candidates of mixfp4_fake_quantize, bit c of the mask.
 CAND_E2M1_6, CAND_E1M2, CAND_E2M1_4, CAND_E3M0 = 1, 2, 4, 8
 
@@ -26,6 +27,16 @@ _ERR_CUDA = -5
 
 _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libmixfp4.so")
 _lib = None
+
+
+class _CKVCache(ctypes.Structure):
+    """struct mixfp4_kv_cache of include/mixfp4.h."""
+    _fields_ = [("dtype", ctypes.c_int32), ("page_size", ctypes.c_int32), ("heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("pages", ctypes.c_int64), ("k", ctypes.c_void_p),
+                ("v", ctypes.c_void_p), ("page_stride", ctypes.c_int64), ("token_stride", ctypes.c_int64),
+                ("head_stride", ctypes.c_int64), ("k_scales", ctypes.c_void_p), ("v_scales", ctypes.c_void_p),
+                ("scale_page_stride", ctypes.c_int64), ("scale_token_stride", ctypes.c_int64),
+                ("scale_head_stride", ctypes.c_int64), ("k_ts", ctypes.c_void_p), ("v_ts", ctypes.c_void_p)]
 
 
 class MixFP4Error(RuntimeError):
@@ -85,6 +96,21 @@ def lib() -> ctypes.CDLL:
                                                          ctypes.c_uint64, P]
         L.mixfp4_selftest_bounded_wait.restype = I
         L.mixfp4_selftest_bounded_wait.argtypes = [P, ctypes.c_uint64, P]
+        C, F = ctypes.POINTER(_CKVCache), ctypes.c_float
+        L.mixfp4_kv_append.restype = I
+        L.mixfp4_kv_append.argtypes = [P, I64, I64, I64, P, I64, I64, P, I64, I64, I, I64, P, P, I64, I64, I, C, P, P,
+                                       I, P]
+        L.mixfp4_kv_gather.restype = I
+        L.mixfp4_kv_gather.argtypes = [C, P, I64, P, P, I, P]
+        L.mixfp4_paged_attention.restype = I
+        L.mixfp4_paged_attention.argtypes = [P, I64, I64, I64, I64, C, P, I64, I64, P, F, I64, P, P, P, I64, P]
+        L.mixfp4_paged_attention_workspace.restype = I
+        L.mixfp4_paged_attention_workspace.argtypes = [C, I64, I64, ctypes.POINTER(I64)]
+        L.mixfp4_lora.restype = I
+        L.mixfp4_lora.argtypes = [P, I, I64, I64, I64, P, P, P, I64, I64, I64, P, P, I64, P, I64, P, I64, P, P]
+        L.mixfp4_lora_backward.restype = I
+        L.mixfp4_lora_backward.argtypes = [P, I64, P, I64, I, I64, I64, P, P, P, P, I64, I64, I64, P, P, I64, P, I64,
+                                           P, I64, P, P, P, P]
         L.mixfp4_status_string.restype = ctypes.c_char_p
         L.mixfp4_status_string.argtypes = [I]
         L.mixfp4_version.restype = I
@@ -676,3 +702,370 @@ def linear(x: torch.Tensor, w_q: QTensor, mode: int = MODE_MIX, stream=None,
                 return C
             # Refused, with nothing enqueued: the two calls below say which one refuses it, and why.
     return mixfp4_gemm(mixfp4_quantize(x, mode, stream=stream), w_q, out=C, stream=stream, workspace=workspace)
+
+
+# ---- paged key-value cache and attention ---------------------------------------
+
+
+class KVCache:
+    """One layer's paged cache of keys and values (struct mixfp4_kv_cache).
+
+    bf16: k and v are bf16 [pages, page_size, heads, head_dim].
+    MixFP4: k and v are uint8 codes [..., head_dim / 2], k_scales and v_scales
+    uint8 [..., head_dim / 16], and k_ts and v_ts the float32 tensor scales (one
+    for all keys, one for all values: largest expected magnitude / 2688).
+
+    Any strides will do whose last is 1 and that k and v (and both scales) share:
+    dense pages, a [pages, heads, page_size, ...] tensor transposed, or the two
+    halves of one buffer.  The tensors stay the caller's; the cache refers to
+    them and is made once."""
+
+    def __init__(self, k, v, k_scales=None, v_scales=None, k_ts=None, v_ts=None):
+        fp4 = k_scales is not None
+        last = "head_dim / 2" if fp4 else "head_dim"
+        dtype = torch.uint8 if fp4 else torch.bfloat16
+        for t, what in ((k, "k"), (v, "v")):
+            if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype is dtype and t.dim() == 4):
+                raise ValueError(f"{what} must be a CUDA tensor [pages, page_size, heads, {last}] of {dtype}")
+        _require(k.shape == v.shape and k.device == v.device, "k and v must have one shape and device")
+        D = k.shape[3] * (2 if fp4 else 1)
+        _require(D % 16 == 0 and 16 <= D <= 256, "head_dim must be a multiple of 16 up to 256")
+        _require(k.shape[1] >= 1 and k.shape[2] >= 1, "page_size and heads must be at least 1")
+        _require(k.stride() == v.stride() and k.stride(3) == 1, "k and v must share their strides, the last of them 1")
+        self.k, self.v, self.k_scales, self.v_scales, self.k_ts, self.v_ts = k, v, k_scales, v_scales, k_ts, v_ts
+        c = _CKVCache(CACHE_MIXFP4 if fp4 else CACHE_BF16, k.shape[1], k.shape[2], D, k.shape[0], _ptr(k), _ptr(v),
+                      k.stride(0), k.stride(1), k.stride(2))
+        if fp4:
+            for t, what in ((k_scales, "k_scales"), (v_scales, "v_scales")):
+                _check_dev(t, k.device, what)
+                _require(t.dtype is torch.uint8 and t.shape == (*k.shape[:3], D // 16),
+                         f"{what} must be a uint8 tensor [pages, page_size, heads, head_dim / 16]")
+            _require(k_scales.stride() == v_scales.stride() and (k_scales.stride(3) == 1 or D == 16),
+                     "k_scales and v_scales must share their strides, the last of them 1")
+            for t, what in ((k_ts, "k_ts"), (v_ts, "v_ts")):
+                _check_scalar_f32(t, k.device, what)
+            c.k_scales, c.v_scales, c.k_ts, c.v_ts = _ptr(k_scales), _ptr(v_scales), _ptr(k_ts), _ptr(v_ts)
+            c.scale_page_stride, c.scale_token_stride, c.scale_head_stride = k_scales.stride()[:3]
+        else:
+            _require(v_scales is None and k_ts is None and v_ts is None, "a bf16 cache has no scales")
+        self._c = c
+        self._ref = ctypes.byref(c)
+        self._workspace_bytes = {}
+        self.device = k.device
+
+    @property
+    def pages(self) -> int:
+        return self._c.pages
+
+    @property
+    def page_size(self) -> int:
+        return self._c.page_size
+
+    @property
+    def heads(self) -> int:
+        return self._c.heads
+
+    @property
+    def head_dim(self) -> int:
+        return self._c.head_dim
+
+    @property
+    def mixfp4(self) -> bool:
+        return self._c.dtype == CACHE_MIXFP4
+
+
+def empty_kv_cache(pages: int, page_size: int, heads: int, head_dim: int, device, k_ts=None, v_ts=None) -> KVCache:
+    """A dense cache with uninitialised rows: bf16, or with the tensor scales k_ts
+    and v_ts (1-element float32 CUDA tensors) MixFP4."""
+    shape = (pages, page_size, heads)
+    if k_ts is None and v_ts is None:
+        return KVCache(*(torch.empty(*shape, head_dim, dtype=torch.bfloat16, device=device) for _ in range(2)))
+    parts = [torch.empty(*shape, head_dim // n, dtype=torch.uint8, device=device) for n in (2, 2, 16, 16)]
+    return KVCache(*parts, k_ts, v_ts)
+
+
+def _check_cache(cache):
+    if not isinstance(cache, KVCache):
+        raise ValueError("cache must be a KVCache")
+
+
+def _check_heads(t, dtype, heads, D, device, what: str):
+    """[tokens, heads, head_dim] on `device`, dense along head_dim."""
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.device == device and t.dtype is dtype and t.dim() == 3
+            and t.shape[2] == D and (heads is None or t.shape[1] == heads) and t.stride(2) == 1):
+        raise ValueError(f"{what} must be a {dtype} CUDA tensor [tokens, {heads if heads else 'heads'}, {D}] on "
+                         f"{device} with unit last stride")
+
+
+def _check_index(t, dtype, n, device, what: str):
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.device == device and t.dtype is dtype and t.dim() == 1
+            and t.shape[0] == n and t.is_contiguous()):
+        raise ValueError(f"{what} must be a dense {dtype} CUDA tensor of {n} elements on {device}")
+
+
+def _float_type(t):
+    if not (isinstance(t, torch.Tensor) and t.dtype in (torch.bfloat16, torch.float32)):
+        raise ValueError("k must be a bfloat16 or float32 CUDA tensor")
+    return DTYPE_BF16 if t.dtype is torch.bfloat16 else DTYPE_F32
+
+
+def mixfp4_kv_append(k: torch.Tensor, v: torch.Tensor, cache: KVCache, slots: torch.Tensor,
+                     q: torch.Tensor | None = None, positions: torch.Tensor | None = None,
+                     cos_sin: torch.Tensor | None = None, interleaved: bool = False, mode: int = MODE_MIX,
+                     out: torch.Tensor | None = None, stream=None) -> torch.Tensor | None:
+    """Put new tokens' keys and values [T, heads, head_dim] (bf16, or fp32 as
+    linear() returns them; slices of a fused projection's result will do) into
+    the cache's slots (int64 [T], page * page_size + place; -1: kept nowhere).
+
+    With cos_sin (float32 [positions, rot_dim]: cosines, then sines) and positions
+    (int64 [T]; not looked at without) keys, and queries q [T, q_heads, head_dim] of the same dtype, are
+    rotated on the way: pairs (i, i + rot_dim / 2), or (2i, 2i + 1) if interleaved.
+    Returns the (rotated) queries as bf16 [T, q_heads, head_dim], or None."""
+    _check_cache(cache)
+    code, D, dev = _float_type(k), cache.head_dim, cache.device
+    _check_heads(k, k.dtype, cache.heads, D, dev, "k")
+    _check_heads(v, k.dtype, cache.heads, D, dev, "v")
+    T = k.shape[0]
+    _require(v.shape[0] == T, "k and v must have as many tokens")
+    _check_index(slots, torch.int64, T, dev, "slots")
+    rot = rows = 0
+    if cos_sin is not None:
+        _check_index(positions, torch.int64, T, dev, "positions")
+        if not (isinstance(cos_sin, torch.Tensor) and cos_sin.is_cuda and cos_sin.device == dev
+                and cos_sin.dtype is torch.float32 and cos_sin.dim() == 2 and cos_sin.is_contiguous()
+                and cos_sin.shape[1] % 2 == 0 and cos_sin.shape[1] <= D):
+            raise ValueError("cos_sin must be a dense float32 CUDA tensor [positions, rot_dim], rot_dim even and at "
+                             "most head_dim")
+        rows, rot = cos_sin.shape
+    o, qs, heads = None, (0, 0, 0), 0
+    if q is not None:
+        _check_heads(q, k.dtype, None, D, dev, "q")
+        _require(q.shape[0] == T, "q must have as many tokens as k")
+        heads, qs = q.shape[1], q.stride()
+        if out is None:
+            o = _empty((T, heads, D), torch.bfloat16, dev, stream)
+        else:
+            o = out
+            _check_heads(o, torch.bfloat16, heads, D, dev, "out")
+            _require(o.shape[0] == T and o.is_contiguous(), "out must be dense, with as many tokens as q")
+    ks, vs = k.stride(), v.stride()
+    st = lib().mixfp4_kv_append(_ptr(q), qs[0], qs[1], heads, k.data_ptr(), ks[0], ks[1], v.data_ptr(), vs[0], vs[1],
+                                code, T, _ptr(positions), _ptr(cos_sin), rows, rot, int(interleaved), cache._ref,
+                                slots.data_ptr(), _ptr(o), int(mode), _stream(stream))
+    _check("mixfp4_kv_append", st)
+    return o
+
+
+def mixfp4_kv_gather(cache: KVCache, slots: torch.Tensor, out_dtype=torch.bfloat16, out=None, stream=None):
+    """The cache's rows in the given slots (int64 [T]) as values: (k, v), each
+    [T, heads, head_dim] of out_dtype (bfloat16 or float32); a slot outside the
+    cache gives zeros.  out: a pair of dense tensors to write."""
+    _check_cache(cache)
+    _require(out_dtype in (torch.float32, torch.bfloat16), "out_dtype must be torch.float32 or torch.bfloat16")
+    _require(isinstance(slots, torch.Tensor) and slots.dim() == 1, "slots must be 1-D")
+    T, dev = slots.shape[0], cache.device
+    _check_index(slots, torch.int64, T, dev, "slots")
+    shape = (T, cache.heads, cache.head_dim)
+    if out is None:
+        k, v = (_empty(shape, out_dtype, dev, stream) for _ in range(2))
+    else:
+        k, v = out
+        for t in (k, v):
+            _check_heads(t, out_dtype, cache.heads, cache.head_dim, dev, "out")
+            _require(t.shape[0] == T and t.is_contiguous(), "out must be dense tensors with a row per slot")
+    st = lib().mixfp4_kv_gather(cache._ref, slots.data_ptr(), T, k.data_ptr(), v.data_ptr(),
+                                DTYPE_F32 if out_dtype is torch.float32 else DTYPE_BF16, _stream(stream))
+    _check("mixfp4_kv_gather", st)
+    return k, v
+
+
+def paged_attention_workspace_bytes(cache: KVCache, B: int, q_heads: int) -> int:
+    """Bytes of scratch memory mixfp4_paged_attention takes."""
+    _check_cache(cache)
+    n = ctypes.c_int64(0)
+    _check("mixfp4_paged_attention", lib().mixfp4_paged_attention_workspace(cache._ref, B, q_heads, ctypes.byref(n)))
+    return n.value
+
+
+def mixfp4_paged_attention(q: torch.Tensor, cache: KVCache, block_table: torch.Tensor, lengths: torch.Tensor,
+                           scale: float | None = None, window: int = 0, return_lse: bool = False,
+                           out: torch.Tensor | None = None, lse: torch.Tensor | None = None,
+                           workspace: torch.Tensor | None = None, stream=None):
+    """Attention of one new token per sequence over the paged cache.
+
+    q: bf16 [B, q_heads, head_dim], q_heads a multiple of the cache's heads.
+    block_table: int32 [B, pages]: each sequence's pages in order.
+    lengths: int32 [B]: tokens of each sequence in the cache, the new one included.
+    scale: of the scores, 1 / sqrt(head_dim) by default.  window: 0, or the number
+    of last tokens that are seen.
+    Returns bf16 [B, q_heads, head_dim], with return_lse (or lse=) also the
+    log-sum-exp of the scaled scores, float32 [B, q_heads].  A sequence without
+    tokens gives zeros and -inf.
+    workspace: scratch memory of the caller's, at least
+    paged_attention_workspace_bytes(cache, B, q_heads), aligned to 256 bytes."""
+    _check_cache(cache)
+    D, dev = cache.head_dim, cache.device
+    _check_heads(q, torch.bfloat16, None, D, dev, "q")
+    B, H = q.shape[0], q.shape[1]
+    _require(H % cache.heads == 0, "q_heads must be a multiple of the cache's heads")
+    if not (isinstance(block_table, torch.Tensor) and block_table.is_cuda and block_table.device == dev
+            and block_table.dtype is torch.int32 and block_table.dim() == 2 and block_table.shape[0] == B
+            and (block_table.stride(1) == 1 or block_table.shape[1] <= 1)):
+        raise ValueError(f"block_table must be an int32 CUDA tensor [{B}, pages] on {dev} with unit column stride")
+    _check_index(lengths, torch.int32, B, dev, "lengths")
+    _require(window >= 0, "window must not be negative")
+    if out is None:
+        out = _empty((B, H, D), torch.bfloat16, dev, stream)
+    else:
+        _check_heads(out, torch.bfloat16, H, D, dev, "out")
+        _require(out.shape[0] == B and out.is_contiguous(), "out must be dense, with a row per sequence")
+    if lse is not None:
+        _check_dev(lse, dev, "lse")
+        _require(lse.dtype is torch.float32 and lse.shape == (B, H) and lse.is_contiguous(),
+                 "lse must be a dense float32 [B, q_heads] tensor")
+    elif return_lse:
+        lse = _empty((B, H), torch.float32, dev, stream)
+    if workspace is None:
+        n = cache._workspace_bytes.get((B, H))
+        if n is None:
+            n = cache._workspace_bytes[(B, H)] = paged_attention_workspace_bytes(cache, B, H)
+        workspace = _empty(n, torch.uint8, dev, stream, scratch=True)
+    else:
+        _check_scratch(workspace, dev)
+    qs, pages = q.stride(), block_table.shape[1]
+    st = lib().mixfp4_paged_attention(q.data_ptr(), qs[0], qs[1], B, H, cache._ref, block_table.data_ptr(),
+                                      max(block_table.stride(0), pages), pages, lengths.data_ptr(),
+                                      D ** -0.5 if scale is None else float(scale), int(window), out.data_ptr(),
+                                      _ptr(lse), workspace.data_ptr(), _bytes(workspace), _stream(stream))
+    _check("mixfp4_paged_attention", st)
+    return out if lse is None else (out, lse)
+
+
+# ---- low-rank adapters ----------------------------------------------------------
+
+
+class Adapters:
+    """Low-rank adapters of one projection: a bf16 [adapters, R, K], b bf16
+    [adapters, N, R], scaling float32 [adapters], dense, on one device; R a
+    multiple of 8 up to 128 (fill smaller ranks with zeros).  The tensors stay the
+    caller's, and may be changed between calls."""
+
+    def __init__(self, a: torch.Tensor, b: torch.Tensor, scaling: torch.Tensor):
+        for t, what in ((a, "a"), (b, "b")):
+            if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype is torch.bfloat16 and t.dim() == 3
+                    and t.is_contiguous()):
+                raise ValueError(f"{what} must be a dense 3-D bf16 CUDA tensor")
+        L, R, K = a.shape
+        _require(b.shape[0] == L and b.shape[2] == R and b.device == a.device,
+                 "b must be [adapters, N, R] on a's device, a [adapters, R, K]")
+        _require(8 <= R <= 128 and R % 8 == 0, "the rank must be a multiple of 8 up to 128")
+        _require(K % 16 == 0, "K must be a multiple of 16")
+        _check_index(scaling, torch.float32, L, a.device, "scaling")
+        self.a, self.b, self.scaling = a, b, scaling
+        self.count, self.rank, self.K, self.N, self.device = L, R, K, b.shape[1], a.device
+
+
+def _check_rows(t, dtype, rows, cols, device, what: str):
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.device == device and t.dtype is dtype and t.dim() == 2
+            and t.shape[0] == rows and t.shape[1] == cols and (t.stride(1) == 1 or cols <= 1)
+            and t.stride(0) >= cols):
+        raise ValueError(f"{what} must be a {dtype} CUDA tensor [{rows}, {cols}] on {device} with unit column stride")
+
+
+def _check_segments(starts, ids, T: int, device) -> int:
+    if not (isinstance(ids, torch.Tensor) and ids.dim() == 1):
+        raise ValueError("ids must be a 1-D int32 CUDA tensor")
+    S = ids.shape[0]
+    _check_index(ids, torch.int32, S, device, "ids")
+    _check_index(starts, torch.int32, S + 1, device, "starts")
+    _require(S > 0 or T == 0, "tokens without a segment")
+    return S
+
+
+def mixfp4_lora(x: torch.Tensor, adapters: Adapters, starts: torch.Tensor, ids: torch.Tensor,
+                base: torch.Tensor | None = None, out: torch.Tensor | None = None, u: torch.Tensor | None = None,
+                stream=None):
+    """The adapters of many requests beside a shared projection: for the tokens of
+    segment i, base + scaling * (x a^T) b^T with adapter ids[i].
+
+    x: bf16 [T, K], the projection's input.  starts: int32 [segments + 1], each
+    segment's first token (starts[0] = 0, the last T); ids: int32 [segments], -1
+    for none.  base: float32 [T, N], the projection's result (linear()), or None.
+    Returns (out, u): out float32 [T, N] (out=base adds in place) and u = x a^T
+    float32 [T, R], which the backward pass takes."""
+    if not isinstance(adapters, Adapters):
+        raise ValueError("adapters must be Adapters")
+    ad, dev = adapters, adapters.device
+    _check_x(x)
+    T, K = x.shape
+    _require(K == ad.K and x.device == dev, "x must have K columns, on the adapters' device")
+    S = _check_segments(starts, ids, T, dev)
+    if base is not None:
+        _check_rows(base, torch.float32, T, ad.N, dev, "base")
+    if out is None:
+        out = _empty((T, ad.N), torch.float32, dev, stream)
+    else:
+        _check_rows(out, torch.float32, T, ad.N, dev, "out")
+    u = _lora_rows(u, T, ad, stream, "u")
+    st = lib().mixfp4_lora(x.data_ptr(), DTYPE_BF16, T, K, x.stride(0), ad.a.data_ptr(), ad.b.data_ptr(),
+                           ad.scaling.data_ptr(), ad.count, ad.rank, ad.N, starts.data_ptr(), ids.data_ptr(), S,
+                           _ptr(base), 0 if base is None else max(base.stride(0), ad.N), out.data_ptr(),
+                           max(out.stride(0), ad.N), u.data_ptr(), _stream(stream))
+    _check("mixfp4_lora", st)
+    return out, u
+
+
+def _lora_rows(u, T: int, ad: Adapters, stream, what: str, scratch: bool = False):
+    if u is None:
+        return _empty((T, ad.rank), torch.float32, ad.device, stream, scratch)
+    _check_rows(u, torch.float32, T, ad.rank, ad.device, what)
+    _require(u.is_contiguous(), f"{what} must be dense")
+    return u
+
+
+def mixfp4_lora_backward(dy: torch.Tensor, x: torch.Tensor, u: torch.Tensor, adapters: Adapters,
+                         starts: torch.Tensor, ids: torch.Tensor, base: torch.Tensor | None = None,
+                         out: torch.Tensor | None = None, da: torch.Tensor | None = None,
+                         db: torch.Tensor | None = None, workspace: torch.Tensor | None = None, stream=None):
+    """Gradients of mixfp4_lora, given that of its result, dy bf16 [T, N] (N % 16 == 0),
+    and the x and u of the forward pass: (dx, da, db), all float32.
+
+    dx [T, K] = base + the adapters' share (base: the projection's own input
+    gradient, or None; out=base adds in place); da [adapters, R, K] and
+    db [adapters, N, R], zeros for an adapter without tokens.
+    workspace: dense float32 [T, R] scratch memory of the caller's."""
+    if not isinstance(adapters, Adapters):
+        raise ValueError("adapters must be Adapters")
+    ad, dev = adapters, adapters.device
+    _check_x(x)
+    T, K = x.shape
+    _require(K == ad.K and x.device == dev, "x must have K columns, on the adapters' device")
+    _check_rows(dy, torch.bfloat16, T, ad.N, dev, "dy")
+    _require(ad.N % 16 == 0, "N must be a multiple of 16")
+    S = _check_segments(starts, ids, T, dev)
+    _require(u is not None, "u is what the forward pass returned")
+    u = _lora_rows(u, T, ad, stream, "u")
+    v = _lora_rows(workspace, T, ad, stream, "workspace", scratch=True)
+    if base is not None:
+        _check_rows(base, torch.float32, T, K, dev, "base")
+    if out is None:
+        out = _empty((T, K), torch.float32, dev, stream)
+    else:
+        _check_rows(out, torch.float32, T, K, dev, "out")
+    grads = []
+    for t, like, what in ((da, ad.a, "da"), (db, ad.b, "db")):
+        if t is None:
+            t = _empty(tuple(like.shape), torch.float32, dev, stream)
+        else:
+            _check_dev(t, dev, what)
+            _require(t.dtype is torch.float32 and t.shape == like.shape and t.is_contiguous(),
+                     f"{what} must be a dense float32 tensor of the adapters' shape")
+        grads.append(t)
+    st = lib().mixfp4_lora_backward(dy.data_ptr(), max(dy.stride(0), ad.N), x.data_ptr(), x.stride(0), DTYPE_BF16, T,
+                                    K, u.data_ptr(), ad.a.data_ptr(), ad.b.data_ptr(), ad.scaling.data_ptr(),
+                                    ad.count, ad.rank, ad.N, starts.data_ptr(), ids.data_ptr(), S, _ptr(base),
+                                    0 if base is None else max(base.stride(0), K), out.data_ptr(),
+                                    max(out.stride(0), K), grads[0].data_ptr(), grads[1].data_ptr(), v.data_ptr(),
+                                    _stream(stream))
+    _check("mixfp4_lora_backward", st)
+    return out, grads[0], grads[1]
