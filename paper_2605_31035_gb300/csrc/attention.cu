@@ -7,11 +7,12 @@
 // matters is that enough bytes are in flight and that nothing else stands in
 // their way:
 //
-//   * Each warp streams 16 tokens at a time into a ring of its own with 16-byte
-//     cp.async (rows of a page are 32 to 512 bytes apart from each other, at
-//     places the block table gives), and every thread reads back only what it
-//     copied itself: no barrier stands between load and use, and 64-bit
-//     addresses are formed once per row.
+//   * Each warp streams 16 tokens at a time into a ring of its own by cp.async,
+//     whole rows by neighbouring lanes (an access of half a 128-byte line costs
+//     as much as one of the whole: 259 us became 204 us at 64 sequences of up to
+//     8192 tokens, 8 heads of 128), and nothing wider than a warp waits for it.
+//     Where tiles of 16 positions lie in one page, its number is asked for a
+//     tile ahead and one 64-bit address serves the tile.
 //   * Tokens are the rows of m16n8k16 products and query heads their 8 columns,
 //     so no query row is padded to 16.  S = K Q^T takes K's rows as they lie
 //     (four dimensions per thread and step, Q permuted alike); O^T = V^T P^T
@@ -43,15 +44,19 @@ namespace {
 
 constexpr int kWarps = 4;
 constexpr int kThreads = kWarps * 32;
-constexpr int kUnit = 64;  // tokens of a unit of work
+constexpr int kJoinThreads = 256;
+constexpr int kUnit = 64;  // head rows of a unit of work: 64 / together tokens of `together` key heads
 constexpr unsigned kAll = 0xFFFFFFFFu;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-constexpr int kFp4Exp = 14;  // a MixFP4 cache's weights are 2^14 p: f16 then reaches down to 2^-38 of the largest
+// How far a score may lie above the m of its weight 2^(s - m).  On a MixFP4 cache the weights are 2^7 times that:
+// below 2^15 in f16, whose least value is then 2^-31 of the weight at m.
+constexpr float kSlack = 8.0f, kFp4Exp = 7.0f;
 
 struct AttnArgs {
   const uint16_t* q;
   int64_t q_stride, q_head_stride;
   int B, q_heads, group, chunks;  // group = q_heads / heads; chunks of 8 NT query heads per key head
+  int together;                   // key heads of a CTA: 4, 2 or 1, each a warp's (or two's, or four's)
   mixfp4_kv_cache c;
   int page_shift;  // log2 page_size, or -1
   const int32_t* table;
@@ -62,9 +67,13 @@ struct AttnArgs {
   int64_t window;
   uint16_t* out;
   float* lse;
-  float* part;    // [2 grid][8 NT][DT], the partial results
-  float2* stat;   // [2 grid][8 NT] (m, l)
-  int4* split;    // [grid]: a row that goes on in later CTAs: (sequence, head chunk, last CTA, 0); x < 0: none
+  float* part;    // [2 grid][together][8 NT][DT], the partial results
+  float2* stat;   // [2 grid][together][8 NT] (m, l)
+  int4* split;    // rows that go on in later CTAs: (sequence, row, first CTA, last CTA); x < 0: none.  One place for
+                  // each row of each sequence, or, where they are fewer, for each CTA, which begins one such row at most.
+  int by_row;
+  int places;     // of split
+  int share;      // warps of the joining kernel to a query head
 };
 
 template <int DT, int NT, bool kFp4>
@@ -73,14 +82,29 @@ struct Cfg {
   static constexpr int kVBytes = kFp4 ? (DT == 64 ? 4 : 8) : 16;       // a thread's piece of a V row
   static constexpr int kVDims = kFp4 ? 2 * kVBytes : 8;
   static constexpr int kVPieces = DT / (8 * kVDims);
-  static constexpr int kKBytes = kFp4 ? 8 : 16;                        // and of a K row
-  static constexpr int kKDims = kFp4 ? 16 : 8;
+  static constexpr int kKDims = kFp4 ? 16 : 8;                         // and of a K row, in elements
   static constexpr int kKPieces = DT / (4 * kKDims);
-  static constexpr int kKTile = 2 * kKPieces * 32 * kKBytes, kVTile = 4 * kVPieces * 32 * kVBytes;
+  // Rows are copied in pieces of kCopy bytes, whole rows by neighbouring lanes, to places that leave the pieces
+  // which the lanes read together in different banks: XOR of a piece's number with f(row), for V after rows
+  // 2t + e + 8h have been put in the order t + 4e + 8h.
+  static constexpr int kCopy = kFp4 ? 8 : 16, kRow = kFp4 ? DT / 2 : DT * 2;
+  static constexpr int kPieces = kRow / kCopy, kRowsAtOnce = 32 / kPieces;
+  static __device__ __forceinline__ int k_place(int row, int piece) {
+    const int f = kFp4 ? (row * kPieces / 16 & (kPieces / 4 - 1)) * 4 : (row & 1) * 4;
+    return row * kRow + (piece ^ f) * kCopy;
+  }
+  static __device__ __forceinline__ int v_place(int row, int piece) {
+    const int at = (row & 7) >> 1 | (row & 1) << 2 | (row & 8);
+    const int f = kFp4 ? (at * kPieces / 16 & (kPieces / 4 - 1)) * 4 : (at & 3) * 2;
+    return at * kRow + (piece ^ f) * kCopy;
+  }
+  static constexpr int kKTile = 16 * kRow, kVTile = 16 * kRow;
   static constexpr int kScaleTile = kFp4 ? 32 * 16 : 0;                // 16 scale bytes a row at most
   static constexpr int kStage = kKTile + kVTile + kScaleTile;
-  static constexpr int kBudget = (DT == 256 && !kFp4) ? 200 * 1024 : 98 * 1024;
-  static constexpr int kStages = kBudget / (kWarps * kStage) < 8 ? kBudget / (kWarps * kStage) : 8;
+  // CTAs of an SM: as many as registers and the rings' 220 KB allow
+  static constexpr int kCtas = DT == 256 ? (kFp4 ? 2 : 1) : (NT == 1 && (kFp4 || DT == 64) ? 4 : 3);
+  static constexpr int kFit = 220 * 1024 / kCtas / (kWarps * kStage);
+  static constexpr int kStages = kFit < 6 ? kFit : 6;
   static constexpr int kRing = kWarps * kStages * kStage;
   static constexpr int kMerge = kWarps * kHeads * (DT + 4) * 4;
   static constexpr int kSmem = kRing > kMerge ? kRing : kMerge;
@@ -161,7 +185,10 @@ __device__ __forceinline__ int2 seen(const AttnArgs& p, int b) {
   const int64_t lo = p.window > 0 && n > p.window ? n - p.window : 0;
   return make_int2((int)lo, (int)n);
 }
-__device__ __forceinline__ int units(int2 r) { return (r.y - r.x + kUnit - 1) / kUnit; }
+__device__ __forceinline__ int units(const AttnArgs& p, int2 r) {
+  const int n = kUnit / p.together;
+  return r.y > r.x ? (r.y - (r.x & ~15) + n - 1) / n : 0;
+}
 
 // One output element pair of a finished row.
 __device__ __forceinline__ void store_out(const AttnArgs& p, int b, int h, int d, float x, float y) {
@@ -169,7 +196,7 @@ __device__ __forceinline__ void store_out(const AttnArgs& p, int b, int h, int d
 }
 
 template <int DT, int NT, bool kFp4>
-__global__ void __launch_bounds__(kThreads) paged_attention_kernel(const AttnArgs p) {
+__global__ void __launch_bounds__(kThreads, Cfg<DT, NT, kFp4>::kCtas) paged_attention_kernel(const AttnArgs p) {
   using C = Cfg<DT, NT, kFp4>;
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ int sh_b;
@@ -177,12 +204,13 @@ __global__ void __launch_bounds__(kThreads) paged_attention_kernel(const AttnArg
   griddep_launch_dependents();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
   const int D = p.c.head_dim;
-  const int rows = p.c.heads * p.chunks;  // rows of work of a sequence
+  const int rows = p.c.heads / p.together * p.chunks;  // rows of work of a sequence
+  const int mate = warp % p.together, phase = warp / p.together, phases = kWarps / p.together;
 
   // This CTA's share [pos, end) of all units, and the sequence it starts in.
   const int strip = (p.B + kThreads - 1) / kThreads;
   int64_t mine = 0;
-  for (int b = tid * strip; b < min(p.B, (tid + 1) * strip); ++b) mine += units(seen(p, b));
+  for (int b = tid * strip; b < min(p.B, (tid + 1) * strip); ++b) mine += units(p, seen(p, b));
   int64_t before = mine;
 #pragma unroll
   for (int d = 1; d < 32; d <<= 1) {
@@ -203,12 +231,14 @@ __global__ void __launch_bounds__(kThreads) paged_attention_kernel(const AttnArg
   for (int b = blockIdx.x; b < p.B; b += gridDim.x) {  // sequences that see nothing
     const int2 r = seen(p, b);
     if (r.y > r.x) continue;
+    if (p.by_row)
+      for (int i = tid; i < rows; i += kThreads) p.split[(int64_t)b * rows + i] = make_int4(-1, 0, 0, 0);
     for (int i = tid; i < p.q_heads * D / 2; i += kThreads)
       reinterpret_cast<uint32_t*>(p.out)[(int64_t)b * p.q_heads * D / 2 + i] = 0u;
     if (p.lse)
       for (int h = tid; h < p.q_heads; h += kThreads) p.lse[(int64_t)b * p.q_heads + h] = -INFINITY;
   }
-  if (tid == 0) p.split[blockIdx.x] = make_int4(-1, 0, 0, 0);
+  if (tid == 0 && !p.by_row) p.split[blockIdx.x] = make_int4(-1, 0, 0, 0);
   if ((int64_t)blockIdx.x >= grid) return;
   int64_t pos = all * blockIdx.x / grid;
   const int64_t end = all * (blockIdx.x + 1) / grid;
@@ -216,7 +246,7 @@ __global__ void __launch_bounds__(kThreads) paged_attention_kernel(const AttnArg
     int b = tid * strip;
     int64_t at = before;
     for (const int to = min(p.B, b + strip) - 1; b < to; ++b) {
-      const int u = units(seen(p, b));
+      const int u = units(p, seen(p, b));
       if (pos < (at + u) * rows) break;
       at += u;
     }
@@ -232,7 +262,7 @@ __global__ void __launch_bounds__(kThreads) paged_attention_kernel(const AttnArg
 
   while (pos < end && b < p.B) {
     const int2 range = seen(p, b);
-    const int u = units(range);
+    const int u = units(p, range);
     if (u == 0 || pos >= base + (int64_t)u * rows) {  // the next sequence (this one may have no unit)
       base += (int64_t)u * rows;
       ++b;
@@ -241,9 +271,11 @@ __global__ void __launch_bounds__(kThreads) paged_attention_kernel(const AttnArg
     const int row = (int)((pos - base) / u);
     const int k0 = (int)((pos - base) - (int64_t)row * u);
     const int cnt = (int)min((int64_t)(u - k0), end - pos);
-    const int head = row / p.chunks, h0 = head * p.group + (row - head * p.chunks) * C::kHeads;
-    const int nh = min(C::kHeads, (head + 1) * p.group - h0);  // query heads of this row
-    const int tok0 = range.x + k0 * kUnit, tok1 = min(range.y, tok0 + cnt * kUnit);
+    const int chunk = row % p.chunks, head = row / p.chunks * p.together + mate;
+    const int h0 = head * p.group + chunk * C::kHeads;
+    const int nh = min(C::kHeads, p.group - chunk * C::kHeads);  // query heads of this row
+    const int n = kUnit / p.together;
+    const int tok0 = (range.x & ~15) + k0 * n, tok1 = min(range.y, tok0 + cnt * n);
 
     // ---- the queries: B fragments, thread (g, t) holding head g's dimensions of its K pieces
     uint32_t qf[NT][DT / 16][2];
@@ -287,68 +319,76 @@ __global__ void __launch_bounds__(kThreads) paged_attention_kernel(const AttnArg
       for (int j = 0; j < 2; ++j) fs[n][j] = f * (kFp4 ? __shfl_sync(kAll, back, (2 * t + j) * 4) : 1.0f);
     }
 
-    // ---- the ring: this warp's tiles are 16 tokens at tok0 + 16 (warp + kWarps i)
+    // ---- the ring: this warp's tiles are 16 tokens at tok0 + 16 (phase + phases i)
     const int tiles_all = (tok1 - tok0 + 15) / 16;
-    const int tiles = tiles_all > warp ? (tiles_all - warp + kWarps - 1) / kWarps : 0;
+    const int tiles = tiles_all > phase ? (tiles_all - phase + phases - 1) / phases : 0;
     const int32_t* table = p.table + (int64_t)b * p.table_stride;
     const uint8_t* kb = static_cast<const uint8_t*>(p.c.k) + (int64_t)head * p.c.head_stride * (kFp4 ? 1 : 2);
     const uint8_t* vb = static_cast<const uint8_t*>(p.c.v) + (int64_t)head * p.c.head_stride * (kFp4 ? 1 : 2);
     const uint8_t* sb = nullptr;
     if (kFp4) sb = (lane < 16 ? p.c.k_scales : p.c.v_scales) + (int64_t)head * p.c.scale_head_stride;
 
-    // Lane l looks after token l % 16 of a tile: its page, asked for a tile ahead.
-    auto tile_token = [&](int i) { return tok0 + 16 * (warp + kWarps * i) + (lane & 15); };
+    // Where tiles lie in one page each (page_size % 16 == 0), its number is asked for a tile ahead and a
+    // row is token_stride behind the one before; else every row's page is looked up.
+    const bool whole = (p.c.page_size & 15) == 0;
+    const int64_t esize = kFp4 ? 1 : 2, step = p.c.token_stride * esize;
     auto page_of = [&](int tok) { return p.page_shift >= 0 ? tok >> p.page_shift : tok / p.c.page_size; };
     auto ask = [&](int i) -> int {
-      const int tok = tile_token(i);
-      return i < tiles && tok < tok1 ? table[page_of(tok)] : -1;
+      const int tok = tok0 + 16 * (phase + phases * i);
+      return whole && i < tiles ? table[page_of(tok)] : -1;
     };
     int asked = ask(0);
+    // Asks for tile i; the result has a bit for each of its tokens that is there.
     auto issue = [&](int i) -> uint32_t {
-      const int page = asked;
-      asked = ask(i + 1);
-      const bool ok = page >= 0 && page < p.c.pages;
-      const int tok = tile_token(i);
-      const int off = tok - page_of(tok) * p.c.page_size;
-      int64_t at = ok ? (int64_t)page * p.c.page_stride + (int64_t)off * p.c.token_stride : 0;
-      if (!kFp4) at *= 2;
-      const uint32_t there = __ballot_sync(kAll, ok) & 0xFFFFu;
-      const uint32_t dst = ring + (i % C::kStages) * C::kStage;
-      const uint32_t kd = dst + lane * C::kKBytes, vd = dst + C::kKTile + lane * C::kVBytes;
-#pragma unroll
-      for (int r = 0; r < 2; ++r) {
-        const int64_t ra = __shfl_sync(kAll, at, g + 8 * r);
-        const bool take = (there >> (g + 8 * r)) & 1u;
-#pragma unroll
-        for (int k = 0; k < C::kKPieces; ++k) {
-          const int c = t + 4 * k;
-          cp_async<C::kKBytes>(kd + (r * C::kKPieces + k) * 32 * C::kKBytes, kb + ra + c * C::kKBytes,
-                               take && c * C::kKDims < D);
+      const int tok = tok0 + 16 * (phase + phases * i);
+      uint32_t there = (tok1 - tok >= 16 ? 0xFFFFu : (1u << (tok1 - tok)) - 1u);
+      if (tok < range.x) there &= 0xFFFFu << (range.x - tok);
+      int64_t at = 0, sat = 0;  // of the tile, or of lane l's token l % 16
+      if (whole) {
+        const int page = asked, off = tok - page_of(tok) * p.c.page_size;
+        asked = ask(i + 1);
+        if (page < 0 || page >= p.c.pages) there = 0;
+        if (there) {
+          at = ((int64_t)page * p.c.page_stride + (int64_t)off * p.c.token_stride) * esize;
+          sat = (int64_t)page * p.c.scale_page_stride + (int64_t)(off + (lane & 15)) * p.c.scale_token_stride;
+        }
+      } else {
+        const int tk = tok + (lane & 15);
+        int page = -1;
+        if ((there >> (lane & 15)) & 1u) page = table[page_of(tk)];
+        const bool ok = page >= 0 && page < p.c.pages;
+        there = __ballot_sync(kAll, ok) & 0xFFFFu;
+        if (ok) {
+          const int off = tk - page_of(tk) * p.c.page_size;
+          at = ((int64_t)page * p.c.page_stride + (int64_t)off * p.c.token_stride) * esize;
+          sat = (int64_t)page * p.c.scale_page_stride + (int64_t)off * p.c.scale_token_stride;
         }
       }
+      const uint32_t dst = ring + (i % C::kStages) * C::kStage;
+      const int r0 = lane / C::kPieces, piece = lane % C::kPieces;
+      const bool in_row = piece * (kFp4 ? 16 : 8) < D;
+      const int64_t lane_at = r0 * step + piece * C::kCopy;
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int tr = 2 * t + (r & 1) + 8 * (r >> 1);
-        const int64_t ra = __shfl_sync(kAll, at, tr);
-        const bool take = (there >> tr) & 1u;
-#pragma unroll
-        for (int k = 0; k < C::kVPieces; ++k) {
-          const int c = g + 8 * k;
-          cp_async<C::kVBytes>(vd + (r * C::kVPieces + k) * 32 * C::kVBytes, vb + ra + c * C::kVBytes,
-                               take && c * C::kVDims < D);
-        }
+      for (int j = 0; j < 16 / C::kRowsAtOnce; ++j) {
+        const int r = r0 + j * C::kRowsAtOnce;
+        const bool take = ((there >> r) & 1u) && in_row;
+        const int64_t from = whole ? at + lane_at + j * C::kRowsAtOnce * step
+                                   : __shfl_sync(kAll, at, r) + piece * C::kCopy;
+        cp_async<C::kCopy>(dst + C::k_place(r, piece), kb + from, take);
+        cp_async<C::kCopy>(dst + C::kKTile + C::v_place(r, piece), vb + from, take);
       }
       if (kFp4) {
-        const int64_t sa = ok ? (int64_t)page * p.c.scale_page_stride + (int64_t)off * p.c.scale_token_stride : 0;
+        const bool ok = (there >> (lane & 15)) & 1u;
+        const uint8_t* src = sb + sat;
         const uint32_t sd = dst + C::kKTile + C::kVTile + lane * 16;
         if (D == 128) {
-          cp_async<8>(sd, sb + sa, ok);
+          cp_async<8>(sd, src, ok);
         } else if (D == 256) {
-          cp_async<16>(sd, sb + sa, ok);
+          cp_async<16>(sd, src, ok);
         } else if (D % 64 == 0) {
-          for (int k = 0; k < D / 16; k += 4) cp_async<4>(sd + k, sb + sa + k, ok);
+          for (int k = 0; k < D / 16; k += 4) cp_async<4>(sd + k, src + k, ok);
         } else {  // rows of an odd number of scale bytes
-          for (int k = 0; k < D / 16; ++k) sts8(sd + k, ok ? sb[sa + k] : 0u);
+          for (int k = 0; k < D / 16; ++k) sts8(sd + k, ok ? src[k] : 0u);
         }
       }
       return there;
@@ -381,7 +421,7 @@ __global__ void __launch_bounds__(kThreads) paged_attention_kernel(const AttnArg
       cp_wait<C::kStages - 1>();
       __syncwarp();
       const uint32_t src = ring + (i % C::kStages) * C::kStage;
-      const uint32_t ks = src + lane * C::kKBytes, vs = src + C::kKTile + lane * C::kVBytes;
+      const uint32_t vs = src + C::kKTile;
       const uint32_t ss = src + C::kKTile + C::kVTile;
 
       // ---- scores of 16 tokens x 8 NT heads
@@ -393,7 +433,7 @@ __global__ void __launch_bounds__(kThreads) paged_attention_kernel(const AttnArg
         uint32_t w[2][C::kKDims / 2];  // rows g and g + 8
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
-          const uint32_t a = ks + (r * C::kKPieces + k) * 32 * C::kKBytes;
+          const uint32_t a = src + C::k_place(g, t + 4 * k) + 8 * r * C::kRow;
           if constexpr (kFp4) {
             const uint2 v = lds64(a);
             // beyond D the codes are zeros and the scale bytes whatever lay there
@@ -417,28 +457,32 @@ __global__ void __launch_bounds__(kThreads) paged_attention_kernel(const AttnArg
       }
       const bool ok0 = (there[0] >> g) & 1u, ok1 = (there[0] >> (g + 8)) & 1u;
 
-      // ---- softmax: running maximum and weights, thread (g, t) for tokens g, g + 8 and heads 2t, 2t + 1
+      // ---- softmax: thread (g, t) has tokens g, g + 8 and heads 2t, 2t + 1.  The weights are 2^(s - m) for
+      // an m that follows the maximum from afar: it moves (and what was summed is scaled) when a score is
+      // kSlack above it, which takes a vote a tile instead of a maximum over the lanes.
       uint32_t ph[NT][2], pl[NT][2];
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
-        float mn[2], cor[2];
+        bool far = false;
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
           s[n][j] = ok0 ? s[n][j] * fs[n][j] : -INFINITY;
           s[n][2 + j] = ok1 ? s[n][2 + j] * fs[n][j] : -INFINITY;
-          float v = fmaxf(s[n][j], s[n][2 + j]);
-          v = fmaxf(v, __shfl_xor_sync(kAll, v, 4));
-          v = fmaxf(v, __shfl_xor_sync(kAll, v, 8));
-          v = fmaxf(v, __shfl_xor_sync(kAll, v, 16));
-          mn[j] = fmaxf(m[n][j], v);
+          far = far || fmaxf(s[n][j], s[n][2 + j]) > m[n][j] + kSlack;
         }
-        const bool moved = mn[0] > m[n][0] || mn[1] > m[n][1];
-        if (__any_sync(kAll, moved)) {
+        if (__any_sync(kAll, far)) {
+          float cor[2];
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
-            cor[j] = mn[j] == -INFINITY ? 1.0f : exp2f(m[n][j] - mn[j]);
+            float v = fmaxf(s[n][j], s[n][2 + j]);
+            v = fmaxf(v, __shfl_xor_sync(kAll, v, 4));
+            v = fmaxf(v, __shfl_xor_sync(kAll, v, 8));
+            v = fmaxf(v, __shfl_xor_sync(kAll, v, 16));
+            v = fmaxf(m[n][j], v);
+            cor[j] = exp2f(m[n][j] - v);  // 0 at the first score
+            if (v == -INFINITY) cor[j] = 1.0f;
+            m[n][j] = v;
             l[n][j] *= cor[j];
-            m[n][j] = mn[j];
           }
 #pragma unroll
           for (int k = 0; k < DT / 16; ++k) {
@@ -448,9 +492,9 @@ __global__ void __launch_bounds__(kThreads) paged_attention_kernel(const AttnArg
         float w[4];
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-          const float top = m[n][j] == -INFINITY ? 0.0f : m[n][j];
-          w[j] = exp2f(s[n][j] - top + (kFp4 ? (float)kFp4Exp : 0.0f));
-          w[2 + j] = exp2f(s[n][2 + j] - top + (kFp4 ? (float)kFp4Exp : 0.0f));
+          const float top = (m[n][j] == -INFINITY ? 0.0f : m[n][j]) - (kFp4 ? kFp4Exp : 0.0f);
+          w[j] = exp2f(s[n][j] - top);
+          w[2 + j] = exp2f(s[n][2 + j] - top);
           l[n][j] += w[j] + w[2 + j];
         }
         if (kFp4) {
@@ -471,7 +515,9 @@ __global__ void __launch_bounds__(kThreads) paged_attention_kernel(const AttnArg
         uint32_t w[4][C::kVDims / 2];  // tokens 2t, 2t + 1, 2t + 8, 2t + 9
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const uint32_t a = vs + (r * C::kVPieces + k) * 32 * C::kVBytes;
+          const int piece = C::kVBytes == C::kCopy ? g + 8 * k : (g + 8 * k) / 2;
+          const uint32_t a = vs + C::v_place(2 * t + (r & 1) + 8 * (r >> 1), piece) +
+                             (C::kVBytes == C::kCopy ? 0 : (g & 1) * C::kVBytes);
           if constexpr (kFp4) {
             const int tr = 2 * t + (r & 1) + 8 * (r >> 1);
             const int d = (g + 8 * k) * C::kVDims;
@@ -538,15 +584,15 @@ __global__ void __launch_bounds__(kThreads) paged_attention_kernel(const AttnArg
     }
     __syncthreads();
     const bool first = k0 == 0, last = k0 + cnt == u;
-    const int64_t slot = 2 * (int64_t)blockIdx.x + (first ? 1 : 0);
-    for (int i = tid; i < nh * (DT / 2); i += kThreads) {
-      const int h = i / (DT / 2), d = (i - h * (DT / 2)) * 2;
+    const int64_t slot = (2 * (int64_t)blockIdx.x + (first ? 1 : 0)) * p.together;
+    for (int i = tid; i < p.together * nh * (DT / 2); i += kThreads) {
+      const int hh = i / (DT / 2), d = (i - hh * (DT / 2)) * 2;
+      const int w0 = hh / nh, h = hh - w0 * nh;  // key head of the CTA, query head of it
+      const int ho = (row / p.chunks * p.together + w0) * p.group + chunk * C::kHeads + h;
       float M = -INFINITY, L = 0.0f;
-#pragma unroll
-      for (int w = 0; w < kWarps; ++w) M = fmaxf(M, ms[(w * C::kHeads + h) * 2]);
+      for (int w = w0; w < kWarps; w += p.together) M = fmaxf(M, ms[(w * C::kHeads + h) * 2]);
       float x = 0.0f, y = 0.0f;
-#pragma unroll
-      for (int w = 0; w < kWarps; ++w) {
+      for (int w = w0; w < kWarps; w += p.together) {
         const float f = M == -INFINITY ? 0.0f : exp2f(ms[(w * C::kHeads + h) * 2] - M);
         const float2 v = *reinterpret_cast<const float2*>(mo + (w * C::kHeads + h) * DT + d);
         L += f * ms[(w * C::kHeads + h) * 2 + 1];
@@ -555,71 +601,80 @@ __global__ void __launch_bounds__(kThreads) paged_attention_kernel(const AttnArg
       }
       if (first && last) {
         const float f = L > 0.0f ? (kFp4 ? 0.5f * vts : 1.0f) / L : 0.0f;
-        if (d < D) store_out(p, b, h0 + h, d, x * f, y * f);
+        if (d < D) store_out(p, b, ho, d, x * f, y * f);
         if (d == 0 && p.lse)
-          p.lse[(int64_t)b * p.q_heads + h0 + h] =
-              L > 0.0f ? (M + log2f(L) - (kFp4 ? (float)kFp4Exp : 0.0f)) * kLn2 : -INFINITY;
+          p.lse[(int64_t)b * p.q_heads + ho] =
+              L > 0.0f ? (M + log2f(L) - (kFp4 ? kFp4Exp : 0.0f)) * kLn2 : -INFINITY;
       } else {
-        *reinterpret_cast<float2*>(p.part + (slot * C::kHeads + h) * DT + d) = make_float2(x, y);
-        if (d == 0) p.stat[slot * C::kHeads + h] = make_float2(M, L);
+        *reinterpret_cast<float2*>(p.part + ((slot + w0) * C::kHeads + h) * DT + d) = make_float2(x, y);
+        if (d == 0) p.stat[(slot + w0) * C::kHeads + h] = make_float2(M, L);
       }
     }
-    if (tid == 0 && first && !last) {
+    if (tid == 0 && first && (p.by_row || !last)) {
       const int64_t x = base + (int64_t)(row + 1) * u;  // behind the row's last unit
-      p.split[blockIdx.x] = make_int4(b, row, (int)((x * grid - 1) / all), 0);
+      p.split[p.by_row ? (int64_t)b * rows + row : (int64_t)blockIdx.x] =
+          last ? make_int4(-1, 0, 0, 0) : make_int4(b, row, (int)blockIdx.x, (int)((x * grid - 1) / all));
     }
     __syncthreads();
     pos += cnt;
   }
 }
 
-// Joins the parts of the row that CTA blockIdx.x of the first kernel began and
-// did not finish, for one query head of it: 32 lanes over the dimensions, the
-// parts shared out to the four warps.
+// Joins the parts of the row in place blockIdx.x of `split`, key head
+// blockIdx.y of it, the query heads of blockIdx.z; `share` warps take one query
+// head, in turn over its parts.
 template <int DT, int NT, bool kFp4>
-__global__ void __launch_bounds__(kThreads) paged_attention_join_kernel(const AttnArgs p) {
-  constexpr int kHeads = 8 * NT, kV = DT / 32;
-  __shared__ float red[kWarps][DT + 2];
+__global__ void __launch_bounds__(kJoinThreads) paged_attention_join_kernel(const AttnArgs p) {
+  constexpr int kHeads = 8 * NT, kV = DT / 32, kW = kJoinThreads / 32;
+  __shared__ float red[kW][DT + 2];
   griddep_wait();
   const int4 s = p.split[blockIdx.x];
   if (s.x < 0) return;
-  const int h = blockIdx.y, head = s.y / p.chunks, h0 = head * p.group + (s.y - head * p.chunks) * kHeads;
-  if (h0 + h >= (head + 1) * p.group) return;
+  const int chunk = s.y % p.chunks, mate = blockIdx.y;
+  const int nh = min(kHeads, p.group - chunk * kHeads);
+  const int h0 = (s.y / p.chunks * p.together + mate) * p.group + chunk * kHeads;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int parts = s.z - (int)blockIdx.x + 1;
-  auto slot = [&](int i) { return (2 * ((int64_t)blockIdx.x + i) + (i == 0 ? 1 : 0)) * kHeads + h; };
-  float M = -INFINITY;
-  for (int i = lane; i < parts; i += 32) M = fmaxf(M, p.stat[slot(i)].x);
+  const int share = p.share, parts = s.w - s.z + 1;
+  {
+    const int h = blockIdx.z * (kW / share) + warp / share, ph = warp % share;
+    auto slot = [&](int i) { return ((2 * ((int64_t)s.z + i) + (i == 0 ? 1 : 0)) * p.together + mate) * kHeads + h; };
+    float M = -INFINITY, acc[kV], L = 0.0f;
 #pragma unroll
-  for (int d = 16; d; d >>= 1) M = fmaxf(M, __shfl_xor_sync(kAll, M, d));
-  float acc[kV], L = 0.0f;
+    for (int j = 0; j < kV; ++j) acc[j] = 0.0f;
+    if (h < nh) {
+      for (int i = lane; i < parts; i += 32) M = fmaxf(M, p.stat[slot(i)].x);
 #pragma unroll
-  for (int j = 0; j < kV; ++j) acc[j] = 0.0f;
-  if (M != -INFINITY) {
+      for (int d = 16; d; d >>= 1) M = fmaxf(M, __shfl_xor_sync(kAll, M, d));
+      if (M != -INFINITY) {
 #pragma unroll 4
-    for (int i = warp; i < parts; i += kWarps) {
-      const float2 st = p.stat[slot(i)];
-      const float f = exp2f(st.x - M);
-      L += f * st.y;
-      const float* o = p.part + slot(i) * DT + lane;
+        for (int i = ph; i < parts; i += share) {
+          const float2 st = p.stat[slot(i)];
+          const float f = exp2f(st.x - M);
+          L += f * st.y;
+          const float* o = p.part + slot(i) * DT + lane;
 #pragma unroll
-      for (int j = 0; j < kV; ++j) acc[j] += f * o[32 * j];
+          for (int j = 0; j < kV; ++j) acc[j] += f * o[32 * j];
+        }
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < kV; ++j) red[warp][lane + 32 * j] = acc[j];
+    if (lane == 0) red[warp][DT] = L;
+    __syncthreads();
+    if (h < nh && ph == 0) {
+      L = 0.0f;
+      for (int w = 0; w < share; ++w) L += red[warp + w][DT];
+      const float f = L > 0.0f ? (kFp4 ? 0.5f * *p.c.v_ts : 1.0f) / L : 0.0f;
+      for (int d = 2 * lane; d < p.c.head_dim; d += 64) {
+        float x = 0.0f, y = 0.0f;
+        for (int w = 0; w < share; ++w) x += red[warp + w][d], y += red[warp + w][d + 1];
+        store_out(p, s.x, h0 + h, d, x * f, y * f);
+      }
+      if (lane == 0 && p.lse)
+        p.lse[(int64_t)s.x * p.q_heads + h0 + h] =
+            L > 0.0f ? (M + log2f(L) - (kFp4 ? kFp4Exp : 0.0f)) * kLn2 : -INFINITY;
     }
   }
-#pragma unroll
-  for (int j = 0; j < kV; ++j) red[warp][lane + 32 * j] = acc[j];
-  if (lane == 0) red[warp][DT] = L;
-  __syncthreads();
-  L = red[0][DT] + red[1][DT] + red[2][DT] + red[3][DT];
-  const float f = L > 0.0f ? (kFp4 ? 0.5f * *p.c.v_ts : 1.0f) / L : 0.0f;
-  for (int d = 2 * threadIdx.x; d < p.c.head_dim; d += 2 * kThreads) {
-    const float x = red[0][d] + red[1][d] + red[2][d] + red[3][d];
-    const float y = red[0][d + 1] + red[1][d + 1] + red[2][d + 1] + red[3][d + 1];
-    store_out(p, s.x, h0 + h, d, x * f, y * f);
-  }
-  if (threadIdx.x == 0 && p.lse)
-    p.lse[(int64_t)s.x * p.q_heads + h0 + h] =
-        L > 0.0f ? (M + log2f(L) - (kFp4 ? (float)kFp4Exp : 0.0f)) * kLn2 : -INFINITY;
 }
 
 inline bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
@@ -627,10 +682,25 @@ inline int launch_status() { return cudaGetLastError() == cudaSuccess ? MIXFP4_O
 
 inline int padded_dim(int D) { return D <= 64 ? 64 : (D <= 128 ? 128 : 256); }
 inline int padded_heads(int64_t group) { return group <= 8 ? 8 : 16; }
-// CTAs of the first kernel: as many as the device holds at once, two to an SM
-// where two rings fit.
-inline int grid_of(const mixfp4_kv_cache* c) {
-  return num_sms() * (padded_dim(c->head_dim) == 256 && c->dtype == MIXFP4_CACHE_BF16 ? 1 : 2);
+// Key heads of a CTA.  Where the heads of a token lie together, neighbouring heads' rows are asked for at the same
+// time (64 sequences of up to 8192 tokens, 8 heads of 128: MixFP4 162 us against 185 us with one head to a CTA, whose
+// 8 scale bytes of a row cost a whole access; 32 bf16 heads of 128: 91 against 111 us).  Where a head's tokens lie
+// together that gains nothing, and one head to a CTA leaves fewer parts to join (2 sequences of 131072: 175 us
+// against 188).
+inline int together_of(const mixfp4_kv_cache* c) {
+  if (c->head_stride >= c->token_stride) return 1;
+  return c->heads % 4 == 0 ? 4 : (c->heads % 2 == 0 ? 2 : 1);
+}
+// CTAs of the first kernel.
+template <int DT>
+int ctas_of(bool fp4, bool wide) {
+  return fp4 ? (wide ? Cfg<DT, 2, true>::kCtas : Cfg<DT, 1, true>::kCtas)
+             : (wide ? Cfg<DT, 2, false>::kCtas : Cfg<DT, 1, false>::kCtas);
+}
+inline int grid_of(const mixfp4_kv_cache* c, int64_t q_heads) {
+  const bool fp4 = c->dtype == MIXFP4_CACHE_MIXFP4, wide = padded_heads(q_heads / c->heads) > 8;
+  const int d = padded_dim(c->head_dim);
+  return num_sms() * (d == 64 ? ctas_of<64>(fp4, wide) : (d == 128 ? ctas_of<128>(fp4, wide) : ctas_of<256>(fp4, wide)));
 }
 
 template <int DT, int NT, bool kFp4>
@@ -641,8 +711,9 @@ int launch(const AttnArgs& p, int grid, cudaStream_t s) {
   if (!set_dynamic_smem_once(reinterpret_cast<const void*>(kernel), C::kSmem, done)) return MIXFP4_ERR_CUDA;
   kernel<<<grid, kThreads, C::kSmem, s>>>(p);
   if (int st = launch_status()) return st;
-  const dim3 jg((unsigned)grid, (unsigned)(p.group < C::kHeads ? p.group : C::kHeads));
-  return launch_pdl(paged_attention_join_kernel<DT, NT, kFp4>, jg, dim3(kThreads), 0, s, p) == cudaSuccess
+  const int nh = p.group < C::kHeads ? p.group : C::kHeads, heads = kJoinThreads / 32 / p.share;
+  const dim3 jg((unsigned)p.places, (unsigned)p.together, (unsigned)((nh + heads - 1) / heads));
+  return launch_pdl(paged_attention_join_kernel<DT, NT, kFp4>, jg, dim3(kJoinThreads), 0, s, p) == cudaSuccess
              ? MIXFP4_OK
              : MIXFP4_ERR_CUDA;
 }
@@ -673,8 +744,8 @@ int mixfp4_paged_attention_workspace(const mixfp4_kv_cache* cache, int64_t B, in
   if (B < 0 || q_heads < 0 || q_heads % cache->heads != 0) return MIXFP4_ERR_SHAPE;
   *bytes = 0;
   if (B == 0 || q_heads == 0) return MIXFP4_OK;
-  const int64_t grid = grid_of(cache), heads = padded_heads(q_heads / cache->heads);
-  *bytes = grid * 16 + 2 * grid * heads * 8 + 2 * grid * heads * padded_dim(cache->head_dim) * 4;
+  const int64_t grid = grid_of(cache, q_heads), heads = padded_heads(q_heads / cache->heads) * together_of(cache);
+  *bytes = (grid * 16 + 255) / 256 * 256 + 2 * grid * heads * 8 + 2 * grid * heads * padded_dim(cache->head_dim) * 4;
   return MIXFP4_OK;
 }
 
@@ -694,7 +765,7 @@ int mixfp4_paged_attention(const void* q, int64_t q_stride, int64_t q_head_strid
   if (!aligned(q, 16) || q_stride % 8 || q_head_stride % 8 || !aligned(block_table, 4) || !aligned(lengths, 4) ||
       !aligned(out, 16) || !aligned(lse, 4) || !aligned(workspace, 256))
     return MIXFP4_ERR_ALIGN;
-  const int grid = grid_of(cache);
+  const int grid = grid_of(cache, q_heads);
   const int64_t heads = padded_heads(q_heads / cache->heads);
   AttnArgs p = {};
   p.q = static_cast<const uint16_t*>(q);
@@ -702,6 +773,7 @@ int mixfp4_paged_attention(const void* q, int64_t q_stride, int64_t q_head_strid
   p.B = (int)B, p.q_heads = (int)q_heads, p.group = (int)(q_heads / cache->heads);
   p.chunks = (int)((p.group + heads - 1) / heads);
   p.c = *cache;
+  p.together = together_of(cache);
   p.page_shift = -1;
   for (int i = 0; i < 31; ++i)
     if (cache->page_size == 1 << i) p.page_shift = i;
@@ -710,10 +782,19 @@ int mixfp4_paged_attention(const void* q, int64_t q_stride, int64_t q_head_strid
   p.lengths = lengths;
   p.scale = scale, p.window = window;
   p.out = static_cast<uint16_t*>(out), p.lse = lse;
+  // The joining kernel gets a CTA for each place, key head and few query heads: where they would be few,
+  // more warps to a query head.
+  const int64_t all_rows = B * (cache->heads / p.together) * p.chunks;
+  p.by_row = all_rows <= grid;
+  p.places = (int)(p.by_row ? all_rows : grid);
+  p.share = 1;
+  while (p.share < 8 && (p.share * 2 * p.group <= 8 || (int64_t)p.places * p.together * p.group * p.share < 4096))
+    p.share *= 2;
   uint8_t* w = static_cast<uint8_t*>(workspace);
   p.split = reinterpret_cast<int4*>(w);
-  p.stat = reinterpret_cast<float2*>(w + (int64_t)grid * 16);
-  p.part = reinterpret_cast<float*>(w + (int64_t)grid * 16 + 2 * (int64_t)grid * heads * 8);
+  w += ((int64_t)grid * 16 + 255) / 256 * 256;
+  p.stat = reinterpret_cast<float2*>(w);
+  p.part = reinterpret_cast<float*>(w + 2 * (int64_t)grid * p.together * heads * 8);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   return cache->dtype == MIXFP4_CACHE_MIXFP4 ? launch_dim<true>(p, grid, s) : launch_dim<false>(p, grid, s);
 }
