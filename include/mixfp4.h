@@ -580,9 +580,9 @@ int mixfp4_paged_attention_workspace(const mixfp4_kv_cache* cache, int64_t B, in
  * Products are exact, u and all sums fp32.  A segment whose id is outside
  * 0 .. adapters - 1 (-1) has no adapter: u = 0, out = base.
  *
- * x, dtype     device, bf16 (MIXFP4_DTYPE_BF16) [T][ldx]; 16-byte aligned, ldx % 8 == 0.
+ * x, dtype     device, bf16 (MIXFP4_DTYPE_BF16) [T][ldx]; 32-byte aligned, ldx % 16 == 0.
  * K, N         K % 16 == 0; N needs no padding; both at most 2^24.
- * a, b         device, bf16 [adapters][R][K] and [adapters][N][R], 16-byte aligned.
+ * a, b         device, bf16 [adapters][R][K] and [adapters][N][R], 32-byte aligned.
  *              R % 8 == 0, 8 .. 128 (smaller ranks: zeros).
  * scaling      device, float [adapters].    adapters  0 .. 65535.
  * starts       device, int32 [segments + 1], not decreasing, starts[0] = 0 and
@@ -590,8 +590,8 @@ int mixfp4_paged_attention_workspace(const mixfp4_kv_cache* cache, int64_t B, in
  *              segment are neither read nor written.
  * ids          device, int32 [segments].    segments  at most 2^20.
  * base         device, float [T][ld_base], or NULL for zeros; may be out.
- * out          device, float [T][ld_out] (16-byte alignment and strides % 4 == 0
- *              enable vector stores).                                    (output)
+ * out          device, float [T][ld_out] (32-byte alignment and strides % 8 == 0
+ *              of base and out enable vector access).                    (output)
  * u            device, float [T][R], 16-byte aligned: what the backward pass
  *              needs.                                                    (output)
  */
@@ -607,10 +607,11 @@ int mixfp4_lora(const void* x, int dtype, int64_t T, int64_t K, int64_t ldx, con
  * the sums over the tokens of all segments with adapter j (zeros where there are
  * none).  base is the input gradient of the projection itself, or NULL.
  *
- * dy           device, bf16 [T][ldy]; 16-byte aligned, ldy % 8 == 0; N % 16 == 0.
+ * dy           device, bf16 [T][ldy]; 32-byte aligned, ldy % 16 == 0; N % 16 == 0.
  * u            device, float [T][R], as mixfp4_lora wrote it.
  * dx           device, float [T][ld_dx]; may be base.                    (output)
- * da, db       device, float [adapters][R][K] and [adapters][N][R].      (output)
+ * da, db       device, float [adapters][R][K] and [adapters][N][R], 32-byte
+ *              aligned.                                                  (output)
  * v            device, float [T][R], 16-byte aligned: scratch memory.
  * Other arguments, alignment and errors: as mixfp4_lora.
  */

@@ -67,6 +67,16 @@ __device__ __forceinline__ void cluster_barrier() {
   asm volatile("barrier.cluster.arrive.aligned;\n barrier.cluster.wait.aligned;" ::: "memory");
 }
 
+// 32 bytes of global memory, or zeros.
+__device__ __forceinline__ void load32(uint32_t w[8], const void* p, bool ok) {
+  if (ok)
+    asm volatile("ld.global.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7])
+                 : "l"(p) : "memory");
+  else
+    w[0] = w[1] = w[2] = w[3] = w[4] = w[5] = w[6] = w[7] = 0u;
+}
+
 struct Segments {
   const int32_t* starts;  // [count + 1]
   const int32_t* ids;     // [count]
@@ -135,8 +145,8 @@ __device__ __forceinline__ Tile find_tile(const Segments& s, int index) {
 
 // ---- shrink: out[t][r] = factor_a sum_k in[t][k] W_a[r][k], k < kdim -------------------------------
 // Ranks are the rows of the products (RT tiles of 16), tokens their columns
-// (TT / 8 tiles of 8).  A step covers 32 k: thread (g, t) holds k 8t .. 8t + 7
-// of its rows.  Warps take steps in turn, the CTAs of a cluster shares of k;
+// (TT / 8 tiles of 8).  A step covers 64 k, a whole 128-byte line of a row:
+// thread (g, t) holds k 16t .. 16t + 15 of its rows.  Warps take steps in turn, the CTAs of a cluster shares of k;
 // both are summed in order through shared memory.
 struct ShrinkArgs {
   const uint16_t* in;  // [tokens][ld]
@@ -150,7 +160,7 @@ struct ShrinkArgs {
 };
 
 template <int RT, int TT, bool kTrans>
-__global__ void __launch_bounds__(kThreads) lora_shrink_kernel(const ShrinkArgs p) {
+__global__ void __launch_bounds__(kThreads, 2) lora_shrink_kernel(const ShrinkArgs p) {
   extern __shared__ float part[];  // [warps][16 RT][TT], then the CTA's sum in the first
   constexpr int kOut = 16 * RT * TT;
   griddep_wait();  // `in` may be what the kernel before it on the stream writes
@@ -169,7 +179,7 @@ __global__ void __launch_bounds__(kThreads) lora_shrink_kernel(const ShrinkArgs 
     return;
   }
   const uint16_t* w = p.w + (int64_t)tile.adapter * p.R * p.kdim;
-  const int64_t steps = (p.kdim + 31) / 32;
+  const int64_t steps = (p.kdim + 63) / 64;
   const int64_t s0 = steps * split / p.splits, s1 = steps * (split + 1) / p.splits;
 
   float acc[RT][TT / 8][4];
@@ -178,45 +188,41 @@ __global__ void __launch_bounds__(kThreads) lora_shrink_kernel(const ShrinkArgs 
 #pragma unroll
     for (int n = 0; n < TT / 8; ++n) acc[i][n][0] = acc[i][n][1] = acc[i][n][2] = acc[i][n][3] = 0.0f;
 
-  const uint4 zero = make_uint4(0, 0, 0, 0);
-#pragma unroll 2
   for (int64_t s = s0 + warp; s < s1; s += kWarps) {
-    const int64_t k = s * 32 + 8 * t;
+    const int64_t k = s * 64 + 16 * t;
     const bool in_k = k < p.kdim;
-    uint4 x[TT / 8];
+    uint32_t x[TT / 8][8];
 #pragma unroll
     for (int n = 0; n < TT / 8; ++n) {
       const int tok = tile.t0 + 8 * n + g;
-      x[n] = in_k && tok < tile.t1 ? *reinterpret_cast<const uint4*>(p.in + (int64_t)tok * p.ld + k) : zero;
+      load32(x[n], p.in + (int64_t)tok * p.ld + k, in_k && tok < tile.t1);
     }
     if (!kTrans) {
-      uint4 a[RT][2];
+      uint32_t a[RT][2][8];
 #pragma unroll
       for (int i = 0; i < RT; ++i)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           const int r = r0 + 16 * i + 8 * h + g;
-          a[i][h] = in_k && r < p.R ? *reinterpret_cast<const uint4*>(w + (int64_t)r * p.kdim + k) : zero;
+          load32(a[i][h], w + (int64_t)r * p.kdim + k, in_k && r < p.R);
         }
 #pragma unroll
-      for (int i = 0; i < RT; ++i)
+      for (int q = 0; q < 4; ++q)
 #pragma unroll
-        for (int n = 0; n < TT / 8; ++n) {
-          mma_bf16(acc[i][n], a[i][0].x, a[i][1].x, a[i][0].y, a[i][1].y, x[n].x, x[n].y);
-          mma_bf16(acc[i][n], a[i][0].z, a[i][1].z, a[i][0].w, a[i][1].w, x[n].z, x[n].w);
-        }
+        for (int i = 0; i < RT; ++i)
+#pragma unroll
+          for (int n = 0; n < TT / 8; ++n)
+            mma_bf16(acc[i][n], a[i][0][2 * q], a[i][1][2 * q], a[i][0][2 * q + 1], a[i][1][2 * q + 1], x[n][2 * q],
+                     x[n][2 * q + 1]);
     } else {
-      // Rows k .. k + 7 at the thread's ranks 2 RT g ..: words of rank pairs, permuted to k pairs.
-      uint32_t a[8][RT];
+      // Rows k .. k + 15 at the thread's ranks 2 RT g ..: words of rank pairs, permuted to k pairs.
+      uint32_t a[16][RT];
       const int r = r0 + 2 * RT * g;
+      const bool ok = in_k && r < p.R;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
+      for (int j = 0; j < 16; ++j) {
         const uint16_t* src = w + (k + j) * p.R + r;
-        const bool ok = in_k && r < p.R;
-        if constexpr (RT == 4) {
-          const uint4 v = ok ? *reinterpret_cast<const uint4*>(src) : zero;
-          a[j][0] = v.x, a[j][1] = v.y, a[j][2] = v.z, a[j][3] = v.w;
-        } else if constexpr (RT == 2) {
+        if constexpr (RT == 2) {
           const uint2 v = ok ? *reinterpret_cast<const uint2*>(src) : make_uint2(0, 0);
           a[j][0] = v.x, a[j][1] = v.y;
         } else {
@@ -224,16 +230,15 @@ __global__ void __launch_bounds__(kThreads) lora_shrink_kernel(const ShrinkArgs 
         }
       }
 #pragma unroll
-      for (int i = 0; i < RT; ++i)
+      for (int q = 0; q < 4; ++q)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const uint32_t a0 = prmt(a[4 * h][i], a[4 * h + 1][i], 0x5410u);
-          const uint32_t a1 = prmt(a[4 * h][i], a[4 * h + 1][i], 0x7632u);
-          const uint32_t a2 = prmt(a[4 * h + 2][i], a[4 * h + 3][i], 0x5410u);
-          const uint32_t a3 = prmt(a[4 * h + 2][i], a[4 * h + 3][i], 0x7632u);
+        for (int i = 0; i < RT; ++i) {
+          const uint32_t a0 = prmt(a[4 * q][i], a[4 * q + 1][i], 0x5410u);
+          const uint32_t a1 = prmt(a[4 * q][i], a[4 * q + 1][i], 0x7632u);
+          const uint32_t a2 = prmt(a[4 * q + 2][i], a[4 * q + 3][i], 0x5410u);
+          const uint32_t a3 = prmt(a[4 * q + 2][i], a[4 * q + 3][i], 0x7632u);
 #pragma unroll
-          for (int n = 0; n < TT / 8; ++n)
-            mma_bf16(acc[i][n], a0, a1, a2, a3, h ? x[n].z : x[n].x, h ? x[n].w : x[n].y);
+          for (int n = 0; n < TT / 8; ++n) mma_bf16(acc[i][n], a0, a1, a2, a3, x[n][2 * q], x[n][2 * q + 1]);
         }
     }
   }
@@ -270,8 +275,10 @@ __global__ void __launch_bounds__(kThreads) lora_shrink_kernel(const ShrinkArgs 
 // ---- expand: out[t][n] = base[t][n] + factor_a sum_r u[t][r] W_a[n][r] -----------------------------
 // Tokens are the rows of the products (16), features their columns: product j
 // of a warp's 64 features has column c at feature 8 c + j, so that thread
-// (g, t) ends with features 16 t .. 16 t + 15 of tokens g and g + 8.  A step
-// covers 16 ranks, thread t holding 4 t .. 4 t + 3.
+// (g, t) ends with features 16 t .. 16 t + 15 of tokens g and g + 8, 64 bytes
+// of a row.  A step covers 16 ranks, thread t holding 4 t .. 4 t + 3.  The
+// CTA's warps share the tokens: u is cut into its three parts once, in shared
+// memory as the fragments they read.
 struct ExpandArgs {
   const float* u;      // [tokens][R]
   const uint16_t* w;   // [adapters][N][R], or kTrans: [adapters][R][N]
@@ -286,50 +293,75 @@ struct ExpandArgs {
 };
 
 template <int TT, bool kTrans>
-__global__ void __launch_bounds__(kThreads) lora_expand_kernel(const ExpandArgs p) {
+__global__ void __launch_bounds__(kThreads, 2) lora_expand_kernel(const ExpandArgs p) {
+  extern __shared__ uint4 frag[];  // [m][step][part][lane]
   griddep_launch_dependents();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
   const Tile tile = find_tile<TT>(p.seg, (int)blockIdx.x);
+  const int steps = (p.R + 15) / 16;
   griddep_wait();
+  if (tile.t0 >= tile.t1) return;
+  if (tile.adapter >= 0)
+    for (int i = threadIdx.x; i < (TT / 16) * steps * 32; i += kThreads) {
+      const int ms = i / 32, m = ms / steps, l = i % 32;
+      const int r = (ms - m * steps) * 16 + 4 * (l & 3), ta = tile.t0 + 16 * m + (l >> 2);
+      const float4 z = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+      const float4 ua = r < p.R && ta < tile.t1 ? *reinterpret_cast<const float4*>(p.u + (int64_t)ta * p.R + r) : z;
+      const float4 ub =
+          r < p.R && ta + 8 < tile.t1 ? *reinterpret_cast<const float4*>(p.u + (int64_t)(ta + 8) * p.R + r) : z;
+      uint32_t a0[3], a1[3], a2[3], a3[3];
+      split3(ua.x, ua.y, a0);
+      split3(ub.x, ub.y, a1);
+      split3(ua.z, ua.w, a2);
+      split3(ub.z, ub.w, a3);
+#pragma unroll
+      for (int q = 0; q < 3; ++q) frag[(ms * 3 + q) * 32 + l] = make_uint4(a0[q], a1[q], a2[q], a3[q]);
+    }
+  __syncthreads();
   const int64_t n0 = ((int64_t)blockIdx.y * kWarps + warp) * 64;
-  if (tile.t0 >= tile.t1 || n0 >= p.N) return;
+  if (n0 >= p.N) return;
   const uint16_t* w = p.w + (int64_t)max(tile.adapter, 0) * p.R * p.N;
   const float f = tile.adapter < 0 ? 0.0f : (p.factor ? p.factor[tile.adapter] : 1.0f);
   const int64_t nt = n0 + 16 * t;  // this thread's results
-  for (int m = tile.t0; m < tile.t1; m += 16) {
+  const bool vec = p.vec && nt + 16 <= p.N;
+  for (int m = 0; tile.t0 + 16 * m < tile.t1; ++m) {
+    const int ta = tile.t0 + 16 * m + g;
+    float v[2][16];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const float* b = p.base + (int64_t)(ta + 8 * h) * p.ld_base + nt;
+      const bool there = p.base && ta + 8 * h < tile.t1;
+      if (vec) {
+        load32(reinterpret_cast<uint32_t*>(v[h]), b, there);
+        load32(reinterpret_cast<uint32_t*>(v[h] + 8), b + 8, there);
+      } else {
+#pragma unroll
+        for (int q = 0; q < 16; ++q) v[h][q] = there && nt + q < p.N ? b[q] : 0.0f;
+      }
+    }
     float acc[8][4];
 #pragma unroll
     for (int j = 0; j < 8; ++j) acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.0f;
-    const int ta = m + g, tb = m + g + 8;
-    const bool oka = ta < tile.t1, okb = tb < tile.t1;
     if (tile.adapter >= 0)
-      for (int r0 = 0; r0 < p.R; r0 += 16) {
-        const int r = r0 + 4 * t;
+      for (int st = 0; st < steps; ++st) {
+        const int r = st * 16 + 4 * t;
         const bool in_r = r < p.R;
-        const float4 z = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        const float4 ua = in_r && oka ? *reinterpret_cast<const float4*>(p.u + (int64_t)ta * p.R + r) : z;
-        const float4 ub = in_r && okb ? *reinterpret_cast<const float4*>(p.u + (int64_t)tb * p.R + r) : z;
-        uint32_t a0[3], a1[3], a2[3], a3[3];
-        split3(ua.x, ua.y, a0);
-        split3(ub.x, ub.y, a1);
-        split3(ua.z, ua.w, a2);
-        split3(ub.z, ub.w, a3);
         uint32_t b[8][2];
         if (!kTrans) {
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
             const int64_t n = n0 + 8 * g + j;
-            const uint2 v = in_r && n < p.N ? *reinterpret_cast<const uint2*>(w + n * p.R + r) : make_uint2(0, 0);
-            b[j][0] = v.x, b[j][1] = v.y;
+            const uint2 q = in_r && n < p.N ? *reinterpret_cast<const uint2*>(w + n * p.R + r) : make_uint2(0, 0);
+            b[j][0] = q.x, b[j][1] = q.y;
           }
         } else {
           uint32_t q[4][4];
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const int64_t n = n0 + 8 * g;
-            const uint4 v = in_r && n < p.N ? *reinterpret_cast<const uint4*>(w + (int64_t)(r + i) * p.N + n)
+            const uint4 x = in_r && n < p.N ? *reinterpret_cast<const uint4*>(w + (int64_t)(r + i) * p.N + n)
                                             : make_uint4(0, 0, 0, 0);
-            q[i][0] = v.x, q[i][1] = v.y, q[i][2] = v.z, q[i][3] = v.w;
+            q[i][0] = x.x, q[i][1] = x.y, q[i][2] = x.z, q[i][3] = x.w;
           }
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
@@ -338,30 +370,26 @@ __global__ void __launch_bounds__(kThreads) lora_expand_kernel(const ExpandArgs 
           }
         }
 #pragma unroll
-        for (int i = 2; i >= 0; --i)  // the small parts first
+        for (int i = 2; i >= 0; --i) {  // the small parts first
+          const uint4 a = frag[((m * steps + st) * 3 + i) * 32 + lane];
 #pragma unroll
-          for (int j = 0; j < 8; ++j) mma_bf16(acc[j], a0[i], a1[i], a2[i], a3[i], b[j][0], b[j][1]);
+          for (int j = 0; j < 8; ++j) mma_bf16(acc[j], a.x, a.y, a.z, a.w, b[j][0], b[j][1]);
+        }
       }
     // acc[j]: (token g, features 16 t + j and 16 t + 8 + j), then token g + 8
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      if (!(h ? okb : oka)) continue;
-      const int64_t tok = h ? tb : ta;
-      float* o = p.out + tok * p.ld_out + nt;
-      const float* s = p.base ? p.base + tok * p.ld_base + nt : nullptr;
-      if (p.vec && nt + 16 <= p.N) {
+      if (ta + 8 * h >= tile.t1) continue;
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const int c = 2 * h + (q >> 1), j = 4 * (q & 1);
-          float4 v = s ? *reinterpret_cast<const float4*>(s + 4 * q) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-          v.x = fmaf(f, acc[j][c], v.x), v.y = fmaf(f, acc[j + 1][c], v.y);
-          v.z = fmaf(f, acc[j + 2][c], v.z), v.w = fmaf(f, acc[j + 3][c], v.w);
-          *reinterpret_cast<float4*>(o + 4 * q) = v;
-        }
+      for (int q = 0; q < 16; ++q) v[h][q] = fmaf(f, acc[q & 7][2 * h + (q >> 3)], v[h][q]);
+      float* o = p.out + (int64_t)(ta + 8 * h) * p.ld_out + nt;
+      if (vec) {
+        stg256(o, reinterpret_cast<const uint32_t*>(v[h]));
+        stg256(o + 8, reinterpret_cast<const uint32_t*>(v[h] + 8));
       } else {
 #pragma unroll
         for (int q = 0; q < 16; ++q)
-          if (nt + q < p.N) o[q] = fmaf(f, acc[q & 7][2 * h + (q >> 3)], s ? s[q] : 0.0f);
+          if (nt + q < p.N) o[q] = v[h][q];
       }
     }
   }
@@ -370,8 +398,12 @@ __global__ void __launch_bounds__(kThreads) lora_expand_kernel(const ExpandArgs 
 // ---- grad: dW_a[r][n] = factor_a sum_t c[t][r] z[t][n] over adapter a's tokens ----------------------
 // Ranks are the rows of the products (RT tiles of 16, thread g holding ranks
 // 2 RT g ..), features their columns as in expand, tokens the contraction (16
-// a step).  The tokens of an adapter are one list through its segments; the
-// CTA's warps take its steps in turn and are summed in order.
+// a step).  The tokens of an adapter are one list through its segments, taken
+// in chunks of 64: the CTA cuts c's rows into their three parts once a chunk,
+// as fragments in shared memory, a chunk ahead of the products.  `wide` of its
+// warps take 64 features each; where the features alone would not fill the
+// device, the others take every second (fourth, eighth) step, and their sums
+// are added in order at the end.
 struct GradArgs {
   const float* c[2];       // v, u: [tokens][R]
   const uint16_t* z[2];    // x, dy: [tokens][ld]
@@ -379,24 +411,33 @@ struct GradArgs {
   const float* factor[2];  // NULL, scaling
   float* out[2];           // dA [adapters][R][K], dB [adapters][N][R]
   int64_t dim[2];          // K, N
-  int blocks[2];           // 64-feature blocks of each
-  int R;
+  int blocks[2];           // blocks of 64 wide features of each
+  int R, wide;
   Segments seg;
 };
 
+constexpr int kChunk = 64, kChunkSteps = kChunk / 16;
+
 template <int RT>
-__global__ void __launch_bounds__(kThreads) lora_grad_kernel(const GradArgs p) {
-  extern __shared__ float part[];  // [warps][64 features][16 RT]
-  constexpr int kOut = 16 * RT * 64;
-  __shared__ int ends[kThreads + 1], first[kThreads], count[kWarps + 1];
+constexpr int grad_smem() {  // two chunks' fragments, or half the warps' sums
+  return 2 * kChunkSteps * RT * 3 * 512 > 4 * RT * 32 * 32 * 4 ? 2 * kChunkSteps * RT * 3 * 512 : 4 * RT * 32 * 32 * 4;
+}
+
+template <int RT>
+__global__ void __launch_bounds__(kThreads, RT == 4 ? 1 : 2) lora_grad_kernel(const GradArgs p) {
+  extern __shared__ uint4 frag[];  // [2][step][tile][part][lane], then the sums
+  constexpr int kItems = kChunkSteps * RT * 32 / kThreads > 0 ? kChunkSteps * RT * 32 / kThreads : 1;
+  __shared__ int ends[kThreads], first[kThreads], count[kWarps], found[kWarps], toks[3][kChunk];
   griddep_wait();
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
   const int which = (int)blockIdx.x >= p.blocks[0];
-  const int64_t n0 = (int64_t)((int)blockIdx.x - (which ? p.blocks[0] : 0)) * 64;
+  const int wf = warp % p.wide, wt = warp / p.wide, turns = kWarps / p.wide;
+  const int64_t n0 = ((int64_t)((int)blockIdx.x - (which ? p.blocks[0] : 0)) * p.wide + wf) * 64;
   const int adapter = blockIdx.y, r0 = blockIdx.z * 16 * RT;
   const float* c = p.c[which];
-  const uint16_t* z = p.z[which];
   const int64_t ld = p.ld[which], N = p.dim[which];
+  const bool in_n = n0 + 8 * g < N;
+  const uint16_t* z = p.z[which] + n0 + 8 * g;
 
   float acc[RT][8][4];
 #pragma unroll
@@ -406,7 +447,7 @@ __global__ void __launch_bounds__(kThreads) lora_grad_kernel(const GradArgs p) {
 
   for (int s0 = 0; s0 < p.seg.count; s0 += kThreads) {
     // This batch's segments of the adapter, in order: first tokens and running ends of their lengths.
-    const int i = s0 + (int)threadIdx.x;
+    const int i = s0 + tid;
     int2 r = make_int2(0, 0);
     if (i < p.seg.count && adapter_of(p.seg, i) == adapter) r = bounds(p.seg, i);
     const int len = r.y - r.x;
@@ -418,87 +459,166 @@ __global__ void __launch_bounds__(kThreads) lora_grad_kernel(const GradArgs p) {
       if (lane >= d) sum += v;
     }
     __syncthreads();  // the batch before has been used
-    if (lane == 31) count[warp] = sum, first[warp] = __popc(some);
+    if (lane == 31) count[warp] = sum, found[warp] = __popc(some);
     __syncthreads();
     int at = __popc(some & ((1u << lane) - 1u)), off = sum, lists = 0, total = 0;
     for (int q = 0; q < kWarps; ++q) {
-      if (q < warp) at += first[q], off += count[q];
-      lists += first[q], total += count[q];
+      if (q < warp) at += found[q], off += count[q];
+      lists += found[q], total += count[q];
     }
-    __syncthreads();
     if (len > 0) first[at] = r.x - (off - len), ends[at] = off;  // token = index + first
-    __syncthreads();
     if (total == 0) continue;
+    __syncthreads();
     int top = 1;
     while (top < lists) top <<= 1;
-
-    for (int step = warp; step * 16 < total; step += kWarps) {
-      // Lane l finds token l % 16 of the step: the first list whose end lies beyond it.
-      const int want = step * 16 + (lane & 15);
-      int lo = 0;
-      for (int h = top >> 1; h; h >>= 1)
-        if (lo + h <= lists - 1 && ends[lo + h - 1] <= want) lo += h;
-      const int tok = want < total ? want + first[lo] : -1;
-      uint32_t cw[RT][2][2][3];  // [tile][row half][token pair][part]
-      uint4 zw[4];
-      float cv[4][2 * RT];
+    // The tokens of a chunk (-1 behind the last): for each, the first list whose end lies beyond it.
+    auto list_tokens = [&](int chunk) {
+      if (tid < kChunk) {
+        const int want = chunk * kChunk + tid;
+        int lo = 0;
+        for (int h = top >> 1; h; h >>= 1)
+          if (lo + h <= lists - 1 && ends[lo + h - 1] <= want) lo += h;
+        toks[chunk % 3][tid] = want < total ? want + first[lo] : -1;
+      }
+    };
+    float2 cv[kItems][4];
+    auto load_c = [&](int chunk) {
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int64_t tk = __shfl_sync(kAll, tok, 2 * t + (q & 1) + 8 * (q >> 1));
-        zw[q] = tk >= 0 && n0 + 8 * g < N ? *reinterpret_cast<const uint4*>(z + tk * ld + n0 + 8 * g)
-                                          : make_uint4(0, 0, 0, 0);
-        const int rr = r0 + 2 * RT * g;
+      for (int it = 0; it < kItems; ++it) {
+        const int item = it * kThreads + tid, l = item % 32, h = item / 32 % RT, st = item / 32 / RT;
+        const int rr = r0 + 2 * RT * (l >> 2) + 2 * h;
 #pragma unroll
-        for (int h = 0; h < RT; ++h) {
-          const float2 v = tk >= 0 && rr < p.R ? *reinterpret_cast<const float2*>(c + tk * p.R + rr + 2 * h)
-                                               : make_float2(0.0f, 0.0f);
-          cv[q][2 * h] = v.x, cv[q][2 * h + 1] = v.y;
+        for (int q = 0; q < 4; ++q) {
+          const int tk = st < kChunkSteps ? toks[chunk % 3][st * 16 + 2 * (l & 3) + (q & 1) + 8 * (q >> 1)] : -1;
+          cv[it][q] = tk >= 0 && rr < p.R ? *reinterpret_cast<const float2*>(c + (int64_t)tk * p.R + rr)
+                                          : make_float2(0.0f, 0.0f);
         }
       }
+    };
+    auto store_c = [&](int chunk) {
 #pragma unroll
-      for (int h = 0; h < RT; ++h)
+      for (int it = 0; it < kItems; ++it) {
+        const int item = it * kThreads + tid, l = item % 32, h = item / 32 % RT, st = item / 32 / RT;
+        if (st >= kChunkSteps) continue;
+        uint32_t a[4][3];
+        split3(cv[it][0].x, cv[it][1].x, a[0]);
+        split3(cv[it][0].y, cv[it][1].y, a[1]);
+        split3(cv[it][2].x, cv[it][3].x, a[2]);
+        split3(cv[it][2].y, cv[it][3].y, a[3]);
 #pragma unroll
-        for (int e = 0; e < 2; ++e)
-#pragma unroll
-          for (int q = 0; q < 2; ++q) split3(cv[2 * q][2 * h + e], cv[2 * q + 1][2 * h + e], cw[h][e][q]);
-      const uint32_t zz[4][4] = {{zw[0].x, zw[0].y, zw[0].z, zw[0].w},
-                                 {zw[1].x, zw[1].y, zw[1].z, zw[1].w},
-                                 {zw[2].x, zw[2].y, zw[2].z, zw[2].w},
-                                 {zw[3].x, zw[3].y, zw[3].z, zw[3].w}};
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const uint32_t sel = j & 1 ? 0x7632u : 0x5410u;
-        const uint32_t b0 = prmt(zz[0][j / 2], zz[1][j / 2], sel), b1 = prmt(zz[2][j / 2], zz[3][j / 2], sel);
-#pragma unroll
-        for (int h = 0; h < RT; ++h)
-#pragma unroll
-          for (int q = 2; q >= 0; --q)
-            mma_bf16(acc[h][j], cw[h][0][0][q], cw[h][1][0][q], cw[h][0][1][q], cw[h][1][1][q], b0, b1);
+        for (int q = 0; q < 3; ++q)
+          frag[((((chunk & 1) * kChunkSteps + st) * RT + h) * 3 + q) * 32 + l] =
+              make_uint4(a[0][q], a[1][q], a[2][q], a[3][q]);
       }
+    };
+    uint4 zw[4];
+    auto load_z = [&](int chunk, int st) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int tk = toks[chunk % 3][st * 16 + 2 * t + (q & 1) + 8 * (q >> 1)];
+        zw[q] = tk >= 0 && in_n ? *reinterpret_cast<const uint4*>(z + tk * ld) : make_uint4(0, 0, 0, 0);
+      }
+    };
+
+    const int chunks = (total + kChunk - 1) / kChunk;
+    list_tokens(0);
+    list_tokens(1);
+    __syncthreads();
+    load_c(0);
+    if (wt < kChunkSteps) load_z(0, wt);
+    store_c(0);
+    __syncthreads();
+    for (int ch = 0; ch < chunks; ++ch) {
+      const bool more = ch + 1 < chunks;
+      list_tokens(ch + 2);
+      if (more) load_c(ch + 1);
+      for (int st = wt; st < kChunkSteps; st += turns) {
+        const uint32_t zz[4][4] = {{zw[0].x, zw[0].y, zw[0].z, zw[0].w},
+                                   {zw[1].x, zw[1].y, zw[1].z, zw[1].w},
+                                   {zw[2].x, zw[2].y, zw[2].z, zw[2].w},
+                                   {zw[3].x, zw[3].y, zw[3].z, zw[3].w}};
+        uint32_t b[8][2];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const uint32_t sel = j & 1 ? 0x7632u : 0x5410u;
+          b[j][0] = prmt(zz[0][j / 2], zz[1][j / 2], sel), b[j][1] = prmt(zz[2][j / 2], zz[3][j / 2], sel);
+        }
+        if (st + turns < kChunkSteps) load_z(ch, st + turns);
+        else if (more) load_z(ch + 1, wt);
+        // A step's sum is its own and is added by the fp32 units: the tensor cores round a long chain of sums
+        // towards zero (4096 tokens of four adapters: the gradients' error 1.9e-6 in one chain).
+#pragma unroll
+        for (int h = 0; h < RT; ++h) {
+          uint4 a[3];
+#pragma unroll
+          for (int q = 0; q < 3; ++q) a[q] = frag[((((ch & 1) * kChunkSteps + st) * RT + h) * 3 + q) * 32 + lane];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            float d[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int q = 2; q >= 0; --q) mma_bf16(d, a[q].x, a[q].y, a[q].z, a[q].w, b[j][0], b[j][1]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[h][j][e] += d[e];
+          }
+        }
+      }
+      if (more) store_c(ch + 1);
+      __syncthreads();
     }
   }
 
-  // acc[h][j]: ranks 2 RT g + 2 h (+ 1 for registers 2, 3), features 16 t + j (+ 8 for registers 1, 3)
+  // The warps that shared features: the upper half's sums are added to the lower's, and so on.
+  float4* sums = reinterpret_cast<float4*>(frag);
+  for (int half = turns / 2; half >= 1; half /= 2) {
+    __syncthreads();
+    if (wt >= half && wt < 2 * half) {
 #pragma unroll
-  for (int h = 0; h < RT; ++h)
+      for (int h = 0; h < RT; ++h)
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        part[(warp * 64 + 16 * t + j + 8 * (e & 1)) * (16 * RT) + 2 * RT * g + 2 * h + (e >> 1)] = acc[h][j][e];
-  __syncthreads();
-  const float f = p.factor[which] ? p.factor[which][adapter] : 1.0f;
-  for (int i = threadIdx.x; i < kOut; i += kThreads) {
-    // dA: features run fastest; dB: ranks do
-    const int n = which ? i / (16 * RT) : i % 64, r = which ? i % (16 * RT) : i / 64;
-    float v = 0.0f;
-#pragma unroll
-    for (int q = 0; q < kWarps; ++q) v += part[(q * 64 + n) * (16 * RT) + r];
-    if (n0 + n < N && r0 + r < p.R) {
-      const int64_t to = which ? ((int64_t)adapter * N + n0 + n) * p.R + r0 + r
-                               : ((int64_t)adapter * p.R + r0 + r) * N + n0 + n;
-      p.out[which][to] = f * v;
+        for (int j = 0; j < 8; ++j)
+          sums[(((wt - half) * p.wide + wf) * RT * 8 + h * 8 + j) * 32 + lane] =
+              make_float4(acc[h][j][0], acc[h][j][1], acc[h][j][2], acc[h][j][3]);
     }
+    __syncthreads();
+    if (wt < half) {
+#pragma unroll
+      for (int h = 0; h < RT; ++h)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float4 v = sums[((wt * p.wide + wf) * RT * 8 + h * 8 + j) * 32 + lane];
+          acc[h][j][0] += v.x, acc[h][j][1] += v.y, acc[h][j][2] += v.z, acc[h][j][3] += v.w;
+        }
+    }
+  }
+  // acc[h][j]: ranks 2 RT g + 2 h (+ 1 for registers 2, 3), features 16 t + j (+ 8 for registers 1, 3)
+  if (wt > 0 || n0 + 16 * t >= N) return;
+  const float f = p.factor[which] ? p.factor[which][adapter] : 1.0f;
+  const int rg = r0 + 2 * RT * g;
+  if (rg >= p.R) return;
+  if (!which) {  // rows of features
+#pragma unroll
+    for (int h = 0; h < RT; ++h)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        float* to = p.out[0] + ((int64_t)adapter * p.R + rg + 2 * h + e) * N + n0 + 16 * t;
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          uint32_t v[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) v[j] = __float_as_uint(f * acc[h][j][2 * e + q]);
+          stg256(to + 8 * q, v);
+        }
+      }
+  } else {  // rows of ranks
+#pragma unroll
+    for (int q = 0; q < 2; ++q)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        float* to = p.out[1] + ((int64_t)adapter * N + n0 + 16 * t + 8 * q + j) * p.R + rg;
+#pragma unroll
+        for (int h = 0; h < RT; ++h)
+          *reinterpret_cast<float2*>(to + 2 * h) = make_float2(f * acc[h][j][q], f * acc[h][j][2 + q]);
+      }
   }
 }
 
@@ -531,39 +651,48 @@ template <bool kTrans>
 int shrink(ShrinkArgs p, bool dependent, cudaStream_t s) {
   const bool few = p.seg.tokens <= 8 * (int64_t)p.seg.count;
   const int64_t tiles = p.seg.tokens / (few ? 8 : 32) + p.seg.count;
-  const int rt = p.R <= 16 ? 1 : (p.R <= 32 ? 2 : 4);
+  // Ranks of a CTA: 16, or 32 (x is read again for every 32 ranks, from L2; 64 in one CTA left registers for
+  // half the loads in flight).  CTAs: k is cut until they fill the device's two places to an SM.
+  const int rt = p.R <= 16 ? 1 : 2;
   const int64_t ctas = tiles * ((p.R + 16 * rt - 1) / (16 * rt));
   p.splits = 1;
-  while (p.splits < 8 && ctas * p.splits < 2 * num_sms() && p.kdim / (p.splits * 2) >= 32 * kWarps) p.splits *= 2;
-  if (few)
-    return rt == 1   ? launch_shrink<1, 8, kTrans>(p, dependent, s)
-           : rt == 2 ? launch_shrink<2, 8, kTrans>(p, dependent, s)
-                     : launch_shrink<4, 8, kTrans>(p, dependent, s);
-  return rt == 1   ? launch_shrink<1, 32, kTrans>(p, dependent, s)
-         : rt == 2 ? launch_shrink<2, 32, kTrans>(p, dependent, s)
-                   : launch_shrink<4, 32, kTrans>(p, dependent, s);
+  while (p.splits < 8 && ctas * p.splits <= num_sms() && p.kdim >= 128 * kWarps * p.splits) p.splits *= 2;
+  if (few) return rt == 1 ? launch_shrink<1, 8, kTrans>(p, dependent, s) : launch_shrink<2, 8, kTrans>(p, dependent, s);
+  return rt == 1 ? launch_shrink<1, 32, kTrans>(p, dependent, s) : launch_shrink<2, 32, kTrans>(p, dependent, s);
+}
+
+template <int TT, bool kTrans>
+int launch_expand(const ExpandArgs& p, cudaStream_t s) {
+  constexpr int kStep = TT / 16 * 3 * 512, kMost = 8 * kStep;  // fragments of 16 ranks, of 128
+  auto* kernel = lora_expand_kernel<TT, kTrans>;
+  static std::atomic<uint64_t> done{0};
+  if (!set_dynamic_smem_once(reinterpret_cast<const void*>(kernel), kMost, done)) return MIXFP4_ERR_CUDA;
+  const dim3 grid((unsigned)(p.seg.tokens / TT + p.seg.count), (unsigned)((p.N + 64 * kWarps - 1) / (64 * kWarps)));
+  return launch_pdl(kernel, grid, dim3(kThreads), (size_t)((p.R + 15) / 16 * kStep), s, p) == cudaSuccess
+             ? MIXFP4_OK
+             : MIXFP4_ERR_CUDA;
 }
 
 template <bool kTrans>
 int expand(const ExpandArgs& p, cudaStream_t s) {
-  const bool few = p.seg.tokens <= 16 * (int64_t)p.seg.count;
-  const int64_t tiles = p.seg.tokens / (few ? 16 : 64) + p.seg.count;
-  const dim3 grid((unsigned)tiles, (unsigned)((p.N + 64 * kWarps - 1) / (64 * kWarps)));
-  const cudaError_t e = few ? launch_pdl(lora_expand_kernel<16, kTrans>, grid, dim3(kThreads), 0, s, p)
-                            : launch_pdl(lora_expand_kernel<64, kTrans>, grid, dim3(kThreads), 0, s, p);
-  return e == cudaSuccess ? MIXFP4_OK : MIXFP4_ERR_CUDA;
+  return p.seg.tokens <= 16 * (int64_t)p.seg.count ? launch_expand<16, kTrans>(p, s) : launch_expand<64, kTrans>(p, s);
 }
 
 template <int RT>
-int launch_grad(const GradArgs& p, cudaStream_t s) {
-  const int smem = kWarps * 16 * RT * 64 * 4;
+int launch_grad(GradArgs p, cudaStream_t s) {
   auto* kernel = lora_grad_kernel<RT>;
   static std::atomic<uint64_t> done{0};
-  if (smem > 48 * 1024 && !set_dynamic_smem_once(reinterpret_cast<const void*>(kernel), smem, done))
+  if (grad_smem<RT>() > 48 * 1024 &&
+      !set_dynamic_smem_once(reinterpret_cast<const void*>(kernel), grad_smem<RT>(), done))
     return MIXFP4_ERR_CUDA;
+  // As many of a CTA's warps side by side as leave a CTA for every SM.
+  const int64_t groups = (p.R + 16 * RT - 1) / (16 * RT) * (int64_t)p.seg.adapters;
+  for (p.wide = 8; p.wide > 2; p.wide /= 2)
+    if ((p.dim[0] + p.dim[1]) / (64 * p.wide) * groups >= num_sms()) break;
+  for (int i = 0; i < 2; ++i) p.blocks[i] = (int)((p.dim[i] + 64 * p.wide - 1) / (64 * p.wide));
   const dim3 grid((unsigned)(p.blocks[0] + p.blocks[1]), (unsigned)p.seg.adapters,
                   (unsigned)((p.R + 16 * RT - 1) / (16 * RT)));
-  return launch_pdl(kernel, grid, dim3(kThreads), smem, s, p) == cudaSuccess ? MIXFP4_OK : MIXFP4_ERR_CUDA;
+  return launch_pdl(kernel, grid, dim3(kThreads), grad_smem<RT>(), s, p) == cudaSuccess ? MIXFP4_OK : MIXFP4_ERR_CUDA;
 }
 
 // The arguments both entry points share.
@@ -575,12 +704,12 @@ int check_lora(int64_t T, int64_t K, int64_t N, int64_t R, int64_t adapters, con
     return MIXFP4_ERR_SHAPE;
   if (!starts || (segments > 0 && !ids) || (adapters > 0 && ((K > 0 && !a) || (N > 0 && !b) || !scaling)))
     return MIXFP4_ERR_NULL;
-  if (!aligned(a, 16) || !aligned(b, 16) || !aligned(scaling, 4) || !aligned(starts, 4) || !aligned(ids, 4))
+  if (!aligned(a, 32) || !aligned(b, 32) || !aligned(scaling, 4) || !aligned(starts, 4) || !aligned(ids, 4))
     return MIXFP4_ERR_ALIGN;
   return MIXFP4_OK;
 }
 
-inline bool vec_ok(const float* p, int64_t ld) { return aligned(p, 16) && ld % 4 == 0; }
+inline bool vec_ok(const float* p, int64_t ld) { return aligned(p, 32) && ld % 8 == 0; }
 
 }  // namespace
 }  // namespace mixfp4
@@ -597,7 +726,7 @@ int mixfp4_lora(const void* x, int dtype, int64_t T, int64_t K, int64_t ldx, con
   if (ldx < K || ld_out < N || (base && ld_base < N)) return MIXFP4_ERR_SHAPE;
   if (T == 0 || segments == 0) return MIXFP4_OK;
   if ((K > 0 && !x) || (N > 0 && !out) || !u) return MIXFP4_ERR_NULL;
-  if (!aligned(x, 16) || ldx % 8 || !aligned(u, 16) || !aligned(out, 4) || !aligned(base, 4)) return MIXFP4_ERR_ALIGN;
+  if (!aligned(x, 32) || ldx % 16 || !aligned(u, 16) || !aligned(out, 4) || !aligned(base, 4)) return MIXFP4_ERR_ALIGN;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   const Segments seg{starts, ids, (int)segments, (int)adapters, T};
   const ShrinkArgs sp{static_cast<const uint16_t*>(x), ldx, static_cast<const uint16_t*>(a), nullptr, u, K,
@@ -621,8 +750,8 @@ int mixfp4_lora_backward(const void* dy, int64_t ldy, const void* x, int64_t ldx
   const bool tokens = T > 0 && segments > 0;
   if (tokens && ((K > 0 && (!x || !dx)) || (N > 0 && !dy) || !u || !v)) return MIXFP4_ERR_NULL;
   if (adapters > 0 && ((K > 0 && !da) || (N > 0 && !db))) return MIXFP4_ERR_NULL;
-  if (!aligned(x, 16) || ldx % 8 || !aligned(dy, 16) || ldy % 8 || !aligned(u, 16) || !aligned(v, 16) ||
-      !aligned(dx, 4) || !aligned(base, 4) || !aligned(da, 4) || !aligned(db, 4))
+  if (!aligned(x, 32) || ldx % 16 || !aligned(dy, 32) || ldy % 16 || !aligned(u, 16) || !aligned(v, 16) ||
+      !aligned(dx, 4) || !aligned(base, 4) || !aligned(da, 32) || !aligned(db, 32))
     return MIXFP4_ERR_ALIGN;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   const Segments seg{starts, ids, (int)segments, (int)adapters, T};
@@ -643,12 +772,11 @@ int mixfp4_lora_backward(const void* dy, int64_t ldy, const void* x, int64_t ldx
   gp.factor[1] = scaling;
   gp.out[0] = da, gp.out[1] = db;
   gp.dim[0] = K, gp.dim[1] = N;
-  gp.blocks[0] = (int)((K + 63) / 64), gp.blocks[1] = (int)((N + 63) / 64);
   gp.R = (int)R;
   gp.seg = seg;
   if (!tokens) gp.seg.count = 0;
-  if (adapters == 0 || gp.blocks[0] + gp.blocks[1] == 0) return MIXFP4_OK;
-  return R <= 16 ? launch_grad<1>(gp, s) : launch_grad<2>(gp, s);
+  if (adapters == 0 || K + N == 0) return MIXFP4_OK;
+  return R <= 16 ? launch_grad<1>(gp, s) : (R <= 32 ? launch_grad<2>(gp, s) : launch_grad<4>(gp, s));
 }
 
 }  // extern "C"
