@@ -11,6 +11,7 @@
 #include <cstdint>
 
 #include "decode.cuh"
+#include "host_util.cuh"
 #include "kvcache.cuh"
 #include "quant_core.cuh"
 
@@ -18,6 +19,11 @@ namespace mixfp4 {
 namespace {
 
 constexpr int kThreads = 128;
+// CTAs of an SM by registers, and rounds of them that many tokens are spread over.  Swept at 8111 tokens of 32 + 16
+// heads of 128 in fp32, (3, 2) / (3, 4) / (4, 2) / (4, 4) / (4, 8): MixFP4 cache 80 / 85 / 89 / 85 / 109 us with the
+// gather behind it (at 4, registers spill), bf16 cache 57 / 59 / 57 / 54 / 63 us.
+template <int kMode>
+constexpr int kCtas = kMode < 0 ? 4 : 3;
 
 struct AppendArgs {
   const void* src[3];  // q, k, v
@@ -28,28 +34,31 @@ struct AppendArgs {
   const float* cos_sin;
   int64_t max_positions;
   int rot, interleaved, paired;
-  int units, groups;  // units of a head row; threads of a token per unit
+  int units, groups, at_once;  // units of a head row; a CTA's threads of a token per unit; its tokens
+  int stride;                  // a token's threads per unit, over all CTAs of its tokens (blockIdx.y)
   mixfp4_kv_cache c;
   const int64_t* slots;
   uint16_t* q_out;
 };
 
-// 16 consecutive elements as fp32.
+// 16 consecutive elements as they lie: 16 words of fp32, 8 of bf16.
 template <bool kF32>
-__device__ __forceinline__ void load16(const void* base, int64_t at, float x[16]) {
-  uint32_t w[8];
+__device__ __forceinline__ void load16(const void* base, int64_t at, uint32_t* w) {
   if (kF32) {
     const float* p = static_cast<const float*>(base) + at;
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      ldg256_stream(p + 8 * h, w);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) x[8 * h + j] = __uint_as_float(w[j]);
-    }
+    ldg256_stream(p, w);
+    ldg256_stream(p + 8, w + 8);
   } else {
     ldg256_stream(static_cast<const uint16_t*>(base) + at, w);
+  }
+}
+template <bool kF32>
+__device__ __forceinline__ void to_float(const uint32_t* w, float x[16]) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
+  for (int j = 0; j < (kF32 ? 16 : 8); ++j) {
+    if (kF32) {
+      x[j] = __uint_as_float(w[j]);
+    } else {
       x[2 * j] = __uint_as_float(w[j] << 16);
       x[2 * j + 1] = __uint_as_float(w[j] & 0xFFFF0000u);
     }
@@ -93,8 +102,46 @@ __device__ __forceinline__ void store16_mixfp4(uint8_t* codes, uint8_t* scale, c
 
 // kMode: a MixFP4 cache's MIXFP4_MODE_*, or -1 for a bf16 cache.
 template <bool kF32, int kMode>
-__global__ void __launch_bounds__(kThreads) kv_append_kernel(const AppendArgs p) {
+__global__ void __launch_bounds__(kThreads, kCtas<kMode>) kv_append_kernel(const AppendArgs p) {
   __shared__ float4 tab[kMode >= 0 ? 128 : 1];
+  const int row = (int)threadIdx.x / p.units, u = (int)threadIdx.x - row * p.units;
+  const int tl = row / p.groups, g = (int)blockIdx.y * p.groups + row - tl * p.groups;
+  const int64_t t = (int64_t)blockIdx.x * p.at_once + tl;
+  const bool mine = tl < p.at_once && t < p.tokens;
+
+  const int D = p.c.head_dim, rot = p.rot, half = rot / 2;
+  // The unit's blocks: with `paired`, u and u + half / 16 while they rotate, then one block each.
+  const int nrot = p.paired ? rot / 32 : 0;
+  const bool pair = u < nrot;
+  const int b0 = pair ? u : (p.paired ? rot / 16 : 0) + u - nrot;
+  const bool turns = b0 * 16 < rot;
+  const int heads = p.q_heads + 2 * p.c.heads;
+
+  // One head row's blocks, asked for a head ahead of their use.
+  constexpr int kWords = kF32 ? 16 : 8;
+  uint32_t next[2][kWords];
+  auto role_of = [&](int hh) { return hh < p.q_heads ? 0 : (hh < p.q_heads + p.c.heads ? 1 : 2); };
+  auto place = [&](int hh, const void*& base, int64_t& from) {
+    const int role = role_of(hh);
+    base = role == 0 ? p.src[0] : (role == 1 ? p.src[1] : p.src[2]);
+    from = role == 0   ? t * p.token_stride[0] + hh * p.head_stride[0]
+           : role == 1 ? t * p.token_stride[1] + (hh - p.q_heads) * p.head_stride[1]
+                       : t * p.token_stride[2] + (hh - p.q_heads - p.c.heads) * p.head_stride[2];
+  };
+  auto fetch = [&](int hh) {
+    const void* base;
+    int64_t from;
+    place(hh, base, from);
+    load16<kF32>(base, from + b0 * 16, next[0]);
+    if (pair) load16<kF32>(base, from + half + b0 * 16, next[1]);
+  };
+
+  int64_t slot = -1, pos = 0;
+  if (mine) {
+    slot = p.slots[t];
+    if (rot > 0) pos = p.positions[t];
+    if (g < heads) fetch(g);
+  }
   TensorConsts tk, tv;
   if (kMode >= 0) {
     fill_scale_table(tab);
@@ -102,66 +149,45 @@ __global__ void __launch_bounds__(kThreads) kv_append_kernel(const AppendArgs p)
     tv = tensor_consts(const_cast<float*>(p.c.v_ts), nullptr, 1);
     __syncthreads();
   }
-  const int64_t id = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  const int64_t row = id / p.units;
-  const int u = (int)(id - row * p.units);
-  const int64_t t = row / p.groups;
-  const int g = (int)(row - t * p.groups);
-  if (t >= p.tokens) return;
+  if (!mine) return;
 
-  const int D = p.c.head_dim, rot = p.rot, half = rot / 2;
-  // The unit's blocks: with `paired`, u and u + half / 16 while they rotate, then one block each.
-  const int nrot = p.paired ? rot / 32 : 0;
-  const bool pair = u < nrot;
-  const int b0 = pair ? u : rot / 16 * (p.paired ? 1 : 0) + u - nrot;
-  const bool turns = b0 * 16 < rot;
-
-  const int64_t slot = p.slots[t];
   bool keep = slot >= 0 && slot < p.c.pages * p.c.page_size;
-  bool placed = true;  // its position has a row of angles
+  const bool placed = pos >= 0 && (rot == 0 || pos < p.max_positions);  // the position has a row of angles
+  keep = keep && placed;
   float c[16], s[16];
-  if (rot > 0) {
-    const int64_t pos = p.positions[t];
-    placed = pos >= 0 && pos < p.max_positions;
-    keep = keep && placed;
-    if (turns && placed) {
-      const float* cs = p.cos_sin + pos * rot;
-      if (pair) {
-        load16<true>(cs, b0 * 16, c);
-        load16<true>(cs, half + b0 * 16, s);
-      } else {
+  if (rot > 0 && turns && placed) {
+    const float* cs = p.cos_sin + pos * rot;
+    if (pair) {
+      load16<true>(cs, b0 * 16, reinterpret_cast<uint32_t*>(c));
+      load16<true>(cs, half + b0 * 16, reinterpret_cast<uint32_t*>(s));
+    } else {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int d = b0 * 16 + e;
-          const int i = p.interleaved ? d / 2 : (d < half ? d : d - half);
-          const bool first = p.interleaved ? (e & 1) == 0 : d < half;
-          c[e] = d < rot ? cs[i] : 0.0f;
-          s[e] = d < rot ? (first ? -cs[half + i] : cs[half + i]) : 0.0f;
-        }
+      for (int e = 0; e < 16; ++e) {
+        const int d = b0 * 16 + e;
+        const int i = p.interleaved ? d / 2 : (d < half ? d : d - half);
+        const bool first = p.interleaved ? (e & 1) == 0 : d < half;
+        c[e] = d < rot ? cs[i] : 0.0f;
+        s[e] = d < rot ? (first ? -cs[half + i] : cs[half + i]) : 0.0f;
       }
     }
   }
-  int64_t page = 0, off = 0;
+  int64_t at = 0, sat = 0;
   if (keep) {
-    page = slot / p.c.page_size;
-    off = slot - page * p.c.page_size;
+    const int64_t page = slot / p.c.page_size, off = slot - page * p.c.page_size;
+    at = page * p.c.page_stride + off * p.c.token_stride;
+    sat = page * p.c.scale_page_stride + off * p.c.scale_token_stride;
   }
-  const int64_t at = page * p.c.page_stride + off * p.c.token_stride;
-  const int64_t sat = page * p.c.scale_page_stride + off * p.c.scale_token_stride;
 
-  const int heads = p.q_heads + 2 * p.c.heads;
-  for (int hh = g; hh < heads; hh += p.groups) {
-    const int role = hh < p.q_heads ? 0 : (hh < p.q_heads + p.c.heads ? 1 : 2);
-    const int h = role == 0 ? hh : (role == 1 ? hh - p.q_heads : hh - p.q_heads - p.c.heads);
-    if (role != 0 && !keep) continue;
-    const void* src = role == 0 ? p.src[0] : (role == 1 ? p.src[1] : p.src[2]);
-    const int64_t from = role == 0   ? t * p.token_stride[0] + h * p.head_stride[0]
-                         : role == 1 ? t * p.token_stride[1] + h * p.head_stride[1]
-                                     : t * p.token_stride[2] + h * p.head_stride[2];
+#pragma unroll 1
+  for (int hh = g; hh < heads; hh += p.stride) {
     float x[2][16];
-    load16<kF32>(src, from + b0 * 16, x[0]);
-    if (pair) load16<kF32>(src, from + half + b0 * 16, x[1]);
-    if (role != 2 && turns) {
+    to_float<kF32>(next[0], x[0]);
+    if (pair) to_float<kF32>(next[1], x[1]);
+    if (hh + p.stride < heads) fetch(hh + p.stride);
+    const int role = role_of(hh);
+    if (role != 0 && !keep) continue;
+    const int h = role == 0 ? hh : (role == 1 ? hh - p.q_heads : hh - p.q_heads - p.c.heads);
+    if (role != 2 && turns && placed) {
       if (pair) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
@@ -179,11 +205,14 @@ __global__ void __launch_bounds__(kThreads) kv_append_kernel(const AppendArgs p)
           }
         }
       } else {
+        const void* base;
+        int64_t from;
+        place(hh, base, from);
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
           const int d = b0 * 16 + e;
           if (d < rot) {
-            const float b = load1<kF32>(src, from + (d < half ? d + half : d - half));
+            const float b = load1<kF32>(base, from + (d < half ? d + half : d - half));
             x[0][e] = __fadd_rn(__fmul_rn(x[0][e], c[e]), __fmul_rn(b, s[e]));
           }
         }
@@ -211,18 +240,17 @@ __global__ void __launch_bounds__(kThreads) kv_append_kernel(const AppendArgs p)
   }
 }
 
-// One 16-element block per thread: slot's row t, tensor (k or v), head, block.
+// One 16-element block per thread: slot t's row, tensor (k or v), head, block.
 template <bool kFp4, bool kF32>
 __global__ void __launch_bounds__(kThreads) kv_gather_kernel(const mixfp4_kv_cache c, const int64_t* slots, int64_t T,
                                                              void* k_out, void* v_out) {
   const int blocks = c.head_dim / 16;
-  const int64_t id = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  const int64_t per_token = (int64_t)c.heads * blocks;
-  const int64_t row = id / per_token;
-  if (row >= 2 * T) return;
-  const bool is_v = row >= T;
-  const int64_t t = is_v ? row - T : row;
-  const int r = (int)(id - row * per_token);
+  const int units = c.heads * blocks, per_cta = kThreads / units > 0 ? kThreads / units : 1;  // rows of a CTA
+  const int tl = (int)threadIdx.x / units;
+  const int64_t t = (int64_t)blockIdx.x * per_cta + tl;
+  const bool is_v = blockIdx.y & 1;
+  const int r = (int)(blockIdx.y >> 1) * kThreads + (int)threadIdx.x - tl * units;  // head and block
+  if (tl >= per_cta || t >= T || r >= units) return;
   const int h = r / blocks, b = r - h * blocks;
   const int64_t slot = slots[t];
   float y[16];
@@ -250,7 +278,9 @@ __global__ void __launch_bounds__(kThreads) kv_gather_kernel(const mixfp4_kv_cac
         y[2 * j + 1] = __fmul_rn(0.5f * hi, ts);
       }
     } else {
-      load16<false>(src, at + b * 16, y);
+      uint32_t w[8];
+      load16<false>(src, at + b * 16, w);
+      to_float<false>(w, y);
     }
   }
   const int64_t to = (t * c.heads + h) * c.head_dim + b * 16;
@@ -273,7 +303,7 @@ inline int launch_status() { return cudaGetLastError() == cudaSuccess ? MIXFP4_O
 
 template <bool kF32>
 void launch_append(const AppendArgs& p, int mode, int64_t blocks, cudaStream_t s) {
-  const unsigned grid = (unsigned)blocks;
+  const dim3 grid((unsigned)blocks, (unsigned)(p.stride / p.groups));
   if (p.c.dtype == MIXFP4_CACHE_BF16) return kv_append_kernel<kF32, -1><<<grid, kThreads, 0, s>>>(p);
   switch (mode) {
     case MIXFP4_MODE_MIX: return kv_append_kernel<kF32, MIXFP4_MODE_MIX><<<grid, kThreads, 0, s>>>(p);
@@ -352,9 +382,18 @@ int mixfp4_kv_append(const void* q, int64_t q_token_stride, int64_t q_head_strid
   p.slots = slots;
   p.q_out = static_cast<uint16_t*>(q_out);
   p.units = p.paired ? p.rot / 32 + (cache->head_dim - p.rot) / 16 : cache->head_dim / 16;
-  const int64_t heads = q_heads + 2 * (int64_t)cache->heads;
-  p.groups = (int)heads;
-  const int64_t blocks = (T * p.groups * p.units + kThreads - 1) / kThreads;
+  // Threads of a token: for few tokens one for each head and unit, spread over CTAs; for many as few as leave the
+  // device some rounds of CTAs, so that a thread walks over several heads with the same angles.
+  const int heads = (int)q_heads + 2 * cache->heads, most = kThreads / p.units;
+  const bool bf16_cache = cache->dtype == MIXFP4_CACHE_BF16;
+  const int64_t wanted = (int64_t)num_sms() * kThreads * (bf16_cache ? kCtas<-1> * 4 : kCtas<0> * 2);
+  int64_t groups = (wanted + T * p.units - 1) / (T * p.units);
+  groups = groups < heads ? groups : heads;
+  const int slices = (int)((groups + most - 1) / most);
+  p.groups = (int)((groups + slices - 1) / slices);
+  p.stride = p.groups * slices;
+  p.at_once = most / p.groups;
+  const int64_t blocks = (T + p.at_once - 1) / p.at_once;
   if (blocks > INT32_MAX) return MIXFP4_ERR_SHAPE;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   if (dtype == MIXFP4_DTYPE_F32)
@@ -373,9 +412,11 @@ int mixfp4_kv_gather(const mixfp4_kv_cache* cache, const int64_t* slots, int64_t
   if (T == 0) return MIXFP4_OK;
   if (!slots || !k_out || !v_out) return MIXFP4_ERR_NULL;
   if (!aligned(slots, 8) || !aligned(k_out, 32) || !aligned(v_out, 32)) return MIXFP4_ERR_ALIGN;
-  const int64_t blocks = (2 * T * cache->heads * (cache->head_dim / 16) + kThreads - 1) / kThreads;
-  if (blocks > INT32_MAX) return MIXFP4_ERR_SHAPE;
-  const unsigned grid = (unsigned)blocks;
+  // CTAs of whole rows, or, where a row has more blocks than a CTA threads, of a part of one; keys and values.
+  const int64_t units = (int64_t)cache->heads * (cache->head_dim / 16), rows = kThreads / units > 0 ? kThreads / units : 1;
+  const int64_t blocks = (T + rows - 1) / rows, slices = (units + kThreads - 1) / kThreads;
+  if (blocks > INT32_MAX || slices > 32767) return MIXFP4_ERR_SHAPE;
+  const dim3 grid((unsigned)blocks, (unsigned)(2 * slices));
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   const bool fp4 = cache->dtype == MIXFP4_CACHE_MIXFP4, f32 = out_dtype == MIXFP4_DTYPE_F32;
   if (fp4 && f32)

@@ -292,13 +292,48 @@ struct ExpandArgs {
   Segments seg;
 };
 
-template <int TT, bool kTrans>
-__global__ void __launch_bounds__(kThreads, 2) lora_expand_kernel(const ExpandArgs p) {
+// The B fragments of 16 ranks for the warp's 64 features.
+template <bool kTrans>
+__device__ __forceinline__ void expand_w(uint32_t b[8][2], const uint16_t* w, int r, int R, int64_t n, int64_t N) {
+  const bool in_r = r < R;
+  if (!kTrans) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const uint2 q = in_r && n + j < N ? *reinterpret_cast<const uint2*>(w + (n + j) * R + r) : make_uint2(0, 0);
+      b[j][0] = q.x, b[j][1] = q.y;
+    }
+  } else {
+    uint32_t q[4][4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint4 x = in_r && n < N ? *reinterpret_cast<const uint4*>(w + (int64_t)(r + i) * N + n)
+                                    : make_uint4(0, 0, 0, 0);
+      q[i][0] = x.x, q[i][1] = x.y, q[i][2] = x.z, q[i][3] = x.w;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      b[2 * i][0] = prmt(q[0][i], q[1][i], 0x5410u), b[2 * i + 1][0] = prmt(q[0][i], q[1][i], 0x7632u);
+      b[2 * i][1] = prmt(q[2][i], q[3][i], 0x5410u), b[2 * i + 1][1] = prmt(q[2][i], q[3][i], 0x7632u);
+    }
+  }
+}
+
+// kHeld: steps (of 16 ranks) whose part of W a warp keeps in registers for all its tokens; further ranks are read
+// again for every 16 tokens.
+template <int TT, bool kTrans, int kHeld>
+__global__ void __launch_bounds__(kThreads, kHeld > 2 ? 1 : 2) lora_expand_kernel(const ExpandArgs p) {
   extern __shared__ uint4 frag[];  // [m][step][part][lane]
   griddep_launch_dependents();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
   const Tile tile = find_tile<TT>(p.seg, (int)blockIdx.x);
   const int steps = (p.R + 15) / 16;
+  const int64_t n0 = ((int64_t)blockIdx.y * kWarps + warp) * 64;
+  const uint16_t* w = p.w + (int64_t)max(tile.adapter, 0) * p.R * p.N;
+  const bool some = tile.t0 < tile.t1 && tile.adapter >= 0;
+  uint32_t held[kHeld][8][2];
+#pragma unroll
+  for (int st = 0; st < kHeld; ++st)
+    expand_w<kTrans>(held[st], w, some ? st * 16 + 4 * t : p.R, p.R, n0 + 8 * g, p.N);
   griddep_wait();
   if (tile.t0 >= tile.t1) return;
   if (tile.adapter >= 0)
@@ -318,9 +353,7 @@ __global__ void __launch_bounds__(kThreads, 2) lora_expand_kernel(const ExpandAr
       for (int q = 0; q < 3; ++q) frag[(ms * 3 + q) * 32 + l] = make_uint4(a0[q], a1[q], a2[q], a3[q]);
     }
   __syncthreads();
-  const int64_t n0 = ((int64_t)blockIdx.y * kWarps + warp) * 64;
   if (n0 >= p.N) return;
-  const uint16_t* w = p.w + (int64_t)max(tile.adapter, 0) * p.R * p.N;
   const float f = tile.adapter < 0 ? 0.0f : (p.factor ? p.factor[tile.adapter] : 1.0f);
   const int64_t nt = n0 + 16 * t;  // this thread's results
   const bool vec = p.vec && nt + 16 <= p.N;
@@ -342,40 +375,25 @@ __global__ void __launch_bounds__(kThreads, 2) lora_expand_kernel(const ExpandAr
     float acc[8][4];
 #pragma unroll
     for (int j = 0; j < 8; ++j) acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.0f;
-    if (tile.adapter >= 0)
-      for (int st = 0; st < steps; ++st) {
-        const int r = st * 16 + 4 * t;
-        const bool in_r = r < p.R;
-        uint32_t b[8][2];
-        if (!kTrans) {
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const int64_t n = n0 + 8 * g + j;
-            const uint2 q = in_r && n < p.N ? *reinterpret_cast<const uint2*>(w + n * p.R + r) : make_uint2(0, 0);
-            b[j][0] = q.x, b[j][1] = q.y;
-          }
-        } else {
-          uint32_t q[4][4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int64_t n = n0 + 8 * g;
-            const uint4 x = in_r && n < p.N ? *reinterpret_cast<const uint4*>(w + (int64_t)(r + i) * p.N + n)
-                                            : make_uint4(0, 0, 0, 0);
-            q[i][0] = x.x, q[i][1] = x.y, q[i][2] = x.z, q[i][3] = x.w;
-          }
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            b[2 * i][0] = prmt(q[0][i], q[1][i], 0x5410u), b[2 * i + 1][0] = prmt(q[0][i], q[1][i], 0x7632u);
-            b[2 * i][1] = prmt(q[2][i], q[3][i], 0x5410u), b[2 * i + 1][1] = prmt(q[2][i], q[3][i], 0x7632u);
-          }
-        }
+    if (tile.adapter >= 0) {
+      auto multiply = [&](int st, const uint32_t(&b)[8][2]) {
 #pragma unroll
         for (int i = 2; i >= 0; --i) {  // the small parts first
           const uint4 a = frag[((m * steps + st) * 3 + i) * 32 + lane];
 #pragma unroll
           for (int j = 0; j < 8; ++j) mma_bf16(acc[j], a.x, a.y, a.z, a.w, b[j][0], b[j][1]);
         }
-      }
+      };
+#pragma unroll
+      for (int st = 0; st < kHeld; ++st)
+        if (st < steps) multiply(st, held[st]);
+      if (kHeld == 4)
+        for (int st = kHeld; st < steps; ++st) {
+          uint32_t b[8][2];
+          expand_w<kTrans>(b, w, st * 16 + 4 * t, p.R, n0 + 8 * g, p.N);
+          multiply(st, b);
+        }
+    }
     // acc[j]: (token g, features 16 t + j and 16 t + 8 + j), then token g + 8
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -397,13 +415,11 @@ __global__ void __launch_bounds__(kThreads, 2) lora_expand_kernel(const ExpandAr
 
 // ---- grad: dW_a[r][n] = factor_a sum_t c[t][r] z[t][n] over adapter a's tokens ----------------------
 // Ranks are the rows of the products (RT tiles of 16, thread g holding ranks
-// 2 RT g ..), features their columns as in expand, tokens the contraction (16
-// a step).  The tokens of an adapter are one list through its segments, taken
-// in chunks of 64: the CTA cuts c's rows into their three parts once a chunk,
-// as fragments in shared memory, a chunk ahead of the products.  `wide` of its
-// warps take 64 features each; where the features alone would not fill the
-// device, the others take every second (fourth, eighth) step, and their sums
-// are added in order at the end.
+// 2 RT g ..), features their columns as in expand (64 to a CTA), tokens the
+// contraction (16 a step).  The tokens of an adapter are one list through its
+// segments; the CTA's warps take its steps in turn, each on its own (rows of c
+// and z asked for a step ahead, c cut into its three parts in registers), and
+// their sums are added in order at the end.
 struct GradArgs {
   const float* c[2];       // v, u: [tokens][R]
   const uint16_t* z[2];    // x, dy: [tokens][ld]
@@ -411,33 +427,25 @@ struct GradArgs {
   const float* factor[2];  // NULL, scaling
   float* out[2];           // dA [adapters][R][K], dB [adapters][N][R]
   int64_t dim[2];          // K, N
-  int blocks[2];           // blocks of 64 wide features of each
-  int R, wide;
+  int blocks[2];           // 64-feature blocks of each
+  int R;
   Segments seg;
 };
 
-constexpr int kChunk = 64, kChunkSteps = kChunk / 16;
-
 template <int RT>
-constexpr int grad_smem() {  // two chunks' fragments, or half the warps' sums
-  return 2 * kChunkSteps * RT * 3 * 512 > 4 * RT * 32 * 32 * 4 ? 2 * kChunkSteps * RT * 3 * 512 : 4 * RT * 32 * 32 * 4;
-}
-
-template <int RT>
-__global__ void __launch_bounds__(kThreads, RT == 4 ? 1 : 2) lora_grad_kernel(const GradArgs p) {
-  extern __shared__ uint4 frag[];  // [2][step][tile][part][lane], then the sums
-  constexpr int kItems = kChunkSteps * RT * 32 / kThreads > 0 ? kChunkSteps * RT * 32 / kThreads : 1;
-  __shared__ int ends[kThreads], first[kThreads], count[kWarps], found[kWarps], toks[3][kChunk];
+__global__ void __launch_bounds__(kThreads, RT == 1 ? 2 : 1) lora_grad_kernel(const GradArgs p) {
+  extern __shared__ float4 sums[];  // [half the warps][tile][product][lane]
+  __shared__ int ends[kThreads], first[kThreads], count[kWarps], found[kWarps];
   griddep_wait();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
+  const int threads = blockDim.x, warps = threads >> 5;
   const int which = (int)blockIdx.x >= p.blocks[0];
-  const int wf = warp % p.wide, wt = warp / p.wide, turns = kWarps / p.wide;
-  const int64_t n0 = ((int64_t)((int)blockIdx.x - (which ? p.blocks[0] : 0)) * p.wide + wf) * 64;
-  const int adapter = blockIdx.y, r0 = blockIdx.z * 16 * RT;
-  const float* c = p.c[which];
+  const int64_t n0 = (int64_t)((int)blockIdx.x - (which ? p.blocks[0] : 0)) * 64;
+  const int adapter = blockIdx.y, r0 = blockIdx.z * 16 * RT, rg = r0 + 2 * RT * g;
   const int64_t ld = p.ld[which], N = p.dim[which];
-  const bool in_n = n0 + 8 * g < N;
+  const bool in_n = n0 + 8 * g < N, in_r = rg < p.R;
   const uint16_t* z = p.z[which] + n0 + 8 * g;
+  const float* c = p.c[which] + rg;
 
   float acc[RT][8][4];
 #pragma unroll
@@ -445,7 +453,7 @@ __global__ void __launch_bounds__(kThreads, RT == 4 ? 1 : 2) lora_grad_kernel(co
 #pragma unroll
     for (int j = 0; j < 8; ++j) acc[i][j][0] = acc[i][j][1] = acc[i][j][2] = acc[i][j][3] = 0.0f;
 
-  for (int s0 = 0; s0 < p.seg.count; s0 += kThreads) {
+  for (int s0 = 0; s0 < p.seg.count; s0 += threads) {
     // This batch's segments of the adapter, in order: first tokens and running ends of their lengths.
     const int i = s0 + tid;
     int2 r = make_int2(0, 0);
@@ -462,139 +470,110 @@ __global__ void __launch_bounds__(kThreads, RT == 4 ? 1 : 2) lora_grad_kernel(co
     if (lane == 31) count[warp] = sum, found[warp] = __popc(some);
     __syncthreads();
     int at = __popc(some & ((1u << lane) - 1u)), off = sum, lists = 0, total = 0;
-    for (int q = 0; q < kWarps; ++q) {
+    for (int q = 0; q < warps; ++q) {
       if (q < warp) at += found[q], off += count[q];
       lists += found[q], total += count[q];
     }
     if (len > 0) first[at] = r.x - (off - len), ends[at] = off;  // token = index + first
-    if (total == 0) continue;
     __syncthreads();
     int top = 1;
     while (top < lists) top <<= 1;
-    // The tokens of a chunk (-1 behind the last): for each, the first list whose end lies beyond it.
-    auto list_tokens = [&](int chunk) {
-      if (tid < kChunk) {
-        const int want = chunk * kChunk + tid;
-        int lo = 0;
-        for (int h = top >> 1; h; h >>= 1)
-          if (lo + h <= lists - 1 && ends[lo + h - 1] <= want) lo += h;
-        toks[chunk % 3][tid] = want < total ? want + first[lo] : -1;
-      }
-    };
-    float2 cv[kItems][4];
-    auto load_c = [&](int chunk) {
+    const int steps = (total + 15) / 16;
+
+    // Tokens 2t, 2t + 1, 2t + 8, 2t + 9 of a step (-1 behind the last).  Lane l finds token l % 16: it lies in the
+    // first list whose end lies beyond it.
+    int tk[4];
+    auto find = [&](int step) {
+      const int want = step * 16 + (lane & 15);
+      int lo = 0;
+      for (int h = top >> 1; h; h >>= 1)
+        if (lo + h <= lists - 1 && ends[lo + h - 1] <= want) lo += h;
+      const int tok = want < total ? want + first[lo] : -1;
 #pragma unroll
-      for (int it = 0; it < kItems; ++it) {
-        const int item = it * kThreads + tid, l = item % 32, h = item / 32 % RT, st = item / 32 / RT;
-        const int rr = r0 + 2 * RT * (l >> 2) + 2 * h;
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const int tk = st < kChunkSteps ? toks[chunk % 3][st * 16 + 2 * (l & 3) + (q & 1) + 8 * (q >> 1)] : -1;
-          cv[it][q] = tk >= 0 && rr < p.R ? *reinterpret_cast<const float2*>(c + (int64_t)tk * p.R + rr)
-                                          : make_float2(0.0f, 0.0f);
-        }
-      }
-    };
-    auto store_c = [&](int chunk) {
-#pragma unroll
-      for (int it = 0; it < kItems; ++it) {
-        const int item = it * kThreads + tid, l = item % 32, h = item / 32 % RT, st = item / 32 / RT;
-        if (st >= kChunkSteps) continue;
-        uint32_t a[4][3];
-        split3(cv[it][0].x, cv[it][1].x, a[0]);
-        split3(cv[it][0].y, cv[it][1].y, a[1]);
-        split3(cv[it][2].x, cv[it][3].x, a[2]);
-        split3(cv[it][2].y, cv[it][3].y, a[3]);
-#pragma unroll
-        for (int q = 0; q < 3; ++q)
-          frag[((((chunk & 1) * kChunkSteps + st) * RT + h) * 3 + q) * 32 + l] =
-              make_uint4(a[0][q], a[1][q], a[2][q], a[3][q]);
-      }
+      for (int q = 0; q < 4; ++q) tk[q] = __shfl_sync(kAll, tok, 2 * t + (q & 1) + 8 * (q >> 1));
     };
     uint4 zw[4];
-    auto load_z = [&](int chunk, int st) {
+    float2 cv[RT][4];
+    auto load_z = [&]() {
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int tk = toks[chunk % 3][st * 16 + 2 * t + (q & 1) + 8 * (q >> 1)];
-        zw[q] = tk >= 0 && in_n ? *reinterpret_cast<const uint4*>(z + tk * ld) : make_uint4(0, 0, 0, 0);
-      }
+      for (int q = 0; q < 4; ++q)
+        zw[q] = tk[q] >= 0 && in_n ? *reinterpret_cast<const uint4*>(z + tk[q] * ld) : make_uint4(0, 0, 0, 0);
     };
-
-    const int chunks = (total + kChunk - 1) / kChunk;
-    list_tokens(0);
-    list_tokens(1);
-    __syncthreads();
-    load_c(0);
-    if (wt < kChunkSteps) load_z(0, wt);
-    store_c(0);
-    __syncthreads();
-    for (int ch = 0; ch < chunks; ++ch) {
-      const bool more = ch + 1 < chunks;
-      list_tokens(ch + 2);
-      if (more) load_c(ch + 1);
-      for (int st = wt; st < kChunkSteps; st += turns) {
-        const uint32_t zz[4][4] = {{zw[0].x, zw[0].y, zw[0].z, zw[0].w},
-                                   {zw[1].x, zw[1].y, zw[1].z, zw[1].w},
-                                   {zw[2].x, zw[2].y, zw[2].z, zw[2].w},
-                                   {zw[3].x, zw[3].y, zw[3].z, zw[3].w}};
-        uint32_t b[8][2];
+    auto load_c = [&](int h) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        cv[h][q] = tk[q] >= 0 && in_r ? *reinterpret_cast<const float2*>(c + (int64_t)tk[q] * p.R + 2 * h)
+                                      : make_float2(0.0f, 0.0f);
+    };
+    if (warp < steps) {
+      find(warp);
+      load_z();
+#pragma unroll
+      for (int h = 0; h < RT; ++h) load_c(h);
+    }
+    for (int step = warp; step < steps; step += warps) {
+      const bool more = step + warps < steps;
+      const uint32_t zz[4][4] = {{zw[0].x, zw[0].y, zw[0].z, zw[0].w},
+                                 {zw[1].x, zw[1].y, zw[1].z, zw[1].w},
+                                 {zw[2].x, zw[2].y, zw[2].z, zw[2].w},
+                                 {zw[3].x, zw[3].y, zw[3].z, zw[3].w}};
+      uint32_t b[8][2];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const uint32_t sel = j & 1 ? 0x7632u : 0x5410u;
+        b[j][0] = prmt(zz[0][j / 2], zz[1][j / 2], sel), b[j][1] = prmt(zz[2][j / 2], zz[3][j / 2], sel);
+      }
+      if (more) {
+        find(step + warps);
+        load_z();
+      }
+      // A step's sum is its own and is added by the fp32 units: the tensor cores round a long chain of sums
+      // towards zero (4096 tokens of four adapters: the gradients' error 1.9e-6 in one chain, 5.2e-7 so).
+#pragma unroll
+      for (int h = 0; h < RT; ++h) {
+        uint32_t a[4][3];
+        split3(cv[h][0].x, cv[h][1].x, a[0]);
+        split3(cv[h][0].y, cv[h][1].y, a[1]);
+        split3(cv[h][2].x, cv[h][3].x, a[2]);
+        split3(cv[h][2].y, cv[h][3].y, a[3]);
+        if (more) load_c(h);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          const uint32_t sel = j & 1 ? 0x7632u : 0x5410u;
-          b[j][0] = prmt(zz[0][j / 2], zz[1][j / 2], sel), b[j][1] = prmt(zz[2][j / 2], zz[3][j / 2], sel);
-        }
-        if (st + turns < kChunkSteps) load_z(ch, st + turns);
-        else if (more) load_z(ch + 1, wt);
-        // A step's sum is its own and is added by the fp32 units: the tensor cores round a long chain of sums
-        // towards zero (4096 tokens of four adapters: the gradients' error 1.9e-6 in one chain).
+          float d[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int h = 0; h < RT; ++h) {
-          uint4 a[3];
+          for (int q = 2; q >= 0; --q) mma_bf16(d, a[0][q], a[1][q], a[2][q], a[3][q], b[j][0], b[j][1]);
 #pragma unroll
-          for (int q = 0; q < 3; ++q) a[q] = frag[((((ch & 1) * kChunkSteps + st) * RT + h) * 3 + q) * 32 + lane];
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            float d[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-            for (int q = 2; q >= 0; --q) mma_bf16(d, a[q].x, a[q].y, a[q].z, a[q].w, b[j][0], b[j][1]);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) acc[h][j][e] += d[e];
-          }
+          for (int e = 0; e < 4; ++e) acc[h][j][e] += d[e];
         }
       }
-      if (more) store_c(ch + 1);
-      __syncthreads();
     }
   }
 
-  // The warps that shared features: the upper half's sums are added to the lower's, and so on.
-  float4* sums = reinterpret_cast<float4*>(frag);
-  for (int half = turns / 2; half >= 1; half /= 2) {
+  // The upper half of the warps' sums are added to the lower's, and so on.
+  for (int half = warps / 2; half >= 1; half /= 2) {
     __syncthreads();
-    if (wt >= half && wt < 2 * half) {
+    if (warp >= half && warp < 2 * half) {
 #pragma unroll
       for (int h = 0; h < RT; ++h)
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-          sums[(((wt - half) * p.wide + wf) * RT * 8 + h * 8 + j) * 32 + lane] =
+          sums[((warp - half) * RT * 8 + h * 8 + j) * 32 + lane] =
               make_float4(acc[h][j][0], acc[h][j][1], acc[h][j][2], acc[h][j][3]);
     }
     __syncthreads();
-    if (wt < half) {
+    if (warp < half) {
 #pragma unroll
       for (int h = 0; h < RT; ++h)
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          const float4 v = sums[((wt * p.wide + wf) * RT * 8 + h * 8 + j) * 32 + lane];
+          const float4 v = sums[(warp * RT * 8 + h * 8 + j) * 32 + lane];
           acc[h][j][0] += v.x, acc[h][j][1] += v.y, acc[h][j][2] += v.z, acc[h][j][3] += v.w;
         }
     }
   }
   // acc[h][j]: ranks 2 RT g + 2 h (+ 1 for registers 2, 3), features 16 t + j (+ 8 for registers 1, 3)
-  if (wt > 0 || n0 + 16 * t >= N) return;
+  if (warp > 0 || n0 + 16 * t >= N || !in_r) return;
   const float f = p.factor[which] ? p.factor[which][adapter] : 1.0f;
-  const int rg = r0 + 2 * RT * g;
-  if (rg >= p.R) return;
   if (!which) {  // rows of features
 #pragma unroll
     for (int h = 0; h < RT; ++h)
@@ -661,10 +640,10 @@ int shrink(ShrinkArgs p, bool dependent, cudaStream_t s) {
   return rt == 1 ? launch_shrink<1, 32, kTrans>(p, dependent, s) : launch_shrink<2, 32, kTrans>(p, dependent, s);
 }
 
-template <int TT, bool kTrans>
+template <int TT, bool kTrans, int kHeld>
 int launch_expand(const ExpandArgs& p, cudaStream_t s) {
   constexpr int kStep = TT / 16 * 3 * 512, kMost = 8 * kStep;  // fragments of 16 ranks, of 128
-  auto* kernel = lora_expand_kernel<TT, kTrans>;
+  auto* kernel = lora_expand_kernel<TT, kTrans, kHeld>;
   static std::atomic<uint64_t> done{0};
   if (!set_dynamic_smem_once(reinterpret_cast<const void*>(kernel), kMost, done)) return MIXFP4_ERR_CUDA;
   const dim3 grid((unsigned)(p.seg.tokens / TT + p.seg.count), (unsigned)((p.N + 64 * kWarps - 1) / (64 * kWarps)));
@@ -673,26 +652,32 @@ int launch_expand(const ExpandArgs& p, cudaStream_t s) {
              : MIXFP4_ERR_CUDA;
 }
 
+template <int TT, bool kTrans>
+int expand_held(const ExpandArgs& p, cudaStream_t s) {
+  if (p.R <= 16) return launch_expand<TT, kTrans, 1>(p, s);
+  return p.R <= 32 ? launch_expand<TT, kTrans, 2>(p, s) : launch_expand<TT, kTrans, 4>(p, s);
+}
+
 template <bool kTrans>
 int expand(const ExpandArgs& p, cudaStream_t s) {
-  return p.seg.tokens <= 16 * (int64_t)p.seg.count ? launch_expand<16, kTrans>(p, s) : launch_expand<64, kTrans>(p, s);
+  return p.seg.tokens <= 16 * (int64_t)p.seg.count ? expand_held<16, kTrans>(p, s) : expand_held<64, kTrans>(p, s);
 }
 
 template <int RT>
 int launch_grad(GradArgs p, cudaStream_t s) {
   auto* kernel = lora_grad_kernel<RT>;
   static std::atomic<uint64_t> done{0};
-  if (grad_smem<RT>() > 48 * 1024 &&
-      !set_dynamic_smem_once(reinterpret_cast<const void*>(kernel), grad_smem<RT>(), done))
+  constexpr int kMost = kWarps / 2 * RT * 8 * 512;
+  if (kMost > 32 * 1024 && !set_dynamic_smem_once(reinterpret_cast<const void*>(kernel), kMost, done))
     return MIXFP4_ERR_CUDA;
-  // As many of a CTA's warps side by side as leave a CTA for every SM.
-  const int64_t groups = (p.R + 16 * RT - 1) / (16 * RT) * (int64_t)p.seg.adapters;
-  for (p.wide = 8; p.wide > 2; p.wide /= 2)
-    if ((p.dim[0] + p.dim[1]) / (64 * p.wide) * groups >= num_sms()) break;
-  for (int i = 0; i < 2; ++i) p.blocks[i] = (int)((p.dim[i] + 64 * p.wide - 1) / (64 * p.wide));
+  for (int i = 0; i < 2; ++i) p.blocks[i] = (int)((p.dim[i] + 63) / 64);
   const dim3 grid((unsigned)(p.blocks[0] + p.blocks[1]), (unsigned)p.seg.adapters,
                   (unsigned)((p.R + 16 * RT - 1) / (16 * RT)));
-  return launch_pdl(kernel, grid, dim3(kThreads), grad_smem<RT>(), s, p) == cudaSuccess ? MIXFP4_OK : MIXFP4_ERR_CUDA;
+  // Four warps to a CTA, two CTAs side by side on an SM; eight where there would not be two CTAs to an SM.
+  const int warps = (int64_t)grid.x * grid.y * grid.z >= 2 * num_sms() ? 4 : 8;
+  return launch_pdl(kernel, grid, dim3(32 * warps), (size_t)(warps / 2 * RT * 8 * 512), s, p) == cudaSuccess
+             ? MIXFP4_OK
+             : MIXFP4_ERR_CUDA;
 }
 
 // The arguments both entry points share.

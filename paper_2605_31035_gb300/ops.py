@@ -751,7 +751,7 @@ class KVCache:
         self._c = c
         self._ref = ctypes.byref(c)
         self._workspace_bytes = {}
-        self.device = k.device
+        self.device, self._index = k.device, k.get_device()
 
     @property
     def pages(self) -> int:
@@ -789,24 +789,41 @@ def _check_cache(cache):
         raise ValueError("cache must be a KVCache")
 
 
-def _check_heads(t, dtype, heads, D, device, what: str):
-    """[tokens, heads, head_dim] on `device`, dense along head_dim."""
-    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.device == device and t.dtype is dtype and t.dim() == 3
-            and t.shape[2] == D and (heads is None or t.shape[1] == heads) and t.stride(2) == 1):
-        raise ValueError(f"{what} must be a {dtype} CUDA tensor [tokens, {heads if heads else 'heads'}, {D}] on "
-                         f"{device} with unit last stride")
+# A call on a few tokens runs for less time on the GPU than its arguments take
+# to look at here, so the checks ask each tensor for as little as will do:
+# get_device() is the device's index, -1 for a tensor elsewhere.
 
 
-def _check_index(t, dtype, n, device, what: str):
-    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.device == device and t.dtype is dtype and t.dim() == 1
-            and t.shape[0] == n and t.is_contiguous()):
-        raise ValueError(f"{what} must be a dense {dtype} CUDA tensor of {n} elements on {device}")
+def _dense(shape, dtype, device, stream, scratch: bool = False):
+    """_empty of up to three dimensions, by torch's quickest constructor on the current stream."""
+    if stream is not None:
+        return _empty(shape, dtype, device, stream, scratch)
+    n = len(shape)
+    strides = (1,) if n == 1 else (shape[1], 1) if n == 2 else (shape[1] * shape[2], shape[2], 1)
+    return torch.empty_strided(shape, strides, dtype=dtype, device=device)
 
 
-def _float_type(t):
-    if not (isinstance(t, torch.Tensor) and t.dtype in (torch.bfloat16, torch.float32)):
-        raise ValueError("k must be a bfloat16 or float32 CUDA tensor")
-    return DTYPE_BF16 if t.dtype is torch.bfloat16 else DTYPE_F32
+def _check_heads(t, dtype, heads, D, index, what: str):
+    """[tokens, heads, head_dim] on CUDA device `index`, dense along head_dim: its sizes and strides."""
+    try:
+        if t.dtype is dtype and t.get_device() == index:
+            shape, stride = t.shape, t.stride()
+            T, H, d = shape
+            if d == D and (heads is None or H == heads) and stride[2] == 1:
+                return shape, stride
+    except (AttributeError, ValueError):
+        pass
+    raise ValueError(f"{what} must be a {dtype} CUDA tensor [tokens, {heads if heads else 'heads'}, {D}] on "
+                     f"device {index} with unit last stride")
+
+
+def _check_index(t, dtype, n, index, what: str):
+    try:
+        if t.dtype is dtype and t.get_device() == index and t.shape == (n,) and (n <= 1 or t.stride(0) == 1):
+            return
+    except AttributeError:
+        pass
+    raise ValueError(f"{what} must be a dense {dtype} CUDA tensor of {n} elements on device {index}")
 
 
 def mixfp4_kv_append(k: torch.Tensor, v: torch.Tensor, cache: KVCache, slots: torch.Tensor,
@@ -822,37 +839,44 @@ def mixfp4_kv_append(k: torch.Tensor, v: torch.Tensor, cache: KVCache, slots: to
     rotated on the way: pairs (i, i + rot_dim / 2), or (2i, 2i + 1) if interleaved.
     Returns the (rotated) queries as bf16 [T, q_heads, head_dim], or None."""
     _check_cache(cache)
-    code, D, dev = _float_type(k), cache.head_dim, cache.device
-    _check_heads(k, k.dtype, cache.heads, D, dev, "k")
-    _check_heads(v, k.dtype, cache.heads, D, dev, "v")
-    T = k.shape[0]
-    _require(v.shape[0] == T, "k and v must have as many tokens")
-    _check_index(slots, torch.int64, T, dev, "slots")
-    rot = rows = 0
+    c, at = cache._c, cache._index
+    D, dtype = c.head_dim, getattr(k, "dtype", None)
+    if dtype is not torch.float32 and dtype is not torch.bfloat16:
+        raise ValueError("k must be a bfloat16 or float32 CUDA tensor")
+    shape, ks = _check_heads(k, dtype, c.heads, D, at, "k")
+    vshape, vs = _check_heads(v, dtype, c.heads, D, at, "v")
+    T = shape[0]
+    if vshape != shape:
+        raise ValueError("k and v must have as many tokens")
+    _check_index(slots, torch.int64, T, at, "slots")
+    rot = rows = angles = places = 0
     if cos_sin is not None:
-        _check_index(positions, torch.int64, T, dev, "positions")
-        if not (isinstance(cos_sin, torch.Tensor) and cos_sin.is_cuda and cos_sin.device == dev
-                and cos_sin.dtype is torch.float32 and cos_sin.dim() == 2 and cos_sin.is_contiguous()
-                and cos_sin.shape[1] % 2 == 0 and cos_sin.shape[1] <= D):
-            raise ValueError("cos_sin must be a dense float32 CUDA tensor [positions, rot_dim], rot_dim even and at "
-                             "most head_dim")
+        _check_index(positions, torch.int64, T, at, "positions")
+        if not (isinstance(cos_sin, torch.Tensor) and cos_sin.get_device() == at and cos_sin.dtype is torch.float32
+                and cos_sin.dim() == 2 and cos_sin.is_contiguous()):
+            raise ValueError("cos_sin must be a dense float32 CUDA tensor [positions, rot_dim]")
         rows, rot = cos_sin.shape
-    o, qs, heads = None, (0, 0, 0), 0
+        if rot % 2 or rot > D:
+            raise ValueError("rot_dim must be even and at most head_dim")
+        angles, places = cos_sin.data_ptr(), positions.data_ptr()
+    o, qs, heads, qp, op = None, (0, 0), 0, None, None
     if q is not None:
-        _check_heads(q, k.dtype, None, D, dev, "q")
-        _require(q.shape[0] == T, "q must have as many tokens as k")
-        heads, qs = q.shape[1], q.stride()
+        qshape, qs = _check_heads(q, dtype, None, D, at, "q")
+        heads = qshape[1]
+        if qshape[0] != T:
+            raise ValueError("q must have as many tokens as k")
         if out is None:
-            o = _empty((T, heads, D), torch.bfloat16, dev, stream)
+            o = _dense((T, heads, D), torch.bfloat16, cache.device, stream)
         else:
             o = out
-            _check_heads(o, torch.bfloat16, heads, D, dev, "out")
-            _require(o.shape[0] == T and o.is_contiguous(), "out must be dense, with as many tokens as q")
-    ks, vs = k.stride(), v.stride()
-    st = lib().mixfp4_kv_append(_ptr(q), qs[0], qs[1], heads, k.data_ptr(), ks[0], ks[1], v.data_ptr(), vs[0], vs[1],
-                                code, T, _ptr(positions), _ptr(cos_sin), rows, rot, int(interleaved), cache._ref,
-                                slots.data_ptr(), _ptr(o), int(mode), _stream(stream))
-    _check("mixfp4_kv_append", st)
+            oshape, _ = _check_heads(o, torch.bfloat16, heads, D, at, "out")
+            _require(oshape[0] == T and o.is_contiguous(), "out must be dense, with as many tokens as q")
+        qp, op = q.data_ptr(), o.data_ptr()
+    st = lib().mixfp4_kv_append(qp, qs[0], qs[1], heads, k.data_ptr(), ks[0], ks[1], v.data_ptr(), vs[0], vs[1],
+                                DTYPE_BF16 if dtype is torch.bfloat16 else DTYPE_F32, T, places, angles, rows, rot,
+                                1 if interleaved else 0, cache._ref, slots.data_ptr(), op, mode, _stream(stream))
+    if st:
+        _check("mixfp4_kv_append", st)
     return o
 
 
@@ -863,16 +887,15 @@ def mixfp4_kv_gather(cache: KVCache, slots: torch.Tensor, out_dtype=torch.bfloat
     _check_cache(cache)
     _require(out_dtype in (torch.float32, torch.bfloat16), "out_dtype must be torch.float32 or torch.bfloat16")
     _require(isinstance(slots, torch.Tensor) and slots.dim() == 1, "slots must be 1-D")
-    T, dev = slots.shape[0], cache.device
-    _check_index(slots, torch.int64, T, dev, "slots")
-    shape = (T, cache.heads, cache.head_dim)
+    c, at, T = cache._c, cache._index, slots.shape[0]
+    _check_index(slots, torch.int64, T, at, "slots")
     if out is None:
-        k, v = (_empty(shape, out_dtype, dev, stream) for _ in range(2))
+        k, v = (_dense((T, c.heads, c.head_dim), out_dtype, cache.device, stream) for _ in range(2))
     else:
         k, v = out
         for t in (k, v):
-            _check_heads(t, out_dtype, cache.heads, cache.head_dim, dev, "out")
-            _require(t.shape[0] == T and t.is_contiguous(), "out must be dense tensors with a row per slot")
+            shape, _ = _check_heads(t, out_dtype, c.heads, c.head_dim, at, "out")
+            _require(shape[0] == T and t.is_contiguous(), "out must be dense tensors with a row per slot")
     st = lib().mixfp4_kv_gather(cache._ref, slots.data_ptr(), T, k.data_ptr(), v.data_ptr(),
                                 DTYPE_F32 if out_dtype is torch.float32 else DTYPE_BF16, _stream(stream))
     _check("mixfp4_kv_gather", st)
@@ -904,40 +927,51 @@ def mixfp4_paged_attention(q: torch.Tensor, cache: KVCache, block_table: torch.T
     workspace: scratch memory of the caller's, at least
     paged_attention_workspace_bytes(cache, B, q_heads), aligned to 256 bytes."""
     _check_cache(cache)
-    D, dev = cache.head_dim, cache.device
-    _check_heads(q, torch.bfloat16, None, D, dev, "q")
-    B, H = q.shape[0], q.shape[1]
-    _require(H % cache.heads == 0, "q_heads must be a multiple of the cache's heads")
-    if not (isinstance(block_table, torch.Tensor) and block_table.is_cuda and block_table.device == dev
-            and block_table.dtype is torch.int32 and block_table.dim() == 2 and block_table.shape[0] == B
-            and (block_table.stride(1) == 1 or block_table.shape[1] <= 1)):
-        raise ValueError(f"block_table must be an int32 CUDA tensor [{B}, pages] on {dev} with unit column stride")
-    _check_index(lengths, torch.int32, B, dev, "lengths")
-    _require(window >= 0, "window must not be negative")
+    c, at = cache._c, cache._index
+    D = c.head_dim
+    shape, qs = _check_heads(q, torch.bfloat16, None, D, at, "q")
+    B, H, _ = shape
+    if H % c.heads:
+        raise ValueError("q_heads must be a multiple of the cache's heads")
+    try:
+        rows, pages = block_table.shape
+        ts, unit = block_table.stride()
+        good = (rows == B and block_table.dtype is torch.int32 and block_table.get_device() == at
+                and (unit == 1 or pages <= 1))
+    except (AttributeError, ValueError):
+        good = False
+    if not good:
+        raise ValueError(f"block_table must be an int32 CUDA tensor [{B}, pages] on device {at} with unit column "
+                         "stride")
+    _check_index(lengths, torch.int32, B, at, "lengths")
+    if window < 0:
+        raise ValueError("window must not be negative")
     if out is None:
-        out = _empty((B, H, D), torch.bfloat16, dev, stream)
+        out = _dense(shape, torch.bfloat16, cache.device, stream)
     else:
-        _check_heads(out, torch.bfloat16, H, D, dev, "out")
-        _require(out.shape[0] == B and out.is_contiguous(), "out must be dense, with a row per sequence")
+        oshape, _ = _check_heads(out, torch.bfloat16, H, D, at, "out")
+        _require(oshape[0] == B and out.is_contiguous(), "out must be dense, with a row per sequence")
     if lse is not None:
-        _check_dev(lse, dev, "lse")
+        _check_dev(lse, cache.device, "lse")
         _require(lse.dtype is torch.float32 and lse.shape == (B, H) and lse.is_contiguous(),
                  "lse must be a dense float32 [B, q_heads] tensor")
     elif return_lse:
-        lse = _empty((B, H), torch.float32, dev, stream)
+        lse = _dense((B, H), torch.float32, cache.device, stream)
     if workspace is None:
         n = cache._workspace_bytes.get((B, H))
         if n is None:
             n = cache._workspace_bytes[(B, H)] = paged_attention_workspace_bytes(cache, B, H)
-        workspace = _empty(n, torch.uint8, dev, stream, scratch=True)
+        workspace = _dense((n,), torch.uint8, cache.device, stream, scratch=True)
     else:
-        _check_scratch(workspace, dev)
-    qs, pages = q.stride(), block_table.shape[1]
+        _check_scratch(workspace, cache.device)
+        n = _bytes(workspace)
     st = lib().mixfp4_paged_attention(q.data_ptr(), qs[0], qs[1], B, H, cache._ref, block_table.data_ptr(),
-                                      max(block_table.stride(0), pages), pages, lengths.data_ptr(),
-                                      D ** -0.5 if scale is None else float(scale), int(window), out.data_ptr(),
-                                      _ptr(lse), workspace.data_ptr(), _bytes(workspace), _stream(stream))
-    _check("mixfp4_paged_attention", st)
+                                      ts if ts > pages else pages, pages, lengths.data_ptr(),
+                                      D ** -0.5 if scale is None else scale, window, out.data_ptr(),
+                                      None if lse is None else lse.data_ptr(), workspace.data_ptr(), n,
+                                      _stream(stream))
+    if st:
+        _check("mixfp4_paged_attention", st)
     return out if lse is None else (out, lse)
 
 
@@ -960,25 +994,35 @@ class Adapters:
                  "b must be [adapters, N, R] on a's device, a [adapters, R, K]")
         _require(8 <= R <= 128 and R % 8 == 0, "the rank must be a multiple of 8 up to 128")
         _require(K % 16 == 0, "K must be a multiple of 16")
-        _check_index(scaling, torch.float32, L, a.device, "scaling")
+        _check_index(scaling, torch.float32, L, a.get_device(), "scaling")
         self.a, self.b, self.scaling = a, b, scaling
-        self.count, self.rank, self.K, self.N, self.device = L, R, K, b.shape[1], a.device
+        self.count, self.rank, self.K, self.N = L, R, K, b.shape[1]
+        self.device, self._index = a.device, a.get_device()
 
 
-def _check_rows(t, dtype, rows, cols, device, what: str):
-    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.device == device and t.dtype is dtype and t.dim() == 2
-            and t.shape[0] == rows and t.shape[1] == cols and (t.stride(1) == 1 or cols <= 1)
-            and t.stride(0) >= cols):
-        raise ValueError(f"{what} must be a {dtype} CUDA tensor [{rows}, {cols}] on {device} with unit column stride")
+def _check_rows(t, dtype, rows, cols, index, what: str):
+    """[rows, cols] on CUDA device `index`, dense along a row: its row stride, at least cols."""
+    try:
+        if t.dtype is dtype and t.get_device() == index and t.shape == (rows, cols):
+            ld, unit = t.stride()
+            if rows <= 1:
+                ld = max(ld, cols)
+            if (unit == 1 or cols <= 1) and ld >= cols:
+                return ld
+    except AttributeError:
+        pass
+    raise ValueError(f"{what} must be a {dtype} CUDA tensor [{rows}, {cols}] on device {index} with unit column "
+                     "stride")
 
 
-def _check_segments(starts, ids, T: int, device) -> int:
+def _check_segments(starts, ids, T: int, index) -> int:
     if not (isinstance(ids, torch.Tensor) and ids.dim() == 1):
         raise ValueError("ids must be a 1-D int32 CUDA tensor")
     S = ids.shape[0]
-    _check_index(ids, torch.int32, S, device, "ids")
-    _check_index(starts, torch.int32, S + 1, device, "starts")
-    _require(S > 0 or T == 0, "tokens without a segment")
+    _check_index(ids, torch.int32, S, index, "ids")
+    _check_index(starts, torch.int32, S + 1, index, "starts")
+    if S == 0 and T > 0:
+        raise ValueError("tokens without a segment")
     return S
 
 
@@ -993,33 +1037,41 @@ def mixfp4_lora(x: torch.Tensor, adapters: Adapters, starts: torch.Tensor, ids: 
     for none.  base: float32 [T, N], the projection's result (linear()), or None.
     Returns (out, u): out float32 [T, N] (out=base adds in place) and u = x a^T
     float32 [T, R], which the backward pass takes."""
+    ad, T, ldx, S = _lora_args(adapters, x, starts, ids)
+    N, at, bp, ldb = ad.N, ad._index, None, 0
+    if base is not None:
+        ldb, bp = _check_rows(base, torch.float32, T, N, at, "base"), base.data_ptr()
+    if out is None:
+        out, ldo = _dense((T, N), torch.float32, ad.device, stream), N
+    else:
+        ldo = _check_rows(out, torch.float32, T, N, at, "out")
+    u = _lora_rows(u, T, ad, stream, "u")
+    st = lib().mixfp4_lora(x.data_ptr(), DTYPE_BF16, T, ad.K, ldx, ad.a.data_ptr(), ad.b.data_ptr(),
+                           ad.scaling.data_ptr(), ad.count, ad.rank, N, starts.data_ptr(), ids.data_ptr(), S, bp, ldb,
+                           out.data_ptr(), ldo, u.data_ptr(), _stream(stream))
+    if st:
+        _check("mixfp4_lora", st)
+    return out, u
+
+
+def _lora_args(adapters, x, starts, ids):
+    """The checks of the arguments both passes share: (adapters, tokens, x's row stride, segments)."""
     if not isinstance(adapters, Adapters):
         raise ValueError("adapters must be Adapters")
-    ad, dev = adapters, adapters.device
-    _check_x(x)
-    T, K = x.shape
-    _require(K == ad.K and x.device == dev, "x must have K columns, on the adapters' device")
-    S = _check_segments(starts, ids, T, dev)
-    if base is not None:
-        _check_rows(base, torch.float32, T, ad.N, dev, "base")
-    if out is None:
-        out = _empty((T, ad.N), torch.float32, dev, stream)
-    else:
-        _check_rows(out, torch.float32, T, ad.N, dev, "out")
-    u = _lora_rows(u, T, ad, stream, "u")
-    st = lib().mixfp4_lora(x.data_ptr(), DTYPE_BF16, T, K, x.stride(0), ad.a.data_ptr(), ad.b.data_ptr(),
-                           ad.scaling.data_ptr(), ad.count, ad.rank, ad.N, starts.data_ptr(), ids.data_ptr(), S,
-                           _ptr(base), 0 if base is None else max(base.stride(0), ad.N), out.data_ptr(),
-                           max(out.stride(0), ad.N), u.data_ptr(), _stream(stream))
-    _check("mixfp4_lora", st)
-    return out, u
+    try:
+        T = x.shape[0]
+    except (AttributeError, IndexError):
+        raise ValueError("x must be a 2-D bf16 CUDA tensor") from None
+    ldx = _check_rows(x, torch.bfloat16, T, adapters.K, adapters._index, "x")
+    return adapters, T, ldx, _check_segments(starts, ids, T, adapters._index)
 
 
 def _lora_rows(u, T: int, ad: Adapters, stream, what: str, scratch: bool = False):
     if u is None:
-        return _empty((T, ad.rank), torch.float32, ad.device, stream, scratch)
-    _check_rows(u, torch.float32, T, ad.rank, ad.device, what)
-    _require(u.is_contiguous(), f"{what} must be dense")
+        return _dense((T, ad.rank), torch.float32, ad.device, stream, scratch)
+    _check_rows(u, torch.float32, T, ad.rank, ad._index, what)
+    if not u.is_contiguous():
+        raise ValueError(f"{what} must be dense")
     return u
 
 
@@ -1034,38 +1086,35 @@ def mixfp4_lora_backward(dy: torch.Tensor, x: torch.Tensor, u: torch.Tensor, ada
     gradient, or None; out=base adds in place); da [adapters, R, K] and
     db [adapters, N, R], zeros for an adapter without tokens.
     workspace: dense float32 [T, R] scratch memory of the caller's."""
-    if not isinstance(adapters, Adapters):
-        raise ValueError("adapters must be Adapters")
-    ad, dev = adapters, adapters.device
-    _check_x(x)
-    T, K = x.shape
-    _require(K == ad.K and x.device == dev, "x must have K columns, on the adapters' device")
-    _check_rows(dy, torch.bfloat16, T, ad.N, dev, "dy")
-    _require(ad.N % 16 == 0, "N must be a multiple of 16")
-    S = _check_segments(starts, ids, T, dev)
-    _require(u is not None, "u is what the forward pass returned")
+    ad, T, ldx, S = _lora_args(adapters, x, starts, ids)
+    K, N, at, dev = ad.K, ad.N, ad._index, ad.device
+    ldy = _check_rows(dy, torch.bfloat16, T, N, at, "dy")
+    if N % 16:
+        raise ValueError("N must be a multiple of 16")
+    if u is None:
+        raise ValueError("u is what the forward pass returned")
     u = _lora_rows(u, T, ad, stream, "u")
     v = _lora_rows(workspace, T, ad, stream, "workspace", scratch=True)
+    bp, ldb = None, 0
     if base is not None:
-        _check_rows(base, torch.float32, T, K, dev, "base")
+        ldb, bp = _check_rows(base, torch.float32, T, K, at, "base"), base.data_ptr()
     if out is None:
-        out = _empty((T, K), torch.float32, dev, stream)
+        out, ldo = _dense((T, K), torch.float32, dev, stream), K
     else:
-        _check_rows(out, torch.float32, T, K, dev, "out")
+        ldo = _check_rows(out, torch.float32, T, K, at, "out")
     grads = []
     for t, like, what in ((da, ad.a, "da"), (db, ad.b, "db")):
         if t is None:
-            t = _empty(tuple(like.shape), torch.float32, dev, stream)
+            t = _dense(like.shape, torch.float32, dev, stream)
         else:
             _check_dev(t, dev, what)
             _require(t.dtype is torch.float32 and t.shape == like.shape and t.is_contiguous(),
                      f"{what} must be a dense float32 tensor of the adapters' shape")
         grads.append(t)
-    st = lib().mixfp4_lora_backward(dy.data_ptr(), max(dy.stride(0), ad.N), x.data_ptr(), x.stride(0), DTYPE_BF16, T,
-                                    K, u.data_ptr(), ad.a.data_ptr(), ad.b.data_ptr(), ad.scaling.data_ptr(),
-                                    ad.count, ad.rank, ad.N, starts.data_ptr(), ids.data_ptr(), S, _ptr(base),
-                                    0 if base is None else max(base.stride(0), K), out.data_ptr(),
-                                    max(out.stride(0), K), grads[0].data_ptr(), grads[1].data_ptr(), v.data_ptr(),
-                                    _stream(stream))
-    _check("mixfp4_lora_backward", st)
+    st = lib().mixfp4_lora_backward(dy.data_ptr(), ldy, x.data_ptr(), ldx, DTYPE_BF16, T, K, u.data_ptr(),
+                                    ad.a.data_ptr(), ad.b.data_ptr(), ad.scaling.data_ptr(), ad.count, ad.rank, N,
+                                    starts.data_ptr(), ids.data_ptr(), S, bp, ldb, out.data_ptr(), ldo,
+                                    grads[0].data_ptr(), grads[1].data_ptr(), v.data_ptr(), _stream(stream))
+    if st:
+        _check("mixfp4_lora_backward", st)
     return out, grads[0], grads[1]
