@@ -142,6 +142,9 @@ __device__ __forceinline__ uint32_t lds8(uint32_t a) {
   asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
   return v;
 }
+__device__ __forceinline__ void sts32(uint32_t a, uint32_t v) {
+  asm volatile("st.shared.b32 [%0], %1;" ::"r"(a), "r"(v) : "memory");
+}
 __device__ __forceinline__ void sts8(uint32_t a, uint32_t v) {
   asm volatile("st.shared.u8 [%0], %1;" ::"r"(a), "r"(v) : "memory");
 }
@@ -173,6 +176,21 @@ __device__ __forceinline__ uint32_t f16x2(float lo, float hi) {
   uint32_t d;
   asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
   return d;
+}
+// 2^x, results below 2^-126 as zero.
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// The factor (f16x2) and the payload tables of a block's scale byte.
+struct BlockScale {
+  uint32_t s2, lo, hi;
+};
+__device__ __forceinline__ BlockScale block_scale(uint32_t sc) {
+  const uint32_t e1m2 = sc >> 7;  // tables by multiplication: the integer pipe is the one that decoding fills
+  return BlockScale{cvt_f16x2_from_e4m3x2((uint16_t)((sc & 0x7Fu) * 0x0101u)),
+                    kLutE2M1Lo + e1m2 * (kLutE1M2Lo - kLutE2M1Lo), kLutE2M1Hi + e1m2 * (kLutE1M2Hi - kLutE2M1Hi)};
 }
 __device__ __forceinline__ float bf_lo(uint32_t v) { return __uint_as_float(v << 16); }
 __device__ __forceinline__ float bf_hi(uint32_t v) { return __uint_as_float(v & 0xFFFF0000u); }
@@ -339,7 +357,7 @@ __global__ void __launch_bounds__(kThreads, Cfg<DT, NT, kFp4>::kCtas) paged_atte
     };
     int asked = ask(0);
     // Asks for tile i; the result has a bit for each of its tokens that is there.
-    auto issue = [&](int i) -> uint32_t {
+    auto issue = [&](int i, uint32_t dst) -> uint32_t {
       const int tok = tok0 + 16 * (phase + phases * i);
       uint32_t there = (tok1 - tok >= 16 ? 0xFFFFu : (1u << (tok1 - tok)) - 1u);
       if (tok < range.x) there &= 0xFFFFu << (range.x - tok);
@@ -364,18 +382,29 @@ __global__ void __launch_bounds__(kThreads, Cfg<DT, NT, kFp4>::kCtas) paged_atte
           sat = (int64_t)page * p.c.scale_page_stride + (int64_t)off * p.c.scale_token_stride;
         }
       }
-      const uint32_t dst = ring + (i % C::kStages) * C::kStage;
       const int r0 = lane / C::kPieces, piece = lane % C::kPieces;
       const bool in_row = piece * (kFp4 ? 16 : 8) < D;
       const int64_t lane_at = r0 * step + piece * C::kCopy;
+      if (whole && there == 0xFFFFu) {  // as most tiles are
+        const uint8_t *ks = kb + (at + lane_at), *vs = vb + (at + lane_at);
 #pragma unroll
-      for (int j = 0; j < 16 / C::kRowsAtOnce; ++j) {
+        for (int j = 0; j < 16 / C::kRowsAtOnce; ++j) {
+          const int r = r0 + j * C::kRowsAtOnce;
+          cp_async<C::kCopy>(dst + C::k_place(r, piece), ks, in_row);
+          cp_async<C::kCopy>(dst + C::kKTile + C::v_place(r, piece), vs, in_row);
+          ks += C::kRowsAtOnce * step;
+          vs += C::kRowsAtOnce * step;
+        }
+      } else {
+#pragma unroll 1
+        for (int j = 0; j < 16 / C::kRowsAtOnce; ++j) {
         const int r = r0 + j * C::kRowsAtOnce;
         const bool take = ((there >> r) & 1u) && in_row;
         const int64_t from = whole ? at + lane_at + j * C::kRowsAtOnce * step
                                    : __shfl_sync(kAll, at, r) + piece * C::kCopy;
         cp_async<C::kCopy>(dst + C::k_place(r, piece), kb + from, take);
         cp_async<C::kCopy>(dst + C::kKTile + C::v_place(r, piece), vb + from, take);
+        }
       }
       if (kFp4) {
         const bool ok = (there >> (lane & 15)) & 1u;
@@ -397,12 +426,19 @@ __global__ void __launch_bounds__(kThreads, Cfg<DT, NT, kFp4>::kCtas) paged_atte
     uint32_t there[C::kStages];  // which of a tile's tokens there are; there[0]: the tile to be used next
 #pragma unroll
     for (int i = 0; i < C::kStages; ++i) there[i] = 0;
+    if constexpr (kFp4) {
+      if (D < DT)  // scale bytes behind D are read too, and stay as they are from here on
+        for (int i = lane; i < C::kStages * C::kScaleTile / 4; i += 32)
+          sts32(ring + i / (C::kScaleTile / 4) * C::kStage + C::kKTile + C::kVTile + i % (C::kScaleTile / 4) * 4, 0u);
+    }
     __syncwarp();
 #pragma unroll
     for (int i = 0; i < C::kStages - 1; ++i) {
-      if (i < tiles) there[i] = issue(i);
+      if (i < tiles) there[i] = issue(i, ring + i * C::kStage);
       cp_commit();
     }
+    uint32_t put = ring + (C::kStages - 1) * C::kStage, src = ring;  // the stages to fill and to use next
+    const uint32_t behind = ring + C::kStages * C::kStage;
 
     float o[NT][DT / 16][4];
     float m[NT][2], l[NT][2];
@@ -416,11 +452,10 @@ __global__ void __launch_bounds__(kThreads, Cfg<DT, NT, kFp4>::kCtas) paged_atte
 
     for (int i = 0; i < tiles; ++i) {
       __syncwarp();  // the stage about to be filled again has been read by every lane
-      if (i + C::kStages - 1 < tiles) there[C::kStages - 1] = issue(i + C::kStages - 1);
+      if (i + C::kStages - 1 < tiles) there[C::kStages - 1] = issue(i + C::kStages - 1, put);
       cp_commit();
       cp_wait<C::kStages - 1>();
       __syncwarp();
-      const uint32_t src = ring + (i % C::kStages) * C::kStage;
       const uint32_t vs = src + C::kKTile;
       const uint32_t ss = src + C::kKTile + C::kVTile;
 
@@ -436,13 +471,9 @@ __global__ void __launch_bounds__(kThreads, Cfg<DT, NT, kFp4>::kCtas) paged_atte
           const uint32_t a = src + C::k_place(g, t + 4 * k) + 8 * r * C::kRow;
           if constexpr (kFp4) {
             const uint2 v = lds64(a);
-            // beyond D the codes are zeros and the scale bytes whatever lay there
-            const uint32_t sc = (t + 4 * k) * 16 < D ? lds8(ss + (g + 8 * r) * 16 + t + 4 * k) : 0u;
-            const bool one = sc >> 7;
-            const uint32_t s2 = cvt_f16x2_from_e4m3x2((uint16_t)((sc & 0x7Fu) * 0x0101u));
-            const uint32_t ll = one ? kLutE1M2Lo : kLutE2M1Lo, lh = one ? kLutE1M2Hi : kLutE2M1Hi;
-            decode8(v.x, ll, lh, s2, w[r]);
-            decode8(v.y, ll, lh, s2, w[r] + 4);
+            const BlockScale f = block_scale(lds8(ss + (g + 8 * r) * 16 + t + 4 * k));
+            decode8(v.x, f.lo, f.hi, f.s2, w[r]);
+            decode8(v.y, f.lo, f.hi, f.s2, w[r] + 4);
           } else {
             const uint4 v = lds128(a);
             w[r][0] = v.x, w[r][1] = v.y, w[r][2] = v.z, w[r][3] = v.w;
@@ -479,7 +510,7 @@ __global__ void __launch_bounds__(kThreads, Cfg<DT, NT, kFp4>::kCtas) paged_atte
             v = fmaxf(v, __shfl_xor_sync(kAll, v, 8));
             v = fmaxf(v, __shfl_xor_sync(kAll, v, 16));
             v = fmaxf(m[n][j], v);
-            cor[j] = exp2f(m[n][j] - v);  // 0 at the first score
+            cor[j] = ex2(m[n][j] - v);  // 0 at the first score
             if (v == -INFINITY) cor[j] = 1.0f;
             m[n][j] = v;
             l[n][j] *= cor[j];
@@ -493,8 +524,8 @@ __global__ void __launch_bounds__(kThreads, Cfg<DT, NT, kFp4>::kCtas) paged_atte
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
           const float top = (m[n][j] == -INFINITY ? 0.0f : m[n][j]) - (kFp4 ? kFp4Exp : 0.0f);
-          w[j] = exp2f(s[n][j] - top);
-          w[2 + j] = exp2f(s[n][2 + j] - top);
+          w[j] = ex2(s[n][j] - top);
+          w[2 + j] = ex2(s[n][2 + j] - top);
           l[n][j] += w[j] + w[2 + j];
         }
         if (kFp4) {
@@ -520,17 +551,13 @@ __global__ void __launch_bounds__(kThreads, Cfg<DT, NT, kFp4>::kCtas) paged_atte
                              (C::kVBytes == C::kCopy ? 0 : (g & 1) * C::kVBytes);
           if constexpr (kFp4) {
             const int tr = 2 * t + (r & 1) + 8 * (r >> 1);
-            const int d = (g + 8 * k) * C::kVDims;
-            const uint32_t sc = d < D ? lds8(ss + (16 + tr) * 16 + d / 16) : 0u;
-            const bool one = sc >> 7;
-            const uint32_t s2 = cvt_f16x2_from_e4m3x2((uint16_t)((sc & 0x7Fu) * 0x0101u));
-            const uint32_t ll = one ? kLutE1M2Lo : kLutE2M1Lo, lh = one ? kLutE1M2Hi : kLutE2M1Hi;
+            const BlockScale f = block_scale(lds8(ss + (16 + tr) * 16 + (g + 8 * k) * C::kVDims / 16));
             if constexpr (C::kVBytes == 8) {
               const uint2 v = lds64(a);
-              decode8(v.x, ll, lh, s2, w[r]);
-              decode8(v.y, ll, lh, s2, w[r] + 4);
+              decode8(v.x, f.lo, f.hi, f.s2, w[r]);
+              decode8(v.y, f.lo, f.hi, f.s2, w[r] + 4);
             } else {
-              decode8(lds32(a), ll, lh, s2, w[r]);
+              decode8(lds32(a), f.lo, f.hi, f.s2, w[r]);
             }
           } else {
             const uint4 v = lds128(a);
@@ -551,6 +578,8 @@ __global__ void __launch_bounds__(kThreads, Cfg<DT, NT, kFp4>::kCtas) paged_atte
       }
 #pragma unroll
       for (int k = 0; k + 1 < C::kStages; ++k) there[k] = there[k + 1];
+      put = src;
+      src = src + C::kStage == behind ? ring : src + C::kStage;
     }
     cp_wait<0>();
 
