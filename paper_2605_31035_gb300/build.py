@@ -1,4 +1,5 @@
-"""Build libmixfp4.so (sm_103a) in-tree with nvcc.
+"""Build libmixfp4.so (sm_103a) in-tree with nvcc, and the Python binding
+_binding.so of its latency-bound entry points with the host compiler.
 
 Each translation unit under csrc/ is compiled in parallel with
 ``-gencode arch=compute_103a,code=sm_103a -lineinfo`` and linked into a
@@ -12,11 +13,13 @@ import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libmixfp4.so")
+BINDING = os.path.join(HERE, "_binding.so")
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 
 SOURCES = ["api.cu", "quantize.cu", "train.cu", "gemm.cu", "gemm_f16a.cu", "fewrows.cu", "native.cu", "candidates.cu", "noalloc.cu", "selftest.cu",
@@ -41,9 +44,9 @@ def _deps():
 
 
 def up_to_date() -> bool:
-    if not os.path.exists(LIB):
+    if not (os.path.exists(LIB) and os.path.exists(BINDING)):
         return False
-    t = os.path.getmtime(LIB)
+    t = min(os.path.getmtime(LIB), os.path.getmtime(BINDING))
     return all(os.path.getmtime(f) <= t for f in _deps())
 
 
@@ -56,12 +59,41 @@ def _compile(src: str) -> tuple[str, str]:
     return obj, res.stderr
 
 
+def _compile_binding() -> str:
+    """csrc/binding.cpp against this interpreter's and this torch's headers."""
+    import torch
+    root = os.path.dirname(torch.__file__)
+    obj = os.path.join(BUILD, "binding.o")
+    cmd = [shutil.which("g++") or shutil.which("c++") or "g++", "-O2", "-std=c++17", "-fPIC",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", f"-I{INCLUDE}",
+           f"-I{sysconfig.get_paths()['include']}", f"-I{root}/include", f"-I{root}/include/torch/csrc/api/include",
+           "-c", os.path.join(CSRC, "binding.cpp"), "-o", obj]
+    res = subprocess.run(cmd, capture_output=True, text=True)
+    if res.returncode != 0:
+        raise RuntimeError(f"the host compiler failed for binding.cpp:\n{res.stderr}")
+    return obj
+
+
+def _link_binding(obj: str):
+    import torch
+    tmp = BINDING + f".tmp{os.getpid()}"
+    cmd = [shutil.which("g++") or shutil.which("c++") or "g++", "-shared", "-o", tmp, obj, f"-L{HERE}",
+           f"-l:{os.path.basename(LIB)}", "-Wl,-rpath,$ORIGIN",
+           f"-L{os.path.dirname(torch.__file__)}/lib", "-ltorch_python", "-ltorch_cpu", "-ltorch", "-lc10"]
+    res = subprocess.run(cmd, capture_output=True, text=True)
+    if res.returncode != 0:
+        raise RuntimeError(f"link of the binding failed:\n{res.stderr}")
+    os.replace(tmp, BINDING)
+
+
 def build(force: bool = False, verbose: bool = False) -> str:
     if not force and up_to_date():
         return LIB
     os.makedirs(BUILD, exist_ok=True)
-    with cf.ThreadPoolExecutor(max_workers=len(SOURCES)) as ex:
+    with cf.ThreadPoolExecutor(max_workers=len(SOURCES) + 1) as ex:
+        binding = ex.submit(_compile_binding)
         results = list(ex.map(_compile, SOURCES))
+        binding = binding.result()
     if verbose:
         for _, log in results:
             sys.stderr.write(log)
@@ -71,6 +103,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
     if res.returncode != 0:
         raise RuntimeError(f"link failed:\n{res.stderr}")
     os.replace(tmp, LIB)
+    _link_binding(binding)
     return LIB
 
 

@@ -432,13 +432,15 @@ struct GradArgs {
   Segments seg;
 };
 
-template <int RT>
-__global__ void __launch_bounds__(kThreads, RT == 1 ? 2 : 1) lora_grad_kernel(const GradArgs p) {
+constexpr int kTogether = 2;
+
+template <int RT, int NW>
+__global__ void __launch_bounds__(32 * NW, NW == 8 ? 1 : (RT == 4 ? 2 : 3)) lora_grad_kernel(const GradArgs p) {
   extern __shared__ float4 sums[];  // [half the warps][tile][product][lane]
-  __shared__ int ends[kThreads], first[kThreads], count[kWarps], found[kWarps];
+  constexpr int threads = 32 * NW, warps = NW;
+  __shared__ int ends[threads], first[threads], count[warps], found[warps];
   griddep_wait();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
-  const int threads = blockDim.x, warps = threads >> 5;
   const int which = (int)blockIdx.x >= p.blocks[0];
   const int64_t n0 = (int64_t)((int)blockIdx.x - (which ? p.blocks[0] : 0)) * 64;
   const int adapter = blockIdx.y, r0 = blockIdx.z * 16 * RT, rg = r0 + 2 * RT * g;
@@ -538,12 +540,19 @@ __global__ void __launch_bounds__(kThreads, RT == 1 ? 2 : 1) lora_grad_kernel(co
         split3(cv[h][2].y, cv[h][3].y, a[3]);
         if (more) load_c(h);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          float d[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        for (int j0 = 0; j0 < 8; j0 += kTogether) {
+          float d[kTogether][4];
 #pragma unroll
-          for (int q = 2; q >= 0; --q) mma_bf16(d, a[0][q], a[1][q], a[2][q], a[3][q], b[j][0], b[j][1]);
+          for (int j = 0; j < kTogether; ++j) d[j][0] = d[j][1] = d[j][2] = d[j][3] = 0.0f;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) acc[h][j][e] += d[e];
+          for (int q = 2; q >= 0; --q)
+#pragma unroll
+            for (int j = 0; j < kTogether; ++j)
+              mma_bf16(d[j], a[0][q], a[1][q], a[2][q], a[3][q], b[j0 + j][0], b[j0 + j][1]);
+#pragma unroll
+          for (int j = 0; j < kTogether; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[h][j0 + j][e] += d[j][e];
         }
       }
     }
@@ -663,21 +672,24 @@ int expand(const ExpandArgs& p, cudaStream_t s) {
   return p.seg.tokens <= 16 * (int64_t)p.seg.count ? expand_held<16, kTrans>(p, s) : expand_held<64, kTrans>(p, s);
 }
 
-template <int RT>
-int launch_grad(GradArgs p, cudaStream_t s) {
-  auto* kernel = lora_grad_kernel<RT>;
+template <int RT, int NW>
+int launch_grad(const GradArgs& p, dim3 grid, cudaStream_t s) {
+  auto* kernel = lora_grad_kernel<RT, NW>;
   static std::atomic<uint64_t> done{0};
-  constexpr int kMost = kWarps / 2 * RT * 8 * 512;
-  if (kMost > 32 * 1024 && !set_dynamic_smem_once(reinterpret_cast<const void*>(kernel), kMost, done))
+  constexpr int kSums = NW / 2 * RT * 8 * 512;
+  if (kSums > 32 * 1024 && !set_dynamic_smem_once(reinterpret_cast<const void*>(kernel), kSums, done))
     return MIXFP4_ERR_CUDA;
+  return launch_pdl(kernel, grid, dim3(32 * NW), (size_t)kSums, s, p) == cudaSuccess ? MIXFP4_OK : MIXFP4_ERR_CUDA;
+}
+
+template <int RT>
+int grad(GradArgs p, cudaStream_t s) {
   for (int i = 0; i < 2; ++i) p.blocks[i] = (int)((p.dim[i] + 63) / 64);
   const dim3 grid((unsigned)(p.blocks[0] + p.blocks[1]), (unsigned)p.seg.adapters,
                   (unsigned)((p.R + 16 * RT - 1) / (16 * RT)));
-  // Four warps to a CTA, two CTAs side by side on an SM; eight where there would not be two CTAs to an SM.
-  const int warps = (int64_t)grid.x * grid.y * grid.z >= 2 * num_sms() ? 4 : 8;
-  return launch_pdl(kernel, grid, dim3(32 * warps), (size_t)(warps / 2 * RT * 8 * 512), s, p) == cudaSuccess
-             ? MIXFP4_OK
-             : MIXFP4_ERR_CUDA;
+  // Four warps to a CTA, some CTAs side by side on an SM; eight where there would not be two CTAs to an SM.
+  return (int64_t)grid.x * grid.y * grid.z >= 2 * num_sms() ? launch_grad<RT, 4>(p, grid, s)
+                                                            : launch_grad<RT, 8>(p, grid, s);
 }
 
 // The arguments both entry points share.
@@ -761,7 +773,7 @@ int mixfp4_lora_backward(const void* dy, int64_t ldy, const void* x, int64_t ldx
   gp.seg = seg;
   if (!tokens) gp.seg.count = 0;
   if (adapters == 0 || K + N == 0) return MIXFP4_OK;
-  return R <= 16 ? launch_grad<1>(gp, s) : (R <= 32 ? launch_grad<2>(gp, s) : launch_grad<4>(gp, s));
+  return R <= 16 ? grad<1>(gp, s) : (R <= 32 ? grad<2>(gp, s) : grad<4>(gp, s));
 }
 
 }  // extern "C"

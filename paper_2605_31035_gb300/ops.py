@@ -1,4 +1,6 @@
-"""Thin ctypes binding over libmixfp4.so (C ABI in include/mixfp4.h).
+"""Thin binding over libmixfp4.so (C ABI in include/mixfp4.h), by ctypes or,
+for the cache, its attention and the adapters, by the native module _binding
+(csrc/binding.cpp: the same checks and calls in a fraction of the time).
 
 Each function marshals torch CUDA tensors to device pointers and the current
 stream, calls the entry point of the same name, and raises on a nonzero status.
@@ -26,7 +28,9 @@ STATUS = {0: "ok", -1: "null pointer", -2: "invalid shape", -3: "misaligned", -4
 _ERR_CUDA = -5
 
 _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libmixfp4.so")
+_BINDING_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "_binding.so")
 _lib = None
+_binding = None
 
 
 class _CKVCache(ctypes.Structure):
@@ -96,27 +100,29 @@ def lib() -> ctypes.CDLL:
                                                          ctypes.c_uint64, P]
         L.mixfp4_selftest_bounded_wait.restype = I
         L.mixfp4_selftest_bounded_wait.argtypes = [P, ctypes.c_uint64, P]
-        C, F = ctypes.POINTER(_CKVCache), ctypes.c_float
-        L.mixfp4_kv_append.restype = I
-        L.mixfp4_kv_append.argtypes = [P, I64, I64, I64, P, I64, I64, P, I64, I64, I, I64, P, P, I64, I64, I, C, P, P,
-                                       I, P]
-        L.mixfp4_kv_gather.restype = I
-        L.mixfp4_kv_gather.argtypes = [C, P, I64, P, P, I, P]
-        L.mixfp4_paged_attention.restype = I
-        L.mixfp4_paged_attention.argtypes = [P, I64, I64, I64, I64, C, P, I64, I64, P, F, I64, P, P, P, I64, P]
         L.mixfp4_paged_attention_workspace.restype = I
-        L.mixfp4_paged_attention_workspace.argtypes = [C, I64, I64, ctypes.POINTER(I64)]
-        L.mixfp4_lora.restype = I
-        L.mixfp4_lora.argtypes = [P, I, I64, I64, I64, P, P, P, I64, I64, I64, P, P, I64, P, I64, P, I64, P, P]
-        L.mixfp4_lora_backward.restype = I
-        L.mixfp4_lora_backward.argtypes = [P, I64, P, I64, I, I64, I64, P, P, P, P, I64, I64, I64, P, P, I64, P, I64,
-                                           P, I64, P, P, P, P]
+        L.mixfp4_paged_attention_workspace.argtypes = [ctypes.POINTER(_CKVCache), I64, I64, ctypes.POINTER(I64)]
         L.mixfp4_status_string.restype = ctypes.c_char_p
         L.mixfp4_status_string.argtypes = [I]
         L.mixfp4_version.restype = I
         L.mixfp4_version.argtypes = []
         _lib = L
     return _lib
+
+
+def _native():
+    """Load _binding.so, and the library with it; raise if they have not been built."""
+    global _binding
+    if _binding is None:
+        lib()
+        if not os.path.exists(_BINDING_PATH):
+            raise RuntimeError(
+                f"{_BINDING_PATH} is missing: build it with `python -c 'import __graft_entry__ as g; g.build()'`")
+        from importlib import machinery, util
+        loader = machinery.ExtensionFileLoader("_binding", _BINDING_PATH)
+        _binding = util.module_from_spec(util.spec_from_file_location("_binding", _BINDING_PATH, loader=loader))
+        loader.exec_module(_binding)
+    return _binding
 
 
 def _require(cond: bool, msg: str):
@@ -749,8 +755,7 @@ class KVCache:
         else:
             _require(v_scales is None and k_ts is None and v_ts is None, "a bf16 cache has no scales")
         self._c = c
-        self._ref = ctypes.byref(c)
-        self._workspace_bytes = {}
+        self._address = ctypes.addressof(c)
         self.device, self._index = k.device, k.get_device()
 
     @property
@@ -789,41 +794,17 @@ def _check_cache(cache):
         raise ValueError("cache must be a KVCache")
 
 
-# A call on a few tokens runs for less time on the GPU than its arguments take
-# to look at here, so the checks ask each tensor for as little as will do:
-# get_device() is the device's index, -1 for a tensor elsewhere.
+def _result(shape, dtype, device, stream, scratch: bool = False):
+    """Memory for a call on another stream than the current one, which the
+    binding allocates on; None where it can."""
+    return _empty(shape, dtype, device, stream, scratch) if _elsewhere(stream, device) else None
 
 
-def _dense(shape, dtype, device, stream, scratch: bool = False):
-    """_empty of up to three dimensions, by torch's quickest constructor on the current stream."""
-    if stream is not None:
-        return _empty(shape, dtype, device, stream, scratch)
-    n = len(shape)
-    strides = (1,) if n == 1 else (shape[1], 1) if n == 2 else (shape[1] * shape[2], shape[2], 1)
-    return torch.empty_strided(shape, strides, dtype=dtype, device=device)
-
-
-def _check_heads(t, dtype, heads, D, index, what: str):
-    """[tokens, heads, head_dim] on CUDA device `index`, dense along head_dim: its sizes and strides."""
-    try:
-        if t.dtype is dtype and t.get_device() == index:
-            shape, stride = t.shape, t.stride()
-            T, H, d = shape
-            if d == D and (heads is None or H == heads) and stride[2] == 1:
-                return shape, stride
-    except (AttributeError, ValueError):
-        pass
-    raise ValueError(f"{what} must be a {dtype} CUDA tensor [tokens, {heads if heads else 'heads'}, {D}] on "
-                     f"device {index} with unit last stride")
-
-
-def _check_index(t, dtype, n, index, what: str):
-    try:
-        if t.dtype is dtype and t.get_device() == index and t.shape == (n,) and (n <= 1 or t.stride(0) == 1):
-            return
-    except AttributeError:
-        pass
-    raise ValueError(f"{what} must be a dense {dtype} CUDA tensor of {n} elements on device {index}")
+def _shape(t, dims: int):
+    """A tensor's shape, checked as far as results of a call depend on it (the binding checks the rest)."""
+    if not (isinstance(t, torch.Tensor) and t.dim() == dims):
+        raise ValueError(f"a CUDA tensor of {dims} dimensions is wanted")
+    return t.shape
 
 
 def mixfp4_kv_append(k: torch.Tensor, v: torch.Tensor, cache: KVCache, slots: torch.Tensor,
@@ -839,45 +820,13 @@ def mixfp4_kv_append(k: torch.Tensor, v: torch.Tensor, cache: KVCache, slots: to
     rotated on the way: pairs (i, i + rot_dim / 2), or (2i, 2i + 1) if interleaved.
     Returns the (rotated) queries as bf16 [T, q_heads, head_dim], or None."""
     _check_cache(cache)
-    c, at = cache._c, cache._index
-    D, dtype = c.head_dim, getattr(k, "dtype", None)
-    if dtype is not torch.float32 and dtype is not torch.bfloat16:
-        raise ValueError("k must be a bfloat16 or float32 CUDA tensor")
-    shape, ks = _check_heads(k, dtype, c.heads, D, at, "k")
-    vshape, vs = _check_heads(v, dtype, c.heads, D, at, "v")
-    T = shape[0]
-    if vshape != shape:
-        raise ValueError("k and v must have as many tokens")
-    _check_index(slots, torch.int64, T, at, "slots")
-    rot = rows = angles = places = 0
-    if cos_sin is not None:
-        _check_index(positions, torch.int64, T, at, "positions")
-        if not (isinstance(cos_sin, torch.Tensor) and cos_sin.get_device() == at and cos_sin.dtype is torch.float32
-                and cos_sin.dim() == 2 and cos_sin.is_contiguous()):
-            raise ValueError("cos_sin must be a dense float32 CUDA tensor [positions, rot_dim]")
-        rows, rot = cos_sin.shape
-        if rot % 2 or rot > D:
-            raise ValueError("rot_dim must be even and at most head_dim")
-        angles, places = cos_sin.data_ptr(), positions.data_ptr()
-    o, qs, heads, qp, op = None, (0, 0), 0, None, None
-    if q is not None:
-        qshape, qs = _check_heads(q, dtype, None, D, at, "q")
-        heads = qshape[1]
-        if qshape[0] != T:
-            raise ValueError("q must have as many tokens as k")
-        if out is None:
-            o = _dense((T, heads, D), torch.bfloat16, cache.device, stream)
-        else:
-            o = out
-            oshape, _ = _check_heads(o, torch.bfloat16, heads, D, at, "out")
-            _require(oshape[0] == T and o.is_contiguous(), "out must be dense, with as many tokens as q")
-        qp, op = q.data_ptr(), o.data_ptr()
-    st = lib().mixfp4_kv_append(qp, qs[0], qs[1], heads, k.data_ptr(), ks[0], ks[1], v.data_ptr(), vs[0], vs[1],
-                                DTYPE_BF16 if dtype is torch.bfloat16 else DTYPE_F32, T, places, angles, rows, rot,
-                                1 if interleaved else 0, cache._ref, slots.data_ptr(), op, mode, _stream(stream))
-    if st:
-        _check("mixfp4_kv_append", st)
-    return o
+    if stream is not None and q is not None and out is None:
+        out = _result(_shape(q, 3), torch.bfloat16, cache.device, stream)
+    r = _native().kv_append(cache._address, cache._index, k, v, slots, q, positions, cos_sin, interleaved, mode, out,
+                            _stream(stream))
+    if r.__class__ is int:
+        _check("mixfp4_kv_append", r)
+    return r
 
 
 def mixfp4_kv_gather(cache: KVCache, slots: torch.Tensor, out_dtype=torch.bfloat16, out=None, stream=None):
@@ -886,27 +835,23 @@ def mixfp4_kv_gather(cache: KVCache, slots: torch.Tensor, out_dtype=torch.bfloat
     cache gives zeros.  out: a pair of dense tensors to write."""
     _check_cache(cache)
     _require(out_dtype in (torch.float32, torch.bfloat16), "out_dtype must be torch.float32 or torch.bfloat16")
-    _require(isinstance(slots, torch.Tensor) and slots.dim() == 1, "slots must be 1-D")
-    c, at, T = cache._c, cache._index, slots.shape[0]
-    _check_index(slots, torch.int64, T, at, "slots")
-    if out is None:
-        k, v = (_dense((T, c.heads, c.head_dim), out_dtype, cache.device, stream) for _ in range(2))
-    else:
-        k, v = out
-        for t in (k, v):
-            shape, _ = _check_heads(t, out_dtype, c.heads, c.head_dim, at, "out")
-            _require(shape[0] == T and t.is_contiguous(), "out must be dense tensors with a row per slot")
-    st = lib().mixfp4_kv_gather(cache._ref, slots.data_ptr(), T, k.data_ptr(), v.data_ptr(),
-                                DTYPE_F32 if out_dtype is torch.float32 else DTYPE_BF16, _stream(stream))
-    _check("mixfp4_kv_gather", st)
-    return k, v
+    k, v = (None, None) if out is None else out
+    if stream is not None and out is None:
+        shape = (*_shape(slots, 1), cache.heads, cache.head_dim)
+        k, v = (_result(shape, out_dtype, cache.device, stream) for _ in range(2))
+    r = _native().kv_gather(cache._address, cache._index, slots, out_dtype is torch.float32, k, v,
+                            _stream(stream))
+    if r.__class__ is int:
+        _check("mixfp4_kv_gather", r)
+    return r
 
 
 def paged_attention_workspace_bytes(cache: KVCache, B: int, q_heads: int) -> int:
     """Bytes of scratch memory mixfp4_paged_attention takes."""
     _check_cache(cache)
     n = ctypes.c_int64(0)
-    _check("mixfp4_paged_attention", lib().mixfp4_paged_attention_workspace(cache._ref, B, q_heads, ctypes.byref(n)))
+    _check("mixfp4_paged_attention", lib().mixfp4_paged_attention_workspace(ctypes.byref(cache._c), B, q_heads,
+                                                                                 ctypes.byref(n)))
     return n.value
 
 
@@ -927,52 +872,18 @@ def mixfp4_paged_attention(q: torch.Tensor, cache: KVCache, block_table: torch.T
     workspace: scratch memory of the caller's, at least
     paged_attention_workspace_bytes(cache, B, q_heads), aligned to 256 bytes."""
     _check_cache(cache)
-    c, at = cache._c, cache._index
-    D = c.head_dim
-    shape, qs = _check_heads(q, torch.bfloat16, None, D, at, "q")
-    B, H, _ = shape
-    if H % c.heads:
-        raise ValueError("q_heads must be a multiple of the cache's heads")
-    try:
-        rows, pages = block_table.shape
-        ts, unit = block_table.stride()
-        good = (rows == B and block_table.dtype is torch.int32 and block_table.get_device() == at
-                and (unit == 1 or pages <= 1))
-    except (AttributeError, ValueError):
-        good = False
-    if not good:
-        raise ValueError(f"block_table must be an int32 CUDA tensor [{B}, pages] on device {at} with unit column "
-                         "stride")
-    _check_index(lengths, torch.int32, B, at, "lengths")
-    if window < 0:
-        raise ValueError("window must not be negative")
-    if out is None:
-        out = _dense(shape, torch.bfloat16, cache.device, stream)
-    else:
-        oshape, _ = _check_heads(out, torch.bfloat16, H, D, at, "out")
-        _require(oshape[0] == B and out.is_contiguous(), "out must be dense, with a row per sequence")
-    if lse is not None:
-        _check_dev(lse, cache.device, "lse")
-        _require(lse.dtype is torch.float32 and lse.shape == (B, H) and lse.is_contiguous(),
-                 "lse must be a dense float32 [B, q_heads] tensor")
-    elif return_lse:
-        lse = _dense((B, H), torch.float32, cache.device, stream)
-    if workspace is None:
-        n = cache._workspace_bytes.get((B, H))
-        if n is None:
-            n = cache._workspace_bytes[(B, H)] = paged_attention_workspace_bytes(cache, B, H)
-        workspace = _dense((n,), torch.uint8, cache.device, stream, scratch=True)
-    else:
-        _check_scratch(workspace, cache.device)
-        n = _bytes(workspace)
-    st = lib().mixfp4_paged_attention(q.data_ptr(), qs[0], qs[1], B, H, cache._ref, block_table.data_ptr(),
-                                      ts if ts > pages else pages, pages, lengths.data_ptr(),
-                                      D ** -0.5 if scale is None else scale, window, out.data_ptr(),
-                                      None if lse is None else lse.data_ptr(), workspace.data_ptr(), n,
-                                      _stream(stream))
-    if st:
-        _check("mixfp4_paged_attention", st)
-    return out if lse is None else (out, lse)
+    if stream is not None:
+        B, H, D = _shape(q, 3)
+        out = _result((B, H, D), torch.bfloat16, cache.device, stream) if out is None else out
+        if lse is None and return_lse:
+            lse = _result((B, H), torch.float32, cache.device, stream)
+        if workspace is None and _elsewhere(stream, cache.device) and H % cache.heads == 0:
+            workspace = _empty(paged_attention_workspace_bytes(cache, B, H), torch.uint8, cache.device, stream, True)
+    r = _native().paged_attention(cache._address, cache._index, q, block_table, lengths, scale, window, out, lse,
+                                  return_lse, workspace, _stream(stream))
+    if r.__class__ is int:
+        _check("mixfp4_paged_attention", r)
+    return r
 
 
 # ---- low-rank adapters ----------------------------------------------------------
@@ -994,36 +905,17 @@ class Adapters:
                  "b must be [adapters, N, R] on a's device, a [adapters, R, K]")
         _require(8 <= R <= 128 and R % 8 == 0, "the rank must be a multiple of 8 up to 128")
         _require(K % 16 == 0, "K must be a multiple of 16")
-        _check_index(scaling, torch.float32, L, a.get_device(), "scaling")
+        _check_dev(scaling, a.device, "scaling")
+        _require(scaling.dtype is torch.float32 and scaling.shape == (L,) and scaling.is_contiguous(),
+                 "scaling must be a dense float32 tensor with an element per adapter")
         self.a, self.b, self.scaling = a, b, scaling
         self.count, self.rank, self.K, self.N = L, R, K, b.shape[1]
         self.device, self._index = a.device, a.get_device()
 
 
-def _check_rows(t, dtype, rows, cols, index, what: str):
-    """[rows, cols] on CUDA device `index`, dense along a row: its row stride, at least cols."""
-    try:
-        if t.dtype is dtype and t.get_device() == index and t.shape == (rows, cols):
-            ld, unit = t.stride()
-            if rows <= 1:
-                ld = max(ld, cols)
-            if (unit == 1 or cols <= 1) and ld >= cols:
-                return ld
-    except AttributeError:
-        pass
-    raise ValueError(f"{what} must be a {dtype} CUDA tensor [{rows}, {cols}] on device {index} with unit column "
-                     "stride")
-
-
-def _check_segments(starts, ids, T: int, index) -> int:
-    if not (isinstance(ids, torch.Tensor) and ids.dim() == 1):
-        raise ValueError("ids must be a 1-D int32 CUDA tensor")
-    S = ids.shape[0]
-    _check_index(ids, torch.int32, S, index, "ids")
-    _check_index(starts, torch.int32, S + 1, index, "starts")
-    if S == 0 and T > 0:
-        raise ValueError("tokens without a segment")
-    return S
+def _check_adapters(adapters):
+    if not isinstance(adapters, Adapters):
+        raise ValueError("adapters must be Adapters")
 
 
 def mixfp4_lora(x: torch.Tensor, adapters: Adapters, starts: torch.Tensor, ids: torch.Tensor,
@@ -1037,42 +929,16 @@ def mixfp4_lora(x: torch.Tensor, adapters: Adapters, starts: torch.Tensor, ids: 
     for none.  base: float32 [T, N], the projection's result (linear()), or None.
     Returns (out, u): out float32 [T, N] (out=base adds in place) and u = x a^T
     float32 [T, R], which the backward pass takes."""
-    ad, T, ldx, S = _lora_args(adapters, x, starts, ids)
-    N, at, bp, ldb = ad.N, ad._index, None, 0
-    if base is not None:
-        ldb, bp = _check_rows(base, torch.float32, T, N, at, "base"), base.data_ptr()
-    if out is None:
-        out, ldo = _dense((T, N), torch.float32, ad.device, stream), N
-    else:
-        ldo = _check_rows(out, torch.float32, T, N, at, "out")
-    u = _lora_rows(u, T, ad, stream, "u")
-    st = lib().mixfp4_lora(x.data_ptr(), DTYPE_BF16, T, ad.K, ldx, ad.a.data_ptr(), ad.b.data_ptr(),
-                           ad.scaling.data_ptr(), ad.count, ad.rank, N, starts.data_ptr(), ids.data_ptr(), S, bp, ldb,
-                           out.data_ptr(), ldo, u.data_ptr(), _stream(stream))
-    if st:
-        _check("mixfp4_lora", st)
-    return out, u
-
-
-def _lora_args(adapters, x, starts, ids):
-    """The checks of the arguments both passes share: (adapters, tokens, x's row stride, segments)."""
-    if not isinstance(adapters, Adapters):
-        raise ValueError("adapters must be Adapters")
-    try:
-        T = x.shape[0]
-    except (AttributeError, IndexError):
-        raise ValueError("x must be a 2-D bf16 CUDA tensor") from None
-    ldx = _check_rows(x, torch.bfloat16, T, adapters.K, adapters._index, "x")
-    return adapters, T, ldx, _check_segments(starts, ids, T, adapters._index)
-
-
-def _lora_rows(u, T: int, ad: Adapters, stream, what: str, scratch: bool = False):
-    if u is None:
-        return _dense((T, ad.rank), torch.float32, ad.device, stream, scratch)
-    _check_rows(u, torch.float32, T, ad.rank, ad._index, what)
-    if not u.is_contiguous():
-        raise ValueError(f"{what} must be dense")
-    return u
+    _check_adapters(adapters)
+    ad = adapters
+    if stream is not None:
+        T = _shape(x, 2)[0]
+        out = _result((T, ad.N), torch.float32, ad.device, stream) if out is None else out
+        u = _result((T, ad.rank), torch.float32, ad.device, stream) if u is None else u
+    r = _native().lora(ad.a, ad.b, ad.scaling, ad._index, x, starts, ids, base, out, u, _stream(stream))
+    if r.__class__ is int:
+        _check("mixfp4_lora", r)
+    return r
 
 
 def mixfp4_lora_backward(dy: torch.Tensor, x: torch.Tensor, u: torch.Tensor, adapters: Adapters,
@@ -1086,35 +952,16 @@ def mixfp4_lora_backward(dy: torch.Tensor, x: torch.Tensor, u: torch.Tensor, ada
     gradient, or None; out=base adds in place); da [adapters, R, K] and
     db [adapters, N, R], zeros for an adapter without tokens.
     workspace: dense float32 [T, R] scratch memory of the caller's."""
-    ad, T, ldx, S = _lora_args(adapters, x, starts, ids)
-    K, N, at, dev = ad.K, ad.N, ad._index, ad.device
-    ldy = _check_rows(dy, torch.bfloat16, T, N, at, "dy")
-    if N % 16:
-        raise ValueError("N must be a multiple of 16")
-    if u is None:
-        raise ValueError("u is what the forward pass returned")
-    u = _lora_rows(u, T, ad, stream, "u")
-    v = _lora_rows(workspace, T, ad, stream, "workspace", scratch=True)
-    bp, ldb = None, 0
-    if base is not None:
-        ldb, bp = _check_rows(base, torch.float32, T, K, at, "base"), base.data_ptr()
-    if out is None:
-        out, ldo = _dense((T, K), torch.float32, dev, stream), K
-    else:
-        ldo = _check_rows(out, torch.float32, T, K, at, "out")
-    grads = []
-    for t, like, what in ((da, ad.a, "da"), (db, ad.b, "db")):
-        if t is None:
-            t = _dense(like.shape, torch.float32, dev, stream)
-        else:
-            _check_dev(t, dev, what)
-            _require(t.dtype is torch.float32 and t.shape == like.shape and t.is_contiguous(),
-                     f"{what} must be a dense float32 tensor of the adapters' shape")
-        grads.append(t)
-    st = lib().mixfp4_lora_backward(dy.data_ptr(), ldy, x.data_ptr(), ldx, DTYPE_BF16, T, K, u.data_ptr(),
-                                    ad.a.data_ptr(), ad.b.data_ptr(), ad.scaling.data_ptr(), ad.count, ad.rank, N,
-                                    starts.data_ptr(), ids.data_ptr(), S, bp, ldb, out.data_ptr(), ldo,
-                                    grads[0].data_ptr(), grads[1].data_ptr(), v.data_ptr(), _stream(stream))
-    if st:
-        _check("mixfp4_lora_backward", st)
-    return out, grads[0], grads[1]
+    _check_adapters(adapters)
+    ad = adapters
+    if stream is not None:
+        T, dev = _shape(x, 2)[0], ad.device
+        out = _result((T, ad.K), torch.float32, dev, stream) if out is None else out
+        da = _result(tuple(ad.a.shape), torch.float32, dev, stream) if da is None else da
+        db = _result(tuple(ad.b.shape), torch.float32, dev, stream) if db is None else db
+        workspace = _result((T, ad.rank), torch.float32, dev, stream, True) if workspace is None else workspace
+    r = _native().lora_backward(ad.a, ad.b, ad.scaling, ad._index, dy, x, u, starts, ids, base, out, da, db, workspace,
+                                _stream(stream))
+    if r.__class__ is int:
+        _check("mixfp4_lora_backward", r)
+    return r
