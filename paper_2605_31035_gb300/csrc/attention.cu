@@ -45,6 +45,8 @@ namespace {
 constexpr int kWarps = 4;
 constexpr int kThreads = kWarps * 32;
 constexpr int kJoinThreads = 256;
+constexpr int kCluster = 8;
+constexpr int kClusterTokens = 4096;
 constexpr int kUnit = 64;  // head rows of a unit of work: 64 / together tokens of `together` key heads
 constexpr unsigned kAll = 0xFFFFFFFFu;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
@@ -57,6 +59,7 @@ struct AttnArgs {
   int64_t q_stride, q_head_stride;
   int B, q_heads, group, chunks;  // group = q_heads / heads; chunks of 8 NT query heads per key head
   int together;                   // key heads of a CTA: 4, 2 or 1, each a warp's (or two's, or four's)
+  int clustered;                  // one cluster of kCluster CTAs to a row, joined in shared memory
   mixfp4_kv_cache c;
   int page_shift;  // log2 page_size, or -1
   const int32_t* table;
@@ -106,7 +109,7 @@ struct Cfg {
   static constexpr int kFit = 220 * 1024 / kCtas / (kWarps * kStage);
   static constexpr int kStages = kFit < 6 ? kFit : 6;
   static constexpr int kRing = kWarps * kStages * kStage;
-  static constexpr int kMerge = kWarps * kHeads * (DT + 4) * 4;
+  static constexpr int kMerge = (kWarps + 1) * kHeads * (DT + 4) * 4;  // the warps' results, and in a cluster the CTA's
   static constexpr int kSmem = kRing > kMerge ? kRing : kMerge;
 };
 
@@ -195,6 +198,24 @@ __device__ __forceinline__ BlockScale block_scale(uint32_t sc) {
 __device__ __forceinline__ float bf_lo(uint32_t v) { return __uint_as_float(v << 16); }
 __device__ __forceinline__ float bf_hi(uint32_t v) { return __uint_as_float(v & 0xFFFF0000u); }
 
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void cluster_barrier() {
+  asm volatile("barrier.cluster.arrive.aligned;\n barrier.cluster.wait.aligned;" ::: "memory");
+}
+// Two floats of CTA `rank`'s shared memory, at the address they have in this one's (after a cluster barrier).
+__device__ __forceinline__ float2 peer_load(const float* p, uint32_t rank) {
+  float2 v;
+  asm volatile("{ .reg .b32 r; mapa.shared::cluster.u32 r, %2, %3; ld.shared::cluster.v2.f32 {%0, %1}, [r]; }"
+               : "=f"(v.x), "=f"(v.y)
+               : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(rank)
+               : "memory");
+  return v;
+}
+
 // Tokens [first, end) of sequence b that are seen.
 __device__ __forceinline__ int2 seen(const AttnArgs& p, int b) {
   int64_t n = p.lengths[b];
@@ -213,6 +234,14 @@ __device__ __forceinline__ void store_out(const AttnArgs& p, int b, int h, int d
   *reinterpret_cast<uint32_t*>(p.out + ((int64_t)b * p.q_heads + h) * p.c.head_dim + d) = bf16x2(x, y);
 }
 
+// Sequence b's results where it sees no token.
+__device__ __forceinline__ void nothing_seen(const AttnArgs& p, int b, int tid) {
+  const int64_t words = (int64_t)p.q_heads * p.c.head_dim / 2;
+  for (int64_t i = tid; i < words; i += kThreads) reinterpret_cast<uint32_t*>(p.out)[b * words + i] = 0u;
+  if (p.lse)
+    for (int h = tid; h < p.q_heads; h += kThreads) p.lse[(int64_t)b * p.q_heads + h] = -INFINITY;
+}
+
 template <int DT, int NT, bool kFp4>
 __global__ void __launch_bounds__(kThreads, Cfg<DT, NT, kFp4>::kCtas) paged_attention_kernel(const AttnArgs p) {
   using C = Cfg<DT, NT, kFp4>;
@@ -226,54 +255,63 @@ __global__ void __launch_bounds__(kThreads, Cfg<DT, NT, kFp4>::kCtas) paged_atte
   const int mate = warp % p.together, phase = warp / p.together, phases = kWarps / p.together;
 
   // This CTA's share [pos, end) of all units, and the sequence it starts in.
-  const int strip = (p.B + kThreads - 1) / kThreads;
-  int64_t mine = 0;
-  for (int b = tid * strip; b < min(p.B, (tid + 1) * strip); ++b) mine += units(p, seen(p, b));
-  int64_t before = mine;
-#pragma unroll
-  for (int d = 1; d < 32; d <<= 1) {
-    const int64_t v = __shfl_up_sync(kAll, before, d);
-    if (lane >= d) before += v;
-  }
-  if (lane == 31) sh_scan[warp] = before;
-  __syncthreads();
-  int64_t total = 0;
-#pragma unroll
-  for (int w = 0; w < kWarps; ++w) {
-    if (w < warp) before += sh_scan[w];
-    total += sh_scan[w];
-  }
-  before -= mine;
-  const int64_t all = total * rows;
-  const int64_t grid = all < (int64_t)gridDim.x ? all : (int64_t)gridDim.x;  // CTAs with a share
-  for (int b = blockIdx.x; b < p.B; b += gridDim.x) {  // sequences that see nothing
+  int b = 0;
+  int64_t pos = 0, end = 1, base = 0, all = 0, grid = 0;
+  if (p.clustered) {
+    b = (int)(blockIdx.x / kCluster) / rows;
     const int2 r = seen(p, b);
-    if (r.y > r.x) continue;
-    if (p.by_row)
-      for (int i = tid; i < rows; i += kThreads) p.split[(int64_t)b * rows + i] = make_int4(-1, 0, 0, 0);
-    for (int i = tid; i < p.q_heads * D / 2; i += kThreads)
-      reinterpret_cast<uint32_t*>(p.out)[(int64_t)b * p.q_heads * D / 2 + i] = 0u;
-    if (p.lse)
-      for (int h = tid; h < p.q_heads; h += kThreads) p.lse[(int64_t)b * p.q_heads + h] = -INFINITY;
-  }
-  if (tid == 0 && !p.by_row) p.split[blockIdx.x] = make_int4(-1, 0, 0, 0);
-  if ((int64_t)blockIdx.x >= grid) return;
-  int64_t pos = all * blockIdx.x / grid;
-  const int64_t end = all * (blockIdx.x + 1) / grid;
-  if (pos >= before * rows && pos < (before + mine) * rows) {
-    int b = tid * strip;
-    int64_t at = before;
-    for (const int to = min(p.B, b + strip) - 1; b < to; ++b) {
-      const int u = units(p, seen(p, b));
-      if (pos < (at + u) * rows) break;
-      at += u;
+    if (r.y <= r.x) {  // the cluster's row sees nothing
+      if (blockIdx.x % (kCluster * rows) == 0) nothing_seen(p, b, tid);
+      return;
     }
-    sh_b = b;
-    sh_before = at;
+  } else {
+    const int strip = (p.B + kThreads - 1) / kThreads;
+    int64_t mine = 0;
+    for (int i = tid * strip; i < min(p.B, (tid + 1) * strip); ++i) mine += units(p, seen(p, i));
+    int64_t before = mine;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int64_t v = __shfl_up_sync(kAll, before, d);
+      if (lane >= d) before += v;
+    }
+    if (lane == 31) sh_scan[warp] = before;
+    if (tid == 0) sh_b = p.B;
+    __syncthreads();
+    int64_t total = 0;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) {
+      if (w < warp) before += sh_scan[w];
+      total += sh_scan[w];
+    }
+    before -= mine;
+    all = total * rows;
+    grid = all < (int64_t)gridDim.x ? all : (int64_t)gridDim.x;  // CTAs with a share
+    for (int i = blockIdx.x; i < p.B; i += gridDim.x) {  // sequences that see nothing
+      const int2 r = seen(p, i);
+      if (r.y > r.x) continue;
+      if (p.by_row)
+        for (int k = tid; k < rows; k += kThreads) p.split[(int64_t)i * rows + k] = make_int4(-1, 0, 0, 0);
+      nothing_seen(p, i, tid);
+    }
+    if (tid == 0 && !p.by_row) p.split[blockIdx.x] = make_int4(-1, 0, 0, 0);
+    if ((int64_t)blockIdx.x >= grid) return;
+    pos = all * blockIdx.x / grid;
+    end = all * (blockIdx.x + 1) / grid;
+    if (pos >= before * rows && pos < (before + mine) * rows) {
+      int i = tid * strip;
+      int64_t at = before;
+      for (const int to = min(p.B, i + strip) - 1; i < to; ++i) {
+        const int u = units(p, seen(p, i));
+        if (pos < (at + u) * rows) break;
+        at += u;
+      }
+      sh_b = i;
+      sh_before = at;
+    }
+    __syncthreads();
+    b = sh_b;
+    base = sh_before * rows;  // first unit of sequence b
   }
-  __syncthreads();
-  int b = sh_b;
-  int64_t base = sh_before * rows;  // first unit of sequence b
 
   const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem) + warp * C::kStages * C::kStage;
   const float kts = kFp4 ? *p.c.k_ts : 1.0f, vts = kFp4 ? *p.c.v_ts : 1.0f;
@@ -281,14 +319,22 @@ __global__ void __launch_bounds__(kThreads, Cfg<DT, NT, kFp4>::kCtas) paged_atte
   while (pos < end && b < p.B) {
     const int2 range = seen(p, b);
     const int u = units(p, range);
-    if (u == 0 || pos >= base + (int64_t)u * rows) {  // the next sequence (this one may have no unit)
+    if (!p.clustered && (u == 0 || pos >= base + (int64_t)u * rows)) {  // the next sequence (this one may have no unit)
       base += (int64_t)u * rows;
       ++b;
       continue;
     }
-    const int row = (int)((pos - base) / u);
-    const int k0 = (int)((pos - base) - (int64_t)row * u);
-    const int cnt = (int)min((int64_t)(u - k0), end - pos);
+    int row, k0, cnt;  // row of the sequence, first unit and units of it
+    if (p.clustered) {
+      const int rank = (int)cluster_rank();
+      row = (int)(blockIdx.x / kCluster) % rows;
+      k0 = (int)((int64_t)u * rank / kCluster);
+      cnt = (int)((int64_t)u * (rank + 1) / kCluster) - k0;
+    } else {
+      row = (int)((pos - base) / u);
+      k0 = (int)((pos - base) - (int64_t)row * u);
+      cnt = (int)min((int64_t)(u - k0), end - pos);
+    }
     const int chunk = row % p.chunks, head = row / p.chunks * p.together + mate;
     const int h0 = head * p.group + chunk * C::kHeads;
     const int nh = min(C::kHeads, p.group - chunk * C::kHeads);  // query heads of this row
@@ -612,6 +658,8 @@ __global__ void __launch_bounds__(kThreads, Cfg<DT, NT, kFp4>::kCtas) paged_atte
       }
     }
     __syncthreads();
+    float* js = ms + kWarps * C::kHeads * 2;                                 // [head] m, l of a clustered CTA
+    float* jo = js + C::kHeads * 2;                                          // [head][DT]
     const bool first = k0 == 0, last = k0 + cnt == u;
     const int64_t slot = (2 * (int64_t)blockIdx.x + (first ? 1 : 0)) * p.together;
     for (int i = tid; i < p.together * nh * (DT / 2); i += kThreads) {
@@ -628,7 +676,10 @@ __global__ void __launch_bounds__(kThreads, Cfg<DT, NT, kFp4>::kCtas) paged_atte
         x += f * v.x;
         y += f * v.y;
       }
-      if (first && last) {
+      if (p.clustered) {
+        *reinterpret_cast<float2*>(jo + h * DT + d) = make_float2(x, y);
+        if (d == 0) *reinterpret_cast<float2*>(js + 2 * h) = make_float2(M, L);
+      } else if (first && last) {
         const float f = L > 0.0f ? (kFp4 ? 0.5f * vts : 1.0f) / L : 0.0f;
         if (d < D) store_out(p, b, ho, d, x * f, y * f);
         if (d == 0 && p.lse)
@@ -638,6 +689,31 @@ __global__ void __launch_bounds__(kThreads, Cfg<DT, NT, kFp4>::kCtas) paged_atte
         *reinterpret_cast<float2*>(p.part + ((slot + w0) * C::kHeads + h) * DT + d) = make_float2(x, y);
         if (d == 0) p.stat[(slot + w0) * C::kHeads + h] = make_float2(M, L);
       }
+    }
+    if (p.clustered) {  // each CTA joins its share of the row's outputs
+      cluster_barrier();
+      for (int i = (int)cluster_rank() * kThreads + tid; i < nh * (DT / 2); i += kCluster * kThreads) {
+        const int h = i / (DT / 2), d = (i - h * (DT / 2)) * 2;
+        float2 st[kCluster], v[kCluster];
+        float M = -INFINITY, L = 0.0f, x = 0.0f, y = 0.0f;
+#pragma unroll
+        for (int q = 0; q < kCluster; ++q) st[q] = peer_load(js + 2 * h, q), v[q] = peer_load(jo + h * DT + d, q);
+#pragma unroll
+        for (int q = 0; q < kCluster; ++q) M = fmaxf(M, st[q].x);
+#pragma unroll
+        for (int q = 0; q < kCluster; ++q) {
+          const float f = M == -INFINITY ? 0.0f : exp2f(st[q].x - M);
+          L += f * st[q].y;
+          x += f * v[q].x;
+          y += f * v[q].y;
+        }
+        const float f = L > 0.0f ? (kFp4 ? 0.5f * vts : 1.0f) / L : 0.0f;
+        if (d < D) store_out(p, b, h0 + h, d, x * f, y * f);
+        if (d == 0 && p.lse)
+          p.lse[(int64_t)b * p.q_heads + h0 + h] = L > 0.0f ? (M + log2f(L) - (kFp4 ? kFp4Exp : 0.0f)) * kLn2 : -INFINITY;
+      }
+      cluster_barrier();  // no CTA leaves while others read its results
+      return;
     }
     if (tid == 0 && first && (p.by_row || !last)) {
       const int64_t x = base + (int64_t)(row + 1) * u;  // behind the row's last unit
@@ -738,6 +814,19 @@ int launch(const AttnArgs& p, int grid, cudaStream_t s) {
   static std::atomic<uint64_t> done{0};
   auto* kernel = paged_attention_kernel<DT, NT, kFp4>;
   if (!set_dynamic_smem_once(reinterpret_cast<const void*>(kernel), C::kSmem, done)) return MIXFP4_ERR_CUDA;
+  if (p.clustered) {
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = kCluster, attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(p.B * p.c.heads * p.chunks * kCluster));
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = C::kSmem;
+    cfg.stream = s;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, p) == cudaSuccess ? MIXFP4_OK : MIXFP4_ERR_CUDA;
+  }
   kernel<<<grid, kThreads, C::kSmem, s>>>(p);
   if (int st = launch_status()) return st;
   const int nh = p.group < C::kHeads ? p.group : C::kHeads, heads = kJoinThreads / 32 / p.share;
@@ -803,6 +892,11 @@ int mixfp4_paged_attention(const void* q, int64_t q_stride, int64_t q_head_strid
   p.chunks = (int)((p.group + heads - 1) / heads);
   p.c = *cache;
   p.together = together_of(cache);
+  // Few rows that cannot be long: a cluster to each, all resident at once, which joins its CTAs' parts in shared
+  // memory and so saves the second launch and its wait.
+  const int64_t bound = window > 0 && window < table_pages * cache->page_size ? window : table_pages * cache->page_size;
+  p.clustered = bound <= kClusterTokens && B * cache->heads * p.chunks * kCluster <= grid;
+  if (p.clustered) p.together = 1;
   p.page_shift = -1;
   for (int i = 0; i < 31; ++i)
     if (cache->page_size == 1 << i) p.page_shift = i;

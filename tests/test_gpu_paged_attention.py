@@ -136,6 +136,14 @@ def test_matches_the_definition(fp4, lengths, Hq, Hkv, D, page, window, layout):
     check(out, lse, q, lengths, k, v, scale, window, fp4)
     again, lse2 = o.mixfp4_paged_attention(q, cache, table, n, window=window, return_lse=True)
     assert torch.equal(out, again) and torch.equal(lse, lse2)
+    # a table with room for long sequences: the rows are then cut over the device, not over a cluster
+    wide = torch.full((len(lengths), 6000 // page + 9), -1, dtype=torch.int32, device=DEV)
+    wide[:, :table.shape[1]] = table
+    out, lse = o.mixfp4_paged_attention(q, cache, wide, n, window=window if window < 3000 else 0, return_lse=True)
+    check(out, lse, q, lengths, k, v, scale, window, fp4)
+    if window:  # a window below 4096 would bound them again: the same sequences as their last tokens alone
+        out, lse = o.mixfp4_paged_attention(q, cache, wide, n, return_lse=True)
+        check(out, lse, q, lengths, k, v, scale, 0, fp4)
 
 
 @pytest.mark.parametrize("fp4", [False, True])
