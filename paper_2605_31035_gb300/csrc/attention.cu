@@ -46,7 +46,14 @@ constexpr int kWarps = 4;
 constexpr int kThreads = kWarps * 32;
 constexpr int kJoinThreads = 256;
 constexpr int kCluster = 8;
+// Tokens up to which one cluster to a row is the quicker way, four times that where clusters fill half the device.
+// One sequence of 8 key heads of 128, clusters against shares of the whole device and a joining kernel: 4000 tokens 13
+// against 25 us, 8000 19 against 17, 32000 54 against 33; six sequences of 8000 39 against 45, of 16000 67 against 73.
 constexpr int kClusterTokens = 4096;
+// What beginning a row costs (its queries, the way to its first pages, the join of the warps), in units.  Swept, 0 / 2 /
+// 4 / 8: 256 sequences of up to 200 tokens, 8 heads of 128, 58 / 46 / 41 / 39 us; 64 of up to 8192 on a MixFP4 cache
+// 149 / 146 / 146 / 149 us.
+constexpr int kRowCost = 6;
 constexpr int kUnit = 64;  // head rows of a unit of work: 64 / together tokens of `together` key heads
 constexpr unsigned kAll = 0xFFFFFFFFu;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
@@ -105,7 +112,7 @@ struct Cfg {
   static constexpr int kScaleTile = kFp4 ? 32 * 16 : 0;                // 16 scale bytes a row at most
   static constexpr int kStage = kKTile + kVTile + kScaleTile;
   // CTAs of an SM: as many as registers and the rings' 220 KB allow
-  static constexpr int kCtas = DT == 256 ? (kFp4 ? 2 : 1) : (NT == 1 && (kFp4 || DT == 64) ? 4 : 3);
+  static constexpr int kCtas = DT == 256 ? (kFp4 ? 2 : 1) : (NT == 3 ? 2 : (NT == 1 && (kFp4 || DT == 64) ? 4 : 3));
   static constexpr int kFit = 220 * 1024 / kCtas / (kWarps * kStage);
   static constexpr int kStages = kFit < 6 ? kFit : 6;
   static constexpr int kRing = kWarps * kStages * kStage;
@@ -224,9 +231,10 @@ __device__ __forceinline__ int2 seen(const AttnArgs& p, int b) {
   const int64_t lo = p.window > 0 && n > p.window ? n - p.window : 0;
   return make_int2((int)lo, (int)n);
 }
+// Units of work of a row of the sequence: kRowCost for its beginning, then one to 64 head rows.
 __device__ __forceinline__ int units(const AttnArgs& p, int2 r) {
   const int n = kUnit / p.together;
-  return r.y > r.x ? (r.y - (r.x & ~15) + n - 1) / n : 0;
+  return r.y > r.x ? kRowCost + (r.y - (r.x & ~15) + n - 1) / n : 0;
 }
 
 // One output element pair of a finished row.
@@ -247,7 +255,7 @@ __global__ void __launch_bounds__(kThreads, Cfg<DT, NT, kFp4>::kCtas) paged_atte
   using C = Cfg<DT, NT, kFp4>;
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ int sh_b;
-  __shared__ int64_t sh_before, sh_scan[kWarps];
+  __shared__ int64_t sh_before, sh_edge[2], sh_scan[kWarps];
   griddep_launch_dependents();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
   const int D = p.c.head_dim;
@@ -295,20 +303,28 @@ __global__ void __launch_bounds__(kThreads, Cfg<DT, NT, kFp4>::kCtas) paged_atte
     }
     if (tid == 0 && !p.by_row) p.split[blockIdx.x] = make_int4(-1, 0, 0, 0);
     if ((int64_t)blockIdx.x >= grid) return;
-    pos = all * blockIdx.x / grid;
-    end = all * (blockIdx.x + 1) / grid;
-    if (pos >= before * rows && pos < (before + mine) * rows) {
-      int i = tid * strip;
-      int64_t at = before;
-      for (const int to = min(p.B, i + strip) - 1; i < to; ++i) {
-        const int u = units(p, seen(p, i));
-        if (pos < (at + u) * rows) break;
-        at += u;
+    // An edge between shares that falls into a row's beginning lies before the row.
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int64_t edge = all * (blockIdx.x + k) / grid;
+      if (edge >= before * rows && edge < (before + mine) * rows) {
+        int i = tid * strip;
+        int64_t at = before;
+        int u = units(p, seen(p, i));
+        for (const int to = min(p.B, i + strip) - 1; i < to && edge >= (at + u) * rows;) {
+          at += u;
+          u = units(p, seen(p, ++i));
+        }
+        const int64_t into = u > 0 ? (edge - at * rows) % u : 0;
+        sh_edge[k] = into <= kRowCost ? edge - into : edge;
+        if (k == 0) sh_b = i, sh_before = at;
+      } else if (edge == all && tid == 0) {
+        sh_edge[k] = all;
       }
-      sh_b = i;
-      sh_before = at;
     }
     __syncthreads();
+    pos = sh_edge[0];
+    end = sh_edge[1];
     b = sh_b;
     base = sh_before * rows;  // first unit of sequence b
   }
@@ -328,8 +344,9 @@ __global__ void __launch_bounds__(kThreads, Cfg<DT, NT, kFp4>::kCtas) paged_atte
     if (p.clustered) {
       const int rank = (int)cluster_rank();
       row = (int)(blockIdx.x / kCluster) % rows;
-      k0 = (int)((int64_t)u * rank / kCluster);
-      cnt = (int)((int64_t)u * (rank + 1) / kCluster) - k0;
+      const int tu = u - kRowCost, k1 = kRowCost + (int)((int64_t)tu * (rank + 1) / kCluster);
+      k0 = kRowCost + (int)((int64_t)tu * rank / kCluster);
+      cnt = k1 - k0;
     } else {
       row = (int)((pos - base) / u);
       k0 = (int)((pos - base) - (int64_t)row * u);
@@ -338,8 +355,8 @@ __global__ void __launch_bounds__(kThreads, Cfg<DT, NT, kFp4>::kCtas) paged_atte
     const int chunk = row % p.chunks, head = row / p.chunks * p.together + mate;
     const int h0 = head * p.group + chunk * C::kHeads;
     const int nh = min(C::kHeads, p.group - chunk * C::kHeads);  // query heads of this row
-    const int n = kUnit / p.together;
-    const int tok0 = (range.x & ~15) + k0 * n, tok1 = min(range.y, tok0 + cnt * n);
+    const int n = kUnit / p.together, from = max(k0 - kRowCost, 0), to = max(k0 + cnt - kRowCost, 0);
+    const int tok0 = (range.x & ~15) + from * n, tok1 = min(range.y, (range.x & ~15) + to * n);
 
     // ---- the queries: B fragments, thread (g, t) holding head g's dimensions of its K pieces
     uint32_t qf[NT][DT / 16][2];
@@ -730,8 +747,8 @@ __global__ void __launch_bounds__(kThreads, Cfg<DT, NT, kFp4>::kCtas) paged_atte
 // head, in turn over its parts.
 template <int DT, int NT, bool kFp4>
 __global__ void __launch_bounds__(kJoinThreads) paged_attention_join_kernel(const AttnArgs p) {
-  constexpr int kHeads = 8 * NT, kV = DT / 32, kW = kJoinThreads / 32;
-  __shared__ float red[kW][DT + 2];
+  constexpr int kHeads = 8 * NT, kV = DT / 64, kW = kJoinThreads / 32;
+  __shared__ float2 red[kW][DT / 2 + 1];
   griddep_wait();
   const int4 s = p.split[blockIdx.x];
   if (s.x < 0) return;
@@ -740,72 +757,119 @@ __global__ void __launch_bounds__(kJoinThreads) paged_attention_join_kernel(cons
   const int h0 = (s.y / p.chunks * p.together + mate) * p.group + chunk * kHeads;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int share = p.share, parts = s.w - s.z + 1;
-  {
-    const int h = blockIdx.z * (kW / share) + warp / share, ph = warp % share;
-    auto slot = [&](int i) { return ((2 * ((int64_t)s.z + i) + (i == 0 ? 1 : 0)) * p.together + mate) * kHeads + h; };
-    float M = -INFINITY, acc[kV], L = 0.0f;
+  const int h = blockIdx.z * (kW / share) + warp / share, ph = warp % share;
+  auto slot = [&](int i) { return ((2 * ((int64_t)s.z + i) + (i == 0 ? 1 : 0)) * p.together + mate) * kHeads + h; };
+  float2 acc[kV];  // dimensions 2 lane + 64 j and the next
+  float M = -INFINITY, L = 0.0f;
 #pragma unroll
-    for (int j = 0; j < kV; ++j) acc[j] = 0.0f;
-    if (h < nh) {
-      for (int i = lane; i < parts; i += 32) M = fmaxf(M, p.stat[slot(i)].x);
+  for (int j = 0; j < kV; ++j) acc[j] = make_float2(0.0f, 0.0f);
+  if (h < nh) {
+    constexpr int kAtOnce = 4;  // parts asked for at once, with their (m, l)
+    for (int i0 = ph; i0 < parts; i0 += kAtOnce * share) {
+      float2 st[kAtOnce], v[kAtOnce][kV];
 #pragma unroll
-      for (int d = 16; d; d >>= 1) M = fmaxf(M, __shfl_xor_sync(kAll, M, d));
-      if (M != -INFINITY) {
-#pragma unroll 4
-        for (int i = ph; i < parts; i += share) {
-          const float2 st = p.stat[slot(i)];
-          const float f = exp2f(st.x - M);
-          L += f * st.y;
-          const float* o = p.part + slot(i) * DT + lane;
+      for (int a = 0; a < kAtOnce; ++a) {
+        const int i = i0 + a * share;
+        st[a] = make_float2(-INFINITY, 0.0f);
 #pragma unroll
-          for (int j = 0; j < kV; ++j) acc[j] += f * o[32 * j];
+        for (int j = 0; j < kV; ++j) v[a][j] = make_float2(0.0f, 0.0f);
+        if (i < parts) {
+          st[a] = p.stat[slot(i)];
+          const float2* o = reinterpret_cast<const float2*>(p.part + slot(i) * DT) + lane;
+#pragma unroll
+          for (int j = 0; j < kV; ++j) v[a][j] = o[32 * j];
         }
       }
-    }
+      float top = M;
 #pragma unroll
-    for (int j = 0; j < kV; ++j) red[warp][lane + 32 * j] = acc[j];
-    if (lane == 0) red[warp][DT] = L;
-    __syncthreads();
-    if (h < nh && ph == 0) {
-      L = 0.0f;
-      for (int w = 0; w < share; ++w) L += red[warp + w][DT];
-      const float f = L > 0.0f ? (kFp4 ? 0.5f * *p.c.v_ts : 1.0f) / L : 0.0f;
-      for (int d = 2 * lane; d < p.c.head_dim; d += 64) {
-        float x = 0.0f, y = 0.0f;
-        for (int w = 0; w < share; ++w) x += red[warp + w][d], y += red[warp + w][d + 1];
-        store_out(p, s.x, h0 + h, d, x * f, y * f);
+      for (int a = 0; a < kAtOnce; ++a) top = fmaxf(top, st[a].x);
+      if (top == -INFINITY) continue;
+      const float old = exp2f(M - top);
+      M = top;
+      L *= old;
+#pragma unroll
+      for (int j = 0; j < kV; ++j) acc[j].x *= old, acc[j].y *= old;
+#pragma unroll
+      for (int a = 0; a < kAtOnce; ++a) {
+        const float f = exp2f(st[a].x - M);
+        L += f * st[a].y;
+#pragma unroll
+        for (int j = 0; j < kV; ++j) acc[j].x += f * v[a][j].x, acc[j].y += f * v[a][j].y;
       }
-      if (lane == 0 && p.lse)
-        p.lse[(int64_t)s.x * p.q_heads + h0 + h] =
-            L > 0.0f ? (M + log2f(L) - (kFp4 ? kFp4Exp : 0.0f)) * kLn2 : -INFINITY;
     }
   }
+  if (share > 1) {  // the first of a head's warps adds the others' sums
+#pragma unroll
+    for (int j = 0; j < kV; ++j) red[warp][lane + 32 * j] = acc[j];
+    if (lane == 0) red[warp][DT / 2] = make_float2(M, L);
+    __syncthreads();
+    if (ph != 0) return;
+    float top = M;
+    for (int w = 1; w < share; ++w) top = fmaxf(top, red[warp + w][DT / 2].x);
+    if (top != -INFINITY) {
+      const float old = exp2f(M - top);
+      L *= old;
+#pragma unroll
+      for (int j = 0; j < kV; ++j) acc[j].x *= old, acc[j].y *= old;
+      for (int w = 1; w < share; ++w) {
+        const float2 st = red[warp + w][DT / 2];
+        const float f = exp2f(st.x - top);
+        L += f * st.y;
+#pragma unroll
+        for (int j = 0; j < kV; ++j) {
+          const float2 v = red[warp + w][lane + 32 * j];
+          acc[j].x += f * v.x, acc[j].y += f * v.y;
+        }
+      }
+      M = top;
+    }
+  }
+  if (h >= nh) return;
+  const float f = L > 0.0f ? (kFp4 ? 0.5f * *p.c.v_ts : 1.0f) / L : 0.0f;
+#pragma unroll
+  for (int j = 0; j < kV; ++j) {
+    const int d = 2 * lane + 64 * j;
+    if (d < p.c.head_dim) store_out(p, s.x, h0 + h, d, acc[j].x * f, acc[j].y * f);
+  }
+  if (lane == 0 && p.lse)
+    p.lse[(int64_t)s.x * p.q_heads + h0 + h] = L > 0.0f ? (M + log2f(L) - (kFp4 ? kFp4Exp : 0.0f)) * kLn2 : -INFINITY;
 }
 
 inline bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 inline int launch_status() { return cudaGetLastError() == cudaSuccess ? MIXFP4_OK : MIXFP4_ERR_CUDA; }
 
 inline int padded_dim(int D) { return D <= 64 ? 64 : (D <= 128 ? 128 : 256); }
-inline int padded_heads(int64_t group) { return group <= 8 ? 8 : 16; }
+// Query heads of a row: 24 hold registers for rows of up to 128 dimensions only, and pay where 16 would read the
+// cache twice (24 heads to a key head).
+inline int padded_heads(const mixfp4_kv_cache* c, int64_t q_heads) {
+  const int64_t group = q_heads / c->heads;
+  return group <= 8 ? 8 : (group <= 16 || c->head_dim > 128 || (group + 15) / 16 == (group + 23) / 24 ? 16 : 24);
+}
 // Key heads of a CTA.  Where the heads of a token lie together, neighbouring heads' rows are asked for at the same
 // time (64 sequences of up to 8192 tokens, 8 heads of 128: MixFP4 162 us against 185 us with one head to a CTA, whose
 // 8 scale bytes of a row cost a whole access; 32 bf16 heads of 128: 91 against 111 us).  Where a head's tokens lie
-// together that gains nothing, and one head to a CTA leaves fewer parts to join (2 sequences of 131072: 175 us
-// against 188).
-inline int together_of(const mixfp4_kv_cache* c) {
+// together that gains nothing, and with few rows one head to a CTA leaves fewer parts of each to join (2 sequences of
+// 131072: 175 us against 188).
+inline int together_of(const mixfp4_kv_cache* c, int64_t B, int64_t chunks, int grid) {
   if (c->head_stride >= c->token_stride) return 1;
-  return c->heads % 4 == 0 ? 4 : (c->heads % 2 == 0 ? 2 : 1);
+  for (int n = 4; n > 1; n /= 2)
+    if (c->heads % n == 0 && B * (c->heads / n) * chunks >= grid / 4) return n;
+  return 1;
 }
 // CTAs of the first kernel.
-template <int DT>
-int ctas_of(bool fp4, bool wide) {
-  return fp4 ? (wide ? Cfg<DT, 2, true>::kCtas : Cfg<DT, 1, true>::kCtas)
-             : (wide ? Cfg<DT, 2, false>::kCtas : Cfg<DT, 1, false>::kCtas);
+template <int DT, bool kFp4>
+int ctas_of(int heads) {
+  if constexpr (DT <= 128)
+    if (heads == 24) return Cfg<DT, 3, kFp4>::kCtas;
+  return heads == 8 ? Cfg<DT, 1, kFp4>::kCtas : Cfg<DT, 2, kFp4>::kCtas;
+}
+template <bool kFp4>
+int ctas_of(int dim, int heads) {
+  return dim == 64 ? ctas_of<64, kFp4>(heads) : (dim == 128 ? ctas_of<128, kFp4>(heads) : ctas_of<256, kFp4>(heads));
 }
 inline int grid_of(const mixfp4_kv_cache* c, int64_t q_heads) {
-  const bool fp4 = c->dtype == MIXFP4_CACHE_MIXFP4, wide = padded_heads(q_heads / c->heads) > 8;
-  const int d = padded_dim(c->head_dim);
-  return num_sms() * (d == 64 ? ctas_of<64>(fp4, wide) : (d == 128 ? ctas_of<128>(fp4, wide) : ctas_of<256>(fp4, wide)));
+  const int dim = padded_dim(c->head_dim), heads = padded_heads(c, q_heads);
+  return num_sms() * (c->dtype == MIXFP4_CACHE_MIXFP4 ? ctas_of<true>(dim, heads) : ctas_of<false>(dim, heads));
 }
 
 template <int DT, int NT, bool kFp4>
@@ -837,16 +901,18 @@ int launch(const AttnArgs& p, int grid, cudaStream_t s) {
 }
 
 template <int DT, bool kFp4>
-int launch_heads(const AttnArgs& p, int grid, cudaStream_t s) {
-  return padded_heads(p.group) == 8 ? launch<DT, 1, kFp4>(p, grid, s) : launch<DT, 2, kFp4>(p, grid, s);
+int launch_heads(const AttnArgs& p, int grid, int heads, cudaStream_t s) {
+  if constexpr (DT <= 128)
+    if (heads == 24) return launch<DT, 3, kFp4>(p, grid, s);
+  return heads == 8 ? launch<DT, 1, kFp4>(p, grid, s) : launch<DT, 2, kFp4>(p, grid, s);
 }
 
 template <bool kFp4>
-int launch_dim(const AttnArgs& p, int grid, cudaStream_t s) {
+int launch_dim(const AttnArgs& p, int grid, int heads, cudaStream_t s) {
   switch (padded_dim(p.c.head_dim)) {
-    case 64: return launch_heads<64, kFp4>(p, grid, s);
-    case 128: return launch_heads<128, kFp4>(p, grid, s);
-    default: return launch_heads<256, kFp4>(p, grid, s);
+    case 64: return launch_heads<64, kFp4>(p, grid, heads, s);
+    case 128: return launch_heads<128, kFp4>(p, grid, heads, s);
+    default: return launch_heads<256, kFp4>(p, grid, heads, s);
   }
 }
 
@@ -862,7 +928,7 @@ int mixfp4_paged_attention_workspace(const mixfp4_kv_cache* cache, int64_t B, in
   if (B < 0 || q_heads < 0 || q_heads % cache->heads != 0) return MIXFP4_ERR_SHAPE;
   *bytes = 0;
   if (B == 0 || q_heads == 0) return MIXFP4_OK;
-  const int64_t grid = grid_of(cache, q_heads), heads = padded_heads(q_heads / cache->heads) * together_of(cache);
+  const int64_t grid = grid_of(cache, q_heads), heads = padded_heads(cache, q_heads) * 4;  // at most 4 together
   *bytes = (grid * 16 + 255) / 256 * 256 + 2 * grid * heads * 8 + 2 * grid * heads * padded_dim(cache->head_dim) * 4;
   return MIXFP4_OK;
 }
@@ -884,18 +950,19 @@ int mixfp4_paged_attention(const void* q, int64_t q_stride, int64_t q_head_strid
       !aligned(out, 16) || !aligned(lse, 4) || !aligned(workspace, 256))
     return MIXFP4_ERR_ALIGN;
   const int grid = grid_of(cache, q_heads);
-  const int64_t heads = padded_heads(q_heads / cache->heads);
+  const int heads = padded_heads(cache, q_heads);
   AttnArgs p = {};
   p.q = static_cast<const uint16_t*>(q);
   p.q_stride = q_stride, p.q_head_stride = q_head_stride;
   p.B = (int)B, p.q_heads = (int)q_heads, p.group = (int)(q_heads / cache->heads);
   p.chunks = (int)((p.group + heads - 1) / heads);
   p.c = *cache;
-  p.together = together_of(cache);
+  p.together = together_of(cache, B, p.chunks, grid);
   // Few rows that cannot be long: a cluster to each, all resident at once, which joins its CTAs' parts in shared
   // memory and so saves the second launch and its wait.
   const int64_t bound = window > 0 && window < table_pages * cache->page_size ? window : table_pages * cache->page_size;
-  p.clustered = bound <= kClusterTokens && B * cache->heads * p.chunks * kCluster <= grid;
+  const int64_t in_clusters = B * cache->heads * p.chunks * kCluster;
+  p.clustered = in_clusters <= grid && bound <= (in_clusters >= grid / 2 ? 4 : 1) * kClusterTokens;
   if (p.clustered) p.together = 1;
   p.page_shift = -1;
   for (int i = 0; i < 31; ++i)
@@ -919,7 +986,7 @@ int mixfp4_paged_attention(const void* q, int64_t q_stride, int64_t q_head_strid
   p.stat = reinterpret_cast<float2*>(w);
   p.part = reinterpret_cast<float*>(w + 2 * (int64_t)grid * p.together * heads * 8);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  return cache->dtype == MIXFP4_CACHE_MIXFP4 ? launch_dim<true>(p, grid, s) : launch_dim<false>(p, grid, s);
+  return cache->dtype == MIXFP4_CACHE_MIXFP4 ? launch_dim<true>(p, grid, heads, s) : launch_dim<false>(p, grid, heads, s);
 }
 
 }  // extern "C"

@@ -108,6 +108,8 @@ CASES = [
     (False, [250, 1111], 16, 16, 80, 16, 0, "nhd"),
     (False, [100, 900], 8, 1, 256, 32, 0, "nhd"),
     (False, [50], 40, 2, 192, 16, 0, "kv"),
+    (False, [200, 31], 71, 1, 64, 16, 0, "nhd"),
+    (False, [200, 31], 32, 1, 128, 16, 0, "nhd"),
     (False, [5000, 10, 100], 9, 3, 96, 16, 7, "nhd"),     # windows that start and end inside pages
     (False, [5000, 10, 100], 12, 4, 128, 32, 1000, "hnd"),
     (False, [40, 3], 2, 2, 64, 16, 1, "nhd"),
@@ -121,6 +123,8 @@ CASES = [
     (True, [100, 900], 8, 1, 256, 32, 0, "nhd"),
     (True, [100, 900], 20, 1, 256, 32, 50, "nhd"),
     (True, [50], 40, 2, 192, 16, 0, "kv"),
+    (True, [200, 31], 71, 1, 64, 16, 0, "nhd"),
+    (True, [200, 31], 18, 1, 112, 16, 0, "nhd"),
     (True, [5000, 10, 100], 9, 3, 96, 16, 7, "nhd"),
 ]
 
