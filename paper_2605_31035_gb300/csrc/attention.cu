@@ -60,6 +60,7 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // How far a score may lie above the m of its weight 2^(s - m).  On a MixFP4 cache the weights are 2^7 times that:
 // below 2^15 in f16, whose least value is then 2^-31 of the weight at m.
 constexpr float kSlack = 8.0f, kFp4Exp = 7.0f;
+constexpr float kNoScore = -3e38f;  // m where no token has been seen: no difference to a score or to itself is NaN
 
 struct AttnArgs {
   const uint16_t* q;
@@ -507,7 +508,7 @@ __global__ void __launch_bounds__(kThreads, Cfg<DT, NT, kFp4>::kCtas) paged_atte
     float m[NT][2], l[NT][2];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-      m[n][0] = m[n][1] = -INFINITY;
+      m[n][0] = m[n][1] = kNoScore;
       l[n][0] = l[n][1] = 0.0f;
 #pragma unroll
       for (int i = 0; i < DT / 16; ++i) o[n][i][0] = o[n][i][1] = o[n][i][2] = o[n][i][3] = 0.0f;
@@ -574,7 +575,6 @@ __global__ void __launch_bounds__(kThreads, Cfg<DT, NT, kFp4>::kCtas) paged_atte
             v = fmaxf(v, __shfl_xor_sync(kAll, v, 16));
             v = fmaxf(m[n][j], v);
             cor[j] = ex2(m[n][j] - v);  // 0 at the first score
-            if (v == -INFINITY) cor[j] = 1.0f;
             m[n][j] = v;
             l[n][j] *= cor[j];
           }
@@ -586,7 +586,7 @@ __global__ void __launch_bounds__(kThreads, Cfg<DT, NT, kFp4>::kCtas) paged_atte
         float w[4];
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-          const float top = (m[n][j] == -INFINITY ? 0.0f : m[n][j]) - (kFp4 ? kFp4Exp : 0.0f);
+          const float top = m[n][j] - (kFp4 ? kFp4Exp : 0.0f);
           w[j] = ex2(s[n][j] - top);
           w[2 + j] = ex2(s[n][2 + j] - top);
           l[n][j] += w[j] + w[2 + j];
@@ -683,11 +683,11 @@ __global__ void __launch_bounds__(kThreads, Cfg<DT, NT, kFp4>::kCtas) paged_atte
       const int hh = i / (DT / 2), d = (i - hh * (DT / 2)) * 2;
       const int w0 = hh / nh, h = hh - w0 * nh;  // key head of the CTA, query head of it
       const int ho = (row / p.chunks * p.together + w0) * p.group + chunk * C::kHeads + h;
-      float M = -INFINITY, L = 0.0f;
+      float M = kNoScore, L = 0.0f;
       for (int w = w0; w < kWarps; w += p.together) M = fmaxf(M, ms[(w * C::kHeads + h) * 2]);
       float x = 0.0f, y = 0.0f;
       for (int w = w0; w < kWarps; w += p.together) {
-        const float f = M == -INFINITY ? 0.0f : exp2f(ms[(w * C::kHeads + h) * 2] - M);
+        const float f = exp2f(ms[(w * C::kHeads + h) * 2] - M);
         const float2 v = *reinterpret_cast<const float2*>(mo + (w * C::kHeads + h) * DT + d);
         L += f * ms[(w * C::kHeads + h) * 2 + 1];
         x += f * v.x;
@@ -712,14 +712,14 @@ __global__ void __launch_bounds__(kThreads, Cfg<DT, NT, kFp4>::kCtas) paged_atte
       for (int i = (int)cluster_rank() * kThreads + tid; i < nh * (DT / 2); i += kCluster * kThreads) {
         const int h = i / (DT / 2), d = (i - h * (DT / 2)) * 2;
         float2 st[kCluster], v[kCluster];
-        float M = -INFINITY, L = 0.0f, x = 0.0f, y = 0.0f;
+        float M = kNoScore, L = 0.0f, x = 0.0f, y = 0.0f;
 #pragma unroll
         for (int q = 0; q < kCluster; ++q) st[q] = peer_load(js + 2 * h, q), v[q] = peer_load(jo + h * DT + d, q);
 #pragma unroll
         for (int q = 0; q < kCluster; ++q) M = fmaxf(M, st[q].x);
 #pragma unroll
         for (int q = 0; q < kCluster; ++q) {
-          const float f = M == -INFINITY ? 0.0f : exp2f(st[q].x - M);
+          const float f = exp2f(st[q].x - M);
           L += f * st[q].y;
           x += f * v[q].x;
           y += f * v[q].y;
@@ -760,7 +760,7 @@ __global__ void __launch_bounds__(kJoinThreads) paged_attention_join_kernel(cons
   const int h = blockIdx.z * (kW / share) + warp / share, ph = warp % share;
   auto slot = [&](int i) { return ((2 * ((int64_t)s.z + i) + (i == 0 ? 1 : 0)) * p.together + mate) * kHeads + h; };
   float2 acc[kV];  // dimensions 2 lane + 64 j and the next
-  float M = -INFINITY, L = 0.0f;
+  float M = kNoScore, L = 0.0f;
 #pragma unroll
   for (int j = 0; j < kV; ++j) acc[j] = make_float2(0.0f, 0.0f);
   if (h < nh) {
@@ -770,7 +770,7 @@ __global__ void __launch_bounds__(kJoinThreads) paged_attention_join_kernel(cons
 #pragma unroll
       for (int a = 0; a < kAtOnce; ++a) {
         const int i = i0 + a * share;
-        st[a] = make_float2(-INFINITY, 0.0f);
+        st[a] = make_float2(kNoScore, 0.0f);
 #pragma unroll
         for (int j = 0; j < kV; ++j) v[a][j] = make_float2(0.0f, 0.0f);
         if (i < parts) {
@@ -783,7 +783,6 @@ __global__ void __launch_bounds__(kJoinThreads) paged_attention_join_kernel(cons
       float top = M;
 #pragma unroll
       for (int a = 0; a < kAtOnce; ++a) top = fmaxf(top, st[a].x);
-      if (top == -INFINITY) continue;
       const float old = exp2f(M - top);
       M = top;
       L *= old;
@@ -806,23 +805,21 @@ __global__ void __launch_bounds__(kJoinThreads) paged_attention_join_kernel(cons
     if (ph != 0) return;
     float top = M;
     for (int w = 1; w < share; ++w) top = fmaxf(top, red[warp + w][DT / 2].x);
-    if (top != -INFINITY) {
-      const float old = exp2f(M - top);
-      L *= old;
+    const float old = exp2f(M - top);
+    L *= old;
 #pragma unroll
-      for (int j = 0; j < kV; ++j) acc[j].x *= old, acc[j].y *= old;
-      for (int w = 1; w < share; ++w) {
-        const float2 st = red[warp + w][DT / 2];
-        const float f = exp2f(st.x - top);
-        L += f * st.y;
+    for (int j = 0; j < kV; ++j) acc[j].x *= old, acc[j].y *= old;
+    for (int w = 1; w < share; ++w) {
+      const float2 st = red[warp + w][DT / 2];
+      const float f = exp2f(st.x - top);
+      L += f * st.y;
 #pragma unroll
-        for (int j = 0; j < kV; ++j) {
-          const float2 v = red[warp + w][lane + 32 * j];
-          acc[j].x += f * v.x, acc[j].y += f * v.y;
-        }
+      for (int j = 0; j < kV; ++j) {
+        const float2 v = red[warp + w][lane + 32 * j];
+        acc[j].x += f * v.x, acc[j].y += f * v.y;
       }
-      M = top;
     }
+    M = top;
   }
   if (h >= nh) return;
   const float f = L > 0.0f ? (kFp4 ? 0.5f * *p.c.v_ts : 1.0f) / L : 0.0f;

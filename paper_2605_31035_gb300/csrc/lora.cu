@@ -274,11 +274,11 @@ __global__ void __launch_bounds__(kThreads, 2) lora_shrink_kernel(const ShrinkAr
 
 // ---- expand: out[t][n] = base[t][n] + factor_a sum_r u[t][r] W_a[n][r] -----------------------------
 // Tokens are the rows of the products (16), features their columns: product j
-// of a warp's 64 features has column c at feature 8 c + j, so that thread
-// (g, t) ends with features 16 t .. 16 t + 15 of tokens g and g + 8, 64 bytes
-// of a row.  A step covers 16 ranks, thread t holding 4 t .. 4 t + 3.  The
-// CTA's warps share the tokens: u is cut into its three parts once, in shared
-// memory as the fragments they read.
+// of a warp's 8 NP features has column c at feature NP c + j, so that thread
+// (g, t) ends with features 2 NP t .. of tokens g and g + 8, which it reads and
+// writes 32 bytes at a time.  A step covers 16 ranks, thread t holding
+// 4 t .. 4 t + 3.  The CTA's warps share the tokens: u is cut into its three
+// parts once, in shared memory as the fragments they read.
 struct ExpandArgs {
   const float* u;      // [tokens][R]
   const uint16_t* w;   // [adapters][N][R], or kTrans: [adapters][R][N]
@@ -292,52 +292,56 @@ struct ExpandArgs {
   Segments seg;
 };
 
-// The B fragments of 16 ranks for the warp's 64 features.
-template <bool kTrans>
-__device__ __forceinline__ void expand_w(uint32_t b[8][2], const uint16_t* w, int r, int R, int64_t n, int64_t N) {
+// The B fragments of 16 ranks for the warp's features; n: the thread's first (NP g on).
+template <bool kTrans, int NP>
+__device__ __forceinline__ void expand_w(uint32_t b[NP][2], const uint16_t* w, int r, int R, int64_t n, int64_t N) {
   const bool in_r = r < R;
   if (!kTrans) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
+    for (int j = 0; j < NP; ++j) {
       const uint2 q = in_r && n + j < N ? *reinterpret_cast<const uint2*>(w + (n + j) * R + r) : make_uint2(0, 0);
       b[j][0] = q.x, b[j][1] = q.y;
     }
   } else {
-    uint32_t q[4][4];
+    uint2 q[NP / 4][4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const uint4 x = in_r && n < N ? *reinterpret_cast<const uint4*>(w + (int64_t)(r + i) * N + n)
-                                    : make_uint4(0, 0, 0, 0);
-      q[i][0] = x.x, q[i][1] = x.y, q[i][2] = x.z, q[i][3] = x.w;
-    }
+    for (int k = 0; k < NP / 4; ++k)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      b[2 * i][0] = prmt(q[0][i], q[1][i], 0x5410u), b[2 * i + 1][0] = prmt(q[0][i], q[1][i], 0x7632u);
-      b[2 * i][1] = prmt(q[2][i], q[3][i], 0x5410u), b[2 * i + 1][1] = prmt(q[2][i], q[3][i], 0x7632u);
-    }
+      for (int i = 0; i < 4; ++i)
+        q[k][i] = in_r && n < N ? *reinterpret_cast<const uint2*>(w + (int64_t)(r + i) * N + n + 4 * k)
+                                : make_uint2(0, 0);
+#pragma unroll
+    for (int k = 0; k < NP / 4; ++k)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        b[4 * k][h] = prmt(q[k][2 * h].x, q[k][2 * h + 1].x, 0x5410u);
+        b[4 * k + 1][h] = prmt(q[k][2 * h].x, q[k][2 * h + 1].x, 0x7632u);
+        b[4 * k + 2][h] = prmt(q[k][2 * h].y, q[k][2 * h + 1].y, 0x5410u);
+        b[4 * k + 3][h] = prmt(q[k][2 * h].y, q[k][2 * h + 1].y, 0x7632u);
+      }
   }
 }
 
 // kHeld: steps (of 16 ranks) whose part of W a warp keeps in registers for all its tokens; further ranks are read
 // again for every 16 tokens.
-template <int TT, bool kTrans, int kHeld>
-__global__ void __launch_bounds__(kThreads, kHeld > 2 ? 1 : 2) lora_expand_kernel(const ExpandArgs p) {
+template <int TT, bool kTrans, int kHeld, int NP>
+__global__ void __launch_bounds__(kThreads, 2) lora_expand_kernel(const ExpandArgs p) {
   extern __shared__ uint4 frag[];  // [m][step][part][lane]
-  griddep_launch_dependents();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
   const Tile tile = find_tile<TT>(p.seg, (int)blockIdx.x);
   const int steps = (p.R + 15) / 16;
-  const int64_t n0 = ((int64_t)blockIdx.y * kWarps + warp) * 64;
+  const int64_t n0 = ((int64_t)blockIdx.y * kWarps + warp) * (8 * NP);
   const uint16_t* w = p.w + (int64_t)max(tile.adapter, 0) * p.R * p.N;
   const bool some = tile.t0 < tile.t1 && tile.adapter >= 0;
-  uint32_t held[kHeld][8][2];
+  uint32_t held[kHeld][NP][2];
 #pragma unroll
   for (int st = 0; st < kHeld; ++st)
-    expand_w<kTrans>(held[st], w, some ? st * 16 + 4 * t : p.R, p.R, n0 + 8 * g, p.N);
+    expand_w<kTrans, NP>(held[st], w, some ? st * 16 + 4 * t : p.R, p.R, n0 + NP * g, p.N);
   griddep_wait();
+  griddep_launch_dependents();  // not before: what may start then counts on the kernel before this one
   if (tile.t0 >= tile.t1) return;
   if (tile.adapter >= 0)
-    for (int i = threadIdx.x; i < (TT / 16) * steps * 32; i += kThreads) {
+    for (int i = threadIdx.x; i < (tile.t1 - tile.t0 + 15) / 16 * steps * 32; i += kThreads) {
       const int ms = i / 32, m = ms / steps, l = i % 32;
       const int r = (ms - m * steps) * 16 + 4 * (l & 3), ta = tile.t0 + 16 * m + (l >> 2);
       const float4 z = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
@@ -355,33 +359,33 @@ __global__ void __launch_bounds__(kThreads, kHeld > 2 ? 1 : 2) lora_expand_kerne
   __syncthreads();
   if (n0 >= p.N) return;
   const float f = tile.adapter < 0 ? 0.0f : (p.factor ? p.factor[tile.adapter] : 1.0f);
-  const int64_t nt = n0 + 16 * t;  // this thread's results
-  const bool vec = p.vec && nt + 16 <= p.N;
+  const int64_t nt = n0 + 2 * NP * t;  // this thread's results
+  const bool vec = p.vec && nt + 2 * NP <= p.N;
   for (int m = 0; tile.t0 + 16 * m < tile.t1; ++m) {
     const int ta = tile.t0 + 16 * m + g;
-    float v[2][16];
+    float v[2][2 * NP];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const float* b = p.base + (int64_t)(ta + 8 * h) * p.ld_base + nt;
       const bool there = p.base && ta + 8 * h < tile.t1;
       if (vec) {
-        load32(reinterpret_cast<uint32_t*>(v[h]), b, there);
-        load32(reinterpret_cast<uint32_t*>(v[h] + 8), b + 8, there);
+#pragma unroll
+        for (int q = 0; q < 2 * NP; q += 8) load32(reinterpret_cast<uint32_t*>(v[h] + q), b + q, there);
       } else {
 #pragma unroll
-        for (int q = 0; q < 16; ++q) v[h][q] = there && nt + q < p.N ? b[q] : 0.0f;
+        for (int q = 0; q < 2 * NP; ++q) v[h][q] = there && nt + q < p.N ? b[q] : 0.0f;
       }
     }
-    float acc[8][4];
+    float acc[NP][4];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.0f;
+    for (int j = 0; j < NP; ++j) acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.0f;
     if (tile.adapter >= 0) {
-      auto multiply = [&](int st, const uint32_t(&b)[8][2]) {
+      auto multiply = [&](int st, const uint32_t(&b)[NP][2]) {
 #pragma unroll
         for (int i = 2; i >= 0; --i) {  // the small parts first
           const uint4 a = frag[((m * steps + st) * 3 + i) * 32 + lane];
 #pragma unroll
-          for (int j = 0; j < 8; ++j) mma_bf16(acc[j], a.x, a.y, a.z, a.w, b[j][0], b[j][1]);
+          for (int j = 0; j < NP; ++j) mma_bf16(acc[j], a.x, a.y, a.z, a.w, b[j][0], b[j][1]);
         }
       };
 #pragma unroll
@@ -389,24 +393,24 @@ __global__ void __launch_bounds__(kThreads, kHeld > 2 ? 1 : 2) lora_expand_kerne
         if (st < steps) multiply(st, held[st]);
       if (kHeld == 4)
         for (int st = kHeld; st < steps; ++st) {
-          uint32_t b[8][2];
-          expand_w<kTrans>(b, w, st * 16 + 4 * t, p.R, n0 + 8 * g, p.N);
+          uint32_t b[NP][2];
+          expand_w<kTrans, NP>(b, w, st * 16 + 4 * t, p.R, n0 + NP * g, p.N);
           multiply(st, b);
         }
     }
-    // acc[j]: (token g, features 16 t + j and 16 t + 8 + j), then token g + 8
+    // acc[j]: (token g, features 2 NP t + j and 2 NP t + NP + j), then token g + 8
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       if (ta + 8 * h >= tile.t1) continue;
 #pragma unroll
-      for (int q = 0; q < 16; ++q) v[h][q] = fmaf(f, acc[q & 7][2 * h + (q >> 3)], v[h][q]);
+      for (int q = 0; q < 2 * NP; ++q) v[h][q] = fmaf(f, acc[q % NP][2 * h + q / NP], v[h][q]);
       float* o = p.out + (int64_t)(ta + 8 * h) * p.ld_out + nt;
       if (vec) {
-        stg256(o, reinterpret_cast<const uint32_t*>(v[h]));
-        stg256(o + 8, reinterpret_cast<const uint32_t*>(v[h] + 8));
+#pragma unroll
+        for (int q = 0; q < 2 * NP; q += 8) stg256(o + q, reinterpret_cast<const uint32_t*>(v[h] + q));
       } else {
 #pragma unroll
-        for (int q = 0; q < 16; ++q)
+        for (int q = 0; q < 2 * NP; ++q)
           if (nt + q < p.N) o[q] = v[h][q];
       }
     }
@@ -429,6 +433,7 @@ struct GradArgs {
   int64_t dim[2];          // K, N
   int blocks[2];           // 64-feature blocks of each
   int R;
+  int beside;              // the kernel before this one on the stream writes nothing that is read here
   Segments seg;
 };
 
@@ -439,7 +444,9 @@ __global__ void __launch_bounds__(32 * NW, NW == 8 ? 1 : (RT == 4 ? 2 : 3)) lora
   extern __shared__ float4 sums[];  // [half the warps][tile][product][lane]
   constexpr int threads = 32 * NW, warps = NW;
   __shared__ int ends[threads], first[threads], count[warps], found[warps];
-  griddep_wait();
+  // Beside the expansion of v, which lets this kernel start when v is there, it waits at its end instead: the stream's
+  // next kernel counts on both.
+  if (!p.beside) griddep_wait();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
   const int which = (int)blockIdx.x >= p.blocks[0];
   const int64_t n0 = (int64_t)((int)blockIdx.x - (which ? p.blocks[0] : 0)) * 64;
@@ -581,6 +588,7 @@ __global__ void __launch_bounds__(32 * NW, NW == 8 ? 1 : (RT == 4 ? 2 : 3)) lora
     }
   }
   // acc[h][j]: ranks 2 RT g + 2 h (+ 1 for registers 2, 3), features 16 t + j (+ 8 for registers 1, 3)
+  if (p.beside) griddep_wait();
   if (warp > 0 || n0 + 16 * t >= N || !in_r) return;
   const float f = p.factor[which] ? p.factor[which][adapter] : 1.0f;
   if (!which) {  // rows of features
@@ -649,27 +657,34 @@ int shrink(ShrinkArgs p, bool dependent, cudaStream_t s) {
   return rt == 1 ? launch_shrink<1, 32, kTrans>(p, dependent, s) : launch_shrink<2, 32, kTrans>(p, dependent, s);
 }
 
-template <int TT, bool kTrans, int kHeld>
+template <int TT, bool kTrans, int kHeld, int NP>
 int launch_expand(const ExpandArgs& p, cudaStream_t s) {
   constexpr int kStep = TT / 16 * 3 * 512, kMost = 8 * kStep;  // fragments of 16 ranks, of 128
-  auto* kernel = lora_expand_kernel<TT, kTrans, kHeld>;
+  auto* kernel = lora_expand_kernel<TT, kTrans, kHeld, NP>;
   static std::atomic<uint64_t> done{0};
   if (!set_dynamic_smem_once(reinterpret_cast<const void*>(kernel), kMost, done)) return MIXFP4_ERR_CUDA;
-  const dim3 grid((unsigned)(p.seg.tokens / TT + p.seg.count), (unsigned)((p.N + 64 * kWarps - 1) / (64 * kWarps)));
+  const dim3 grid((unsigned)(p.seg.tokens / TT + p.seg.count), (unsigned)((p.N + 8 * NP * kWarps - 1) / (8 * NP * kWarps)));
   return launch_pdl(kernel, grid, dim3(kThreads), (size_t)((p.R + 15) / 16 * kStep), s, p) == cudaSuccess
              ? MIXFP4_OK
              : MIXFP4_ERR_CUDA;
 }
 
+// Up to 32 ranks a warp takes 64 features (2999 tokens, rank 32, 14336 features: 63 us against 73 us with 32), beyond
+// that 32, whose part of W leaves registers for twice the warps (4096 tokens, rank 64, 4096 features: 41 against 47 us).
 template <int TT, bool kTrans>
 int expand_held(const ExpandArgs& p, cudaStream_t s) {
-  if (p.R <= 16) return launch_expand<TT, kTrans, 1>(p, s);
-  return p.R <= 32 ? launch_expand<TT, kTrans, 2>(p, s) : launch_expand<TT, kTrans, 4>(p, s);
+  if (p.R <= 16) return launch_expand<TT, kTrans, 1, 8>(p, s);
+  return p.R <= 32 ? launch_expand<TT, kTrans, 2, 8>(p, s) : launch_expand<TT, kTrans, 4, 4>(p, s);
 }
 
+// Tokens of a CTA (W is read, and u cut, once a CTA): no more than most segments have, and no more than leave the
+// device a round of CTAs.
 template <bool kTrans>
 int expand(const ExpandArgs& p, cudaStream_t s) {
-  return p.seg.tokens <= 16 * (int64_t)p.seg.count ? expand_held<16, kTrans>(p, s) : expand_held<64, kTrans>(p, s);
+  const int64_t features = (p.R <= 32 ? 64 : 32) * kWarps, blocks = (p.N + features - 1) / features;
+  const int64_t T = p.seg.tokens, S = p.seg.count;
+  auto fits = [&](int tokens) { return T >= tokens / 2 * S && (T / tokens + S / 2) * blocks >= 2 * num_sms(); };
+  return fits(64) ? expand_held<64, kTrans>(p, s) : expand_held<16, kTrans>(p, s);
 }
 
 template <int RT, int NW>
@@ -772,6 +787,7 @@ int mixfp4_lora_backward(const void* dy, int64_t ldy, const void* x, int64_t ldx
   gp.R = (int)R;
   gp.seg = seg;
   if (!tokens) gp.seg.count = 0;
+  gp.beside = tokens && K > 0;
   if (adapters == 0 || K + N == 0) return MIXFP4_OK;
   return R <= 16 ? grad<1>(gp, s) : (R <= 32 ? grad<2>(gp, s) : grad<4>(gp, s));
 }
