@@ -111,11 +111,13 @@ struct Cfg {
   }
   static constexpr int kKTile = 16 * kRow, kVTile = 16 * kRow;
   static constexpr int kScaleTile = kFp4 ? 32 * 16 : 0;                // 16 scale bytes a row at most
-  static constexpr int kStage = kKTile + kVTile + kScaleTile;
+  static constexpr int kThere = kKTile + kVTile + kScaleTile;          // which of the tile's tokens there are, a bit each
+  static constexpr int kStage = kThere + 128;
   // CTAs of an SM: as many as registers and the rings' 220 KB allow
-  static constexpr int kCtas = DT == 256 ? (kFp4 ? 2 : 1) : (NT == 3 ? 2 : (NT == 1 && (kFp4 || DT == 64) ? 4 : 3));
+  static constexpr int kCtas = DT == 256 ? (kFp4 ? 2 : 1) : (NT == 3 ? 2 : (NT == 1 && !kFp4 && DT == 64 ? 4 : 3));
+  static constexpr int kDepth = 3;
   static constexpr int kFit = 220 * 1024 / kCtas / (kWarps * kStage);
-  static constexpr int kStages = kFit < 6 ? kFit : 6;
+  static constexpr int kStages = kFit < kDepth ? kFit : kDepth;
   static constexpr int kRing = kWarps * kStages * kStage;
   static constexpr int kMerge = (kWarps + 1) * kHeads * (DT + 4) * 4;  // the warps' results, and in a cluster the CTA's
   static constexpr int kSmem = kRing > kMerge ? kRing : kMerge;
@@ -420,8 +422,8 @@ __global__ void __launch_bounds__(kThreads, Cfg<DT, NT, kFp4>::kCtas) paged_atte
       return whole && i < tiles ? table[page_of(tok)] : -1;
     };
     int asked = ask(0);
-    // Asks for tile i; the result has a bit for each of its tokens that is there.
-    auto issue = [&](int i, uint32_t dst) -> uint32_t {
+    // Asks for tile i.
+    auto issue = [&](int i, uint32_t dst) {
       const int tok = tok0 + 16 * (phase + phases * i);
       uint32_t there = (tok1 - tok >= 16 ? 0xFFFFu : (1u << (tok1 - tok)) - 1u);
       if (tok < range.x) there &= 0xFFFFu << (range.x - tok);
@@ -484,21 +486,18 @@ __global__ void __launch_bounds__(kThreads, Cfg<DT, NT, kFp4>::kCtas) paged_atte
           for (int k = 0; k < D / 16; ++k) sts8(sd + k, ok ? src[k] : 0u);
         }
       }
-      return there;
+      if (lane == 0) sts32(dst + C::kThere, there);
     };
 
-    uint32_t there[C::kStages];  // which of a tile's tokens there are; there[0]: the tile to be used next
-#pragma unroll
-    for (int i = 0; i < C::kStages; ++i) there[i] = 0;
     if constexpr (kFp4) {
       if (D < DT)  // scale bytes behind D are read too, and stay as they are from here on
         for (int i = lane; i < C::kStages * C::kScaleTile / 4; i += 32)
           sts32(ring + i / (C::kScaleTile / 4) * C::kStage + C::kKTile + C::kVTile + i % (C::kScaleTile / 4) * 4, 0u);
     }
     __syncwarp();
-#pragma unroll
+#pragma unroll 1
     for (int i = 0; i < C::kStages - 1; ++i) {
-      if (i < tiles) there[i] = issue(i, ring + i * C::kStage);
+      if (i < tiles) issue(i, ring + i * C::kStage);
       cp_commit();
     }
     uint32_t put = ring + (C::kStages - 1) * C::kStage, src = ring;  // the stages to fill and to use next
@@ -516,17 +515,38 @@ __global__ void __launch_bounds__(kThreads, Cfg<DT, NT, kFp4>::kCtas) paged_atte
 
     for (int i = 0; i < tiles; ++i) {
       __syncwarp();  // the stage about to be filled again has been read by every lane
-      if (i + C::kStages - 1 < tiles) there[C::kStages - 1] = issue(i + C::kStages - 1, put);
+      if (i + C::kStages - 1 < tiles) issue(i + C::kStages - 1, put);
       cp_commit();
       cp_wait<C::kStages - 1>();
       __syncwarp();
       const uint32_t vs = src + C::kKTile;
       const uint32_t ss = src + C::kKTile + C::kVTile;
 
-      // ---- scores of 16 tokens x 8 NT heads
-      float s[NT][4];
+      const uint32_t there = lds32(src + C::kThere);
+      const bool ok0 = (there >> g) & 1u, ok1 = (there >> (g + 8)) & 1u;
+      // A MixFP4 tile's V codes and scale bytes, asked for before the scores so that neither waits for the other.
+      uint2 vc[kFp4 ? C::kVPieces : 1][4];
+      uint32_t vsc[kFp4 ? C::kVPieces : 1][4];
+      if constexpr (kFp4) {
 #pragma unroll
-      for (int n = 0; n < NT; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.0f;
+        for (int k = 0; k < C::kVPieces; ++k)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int tr = 2 * t + (r & 1) + 8 * (r >> 1);
+            vsc[k][r] = lds8(ss + (16 + tr) * 16 + (g + 8 * k) * C::kVDims / 16);
+            if constexpr (C::kVBytes == 8)
+              vc[k][r] = lds64(vs + C::v_place(tr, g + 8 * k));
+            else
+              vc[k][r].x = lds32(vs + C::v_place(tr, (g + 8 * k) / 2) + (g & 1) * C::kVBytes);
+          }
+      }
+
+      // ---- scores of 16 tokens x 8 NT heads, in two chains of products
+      float s[NT][4], s1[NT][4];
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[n][e] = s1[n][e] = 0.0f;
 #pragma unroll
       for (int k = 0; k < C::kKPieces; ++k) {
         uint32_t w[2][C::kKDims / 2];  // rows g and g + 8
@@ -547,10 +567,13 @@ __global__ void __launch_bounds__(kThreads, Cfg<DT, NT, kFp4>::kCtas) paged_atte
         for (int st = 0; st < C::kKDims / 4; ++st)
 #pragma unroll
           for (int n = 0; n < NT; ++n)
-            mma16816<kFp4>(s[n], w[0][2 * st], w[1][2 * st], w[0][2 * st + 1], w[1][2 * st + 1],
+            mma16816<kFp4>(st & 1 ? s1[n] : s[n], w[0][2 * st], w[1][2 * st], w[0][2 * st + 1], w[1][2 * st + 1],
                            qf[n][k * C::kKDims / 4 + st][0], qf[n][k * C::kKDims / 4 + st][1]);
       }
-      const bool ok0 = (there[0] >> g) & 1u, ok1 = (there[0] >> (g + 8)) & 1u;
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[n][e] += s1[n][e];
 
       // ---- softmax: thread (g, t) has tokens g, g + 8 and heads 2t, 2t + 1.  The weights are 2^(s - m) for
       // an m that follows the maximum from afar: it moves (and what was summed is scaled) when a score is
@@ -609,21 +632,12 @@ __global__ void __launch_bounds__(kThreads, Cfg<DT, NT, kFp4>::kCtas) paged_atte
         uint32_t w[4][C::kVDims / 2];  // tokens 2t, 2t + 1, 2t + 8, 2t + 9
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const int piece = C::kVBytes == C::kCopy ? g + 8 * k : (g + 8 * k) / 2;
-          const uint32_t a = vs + C::v_place(2 * t + (r & 1) + 8 * (r >> 1), piece) +
-                             (C::kVBytes == C::kCopy ? 0 : (g & 1) * C::kVBytes);
           if constexpr (kFp4) {
-            const int tr = 2 * t + (r & 1) + 8 * (r >> 1);
-            const BlockScale f = block_scale(lds8(ss + (16 + tr) * 16 + (g + 8 * k) * C::kVDims / 16));
-            if constexpr (C::kVBytes == 8) {
-              const uint2 v = lds64(a);
-              decode8(v.x, f.lo, f.hi, f.s2, w[r]);
-              decode8(v.y, f.lo, f.hi, f.s2, w[r] + 4);
-            } else {
-              decode8(lds32(a), f.lo, f.hi, f.s2, w[r]);
-            }
+            const BlockScale f = block_scale(vsc[k][r]);
+            decode8(vc[k][r].x, f.lo, f.hi, f.s2, w[r]);
+            if constexpr (C::kVBytes == 8) decode8(vc[k][r].y, f.lo, f.hi, f.s2, w[r] + 4);
           } else {
-            const uint4 v = lds128(a);
+            const uint4 v = lds128(vs + C::v_place(2 * t + (r & 1) + 8 * (r >> 1), g + 8 * k));
             w[r][0] = v.x, w[r][1] = v.y, w[r][2] = v.z, w[r][3] = v.w;
           }
         }
@@ -639,8 +653,6 @@ __global__ void __launch_bounds__(kThreads, Cfg<DT, NT, kFp4>::kCtas) paged_atte
           }
         }
       }
-#pragma unroll
-      for (int k = 0; k + 1 < C::kStages; ++k) there[k] = there[k + 1];
       put = src;
       src = src + C::kStage == behind ? ring : src + C::kStage;
     }
