@@ -146,8 +146,13 @@ __device__ __forceinline__ Tile find_tile(const Segments& s, int index) {
 // ---- shrink: out[t][r] = factor_a sum_k in[t][k] W_a[r][k], k < kdim -------------------------------
 // Ranks are the rows of the products (RT tiles of 16), tokens their columns
 // (TT / 8 tiles of 8).  A step covers 64 k, a whole 128-byte line of a row:
-// thread (g, t) holds k 16t .. 16t + 15 of its rows.  Warps take steps in turn, the CTAs of a cluster shares of k;
-// both are summed in order through shared memory.
+// thread (g, t) holds k 16t .. 16t + 15 of its rows.  A step's sum is its own
+// and is added by the fp32 units: in one chain the tensor cores' rounding
+// towards zero left dB of 13504 features 1.8e-6 off, so it is 1.6e-7.  Warps
+// take steps in turn, the CTAs of a cluster shares of k; both are summed in
+// order through shared memory.  (Staging 64 tokens and W's chunks in shared
+// memory by cp.async, for half the reads from L2, gained nothing: 160 us
+// against 160 us for the training step of 4096 tokens at rank 64.)
 struct ShrinkArgs {
   const uint16_t* in;  // [tokens][ld]
   int64_t ld;
@@ -207,13 +212,17 @@ __global__ void __launch_bounds__(kThreads, 2) lora_shrink_kernel(const ShrinkAr
           load32(a[i][h], w + (int64_t)r * p.kdim + k, in_k && r < p.R);
         }
 #pragma unroll
-      for (int q = 0; q < 4; ++q)
+      for (int i = 0; i < RT; ++i)
 #pragma unroll
-        for (int i = 0; i < RT; ++i)
+        for (int n = 0; n < TT / 8; ++n) {
+          float d[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-          for (int n = 0; n < TT / 8; ++n)
-            mma_bf16(acc[i][n], a[i][0][2 * q], a[i][1][2 * q], a[i][0][2 * q + 1], a[i][1][2 * q + 1], x[n][2 * q],
+          for (int q = 0; q < 4; ++q)
+            mma_bf16(d, a[i][0][2 * q], a[i][1][2 * q], a[i][0][2 * q + 1], a[i][1][2 * q + 1], x[n][2 * q],
                      x[n][2 * q + 1]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[i][n][e] += d[e];
+        }
     } else {
       // Rows k .. k + 15 at the thread's ranks 2 RT g ..: words of rank pairs, permuted to k pairs.
       uint32_t a[16][RT];
@@ -230,16 +239,25 @@ __global__ void __launch_bounds__(kThreads, 2) lora_shrink_kernel(const ShrinkAr
         }
       }
 #pragma unroll
-      for (int q = 0; q < 4; ++q)
+      for (int i = 0; i < RT; ++i) {
+        uint32_t f[4][4];
 #pragma unroll
-        for (int i = 0; i < RT; ++i) {
-          const uint32_t a0 = prmt(a[4 * q][i], a[4 * q + 1][i], 0x5410u);
-          const uint32_t a1 = prmt(a[4 * q][i], a[4 * q + 1][i], 0x7632u);
-          const uint32_t a2 = prmt(a[4 * q + 2][i], a[4 * q + 3][i], 0x5410u);
-          const uint32_t a3 = prmt(a[4 * q + 2][i], a[4 * q + 3][i], 0x7632u);
+        for (int q = 0; q < 4; ++q)
 #pragma unroll
-          for (int n = 0; n < TT / 8; ++n) mma_bf16(acc[i][n], a0, a1, a2, a3, x[n][2 * q], x[n][2 * q + 1]);
+          for (int h = 0; h < 2; ++h) {
+            f[q][2 * h] = prmt(a[4 * q + 2 * h][i], a[4 * q + 2 * h + 1][i], 0x5410u);
+            f[q][2 * h + 1] = prmt(a[4 * q + 2 * h][i], a[4 * q + 2 * h + 1][i], 0x7632u);
+          }
+#pragma unroll
+        for (int n = 0; n < TT / 8; ++n) {
+          float d[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            mma_bf16(d, f[q][0], f[q][1], f[q][2], f[q][3], x[n][2 * q], x[n][2 * q + 1]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[i][n][e] += d[e];
         }
+      }
     }
   }
 

@@ -114,6 +114,27 @@ def test_backward(T, cuts, ids, K, N, R, L, based):
     assert torch.equal(dx, again[0]) and torch.equal(da, again[1]) and torch.equal(db, again[2])
 
 
+def test_long_sums_keep_fp32():
+    """A contraction of 13504 features and one of 3000 tokens: products are exact and a sum of n terms is cut into
+    short chains added in fp32, some sqrt(40) roundings of 2^-24 in all: within 1e-6 of the result's norm."""
+    o = ops()
+    N, R = 288, 32
+    for T, K, cuts in ((187, 13504, list(range(188))), (3000, 512, [0, 3000])):
+        ids = [i % 2 for i in range(len(cuts) - 1)]
+        x, ad, st, ii, _ = problem(T, cuts, ids, K, N, R, 2)
+        dy = (randn(T, N, seed=9) * 1e-3).to(torch.bfloat16)
+        y, u = o.mixfp4_lora(x, ad, st, ii)
+        _, da, db = o.mixfp4_lora_backward(dy, x, u, ad, st, ii)
+        ru, _, ry, _ = reference(x, ad, cuts, ids, torch.zeros(T, N, device=DEV))
+        rda, rdb = torch.zeros_like(ad.a, dtype=torch.float64), torch.zeros_like(ad.b, dtype=torch.float64)
+        for i, j in enumerate(ids):
+            r, s = slice(cuts[i], cuts[i + 1]), ad.scaling[j].double()
+            rda[j] += s * (dy[r].double() @ ad.b[j].double()).T @ x[r].double()
+            rdb[j] += s * (dy[r].double().T @ ru[r])
+        for got, ref in ((u, ru), (y, ry), (da, rda), (db, rdb)):
+            assert (got.double() - ref).norm() <= 1e-6 * ref.norm()
+
+
 def test_gradients_against_differences():
     """y is linear in x, in a and in b, so <dy, y(p + h) - y(p)> = <gradient, h> for any h; within 1e-4 of the sum of
     magnitudes, the differences' own rounding."""
