@@ -581,7 +581,7 @@ int mixfp4_paged_attention_workspace(const mixfp4_kv_cache* cache, int64_t B, in
  * 0 .. adapters - 1 (-1) has no adapter: u = 0, out = base.
  *
  * x, dtype     device, bf16 (MIXFP4_DTYPE_BF16) [T][ldx]; 32-byte aligned, ldx % 16 == 0.
- * K, N         K % 16 == 0; N needs no padding; both at most 2^24.
+ * K, N         K % 16 == 0; N needs no padding; both at most 2^22.
  * a, b         device, bf16 [adapters][R][K] and [adapters][N][R], 32-byte aligned.
  *              R % 8 == 0, 8 .. 128 (smaller ranks: zeros).
  * scaling      device, float [adapters].    adapters  0 .. 65535.

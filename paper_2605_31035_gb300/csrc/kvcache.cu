@@ -1,8 +1,16 @@
 // The paged key-value cache: new tokens appended with the position rotation
 // on the way (mixfp4_kv_append), and rows read back (mixfp4_kv_gather).
 //
-// Both are single passes bound by memory: every input element is read once and
-// every output written once, 32 bytes per lane and access.  A thread owns a
+// Both are single passes: every input element is read once and every output
+// written once, 32 bytes per lane and access.  Appending 8111 tokens of 32 + 16
+// heads of 128 in fp32 to a bf16 cache (300 MB in all) takes 54 us, 82 % of the
+// measured HBM rate.  To a MixFP4 cache it takes 64 us for 258 MB (60 %): the
+// quantizer of a block holds 168 registers, and at 12 warps an SM its chain of
+// maximum, scale and codes is what is waited for.  The gather is a row's few
+// bytes to 16 bf16 values a thread: 14 us for those 8111 tokens, issue-bound
+// (76 %).
+//
+// A thread owns a
 // "unit" of a head row (one 16-element block, or the two blocks that a
 // rotation of pairs (i, i + rot / 2) couples) and walks over several heads of
 // its token, so that the token's angles, slot and address are found once.

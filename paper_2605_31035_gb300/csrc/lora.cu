@@ -82,6 +82,7 @@ struct Segments {
   const int32_t* ids;     // [count]
   int count, adapters;
   int64_t tokens;
+  int grouped;  // tiles of few tokens are taken from all segments of an adapter
 };
 
 __device__ __forceinline__ int2 bounds(const Segments& s, int i) {
@@ -143,6 +144,84 @@ __device__ __forceinline__ Tile find_tile(const Segments& s, int index) {
   return Tile{found[0], found[1], found[2]};
 }
 
+// The same where segments are short: t0 = 0, t1 the number of tokens, and which
+// they are in `rows`.  Grouped, an adapter's tokens are
+// one list through its segments in order, and tokens without one are another's,
+// so that requests that share an adapter share the reading of it: 256 requests
+// of one token on 32 adapters of rank 16, 8192 features either way, 24 us
+// against 27.  The order of a token's own sums does not depend on its tile.
+constexpr int kBins = 1024, kMostGrouped = 4096;
+
+template <int kTile>
+__device__ __forceinline__ Tile find_rows(const Segments& s, int index, int rows[kTile]) {
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  if (!s.grouped) {
+    const Tile tile = find_tile<kTile>(s, index);
+    if (tid < kTile) rows[tid] = tile.t0 + tid;
+    __syncthreads();
+    return Tile{0, tile.t1 - tile.t0, tile.adapter};
+  }
+  __shared__ int bins[kBins + 1];  // tokens of every adapter, and of none
+  __shared__ int scan[kWarps];
+  __shared__ int found[3];         // the adapter, the tile's first token in its list, the tokens from there on
+  const int lists = s.adapters + 1;
+  for (int i = tid; i < lists; i += kThreads) bins[i] = 0;
+  if (tid < kTile) rows[tid] = 0;
+  if (tid == 0) found[0] = -1, found[1] = found[2] = 0;
+  __syncthreads();
+  auto list_of = [&](int i) {
+    const int a = adapter_of(s, i);
+    return a < 0 ? s.adapters : a;
+  };
+  for (int i = tid; i < s.count; i += kThreads) {
+    const int2 r = bounds(s, i);
+    if (r.y > r.x) atomicAdd(&bins[list_of(i)], r.y - r.x);
+  }
+  __syncthreads();
+  const int strip = (lists + kThreads - 1) / kThreads;
+  const int lo = min(lists, tid * strip), hi = min(lists, lo + strip);
+  int mine = 0;
+  for (int i = lo; i < hi; ++i) mine += (bins[i] + kTile - 1) / kTile;
+  auto sum_to = [&](int v) {  // over the threads up to this one
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int o = __shfl_up_sync(kAll, v, d);
+      if (lane >= d) v += o;
+    }
+    if (lane == 31) scan[warp] = v;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w)
+      if (w < warp) v += scan[w];
+    return v;
+  };
+  int at = sum_to(mine) - mine;
+  if (index >= at && index < at + mine)
+    for (int i = lo; i < hi; ++i) {
+      const int n = (bins[i] + kTile - 1) / kTile;
+      if (index < at + n) {
+        found[0] = i, found[1] = (index - at) * kTile, found[2] = bins[i] - found[1];
+        break;
+      }
+      at += n;
+    }
+  __syncthreads();
+  const int list = found[0], first = found[1], count = min(kTile, found[2]);
+  for (int i0 = 0, done = 0; i0 < s.count && done < first + count; i0 += kThreads) {
+    const int i = i0 + tid;
+    const int2 r = i < s.count && list_of(i) == list ? bounds(s, i) : make_int2(0, 0);
+    const int before = done + sum_to(r.y - r.x) - (r.y - r.x);
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) done += scan[w];
+    for (int j = 0; j < count; ++j) {
+      const int x = first + j - before;
+      if (x >= 0 && x < r.y - r.x) rows[j] = r.x + x;
+    }
+    __syncthreads();  // `scan` has been read
+  }
+  return Tile{0, count, list < s.adapters ? list : -1};
+}
+
 // ---- shrink: out[t][r] = factor_a sum_k in[t][k] W_a[r][k], k < kdim -------------------------------
 // Ranks are the rows of the products (RT tiles of 16), tokens their columns
 // (TT / 8 tiles of 8).  A step covers 64 k, a whole 128-byte line of a row:
@@ -172,14 +251,19 @@ __global__ void __launch_bounds__(kThreads, 2) lora_shrink_kernel(const ShrinkAr
   griddep_launch_dependents();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
   const int split = (int)(blockIdx.x % p.splits);
-  const Tile tile = find_tile<TT>(p.seg, (int)(blockIdx.x / p.splits));
-  if (tile.t0 >= tile.t1) return;  // the whole cluster alike
+  constexpr bool kRows = TT == 8;
+  __shared__ int rows[TT];
+  const Tile tile = kRows ? find_rows<TT>(p.seg, (int)(blockIdx.x / p.splits), rows)
+                          : find_tile<TT>(p.seg, (int)(blockIdx.x / p.splits));
+  auto token = [&](int i) -> int64_t { return kRows ? rows[i] : tile.t0 + i; };  // the tile's i-th
+  const int count = tile.t1 - tile.t0;
+  if (count <= 0) return;  // the whole cluster alike
   const int r0 = blockIdx.y * 16 * RT;
   if (tile.adapter < 0) {
     if (split == 0)
       for (int i = threadIdx.x; i < kOut; i += kThreads) {
-        const int tok = tile.t0 + i / (16 * RT), r = r0 + i % (16 * RT);
-        if (tok < tile.t1 && r < p.R) p.out[(int64_t)tok * p.R + r] = 0.0f;
+        const int x = i / (16 * RT), r = r0 + i % (16 * RT);
+        if (x < count && r < p.R) p.out[token(x) * p.R + r] = 0.0f;
       }
     return;
   }
@@ -199,8 +283,7 @@ __global__ void __launch_bounds__(kThreads, 2) lora_shrink_kernel(const ShrinkAr
     uint32_t x[TT / 8][8];
 #pragma unroll
     for (int n = 0; n < TT / 8; ++n) {
-      const int tok = tile.t0 + 8 * n + g;
-      load32(x[n], p.in + (int64_t)tok * p.ld + k, in_k && tok < tile.t1);
+      load32(x[n], p.in + token(8 * n + g) * p.ld + k, in_k && 8 * n + g < count);
     }
     if (!kTrans) {
       uint32_t a[RT][2][8];
@@ -282,10 +365,10 @@ __global__ void __launch_bounds__(kThreads, 2) lora_shrink_kernel(const ShrinkAr
   else __syncthreads();
   const float f = p.factor ? p.factor[tile.adapter] : 1.0f;
   for (int i = split * kThreads + threadIdx.x; i < kOut; i += p.splits * kThreads) {
-    const int tok = tile.t0 + i / (16 * RT), r = r0 + i % (16 * RT);
+    const int x = i / (16 * RT), r = r0 + i % (16 * RT);
     float v = 0.0f;
     for (int q = 0; q < p.splits; ++q) v += p.splits > 1 ? peer_load(smem_addr(part + i), q) : part[i];
-    if (tok < tile.t1 && r < p.R) p.out[(int64_t)tok * p.R + r] = f * v;
+    if (x < count && r < p.R) p.out[token(x) * p.R + r] = f * v;
   }
   if (p.splits > 1) cluster_barrier();  // no CTA leaves while others read its sum
 }
@@ -346,26 +429,30 @@ template <int TT, bool kTrans, int kHeld, int NP>
 __global__ void __launch_bounds__(kThreads, 2) lora_expand_kernel(const ExpandArgs p) {
   extern __shared__ uint4 frag[];  // [m][step][part][lane]
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
-  const Tile tile = find_tile<TT>(p.seg, (int)blockIdx.x);
+  constexpr bool kRows = TT == 16;
+  __shared__ int rows[TT];
+  const Tile tile = kRows ? find_rows<TT>(p.seg, (int)blockIdx.x, rows) : find_tile<TT>(p.seg, (int)blockIdx.x);
+  auto token = [&](int i) -> int64_t { return kRows ? rows[i] : tile.t0 + i; };  // the tile's i-th
+  const int count = tile.t1 - tile.t0;
   const int steps = (p.R + 15) / 16;
   const int64_t n0 = ((int64_t)blockIdx.y * kWarps + warp) * (8 * NP);
   const uint16_t* w = p.w + (int64_t)max(tile.adapter, 0) * p.R * p.N;
-  const bool some = tile.t0 < tile.t1 && tile.adapter >= 0;
+  const bool some = count > 0 && tile.adapter >= 0;
   uint32_t held[kHeld][NP][2];
 #pragma unroll
   for (int st = 0; st < kHeld; ++st)
     expand_w<kTrans, NP>(held[st], w, some ? st * 16 + 4 * t : p.R, p.R, n0 + NP * g, p.N);
   griddep_wait();
   griddep_launch_dependents();  // not before: what may start then counts on the kernel before this one
-  if (tile.t0 >= tile.t1) return;
+  if (count <= 0) return;
   if (tile.adapter >= 0)
-    for (int i = threadIdx.x; i < (tile.t1 - tile.t0 + 15) / 16 * steps * 32; i += kThreads) {
+    for (int i = threadIdx.x; i < (count + 15) / 16 * steps * 32; i += kThreads) {
       const int ms = i / 32, m = ms / steps, l = i % 32;
-      const int r = (ms - m * steps) * 16 + 4 * (l & 3), ta = tile.t0 + 16 * m + (l >> 2);
+      const int r = (ms - m * steps) * 16 + 4 * (l & 3), ta = 16 * m + (l >> 2);
       const float4 z = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-      const float4 ua = r < p.R && ta < tile.t1 ? *reinterpret_cast<const float4*>(p.u + (int64_t)ta * p.R + r) : z;
+      const float4 ua = r < p.R && ta < count ? *reinterpret_cast<const float4*>(p.u + token(ta) * p.R + r) : z;
       const float4 ub =
-          r < p.R && ta + 8 < tile.t1 ? *reinterpret_cast<const float4*>(p.u + (int64_t)(ta + 8) * p.R + r) : z;
+          r < p.R && ta + 8 < count ? *reinterpret_cast<const float4*>(p.u + token(ta + 8) * p.R + r) : z;
       uint32_t a0[3], a1[3], a2[3], a3[3];
       split3(ua.x, ua.y, a0);
       split3(ub.x, ub.y, a1);
@@ -379,13 +466,13 @@ __global__ void __launch_bounds__(kThreads, 2) lora_expand_kernel(const ExpandAr
   const float f = tile.adapter < 0 ? 0.0f : (p.factor ? p.factor[tile.adapter] : 1.0f);
   const int64_t nt = n0 + 2 * NP * t;  // this thread's results
   const bool vec = p.vec && nt + 2 * NP <= p.N;
-  for (int m = 0; tile.t0 + 16 * m < tile.t1; ++m) {
-    const int ta = tile.t0 + 16 * m + g;
+  for (int m = 0; 16 * m < count; ++m) {
+    const int ta = 16 * m + g;
     float v[2][2 * NP];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const float* b = p.base + (int64_t)(ta + 8 * h) * p.ld_base + nt;
-      const bool there = p.base && ta + 8 * h < tile.t1;
+      const bool there = p.base && ta + 8 * h < count;
+      const float* b = there ? p.base + token(ta + 8 * h) * p.ld_base + nt : nullptr;
       if (vec) {
 #pragma unroll
         for (int q = 0; q < 2 * NP; q += 8) load32(reinterpret_cast<uint32_t*>(v[h] + q), b + q, there);
@@ -419,10 +506,10 @@ __global__ void __launch_bounds__(kThreads, 2) lora_expand_kernel(const ExpandAr
     // acc[j]: (token g, features 2 NP t + j and 2 NP t + NP + j), then token g + 8
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      if (ta + 8 * h >= tile.t1) continue;
+      if (ta + 8 * h >= count) continue;
 #pragma unroll
       for (int q = 0; q < 2 * NP; ++q) v[h][q] = fmaf(f, acc[q % NP][2 * h + q / NP], v[h][q]);
-      float* o = p.out + (int64_t)(ta + 8 * h) * p.ld_out + nt;
+      float* o = p.out + token(ta + 8 * h) * p.ld_out + nt;
       if (vec) {
 #pragma unroll
         for (int q = 0; q < 2 * NP; q += 8) stg256(o + q, reinterpret_cast<const uint32_t*>(v[h] + q));
@@ -638,6 +725,11 @@ __global__ void __launch_bounds__(32 * NW, NW == 8 ? 1 : (RT == 4 ? 2 : 3)) lora
 
 inline bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 
+// Tiles of at most `size` tokens, no fewer than there are.
+int64_t tiles_of(const Segments& s, int size, bool rows) {
+  return s.tokens / size + (rows && s.grouped && s.adapters < s.count ? s.adapters + 1 : s.count);
+}
+
 template <int RT, int TT, bool kTrans>
 int launch_shrink(const ShrinkArgs& p, bool dependent, cudaStream_t s) {
   const int smem = kWarps * 16 * RT * TT * 4;
@@ -645,7 +737,7 @@ int launch_shrink(const ShrinkArgs& p, bool dependent, cudaStream_t s) {
   static std::atomic<uint64_t> done{0};
   if (smem > 48 * 1024 && !set_dynamic_smem_once(reinterpret_cast<const void*>(kernel), smem, done))
     return MIXFP4_ERR_CUDA;
-  const int64_t tiles = p.seg.tokens / TT + p.seg.count;
+  const int64_t tiles = tiles_of(p.seg, TT, TT == 8);
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = (unsigned)p.splits, attr[0].val.clusterDim.y = 1, attr[0].val.clusterDim.z = 1;
@@ -664,7 +756,7 @@ int launch_shrink(const ShrinkArgs& p, bool dependent, cudaStream_t s) {
 template <bool kTrans>
 int shrink(ShrinkArgs p, bool dependent, cudaStream_t s) {
   const bool few = p.seg.tokens <= 8 * (int64_t)p.seg.count;
-  const int64_t tiles = p.seg.tokens / (few ? 8 : 32) + p.seg.count;
+  const int64_t tiles = few ? tiles_of(p.seg, 8, true) : tiles_of(p.seg, 32, false);
   // Ranks of a CTA: 16, or 32 (x is read again for every 32 ranks, from L2; 64 in one CTA left registers for
   // half the loads in flight).  CTAs: k is cut until they fill the device's two places to an SM.
   const int rt = p.R <= 16 ? 1 : 2;
@@ -681,7 +773,7 @@ int launch_expand(const ExpandArgs& p, cudaStream_t s) {
   auto* kernel = lora_expand_kernel<TT, kTrans, kHeld, NP>;
   static std::atomic<uint64_t> done{0};
   if (!set_dynamic_smem_once(reinterpret_cast<const void*>(kernel), kMost, done)) return MIXFP4_ERR_CUDA;
-  const dim3 grid((unsigned)(p.seg.tokens / TT + p.seg.count), (unsigned)((p.N + 8 * NP * kWarps - 1) / (8 * NP * kWarps)));
+  const dim3 grid((unsigned)tiles_of(p.seg, TT, TT == 16), (unsigned)((p.N + 8 * NP * kWarps - 1) / (8 * NP * kWarps)));
   return launch_pdl(kernel, grid, dim3(kThreads), (size_t)((p.R + 15) / 16 * kStep), s, p) == cudaSuccess
              ? MIXFP4_OK
              : MIXFP4_ERR_CUDA;
@@ -725,12 +817,17 @@ int grad(GradArgs p, cudaStream_t s) {
                                                             : launch_grad<RT, 8>(p, grid, s);
 }
 
+// Whether tiles of few tokens are taken from all segments of an adapter.
+bool grouped(int64_t T, int64_t adapters, int64_t segments) {
+  return T <= 8 * segments && segments > 8 && segments <= kMostGrouped && adapters <= kBins;
+}
+
 // The arguments both entry points share.
 int check_lora(int64_t T, int64_t K, int64_t N, int64_t R, int64_t adapters, const void* a, const void* b,
                const float* scaling, const int32_t* starts, const int32_t* ids, int64_t segments) {
   if (T < 0 || T > INT32_MAX - 4096 || K < 0 || K % 16 != 0 || N < 0 || R < 8 || R > 128 || R % 8 != 0 ||
-      adapters < 0 || adapters > 65535 || segments < 0 || segments > (1 << 20) || N > ((int64_t)1 << 24) ||
-      K > ((int64_t)1 << 24))
+      adapters < 0 || adapters > 65535 || segments < 0 || segments > (1 << 20) || N > ((int64_t)1 << 22) ||
+      K > ((int64_t)1 << 22))
     return MIXFP4_ERR_SHAPE;
   if (!starts || (segments > 0 && !ids) || (adapters > 0 && ((K > 0 && !a) || (N > 0 && !b) || !scaling)))
     return MIXFP4_ERR_NULL;
@@ -758,7 +855,7 @@ int mixfp4_lora(const void* x, int dtype, int64_t T, int64_t K, int64_t ldx, con
   if ((K > 0 && !x) || (N > 0 && !out) || !u) return MIXFP4_ERR_NULL;
   if (!aligned(x, 32) || ldx % 16 || !aligned(u, 16) || !aligned(out, 4) || !aligned(base, 4)) return MIXFP4_ERR_ALIGN;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  const Segments seg{starts, ids, (int)segments, (int)adapters, T};
+  const Segments seg{starts, ids, (int)segments, (int)adapters, T, grouped(T, adapters, segments)};
   const ShrinkArgs sp{static_cast<const uint16_t*>(x), ldx, static_cast<const uint16_t*>(a), nullptr, u, K,
                       (int)R, 1, seg};
   if (int st = shrink<false>(sp, false, s)) return st;
@@ -784,7 +881,7 @@ int mixfp4_lora_backward(const void* dy, int64_t ldy, const void* x, int64_t ldx
       !aligned(dx, 4) || !aligned(base, 4) || !aligned(da, 32) || !aligned(db, 32))
     return MIXFP4_ERR_ALIGN;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  const Segments seg{starts, ids, (int)segments, (int)adapters, T};
+  const Segments seg{starts, ids, (int)segments, (int)adapters, T, grouped(T, adapters, segments)};
   if (tokens) {
     const ShrinkArgs sp{static_cast<const uint16_t*>(dy), ldy, static_cast<const uint16_t*>(b), scaling, v, N,
                         (int)R, 1, seg};

@@ -114,6 +114,30 @@ def test_backward(T, cuts, ids, K, N, R, L, based):
     assert torch.equal(dx, again[0]) and torch.equal(da, again[1]) and torch.equal(db, again[2])
 
 
+def short(lengths, ids):
+    """(T, cuts, ids) of segments of the lengths, over and over the ids."""
+    cuts = [0]
+    for n in lengths:
+        cuts.append(cuts[-1] + n)
+    return cuts[-1], cuts, [ids[i % len(ids)] for i in range(len(lengths))]
+
+
+SHORT = [
+    (*short([1] * 600, [0, 3, -1, 5, 2, 2, 9]), 272, 336, 16, 6),           # more segments than threads of a block
+    (*short([i * 5 % 7 % 4 for i in range(301)], [1, 0, 1, 2, -1]), 512, 1040, 40, 3),
+    (*short([1] * 9 + [100] + [1] * 10, [0, 0, 1]), 1024, 80, 8, 2),        # a long segment among short ones
+    (*short([1] * 40, [1099, 0, 511, 0, 1023, 1024]), 64, 64, 8, 1100),     # many adapters
+    (*short([2, 0, 1] * 1400, [0, 1, 2, 3]), 32, 32, 8, 4),                 # many segments
+    (*short([1, 2, 3] * 7, [-1, 7]), 256, 64, 128, 4),                      # none has an adapter
+]
+
+
+@pytest.mark.parametrize("T,cuts,ids,K,N,R,L", SHORT)
+def test_short_segments_share_adapters(T, cuts, ids, K, N, R, L):
+    test_forward(T, cuts, ids, K, N, R, L, True)
+    test_backward(T, cuts, ids, K, N, R, L, True)
+
+
 def test_long_sums_keep_fp32():
     """A contraction of 13504 features and one of 3000 tokens: products are exact and a sum of n terms is cut into
     short chains added in fp32, some sqrt(40) roundings of 2^-24 in all: within 1e-6 of the result's norm."""
