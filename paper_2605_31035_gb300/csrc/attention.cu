@@ -53,10 +53,14 @@ constexpr int kWarps = 4;
 constexpr int kThreads = kWarps * 32;
 constexpr int kJoinThreads = 256;
 constexpr int kCluster = 8;
-// Tokens up to which one cluster to a row is the quicker way, four times that where clusters fill half the device.
-// One sequence of 8 key heads of 128, clusters against shares of the whole device and a joining kernel: 4000 tokens 13
-// against 25 us, 8000 19 against 17, 32000 54 against 33; six sequences of 8000 39 against 45, of 16000 67 against 73.
-constexpr int kClusterTokens = 4096;
+// Tokens to a CTA up to which a cluster to each row (8 CTAs, or 4 or 2 where the rows are more) is the quicker way,
+// four times that where clusters fill half the device.  8 key heads of 128, clusters against shares of the whole device
+// and a joining kernel: one sequence of 4000 tokens 13 against 25 us, of 8000 19 against 17, of 32000 54 against 33; six
+// of 8000 39 against 45, of 16000 67 against 73; 16 of up to 500 10 against 14, of up to 2000 20 against 22.
+constexpr int kCtaTokens = 512;
+// And up to which one CTA to a row is, whatever their number: 40 sequences of up to 250 12 against 16 us, of up to 500
+// 17 against 17; 100 of up to 250 21 against 22, of up to 500 34 against 31; 300 of up to 120 28 against 32.
+constexpr int kRowTokens = 256;
 // What beginning a row costs (its queries, the way to its first pages, the join of the warps), in units.  Swept, 0 / 2 /
 // 4 / 8: 256 sequences of up to 200 tokens, 8 heads of 128, 58 / 46 / 41 / 39 us; 64 of up to 8192 on a MixFP4 cache
 // 149 / 146 / 146 / 149 us.
@@ -74,7 +78,8 @@ struct AttnArgs {
   int64_t q_stride, q_head_stride;
   int B, q_heads, group, chunks;  // group = q_heads / heads; chunks of 8 NT query heads per key head
   int together;                   // key heads of a CTA: 4, 2 or 1, each a warp's (or two's, or four's)
-  int clustered;                  // one cluster of kCluster CTAs to a row, joined in shared memory
+  int cluster;                    // CTAs to a row: 1, or a cluster of 2, 4 or 8 joined in shared memory; 0: equal shares
+  int cluster_shift;              // its log2
   mixfp4_kv_cache c;
   int page_shift;  // log2 page_size, or -1
   const int32_t* table;
@@ -277,11 +282,11 @@ __global__ void __launch_bounds__(kThreads, Cfg<DT, NT, kFp4>::kCtas) paged_atte
   // This CTA's share [pos, end) of all units, and the sequence it starts in.
   int b = 0;
   int64_t pos = 0, end = 1, base = 0, all = 0, grid = 0;
-  if (p.clustered) {
-    b = (int)(blockIdx.x / kCluster) / rows;
+  if (p.cluster) {
+    b = (int)(blockIdx.x >> p.cluster_shift) / rows;
     const int2 r = seen(p, b);
-    if (r.y <= r.x) {  // the cluster's row sees nothing
-      if (blockIdx.x % (kCluster * rows) == 0) nothing_seen(p, b, tid);
+    if (r.y <= r.x) {  // the row sees nothing
+      if (blockIdx.x % (p.cluster * rows) == 0) nothing_seen(p, b, tid);
       return;
     }
   } else {
@@ -347,18 +352,17 @@ __global__ void __launch_bounds__(kThreads, Cfg<DT, NT, kFp4>::kCtas) paged_atte
   while (pos < end && b < p.B) {
     const int2 range = seen(p, b);
     const int u = units(p, range);
-    if (!p.clustered && (u == 0 || pos >= base + (int64_t)u * rows)) {  // the next sequence (this one may have no unit)
+    if (!p.cluster && (u == 0 || pos >= base + (int64_t)u * rows)) {  // the next sequence (this one may have no unit)
       base += (int64_t)u * rows;
       ++b;
       continue;
     }
     int row, k0, cnt;  // row of the sequence, first unit and units of it
-    if (p.clustered) {
-      const int rank = (int)cluster_rank();
-      row = (int)(blockIdx.x / kCluster) % rows;
-      const int tu = u - kRowCost, k1 = kRowCost + (int)((int64_t)tu * (rank + 1) / kCluster);
-      k0 = kRowCost + (int)((int64_t)tu * rank / kCluster);
-      cnt = k1 - k0;
+    if (p.cluster) {
+      const int rank = (int)(blockIdx.x & (p.cluster - 1)), tu = u - kRowCost;
+      row = (int)(blockIdx.x >> p.cluster_shift) % rows;
+      k0 = rank > 0 ? kRowCost + (int)((int64_t)tu * rank >> p.cluster_shift) : 0;
+      cnt = kRowCost + (int)((int64_t)tu * (rank + 1) >> p.cluster_shift) - k0;
     } else {
       row = (int)((pos - base) / u);
       k0 = (int)((pos - base) - (int64_t)row * u);
@@ -696,7 +700,7 @@ __global__ void __launch_bounds__(kThreads, Cfg<DT, NT, kFp4>::kCtas) paged_atte
       }
     }
     __syncthreads();
-    float* js = ms + kWarps * C::kHeads * 2;                                 // [head] m, l of a clustered CTA
+    float* js = ms + kWarps * C::kHeads * 2;                                 // [head] m, l of a cluster's CTA
     float* jo = js + C::kHeads * 2;                                          // [head][DT]
     const bool first = k0 == 0, last = k0 + cnt == u;
     const int64_t slot = (2 * (int64_t)blockIdx.x + (first ? 1 : 0)) * p.together;
@@ -714,7 +718,7 @@ __global__ void __launch_bounds__(kThreads, Cfg<DT, NT, kFp4>::kCtas) paged_atte
         x += f * v.x;
         y += f * v.y;
       }
-      if (p.clustered) {
+      if (p.cluster > 1) {
         *reinterpret_cast<float2*>(jo + h * DT + d) = make_float2(x, y);
         if (d == 0) *reinterpret_cast<float2*>(js + 2 * h) = make_float2(M, L);
       } else if (first && last) {
@@ -728,19 +732,23 @@ __global__ void __launch_bounds__(kThreads, Cfg<DT, NT, kFp4>::kCtas) paged_atte
         if (d == 0) p.stat[(slot + w0) * C::kHeads + h] = make_float2(M, L);
       }
     }
-    if (p.clustered) {  // each CTA joins its share of the row's outputs
+    if (p.cluster == 1) return;
+    if (p.cluster > 1) {  // each CTA joins its share of the row's outputs
       cluster_barrier();
-      for (int i = (int)cluster_rank() * kThreads + tid; i < nh * (DT / 2); i += kCluster * kThreads) {
+      for (int i = (int)cluster_rank() * kThreads + tid; i < nh * (DT / 2); i += p.cluster * kThreads) {
         const int h = i / (DT / 2), d = (i - h * (DT / 2)) * 2;
         float2 st[kCluster], v[kCluster];
         float M = kNoScore, L = 0.0f, x = 0.0f, y = 0.0f;
 #pragma unroll
-        for (int q = 0; q < kCluster; ++q) st[q] = peer_load(js + 2 * h, q), v[q] = peer_load(jo + h * DT + d, q);
+        for (int q = 0; q < kCluster; ++q) {  // of fewer CTAs some twice, the second time with weight 0
+          const int rank = q & (p.cluster - 1);
+          st[q] = peer_load(js + 2 * h, rank), v[q] = peer_load(jo + h * DT + d, rank);
+        }
 #pragma unroll
         for (int q = 0; q < kCluster; ++q) M = fmaxf(M, st[q].x);
 #pragma unroll
         for (int q = 0; q < kCluster; ++q) {
-          const float f = exp2f(st[q].x - M);
+          const float f = q < p.cluster ? exp2f(st[q].x - M) : 0.0f;
           L += f * st[q].y;
           x += f * v[q].x;
           y += f * v[q].y;
@@ -896,12 +904,16 @@ int launch(const AttnArgs& p, int grid, cudaStream_t s) {
   static std::atomic<uint64_t> done{0};
   auto* kernel = paged_attention_kernel<DT, NT, kFp4>;
   if (!set_dynamic_smem_once(reinterpret_cast<const void*>(kernel), C::kSmem, done)) return MIXFP4_ERR_CUDA;
-  if (p.clustered) {
+  if (p.cluster == 1) {
+    kernel<<<(unsigned)(p.B * (p.c.heads / p.together) * p.chunks), kThreads, C::kSmem, s>>>(p);
+    return launch_status();
+  }
+  if (p.cluster) {
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = kCluster, attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    attr[0].val.clusterDim.x = (unsigned)p.cluster, attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(p.B * p.c.heads * p.chunks * kCluster));
+    cfg.gridDim = dim3((unsigned)(p.B * p.c.heads * p.chunks * p.cluster));
     cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = C::kSmem;
     cfg.stream = s;
@@ -977,11 +989,14 @@ int mixfp4_paged_attention(const void* q, int64_t q_stride, int64_t q_head_strid
   p.c = *cache;
   p.together = together_of(cache, B, p.chunks, grid);
   // Few rows that cannot be long: a cluster to each, all resident at once, which joins its CTAs' parts in shared
-  // memory and so saves the second launch and its wait.
+  // memory and so saves the second launch and its wait; many short ones: a CTA to each, and nothing to join.
   const int64_t bound = window > 0 && window < table_pages * cache->page_size ? window : table_pages * cache->page_size;
-  const int64_t in_clusters = B * cache->heads * p.chunks * kCluster;
-  p.clustered = in_clusters <= grid && bound <= (in_clusters >= grid / 2 ? 4 : 1) * kClusterTokens;
-  if (p.clustered) p.together = 1;
+  const int64_t single = B * cache->heads * p.chunks;
+  for (int n = kCluster; n > 1 && !p.cluster; n /= 2)
+    if (single * n <= grid && bound <= n * kCtaTokens * (single * n >= grid / 2 ? 4 : 1)) p.cluster = n;
+  if (!p.cluster && bound <= kRowTokens && single <= INT32_MAX) p.cluster = 1;
+  if (p.cluster > 1) p.together = 1;
+  while (1 << p.cluster_shift < p.cluster) ++p.cluster_shift;
   p.page_shift = -1;
   for (int i = 0; i < 31; ++i)
     if (cache->page_size == 1 << i) p.page_shift = i;

@@ -166,6 +166,23 @@ def test_many_shares(fp4, B, longest):
 
 
 @pytest.mark.parametrize("fp4", [False, True])
+@pytest.mark.parametrize("Hq,Hkv,D", [(8, 2, 128), (16, 2, 256), (24, 1, 64), (6, 3, 80), (48, 1, 32)])
+@pytest.mark.parametrize("B,longest,window", [(1, 300, 0), (7, 250, 50), (12, 1000, 0), (40, 100, 0), (60, 130, 50),
+                                              (150, 240, 0), (500, 33, 0)])
+def test_rows_of_bounded_length(fp4, Hq, Hkv, D, B, longest, window):
+    """A cluster of 8, 4 or 2 CTAs to a row, one CTA, or shares of all, as the number of rows and the table allow."""
+    o = ops()
+    g = torch.Generator().manual_seed(B + D)
+    lengths = [int(torch.randint(0, longest + 1, (1,), generator=g)) for _ in range(B)]
+    lengths[0], lengths[B // 2] = longest, 0 if B > 1 else longest
+    cache, table, k, v = build(fp4, lengths, Hkv, D, 16, "nhd" if B % 2 else "hnd", seed=B)
+    q = (randn(B, Hq, D, seed=5) * 1.5).to(torch.bfloat16)
+    lens = torch.tensor(lengths, dtype=torch.int32, device=DEV)
+    out, lse = o.mixfp4_paged_attention(q, cache, table, lens, window=window, return_lse=True)
+    check(out, lse, q, lengths, k, v, D ** -0.5, window, fp4)
+
+
+@pytest.mark.parametrize("fp4", [False, True])
 def test_scores_that_grow_or_shrink_along_the_sequence(fp4):
     """The running maximum moves at every tile, or never after the first."""
     o = ops()
