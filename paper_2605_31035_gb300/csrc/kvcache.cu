@@ -3,17 +3,15 @@
 //
 // Both are single passes: every input element is read once and every output
 // written once, 32 bytes per lane and access.  Appending 8111 tokens of 32 + 16
-// heads of 128 in fp32 to a bf16 cache (300 MB in all) takes 54 us, 82 % of the
-// measured HBM rate.  To a MixFP4 cache it takes 64 us for 258 MB (60 %): the
-// quantizer of a block holds 168 registers, and at 12 warps an SM its chain of
-// maximum, scale and codes is what is waited for.  The gather is a row's few
-// bytes to 16 bf16 values a thread: 14 us for those 8111 tokens, issue-bound
-// (76 %).
+// heads of 128 in fp32 to a bf16 cache (300 MB in all) takes 48 us, 92 % of the
+// measured HBM rate.  To a MixFP4 cache it takes 52 us for 258 MB (73 %), the
+// rest being the quantizer's steps.  The gather is a row's few bytes to 16 bf16
+// values a thread: 14 us for those 8111 tokens, issue-bound (76 %).
 //
-// A thread owns a
-// "unit" of a head row (one 16-element block, or the two blocks that a
-// rotation of pairs (i, i + rot / 2) couples) and walks over several heads of
-// its token, so that the token's angles, slot and address are found once.
+// A thread owns a "unit" of a head row (one 16-element block, or the two blocks
+// that a rotation of pairs (i, i + rot / 2) couples) and walks over several
+// heads of its token, so that the token's angles, slot and address are found
+// once.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <cstdint>
@@ -27,11 +25,15 @@ namespace mixfp4 {
 namespace {
 
 constexpr int kThreads = 128;
-// CTAs of an SM by registers, and rounds of them that many tokens are spread over.  Swept at 8111 tokens of 32 + 16
-// heads of 128 in fp32, (3, 2) / (3, 4) / (4, 2) / (4, 4) / (4, 8): MixFP4 cache 80 / 85 / 89 / 85 / 109 us with the
-// gather behind it (at 4, registers spill), bf16 cache 57 / 59 / 57 / 54 / 63 us.
+// CTAs of an SM by registers.  A MixFP4 cache's quantizer is a long chain of dependent steps and lives on other warps, so
+// its angles lie in shared memory and rows are asked for when they are due: 5 / 6 / 7 CTAs 47 / 42 / 40 us at 4000
+// interleaved tokens of 32 + 16 heads of 128 in fp32, 22 / 22 / 24 us at 5372 of 8 + 2 heads of 256, 33 / 29 / 31 us at
+// 3170 of 40 + 16 heads of 128 in bf16 (with angles in registers and a row ahead, 3 CTAs: 54, 32 and 39 us).  A bf16
+// cache keeps both in registers: rows a head ahead are what HBM needs.
 template <int kMode>
-constexpr int kCtas = kMode < 0 ? 4 : 3;
+constexpr int kCtas = kMode < 0 ? 4 : 6;
+// What a thread's beginning (slot, angles) costs in head rows; 1 to 8 choose alike.
+constexpr int kBegin = 2;
 
 struct AppendArgs {
   const void* src[3];  // q, k, v
@@ -112,6 +114,7 @@ __device__ __forceinline__ void store16_mixfp4(uint8_t* codes, uint8_t* scale, c
 template <bool kF32, int kMode>
 __global__ void __launch_bounds__(kThreads, kCtas<kMode>) kv_append_kernel(const AppendArgs p) {
   __shared__ float4 tab[kMode >= 0 ? 128 : 1];
+  __shared__ float angles[kMode >= 0 ? 32 * kThreads : 1];  // [16 cosines, 16 sines][thread]
   const int row = (int)threadIdx.x / p.units, u = (int)threadIdx.x - row * p.units;
   const int tl = row / p.groups, g = (int)blockIdx.y * p.groups + row - tl * p.groups;
   const int64_t t = (int64_t)blockIdx.x * p.at_once + tl;
@@ -125,7 +128,7 @@ __global__ void __launch_bounds__(kThreads, kCtas<kMode>) kv_append_kernel(const
   const bool turns = b0 * 16 < rot;
   const int heads = p.q_heads + 2 * p.c.heads;
 
-  // One head row's blocks, asked for a head ahead of their use.
+  // One head row's blocks, for a bf16 cache asked for a head ahead of their use.
   constexpr int kWords = kF32 ? 16 : 8;
   uint32_t next[2][kWords];
   auto role_of = [&](int hh) { return hh < p.q_heads ? 0 : (hh < p.q_heads + p.c.heads ? 1 : 2); };
@@ -148,7 +151,7 @@ __global__ void __launch_bounds__(kThreads, kCtas<kMode>) kv_append_kernel(const
   if (mine) {
     slot = p.slots[t];
     if (rot > 0) pos = p.positions[t];
-    if (g < heads) fetch(g);
+    if (kMode < 0 && g < heads) fetch(g);
   }
   TensorConsts tk, tv;
   if (kMode >= 0) {
@@ -179,6 +182,13 @@ __global__ void __launch_bounds__(kThreads, kCtas<kMode>) kv_append_kernel(const
       }
     }
   }
+  if (kMode >= 0) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e)
+      angles[e * kThreads + threadIdx.x] = c[e], angles[(16 + e) * kThreads + threadIdx.x] = s[e];
+  }
+  auto cosine = [&](int e) { return kMode >= 0 ? angles[e * kThreads + threadIdx.x] : c[e]; };
+  auto sine = [&](int e) { return kMode >= 0 ? angles[(16 + e) * kThreads + threadIdx.x] : s[e]; };
   int64_t at = 0, sat = 0;
   if (keep) {
     const int64_t page = slot / p.c.page_size, off = slot - page * p.c.page_size;
@@ -188,10 +198,11 @@ __global__ void __launch_bounds__(kThreads, kCtas<kMode>) kv_append_kernel(const
 
 #pragma unroll 1
   for (int hh = g; hh < heads; hh += p.stride) {
+    if (kMode >= 0) fetch(hh);
     float x[2][16];
     to_float<kF32>(next[0], x[0]);
     if (pair) to_float<kF32>(next[1], x[1]);
-    if (hh + p.stride < heads) fetch(hh + p.stride);
+    if (kMode < 0 && hh + p.stride < heads) fetch(hh + p.stride);
     const int role = role_of(hh);
     if (role != 0 && !keep) continue;
     const int h = role == 0 ? hh : (role == 1 ? hh - p.q_heads : hh - p.q_heads - p.c.heads);
@@ -200,16 +211,16 @@ __global__ void __launch_bounds__(kThreads, kCtas<kMode>) kv_append_kernel(const
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
           const float a = x[0][e], b = x[1][e];
-          x[0][e] = __fsub_rn(__fmul_rn(a, c[e]), __fmul_rn(b, s[e]));
-          x[1][e] = __fadd_rn(__fmul_rn(b, c[e]), __fmul_rn(a, s[e]));
+          x[0][e] = __fsub_rn(__fmul_rn(a, cosine(e)), __fmul_rn(b, sine(e)));
+          x[1][e] = __fadd_rn(__fmul_rn(b, cosine(e)), __fmul_rn(a, sine(e)));
         }
       } else if (p.interleaved) {
 #pragma unroll
         for (int e = 0; e < 16; e += 2) {  // rot is even: a pair turns or stays as a whole
           const float a = x[0][e], b = x[0][e + 1];
           if (b0 * 16 + e < rot) {
-            x[0][e] = __fadd_rn(__fmul_rn(a, c[e]), __fmul_rn(b, s[e]));
-            x[0][e + 1] = __fadd_rn(__fmul_rn(b, c[e + 1]), __fmul_rn(a, s[e + 1]));
+            x[0][e] = __fadd_rn(__fmul_rn(a, cosine(e)), __fmul_rn(b, sine(e)));
+            x[0][e + 1] = __fadd_rn(__fmul_rn(b, cosine(e + 1)), __fmul_rn(a, sine(e + 1)));
           }
         }
       } else {
@@ -221,7 +232,7 @@ __global__ void __launch_bounds__(kThreads, kCtas<kMode>) kv_append_kernel(const
           const int d = b0 * 16 + e;
           if (d < rot) {
             const float b = load1<kF32>(base, from + (d < half ? d + half : d - half));
-            x[0][e] = __fadd_rn(__fmul_rn(x[0][e], c[e]), __fmul_rn(b, s[e]));
+            x[0][e] = __fadd_rn(__fmul_rn(x[0][e], cosine(e)), __fmul_rn(b, sine(e)));
           }
         }
       }
@@ -390,17 +401,18 @@ int mixfp4_kv_append(const void* q, int64_t q_token_stride, int64_t q_head_strid
   p.slots = slots;
   p.q_out = static_cast<uint16_t*>(q_out);
   p.units = p.paired ? p.rot / 32 + (cache->head_dim - p.rot) / 16 : cache->head_dim / 16;
-  // Threads of a token: for few tokens one for each head and unit, spread over CTAs; for many as few as leave the
-  // device some rounds of CTAs, so that a thread walks over several heads with the same angles.
+  // Threads of a token: for few tokens one for each head and unit, spread over CTAs; else as many as make rounds of CTAs
+  // times heads of a thread the least, so that the last round is full (3305 tokens of 40 + 16 heads of 128: 42 us with
+  // 2.2 rounds, 31 so).
   const int heads = (int)q_heads + 2 * cache->heads, most = kThreads / p.units;
-  const bool bf16_cache = cache->dtype == MIXFP4_CACHE_BF16;
-  const int64_t wanted = (int64_t)num_sms() * kThreads * (bf16_cache ? kCtas<-1> * 4 : kCtas<0> * 2);
-  int64_t groups = (wanted + T * p.units - 1) / (T * p.units);
-  groups = groups < heads ? groups : heads;
-  const int slices = (int)((groups + most - 1) / most);
-  p.groups = (int)((groups + slices - 1) / slices);
-  p.stride = p.groups * slices;
-  p.at_once = most / p.groups;
+  const int64_t places = (int64_t)num_sms() * (cache->dtype == MIXFP4_CACHE_BF16 ? kCtas<-1> : kCtas<0>);
+  int64_t least = INT64_MAX;
+  for (int groups = T * p.units * heads <= places * kThreads ? heads : 1; groups <= heads; ++groups) {
+    const int slices = (groups + most - 1) / most, each = (groups + slices - 1) / slices, at_once = most / each;
+    const int64_t rounds = ((T + at_once - 1) / at_once * slices + places - 1) / places;
+    const int64_t cost = rounds * ((heads + each * slices - 1) / (each * slices) + kBegin);
+    if (cost < least) least = cost, p.groups = each, p.stride = each * slices, p.at_once = at_once;
+  }
   const int64_t blocks = (T + p.at_once - 1) / p.at_once;
   if (blocks > INT32_MAX) return MIXFP4_ERR_SHAPE;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
