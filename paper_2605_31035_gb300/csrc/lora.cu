@@ -24,8 +24,8 @@
 // u and v are fp32.  Where they enter a product they are cut into three bf16
 // parts (24 bits), one product each, so nothing but the inputs' own bf16 is
 // rounded below fp32; sums are fp32, each warp's tensor-core chain a share of
-// the whole.  The order of every sum depends on the arguments alone (no
-// atomics).
+// the whole.  The order of every sum depends on the arguments alone (the only
+// atomics count tokens).
 #include <cuda_runtime.h>
 #include <atomic>
 #include <cstdint>
