@@ -6,9 +6,9 @@
 // read, with G = 4 a twentieth of what the tensor cores do meanwhile.  What
 // matters is that enough bytes are in flight and that nothing else stands in
 // their way.  64 sequences of up to 8192 tokens (half of that on average), 32
-// query heads to 8 of 128: 199 us from a bf16 cache, 94 % of the measured HBM
-// rate; 2 sequences of 131072 tokens 168 us, likewise.  A MixFP4 cache holds
-// 28 % of the bytes, and what is left to do is its decoding: 125 us (44 us of
+// query heads to 8 of 128: 197 us from a bf16 cache, 96 % of the measured HBM
+// rate; 2 sequences of 131072 tokens 166 us, likewise.  A MixFP4 cache holds
+// 28 % of the bytes, and what is left to do is its decoding: 124 us (44 us of
 // HBM time; of the first kernel's 120 us an instruction issues in 63 %, most of
 // them of the integer pipe, and the rest is waiting at 12 warps to an SM).
 //
@@ -34,7 +34,7 @@
 //     into equal shares of 64-token units, one per CTA; where a CTA's share ends
 //     inside a row's tokens, both sides leave a partial result (m, l, O) in the
 //     workspace, and a second small kernel, launched early, joins them in order
-//     (6.6 us of the 199).  Few rows that cannot be long take a cluster of CTAs
+//     (6.6 us of the 197).  Few rows that cannot be long take a cluster of CTAs
 //     each instead, joined in shared memory, and many short ones a CTA each: one
 //     sequence of 700 tokens 7 us, 40 of up to 120 9 us, 256 of up to 200 30 us.
 #include <cuda_runtime.h>
