@@ -73,6 +73,7 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // below 2^15 in f16, whose least value is then 2^-31 of the weight at m.
 constexpr float kSlack = 8.0f, kFp4Exp = 7.0f;
 constexpr float kNoScore = -3e38f;  // m where no token has been seen: no difference to a score or to itself is NaN
+constexpr float kMostScore = 3.402823466e38f;  // m of a score of +inf, whose weight is then +inf instead of NaN
 
 struct AttnArgs {
   const uint16_t* q;
@@ -253,6 +254,17 @@ __device__ __forceinline__ int2 seen(const AttnArgs& p, int b) {
 __device__ __forceinline__ int units(const AttnArgs& p, int2 r) {
   const int n = kUnit / p.together;
   return r.y > r.x ? kRowCost + (r.y - (r.x & ~15) + n - 1) / n : 0;
+}
+
+// A finished row's factor of O, and its log-sum-exp, of m and l.  l is 0 only where no token was seen (or all scores
+// are -inf); NaN goes through, and so does the +inf of a score of +inf.
+template <bool kFp4>
+__device__ __forceinline__ float out_factor(float l, float vts) {
+  return l == 0.0f ? 0.0f : (kFp4 ? 0.5f * vts : 1.0f) / l;
+}
+template <bool kFp4>
+__device__ __forceinline__ float lse_of(float m, float l) {
+  return l == 0.0f ? -INFINITY : (m + log2f(l) - (kFp4 ? kFp4Exp : 0.0f)) * kLn2;
 }
 
 // One output element pair of a finished row.
@@ -610,7 +622,7 @@ __global__ void __launch_bounds__(kThreads, Cfg<DT, NT, kFp4>::kCtas) paged_atte
             v = fmaxf(v, __shfl_xor_sync(kAll, v, 4));
             v = fmaxf(v, __shfl_xor_sync(kAll, v, 8));
             v = fmaxf(v, __shfl_xor_sync(kAll, v, 16));
-            v = fmaxf(m[n][j], v);
+            v = fminf(fmaxf(m[n][j], v), kMostScore);
             cor[j] = ex2(m[n][j] - v);  // 0 at the first score
             m[n][j] = v;
             l[n][j] *= cor[j];
@@ -723,11 +735,9 @@ __global__ void __launch_bounds__(kThreads, Cfg<DT, NT, kFp4>::kCtas) paged_atte
         *reinterpret_cast<float2*>(jo + h * DT + d) = make_float2(x, y);
         if (d == 0) *reinterpret_cast<float2*>(js + 2 * h) = make_float2(M, L);
       } else if (first && last) {
-        const float f = L > 0.0f ? (kFp4 ? 0.5f * vts : 1.0f) / L : 0.0f;
+        const float f = out_factor<kFp4>(L, vts);
         if (d < D) store_out(p, b, ho, d, x * f, y * f);
-        if (d == 0 && p.lse)
-          p.lse[(int64_t)b * p.q_heads + ho] =
-              L > 0.0f ? (M + log2f(L) - (kFp4 ? kFp4Exp : 0.0f)) * kLn2 : -INFINITY;
+        if (d == 0 && p.lse) p.lse[(int64_t)b * p.q_heads + ho] = lse_of<kFp4>(M, L);
       } else {
         *reinterpret_cast<float2*>(p.part + ((slot + w0) * C::kHeads + h) * DT + d) = make_float2(x, y);
         if (d == 0) p.stat[(slot + w0) * C::kHeads + h] = make_float2(M, L);
@@ -741,23 +751,23 @@ __global__ void __launch_bounds__(kThreads, Cfg<DT, NT, kFp4>::kCtas) paged_atte
         float2 st[kCluster], v[kCluster];
         float M = kNoScore, L = 0.0f, x = 0.0f, y = 0.0f;
 #pragma unroll
-        for (int q = 0; q < kCluster; ++q) {  // of fewer CTAs some twice, the second time with weight 0
+        for (int q = 0; q < kCluster; ++q) {  // of fewer CTAs some twice, the second time for nothing
           const int rank = q & (p.cluster - 1);
           st[q] = peer_load(js + 2 * h, rank), v[q] = peer_load(jo + h * DT + d, rank);
+          if (q >= p.cluster) st[q] = make_float2(kNoScore, 0.0f), v[q] = make_float2(0.0f, 0.0f);
         }
 #pragma unroll
         for (int q = 0; q < kCluster; ++q) M = fmaxf(M, st[q].x);
 #pragma unroll
         for (int q = 0; q < kCluster; ++q) {
-          const float f = q < p.cluster ? exp2f(st[q].x - M) : 0.0f;
+          const float f = exp2f(st[q].x - M);
           L += f * st[q].y;
           x += f * v[q].x;
           y += f * v[q].y;
         }
-        const float f = L > 0.0f ? (kFp4 ? 0.5f * vts : 1.0f) / L : 0.0f;
+        const float f = out_factor<kFp4>(L, vts);
         if (d < D) store_out(p, b, h0 + h, d, x * f, y * f);
-        if (d == 0 && p.lse)
-          p.lse[(int64_t)b * p.q_heads + h0 + h] = L > 0.0f ? (M + log2f(L) - (kFp4 ? kFp4Exp : 0.0f)) * kLn2 : -INFINITY;
+        if (d == 0 && p.lse) p.lse[(int64_t)b * p.q_heads + h0 + h] = lse_of<kFp4>(M, L);
       }
       cluster_barrier();  // no CTA leaves while others read its results
       return;
@@ -852,14 +862,13 @@ __global__ void __launch_bounds__(kJoinThreads) paged_attention_join_kernel(cons
     M = top;
   }
   if (h >= nh) return;
-  const float f = L > 0.0f ? (kFp4 ? 0.5f * *p.c.v_ts : 1.0f) / L : 0.0f;
+  const float f = out_factor<kFp4>(L, kFp4 ? *p.c.v_ts : 1.0f);
 #pragma unroll
   for (int j = 0; j < kV; ++j) {
     const int d = 2 * lane + 64 * j;
     if (d < p.c.head_dim) store_out(p, s.x, h0 + h, d, acc[j].x * f, acc[j].y * f);
   }
-  if (lane == 0 && p.lse)
-    p.lse[(int64_t)s.x * p.q_heads + h0 + h] = L > 0.0f ? (M + log2f(L) - (kFp4 ? kFp4Exp : 0.0f)) * kLn2 : -INFINITY;
+  if (lane == 0 && p.lse) p.lse[(int64_t)s.x * p.q_heads + h0 + h] = lse_of<kFp4>(M, L);
 }
 
 inline bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
