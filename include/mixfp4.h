@@ -540,8 +540,9 @@ int mixfp4_kv_gather(const mixfp4_kv_cache* cache, const int64_t* slots, int64_t
  * second product as two bf16 parts, or for a MixFP4 cache as f16 of 11 bits),
  * and out is rounded to bf16.  A sequence that sees no token gives out = 0 and
  * lse = -inf.  A score of NaN makes its head's out and lse NaN; one of +inf out
- * NaN and lse +inf.  The tokens' axis is cut over the GPU and joined, in an order
- * that depends on the arguments alone.
+ * NaN and lse +inf; an infinite element of V makes out infinite (NaN if its
+ * weight is below fp32's normal range).  The tokens' axis is cut over the GPU and
+ * joined, in an order that depends on the arguments alone.
  *
  * q            device, bf16: element d of head h of sequence b at
  *              b * q_stride + h * q_head_stride + d; 16-byte aligned, strides

@@ -25,8 +25,8 @@
 //     S's registers by an 8 x 8 transpose.  m16n8k16 moves these operands from
 //     registers; a tcgen05.mma would want them in shared memory in a layout that
 //     a paged row does not have.
-//   * The weights P keep 16 bits of mantissa in two bf16 parts (one product
-//     each) on a bf16 cache.  On a MixFP4 cache a row's values times its block
+//   * The weights P keep 16 bits of mantissa in two bf16 parts of one sign (one
+//     product each) on a bf16 cache.  On a MixFP4 cache a row's values times its block
 //     scales are exact in f16, Q is scaled per head by a power of two into f16
 //     (exact but for elements 2^-29 below the largest), and P takes 11 bits: the
 //     4-bit rows themselves hold 3.
@@ -644,11 +644,15 @@ __global__ void __launch_bounds__(kThreads, Cfg<DT, NT, kFp4>::kCtas) paged_atte
           ph[n][0] = transpose8(f16x2(w[0], w[1]));
           ph[n][1] = transpose8(f16x2(w[2], w[3]));
         } else {
-          const uint32_t a = bf16x2(w[0], w[1]), c = bf16x2(w[2], w[3]);
-          ph[n][0] = transpose8(a);
-          ph[n][1] = transpose8(c);
-          pl[n][0] = transpose8(bf16x2(w[0] - bf_lo(a), w[1] - bf_hi(a)));
-          pl[n][1] = transpose8(bf16x2(w[2] - bf_lo(c), w[3] - bf_hi(c)));
+          // The upper part by truncation, so that the lower is not negative, and not 0 either where the weight is not
+          // (2^-126 then): times an infinite element of V both give its infinity.
+          float low[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) low[e] = fmaxf(w[e] - bf_hi(__float_as_uint(w[e])), fminf(w[e], 0x1p-126f));
+          ph[n][0] = transpose8(prmt(__float_as_uint(w[0]), __float_as_uint(w[1]), 0x7632u));
+          ph[n][1] = transpose8(prmt(__float_as_uint(w[2]), __float_as_uint(w[3]), 0x7632u));
+          pl[n][0] = transpose8(bf16x2(low[0], low[1]));
+          pl[n][1] = transpose8(bf16x2(low[2], low[3]));
         }
       }
 

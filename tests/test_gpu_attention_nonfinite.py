@@ -2,9 +2,10 @@
 of the definition in 64 bits, NaN for NaN and sign for sign.
 
 A score of NaN makes a head's result and log-sum-exp NaN; one of +inf the result NaN and
-the log-sum-exp +inf; one of -inf has weight 0.  Only a sequence that sees
-nothing has a log-sum-exp of -inf here.  What stays finite keeps the bounds of
-test_gpu_paged_attention.py."""
+the log-sum-exp +inf; one of -inf has weight 0.  An infinite element of V
+makes its dimension infinite, two of different signs NaN.  Only a sequence that
+sees nothing has a log-sum-exp of -inf here.  What stays finite keeps the bounds of
+test_gpu_paged_attention.py; every weight here is above 2^-100 of the largest."""
 import math
 import os
 import sys
@@ -114,3 +115,18 @@ def test_scale_bytes(way, name):
     def spoil(q, cache, slots):
         put(cache, slots[len(slots) // 3], name + "_scales", 1, 2, 0x7F)
     attend(way, True, spoil)
+
+
+@pytest.mark.parametrize("way", WAYS)
+def test_values(way):
+    def spoil(q, cache, slots):
+        j = len(slots) // 2
+        put(cache, slots[0], "v", 0, 0, math.inf)
+        put(cache, slots[j], "v", 0, 64, -math.inf)
+        put(cache, slots[-1], "v", 1, 127, math.inf)
+        put(cache, slots[j], "v", 1, 3, math.inf)
+        put(cache, slots[j + 1], "v", 1, 3, -math.inf)
+        put(cache, slots[1], "v", 1, 50, math.nan)
+    ref, ls = attend(way, False, spoil)
+    assert ls.isfinite().all() and ref[:4, 0].isposinf().all() and ref[:4, 64].isneginf().all()
+    assert ref[4:, 127].isposinf().all() and ref[4:, [3, 50]].isnan().all() and int((~ref.isfinite()).sum()) == 4 * 5
