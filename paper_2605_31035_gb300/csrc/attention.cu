@@ -66,6 +66,11 @@ constexpr int kRowTokens = 256;
 // 4 / 8: 256 sequences of up to 200 tokens, 8 heads of 128, 58 / 46 / 41 / 39 us; 64 of up to 8192 on a MixFP4 cache
 // 149 / 146 / 146 / 149 us.
 constexpr int kRowCost = 6;
+// Tiles of 16 tokens after which a warp sets its O and l aside.  The tensor cores round a chain of sums towards zero,
+// some 2^-25 of the sum a link: a warp that walked 6000 tiles left O 2^-12 too small.  128 tiles (256 links) leave 2^-17,
+// for 1 % more bytes, in L2.  In memory the sums take no registers (O joined from registers: 64 sequences of up to 8192
+// tokens on a MixFP4 cache 136 to 140 us against 134).
+constexpr int kChain = 128;
 constexpr int kUnit = 64;  // head rows of a unit of work: 64 / together tokens of `together` key heads
 constexpr unsigned kAll = 0xFFFFFFFFu;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
@@ -94,6 +99,7 @@ struct AttnArgs {
   float* lse;
   float* part;    // [2 grid][together][8 NT][DT], the partial results
   float2* stat;   // [2 grid][together][8 NT] (m, l)
+  float4* aside;  // [grid][warps][NT][kAside][lane]: a warp's O and l so far, in rows of more than kChain tiles
   int4* split;    // rows that go on in later CTAs: (sequence, row, first CTA, last CTA); x < 0: none.  One place for
                   // each row of each sequence, or, where they are fewer, for each CTA, which begins one such row at most.
   int by_row;
@@ -123,6 +129,7 @@ struct Cfg {
     const int f = kFp4 ? (at * kPieces / 16 & (kPieces / 4 - 1)) * 4 : (at & 3) * 2;
     return at * kRow + (piece ^ f) * kCopy;
   }
+  static constexpr int kAside = 2 * (DT / 16) + 1;                     // places of 32 float4 for 8 query heads
   static constexpr int kKTile = 16 * kRow, kVTile = 16 * kRow;
   static constexpr int kScaleTile = kFp4 ? 32 * 16 : 0;                // 16 scale bytes a row at most
   static constexpr int kThere = kKTile + kVTile + kScaleTile;          // which of the tile's tokens there are, a bit each
@@ -360,6 +367,12 @@ __global__ void __launch_bounds__(kThreads, Cfg<DT, NT, kFp4>::kCtas) paged_atte
   }
 
   const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem) + warp * C::kStages * C::kStage;
+  // Reached in equal shares only: no cluster's or single CTA's part of a row has as many tiles.
+  static_assert(kChain * 16 * kWarps > 4 * kCtaTokens + 2 * kUnit && kChain * 16 > kRowTokens + 16);
+  auto aside = [&](int n) {  // of query heads 8n ..: the sum of O, m and l, the latest chain's O
+    const int64_t w = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5);
+    return p.aside + (w * NT + n) * (C::kAside * 32) + (threadIdx.x & 31);
+  };
   const float kts = kFp4 ? *p.c.k_ts : 1.0f, vts = kFp4 ? *p.c.v_ts : 1.0f;
 
   while (pos < end && b < p.B) {
@@ -539,154 +552,203 @@ __global__ void __launch_bounds__(kThreads, Cfg<DT, NT, kFp4>::kCtas) paged_atte
       for (int i = 0; i < DT / 16; ++i) o[n][i][0] = o[n][i][1] = o[n][i][2] = o[n][i][3] = 0.0f;
     }
 
-    for (int i = 0; i < tiles; ++i) {
-      __syncwarp();  // the stage about to be filled again has been read by every lane
-      if (i + C::kStages - 1 < tiles) issue(i + C::kStages - 1, put);
-      cp_commit();
-      cp_wait<C::kStages - 1>();
-      __syncwarp();
-      const uint32_t vs = src + C::kKTile;
-      const uint32_t ss = src + C::kKTile + C::kVTile;
-
-      const uint32_t there = lds32(src + C::kThere);
-      const bool ok0 = (there >> g) & 1u, ok1 = (there >> (g + 8)) & 1u;
-      // A MixFP4 tile's V codes and scale bytes, asked for before the scores so that neither waits for the other.
-      uint2 vc[kFp4 ? C::kVPieces : 1][4];
-      uint32_t vsc[kFp4 ? C::kVPieces : 1][4];
-      if constexpr (kFp4) {
-#pragma unroll
-        for (int k = 0; k < C::kVPieces; ++k)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const int tr = 2 * t + (r & 1) + 8 * (r >> 1);
-            vsc[k][r] = lds8(ss + (16 + tr) * 16 + (g + 8 * k) * C::kVDims / 16);
-            if constexpr (C::kVBytes == 8)
-              vc[k][r] = lds64(vs + C::v_place(tr, g + 8 * k));
-            else
-              vc[k][r].x = lds32(vs + C::v_place(tr, (g + 8 * k) / 2) + (g & 1) * C::kVBytes);
-          }
-      }
-
-      // ---- scores of 16 tokens x 8 NT heads, in two chains of products
-      float s[NT][4], s1[NT][4];
+    // A chain's end: O and l are put into memory and begin at 0; there, in fp32 and by few registers, they join the sums
+    // of the chains before.
+    auto set_aside = [&](bool more) {
 #pragma unroll
       for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s[n][e] = s1[n][e] = 0.0f;
-#pragma unroll
-      for (int k = 0; k < C::kKPieces; ++k) {
-        uint32_t w[2][C::kKDims / 2];  // rows g and g + 8
-#pragma unroll
-        for (int r = 0; r < 2; ++r) {
-          const uint32_t a = src + C::k_place(g, t + 4 * k) + 8 * r * C::kRow;
-          if constexpr (kFp4) {
-            const uint2 v = lds64(a);
-            const BlockScale f = block_scale(lds8(ss + (g + 8 * r) * 16 + t + 4 * k));
-            decode8(v.x, f.lo, f.hi, f.s2, w[r]);
-            decode8(v.y, f.lo, f.hi, f.s2, w[r] + 4);
-          } else {
-            const uint4 v = lds128(a);
-            w[r][0] = v.x, w[r][1] = v.y, w[r][2] = v.z, w[r][3] = v.w;
-          }
+        for (int k = 0; k < DT / 16; ++k) {
+          float* a = o[n][k];
+          aside(n)[((more ? DT / 16 + 1 : 0) + k) * 32] = make_float4(a[0], a[1], a[2], a[3]);
+          a[0] = a[1] = a[2] = a[3] = 0.0f;
         }
-#pragma unroll
-        for (int st = 0; st < C::kKDims / 4; ++st)
-#pragma unroll
-          for (int n = 0; n < NT; ++n)
-            mma16816<kFp4>(st & 1 ? s1[n] : s[n], w[0][2 * st], w[1][2 * st], w[0][2 * st + 1], w[1][2 * st + 1],
-                           qf[n][k * C::kKDims / 4 + st][0], qf[n][k * C::kKDims / 4 + st][1]);
-      }
-#pragma unroll
-      for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) s[n][e] += s1[n][e];
-
-      // ---- softmax: thread (g, t) has tokens g, g + 8 and heads 2t, 2t + 1.  The weights are 2^(s - m) for
-      // an m that follows the maximum from afar: it moves (and what was summed is scaled) when a score is
-      // kSlack above it, which takes a vote a tile instead of a maximum over the lanes.
-      uint32_t ph[NT][2], pl[NT][2];
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
-        bool far = false;
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          s[n][j] = ok0 ? s[n][j] * fs[n][j] : -INFINITY;
-          s[n][2 + j] = ok1 ? s[n][2 + j] * fs[n][j] : -INFINITY;
-          far = far || fmaxf(s[n][j], s[n][2 + j]) > m[n][j] + kSlack;
+        float4* sum = aside(n);
+        const float4* last = sum + (DT / 16 + 1) * 32;
+        float l0 = l[n][0], l1 = l[n][1];
+        l[n][0] = l[n][1] = 0.0f;
+        if (more) {
+          const float4 then = sum[DT / 16 * 32];
+          const float f0 = ex2(then.x - m[n][0]), f1 = ex2(then.y - m[n][1]);
+          l0 = fmaf(f0, then.z, l0), l1 = fmaf(f1, then.w, l1);
+#pragma unroll 1
+          for (int k = 0; k < DT / 16; ++k) {
+            const float4 v = sum[k * 32], w = last[k * 32];
+            sum[k * 32] = make_float4(fmaf(f0, v.x, w.x), fmaf(f1, v.y, w.y), fmaf(f0, v.z, w.z), fmaf(f1, v.w, w.w));
+          }
         }
-        if (__any_sync(kAll, far)) {
-          float cor[2];
+        sum[DT / 16 * 32] = make_float4(m[n][0], m[n][1], l0, l1);
+      }
+    };
+    int stop = min(tiles, kChain);  // of this chain's tiles
+    for (int i = 0; i < tiles;) {
+#pragma unroll 1
+      for (; i < stop; ++i) {
+        __syncwarp();  // the stage about to be filled again has been read by every lane
+        if (i + C::kStages - 1 < tiles) issue(i + C::kStages - 1, put);
+        cp_commit();
+        cp_wait<C::kStages - 1>();
+        __syncwarp();
+        const uint32_t vs = src + C::kKTile;
+        const uint32_t ss = src + C::kKTile + C::kVTile;
+
+        const uint32_t there = lds32(src + C::kThere);
+        const bool ok0 = (there >> g) & 1u, ok1 = (there >> (g + 8)) & 1u;
+        // A MixFP4 tile's V codes and scale bytes, asked for before the scores so that neither waits for the other.
+        uint2 vc[kFp4 ? C::kVPieces : 1][4];
+        uint32_t vsc[kFp4 ? C::kVPieces : 1][4];
+        if constexpr (kFp4) {
+#pragma unroll
+          for (int k = 0; k < C::kVPieces; ++k)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const int tr = 2 * t + (r & 1) + 8 * (r >> 1);
+              vsc[k][r] = lds8(ss + (16 + tr) * 16 + (g + 8 * k) * C::kVDims / 16);
+              if constexpr (C::kVBytes == 8)
+                vc[k][r] = lds64(vs + C::v_place(tr, g + 8 * k));
+              else
+                vc[k][r].x = lds32(vs + C::v_place(tr, (g + 8 * k) / 2) + (g & 1) * C::kVBytes);
+            }
+        }
+
+        // ---- scores of 16 tokens x 8 NT heads, in two chains of products
+        float s[NT][4], s1[NT][4];
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[n][e] = s1[n][e] = 0.0f;
+#pragma unroll
+        for (int k = 0; k < C::kKPieces; ++k) {
+          uint32_t w[2][C::kKDims / 2];  // rows g and g + 8
+#pragma unroll
+          for (int r = 0; r < 2; ++r) {
+            const uint32_t a = src + C::k_place(g, t + 4 * k) + 8 * r * C::kRow;
+            if constexpr (kFp4) {
+              const uint2 v = lds64(a);
+              const BlockScale f = block_scale(lds8(ss + (g + 8 * r) * 16 + t + 4 * k));
+              decode8(v.x, f.lo, f.hi, f.s2, w[r]);
+              decode8(v.y, f.lo, f.hi, f.s2, w[r] + 4);
+            } else {
+              const uint4 v = lds128(a);
+              w[r][0] = v.x, w[r][1] = v.y, w[r][2] = v.z, w[r][3] = v.w;
+            }
+          }
+#pragma unroll
+          for (int st = 0; st < C::kKDims / 4; ++st)
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+              mma16816<kFp4>(st & 1 ? s1[n] : s[n], w[0][2 * st], w[1][2 * st], w[0][2 * st + 1], w[1][2 * st + 1],
+                             qf[n][k * C::kKDims / 4 + st][0], qf[n][k * C::kKDims / 4 + st][1]);
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[n][e] += s1[n][e];
+
+        // ---- softmax: thread (g, t) has tokens g, g + 8 and heads 2t, 2t + 1.  The weights are 2^(s - m) for
+        // an m that follows the maximum from afar: it moves (and what was summed is scaled) when a score is
+        // kSlack above it, which takes a vote a tile instead of a maximum over the lanes.
+        uint32_t ph[NT][2], pl[NT][2];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          bool far = false;
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
-            float v = fmaxf(s[n][j], s[n][2 + j]);
-            v = fmaxf(v, __shfl_xor_sync(kAll, v, 4));
-            v = fmaxf(v, __shfl_xor_sync(kAll, v, 8));
-            v = fmaxf(v, __shfl_xor_sync(kAll, v, 16));
-            v = fminf(fmaxf(m[n][j], v), kMostScore);
-            cor[j] = ex2(m[n][j] - v);  // 0 at the first score
-            m[n][j] = v;
-            l[n][j] *= cor[j];
+            s[n][j] = ok0 ? s[n][j] * fs[n][j] : -INFINITY;
+            s[n][2 + j] = ok1 ? s[n][2 + j] * fs[n][j] : -INFINITY;
+            far = far || fmaxf(s[n][j], s[n][2 + j]) > m[n][j] + kSlack;
           }
+          if (__any_sync(kAll, far)) {
+            float cor[2];
 #pragma unroll
-          for (int k = 0; k < DT / 16; ++k) {
-            o[n][k][0] *= cor[0], o[n][k][1] *= cor[1], o[n][k][2] *= cor[0], o[n][k][3] *= cor[1];
+            for (int j = 0; j < 2; ++j) {
+              float v = fmaxf(s[n][j], s[n][2 + j]);
+              v = fmaxf(v, __shfl_xor_sync(kAll, v, 4));
+              v = fmaxf(v, __shfl_xor_sync(kAll, v, 8));
+              v = fmaxf(v, __shfl_xor_sync(kAll, v, 16));
+              v = fminf(fmaxf(m[n][j], v), kMostScore);
+              cor[j] = ex2(m[n][j] - v);  // 0 at the first score
+              m[n][j] = v;
+              l[n][j] *= cor[j];
+            }
+#pragma unroll
+            for (int k = 0; k < DT / 16; ++k) {
+              o[n][k][0] *= cor[0], o[n][k][1] *= cor[1], o[n][k][2] *= cor[0], o[n][k][3] *= cor[1];
+            }
           }
-        }
-        float w[4];
+          float w[4];
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const float top = m[n][j] - (kFp4 ? kFp4Exp : 0.0f);
-          w[j] = ex2(s[n][j] - top);
-          w[2 + j] = ex2(s[n][2 + j] - top);
-          l[n][j] += w[j] + w[2 + j];
-        }
-        if (kFp4) {
-          ph[n][0] = transpose8(f16x2(w[0], w[1]));
-          ph[n][1] = transpose8(f16x2(w[2], w[3]));
-        } else {
-          // The upper part by truncation, so that the lower is not negative, and not 0 either where the weight is not
-          // (2^-126 then): times an infinite element of V both give its infinity.
-          float low[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) low[e] = fmaxf(w[e] - bf_hi(__float_as_uint(w[e])), fminf(w[e], 0x1p-126f));
-          ph[n][0] = transpose8(prmt(__float_as_uint(w[0]), __float_as_uint(w[1]), 0x7632u));
-          ph[n][1] = transpose8(prmt(__float_as_uint(w[2]), __float_as_uint(w[3]), 0x7632u));
-          pl[n][0] = transpose8(bf16x2(low[0], low[1]));
-          pl[n][1] = transpose8(bf16x2(low[2], low[3]));
-        }
-      }
-
-      // ---- O^T += V^T P^T: rows g and g + 8 of product (k, j) are dimensions 2j, 2j + 1 of the thread's piece k
-#pragma unroll
-      for (int k = 0; k < C::kVPieces; ++k) {
-        uint32_t w[4][C::kVDims / 2];  // tokens 2t, 2t + 1, 2t + 8, 2t + 9
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          if constexpr (kFp4) {
-            const BlockScale f = block_scale(vsc[k][r]);
-            decode8(vc[k][r].x, f.lo, f.hi, f.s2, w[r]);
-            if constexpr (C::kVBytes == 8) decode8(vc[k][r].y, f.lo, f.hi, f.s2, w[r] + 4);
+          for (int j = 0; j < 2; ++j) {
+            const float top = m[n][j] - (kFp4 ? kFp4Exp : 0.0f);
+            w[j] = ex2(s[n][j] - top);
+            w[2 + j] = ex2(s[n][2 + j] - top);
+            l[n][j] += w[j] + w[2 + j];
+          }
+          if (kFp4) {
+            ph[n][0] = transpose8(f16x2(w[0], w[1]));
+            ph[n][1] = transpose8(f16x2(w[2], w[3]));
           } else {
-            const uint4 v = lds128(vs + C::v_place(2 * t + (r & 1) + 8 * (r >> 1), g + 8 * k));
-            w[r][0] = v.x, w[r][1] = v.y, w[r][2] = v.z, w[r][3] = v.w;
+            // The upper part by truncation, so that the lower is not negative, and not 0 either where the weight is not
+            // (2^-126 then): times an infinite element of V both give its infinity.
+            float low[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) low[e] = fmaxf(w[e] - bf_hi(__float_as_uint(w[e])), fminf(w[e], 0x1p-126f));
+            ph[n][0] = transpose8(prmt(__float_as_uint(w[0]), __float_as_uint(w[1]), 0x7632u));
+            ph[n][1] = transpose8(prmt(__float_as_uint(w[2]), __float_as_uint(w[3]), 0x7632u));
+            pl[n][0] = transpose8(bf16x2(low[0], low[1]));
+            pl[n][1] = transpose8(bf16x2(low[2], low[3]));
           }
         }
+
+        // ---- O^T += V^T P^T: rows g and g + 8 of product (k, j) are dimensions 2j, 2j + 1 of the thread's piece k
 #pragma unroll
-        for (int j = 0; j < C::kVDims / 2; ++j) {
-          const uint32_t a0 = prmt(w[0][j], w[1][j], 0x5410u), a1 = prmt(w[0][j], w[1][j], 0x7632u);
-          const uint32_t a2 = prmt(w[2][j], w[3][j], 0x5410u), a3 = prmt(w[2][j], w[3][j], 0x7632u);
+        for (int k = 0; k < C::kVPieces; ++k) {
+          uint32_t w[4][C::kVDims / 2];  // tokens 2t, 2t + 1, 2t + 8, 2t + 9
 #pragma unroll
-          for (int n = 0; n < NT; ++n) {
-            float* acc = o[n][k * C::kVDims / 2 + j];
-            mma16816<kFp4>(acc, a0, a1, a2, a3, ph[n][0], ph[n][1]);
-            if (!kFp4) mma16816<kFp4>(acc, a0, a1, a2, a3, pl[n][0], pl[n][1]);
+          for (int r = 0; r < 4; ++r) {
+            if constexpr (kFp4) {
+              const BlockScale f = block_scale(vsc[k][r]);
+              decode8(vc[k][r].x, f.lo, f.hi, f.s2, w[r]);
+              if constexpr (C::kVBytes == 8) decode8(vc[k][r].y, f.lo, f.hi, f.s2, w[r] + 4);
+            } else {
+              const uint4 v = lds128(vs + C::v_place(2 * t + (r & 1) + 8 * (r >> 1), g + 8 * k));
+              w[r][0] = v.x, w[r][1] = v.y, w[r][2] = v.z, w[r][3] = v.w;
+            }
+          }
+#pragma unroll
+          for (int j = 0; j < C::kVDims / 2; ++j) {
+            const uint32_t a0 = prmt(w[0][j], w[1][j], 0x5410u), a1 = prmt(w[0][j], w[1][j], 0x7632u);
+            const uint32_t a2 = prmt(w[2][j], w[3][j], 0x5410u), a3 = prmt(w[2][j], w[3][j], 0x7632u);
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+              float* acc = o[n][k * C::kVDims / 2 + j];
+              mma16816<kFp4>(acc, a0, a1, a2, a3, ph[n][0], ph[n][1]);
+              if (!kFp4) mma16816<kFp4>(acc, a0, a1, a2, a3, pl[n][0], pl[n][1]);
+            }
           }
         }
+        put = src;
+        src = src + C::kStage == behind ? ring : src + C::kStage;
       }
-      put = src;
-      src = src + C::kStage == behind ? ring : src + C::kStage;
+      if (stop < tiles) set_aside(stop > kChain);
+      stop = min(tiles, stop + kChain);
     }
     cp_wait<0>();
+    if (tiles > kChain) {
+      set_aside(true);
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+#pragma unroll
+        for (int k = 0; k < DT / 16; ++k) {
+          const float4 v = aside(n)[k * 32];
+          o[n][k][0] = v.x, o[n][k][1] = v.y, o[n][k][2] = v.z, o[n][k][3] = v.w;
+        }
+        const float4 v = aside(n)[DT / 16 * 32];
+        l[n][0] = v.z, l[n][1] = v.w;
+      }
+    }
 
     // ---- the warps' results joined in shared memory (the ring is drained)
     __syncthreads();
@@ -885,6 +947,10 @@ inline int padded_heads(const mixfp4_kv_cache* c, int64_t q_heads) {
   const int64_t group = q_heads / c->heads;
   return group <= 8 ? 8 : (group <= 16 || c->head_dim > 128 || (group + 15) / 16 == (group + 23) / 24 ? 16 : 24);
 }
+// What a CTA of the first kernel may set aside.
+inline int64_t aside_bytes(const mixfp4_kv_cache* c, int64_t q_heads) {
+  return (int64_t)kWarps * (padded_heads(c, q_heads) / 8) * (padded_dim(c->head_dim) / 16 * 2 + 1) * 32 * 16;
+}
 // Key heads of a CTA.  Where the heads of a token lie together, neighbouring heads' rows are asked for at the same
 // time (64 sequences of up to 8192 tokens, 8 heads of 128: MixFP4 162 us against 185 us with one head to a CTA, whose
 // 8 scale bytes of a row cost a whole access; 32 bf16 heads of 128: 91 against 111 us).  Where a head's tokens lie
@@ -973,7 +1039,8 @@ int mixfp4_paged_attention_workspace(const mixfp4_kv_cache* cache, int64_t B, in
   *bytes = 0;
   if (B == 0 || q_heads == 0) return MIXFP4_OK;
   const int64_t grid = grid_of(cache, q_heads), heads = padded_heads(cache, q_heads) * 4;  // at most 4 together
-  *bytes = (grid * 16 + 255) / 256 * 256 + 2 * grid * heads * 8 + 2 * grid * heads * padded_dim(cache->head_dim) * 4;
+  *bytes = (grid * 16 + 255) / 256 * 256 + grid * aside_bytes(cache, q_heads) + 2 * grid * heads * 8 +
+           2 * grid * heads * padded_dim(cache->head_dim) * 4;
   return MIXFP4_OK;
 }
 
@@ -1030,6 +1097,8 @@ int mixfp4_paged_attention(const void* q, int64_t q_stride, int64_t q_head_strid
   uint8_t* w = static_cast<uint8_t*>(workspace);
   p.split = reinterpret_cast<int4*>(w);
   w += ((int64_t)grid * 16 + 255) / 256 * 256;
+  p.aside = reinterpret_cast<float4*>(w);
+  w += grid * aside_bytes(cache, q_heads);
   p.stat = reinterpret_cast<float2*>(w);
   p.part = reinterpret_cast<float*>(w + 2 * (int64_t)grid * p.together * heads * 8);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
