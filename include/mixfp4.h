@@ -579,7 +579,8 @@ int mixfp4_paged_attention_workspace(const mixfp4_kv_cache* cache, int64_t B, in
  * projection (mixfp4_linear; no counterpart in the paper): for the tokens t of
  * segment i, with its adapter j = ids[i],
  *   u_t = A_j x_t,   out_t = base_t + scaling_j B_j u_t.
- * Products are exact, u and all sums fp32.  A segment whose id is outside
+ * Products are exact, u and all sums fp32 (infinities and NaN as the formula
+ * gives them).  A segment whose id is outside
  * 0 .. adapters - 1 (-1) has no adapter: u = 0, out = base.
  *
  * x, dtype     device, bf16 (MIXFP4_DTYPE_BF16) [T][ldx]; 32-byte aligned, ldx % 16 == 0.

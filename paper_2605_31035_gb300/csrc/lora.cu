@@ -47,18 +47,24 @@ __device__ __forceinline__ void mma_bf16(float d[4], uint32_t a0, uint32_t a1, u
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ uint32_t bf16x2(float lo, float hi) {
-  uint32_t d;
-  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
-  return d;
+// x, an infinity or NaN as the largest number of its sign.
+__device__ __forceinline__ float finite(float x) {
+  float y;
+  asm("min.xorsign.abs.f32 %0, %1, %2;" : "=f"(y) : "f"(x), "f"(3.402823466e38f));
+  return y;
 }
-// A pair of fp32 as three pairs of bf16 whose sum it is (to 24 bits).
+// A pair of fp32 as three pairs of bf16 whose sum it is (to 24 bits).  Each part is what the upper 16 bits hold of the
+// rest, so all three have the number's sign, and the two lower ones, which 2^-32 of it is added to, are 0 only where it is 0
+// (or below 2^-101): of an infinity they are finite, and times an infinity they give that same one.
 __device__ __forceinline__ void split3(float lo, float hi, uint32_t w[3]) {
+  w[0] = prmt(__float_as_uint(lo), __float_as_uint(hi), 0x7632u);
+  lo = finite(lo), hi = finite(hi);
+  float l = lo, h = hi;
 #pragma unroll
-  for (int i = 0; i < 3; ++i) {
-    w[i] = bf16x2(lo, hi);
-    lo = __fsub_rn(lo, __uint_as_float(w[i] << 16));
-    hi = __fsub_rn(hi, __uint_as_float(w[i] & 0xFFFF0000u));
+  for (int i = 1; i < 3; ++i) {
+    l = __fmaf_rn(lo, 0x1p-32f, __fsub_rn(l, __uint_as_float(__float_as_uint(l) & 0xFFFF0000u)));
+    h = __fmaf_rn(hi, 0x1p-32f, __fsub_rn(h, __uint_as_float(__float_as_uint(h) & 0xFFFF0000u)));
+    w[i] = prmt(__float_as_uint(l), __float_as_uint(h), 0x7632u);
   }
 }
 
