@@ -43,7 +43,7 @@ typedef enum {
   MIXFP4_ERR_DTYPE = -4,   /* unsupported input dtype */
   MIXFP4_ERR_CUDA = -5,    /* a CUDA runtime call or launch failed */
   MIXFP4_ERR_TIMEOUT = -6, /* a bounded device-side wait gave up (see status_word) */
-  MIXFP4_ERR_ARG = -7      /* an enum argument is out of range */
+  MIXFP4_ERR_ARG = -7      /* an enum argument is out of range, or buffers overlap that must not */
 } mixfp4_status;
 
 enum { MIXFP4_MODE_MIX = 0,        /* Alg. 1: per-block E2M1/E1M2 by lower MSE */
@@ -507,7 +507,9 @@ typedef struct {
  *              rot_dim is even, 0 .. head_dim.
  * slots        device, int64 [T]: where token t goes.  A slot outside the cache (-1
  *              for a padding token) keeps nothing.  Slots of one call differ.
- * q_out        device, bf16 [T][q_heads][head_dim], 32-byte aligned.       (output)
+ * q_out        device, bf16 [T][q_heads][head_dim], 32-byte aligned; may be q (bf16
+ *              and dense) if the rotation is interleaved or rot_dim % 32 == 0, else
+ *              overlaps none of q, k and v (MIXFP4_ERR_ARG).               (output)
  * mode         MIXFP4_MODE_* of a MixFP4 cache's blocks.
  * A token whose position is outside the table keeps nothing, and its rotated
  * query is NaN.

@@ -13,7 +13,7 @@
 
 #include <cmath>
 
-#include "mixfp4.h"
+#include "kvcache.cuh"
 
 namespace {
 
@@ -176,6 +176,13 @@ PyObject* kv_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
       }
     }
     const bool interleaved = truth(a[8]);
+    if (given(a[10]) && qp &&
+        mixfp4::append_overlaps(qp, qt, qh, H, k.const_data_ptr(), k.stride(0), k.stride(1), v.const_data_ptr(),
+                                v.stride(0), v.stride(1),
+                                type == ScalarType::Float ? MIXFP4_DTYPE_F32 : MIXFP4_DTYPE_BF16, T, rot, interleaved,
+                                c->heads, D, out.const_data_ptr()))
+      refuse("%s must not overlap k, v or q (it may be q itself, bf16 and dense, if the rotation is interleaved or over "
+             "a multiple of 32 elements)", "out");
     const int mode = (int)integer(a[9]);
     void* stream = stream_of(a[11]);
     int st;

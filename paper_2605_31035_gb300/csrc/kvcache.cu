@@ -387,6 +387,10 @@ int mixfp4_kv_append(const void* q, int64_t q_token_stride, int64_t q_head_strid
   if (q_heads > 0 && (!aligned(q, 32) || !aligned(q_out, 32) || q_token_stride % 16 || q_head_stride % 16))
     return MIXFP4_ERR_ALIGN;
   if (rot_dim > 0 && (!aligned(positions, 8) || !aligned(cos_sin, 32))) return MIXFP4_ERR_ALIGN;
+  if (q_heads > 0 && append_overlaps(q, q_token_stride, q_head_stride, q_heads, k, k_token_stride, k_head_stride, v,
+                                     v_token_stride, v_head_stride, dtype, T, rot_dim, interleaved != 0, cache->heads,
+                                     cache->head_dim, q_out))
+    return MIXFP4_ERR_ARG;
 
   AppendArgs p = {};
   p.src[0] = q, p.src[1] = k, p.src[2] = v;
@@ -396,7 +400,7 @@ int mixfp4_kv_append(const void* q, int64_t q_token_stride, int64_t q_head_strid
   p.tokens = T;
   p.positions = positions, p.cos_sin = cos_sin, p.max_positions = max_positions;
   p.rot = (int)rot_dim, p.interleaved = interleaved != 0;
-  p.paired = !p.interleaved && rot_dim > 0 && rot_dim % 32 == 0;
+  p.paired = !p.interleaved && rot_dim > 0 && owns_pairs(rot_dim, false);
   p.c = *cache;
   p.slots = slots;
   p.q_out = static_cast<uint16_t*>(q_out);

@@ -818,7 +818,8 @@ def mixfp4_kv_append(k: torch.Tensor, v: torch.Tensor, cache: KVCache, slots: to
     With cos_sin (float32 [positions, rot_dim]: cosines, then sines) and positions
     (int64 [T]; not looked at without) keys, and queries q [T, q_heads, head_dim] of the same dtype, are
     rotated on the way: pairs (i, i + rot_dim / 2), or (2i, 2i + 1) if interleaved.
-    Returns the (rotated) queries as bf16 [T, q_heads, head_dim], or None."""
+    Returns the (rotated) queries as bf16 [T, q_heads, head_dim], or None.
+    out: their memory; may be q (bf16, dense) if interleaved or rot_dim % 32 == 0, and overlaps no input else."""
     _check_cache(cache)
     if stream is not None and q is not None and out is None:
         out = _result(_shape(q, 3), torch.bfloat16, cache.device, stream)
