@@ -459,7 +459,7 @@ int mixfp4_quantize_noalloc(const void* x, int dtype, int64_t rows, int64_t K, i
  * strides (block d / 16).  A slot is p * page_size + o.
  *
  * dtype        MIXFP4_CACHE_BF16 or MIXFP4_CACHE_MIXFP4.
- * page_size    tokens of a page, >= 1.    heads  key heads, >= 1.
+ * page_size    tokens of a page, >= 1.    heads  key heads, 1 .. 2^20.
  * head_dim     a multiple of 16, 16 .. 256.    pages  >= 0.
  * k, v         device, bf16 (32-byte aligned, strides multiples of 16 elements)
  *              or uint8 codes (8-byte aligned, strides multiples of 8 bytes).
@@ -501,7 +501,7 @@ typedef struct {
  *              linear layer returns): element d of head h of token t at
  *              t * token stride + h * head stride + d; 32-byte aligned, strides
  *              multiples of 16 elements.  q = NULL: no queries (q_heads 0).
- * T            tokens, >= 0.
+ * T            tokens, >= 0.    q_heads  0 .. 2^20.
  * positions    device, int64 [T]; cos_sin  device, float [max_positions][rot_dim],
  *              32-byte aligned; both unused with rot_dim = 0 (no rotation).
  *              rot_dim is even, 0 .. head_dim.

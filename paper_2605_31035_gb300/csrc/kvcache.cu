@@ -337,8 +337,9 @@ void launch_append(const AppendArgs& p, int mode, int64_t blocks, cudaStream_t s
 int check_kv_cache(const mixfp4_kv_cache* c) {
   if (!c) return MIXFP4_ERR_NULL;
   if (c->dtype != MIXFP4_CACHE_BF16 && c->dtype != MIXFP4_CACHE_MIXFP4) return MIXFP4_ERR_DTYPE;
-  if (c->page_size < 1 || c->heads < 1 || c->head_dim < 16 || c->head_dim > 256 || c->head_dim % 16 != 0 ||
-      c->pages < 0 || c->pages > INT32_MAX || c->page_stride < 0 || c->token_stride < 0 || c->head_stride < 0)
+  if (c->page_size < 1 || c->heads < 1 || c->heads > (1 << 20) || c->head_dim < 16 || c->head_dim > 256 ||
+      c->head_dim % 16 != 0 || c->pages < 0 || c->pages > INT32_MAX || c->page_stride < 0 ||
+      c->token_stride < 0 || c->head_stride < 0)
     return MIXFP4_ERR_SHAPE;
   const bool fp4 = c->dtype == MIXFP4_CACHE_MIXFP4;
   if (fp4 && (c->scale_page_stride < 0 || c->scale_token_stride < 0 || c->scale_head_stride < 0))
