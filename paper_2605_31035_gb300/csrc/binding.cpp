@@ -59,6 +59,9 @@ const Tensor& heads(PyObject* o, ScalarType type, int64_t H, int64_t D, int64_t 
   return *t;
 }
 
+// The stride of an axis; 0 where it has one element, whose stride leads nowhere and may be anything.
+int64_t step(const Tensor& t, int axis) { return t.size(axis) == 1 ? 0 : t.stride(axis); }
+
 const Tensor& vector(PyObject* o, ScalarType type, int64_t n, int64_t index, const char* what) {
   const Tensor* t = tensor(o);
   if (!on(t, index) || t->scalar_type() != type || t->dim() != 1 || t->size(0) != n || (n > 1 && t->stride(0) != 1))
@@ -68,14 +71,14 @@ const Tensor& vector(PyObject* o, ScalarType type, int64_t n, int64_t index, con
   return *t;
 }
 
-// [rows, cols], dense along a row; its row stride, at least cols, goes to ld.
+// [rows, cols], dense along a row; its row stride, at least cols, goes to ld (cols where there is one row).
 const Tensor& rows(PyObject* o, ScalarType type, int64_t n, int64_t cols, int64_t index, const char* what,
                    int64_t* ld) {
   const Tensor* t = tensor(o);
   bool ok = on(t, index) && t->scalar_type() == type && t->dim() == 2 && t->size(0) == n && t->size(1) == cols &&
             (t->stride(1) == 1 || cols <= 1);
   if (ok) {
-    *ld = n <= 1 ? std::max(t->stride(0), cols) : t->stride(0);
+    *ld = n <= 1 ? cols : t->stride(0);
     ok = *ld >= cols;
   }
   if (!ok)
@@ -166,7 +169,7 @@ PyObject* kv_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (given(a[5])) {
       const Tensor& q = heads(a[5], type, -1, D, index, "q");
       if (q.size(0) != T) refuse("%s must have as many tokens as k", "q");
-      H = q.size(1), qt = q.stride(0), qh = q.stride(1), qp = q.const_data_ptr();
+      H = q.size(1), qt = step(q, 0), qh = step(q, 1), qp = q.const_data_ptr();
       if (given(a[10])) {
         out = heads(a[10], ScalarType::BFloat16, H, D, index, "out");
         if (out.size(0) != T) refuse("%s must have as many tokens as q", "out");
@@ -177,8 +180,8 @@ PyObject* kv_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
     }
     const bool interleaved = truth(a[8]);
     if (given(a[10]) && qp &&
-        mixfp4::append_overlaps(qp, qt, qh, H, k.const_data_ptr(), k.stride(0), k.stride(1), v.const_data_ptr(),
-                                v.stride(0), v.stride(1),
+        mixfp4::append_overlaps(qp, qt, qh, H, k.const_data_ptr(), step(k, 0), step(k, 1), v.const_data_ptr(),
+                                step(v, 0), step(v, 1),
                                 type == ScalarType::Float ? MIXFP4_DTYPE_F32 : MIXFP4_DTYPE_BF16, T, rot, interleaved,
                                 c->heads, D, out.const_data_ptr()))
       refuse("%s must not overlap k, v or q (it may be q itself, bf16 and dense, if the rotation is interleaved or over "
@@ -188,8 +191,8 @@ PyObject* kv_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
     int st;
     {
       Unlocked unlocked;
-      st = mixfp4_kv_append(qp, qt, qh, H, k.const_data_ptr(), k.stride(0), k.stride(1), v.const_data_ptr(),
-                            v.stride(0), v.stride(1),
+      st = mixfp4_kv_append(qp, qt, qh, H, k.const_data_ptr(), step(k, 0), step(k, 1), v.const_data_ptr(), step(v, 0),
+                            step(v, 1),
                             type == ScalarType::Float ? MIXFP4_DTYPE_F32 : MIXFP4_DTYPE_BF16, T, positions, angles,
                             table, rot, interleaved, c, slots.const_data_ptr<int64_t>(),
                             out.defined() ? out.mutable_data_ptr() : nullptr, mode, stream);
@@ -288,8 +291,8 @@ PyObject* paged_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
     int st;
     {
       Unlocked unlocked;
-      st = mixfp4_paged_attention(q.const_data_ptr(), q.stride(0), q.stride(1), B, H, c,
-                                  table->const_data_ptr<int32_t>(), std::max(table->stride(0), pages), pages,
+      st = mixfp4_paged_attention(q.const_data_ptr(), step(q, 0), step(q, 1), B, H, c,
+                                  table->const_data_ptr<int32_t>(), std::max(step(*table, 0), pages), pages,
                                   lengths.const_data_ptr<int32_t>(), scale, window, out.mutable_data_ptr(),
                                   lse.defined() ? lse.mutable_data_ptr<float>() : nullptr,
                                   workspace.mutable_data_ptr(), need, stream);

@@ -713,6 +713,13 @@ def linear(x: torch.Tensor, w_q: QTensor, mode: int = MODE_MIX, stream=None,
 # ---- paged key-value cache and attention ---------------------------------------
 
 
+def _cache_strides(t):
+    """Page, token and head stride.  That of an axis with one element leads nowhere and may be anything: it is taken
+    as 0, and a token's in pages of one token as its page's."""
+    page, token, head = (s if n > 1 else 0 for n, s in zip(t.shape, t.stride()[:3]))
+    return page, token if t.shape[1] > 1 else page, head
+
+
 class KVCache:
     """One layer's paged cache of keys and values (struct mixfp4_kv_cache).
 
@@ -737,21 +744,24 @@ class KVCache:
         D = k.shape[3] * (2 if fp4 else 1)
         _require(D % 16 == 0 and 16 <= D <= 256, "head_dim must be a multiple of 16 up to 256")
         _require(k.shape[1] >= 1 and k.shape[2] >= 1, "page_size and heads must be at least 1")
-        _require(k.stride() == v.stride() and k.stride(3) == 1, "k and v must share their strides, the last of them 1")
+        strides = _cache_strides(k)
+        _require(strides == _cache_strides(v) and k.stride(3) == v.stride(3) == 1,
+                 "k and v must share their strides, the last of them 1")
         self.k, self.v, self.k_scales, self.v_scales, self.k_ts, self.v_ts = k, v, k_scales, v_scales, k_ts, v_ts
         c = _CKVCache(CACHE_MIXFP4 if fp4 else CACHE_BF16, k.shape[1], k.shape[2], D, k.shape[0], _ptr(k), _ptr(v),
-                      k.stride(0), k.stride(1), k.stride(2))
+                      *strides)
         if fp4:
             for t, what in ((k_scales, "k_scales"), (v_scales, "v_scales")):
                 _check_dev(t, k.device, what)
                 _require(t.dtype is torch.uint8 and t.shape == (*k.shape[:3], D // 16),
                          f"{what} must be a uint8 tensor [pages, page_size, heads, head_dim / 16]")
-            _require(k_scales.stride() == v_scales.stride() and (k_scales.stride(3) == 1 or D == 16),
+            strides = _cache_strides(k_scales)
+            _require(strides == _cache_strides(v_scales) and (k_scales.stride(3) == v_scales.stride(3) == 1 or D == 16),
                      "k_scales and v_scales must share their strides, the last of them 1")
             for t, what in ((k_ts, "k_ts"), (v_ts, "v_ts")):
                 _check_scalar_f32(t, k.device, what)
             c.k_scales, c.v_scales, c.k_ts, c.v_ts = _ptr(k_scales), _ptr(v_scales), _ptr(k_ts), _ptr(v_ts)
-            c.scale_page_stride, c.scale_token_stride, c.scale_head_stride = k_scales.stride()[:3]
+            c.scale_page_stride, c.scale_token_stride, c.scale_head_stride = strides
         else:
             _require(v_scales is None and k_ts is None and v_ts is None, "a bf16 cache has no scales")
         self._c = c
