@@ -20,6 +20,7 @@ CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libmixfp4.so")
 BINDING = os.path.join(HERE, "_binding.so")
+BINDING_ABI = os.path.join(HERE, "_binding.abi")  # what _binding.so was compiled for
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 
 SOURCES = ["api.cu", "quantize.cu", "train.cu", "gemm.cu", "gemm_f16a.cu", "fewrows.cu", "native.cu", "candidates.cu", "noalloc.cu", "selftest.cu",
@@ -43,8 +44,24 @@ def _deps():
     return files
 
 
+def abi() -> str:
+    """The Python and the torch that a compiled binding belongs to."""
+    import torch
+    return f"{sysconfig.get_config_var('SOABI')} torch {torch.__version__} cxx11 {int(torch._C._GLIBCXX_USE_CXX11_ABI)}\n"
+
+
+def binding_fits() -> bool:
+    """Whether _binding.so was compiled for this Python and this torch: one for others may fail to load, or read tensors by
+    another layout."""
+    try:
+        with open(BINDING_ABI) as f:
+            return f.read() == abi()
+    except OSError:
+        return False
+
+
 def up_to_date() -> bool:
-    if not (os.path.exists(LIB) and os.path.exists(BINDING)):
+    if not (os.path.exists(LIB) and os.path.exists(BINDING) and binding_fits()):
         return False
     t = min(os.path.getmtime(LIB), os.path.getmtime(BINDING))
     return all(os.path.getmtime(f) <= t for f in _deps())
@@ -83,7 +100,12 @@ def _link_binding(obj: str):
     res = subprocess.run(cmd, capture_output=True, text=True)
     if res.returncode != 0:
         raise RuntimeError(f"link of the binding failed:\n{res.stderr}")
+    if os.path.exists(BINDING_ABI):
+        os.remove(BINDING_ABI)  # never one module's beside another
     os.replace(tmp, BINDING)
+    with open(BINDING_ABI + f".tmp{os.getpid()}", "w") as f:
+        f.write(abi())
+    os.replace(f.name, BINDING_ABI)
 
 
 def build(force: bool = False, verbose: bool = False) -> str:

@@ -118,6 +118,10 @@ def _native():
         if not os.path.exists(_BINDING_PATH):
             raise RuntimeError(
                 f"{_BINDING_PATH} is missing: build it with `python -c 'import __graft_entry__ as g; g.build()'`")
+        from . import build
+        if not build.binding_fits():
+            raise RuntimeError(f"{_BINDING_PATH} was not built for {build.abi().strip()}: build it again with "
+                               "`python -c 'import __graft_entry__ as g; g.build()'`")
         from importlib import machinery, util
         loader = machinery.ExtensionFileLoader("_binding", _BINDING_PATH)
         _binding = util.module_from_spec(util.spec_from_file_location("_binding", _BINDING_PATH, loader=loader))
