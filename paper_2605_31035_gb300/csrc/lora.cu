@@ -262,8 +262,7 @@ template <int RT, int TT, bool kTrans>
 __global__ void __launch_bounds__(kThreads, 2) lora_shrink_kernel(const ShrinkArgs p) {
   extern __shared__ float part[];  // [warps][16 RT][TT], then the CTA's sum in the first
   constexpr int kOut = 16 * RT * TT;
-  griddep_wait();  // `in` may be what the kernel before it on the stream writes
-  griddep_launch_dependents();
+  griddep_launch_dependents();  // launched plainly: what comes before it on the stream is done
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
   const int split = (int)(blockIdx.x % p.splits);
   constexpr bool kRows = TT == 8;
@@ -745,32 +744,30 @@ int64_t tiles_of(const Segments& s, int size, bool rows) {
 }
 
 template <int RT, int TT, bool kTrans>
-int launch_shrink(const ShrinkArgs& p, bool dependent, cudaStream_t s) {
+int launch_shrink(const ShrinkArgs& p, cudaStream_t s) {
   const int smem = kWarps * 16 * RT * TT * 4;
   auto* kernel = lora_shrink_kernel<RT, TT, kTrans>;
   static std::atomic<uint64_t> done{0};
   if (smem > 48 * 1024 && !set_dynamic_smem_once(reinterpret_cast<const void*>(kernel), smem, done))
     return MIXFP4_ERR_CUDA;
   const int64_t tiles = tiles_of(p.seg, TT, TT == 8);
-  cudaLaunchAttribute attr[2];
+  cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = (unsigned)p.splits, attr[0].val.clusterDim.y = 1, attr[0].val.clusterDim.z = 1;
-  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[1].val.programmaticStreamSerializationAllowed = 1;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(tiles * p.splits), (unsigned)((p.R + 16 * RT - 1) / (16 * RT)));
   cfg.blockDim = dim3(kThreads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = s;
   cfg.attrs = attr;
-  cfg.numAttrs = dependent ? 2 : 1;
+  cfg.numAttrs = 1;
   return cudaLaunchKernelEx(&cfg, kernel, p) == cudaSuccess ? MIXFP4_OK : MIXFP4_ERR_CUDA;
 }
 
 // Tiles of 8 tokens where segments are short, of 32 else: 256 requests of one token 46 us against 52 with 32 (before
 // grouping), 4096 tokens of one segment 160 against 206 with 8.
 template <bool kTrans>
-int shrink(ShrinkArgs p, bool dependent, cudaStream_t s) {
+int shrink(ShrinkArgs p, cudaStream_t s) {
   const bool few = p.seg.tokens <= 8 * (int64_t)p.seg.count;
   const int64_t tiles = few ? tiles_of(p.seg, 8, true) : tiles_of(p.seg, 32, false);
   // Ranks of a CTA: 16, or 32 (x is read again for every 32 ranks, from L2; 64 in one CTA left registers for
@@ -780,8 +777,8 @@ int shrink(ShrinkArgs p, bool dependent, cudaStream_t s) {
   const int64_t ctas = tiles * ((p.R + 16 * rt - 1) / (16 * rt));
   p.splits = 1;
   while (p.splits < 8 && ctas * p.splits <= num_sms() && p.kdim >= 128 * kWarps * p.splits) p.splits *= 2;
-  if (few) return rt == 1 ? launch_shrink<1, 8, kTrans>(p, dependent, s) : launch_shrink<2, 8, kTrans>(p, dependent, s);
-  return rt == 1 ? launch_shrink<1, 32, kTrans>(p, dependent, s) : launch_shrink<2, 32, kTrans>(p, dependent, s);
+  if (few) return rt == 1 ? launch_shrink<1, 8, kTrans>(p, s) : launch_shrink<2, 8, kTrans>(p, s);
+  return rt == 1 ? launch_shrink<1, 32, kTrans>(p, s) : launch_shrink<2, 32, kTrans>(p, s);
 }
 
 template <int TT, bool kTrans, int kHeld, int NP>
@@ -878,7 +875,7 @@ int mixfp4_lora(const void* x, int dtype, int64_t T, int64_t K, int64_t ldx, con
   const Segments seg{starts, ids, (int)segments, (int)adapters, T, grouped(T, adapters, segments)};
   const ShrinkArgs sp{static_cast<const uint16_t*>(x), ldx, static_cast<const uint16_t*>(a), nullptr, u, K,
                       (int)R, 1, seg};
-  if (int st = shrink<false>(sp, false, s)) return st;
+  if (int st = shrink<false>(sp, s)) return st;
   if (N == 0) return MIXFP4_OK;
   const ExpandArgs ep{u, static_cast<const uint16_t*>(b), scaling, base, ld_base, out, ld_out, N, (int)R,
                       vec_ok(out, ld_out) && (!base || vec_ok(base, ld_base)), seg};
@@ -905,7 +902,7 @@ int mixfp4_lora_backward(const void* dy, int64_t ldy, const void* x, int64_t ldx
   if (tokens) {
     const ShrinkArgs sp{static_cast<const uint16_t*>(dy), ldy, static_cast<const uint16_t*>(b), scaling, v, N,
                         (int)R, 1, seg};
-    if (int st = shrink<true>(sp, false, s)) return st;
+    if (int st = shrink<true>(sp, s)) return st;
     if (K > 0) {
       const ExpandArgs ep{v, static_cast<const uint16_t*>(a), nullptr, base, ld_base, dx, ld_dx, K, (int)R,
                           vec_ok(dx, ld_dx) && (!base || vec_ok(base, ld_base)), seg};
