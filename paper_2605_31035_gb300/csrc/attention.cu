@@ -6,10 +6,10 @@
 // read, with G = 4 a twentieth of what the tensor cores do meanwhile.  What
 // matters is that enough bytes are in flight and that nothing else stands in
 // their way.  64 sequences of up to 8192 tokens (half of that on average), 32
-// query heads to 8 of 128: 197 us from a bf16 cache, 96 % of the measured HBM
-// rate; 2 sequences of 131072 tokens 166 us, likewise.  A MixFP4 cache holds
+// query heads to 8 of 128: 200 us from a bf16 cache, 94 % of the measured HBM
+// rate; 2 sequences of 131072 tokens 168 us, likewise.  A MixFP4 cache holds
 // 28 % of the bytes, and what is left to do is its decoding: 124 us (44 us of
-// HBM time; of the first kernel's 120 us an instruction issues in 63 %, most of
+// HBM time; of the first kernel's 120 us an instruction issues in 62 %, most of
 // them of the integer pipe, and the rest is waiting at 12 warps to an SM).
 //
 //   * Each warp streams 16 tokens at a time into a ring of its own by cp.async,
@@ -34,9 +34,11 @@
 //     into equal shares of 64-token units, one per CTA; where a CTA's share ends
 //     inside a row's tokens, both sides leave a partial result (m, l, O) in the
 //     workspace, and a second small kernel, launched early, joins them in order
-//     (6.6 us of the 197).  Few rows that cannot be long take a cluster of CTAs
-//     each instead, joined in shared memory, and many short ones a CTA each: one
-//     sequence of 700 tokens 7 us, 40 of up to 120 9 us, 256 of up to 200 30 us.
+//     (6.6 us of the 200).  Few rows that cannot be long take a cluster of CTAs
+//     each instead, joined in shared memory, and many short ones a CTA each (how
+//     long they can be is the table's width and the window, all that the host
+//     knows: short sequences under a wide table take shares): one sequence of 700
+//     tokens 7 us, 40 of up to 120 9 us, 256 of up to 200 30 us.
 #include <cuda_runtime.h>
 #include <atomic>
 #include <cstdint>
@@ -62,9 +64,9 @@ constexpr int kCtaTokens = 512;
 // And up to which one CTA to a row is, whatever their number: 40 sequences of up to 250 12 against 16 us, of up to 500
 // 17 against 17; 100 of up to 250 21 against 22, of up to 500 34 against 31; 300 of up to 120 28 against 32.
 constexpr int kRowTokens = 256;
-// What beginning a row costs (its queries, the way to its first pages, the join of the warps), in units.  Swept, 0 / 2 /
-// 4 / 8: 256 sequences of up to 200 tokens, 8 heads of 128, 58 / 46 / 41 / 39 us; 64 of up to 8192 on a MixFP4 cache
-// 149 / 146 / 146 / 149 us.
+// What beginning a row costs (its queries, the way to its first pages, the join of the warps), in units.  Swept in equal
+// shares, 0 / 2 / 4 / 6 / 8: 256 sequences of up to 200 tokens under a wide table, 8 heads of 128, 58 / 50 / 46 / 44 / 44
+// us; 64 of up to 8192 204 / 198 / 196 / 197 / 197, on a MixFP4 cache 140 / 138 / 136 / 135 / 136.
 constexpr int kRowCost = 6;
 // Tiles of 16 tokens after which a warp sets its O and l aside.  The tensor cores round a chain of sums towards zero,
 // some 2^-25 of the sum a link: a warp that walked 6000 tiles left O 2^-12 too small.  128 tiles (256 links) leave 2^-17,
@@ -136,7 +138,8 @@ struct Cfg {
   static constexpr int kStage = kThere + 128;
   // CTAs of an SM: as many as registers and the rings' 220 KB allow.  A MixFP4 cache of 128 dimensions would hold
   // four with 128 registers each, but three with 168 keep V's codes in registers beside K's: 129 against 145 us.
-  // Three stages: six (with three CTAs) 129 against 126 us on a MixFP4 cache, and a bf16 cache has no room for more.
+  // Three stages, or the two that fit (a bf16 cache of 128 dimensions and up to 16 query heads): six with three CTAs 129
+  // against 126 us on a MixFP4 cache.
   static constexpr int kCtas = DT == 256 ? (kFp4 ? 2 : 1) : (NT == 3 ? 2 : (NT == 1 && !kFp4 && DT == 64 ? 4 : 3));
   static constexpr int kDepth = 3;
   static constexpr int kFit = 220 * 1024 / kCtas / (kWarps * kStage);

@@ -1,17 +1,22 @@
 // The paged key-value cache: new tokens appended with the position rotation
 // on the way (mixfp4_kv_append), and rows read back (mixfp4_kv_gather).
 //
-// Both are single passes: every input element is read once and every output
-// written once, 32 bytes per lane and access.  Appending 8111 tokens of 32 + 16
-// heads of 128 in fp32 to a bf16 cache (300 MB in all) takes 48 us, 92 % of the
-// measured HBM rate.  To a MixFP4 cache it takes 52 us for 258 MB (73 %), the
+// Both are single passes: every input element is read once (but see below) and
+// every output written once, 32 bytes per lane and access.  Appending 8111 tokens of 32 + 16
+// heads of 128 in fp32 to a bf16 cache (303 MB in all) takes 48 us, 93 % of the
+// measured HBM rate.  To a MixFP4 cache it takes 52 us for 279 MB (79 %), the
 // rest being the quantizer's steps.  The gather is a row's few bytes to 16 bf16
-// values a thread: 14 us for those 8111 tokens, issue-bound (76 %).
+// values a thread: 12 us for those 8111 tokens (8.8 from a bf16 cache), with an
+// instruction issued in 76 % of the cycles, most of them the index arithmetic
+// that finds page and address anew for every 16 elements.
 //
 // A thread owns a "unit" of a head row (one 16-element block, or the two blocks
 // that a rotation of pairs (i, i + rot / 2) couples) and walks over several
 // heads of its token, so that the token's angles, slot and address are found
-// once.
+// once.  Where a half-split rotation's width is no multiple of 32 a thread has
+// one block, and reads the 16 partners of its elements one by one: 8111 tokens of
+// 16 + 32 heads of 80 in fp32 to a bf16 cache 71 us with all 80 rotated, 33 with
+// 64 (to a MixFP4 cache 77 and 40).
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <cstdint>

@@ -14,11 +14,11 @@
 // bytes that lie together.  A matrix that lies the other way round is put
 // together from row pairs by byte permutes.
 //
-// Measured: 2999 tokens of 12 requests, rank 32, 4096 -> 14336 features, 77 us:
-// the expansion 64 (344 MB, 79 % of the measured HBM rate), the shrink 15 and
+// Measured: 2999 tokens of 12 requests, rank 32, 4096 -> 14336 features, 79 us:
+// the expansion 65 (344 MB, 78 % of the measured HBM rate), the shrink 15 and
 // mostly behind its own latency.  A training step of 4096 tokens, rank 64, 4096
-// features either way, 154 us: shrinks 20 and 19, expansions 40 and 37, gradients
-// 57, their three products per step at 42 % of the tensor pipe.  32 requests of
+// features either way, 160 us: shrinks 20 and 19, expansions 39 and 36, gradients
+// 60, their three products per step at 40 % of the tensor pipe.  32 requests of
 // one token, rank 16, 4096 features either way, 8 us of two dependent launches.
 //
 // u and v are fp32.  Where they enter a product they are cut into three bf16
@@ -771,7 +771,7 @@ int shrink(ShrinkArgs p, cudaStream_t s) {
   const bool few = p.seg.tokens <= 8 * (int64_t)p.seg.count;
   const int64_t tiles = few ? tiles_of(p.seg, 8, true) : tiles_of(p.seg, 32, false);
   // Ranks of a CTA: 16, or 32 (x is read again for every 32 ranks, from L2; 64 in one CTA left registers for
-  // half the loads in flight).  CTAs: k is cut until they fill the device's two places to an SM (32 requests, 4096
+  // half the loads in flight).  CTAs: k is cut until there are more of them than SMs, which hold two (32 requests, 4096
   // features either way: 10.5 us, 13 with k in one piece).
   const int rt = p.R <= 16 ? 1 : 2;
   const int64_t ctas = tiles * ((p.R + 16 * rt - 1) / (16 * rt));
