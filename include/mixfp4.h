@@ -592,7 +592,9 @@ int mixfp4_paged_attention_workspace(const mixfp4_kv_cache* cache, int64_t B, in
  * scaling      device, float [adapters].    adapters  0 .. 65535.
  * starts       device, int32 [segments + 1], not decreasing, starts[0] = 0 and
  *              starts[segments] = T; a segment may be empty.  Tokens outside every
- *              segment are neither read nor written.
+ *              segment are neither read nor written.  Values outside 0 .. T are
+ *              taken as the nearer end; segments that overlap give undefined
+ *              results, and no access outside the T tokens.
  * ids          device, int32 [segments].    segments  at most 2^20.
  * base         device, float [T][ld_base], or NULL for zeros; may be out.
  * out          device, float [T][ld_out] (32-byte alignment and strides % 8 == 0

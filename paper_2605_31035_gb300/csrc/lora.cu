@@ -587,20 +587,23 @@ __global__ void __launch_bounds__(32 * NW, NW == 8 ? 1 : (RT == 4 ? 2 : 3)) lora
     if (i < p.seg.count && adapter_of(p.seg, i) == adapter) r = bounds(p.seg, i);
     const int len = r.y - r.x;
     const uint32_t some = __ballot_sync(kAll, len > 0);
+    // Sums end at INT_MAX: segments that overlap may hold more tokens than an int counts.
+    auto plus = [](int a, int b) { return (int)min((uint32_t)a + (uint32_t)b, (uint32_t)INT32_MAX); };
     int sum = len;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
       const int v = __shfl_up_sync(kAll, sum, d);
-      if (lane >= d) sum += v;
+      if (lane >= d) sum = plus(sum, v);
     }
     __syncthreads();  // the batch before has been used
     if (lane == 31) count[warp] = sum, found[warp] = __popc(some);
     __syncthreads();
     int at = __popc(some & ((1u << lane) - 1u)), off = sum, lists = 0, total = 0;
     for (int q = 0; q < warps; ++q) {
-      if (q < warp) at += found[q], off += count[q];
-      lists += found[q], total += count[q];
+      if (q < warp) at += found[q], off = plus(off, count[q]);
+      lists += found[q], total = plus(total, count[q]);
     }
+    if (total > (int)p.seg.tokens) total = 0;  // more than there are: none is taken
     if (len > 0) first[at] = r.x - (off - len), ends[at] = off;  // token = index + first
     __syncthreads();
     int top = 1;
