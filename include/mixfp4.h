@@ -577,6 +577,104 @@ int mixfp4_paged_attention(const void* q, int64_t q_stride, int64_t q_head_strid
 int mixfp4_paged_attention_workspace(const mixfp4_kv_cache* cache, int64_t B, int64_t q_heads, int64_t* bytes);
 
 /*
+ * mixfp4_tree_attention -- attention of up to 64 drafted tokens per sequence
+ * over a mixfp4_kv_cache that holds them already (mixfp4_kv_append) behind the
+ * tokens that are certain.  Sequence b has n = lengths[b] tokens in the cache,
+ * the last c = min(counts[b], t, n) of them drafts, the first p = n - c certain.
+ * Bit k of mask[b][i] says whether draft i sees draft k (its own bit is asked for
+ * like any other); without masks a draft sees those up to itself.  Draft i stands
+ * d_i places behind the certain tokens, d_i being the number of drafts it sees
+ * besides itself: its position is p + d_i, as a draft that is seen; a certain token
+ * j has position j.  With i and j a pair that sees and their positions x_i, x_j,
+ *   s = scale * q_i . k_j,  s = softcap tanh(s / softcap) with softcap > 0,
+ *   s = s - slopes[h] (x_i - x_j) with slopes;  window > 0: only where x_i - x_j < window,
+ *   out = sum_j exp(s_j - lse) v_j,   lse = log sum_j exp(s_j).
+ * Products are exact, sums and the softmax in fp32 (the weights enter the
+ * second product as two bf16 parts, or for a MixFP4 cache as f16 of 11 bits), and
+ * out is rounded to bf16.  A draft that sees nothing, and rows i >= c, give out = 0
+ * and lse = -inf.  What a draft does not see does not reach its results, NaN and
+ * infinities included.  Scores of NaN and +inf and infinities of V as
+ * mixfp4_paged_attention has them.  The order of every sum depends on the arguments alone.
+ *
+ * q            device, bf16: element d of head h of draft i of sequence b at
+ *              b * q_stride + i * q_token_stride + h * q_head_stride + d; 16-byte
+ *              aligned, strides multiples of 8.
+ * B, t         B >= 0; t 0 .. 64, rows of a sequence.   q_heads  a multiple of the cache's heads.
+ * block_table, table_stride, table_pages, lengths, window: as mixfp4_paged_attention.
+ * mask         device, int64 [B][mask_stride] or, with mask_stride 0, one [t] for all
+ *              sequences; bits from c on are not looked at.  NULL: a chain.
+ * counts       device, int32 [B], or NULL: t of each sequence.
+ * softcap      0 (none) or 1e-6 .. 1e6 (else MIXFP4_ERR_ARG).
+ * slopes       device, float [q_heads], or NULL.
+ * out          device, bf16 [B][t][q_heads][head_dim], 16-byte aligned; overlaps no input. (output)
+ * lse          device, float [B][t][q_heads], or NULL.                     (output)
+ * workspace    device, 256-byte aligned, at least the bytes
+ *              mixfp4_tree_attention_workspace reports; free for reuse once the
+ *              call's work on `stream` is done.
+ */
+int mixfp4_tree_attention(const void* q, int64_t q_stride, int64_t q_token_stride, int64_t q_head_stride, int64_t B,
+                          int64_t t, int64_t q_heads, const mixfp4_kv_cache* cache, const int32_t* block_table,
+                          int64_t table_stride, int64_t table_pages, const int32_t* lengths, const int64_t* mask,
+                          int64_t mask_stride, const int32_t* counts, float scale, int64_t window, float softcap,
+                          const float* slopes, void* out, float* lse, void* workspace, int64_t workspace_bytes,
+                          void* stream);
+
+/*
+ * mixfp4_tree_attention_workspace -- bytes of workspace mixfp4_tree_attention
+ * takes for t drafts of q_heads of each of B sequences on the current device.
+ *
+ * bytes        host, one int64.                                          (output)
+ */
+int mixfp4_tree_attention_workspace(const mixfp4_kv_cache* cache, int64_t B, int64_t t, int64_t q_heads,
+                                    int64_t* bytes);
+
+/*
+ * mixfp4_kv_accept -- what the verification of drafts leaves in the cache: the row
+ * of draft path[b][k] of sequence b (n, c and p as in mixfp4_tree_attention, with
+ * c = min(counts[b], n)) moves to place p + k, keys and values, bit for bit, and
+ * lengths_out[b] = p + the number of accepted drafts.  A sequence's rows are all read
+ * before one is written.  Its path ends at its first entry outside 0 .. c - 1.
+ *
+ * block_table, table_stride, table_pages, lengths: as mixfp4_paged_attention.  A place
+ *              behind the table or on a page outside the cache is neither read nor written.
+ * counts       device, int32 [B].
+ * path         device, int32 [B][path_stride], depth entries of each sequence.  depth 0 .. 64.
+ * lengths_out  device, int32 [B]; may be lengths, else overlaps no input.  (output)
+ */
+int mixfp4_kv_accept(const mixfp4_kv_cache* cache, const int32_t* block_table, int64_t table_stride,
+                     int64_t table_pages, const int32_t* lengths, const int32_t* counts, int64_t B,
+                     const int32_t* path, int64_t path_stride, int64_t depth, int32_t* lengths_out, void* stream);
+
+/*
+ * mixfp4_kv_fork -- sequences branch: child i goes on from sequence parents[i], with
+ * its length and its pages.  Full pages are shared; a last page that is filled in
+ * part, l = lengths[parent] % page_size > 0 places of it, is shared too unless
+ * fresh[i] names a page of the cache: then the child's table has that page instead,
+ * and its first l places get the parent's rows, bit for bit.
+ *
+ * block_table, table_stride, table_pages, lengths: as mixfp4_paged_attention, of B
+ *              sequences.  A page outside the cache is not copied.
+ * parents      device, int32 [children]; one outside 0 .. B - 1 gives length 0 and pages of -1.
+ * fresh        device, int32 [children]: pages that differ and that no table has; -1
+ *              (or any other number outside the cache): none.
+ * table_out    device, int32 [children][table_pages].                     (output)
+ * lengths_out  device, int32 [children]; neither overlaps an input (MIXFP4_ERR_ARG). (output)
+ */
+int mixfp4_kv_fork(const mixfp4_kv_cache* cache, const int32_t* block_table, int64_t table_stride,
+                   int64_t table_pages, const int32_t* lengths, int64_t B, const int32_t* parents,
+                   const int32_t* fresh, int64_t children, int32_t* table_out, int32_t* lengths_out, void* stream);
+
+/*
+ * mixfp4_kv_copy_pages -- page src[i] of the cache copied to page dst[i], keys and
+ * values (and scales), bit for bit.  The pages in dst differ, and are none of those
+ * in src but their own: else what they hold afterwards is undefined.  A pair with a
+ * page outside the cache is left out.
+ *
+ * src, dst     device, int32 [n].
+ */
+int mixfp4_kv_copy_pages(const mixfp4_kv_cache* cache, const int32_t* src, const int32_t* dst, int64_t n, void* stream);
+
+/*
  * mixfp4_lora -- low-rank adapters of many requests at once beside a shared
  * projection (mixfp4_linear; no counterpart in the paper): for the tokens t of
  * segment i, with its adapter j = ids[i],

@@ -24,7 +24,7 @@ BINDING_ABI = os.path.join(HERE, "_binding.abi")  # what _binding.so was compile
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 
 SOURCES = ["api.cu", "quantize.cu", "train.cu", "gemm.cu", "gemm_f16a.cu", "fewrows.cu", "native.cu", "candidates.cu", "noalloc.cu", "selftest.cu",
-           "kvcache.cu", "attention.cu", "lora.cu"]
+           "kvcache.cu", "kvmove.cu", "attention.cu", "tree_attention.cu", "lora.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-Xptxas", "-v",
               "--ftz=false", "--prec-div=true", "--prec-sqrt=true", "--fmad=false",

@@ -303,6 +303,207 @@ PyObject* paged_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// Masks of drafts, int64: none, [t] for all sequences (`stride` 0), or [B, t].
+const int64_t* masks(PyObject* o, int64_t B, int64_t t, int64_t index, int64_t* stride) {
+  *stride = 0;
+  if (!given(o)) return nullptr;
+  const Tensor* m = tensor(o);
+  const int64_t d = m ? m->dim() : 0;
+  if (!on(m, index) || m->scalar_type() != ScalarType::Long || d < 1 || d > 2 || m->size(d - 1) != t ||
+      (m->stride(d - 1) != 1 && t > 1) || (d == 2 && m->size(0) != B))
+    refuse("%s must be an int64 CUDA tensor [%lld, %lld] or [%lld] with unit last stride", "mask", B, t, t);
+  if (d == 2 && B > 1) *stride = m->stride(0);
+  if (*stride != 0 && *stride < t) refuse("%s must not have overlapping rows", "mask");
+  return m->const_data_ptr<int64_t>();
+}
+
+const Tensor& table_of(PyObject* o, int64_t B, int64_t index) {
+  const Tensor* table = tensor(o);
+  if (!on(table, index) || table->scalar_type() != ScalarType::Int || table->dim() != 2 ||
+      (B >= 0 && table->size(0) != B) || (table->stride(1) != 1 && table->size(1) > 1))
+    refuse("%s must be an int32 CUDA tensor [%lld, pages] on device %lld with unit column stride", "block_table", B,
+           index);
+  return *table;
+}
+// A table's stride from row to row, at least its width.
+int64_t table_step(const Tensor& table) {
+  const int64_t pages = table.size(1);
+  if (table.size(0) > 1 && table.stride(0) < pages) refuse("%s must not have overlapping rows", "block_table");
+  return std::max(step(table, 0), pages);
+}
+
+int64_t length_of(PyObject* o, const char* what) {
+  const Tensor* t = tensor(o);
+  if (!t || t->dim() != 1) refuse("%s must be a 1-D int32 CUDA tensor", what);
+  return t->size(0);
+}
+
+double number(PyObject* o) {
+  const double v = PyFloat_AsDouble(o);
+  if (v == -1.0 && PyErr_Occurred()) throw BadArgument{};
+  return v;
+}
+
+// (cache, index, q, block_table, lengths, mask, counts, scale, window, softcap, slopes, out, lse, want_lse, workspace,
+// stream)
+PyObject* tree_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (!counted(n, 16)) return nullptr;
+  return guarded([&]() -> PyObject* {
+    const mixfp4_kv_cache* c = cache_of(a[0]);
+    const int64_t index = integer(a[1]), D = c->head_dim;
+    const Tensor* qp = tensor(a[2]);
+    if (!on(qp, index) || qp->scalar_type() != ScalarType::BFloat16 || qp->dim() != 4 || qp->size(3) != D ||
+        qp->stride(3) != 1)
+      refuse("%s must be a bfloat16 CUDA tensor [sequences, drafts, heads, %lld] on device %lld with unit last stride", "q",
+             D, index);
+    const Tensor& q = *qp;
+    const int64_t B = q.size(0), t = q.size(1), H = q.size(2);
+    if (t > 64) refuse("%s must have at most 64 drafts of a sequence", "q");
+    if (H % c->heads != 0) refuse("%s must be a multiple of the cache's heads", "q_heads");
+    const Tensor& table = table_of(a[3], B, index);
+    const Tensor& lengths = vector(a[4], ScalarType::Int, B, index, "lengths");
+    int64_t mask_stride;
+    const int64_t* mask = masks(a[5], B, t, index, &mask_stride);
+    const int32_t* counts = nullptr;
+    if (given(a[6])) counts = vector(a[6], ScalarType::Int, B, index, "counts").const_data_ptr<int32_t>();
+    const float scale = given(a[7]) ? (float)number(a[7]) : (float)std::pow((double)D, -0.5);
+    const int64_t window = integer(a[8]);
+    if (window < 0) refuse("%s must not be negative", "window");
+    const float softcap = (float)number(a[9]);
+    if (!(softcap == 0.0f || (softcap >= 1e-6f && softcap <= 1e6f))) refuse("%s must be 0 or 1e-6 to 1e6", "softcap");
+    const float* slopes = nullptr;
+    if (given(a[10])) {
+      const Tensor* s = tensor(a[10]);
+      if (!on(s, index) || s->scalar_type() != ScalarType::Float || s->dim() != 1 || s->size(0) != H ||
+          !s->is_contiguous())
+        refuse("%s must be a dense float32 CUDA tensor of %lld elements on device %lld", "slopes", H, index);
+      slopes = s->const_data_ptr<float>();
+    }
+    Tensor out, lse, workspace;
+    if (given(a[11])) {
+      const Tensor* o = tensor(a[11]);
+      if (!on(o, index) || o->scalar_type() != ScalarType::BFloat16 || o->sizes() != q.sizes() || !o->is_contiguous())
+        refuse("%s must be a dense bfloat16 CUDA tensor of q's shape", "out");
+      out = *o;
+    }
+    if (given(a[12])) {
+      const Tensor* s = tensor(a[12]);
+      if (!on(s, index) || s->scalar_type() != ScalarType::Float || s->dim() != 3 || s->size(0) != B ||
+          s->size(1) != t || s->size(2) != H || !s->is_contiguous())
+        refuse("%s must be a dense float32 CUDA tensor [%lld, %lld, %lld]", "lse", B, t, H);
+      lse = *s;
+    }
+    int64_t need = 0;
+    if (given(a[14])) {
+      const Tensor* w = tensor(a[14]);
+      if (!on(w, index) || !w->is_contiguous())
+        refuse("%s must be a dense CUDA tensor on device %lld", "workspace", index);
+      workspace = *w;
+      need = w->numel() * w->element_size();
+    } else {
+      if (const int st = mixfp4_tree_attention_workspace(c, B, t, H, &need)) return status_of(st);
+      workspace = fresh({need}, ScalarType::Byte, q);
+    }
+    if (!out.defined()) out = fresh(q.sizes(), ScalarType::BFloat16, q);
+    if (!lse.defined() && truth(a[13])) lse = fresh({B, t, H}, ScalarType::Float, q);
+    void* stream = stream_of(a[15]);
+    const int64_t ts = table_step(table);
+    int st;
+    {
+      Unlocked unlocked;
+      st = mixfp4_tree_attention(q.const_data_ptr(), step(q, 0), step(q, 1), step(q, 2), B, t, H, c,
+                                 table.const_data_ptr<int32_t>(), ts, table.size(1),
+                                 lengths.const_data_ptr<int32_t>(), mask, mask_stride, counts, scale, window, softcap,
+                                 slopes, out.mutable_data_ptr(), lse.defined() ? lse.mutable_data_ptr<float>() : nullptr,
+                                 workspace.mutable_data_ptr(), need, stream);
+    }
+    if (st) return status_of(st);
+    if (!lse.defined()) return THPVariable_Wrap(std::move(out));
+    return tuple_of(out, lse);
+  });
+}
+
+// (cache, index, block_table, lengths, path, counts, out, stream)
+PyObject* kv_accept(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (!counted(n, 8)) return nullptr;
+  return guarded([&]() -> PyObject* {
+    const mixfp4_kv_cache* c = cache_of(a[0]);
+    const int64_t index = integer(a[1]), B = length_of(a[3], "lengths");
+    const Tensor& table = table_of(a[2], B, index);
+    const Tensor& lengths = vector(a[3], ScalarType::Int, B, index, "lengths");
+    const Tensor* path = tensor(a[4]);
+    if (!on(path, index) || path->scalar_type() != ScalarType::Int || path->dim() != 2 || path->size(0) != B ||
+        path->size(1) > 64 || (path->stride(1) != 1 && path->size(1) > 1) ||
+        (B > 1 && path->stride(0) < path->size(1)))
+      refuse("%s must be an int32 CUDA tensor [%lld, at most 64] on device %lld with unit column stride", "path", B, index);
+    const Tensor& counts = vector(a[5], ScalarType::Int, B, index, "counts");
+    Tensor out = given(a[6]) ? vector(a[6], ScalarType::Int, B, index, "out") : fresh({B}, ScalarType::Int, lengths);
+    void* stream = stream_of(a[7]);
+    const int64_t ts = table_step(table);
+    int st;
+    {
+      Unlocked unlocked;
+      st = mixfp4_kv_accept(c, table.const_data_ptr<int32_t>(), ts, table.size(1), lengths.const_data_ptr<int32_t>(),
+                            counts.const_data_ptr<int32_t>(), B, path->const_data_ptr<int32_t>(), step(*path, 0),
+                            path->size(1), out.mutable_data_ptr<int32_t>(), stream);
+    }
+    if (st) return status_of(st);
+    return THPVariable_Wrap(std::move(out));
+  });
+}
+
+// (cache, index, block_table, lengths, parents, fresh, table_out, lengths_out, stream)
+PyObject* kv_fork(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (!counted(n, 9)) return nullptr;
+  return guarded([&]() -> PyObject* {
+    const mixfp4_kv_cache* c = cache_of(a[0]);
+    const int64_t index = integer(a[1]), B = length_of(a[3], "lengths"), N = length_of(a[4], "parents");
+    const Tensor& table = table_of(a[2], B, index);
+    const Tensor& lengths = vector(a[3], ScalarType::Int, B, index, "lengths");
+    const Tensor& parents = vector(a[4], ScalarType::Int, N, index, "parents");
+    const Tensor& own = vector(a[5], ScalarType::Int, N, index, "fresh");
+    const int64_t pages = table.size(1);
+    Tensor out;
+    if (given(a[6])) {
+      out = table_of(a[6], N, index);
+      if (out.size(1) != pages) refuse("%s must be as wide as block_table", "out");
+      dense(out, "out");
+    } else {
+      out = fresh({N, pages}, ScalarType::Int, parents);
+    }
+    Tensor lens = given(a[7]) ? vector(a[7], ScalarType::Int, N, index, "out") : fresh({N}, ScalarType::Int, parents);
+    void* stream = stream_of(a[8]);
+    const int64_t ts = table_step(table);
+    int st;
+    {
+      Unlocked unlocked;
+      st = mixfp4_kv_fork(c, table.const_data_ptr<int32_t>(), ts, pages, lengths.const_data_ptr<int32_t>(), B,
+                          parents.const_data_ptr<int32_t>(), own.const_data_ptr<int32_t>(), N,
+                          out.mutable_data_ptr<int32_t>(), lens.mutable_data_ptr<int32_t>(), stream);
+    }
+    if (st) return status_of(st);
+    return tuple_of(out, lens);
+  });
+}
+
+// (cache, index, src, dst, stream)
+PyObject* kv_copy_pages(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (!counted(n, 5)) return nullptr;
+  return guarded([&]() -> PyObject* {
+    const mixfp4_kv_cache* c = cache_of(a[0]);
+    const int64_t index = integer(a[1]), N = length_of(a[2], "src");
+    const Tensor& src = vector(a[2], ScalarType::Int, N, index, "src");
+    const Tensor& dst = vector(a[3], ScalarType::Int, N, index, "dst");
+    void* stream = stream_of(a[4]);
+    int st;
+    {
+      Unlocked unlocked;
+      st = mixfp4_kv_copy_pages(c, src.const_data_ptr<int32_t>(), dst.const_data_ptr<int32_t>(), N, stream);
+    }
+    return status_of(st);
+  });
+}
+
 struct Adapters {
   const Tensor *a, *b, *scaling;
   int64_t count, R, K, N;
@@ -427,7 +628,8 @@ PyObject* lora_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
 
 #define METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {METHOD(kv_append), METHOD(kv_gather),     METHOD(paged_attention),
-                         METHOD(lora),      METHOD(lora_backward), {nullptr, nullptr, 0, nullptr}};
+                         METHOD(lora),      METHOD(lora_backward), METHOD(tree_attention),
+                         METHOD(kv_accept), METHOD(kv_fork),       METHOD(kv_copy_pages),  {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -102,6 +102,8 @@ def lib() -> ctypes.CDLL:
         L.mixfp4_selftest_bounded_wait.argtypes = [P, ctypes.c_uint64, P]
         L.mixfp4_paged_attention_workspace.restype = I
         L.mixfp4_paged_attention_workspace.argtypes = [ctypes.POINTER(_CKVCache), I64, I64, ctypes.POINTER(I64)]
+        L.mixfp4_tree_attention_workspace.restype = I
+        L.mixfp4_tree_attention_workspace.argtypes = [ctypes.POINTER(_CKVCache), I64, I64, I64, ctypes.POINTER(I64)]
         L.mixfp4_status_string.restype = ctypes.c_char_p
         L.mixfp4_status_string.argtypes = [I]
         L.mixfp4_version.restype = I
@@ -899,6 +901,104 @@ def mixfp4_paged_attention(q: torch.Tensor, cache: KVCache, block_table: torch.T
     if r.__class__ is int:
         _check("mixfp4_paged_attention", r)
     return r
+
+
+# ---- drafted tokens, branches and pages -------------------------------------------
+
+
+def tree_attention_workspace_bytes(cache: KVCache, B: int, t: int, q_heads: int) -> int:
+    """Bytes of scratch memory mixfp4_tree_attention takes."""
+    _check_cache(cache)
+    n = ctypes.c_int64(0)
+    _check("mixfp4_tree_attention", lib().mixfp4_tree_attention_workspace(ctypes.byref(cache._c), B, t, q_heads,
+                                                                               ctypes.byref(n)))
+    return n.value
+
+
+def mixfp4_tree_attention(q: torch.Tensor, cache: KVCache, block_table: torch.Tensor, lengths: torch.Tensor,
+                          mask: torch.Tensor | None = None, counts: torch.Tensor | None = None,
+                          scale: float | None = None, window: int = 0, softcap: float = 0.0,
+                          slopes: torch.Tensor | None = None, return_lse: bool = False,
+                          out: torch.Tensor | None = None, lse: torch.Tensor | None = None,
+                          workspace: torch.Tensor | None = None, stream=None):
+    """Attention of up to 64 drafted tokens per sequence over the paged cache, which
+    holds their keys and values behind the tokens that are certain (with one draft
+    a sequence: one-token attention with the options below).
+
+    q: bf16 [B, t, q_heads, head_dim], any strides whose last is 1; q_heads a multiple of the cache's heads.
+    block_table, lengths, scale, window: as mixfp4_paged_attention; lengths count the drafts.
+    mask: int64 [B, t], or [t] for all sequences: bit k of element i says whether draft i
+    sees draft k (its own bit included).  None: a chain, each sees those up to itself.
+    counts: int32 [B], drafts of each sequence where they are fewer than t.
+    softcap: scores become softcap * tanh(score / softcap), 1e-6 to 1e6; 0: they stay.
+    slopes: float32 [q_heads]: scores lose slope * distance, in positions; a draft's
+    position is behind the certain tokens by the number of drafts it sees besides itself.
+    Returns bf16 [B, t, q_heads, head_dim], with return_lse (or lse=) also the
+    log-sum-exp of the scores, float32 [B, t, q_heads].  A draft that sees nothing,
+    and rows behind a sequence's drafts, give zeros and -inf.  out overlaps no input.
+    workspace: scratch memory of the caller's, at least
+    tree_attention_workspace_bytes(cache, B, t, q_heads), aligned to 256 bytes."""
+    _check_cache(cache)
+    if stream is not None:
+        B, t, H, D = _shape(q, 4)
+        out = _result((B, t, H, D), torch.bfloat16, cache.device, stream) if out is None else out
+        if lse is None and return_lse:
+            lse = _result((B, t, H), torch.float32, cache.device, stream)
+        if workspace is None and _elsewhere(stream, cache.device) and H % cache.heads == 0 and t <= 64:
+            workspace = _empty(tree_attention_workspace_bytes(cache, B, t, H), torch.uint8, cache.device, stream, True)
+    r = _native().tree_attention(cache._address, cache._index, q, block_table, lengths, mask, counts, scale, window,
+                                 softcap, slopes, out, lse, return_lse, workspace, _stream(stream))
+    if r.__class__ is int:
+        _check("mixfp4_tree_attention", r)
+    return r
+
+
+def mixfp4_kv_accept(cache: KVCache, block_table: torch.Tensor, lengths: torch.Tensor, path: torch.Tensor,
+                     counts: torch.Tensor, out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """Keep the accepted drafts: the rows of drafts path[b] (int32 [B, depth], depth at
+    most 64; it ends at the first entry that is no draft, -1 say) move to the places
+    behind sequence b's certain tokens, in that order.
+
+    block_table, lengths: as mixfp4_paged_attention, lengths with the drafts;
+    counts: int32 [B], the drafts among them.
+    Returns the new lengths, int32 [B] (out=lengths changes them in place)."""
+    _check_cache(cache)
+    if stream is not None and out is None:
+        out = _result(tuple(_shape(lengths, 1)), torch.int32, cache.device, stream)
+    r = _native().kv_accept(cache._address, cache._index, block_table, lengths, path, counts, out, _stream(stream))
+    if r.__class__ is int:
+        _check("mixfp4_kv_accept", r)
+    return r
+
+
+def mixfp4_kv_fork(cache: KVCache, block_table: torch.Tensor, lengths: torch.Tensor, parents: torch.Tensor,
+                   fresh: torch.Tensor, out=None, stream=None):
+    """Branches of sequences (beams, several answers to one prompt): child i goes on
+    from sequence parents[i] and shares its full pages; of a last page filled in
+    part it gets a copy in page fresh[i] (-1: shares it too).
+
+    block_table, lengths: as mixfp4_paged_attention; parents, fresh: int32 [children].
+    The fresh pages differ, and no table has them.
+    Returns (block_table int32 [children, pages], lengths int32 [children]);
+    out: a pair of dense tensors to write, which overlap no input."""
+    _check_cache(cache)
+    table, lens = (None, None) if out is None else out
+    if stream is not None and out is None:
+        n = _shape(parents, 1)[0]
+        table = _result((n, _shape(block_table, 2)[1]), torch.int32, cache.device, stream)
+        lens = _result((n,), torch.int32, cache.device, stream)
+    r = _native().kv_fork(cache._address, cache._index, block_table, lengths, parents, fresh, table, lens,
+                          _stream(stream))
+    if r.__class__ is int:
+        _check("mixfp4_kv_fork", r)
+    return r
+
+
+def mixfp4_kv_copy_pages(cache: KVCache, src: torch.Tensor, dst: torch.Tensor, stream=None) -> None:
+    """Copy pages src[i] to pages dst[i] of the cache (int32 [n]; a pair with a page
+    outside the cache is left out).  The pages in dst differ, and none of them is another pair's source."""
+    _check_cache(cache)
+    _check("mixfp4_kv_copy_pages", _native().kv_copy_pages(cache._address, cache._index, src, dst, _stream(stream)))
 
 
 # ---- low-rank adapters ----------------------------------------------------------
