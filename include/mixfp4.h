@@ -611,13 +611,15 @@ int mixfp4_paged_attention_workspace(const mixfp4_kv_cache* cache, int64_t B, in
  * workspace    device, 256-byte aligned, at least the bytes
  *              mixfp4_tree_attention_workspace reports; free for reuse once the
  *              call's work on `stream` is done.
+ * status_word  as mixfp4_gemm's: 0 unless a wait of the kernel ran out, in
+ *              which case the results are not to be used.
  */
 int mixfp4_tree_attention(const void* q, int64_t q_stride, int64_t q_token_stride, int64_t q_head_stride, int64_t B,
                           int64_t t, int64_t q_heads, const mixfp4_kv_cache* cache, const int32_t* block_table,
                           int64_t table_stride, int64_t table_pages, const int32_t* lengths, const int64_t* mask,
                           int64_t mask_stride, const int32_t* counts, float scale, int64_t window, float softcap,
                           const float* slopes, void* out, float* lse, void* workspace, int64_t workspace_bytes,
-                          void* stream);
+                          uint32_t* status_word, void* stream);
 
 /*
  * mixfp4_tree_attention_workspace -- bytes of workspace mixfp4_tree_attention

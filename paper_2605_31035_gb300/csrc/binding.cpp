@@ -345,9 +345,9 @@ double number(PyObject* o) {
 }
 
 // (cache, index, q, block_table, lengths, mask, counts, scale, window, softcap, slopes, out, lse, want_lse, workspace,
-// stream)
+// status_word, stream)
 PyObject* tree_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  if (!counted(n, 16)) return nullptr;
+  if (!counted(n, 17)) return nullptr;
   return guarded([&]() -> PyObject* {
     const mixfp4_kv_cache* c = cache_of(a[0]);
     const int64_t index = integer(a[1]), D = c->head_dim;
@@ -406,7 +406,8 @@ PyObject* tree_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
     }
     if (!out.defined()) out = fresh(q.sizes(), ScalarType::BFloat16, q);
     if (!lse.defined() && truth(a[13])) lse = fresh({B, t, H}, ScalarType::Float, q);
-    void* stream = stream_of(a[15]);
+    uint32_t* status = reinterpret_cast<uint32_t*>(given(a[15]) ? static_cast<intptr_t>(integer(a[15])) : 0);
+    void* stream = stream_of(a[16]);
     const int64_t ts = table_step(table);
     int st;
     {
@@ -415,7 +416,7 @@ PyObject* tree_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
                                  table.const_data_ptr<int32_t>(), ts, table.size(1),
                                  lengths.const_data_ptr<int32_t>(), mask, mask_stride, counts, scale, window, softcap,
                                  slopes, out.mutable_data_ptr(), lse.defined() ? lse.mutable_data_ptr<float>() : nullptr,
-                                 workspace.mutable_data_ptr(), need, stream);
+                                 workspace.mutable_data_ptr(), need, status, stream);
     }
     if (st) return status_of(st);
     if (!lse.defined()) return THPVariable_Wrap(std::move(out));

@@ -1,29 +1,71 @@
 // Attention of drafted tokens over the paged cache (mixfp4_tree_attention).
 //
-// The plain kernel: a CTA to a draft and query head, its warps in turn over the
-// tokens, each lane two dimensions of every 64; the softmax's maximum and sum run
-// along, and the warps' results are joined in shared memory.
+// A key head's queries, t drafts times the query heads that share it, are the
+// rows of one tcgen05 tile: 128 of them, or two tiles of 128 over the same tokens.
+// Per tile of 128 tokens (64 with more than 128 dimensions) S = Q K^T goes to
+// tensor memory, four warps a tile of rows take it from there, a row to a thread,
+// and put the softmax's weights P back in its place, and O += P V follows with P
+// from tensor memory.  What bounds it: HBM for a bf16 cache and up to 256 rows,
+// the tensor cores beyond.
+//
+//   * Roles: producer warps bring K and V tiles into a ring, the row's bytes by
+//     cp.async into the places that the 128-byte swizzle gives them (so that any
+//     strides and pages of any size will do), or decode a MixFP4 cache's codes into
+//     them as exact f16; one thread issues the products; the others are softmax.
+//   * Few rows: 32 (or 64) rows are held four times (twice) in the 128 lanes and
+//     each copy takes its quarter (half) of a tile's tokens; the copies are joined
+//     at the end.  A thread then has 32 scores a tile instead of 128.
+//   * The weights keep 16 bits in two bf16 parts of one sign on a bf16 cache, f16's
+//     11 on a MixFP4 one, whose queries are scaled per row by a power of two into f16.
+//   * Where rows of a tile see different tokens (drafts, a window's edge), a weight
+//     of 0 would still make NaN of an infinite or NaN element of V.  Such tiles are
+//     looked over for those, and where there is one the threads take the products
+//     themselves, of what each row sees alone.
+//   * Tokens are cut into equal shares over the device as in the attention of one
+//     token; CTAs of neighbouring heads walk the same tokens at the same time.
 #include <cuda_runtime.h>
+#include <atomic>
 #include <cstdint>
 
+#include "decode.cuh"
 #include "host_util.cuh"
+#include "kernels.cuh"
 #include "kvcache.cuh"
+#include "pipeline.cuh"
 #include "ptx.cuh"
+#include "sm100.cuh"
 
 namespace mixfp4 {
 namespace {
 
-constexpr int kWarps = 8;
-constexpr int kThreads = kWarps * 32;
+using namespace sm100;
+
 constexpr int kMostDrafts = 64;
-constexpr float kNoScore = -3e38f;  // m where nothing has been seen: no difference to a score or to itself is NaN
-constexpr float kMostScore = 3.402823466e38f;
+constexpr int kJoinThreads = 256;
+constexpr uint64_t kWaitLimitNs = 1000000000ull;
+// What beginning a row costs (its queries, the way to its first pages, its end), in tiles.
+constexpr int kRowCost = 2;
+// Tiles after which O is set aside and begins at 0: the tensor cores round a chain of sums towards zero, some 2^-25 of
+// the sum a link, and 64 tiles of 128 tokens are 512 links (1024 with two parts of the weights).
+constexpr int kChain = 64;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+// How far a score may lie above the m of its weight 2^(s - m).  On a MixFP4 cache the weights are 2^7 times that:
+// at most 2^15 in f16, whose least value is then 2^-31 of the weight at m.
+constexpr float kSlack = 8.0f, kFp4Exp = 7.0f;
+constexpr float kNoScore = -3e38f;  // m where no token has been seen: no difference to a score or to itself is NaN
+constexpr float kMostScore = 3.402823466e38f;  // m of a score of +inf, whose weight is then +inf instead of NaN
+constexpr unsigned kAll = 0xFFFFFFFFu;
 
 struct TreeArgs {
   const uint16_t* q;
   int64_t q_stride, q_token_stride, q_head_stride;
   int B, t, q_heads, group;
+  int chunks;    // of 128 (or 256) rows to a key head
+  int together;  // key heads whose CTAs walk together
+  int shares;    // of the tokens; a CTA has one share and one of `together` heads
+  int joined;    // whether rows may be cut, and a second kernel joins them
   mixfp4_kv_cache c;
+  int page_shift;  // log2 page_size, or -1
   const int32_t* table;
   int64_t table_stride, max_tokens;
   const int32_t* lengths;
@@ -35,110 +77,1050 @@ struct TreeArgs {
   const float* slopes;
   uint16_t* out;
   float* lse;
+  int4* split;   // [grid]: the row that a CTA begins and others end: (sequence, row, first share, last); x < 0: none
+  float2* stat;  // [2 grid][rows] (m, l) of parts
+  float4* part;  // [2 grid][row tiles][dimensions / 4][128]: O of parts, and what a row in work has set aside
+  uint32_t* status;
 };
 
-__device__ __forceinline__ float2 pair_of(const void* base, const uint8_t* scales, int64_t at, int64_t sat, int d,
-                                          bool fp4, float ts) {
-  if (!fp4) {
-    const uint32_t w = *reinterpret_cast<const uint32_t*>(static_cast<const uint16_t*>(base) + at + d);
-    return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
+template <int DT, int NM, bool kFp4>
+struct Cfg {
+  static constexpr int kTokens = DT == 256 ? 64 : 128;     // of a tile
+  static constexpr int kCw = kTokens / 4;                  // and of its quarter, a thread's step
+  static constexpr int kBlock = kTokens * 128;             // 64 dimensions of a tile
+  static constexpr int kSlot = kBlock * (DT / 64);
+  static constexpr int kQ = NM * 128 * DT * 2;
+  static constexpr int kSoftmax = 4 * NM;                  // warps
+  static constexpr int kProducers = kFp4 ? 8 : 4;
+  static constexpr int kThreads = (kSoftmax + 1 + kProducers) * 32;
+  static constexpr int kRows = kTokens / kProducers;       // of a tile, to a producer warp
+  static constexpr int kRawRow = DT / 2 + 16;              // a MixFP4 row as it lies: codes, scale bytes
+  static constexpr int kRawSlot = kRows * kRawRow;
+  static constexpr int kRawDepth = 6;
+  static constexpr int kRaw = kFp4 ? kProducers * kRawDepth * kRawSlot : 0;
+  static constexpr int kFit = (227 * 1024 - 2560 - kQ - kRaw) / kSlot;
+  static constexpr int kSlots = kFit < 8 ? kFit : 8;
+  static constexpr int kLag = kFp4 ? kRawDepth - 1 : kSlots - 2;  // copies asked for behind the one handed over
+  static constexpr int kSmem = kQ + kSlots * kSlot + kRaw + 2560;
+  static constexpr uint32_t kScoreCols = 2 * kTokens;      // of tensor memory, O behind them
+};
+
+struct Shared {
+  uint64_t full[8], empty[8], s_full[2], p_full[2], o_done[2], q_full, end;
+  uint32_t tmem;
+  int abort;
+  int skip[2];
+  int edge_b;
+  int64_t before, edge[2], scan[18];
+  uint32_t there[8][4];  // of a tile, which of its tokens there are
+  int depth[2][kMostDrafts];
+  float2 ml[128];
+};
+static_assert(sizeof(Shared) <= 2560);
+
+template <int kBytes>
+__device__ __forceinline__ void cp_async(uint32_t dst, const void* src, bool take) {
+  const int n = take ? kBytes : 0;
+  if constexpr (kBytes == 16)
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+  else
+    asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(dst), "l"(src), "n"(kBytes), "r"(n) : "memory");
+}
+__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int n>
+__device__ __forceinline__ void cp_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(n) : "memory");
+}
+__device__ __forceinline__ void cp_wait_at_most(int n) {
+  switch (n) {
+    case 0: return cp_wait<0>();
+    case 1: return cp_wait<1>();
+    case 2: return cp_wait<2>();
+    case 3: return cp_wait<3>();
+    case 4: return cp_wait<4>();
+    default: return cp_wait<5>();
   }
-  const uint32_t byte = static_cast<const uint8_t*>(base)[at + d / 2], sc = scales[sat + d / 16];
-  float lo, hi;
-  f16x2_to_f32(cvt_f16x2_from_e4m3x2((uint16_t)(sc & 0x7Fu)), lo, hi);
-  auto value = [&](uint32_t nib) {
-    const uint32_t p = nib & 7u;
-    const float m = sc >> 7 ? (float)p : (p < 4 ? 0.5f * p : (p == 4 ? 2.0f : (p == 5 ? 3.0f : (p == 6 ? 4.0f : 6.0f))));
-    return (nib & 8u ? -m : m) * lo * ts;
-  };
-  return make_float2(value(byte & 15u), value(byte >> 4));
+}
+__device__ __forceinline__ uint32_t lds8(uint32_t a) {
+  uint32_t v;
+  asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
+  return v;
+}
+__device__ __forceinline__ void sts8(uint32_t a, uint32_t v) {
+  asm volatile("st.shared.u8 [%0], %1;" ::"r"(a), "r"(v) : "memory");
+}
+__device__ __forceinline__ void bar_sync(int id, int threads) {
+  asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
+}
+__device__ __forceinline__ bool bar_or(int id, int threads, bool v) {
+  int r;
+  asm volatile("{ .reg .pred p, q; setp.ne.s32 p, %3, 0; bar.red.or.pred q, %1, %2, p; selp.s32 %0, 1, 0, q; }"
+               : "=r"(r)
+               : "r"(id), "r"(threads), "r"((int)v)
+               : "memory");
+  return r != 0;
+}
+__device__ __forceinline__ uint32_t bf16x2(float lo, float hi) {
+  uint32_t d;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+  return d;
+}
+__device__ __forceinline__ uint32_t f16x2(float lo, float hi) {
+  uint32_t d;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+  return d;
+}
+__device__ __forceinline__ float bf_lo(uint32_t v) { return __uint_as_float(v << 16); }
+__device__ __forceinline__ float bf_hi(uint32_t v) { return __uint_as_float(v & 0xFFFF0000u); }
+// 2^x, results below 2^-126 as zero.
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float rcp(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// tanh within 2^-21 of itself: x P(x^2) / Q(x^2) for |x| <= 9, beyond which it is 1 in fp32.  The coefficients are a
+// weighted least-squares fit of tanh(x) / x that evens out the relative error (2e-8 before rounding).
+__device__ __forceinline__ float tanh_of(float x) {
+  const float z = fminf(fmaxf(x, -9.0f), 9.0f), y = z * z;
+  float a = fmaf(y, 1.335449179e-08f, 2.060896267e-05f), b = fmaf(y, 7.776489695e-07f, 3.285623034e-04f);
+  a = fmaf(y, a, 3.495580968e-03f), b = fmaf(y, b, 2.587695507e-02f);
+  a = fmaf(y, a, 1.338101964e-01f), b = fmaf(y, b, 4.671433524e-01f);
+  a = fmaf(y, a, 1.0f), b = fmaf(y, b, 1.0f);
+  const float r = fminf(fmaxf(z * a * rcp(b), -1.0f), 1.0f);
+  return x != x ? x : r;
+}
+// D[tmem] (+)= A[smem] . B[smem]^T, one CTA, kind::f16.
+__device__ __forceinline__ void mma_f16(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc,
+                                        uint32_t accumulate) {
+  asm volatile(
+      "{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n"
+      " tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d_tmem),
+      "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+// Descriptor of an operand whose rows are its K: 64 elements of M or N to a row of 128 bytes, swizzled as
+// smem_desc_sw128's; 8 rows to 1024 bytes, `lbo` bytes to the next 64 elements.
+__device__ __forceinline__ uint64_t smem_desc_sw128_mn(uint32_t saddr, uint32_t lbo) {
+  uint64_t d = 0;
+  d |= (uint64_t)((saddr >> 4) & 0x3FFFu);
+  d |= (uint64_t)((lbo >> 4) & 0x3FFFu) << 16;
+  d |= (uint64_t)(1024 >> 4) << 32;
+  d |= (uint64_t)1 << 46;
+  d |= (uint64_t)2 << 61;
+  return d;
+}
+__device__ __forceinline__ void tmem_ld1(uint32_t taddr, uint32_t& v) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];" : "=r"(v) : "r"(taddr) : "memory");
+  tmem_ld_wait();
+  asm volatile("" : "+r"(v));
+}
+// kCols (32 or 16) columns of this thread's lane.
+template <int kCols>
+__device__ __forceinline__ void tmem_load(uint32_t taddr, uint32_t* v) {
+  if constexpr (kCols == 32)
+    tmem_ld_32x32b_x32(taddr, v);
+  else
+    tmem_ld_32x32b_x16(taddr, v);
+}
+template <int kCols>
+__device__ __forceinline__ void tmem_loaded(uint32_t* v) {
+  if constexpr (kCols == 32)
+    tmem_ld_wait_x32(v);
+  else
+    tmem_ld_wait_x16(v);
+}
+template <int kCols>
+__device__ __forceinline__ void tmem_store(uint32_t taddr, const uint32_t* v) {
+  if constexpr (kCols == 32) {
+    tmem_st_32x32b_x32(taddr, v);
+  } else if constexpr (kCols == 16) {
+    tmem_st_32x32b_x16(taddr, v);
+  } else {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(taddr), "r"(v[0]),
+                 "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+                 : "memory");
+  }
 }
 
-__global__ void __launch_bounds__(kThreads) tree_attention_kernel(const TreeArgs p) {
-  __shared__ float so[kWarps][256];
-  __shared__ float sm[kWarps], sl[kWarps];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, D = p.c.head_dim;
-  const int64_t row = blockIdx.x;  // [B][t][q_heads]
-  const int h = (int)(row % p.q_heads), i = (int)(row / p.q_heads % p.t);
-  const int64_t b = row / p.q_heads / p.t;
-  const bool fp4 = p.c.dtype == MIXFP4_CACHE_MIXFP4;
-  const float kts = fp4 ? *p.c.k_ts : 1.0f, vts = fp4 ? *p.c.v_ts : 1.0f;
-  const int n = max(p.lengths[b], 0), c = min(min(p.counts ? max(p.counts[b], 0) : p.t, p.t), n), first = n - c;
-  const int end = (int)min((int64_t)n, p.max_tokens);
-  const uint64_t there = c == 64 ? ~0ull : (1ull << c) - 1;
-  auto bits = [&](int k) {
-    return (p.mask ? (uint64_t)p.mask[b * p.mask_stride + k] : (2ull << k) - 1) & there;
+// What of a sequence is looked at.
+struct Span {
+  int n, c, first;  // tokens, drafts, certain tokens
+  int from, end;    // tokens [from, end) may be seen; from is rounded down to 16
+  int low;          // tokens below are not
+};
+__device__ __forceinline__ Span span_of(const TreeArgs& p, int b) {
+  Span s;
+  s.n = max(p.lengths[b], 0);
+  s.c = p.counts ? min(max(p.counts[b], 0), p.t) : p.t;
+  s.c = min(s.c, s.n);
+  s.first = s.n - s.c;
+  s.end = (int)min((int64_t)s.n, p.max_tokens);
+  s.low = p.window > 0 ? (int)max((int64_t)0, s.first + 1 - p.window) : 0;  // of the drafts, those that see none
+  s.from = s.low & ~15;
+  return s;
+}
+// Units of work of a row of the sequence: kRowCost for its beginning, then one to a tile.
+template <int kTokens>
+__device__ __forceinline__ int units_of(const Span& s) {
+  return s.c > 0 && s.end > s.low ? kRowCost + (s.end - s.from + kTokens - 1) / kTokens : 0;
+}
+
+// A part of a row: tiles [tile, tile + tiles) of chunk `chunk` of key head `head` of sequence b, walked from the last on.
+struct Part {
+  Span s;
+  int b, row, head, chunk, tile, tiles;
+  bool first, last;
+  int64_t behind;  // the unit behind the row's last
+};
+// Every role walks a CTA's share in the same steps.
+template <int kTokens>
+struct Walk {
+  int64_t pos, end, base;
+  int b;
+  __device__ __forceinline__ bool next(const TreeArgs& p, int mate, Part& w) {
+    const int rows = p.c.heads / p.together * p.chunks;
+    while (pos < end && b < p.B) {
+      w.s = span_of(p, b);
+      const int u = units_of<kTokens>(w.s);
+      if (u == 0 || pos >= base + (int64_t)u * rows) {
+        base += (int64_t)u * rows;
+        ++b;
+        continue;
+      }
+      w.b = b;
+      w.row = (int)((pos - base) / u);
+      const int k0 = (int)((pos - base) - (int64_t)w.row * u), cnt = (int)min((int64_t)(u - k0), end - pos);
+      w.head = w.row / p.chunks * p.together + mate;
+      w.chunk = w.row % p.chunks;
+      w.tile = max(k0 - kRowCost, 0);
+      w.tiles = k0 + cnt - kRowCost - w.tile;
+      w.first = k0 == 0;
+      w.last = k0 + cnt == u;
+      w.behind = base + (int64_t)(w.row + 1) * u;
+      pos += cnt;
+      if (w.tiles > 0) return true;
+    }
+    return false;
+  }
+};
+
+// A finished row's factor of O, and its log-sum-exp, of m and l.  l is 0 only where no token was seen (or all scores
+// are -inf); NaN goes through, and so does the +inf of a score of +inf.
+template <bool kFp4>
+__device__ __forceinline__ float out_factor(float l, float vts) {
+  return l == 0.0f ? 0.0f : (kFp4 ? 0.5f * vts : 1.0f) / l;
+}
+template <bool kFp4>
+__device__ __forceinline__ float lse_of(float m, float l) {
+  return l == 0.0f ? -INFINITY : (m + log2f(l) - (kFp4 ? kFp4Exp : 0.0f)) * kLn2;
+}
+
+// Which drafts draft k of sequence b sees, of its c.
+__device__ __forceinline__ uint64_t bits_of(const TreeArgs& p, int b, int k, int c) {
+  const uint64_t all = c >= 64 ? ~0ull : (1ull << c) - 1;
+  return (p.mask ? (uint64_t)p.mask[b * p.mask_stride + k] : (2ull << k) - 1) & all;
+}
+__device__ __forceinline__ int depth_of(uint64_t bits, int k) { return __popcll(bits & ~(1ull << k)); }
+
+// Copy n of a MixFP4 tile's rows (this warp's) decoded to f16 at the operand's swizzled places: a lane to 16 elements,
+// twice their values under the block scale alone.
+template <typename C, typename F>
+__device__ __forceinline__ void decode_tile(uint32_t ring, uint32_t raw0, uint32_t n, int pw, int lane, int D, F free) {
+  constexpr int kPieces = (C::kRawRow - 16) / 8, kAtOnce = 32 / kPieces;  // of a row; rows
+  const uint32_t slot = n % C::kSlots, raw = raw0 + (n % C::kRawDepth) * C::kRawSlot;
+  free(slot, ((n / C::kSlots) & 1) ^ 1);
+  const int piece = lane % kPieces, r0 = lane / kPieces;
+  if (piece * 16 >= D) return;
+  const uint32_t to = ring + slot * C::kSlot + (piece >> 2) * C::kBlock;
+#pragma unroll
+  for (int j = 0; j < C::kRows / kAtOnce; ++j) {
+    const int r = r0 + j * kAtOnce, row = pw * C::kRows + r;
+    const uint2 c = lds64(raw + r * C::kRawRow + piece * 8);
+    const uint32_t sc = lds8(raw + r * C::kRawRow + kPieces * 8 + piece), e1m2 = sc >> 7;
+    const uint32_t s2 = cvt_f16x2_from_e4m3x2((uint16_t)((sc & 0x7Fu) * 0x0101u));
+    const uint32_t lo = kLutE2M1Lo + e1m2 * (kLutE1M2Lo - kLutE2M1Lo), hi = kLutE2M1Hi + e1m2 * (kLutE1M2Hi - kLutE2M1Hi);
+    uint32_t v[2][4];
+    decode8(c.x, lo, hi, s2, v[0]);
+    decode8(c.y, lo, hi, s2, v[1]);
+    const int u0 = (piece & 3) * 2;
+    sts128(to + row * 128 + ((u0 ^ (row & 7)) << 4), v[0][0], v[0][1], v[0][2], v[0][3]);
+    sts128(to + row * 128 + (((u0 + 1) ^ (row & 7)) << 4), v[1][0], v[1][1], v[1][2], v[1][3]);
+  }
+}
+
+template <int DT, int NM, bool kFp4>
+__global__ void __launch_bounds__(Cfg<DT, NM, kFp4>::kThreads, 1) tree_attention_kernel(const TreeArgs p) {
+  using C = Cfg<DT, NM, kFp4>;
+  constexpr int TN = C::kTokens, CW = C::kCw;
+  extern __shared__ __align__(1024) uint8_t smem[];
+  Shared& sh = *reinterpret_cast<Shared*>(smem + C::kQ + C::kSlots * C::kSlot + C::kRaw);
+  const uint32_t q_smem = smem_u32(smem), ring = q_smem + C::kQ;
+  volatile int* abort_flag = &sh.abort;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int share = (int)blockIdx.x / p.together, mate = (int)blockIdx.x % p.together;
+  const int D = p.c.head_dim;
+  griddep_launch_dependents();
+
+  if (warp == C::kSoftmax) {
+    tmem_alloc(smem_u32(&sh.tmem), 512);
+    tmem_relinquish();
+  } else if (tid == 0) {
+    for (int i = 0; i < C::kSlots; ++i) {
+      mbar_init(smem_u32(&sh.full[i]), C::kProducers);
+      mbar_init(smem_u32(&sh.empty[i]), 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(smem_u32(&sh.s_full[i]), 1);
+      mbar_init(smem_u32(&sh.p_full[i]), 4);
+      mbar_init(smem_u32(&sh.o_done[i]), 1);
+    }
+    mbar_init(smem_u32(&sh.q_full), C::kSoftmax);
+    mbar_init(smem_u32(&sh.end), 1);
+    sh.abort = 0;
+    sh.edge_b = p.B;
+    p.split[blockIdx.x] = make_int4(-1, 0, 0, 0);
+    fence_mbar_init();
+  }
+
+  // This CTA's share [pos, end) of all units, and the sequence it starts in.
+  Walk<TN> walk;
+  const int rows = p.c.heads / p.together * p.chunks;
+  {
+    const int strip = (p.B + C::kThreads - 1) / C::kThreads, lo = min(p.B, tid * strip), hi = min(p.B, lo + strip);
+    int64_t mine = 0;
+    for (int i = lo; i < hi; ++i) mine += units_of<TN>(span_of(p, i));
+    int64_t before = mine;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int64_t v = __shfl_up_sync(kAll, before, d);
+      if (lane >= d) before += v;
+    }
+    if (lane == 31) sh.scan[warp] = before;
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    int64_t total = 0;
+    for (int w = 0; w < C::kThreads / 32; ++w) {
+      if (w < warp) before += sh.scan[w];
+      total += sh.scan[w];
+    }
+    before -= mine;
+    const int64_t all = total * rows, shares = min(all, (int64_t)p.shares);
+    for (int64_t i = blockIdx.x; i < p.B; i += gridDim.x) {  // sequences that see nothing
+      if (units_of<TN>(span_of(p, (int)i)) > 0) continue;
+      const int64_t heads = (int64_t)p.t * p.q_heads, words = heads * D / 2;
+      for (int64_t k = tid; k < words; k += C::kThreads) reinterpret_cast<uint32_t*>(p.out)[i * words + k] = 0u;
+      if (p.lse)
+        for (int64_t k = tid; k < heads; k += C::kThreads) p.lse[i * heads + k] = -INFINITY;
+    }
+    walk.pos = 0, walk.end = 0, walk.base = 0, walk.b = 0;
+    if (share < shares) {
+      // An edge between shares that falls into a row's beginning lies before the row.
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const int64_t edge = all * (share + k) / shares;
+        if (edge >= before * rows && edge < (before + mine) * rows) {
+          int i = lo;
+          int64_t at = before;
+          int u = units_of<TN>(span_of(p, i));
+          while (i < hi - 1 && edge >= (at + u) * rows) {
+            at += u;
+            u = units_of<TN>(span_of(p, ++i));
+          }
+          const int64_t into = u > 0 ? (edge - at * rows) % u : 0;
+          sh.edge[k] = into <= kRowCost ? edge - into : edge;
+          if (k == 0) sh.edge_b = i, sh.before = at;
+        } else if (edge == all && tid == 0) {
+          sh.edge[k] = all;
+        }
+      }
+    }
+    __syncthreads();
+    if (share < shares) walk.pos = sh.edge[0], walk.end = sh.edge[1], walk.b = sh.edge_b, walk.base = sh.before * rows;
+    // Last share of the row that ends before unit x (see `split`).
+    if (tid == 0) sh.scan[0] = all, sh.scan[1] = shares;
+  }
+  const uint32_t tmem = sh.tmem;
+  bool dead = false;  // a wait has run out: no more waits and no more results, but every step, so that all warps meet
+  auto wait = [&](uint64_t& bar, uint32_t parity, uint32_t bit) {
+    if (!dead && !mbar_wait(smem_u32(&bar), parity, abort_flag, kWaitLimitNs)) {
+      dead = true;
+      if (p.status && !*abort_flag) atomicOr(p.status, bit);
+      *abort_flag = 1;
+    }
   };
-  auto depth = [&](int k) { return __popcll(bits(k) & ~(1ull << k)); };
-  const uint64_t mine = i < c ? bits(i) : 0;
-  const int place = first + depth(i);
-  float2 q[4], o[4];
+  const float kts = kFp4 ? *p.c.k_ts : 1.0f, vts = kFp4 ? *p.c.v_ts : 1.0f;
+  Part w;
+
+  if (warp < C::kSoftmax) {
+    // ================================================= softmax: a row to a thread
+    const int m = warp >> 2, qd = warp & 3, tl = tid & 127;
+    const uint32_t lanes = tmem + ((uint32_t)qd * 32u << 16);
+    const uint32_t o_col = lanes + C::kScoreCols + m * DT;
+    uint32_t g = 0, turn = 0;
+    while (walk.next(p, mate, w)) {
+      const int R = min(128 * NM, p.t * p.group - w.chunk * 128 * NM);
+      const int copies = NM == 2 || R > 64 ? 1 : (R > 32 ? 2 : 4), own = 128 / copies, steps = 4 / copies;
+      const int r = m * 128 + tl % own, copy = tl / own, step0 = copy * steps;
+      const int idx = w.chunk * 128 * NM + r, i = idx / p.group, h = w.head * p.group + idx - i * p.group;
+      const bool held = r < R, valid = held && i < w.s.c;  // rows behind the drafts have a result too, of zeros
+      const bool idle = m * 128 + (copies == 1 ? qd * 32 : 0) >= R;
+      int* depth = sh.depth[turn & 1];
+      if (tid < kMostDrafts) depth[tid] = tid < w.s.c ? depth_of(bits_of(p, w.b, tid, w.s.c), tid) : 0;
+      uint64_t sees = valid ? bits_of(p, w.b, i, w.s.c) : 0;
+      const int place = w.s.first + (valid ? depth_of(sees, i) : 0);
+      const float slope = p.slopes && valid ? p.slopes[h] * -kLog2e : 0.0f;
+
+      // ---- the row's queries, into the swizzled tile
+      float fs = p.scale * (kFp4 ? 0.5f * kts : 1.0f);
+      {
+        const uint16_t* q = p.q + (int64_t)w.b * p.q_stride + (int64_t)i * p.q_token_stride + (int64_t)h * p.q_head_stride;
+        float up = 1.0f;
+        if (kFp4) {  // q times 2^(14 - exponent of the row's largest) as f16
+          float top = 0.0f;
+          if (valid)
+            for (int d = 0; d < D; d += 8) {
+              const uint4 v = *reinterpret_cast<const uint4*>(q + d);
+              top = max3f(top, fabsf(bf_lo(v.x)), fabsf(bf_hi(v.x)));
+              top = max3f(top, fabsf(bf_lo(v.y)), fabsf(bf_hi(v.y)));
+              top = max3f(top, fabsf(bf_lo(v.z)), fabsf(bf_hi(v.z)));
+              top = max3f(top, fabsf(bf_lo(v.w)), fabsf(bf_hi(v.w)));
+            }
+          const int e = min(max((int)(__float_as_uint(top) >> 23), 15), 253);
+          up = __uint_as_float((uint32_t)(268 - e) << 23);
+          fs *= __uint_as_float((uint32_t)(e - 14) << 23);
+        }
+        const uint32_t at = q_smem + m * (128 * DT * 2) + tl * 128;
+        for (int u = 0; u < D / 8; ++u) {
+          uint4 v = make_uint4(0, 0, 0, 0);
+          if (valid) v = *reinterpret_cast<const uint4*>(q + 8 * u);
+          if (kFp4) {
+            v.x = f16x2(bf_lo(v.x) * up, bf_hi(v.x) * up), v.y = f16x2(bf_lo(v.y) * up, bf_hi(v.y) * up);
+            v.z = f16x2(bf_lo(v.z) * up, bf_hi(v.z) * up), v.w = f16x2(bf_lo(v.w) * up, bf_hi(v.w) * up);
+          }
+          sts128(at + (u >> 3) * 16384 + (((u & 7) ^ (tl & 7)) << 4), v.x, v.y, v.z, v.w);
+        }
+      }
+      const float cap2 = p.softcap * kLog2e;
+      fs *= p.softcap > 0.0f ? 1.0f / p.softcap : kLog2e;
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&sh.q_full));
+      bar_sync(1, 128 * NM);  // the depths
+      if (p.window > 0)
+        for (int k = 0; k < w.s.c; ++k)
+          if (place - w.s.first - depth[k] >= p.window) sees &= ~(1ull << k);
+      const int low = p.window > 0 ? (int)max((int64_t)0, place + 1 - p.window) : 0;
+      const bool plain = p.softcap == 0.0f && !p.slopes && p.scale > 0.0f && kts > 0.0f;
+
+      float mx = kNoScore, l = 0.0f, m_aside = kNoScore;  // mx: the m of the weights
+      bool chained = false;
+      float4* aside = p.part + ((2 * (int64_t)blockIdx.x + (w.first ? 1 : 0)) * NM + m) * (DT / 4 * 128) + tl;
+      auto set_aside = [&] {  // O joins what was set aside before, and begins at 0
+        wait(sh.o_done[m], (g - 1) & 1, 1u);
+        __syncwarp();
+        tc_fence_after();
+        const float f = ex2(m_aside - mx);
+#pragma unroll 1
+        for (int d = 0; d < D; d += 16) {
+          uint32_t v[16];
+          tmem_load<16>(o_col + d, v);
+          tmem_loaded<16>(v);
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const int d = 2 * lane + 64 * j;
-    q[j] = o[j] = make_float2(0.0f, 0.0f);
-    if (d < D) {
-      const uint32_t w = *reinterpret_cast<const uint32_t*>(p.q + b * p.q_stride + i * p.q_token_stride +
-                                                            h * p.q_head_stride + d);
-      q[j] = make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
+          for (int e = 0; e < 4; ++e) {
+            float4* a = aside + (d / 4 + e) * 128;
+            float4 x = make_float4(__uint_as_float(v[4 * e]), __uint_as_float(v[4 * e + 1]),
+                                   __uint_as_float(v[4 * e + 2]), __uint_as_float(v[4 * e + 3]));
+            if (chained) {
+              const float4 y = *a;
+              x = make_float4(fmaf(f, y.x, x.x), fmaf(f, y.y, x.y), fmaf(f, y.z, x.z), fmaf(f, y.w, x.w));
+            }
+            *a = x;
+          }
+        }
+        chained = true;
+        m_aside = mx;
+      };
+
+      for (int it = 0; it < w.tiles; ++it, ++g) {
+        const int buf = NM == 2 ? m : (int)(g & 1);
+        const uint32_t scores = lanes + buf * TN;
+        const bool begins = it % kChain == 0;
+        if (it > 0 && begins) set_aside();
+        wait(sh.s_full[buf], NM == 2 ? g & 1 : (g >> 1) & 1, 2u);
+        __syncwarp();
+        tc_fence_after();
+        const int j0 = w.s.from + (w.tile + w.tiles - 1 - it) * TN;
+        const uint32_t* there = sh.there[g & 7];
+        bool whole = there[0] == kAll && there[1] == kAll;
+        if (TN == 128) whole = whole && there[2] == kAll && there[3] == kAll;
+        const bool edge = p.window > 0 && j0 < w.s.first + w.s.c - p.window;  // some rows' windows begin behind j0
+        const bool uneven = w.s.c > 1 && (edge || j0 + TN > w.s.first);       // rows may see different tokens
+        const bool masked = !whole || edge || j0 + TN > w.s.first;
+        const bool general = masked || !plain;
+
+        bool slow = false;
+        if (uneven) {  // a NaN or an infinity in V?
+          const uint32_t q = 2 * g + 1, slot = q % C::kSlots;
+          wait(sh.full[slot], (q / C::kSlots) & 1, 4u);
+          __syncwarp();
+          bool bad = false;
+          if (tl < TN) {
+            constexpr uint32_t kExp = kFp4 ? 0x7C00u : 0x7F80u;
+            const uint32_t at = ring + slot * C::kSlot + tl * 128;
+#pragma unroll 4
+            for (int u = 0; u < D / 8; ++u) {
+              const uint4 v = lds128(at + (u >> 3) * C::kBlock + (((u & 7) ^ (tl & 7)) << 4));
+              const uint32_t x[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                bad = bad || (x[e] & kExp) == kExp || (x[e] & (kExp << 16)) == kExp << 16;
+            }
+          }
+          slow = bar_or(2 + m, 128, bad);
+        }
+        if (!idle) {
+          // ---- the scores' maximum; scores that need more than a factor are put back as they are to be
+          float top = -INFINITY;
+          // Which of a step's tokens the row sees, a bit each.
+          auto seen_of = [&](int s) -> uint32_t {
+            const int a = j0 + s * CW, x = w.s.first - a;
+            const uint32_t have = CW == 32 ? there[s] : (there[s >> 1] >> (16 * (s & 1))) & 0xFFFFu;
+            auto below = [](int k) -> uint32_t { return k <= 0 ? 0u : (k >= 32 ? kAll : (1u << k) - 1u); };
+            uint32_t v = valid ? below(x) & ~below(low - a) : 0u;
+            if (x <= 0)
+              v |= x > -64 ? (uint32_t)(sees >> -x) : 0u;
+            else if (x < 32)
+              v |= (uint32_t)sees << x;
+            return v & have;
+          };
+          if (!general) {
+#pragma unroll 1
+            for (int s = step0; s < step0 + steps; ++s) {
+              uint32_t v[CW];
+              tmem_load<CW>(scores + s * CW, v);
+              tmem_loaded<CW>(v);
+#pragma unroll
+              for (int e = 0; e < CW; e += 2) top = max3f(top, __uint_as_float(v[e]), __uint_as_float(v[e + 1]));
+            }
+            top *= fs;
+          } else {
+#pragma unroll 1
+            for (int s = step0; s < step0 + steps; ++s) {
+              const int a = j0 + s * CW;
+              const uint32_t seen = masked ? seen_of(s) : kAll;
+              uint32_t v[CW];
+              tmem_load<CW>(scores + s * CW, v);
+              tmem_loaded<CW>(v);
+#pragma unroll
+              for (int e = 0; e < CW; ++e) {
+                float x = __uint_as_float(v[e]) * fs;
+                if (p.softcap > 0.0f) x = cap2 * tanh_of(x);
+                if (p.slopes) {
+                  const int j = a + e;
+                  int far = place - j;
+                  if (j >= w.s.first) far = place - w.s.first - depth[min(j - w.s.first, kMostDrafts - 1)];
+                  x = fmaf(slope, (float)far, x);
+                }
+                x = (seen >> e) & 1u ? x : -INFINITY;
+                top = fmaxf(top, x);
+                v[e] = __float_as_uint(x);
+              }
+              tmem_store<CW>(scores + s * CW, v);
+            }
+            tmem_st_wait();
+          }
+          const float f = general ? 1.0f : fs;
+          if (__any_sync(kAll, top > mx + kSlack)) {
+            const float v = fminf(fmaxf(mx, top), kMostScore), cor = ex2(mx - v);  // 0 at the first score
+            mx = v;
+            l *= cor;
+            if (!begins) {
+              wait(sh.o_done[m], (g - 1) & 1, 8u);
+              __syncwarp();
+              tc_fence_after();
+#pragma unroll 1
+              for (int d = 0; d < D; d += 16) {
+                uint32_t o[16];
+                tmem_load<16>(o_col + d, o);
+                tmem_loaded<16>(o);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * cor);
+                tmem_store<16>(o_col + d, o);
+              }
+              tmem_st_wait();
+            }
+          }
+
+          // ---- the weights
+          const float less = (kFp4 ? kFp4Exp : 0.0f) - mx;
+          float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+          if (!slow) {
+#pragma unroll 1
+            for (int s = 0; s < 4; ++s) {
+              constexpr int kOut = kFp4 ? CW / 2 : CW;
+              uint32_t v[CW], out[kOut];
+              if (s < step0 || s >= step0 + steps) {  // another copy's tokens
+#pragma unroll
+                for (int e = 0; e < kOut; ++e) out[e] = 0u;
+              } else {
+                tmem_load<CW>(scores + s * CW, v);
+                tmem_loaded<CW>(v);
+#pragma unroll
+                for (int e = 0; e < CW; e += 2) {
+                  const float w0 = ex2(fmaf(__uint_as_float(v[e]), f, less)), w1 = ex2(fmaf(__uint_as_float(v[e + 1]), f, less));
+                  sum[e & 2] += w0;
+                  sum[(e & 2) + 1] += w1;
+                  if (kFp4) {
+                    out[e / 2] = f16x2(w0, w1);
+                  } else {
+                    // The upper part by truncation, so that the lower is not negative, and not 0 either where the weight
+                    // is not (2^-126 then): times an infinite element of V both give its infinity.
+                    out[e / 2] = prmt(__float_as_uint(w0), __float_as_uint(w1), 0x7632u);
+                    out[CW / 2 + e / 2] = bf16x2(fmaxf(w0 - bf_hi(__float_as_uint(w0)), fminf(w0, 0x1p-126f)),
+                                                 fmaxf(w1 - bf_hi(__float_as_uint(w1)), fminf(w1, 0x1p-126f)));
+                  }
+                }
+              }
+              tmem_store<kOut>(scores + s * CW, out);
+            }
+          } else {
+            // Products of what the row sees alone.
+            const uint32_t slot = (2 * g + 1) % C::kSlots, v_smem = ring + slot * C::kSlot;
+            if (!begins) {
+              wait(sh.o_done[m], (g - 1) & 1, 16u);
+              __syncwarp();
+              tc_fence_after();
+            }
+#pragma unroll 1
+            for (int d = 0; d < D; d += 16) {
+              uint32_t o[16];
+              if (!begins) {
+                tmem_load<16>(o_col + d, o);
+                tmem_loaded<16>(o);
+              } else {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) o[e] = 0u;
+              }
+#pragma unroll 1
+              for (int k = 0; k < steps * CW; ++k) {
+                const int col = step0 * CW + k;
+                uint32_t xs;
+                tmem_ld1(scores + col, xs);
+                const float x = fmaf(__uint_as_float(xs), f, less), wt = ex2(x);
+                if (d == 0) sum[0] += wt;
+                const bool mine = (seen_of(col / CW) >> (col % CW)) & 1u;
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                  const uint4 v = lds128(v_smem + (d >> 6) * C::kBlock + col * 128 +
+                                         ((((d >> 3) & 7) + u) ^ (col & 7)) * 16);
+                  const uint32_t y[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                  for (int e = 0; e < 4; ++e) {
+                    float a0, a1;
+                    if (kFp4)
+                      f16x2_to_f32(y[e], a0, a1);
+                    else
+                      a0 = bf_lo(y[e]), a1 = bf_hi(y[e]);
+                    const float b0 = __uint_as_float(o[8 * u + 2 * e]), b1 = __uint_as_float(o[8 * u + 2 * e + 1]);
+                    o[8 * u + 2 * e] = __float_as_uint(mine ? fmaf(wt, a0, b0) : b0);
+                    o[8 * u + 2 * e + 1] = __float_as_uint(mine ? fmaf(wt, a1, b1) : b1);
+                  }
+                }
+              }
+              tmem_store<16>(o_col + d, o);
+            }
+          }
+          l += (sum[0] + sum[2]) + (sum[1] + sum[3]);
+          tmem_st_wait();
+        }
+        if (tl == 0) sh.skip[buf] = slow;
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&sh.p_full[buf]));
+      }
+
+      // ---- the part's end: O, m and l of every row, finished where the part is the whole row
+      wait(sh.o_done[m], (g - 1) & 1, 32u);
+      __syncwarp();
+      tc_fence_after();
+      const bool all = w.first && w.last;
+      const int64_t slot = (2 * (int64_t)blockIdx.x + (w.first ? 1 : 0)) * NM + m;
+      float4* part = p.part + slot * (DT / 4 * 128);
+      const int64_t at = ((int64_t)w.b * p.t + i) * p.q_heads + h;  // of the results
+      const float old = chained ? ex2(m_aside - mx) : 0.0f;
+      if (!valid) mx = kNoScore, l = 0.0f;
+      if (copies > 1) {
+        sh.ml[tl] = make_float2(mx, l);
+        bar_sync(2 + m, 128);
+      }
+      float M = mx, L = l;
+      if (copies > 1) {
+        for (int k = 0; k < copies; ++k) M = fmaxf(M, sh.ml[tl % own + k * own].x);
+        L = 0.0f;
+        for (int k = 0; k < copies; ++k) {
+          const float2 s = sh.ml[tl % own + k * own];
+          L += ex2(s.x - M) * s.y;
+        }
+      }
+      const float last = all ? out_factor<kFp4>(L, vts) : 1.0f, f = copies > 1 ? ex2(mx - M) : 1.0f;
+      // Columns [d, d + 8) of the row's sum, to their place.
+      auto put = [&](int d, const float* x) {
+        if (!held || dead || d >= D) return;
+        if (all) {
+          uint4 v;
+          v.x = bf16x2(x[0] * last, x[1] * last), v.y = bf16x2(x[2] * last, x[3] * last);
+          v.z = bf16x2(x[4] * last, x[5] * last), v.w = bf16x2(x[6] * last, x[7] * last);
+          *reinterpret_cast<uint4*>(p.out + at * D + d) = v;
+        } else {
+          part[(d / 4) * 128 + tl % own] = make_float4(x[0], x[1], x[2], x[3]);
+          part[(d / 4 + 1) * 128 + tl % own] = make_float4(x[4], x[5], x[6], x[7]);
+        }
+      };
+      auto take = [&](int d, float* x) {  // 16 columns of O, with what was set aside
+        uint32_t v[16];
+        tmem_load<16>(o_col + d, v);
+        tmem_loaded<16>(v);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) x[e] = __uint_as_float(v[e]);
+        if (chained) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float4 y = aside[(d / 4 + e) * 128];
+            x[4 * e] = fmaf(old, y.x, x[4 * e]), x[4 * e + 1] = fmaf(old, y.y, x[4 * e + 1]);
+            x[4 * e + 2] = fmaf(old, y.z, x[4 * e + 2]), x[4 * e + 3] = fmaf(old, y.w, x[4 * e + 3]);
+          }
+        }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) x[e] = valid ? x[e] * f : 0.0f;
+      };
+      if (copies == 1) {
+        if (!idle)
+#pragma unroll 1
+          for (int d = 0; d < D; d += 16) {
+            float x[16];
+            take(d, x);
+            put(d, x);
+            put(d + 8, x + 8);
+          }
+      } else {
+        float* stage = reinterpret_cast<float*>(smem);  // [half the dimensions][128], where the queries were
+        constexpr int kHalf = DT / 2;
+        const int each = kHalf / copies;
+#pragma unroll 1
+        for (int half = 0; half < 2 && half * kHalf < D; ++half) {
+#pragma unroll 1
+          for (int d = 0; d < kHalf; d += 16) {
+            float x[16];
+            take(half * kHalf + d, x);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) stage[(d + e) * 128 + tl] = x[e];
+          }
+          bar_sync(2 + m, 128);
+#pragma unroll 1
+          for (int d = copy * each; d < (copy + 1) * each; d += 8) {
+            float x[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const float* s = stage + (d + e) * 128 + tl % own;
+              x[e] = s[0] + s[own];
+              if (copies == 4) x[e] += s[2 * own] + s[3 * own];
+            }
+            put(half * kHalf + d, x);
+          }
+          bar_sync(2 + m, 128);
+        }
+      }
+      if (held && copy == 0 && !dead) {
+        if (!all)
+          p.stat[slot * 128 + tl] = make_float2(M, L);
+        else if (p.lse)
+          p.lse[at] = lse_of<kFp4>(M, L);
+      }
+      if (tid == 0 && w.first && !w.last)
+        p.split[blockIdx.x] = make_int4(w.b, w.row, share, (int)((w.behind * sh.scan[1] - 1) / sh.scan[0]));
+      tc_fence_before();
+      __syncwarp();
+      ++turn;
     }
+  } else if (warp == C::kSoftmax) {
+    // ================================================= one thread issues the products
+    if (elect_one()) {
+      constexpr uint32_t kType = kFp4 ? 0u : (1u << 7) | (1u << 10);
+      const uint32_t i_scores = (1u << 4) | kType | ((uint32_t)(TN >> 3) << 17) | (8u << 24);
+      const uint32_t i_out = (1u << 4) | kType | (1u << 16) | ((uint32_t)(D >> 3) << 17) | (8u << 24);
+      uint32_t g = 0, turn = 0;
+      auto scores = [&](uint32_t tile, int m) {  // of tile number `tile`, into its buffer
+        const uint32_t q = 2 * tile, slot = q % C::kSlots;
+        if (m == 0) {
+          wait(sh.full[slot], (q / C::kSlots) & 1, 64u);
+          tc_fence_after();
+        }
+        const int buf = NM == 2 ? m : (int)(tile & 1);
+        const uint32_t a = q_smem + m * (128 * DT * 2), b = ring + slot * C::kSlot;
+#pragma unroll 1
+        for (int k = 0; k < D / 16; ++k)
+          mma_f16(tmem + buf * TN, smem_desc_sw128(a + (k >> 2) * 16384 + (k & 3) * 32),
+                  smem_desc_sw128(b + (k >> 2) * C::kBlock + (k & 3) * 32), i_scores, k > 0);
+        mma_commit(smem_u32(&sh.s_full[buf]));
+        if (m == NM - 1) mma_commit(smem_u32(&sh.empty[slot]));
+      };
+      while (walk.next(p, mate, w)) {
+        wait(sh.q_full, turn & 1, 128u);
+        ++turn;
+        tc_fence_after();
+        for (int m = 0; m < NM; ++m) scores(g, m);
+        for (int it = 0; it < w.tiles; ++it, ++g) {
+          if (NM == 1 && it + 1 < w.tiles) scores(g + 1, 0);
+          const uint32_t q = 2 * g + 1, slot = q % C::kSlots, v = ring + slot * C::kSlot;
+          for (int m = 0; m < NM; ++m) {
+            const int buf = NM == 2 ? m : (int)(g & 1);
+            if (m == 0) wait(sh.full[slot], (q / C::kSlots) & 1, 256u);
+            wait(sh.p_full[buf], NM == 2 ? g & 1 : (g >> 1) & 1, 512u);
+            tc_fence_after();
+            if (!*reinterpret_cast<volatile int*>(&sh.skip[buf])) {
+#pragma unroll 1
+              for (int k = 0; k < TN / 16; ++k) {
+                const uint32_t a = tmem + buf * TN + (k * 16 / CW) * CW + (k * 16 % CW) / 2;
+                const uint64_t b = smem_desc_sw128_mn(v + k * 2048, C::kBlock);
+                mma_f16_tmem_a(tmem + C::kScoreCols + m * DT, a, b, i_out, k > 0 || it % kChain != 0);
+                if (!kFp4) mma_f16_tmem_a(tmem + C::kScoreCols + m * DT, a + CW / 2, b, i_out, 1u);
+              }
+            }
+            mma_commit(smem_u32(&sh.o_done[m]));
+            if (m == NM - 1) mma_commit(smem_u32(&sh.empty[slot]));
+            if (NM == 2 && it + 1 < w.tiles) scores(g + 1, m);
+          }
+        }
+      }
+      mma_commit(smem_u32(&sh.end));
+      mbar_wait(smem_u32(&sh.end), 0, nullptr, kWaitLimitNs);
+    }
+  } else {
+    // ================================================= producers
+    const int pw = warp - C::kSoftmax - 1;
+    constexpr int kRows = C::kRows;
+    uint32_t g = 0, q = 0, sent = 0;  // tiles, copies asked for, copies handed over
+    auto arrive = [&](uint32_t n) {   // copy n has landed, for the tensor cores too
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&sh.full[n % C::kSlots]));
+    };
+    while (walk.next(p, mate, w)) {
+      const int32_t* table = p.table + (int64_t)w.b * p.table_stride;
+      auto page_of = [&](int tok) { return p.page_shift >= 0 ? tok >> p.page_shift : tok / p.c.page_size; };
+      // Page of this lane's token of the tile.
+      auto ask = [&](int it) -> int {
+        const int tok = w.s.from + (w.tile + w.tiles - 1 - it) * TN + pw * kRows + lane;
+        return it < w.tiles && lane < kRows && tok >= w.s.low && tok < w.s.end ? table[page_of(tok)] : -1;
+      };
+      int page = ask(0);
+#pragma unroll 1
+      for (int it = 0; it < w.tiles; ++it, ++g) {
+        const int tok = w.s.from + (w.tile + w.tiles - 1 - it) * TN + pw * kRows + lane;
+        const bool ok = page >= 0 && page < p.c.pages;
+        int64_t at = 0, sat = 0;
+        if (ok) {
+          const int off = tok - page_of(tok) * p.c.page_size;
+          at = ((int64_t)page * p.c.page_stride + (int64_t)off * p.c.token_stride + (int64_t)w.head * p.c.head_stride) *
+               (kFp4 ? 1 : 2);
+          sat = (int64_t)page * p.c.scale_page_stride + (int64_t)off * p.c.scale_token_stride +
+                (int64_t)w.head * p.c.scale_head_stride;
+        }
+        page = ask(it + 1);
+        const uint32_t there = __ballot_sync(kAll, ok);
+        if (lane == 0) {
+          uint8_t* to = reinterpret_cast<uint8_t*>(sh.there[g & 7]) + pw * (kRows / 8);
+          if constexpr (kRows == 32)
+            *reinterpret_cast<uint32_t*>(to) = there;
+          else if constexpr (kRows == 16)
+            *reinterpret_cast<uint16_t*>(to) = (uint16_t)there;
+          else
+            *to = (uint8_t)there;
+        }
+#pragma unroll 1
+        for (int kv = 0; kv < 2; ++kv, ++q) {
+          if constexpr (!kFp4) {
+            const uint32_t slot = q % C::kSlots;
+            wait(sh.empty[slot], ((q / C::kSlots) & 1) ^ 1, 1024u);
+            __syncwarp();
+            const uint8_t* base = static_cast<const uint8_t*>(kv ? p.c.v : p.c.k);
+            constexpr int kPieces = DT / 8, kAtOnce = 32 / kPieces;  // of a row; rows
+            const int piece = lane % kPieces, r0 = lane / kPieces;
+            const bool in_row = piece * 8 < D;
+            const uint32_t dst = ring + slot * C::kSlot + (piece >> 3) * C::kBlock;
+#pragma unroll
+            for (int j = 0; j < kRows / kAtOnce; ++j) {
+              const int r = r0 + j * kAtOnce, row = pw * kRows + r;
+              const int64_t from = __shfl_sync(kAll, at, r);
+              const bool take = in_row && ((there >> r) & 1u);
+              cp_async<16>(dst + row * 128 + (((piece & 7) ^ (row & 7)) << 4), base + (take ? from + piece * 16 : 0), take);
+            }
+            cp_commit();
+            if (q - sent >= C::kLag) {
+              cp_wait<C::kLag>();
+              arrive(sent++);
+            }
+          } else {
+            // ---- the codes as they lie, into this warp's own part
+            const uint32_t raw0 = ring + C::kSlots * C::kSlot + pw * C::kRawDepth * C::kRawSlot;
+            uint32_t raw = raw0 + (q % C::kRawDepth) * C::kRawSlot;
+            const uint8_t* base = static_cast<const uint8_t*>(kv ? p.c.v : p.c.k);
+            const uint8_t* scales = kv ? p.c.v_scales : p.c.k_scales;
+            constexpr int kPieces = DT / 16, kAtOnce = 32 / kPieces;
+            const int piece = lane % kPieces, r0 = lane / kPieces;
+            const bool in_row = piece * 16 < D;
+#pragma unroll
+            for (int j = 0; j < kRows / kAtOnce; ++j) {
+              const int r = r0 + j * kAtOnce;
+              const int64_t from = __shfl_sync(kAll, at, r);
+              const bool take = in_row && ((there >> r) & 1u);
+              cp_async<8>(raw + r * C::kRawRow + piece * 8, base + (take ? from + piece * 8 : 0), take);
+            }
+            if (lane < kRows) {
+              const uint32_t sd = raw + lane * C::kRawRow + DT / 2;
+              const uint8_t* src = scales + (ok ? sat : 0);
+              if (D == 128) {
+                cp_async<8>(sd, src, ok);
+              } else if (D == 256) {
+                cp_async<16>(sd, src, ok);
+              } else if (D % 64 == 0) {
+                for (int k = 0; k < D / 16; k += 4) cp_async<4>(sd + k, src + k, ok);
+              } else {  // rows of an odd number of scale bytes
+                for (int k = 0; k < D / 16; ++k) sts8(sd + k, ok ? src[k] : 0u);
+              }
+            }
+            cp_commit();
+            if (q - sent >= C::kLag) {
+              cp_wait<C::kLag>();
+              __syncwarp();
+              decode_tile<C>(ring, raw0, sent, pw, lane, D, [&](uint32_t slot, uint32_t parity) {
+                wait(sh.empty[slot], parity, 1024u);
+                __syncwarp();
+              });
+              arrive(sent++);
+            }
+          }
+        }
+      }
+    }
+    while (sent < q) {
+      cp_wait_at_most((int)(q - sent - 1));
+      __syncwarp();
+      if constexpr (kFp4)
+        decode_tile<C>(ring, ring + C::kSlots * C::kSlot + pw * C::kRawDepth * C::kRawSlot, sent, pw, lane, D,
+                       [&](uint32_t slot, uint32_t parity) {
+                         wait(sh.empty[slot], parity, 1024u);
+                         __syncwarp();
+                       });
+      arrive(sent++);
+    }
+    cp_async_wait_all();
   }
-  float m = kNoScore, l = 0.0f;
-  for (int j = warp; j < end && i < c; j += kWarps) {
-    const int k = j - first;
-    const int at = k < 0 ? j : first + depth(k);
-    if (k >= 0 && !(mine >> k & 1)) continue;
-    if (p.window > 0 && place - at >= p.window) continue;
-    const int page = p.table[b * p.table_stride + j / p.c.page_size], off = j % p.c.page_size;
-    if (page < 0 || page >= p.c.pages) continue;
-    const int64_t kat = page * p.c.page_stride + off * p.c.token_stride + h / p.group * p.c.head_stride;
-    const int64_t sat = page * p.c.scale_page_stride + off * p.c.scale_token_stride + h / p.group * p.c.scale_head_stride;
-    float s = 0.0f;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int d = 2 * lane + 64 * e;
-      if (d >= D) break;
-      const float2 v = pair_of(p.c.k, p.c.k_scales, kat, sat, d, fp4, kts);
-      s += q[e].x * v.x + q[e].y * v.y;
-    }
-#pragma unroll
-    for (int e = 16; e > 0; e >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, e);
-    s *= p.scale;
-    if (p.softcap > 0.0f) s = p.softcap * tanhf(s / p.softcap);
-    if (p.slopes) s -= p.slopes[h] * (float)(place - at);
-    const float top = fminf(fmaxf(m, s), kMostScore), old = expf(m - top), w = expf(s - top);
-    m = top;
-    l = l * old + w;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int d = 2 * lane + 64 * e;
-      if (d >= D) break;
-      const float2 v = pair_of(p.c.v, p.c.v_scales, kat, sat, d, fp4, vts);
-      o[e].x = o[e].x * old + w * v.x, o[e].y = o[e].y * old + w * v.y;
-    }
-  }
-#pragma unroll
-  for (int e = 0; e < 4; ++e) so[warp][2 * lane + 64 * e] = o[e].x, so[warp][2 * lane + 64 * e + 1] = o[e].y;
-  if (lane == 0) sm[warp] = m, sl[warp] = l;
+  __syncwarp();
+  tc_fence_before();
   __syncthreads();
-  float M = kNoScore, L = 0.0f;
-  for (int w = 0; w < kWarps; ++w) M = fmaxf(M, sm[w]);
-  for (int w = 0; w < kWarps; ++w) L += sl[w] == 0.0f ? 0.0f : sl[w] * expf(sm[w] - M);
-  const int d = threadIdx.x;
-  float x = 0.0f;
-  for (int w = 0; w < kWarps; ++w)
-    if (sl[w] != 0.0f) x += so[w][d] * expf(sm[w] - M);
-  if (L != 0.0f) x /= L;
-  if (d < D) {
-    uint16_t r;
-    asm("cvt.rn.bf16.f32 %0, %1;" : "=h"(r) : "f"(x));
-    p.out[row * D + d] = r;
+  if (warp == C::kSoftmax) {
+    tc_fence_after();
+    tmem_dealloc(tmem, 512);
   }
-  if (d == 0 && p.lse) p.lse[row] = L == 0.0f ? -INFINITY : M + logf(L);
+}
+
+// Joins the parts of the row that CTA blockIdx.x began: a thread to four dimensions of a query row.
+template <int DT, int NM, bool kFp4>
+__global__ void __launch_bounds__(kJoinThreads) tree_attention_join_kernel(const TreeArgs p) {
+  griddep_wait();
+  const int4 s = p.split[blockIdx.x];
+  if (s.x < 0) return;
+  const int mate = (int)blockIdx.x % p.together, chunk = s.y % p.chunks, head = s.y / p.chunks * p.together + mate;
+  const int R = min(128 * NM, p.t * p.group - chunk * 128 * NM), D = p.c.head_dim;
+  const int x = (int)blockIdx.y * kJoinThreads + (int)threadIdx.x, r = x % R, d4 = x / R;
+  if (d4 >= D / 4) return;
+  auto slot = [&](int k) {
+    return (2 * ((int64_t)k * p.together + mate) + (k == s.z ? 1 : 0)) * NM + (r >> 7);
+  };
+  float M = kNoScore, L = 0.0f;
+  float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  constexpr int kAtOnce = 4;  // parts asked for at once, with their (m, l)
+  for (int k0 = s.z; k0 <= s.w; k0 += kAtOnce) {
+    float2 st[kAtOnce];
+    float4 v[kAtOnce];
+#pragma unroll
+    for (int a = 0; a < kAtOnce; ++a) {
+      st[a] = make_float2(kNoScore, 0.0f), v[a] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+      if (k0 + a <= s.w) {
+        st[a] = p.stat[slot(k0 + a) * 128 + (r & 127)];
+        v[a] = p.part[slot(k0 + a) * (DT / 4 * 128) + d4 * 128 + (r & 127)];
+      }
+    }
+    float top = M;
+#pragma unroll
+    for (int a = 0; a < kAtOnce; ++a) top = fmaxf(top, st[a].x);
+    const float old = ex2(M - top);
+    M = top;
+    L *= old;
+    o.x *= old, o.y *= old, o.z *= old, o.w *= old;
+#pragma unroll
+    for (int a = 0; a < kAtOnce; ++a) {
+      const float f = ex2(st[a].x - M);
+      L += f * st[a].y;
+      o.x = fmaf(f, v[a].x, o.x), o.y = fmaf(f, v[a].y, o.y);
+      o.z = fmaf(f, v[a].z, o.z), o.w = fmaf(f, v[a].w, o.w);
+    }
+  }
+  const int idx = chunk * 128 * NM + r, i = idx / p.group, h = head * p.group + idx - i * p.group;
+  const int64_t at = ((int64_t)s.x * p.t + i) * p.q_heads + h;
+  const float f = out_factor<kFp4>(L, kFp4 ? *p.c.v_ts : 1.0f);
+  *reinterpret_cast<uint2*>(p.out + at * D + d4 * 4) = make_uint2(bf16x2(o.x * f, o.y * f), bf16x2(o.z * f, o.w * f));
+  if (d4 == 0 && p.lse) p.lse[at] = lse_of<kFp4>(M, L);
 }
 
 inline bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 inline int launch_status() { return cudaGetLastError() == cudaSuccess ? MIXFP4_OK : MIXFP4_ERR_CUDA; }
+
+inline int padded_dim(int D) { return D <= 64 ? 64 : (D <= 128 ? 128 : 256); }
+// Tiles of 128 rows that share the tokens.
+inline int row_tiles(const mixfp4_kv_cache* c, int64_t t, int64_t q_heads) {
+  return c->head_dim <= 128 && t * (q_heads / c->heads) > 128 ? 2 : 1;
+}
+inline int tile_tokens(const mixfp4_kv_cache* c) { return c->head_dim > 128 ? 64 : 128; }
+// Key heads whose CTAs walk over the same tokens at the same time.
+inline int together_of(const mixfp4_kv_cache* c) {
+  for (int n = 8; n > 1; n /= 2)
+    if (c->heads % n == 0) return n;
+  return 1;
+}
+inline int grid_of(const mixfp4_kv_cache* c) { return num_sms() / together_of(c) * together_of(c); }
+
+template <int DT, int NM, bool kFp4>
+int launch(const TreeArgs& p, int grid, cudaStream_t s) {
+  using C = Cfg<DT, NM, kFp4>;
+  static std::atomic<uint64_t> done{0};
+  auto* kernel = tree_attention_kernel<DT, NM, kFp4>;
+  if (!set_dynamic_smem_once(reinterpret_cast<const void*>(kernel), C::kSmem, done)) return MIXFP4_ERR_CUDA;
+  kernel<<<grid, C::kThreads, C::kSmem, s>>>(p);
+  if (int st = launch_status()) return st;
+  if (!p.joined) return MIXFP4_OK;
+  const int rows = p.t * p.group < 128 * NM ? p.t * p.group : 128 * NM;
+  const dim3 jg((unsigned)grid, (unsigned)((rows * (p.c.head_dim / 4) + kJoinThreads - 1) / kJoinThreads));
+  return launch_pdl(tree_attention_join_kernel<DT, NM, kFp4>, jg, dim3(kJoinThreads), 0, s, p) == cudaSuccess
+             ? MIXFP4_OK
+             : MIXFP4_ERR_CUDA;
+}
+
+template <bool kFp4>
+int launch_dim(const TreeArgs& p, int grid, int tiles, cudaStream_t s) {
+  switch (padded_dim(p.c.head_dim)) {
+    case 64: return tiles == 2 ? launch<64, 2, kFp4>(p, grid, s) : launch<64, 1, kFp4>(p, grid, s);
+    case 128: return tiles == 2 ? launch<128, 2, kFp4>(p, grid, s) : launch<128, 1, kFp4>(p, grid, s);
+    default: return launch<256, 1, kFp4>(p, grid, s);
+  }
+}
 
 }  // namespace
 }  // namespace mixfp4
@@ -153,7 +1135,8 @@ int mixfp4_tree_attention_workspace(const mixfp4_kv_cache* cache, int64_t B, int
   if (B < 0 || t < 0 || t > kMostDrafts || q_heads < 0 || q_heads % cache->heads != 0) return MIXFP4_ERR_SHAPE;
   *bytes = 0;
   if (B == 0 || t == 0 || q_heads == 0) return MIXFP4_OK;
-  *bytes = 256;
+  const int64_t grid = grid_of(cache), rows = 128 * row_tiles(cache, t, q_heads);
+  *bytes = (grid * 16 + 255) / 256 * 256 + 2 * grid * rows * (8 + padded_dim(cache->head_dim) * 4);
   return MIXFP4_OK;
 }
 
@@ -162,7 +1145,7 @@ int mixfp4_tree_attention(const void* q, int64_t q_stride, int64_t q_token_strid
                           int64_t table_stride, int64_t table_pages, const int32_t* lengths, const int64_t* mask,
                           int64_t mask_stride, const int32_t* counts, float scale, int64_t window, float softcap,
                           const float* slopes, void* out, float* lse, void* workspace, int64_t workspace_bytes,
-                          void* stream) {
+                          uint32_t* status_word, void* stream) {
   using namespace mixfp4;
   int64_t need = 0;
   if (int st = mixfp4_tree_attention_workspace(cache, B, t, q_heads, &need)) return st;
@@ -176,7 +1159,7 @@ int mixfp4_tree_attention(const void* q, int64_t q_stride, int64_t q_token_strid
   if (!q || !out || !lengths || !workspace || (table_pages > 0 && !block_table)) return MIXFP4_ERR_NULL;
   if (!aligned(q, 16) || q_stride % 8 || q_token_stride % 8 || q_head_stride % 8 || !aligned(block_table, 4) ||
       !aligned(lengths, 4) || !aligned(mask, 8) || !aligned(counts, 4) || !aligned(slopes, 4) || !aligned(out, 16) ||
-      !aligned(lse, 4) || !aligned(workspace, 256))
+      !aligned(lse, 4) || !aligned(workspace, 256) || !aligned(status_word, 4))
     return MIXFP4_ERR_ALIGN;
   TreeArgs p = {};
   p.q = static_cast<const uint16_t*>(q);
@@ -187,10 +1170,27 @@ int mixfp4_tree_attention(const void* q, int64_t q_stride, int64_t q_token_strid
   p.lengths = lengths, p.mask = mask, p.mask_stride = mask_stride, p.counts = counts;
   p.scale = scale, p.softcap = softcap, p.window = window, p.slopes = slopes;
   p.out = static_cast<uint16_t*>(out), p.lse = lse;
-  const int64_t rows = B * t * q_heads;
-  if (rows > INT32_MAX) return MIXFP4_ERR_SHAPE;
-  tree_attention_kernel<<<(unsigned)rows, kThreads, 0, static_cast<cudaStream_t>(stream)>>>(p);
-  return launch_status();
+  p.status = status_word;
+  const int grid = grid_of(cache), tiles = row_tiles(cache, t, q_heads);
+  const int64_t rows = t * p.group;
+  if (rows > INT32_MAX - 256) return MIXFP4_ERR_SHAPE;
+  p.chunks = (int)((rows + 128 * tiles - 1) / (128 * tiles));
+  p.together = together_of(cache);
+  p.shares = grid / p.together;
+  // Rows of one tile are never cut.
+  const int64_t bound = window > 0 && window + t < p.max_tokens ? window + t + 15 : p.max_tokens;
+  p.joined = bound > tile_tokens(cache);
+  p.page_shift = -1;
+  for (int i = 0; i < 31; ++i)
+    if (cache->page_size == 1 << i) p.page_shift = i;
+  uint8_t* w = static_cast<uint8_t*>(workspace);
+  p.split = reinterpret_cast<int4*>(w);
+  w += ((int64_t)grid * 16 + 255) / 256 * 256;
+  p.stat = reinterpret_cast<float2*>(w);
+  p.part = reinterpret_cast<float4*>(w + 2 * (int64_t)grid * 128 * tiles * 8);
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (status_word && cudaMemsetAsync(status_word, 0, 4, s) != cudaSuccess) return MIXFP4_ERR_CUDA;
+  return cache->dtype == MIXFP4_CACHE_MIXFP4 ? launch_dim<true>(p, grid, tiles, s) : launch_dim<false>(p, grid, tiles, s);
 }
 
 }  // extern "C"

@@ -920,7 +920,7 @@ def mixfp4_tree_attention(q: torch.Tensor, cache: KVCache, block_table: torch.Te
                           scale: float | None = None, window: int = 0, softcap: float = 0.0,
                           slopes: torch.Tensor | None = None, return_lse: bool = False,
                           out: torch.Tensor | None = None, lse: torch.Tensor | None = None,
-                          workspace: torch.Tensor | None = None, stream=None):
+                          workspace: torch.Tensor | None = None, status_word: torch.Tensor | None = None, stream=None):
     """Attention of up to 64 drafted tokens per sequence over the paged cache, which
     holds their keys and values behind the tokens that are certain (with one draft
     a sequence: one-token attention with the options below).
@@ -937,8 +937,11 @@ def mixfp4_tree_attention(q: torch.Tensor, cache: KVCache, block_table: torch.Te
     log-sum-exp of the scores, float32 [B, t, q_heads].  A draft that sees nothing,
     and rows behind a sequence's drafts, give zeros and -inf.  out overlaps no input.
     workspace: scratch memory of the caller's, at least
-    tree_attention_workspace_bytes(cache, B, t, q_heads), aligned to 256 bytes."""
+    tree_attention_workspace_bytes(cache, B, t, q_heads), aligned to 256 bytes.
+    status_word: as mixfp4_gemm's."""
     _check_cache(cache)
+    if status_word is not None:
+        _check_status(status_word, cache.device)
     if stream is not None:
         B, t, H, D = _shape(q, 4)
         out = _result((B, t, H, D), torch.bfloat16, cache.device, stream) if out is None else out
@@ -947,7 +950,8 @@ def mixfp4_tree_attention(q: torch.Tensor, cache: KVCache, block_table: torch.Te
         if workspace is None and _elsewhere(stream, cache.device) and H % cache.heads == 0 and t <= 64:
             workspace = _empty(tree_attention_workspace_bytes(cache, B, t, H), torch.uint8, cache.device, stream, True)
     r = _native().tree_attention(cache._address, cache._index, q, block_table, lengths, mask, counts, scale, window,
-                                 softcap, slopes, out, lse, return_lse, workspace, _stream(stream))
+                                 softcap, slopes, out, lse, return_lse, workspace, _ptr(status_word) if status_word is not None else None,
+                                 _stream(stream))
     if r.__class__ is int:
         _check("mixfp4_tree_attention", r)
     return r

@@ -2,7 +2,11 @@
 
 Bounds as in test_gpu_paged_attention.py: with A = sum_j p_j |v_j| of the exact
 weights p, 2^-13 A on a bf16 cache and 2^-10.5 A on a MixFP4 one, then the rounding to
-bf16; the log-sum-exp within 2^-17 (1 + top).  top is the largest |score| plus
+bf16.  A MixFP4 cache's weights are f16 numbers of 2^7 times 2^(s - m), m at most the
+largest score: those below 2^-14 are off by up to 2^-25, half of f16's smallest
+step, and their sum is at least 2^7, so that each p_j is off by up to 2^-32 besides:
+2^-32 sum_j |v_j| more, which counts where A is next to nothing (a zero of V under all of
+the weight).  The log-sum-exp within 2^-17 (1 + top).  top is the largest |score| plus
 |bias| of what has a weight of 2^-30 or more: capped scores are within 2^-20 of
 themselves and a bias within 2^-23 of itself, so neither widens these."""
 import math
@@ -45,7 +49,7 @@ def chain(t):
     return [(2 << i) - 1 for i in range(t)]
 
 
-def reference(q, k, v, n, c, bits, scale, window=0, cap=0.0, slopes=None, skip=None):
+def reference(q, k, v, n, c, bits, scale, fp4, window=0, cap=0.0, slopes=None, skip=None):
     """One sequence's rows [t, H, D] and [t, H] in 64 bits, the bound of each element, and the bound of lse.
     bits: of each draft; skip: tokens on pages outside the cache."""
     t, H, D = q.shape
@@ -78,7 +82,9 @@ def reference(q, k, v, n, c, bits, scale, window=0, cap=0.0, slopes=None, skip=N
         x = s + bias
         p = x.softmax(-1)
         out[i] = torch.einsum("hgn,nhd->hgd", p, vv).reshape(H, D)
-        mag[i] = torch.einsum("hgn,nhd->hgd", p, vv.abs()).reshape(H, D)
+        mag[i] = (2.0 ** -10.5 if fp4 else 2.0 ** -13) * torch.einsum("hgn,nhd->hgd", p, vv.abs()).reshape(H, D)
+        if fp4:
+            mag[i] += 2.0 ** -32 * vv.abs().sum(0).repeat_interleave(H // Hkv, 0)
         lse[i] = torch.logsumexp(x, -1).reshape(H)
         top = torch.where(p >= 2.0 ** -30, s.abs() + bias.abs(), 0.0).amax(-1).reshape(H)
         lim[i] = 2.0 ** -17 * (1 + top)
@@ -88,12 +94,12 @@ def reference(q, k, v, n, c, bits, scale, window=0, cap=0.0, slopes=None, skip=N
 def check(out, lse, q, k, v, lengths, counts, bits, scale, fp4, skip=None, **kw):
     at = 0
     for b, n in enumerate(lengths):
-        ref, mag, ls, lim = reference(q[b], k[at:at + n], v[at:at + n], n, counts[b], bits[b], scale,
+        ref, mag, ls, lim = reference(q[b], k[at:at + n], v[at:at + n], n, counts[b], bits[b], scale, fp4,
                                       skip=None if skip is None else skip.get(b), **kw)
         at += n
         none = ls == -math.inf
         assert torch.all(out[b][none] == 0) and torch.all(lse[b][none] == -math.inf), b
-        pa.within(out[b], ref, (2.0 ** -10.5 if fp4 else 2.0 ** -13) * mag)
+        pa.within(out[b], ref, mag)
         some = ~none
         assert torch.all((lse[b].double() - ls).abs()[some] <= lim[some]), (b, float((lse[b] - ls).abs()[some].max()))
 
@@ -224,8 +230,8 @@ def test_large_and_tiny_queries(fp4):
     q = (randn(1, t, 2, 64, seed=9) * size[:, None, None]).to(torch.bfloat16)
     for rows, scale in (([0, 1, 3, 4, 5], 0.125), ([2], 0.125 * 2.0 ** -60)):
         out, lse = o.mixfp4_tree_attention(q, cache, table, ints([n]), scale=scale, return_lse=True)
-        ref, mag, ls, lim = reference(q[0], k, v, n, t, chain(t), scale)
-        pa.within(out[0][rows], ref[rows], (2.0 ** -10.5 if fp4 else 2.0 ** -13) * mag[rows])
+        ref, mag, ls, lim = reference(q[0], k, v, n, t, chain(t), scale, fp4)
+        pa.within(out[0][rows], ref[rows], mag[rows])
         assert torch.all((lse[0].double() - ls).abs()[rows] <= lim[rows])
 
 
@@ -286,8 +292,8 @@ def test_infinite_and_nan_scores(n, t, Hq):
     out, lse = o.mixfp4_tree_attention(q, cache, table, ints([n]), return_lse=True)
     assert torch.isnan(out[0, 0, 0]).all() and lse[0, 0, 0] == math.inf
     assert torch.isnan(out[0, 2, G]).all() and torch.isnan(lse[0, 2, G])
-    ref, mag, ls, lim = reference(q[0], k, v, n, t, chain(t), D ** -0.5)
-    pa.within(out[0, 1, 0], ref[1, 0], 2.0 ** -13 * mag[1, 0])
+    ref, mag, ls, lim = reference(q[0], k, v, n, t, chain(t), D ** -0.5, False)
+    pa.within(out[0, 1, 0], ref[1, 0], mag[1, 0])
     assert (lse[0, 1, 0] - ls[1, 0]).abs() <= 2.0 ** -17 * 20
     # infinite values: seen by every row, dimensions 0 (+inf), 1 (-inf) and 2 (both signs)
     cache, table, k, v = pa.build(False, [n], Hkv, D, 16, seed=5)
@@ -326,8 +332,8 @@ def test_lengths_and_counts_outside_their_ranges():
                                        return_lse=True)
     assert torch.all(out[0] == 0) and torch.all(lse[0] == -math.inf)
     # 34 tokens with 4 drafts of which the table holds two; then 2 tokens, both drafts
-    ref, mag, ls, lim = reference(q[1], k[32:64], v[32:64], 34, t, chain(t), 0.125)
-    pa.within(out[1], ref, 2.0 ** -13 * mag)
+    ref, mag, ls, lim = reference(q[1], k[32:64], v[32:64], 34, t, chain(t), 0.125, False)
+    pa.within(out[1], ref, mag)
     assert torch.all((lse[1].double() - ls).abs() <= lim)
     check(out[2:], lse[2:], q[2:], k[64:], v[64:], [2], [2], [chain(t)], 0.125, False)
     out = o.mixfp4_tree_attention(q, cache, table, ints([32, 32, 2]), counts=ints([-1, 0, 0]))

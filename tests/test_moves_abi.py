@@ -16,13 +16,13 @@ from test_serving_abi import FAKE, I, P, cache, fp4, lib, ops  # noqa: E402,F401
 
 def tree(lib, c, **kw):
     f = dict(q=FAKE, qs=768, qt=256, qh=64, B=2, t=3, H=4, table=FAKE, ts=8, pages=8, lengths=FAKE, mask=FAKE, ms=3,
-             counts=FAKE, window=0, cap=0.0, slopes=FAKE, out=FAKE, lse=FAKE, ws=FAKE, bytes=1 << 40)
+             counts=FAKE, window=0, cap=0.0, slopes=FAKE, out=FAKE, lse=FAKE, ws=FAKE, bytes=1 << 40, status=FAKE)
     f.update(kw)
     return lib.mixfp4_tree_attention(P(f["q"]), I(f["qs"]), I(f["qt"]), I(f["qh"]), I(f["B"]), I(f["t"]), I(f["H"]),
                                      ctypes.byref(c) if c else None, P(f["table"]), I(f["ts"]), I(f["pages"]),
                                      P(f["lengths"]), P(f["mask"]), I(f["ms"]), P(f["counts"]), ctypes.c_float(0.1),
                                      I(f["window"]), ctypes.c_float(f["cap"]), P(f["slopes"]), P(f["out"]),
-                                     P(f["lse"]), P(f["ws"]), I(f["bytes"]), None)
+                                     P(f["lse"]), P(f["ws"]), I(f["bytes"]), P(f["status"]), None)
 
 
 @pytest.mark.parametrize("of", [cache, fp4])
@@ -41,7 +41,7 @@ def test_tree_attention_validation(ops, lib, of):  # noqa: F811
         assert tree(lib, c, **kw) == -1, kw
     for kw in (dict(q=FAKE + 8), dict(qs=772), dict(qt=260), dict(qh=68), dict(out=FAKE + 8), dict(lse=FAKE + 2),
                dict(ws=FAKE + 128), dict(mask=FAKE + 4), dict(counts=FAKE + 2), dict(slopes=FAKE + 1),
-               dict(table=FAKE + 2), dict(lengths=FAKE + 1)):
+               dict(table=FAKE + 2), dict(lengths=FAKE + 1), dict(status=FAKE + 1)):
         assert tree(lib, c, **kw) == -3, kw
 
 
@@ -128,9 +128,9 @@ def test_binding_refuses_before_the_library(ops):  # noqa: F811
     at = ctypes.addressof(c)
     t = torch.zeros(2, 3, 4, 64, dtype=torch.bfloat16)
     i = torch.zeros(2, dtype=torch.int32)
-    for call in (lambda: native.tree_attention(at, 0, t, i, i, None, None, None, 0, 0.0, None, None, None, False, None, 0),
+    for call in (lambda: native.tree_attention(at, 0, t, i, i, None, None, None, 0, 0.0, None, None, None, False, None, None, 0),
                  lambda: native.tree_attention(at, 0, None, i, i, None, None, None, 0, 0.0, None, None, None, False,
-                                               None, 0),
+                                               None, None, 0),
                  lambda: native.kv_accept(at, 0, i[:, None], i, i[:, None], i, None, 0),
                  lambda: native.kv_accept(at, 0, i[:, None], 3, i[:, None], i, None, 0),
                  lambda: native.kv_fork(at, 0, i[:, None], i, i, i, None, None, 0),
