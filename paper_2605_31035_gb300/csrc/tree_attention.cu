@@ -100,7 +100,7 @@ struct Cfg {
   static constexpr int kRaw = kFp4 ? kProducers * kRawDepth * kRawSlot : 0;
   static constexpr int kFit = (227 * 1024 - 2560 - kQ - kRaw) / kSlot;
   static constexpr int kSlots = kFit < 8 ? kFit : 8;
-  static constexpr int kLag = kFp4 ? kRawDepth - 1 : kSlots - 2;  // copies asked for behind the one handed over
+  static constexpr int kLag = kRawDepth - 1;               // raw copies behind the one being decoded
   static constexpr int kSmem = kQ + kSlots * kSlot + kRaw + 2560;
   static constexpr uint32_t kScoreCols = 2 * kTokens;      // of tensor memory, O behind them
 };
@@ -138,7 +138,8 @@ __device__ __forceinline__ void cp_wait_at_most(int n) {
     case 2: return cp_wait<2>();
     case 3: return cp_wait<3>();
     case 4: return cp_wait<4>();
-    default: return cp_wait<5>();
+    case 5: return cp_wait<5>();
+    default: return cp_wait<6>();
   }
 }
 __device__ __forceinline__ uint32_t lds8(uint32_t a) {
@@ -329,24 +330,31 @@ __device__ __forceinline__ int depth_of(uint64_t bits, int k) { return __popcll(
 
 // Copy n of a MixFP4 tile's rows (this warp's) decoded to f16 at the operand's swizzled places: a lane to 16 elements,
 // twice their values under the block scale alone.
-template <typename C, typename F>
-__device__ __forceinline__ void decode_tile(uint32_t ring, uint32_t raw0, uint32_t n, int pw, int lane, int D, F free) {
+template <typename C>
+__device__ __forceinline__ void decode_tile(uint32_t ring, uint32_t raw0, uint32_t n, int pw, int lane, int D) {
   constexpr int kPieces = (C::kRawRow - 16) / 8, kAtOnce = 32 / kPieces;  // of a row; rows
   const uint32_t slot = n % C::kSlots, raw = raw0 + (n % C::kRawDepth) * C::kRawSlot;
-  free(slot, ((n / C::kSlots) & 1) ^ 1);
   const int piece = lane % kPieces, r0 = lane / kPieces;
   if (piece * 16 >= D) return;
   const uint32_t to = ring + slot * C::kSlot + (piece >> 2) * C::kBlock;
+  constexpr int kSteps = C::kRows / kAtOnce;
+  uint2 c[kSteps];
+  uint32_t scale[kSteps];
 #pragma unroll
-  for (int j = 0; j < C::kRows / kAtOnce; ++j) {
-    const int r = r0 + j * kAtOnce, row = pw * C::kRows + r;
-    const uint2 c = lds64(raw + r * C::kRawRow + piece * 8);
-    const uint32_t sc = lds8(raw + r * C::kRawRow + kPieces * 8 + piece), e1m2 = sc >> 7;
+  for (int j = 0; j < kSteps; ++j) {  // all asked for before the first is used
+    const uint32_t from = raw + (r0 + j * kAtOnce) * C::kRawRow;
+    c[j] = lds64(from + piece * 8);
+    scale[j] = lds8(from + kPieces * 8 + piece);
+  }
+#pragma unroll
+  for (int j = 0; j < kSteps; ++j) {
+    const int row = pw * C::kRows + r0 + j * kAtOnce;
+    const uint32_t sc = scale[j], e1m2 = sc >> 7;
     const uint32_t s2 = cvt_f16x2_from_e4m3x2((uint16_t)((sc & 0x7Fu) * 0x0101u));
     const uint32_t lo = kLutE2M1Lo + e1m2 * (kLutE1M2Lo - kLutE2M1Lo), hi = kLutE2M1Hi + e1m2 * (kLutE1M2Hi - kLutE2M1Hi);
     uint32_t v[2][4];
-    decode8(c.x, lo, hi, s2, v[0]);
-    decode8(c.y, lo, hi, s2, v[1]);
+    decode8(c[j].x, lo, hi, s2, v[0]);
+    decode8(c[j].y, lo, hi, s2, v[1]);
     const int u0 = (piece & 3) * 2;
     sts128(to + row * 128 + ((u0 ^ (row & 7)) << 4), v[0][0], v[0][1], v[0][2], v[0][3]);
     sts128(to + row * 128 + (((u0 + 1) ^ (row & 7)) << 4), v[1][0], v[1][1], v[1][2], v[1][3]);
@@ -371,7 +379,7 @@ __global__ void __launch_bounds__(Cfg<DT, NM, kFp4>::kThreads, 1) tree_attention
     tmem_relinquish();
   } else if (tid == 0) {
     for (int i = 0; i < C::kSlots; ++i) {
-      mbar_init(smem_u32(&sh.full[i]), C::kProducers);
+      mbar_init(smem_u32(&sh.full[i]), kFp4 ? C::kProducers : C::kProducers * 32);
       mbar_init(smem_u32(&sh.empty[i]), 1);
     }
     for (int i = 0; i < 2; ++i) {
@@ -859,6 +867,7 @@ __global__ void __launch_bounds__(Cfg<DT, NM, kFp4>::kThreads, 1) tree_attention
         const uint32_t q = 2 * tile, slot = q % C::kSlots;
         if (m == 0) {
           wait(sh.full[slot], (q / C::kSlots) & 1, 64u);
+          if (!kFp4) fence_proxy_async_smem();  // of what cp.async has written
           tc_fence_after();
         }
         const int buf = NM == 2 ? m : (int)(tile & 1);
@@ -880,7 +889,10 @@ __global__ void __launch_bounds__(Cfg<DT, NM, kFp4>::kThreads, 1) tree_attention
           const uint32_t q = 2 * g + 1, slot = q % C::kSlots, v = ring + slot * C::kSlot;
           for (int m = 0; m < NM; ++m) {
             const int buf = NM == 2 ? m : (int)(g & 1);
-            if (m == 0) wait(sh.full[slot], (q / C::kSlots) & 1, 256u);
+            if (m == 0) {
+              wait(sh.full[slot], (q / C::kSlots) & 1, 256u);
+              if (!kFp4) fence_proxy_async_smem();
+            }
             wait(sh.p_full[buf], NM == 2 ? g & 1 : (g >> 1) & 1, 512u);
             tc_fence_after();
             if (!*reinterpret_cast<volatile int*>(&sh.skip[buf])) {
@@ -906,10 +918,18 @@ __global__ void __launch_bounds__(Cfg<DT, NM, kFp4>::kThreads, 1) tree_attention
     const int pw = warp - C::kSoftmax - 1;
     constexpr int kRows = C::kRows;
     uint32_t g = 0, q = 0, sent = 0;  // tiles, copies asked for, copies handed over
-    auto arrive = [&](uint32_t n) {   // copy n has landed, for the tensor cores too
+    [[maybe_unused]] const uint32_t raw0 = ring + C::kSlots * C::kSlot + pw * C::kRawDepth * C::kRawSlot;
+    // The oldest copy not decoded yet, with `later` behind it: once it has landed, for the tensor cores.
+    [[maybe_unused]] auto hand_over = [&](int later) {
+      cp_wait_at_most(later);
+      __syncwarp();
+      wait(sh.empty[sent % C::kSlots], ((sent / C::kSlots) & 1) ^ 1, 1024u);
+      __syncwarp();
+      decode_tile<C>(ring, raw0, sent, pw, lane, D);
       fence_proxy_async_smem();
       __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&sh.full[n % C::kSlots]));
+      if (lane == 0) mbar_arrive(smem_u32(&sh.full[sent % C::kSlots]));
+      ++sent;
     };
     while (walk.next(p, mate, w)) {
       const int32_t* table = p.table + (int64_t)w.b * p.table_stride;
@@ -943,45 +963,41 @@ __global__ void __launch_bounds__(Cfg<DT, NM, kFp4>::kThreads, 1) tree_attention
           else
             *to = (uint8_t)there;
         }
+        // Where this lane's pieces of rows begin: all asked of the other lanes at once, for keys and values alike.
+        constexpr int kPieces = kFp4 ? DT / 16 : DT / 8, kAtOnce = 32 / kPieces, kSteps = kRows / kAtOnce;
+        constexpr int kBytes = kFp4 ? 8 : 16;
+        const int piece = lane % kPieces, r0 = lane / kPieces;
+        int64_t from[kSteps];
+        uint32_t take = 0;
+#pragma unroll
+        for (int j = 0; j < kSteps; ++j) from[j] = __shfl_sync(kAll, at, r0 + j * kAtOnce) + piece * kBytes;
+#pragma unroll
+        for (int j = 0; j < kSteps; ++j) {
+          const bool t = piece * kBytes * (kFp4 ? 2 : 1) < D * (kFp4 ? 1 : 2) && ((there >> (r0 + j * kAtOnce)) & 1u);
+          take |= (uint32_t)t << j;
+          if (!t) from[j] = 0;
+        }
 #pragma unroll 1
         for (int kv = 0; kv < 2; ++kv, ++q) {
+          const uint8_t* base = static_cast<const uint8_t*>(kv ? p.c.v : p.c.k);
           if constexpr (!kFp4) {
             const uint32_t slot = q % C::kSlots;
             wait(sh.empty[slot], ((q / C::kSlots) & 1) ^ 1, 1024u);
             __syncwarp();
-            const uint8_t* base = static_cast<const uint8_t*>(kv ? p.c.v : p.c.k);
-            constexpr int kPieces = DT / 8, kAtOnce = 32 / kPieces;  // of a row; rows
-            const int piece = lane % kPieces, r0 = lane / kPieces;
-            const bool in_row = piece * 8 < D;
-            const uint32_t dst = ring + slot * C::kSlot + (piece >> 3) * C::kBlock;
+            const uint32_t dst = ring + slot * C::kSlot + (piece >> 3) * C::kBlock + pw * kRows * 128;
 #pragma unroll
-            for (int j = 0; j < kRows / kAtOnce; ++j) {
-              const int r = r0 + j * kAtOnce, row = pw * kRows + r;
-              const int64_t from = __shfl_sync(kAll, at, r);
-              const bool take = in_row && ((there >> r) & 1u);
-              cp_async<16>(dst + row * 128 + (((piece & 7) ^ (row & 7)) << 4), base + (take ? from + piece * 16 : 0), take);
+            for (int j = 0; j < kSteps; ++j) {
+              const int r = r0 + j * kAtOnce;
+              cp_async<16>(dst + r * 128 + (((piece & 7) ^ (r & 7)) << 4), base + from[j], (take >> j) & 1u);
             }
-            cp_commit();
-            if (q - sent >= C::kLag) {
-              cp_wait<C::kLag>();
-              arrive(sent++);
-            }
+            cp_async_arrive(smem_u32(&sh.full[slot]));  // when this lane's have landed
           } else {
             // ---- the codes as they lie, into this warp's own part
-            const uint32_t raw0 = ring + C::kSlots * C::kSlot + pw * C::kRawDepth * C::kRawSlot;
-            uint32_t raw = raw0 + (q % C::kRawDepth) * C::kRawSlot;
-            const uint8_t* base = static_cast<const uint8_t*>(kv ? p.c.v : p.c.k);
+            const uint32_t raw = raw0 + (q % C::kRawDepth) * C::kRawSlot;
             const uint8_t* scales = kv ? p.c.v_scales : p.c.k_scales;
-            constexpr int kPieces = DT / 16, kAtOnce = 32 / kPieces;
-            const int piece = lane % kPieces, r0 = lane / kPieces;
-            const bool in_row = piece * 16 < D;
 #pragma unroll
-            for (int j = 0; j < kRows / kAtOnce; ++j) {
-              const int r = r0 + j * kAtOnce;
-              const int64_t from = __shfl_sync(kAll, at, r);
-              const bool take = in_row && ((there >> r) & 1u);
-              cp_async<8>(raw + r * C::kRawRow + piece * 8, base + (take ? from + piece * 8 : 0), take);
-            }
+            for (int j = 0; j < kSteps; ++j)
+              cp_async<8>(raw + (r0 + j * kAtOnce) * C::kRawRow + piece * 8, base + from[j], (take >> j) & 1u);
             if (lane < kRows) {
               const uint32_t sd = raw + lane * C::kRawRow + DT / 2;
               const uint8_t* src = scales + (ok ? sat : 0);
@@ -996,30 +1012,13 @@ __global__ void __launch_bounds__(Cfg<DT, NM, kFp4>::kThreads, 1) tree_attention
               }
             }
             cp_commit();
-            if (q - sent >= C::kLag) {
-              cp_wait<C::kLag>();
-              __syncwarp();
-              decode_tile<C>(ring, raw0, sent, pw, lane, D, [&](uint32_t slot, uint32_t parity) {
-                wait(sh.empty[slot], parity, 1024u);
-                __syncwarp();
-              });
-              arrive(sent++);
-            }
+            if (q - sent >= C::kLag) hand_over(C::kLag);
           }
         }
       }
     }
-    while (sent < q) {
-      cp_wait_at_most((int)(q - sent - 1));
-      __syncwarp();
-      if constexpr (kFp4)
-        decode_tile<C>(ring, ring + C::kSlots * C::kSlot + pw * C::kRawDepth * C::kRawSlot, sent, pw, lane, D,
-                       [&](uint32_t slot, uint32_t parity) {
-                         wait(sh.empty[slot], parity, 1024u);
-                         __syncwarp();
-                       });
-      arrive(sent++);
-    }
+    if constexpr (kFp4)
+      while (sent < q) hand_over((int)(q - sent - 1));
     cp_async_wait_all();
   }
   __syncwarp();
