@@ -55,6 +55,8 @@ constexpr float kSlack = 8.0f, kFp4Exp = 7.0f;
 constexpr float kNoScore = -3e38f;  // m where no token has been seen: no difference to a score or to itself is NaN
 constexpr float kMostScore = 3.402823466e38f;  // m of a score of +inf, whose weight is then +inf instead of NaN
 constexpr unsigned kAll = 0xFFFFFFFFu;
+constexpr int kMisc = 3072;  // bytes of shared memory beside the tiles
+constexpr int kThere = 16;   // tiles whose tokens are known at a time
 
 struct TreeArgs {
   const uint16_t* q;
@@ -78,45 +80,55 @@ struct TreeArgs {
   uint16_t* out;
   float* lse;
   int4* split;   // [grid]: the row that a CTA begins and others end: (sequence, row, first share, last); x < 0: none
-  float2* stat;  // [2 grid][rows] (m, l) of parts
-  float4* part;  // [2 grid][row tiles][dimensions / 4][128]: O of parts, and what a row in work has set aside
+  float2* stat;  // [2 grid][groups][128] (m, l) of parts
+  float4* part;  // [2 grid][groups][dimensions / 4][128]: O of parts, and what a row in work has set aside
   uint32_t* status;
+  int box;  // rows of a bf16 page that one TMA copy brings; 0: cp.async does
 };
 
-template <int DT, int NM, bool kFp4>
+template <int DT, int MT, bool kFp4>
 struct Cfg {
   static constexpr int kTokens = DT == 256 ? 64 : 128;     // of a tile
   static constexpr int kCw = kTokens / 4;                  // and of its quarter, a thread's step
   static constexpr int kBlock = kTokens * 128;             // 64 dimensions of a tile
   static constexpr int kSlot = kBlock * (DT / 64);
-  static constexpr int kQ = NM * 128 * DT * 2;
-  static constexpr int kSoftmax = 4 * NM;                  // warps
-  static constexpr int kProducers = kFp4 ? 8 : 4;
-  static constexpr int kThreads = (kSoftmax + 1 + kProducers) * 32;
+  // Groups of four softmax warps: one to each of two tiles of rows; or two that take turns at the tiles of tokens, each with
+  // an O of its own, which tensor memory holds beside both S up to 128 dimensions.
+  static constexpr int kGroups = DT == 256 ? 1 : 2;
+  static constexpr bool kTurns = MT == 1 && kGroups == 2;
+  static constexpr int kQ = MT * 128 * DT * 2 > kGroups * 16384 ? MT * 128 * DT * 2 : kGroups * 16384;
+  static constexpr int kSoftmax = 4 * kGroups;             // warps
+  static constexpr int kProducers = kFp4 ? 8 : 2;          // of a bf16 cache where TMA cannot bring its rows
+  static constexpr int kThreads = (kSoftmax + 4 + (kFp4 ? kProducers : 0)) * 32;  // the four: products, TMA or helpers
+  // Registers of a thread at launch, then of softmax and of the other threads (together no more than at launch).
+  static constexpr int kRegs = 65536 / kThreads / 8 * 8;
+  static constexpr int kOtherRegs = kFp4 ? 72 : 168;
+  static constexpr int kLeft = (kRegs * kThreads - kOtherRegs * (kThreads - kSoftmax * 32)) / (kSoftmax * 32) / 8 * 8;
+  static constexpr int kSoftRegs = kLeft < 232 ? kLeft : 232;
   static constexpr int kRows = kTokens / kProducers;       // of a tile, to a producer warp
-  static constexpr int kRawRow = DT / 2 + 16;              // a MixFP4 row as it lies: codes, scale bytes
-  static constexpr int kRawSlot = kRows * kRawRow;
-  static constexpr int kRawDepth = 6;
-  static constexpr int kRaw = kFp4 ? kProducers * kRawDepth * kRawSlot : 0;
-  static constexpr int kFit = (227 * 1024 - 2560 - kQ - kRaw) / kSlot;
+  static constexpr int kRawSlot = kRows * (DT / 2 + 16);   // MixFP4 rows as they lie: codes, then scale bytes
+  static constexpr int kRawDepth = kFp4 ? 5 : 0;
+  static constexpr int kRaw = kProducers * kRawDepth * kRawSlot;
+  static constexpr int kAddresses = kFp4 ? 4 : 0;          // tiles whose rows' places are known
+  static constexpr int kPlaces = kAddresses * kTokens * 16;
+  static constexpr int kFit = (227 * 1024 - kMisc - kQ - kRaw - kPlaces) / kSlot;
   static constexpr int kSlots = kFit < 8 ? kFit : 8;
-  static constexpr int kLag = kRawDepth - 1;               // raw copies behind the one being decoded
-  static constexpr int kSmem = kQ + kSlots * kSlot + kRaw + 2560;
+  static constexpr int kSmem = kQ + kSlots * kSlot + kRaw + kPlaces + kMisc;
   static constexpr uint32_t kScoreCols = 2 * kTokens;      // of tensor memory, O behind them
 };
 
 struct Shared {
-  uint64_t full[8], empty[8], s_full[2], p_full[2], o_done[2], q_full, end;
+  uint64_t full[8], empty[8], placed[4], used[4], s_full[2], p_full[2], o_done[2], q_full, end;
   uint32_t tmem;
   int abort;
   int skip[2];
   int edge_b;
-  int64_t before, edge[2], scan[18];
-  uint32_t there[8][4];  // of a tile, which of its tokens there are
-  int depth[2][kMostDrafts];
-  float2 ml[128];
+  int64_t before, edge[2], scan[28];
+  uint32_t there[kThere][4];  // of a tile, which of its tokens there are
+  uint8_t depth[2][kMostDrafts];
+  float2 ml[256];
 };
-static_assert(sizeof(Shared) <= 2560);
+static_assert(sizeof(Shared) <= kMisc);
 
 template <int kBytes>
 __device__ __forceinline__ void cp_async(uint32_t dst, const void* src, bool take) {
@@ -195,6 +207,24 @@ __device__ __forceinline__ float tanh_of(float x) {
   const float r = fminf(fmaxf(z * a * rcp(b), -1.0f), 1.0f);
   return x != x ? x : r;
 }
+// As mma_f16_tmem_a, lanes of D whose bit is set in the four words left as they are.
+__device__ __forceinline__ void mma_f16_tmem_a_lanes(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc,
+                                                     uint32_t accumulate, uint4 off) {
+  asm volatile(
+      "{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n"
+      " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, {%5, %6, %7, %8}, p;\n}" ::"r"(d_tmem),
+      "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(off.x), "r"(off.y), "r"(off.z), "r"(off.w)
+      : "memory");
+}
+// A box of a [page][head][token][element] tensor.
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* m, int x, int token, int head, int page,
+                                            uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+      " [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst),
+      "l"(reinterpret_cast<uint64_t>(m)), "r"(x), "r"(token), "r"(head), "r"(page), "r"(bar)
+      : "memory");
+}
 // D[tmem] (+)= A[smem] . B[smem]^T, one CTA, kind::f16.
 __device__ __forceinline__ void mma_f16(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc,
                                         uint32_t accumulate) {
@@ -228,6 +258,12 @@ __device__ __forceinline__ void tmem_load(uint32_t taddr, uint32_t* v) {
   else
     tmem_ld_32x32b_x16(taddr, v);
 }
+// Keeps the use of loaded columns behind the wait for them.
+template <int kCols>
+__device__ __forceinline__ void tmem_fence(uint32_t* v) {
+  reg_fence16(v);
+  if constexpr (kCols == 32) reg_fence16(v + 16);
+}
 template <int kCols>
 __device__ __forceinline__ void tmem_loaded(uint32_t* v) {
   if constexpr (kCols == 32)
@@ -251,9 +287,10 @@ __device__ __forceinline__ void tmem_store(uint32_t taddr, const uint32_t* v) {
 // What of a sequence is looked at.
 struct Span {
   int n, c, first;  // tokens, drafts, certain tokens
-  int from, end;    // tokens [from, end) may be seen; from is rounded down to 16
+  int from, end;    // tokens [from, end) may be seen; from is a tile's first
   int low;          // tokens below are not
 };
+template <int kTokens>
 __device__ __forceinline__ Span span_of(const TreeArgs& p, int b) {
   Span s;
   s.n = max(p.lengths[b], 0);
@@ -262,7 +299,7 @@ __device__ __forceinline__ Span span_of(const TreeArgs& p, int b) {
   s.first = s.n - s.c;
   s.end = (int)min((int64_t)s.n, p.max_tokens);
   s.low = p.window > 0 ? (int)max((int64_t)0, s.first + 1 - p.window) : 0;  // of the drafts, those that see none
-  s.from = s.low & ~15;
+  s.from = s.low & ~(kTokens - 1);
   return s;
 }
 // Units of work of a row of the sequence: kRowCost for its beginning, then one to a tile.
@@ -286,7 +323,7 @@ struct Walk {
   __device__ __forceinline__ bool next(const TreeArgs& p, int mate, Part& w) {
     const int rows = p.c.heads / p.together * p.chunks;
     while (pos < end && b < p.B) {
-      w.s = span_of(p, b);
+      w.s = span_of<kTokens>(p, b);
       const int u = units_of<kTokens>(w.s);
       if (u == 0 || pos >= base + (int64_t)u * rows) {
         base += (int64_t)u * rows;
@@ -328,27 +365,32 @@ __device__ __forceinline__ uint64_t bits_of(const TreeArgs& p, int b, int k, int
 }
 __device__ __forceinline__ int depth_of(uint64_t bits, int k) { return __popcll(bits & ~(1ull << k)); }
 
-// Copy n of a MixFP4 tile's rows (this warp's) decoded to f16 at the operand's swizzled places: a lane to 16 elements,
-// twice their values under the block scale alone.
-template <typename C>
-__device__ __forceinline__ void decode_tile(uint32_t ring, uint32_t raw0, uint32_t n, int pw, int lane, int D) {
-  constexpr int kPieces = (C::kRawRow - 16) / 8, kAtOnce = 32 / kPieces;  // of a row; rows
-  const uint32_t slot = n % C::kSlots, raw = raw0 + (n % C::kRawDepth) * C::kRawSlot;
-  const int piece = lane % kPieces, r0 = lane / kPieces;
-  if (piece * 16 >= D) return;
-  const uint32_t to = ring + slot * C::kSlot + (piece >> 2) * C::kBlock;
-  constexpr int kSteps = C::kRows / kAtOnce;
+// Which 16 elements of which row a lane takes of a MixFP4 tile: eight neighbouring lanes four pieces of two rows, whose
+// places in the operand are then in different banks.
+template <int DT>
+struct Lanes {
+  static constexpr int kPieces = DT / 16, kRowsAtOnce = 32 / kPieces;
+  static constexpr int kShift = DT == 64 ? 3 : (DT == 128 ? 4 : 5);
+  static __device__ __forceinline__ int piece(int lane) { return (lane & 3) | ((lane >> 3 & (kPieces / 4 - 1)) << 2); }
+  static __device__ __forceinline__ int row(int lane) { return (lane >> 2 & 1) | (lane >> kShift << 1); }
+};
+
+// A warp's rows of a MixFP4 tile decoded to f16 at the operand's swizzled places: twice their values under the block
+// scale alone.
+template <typename C, typename L, int kSteps>
+__device__ __forceinline__ void decode_rows(uint32_t to, uint32_t raw, int piece, int r0, int before) {
   uint2 c[kSteps];
   uint32_t scale[kSteps];
 #pragma unroll
   for (int j = 0; j < kSteps; ++j) {  // all asked for before the first is used
-    const uint32_t from = raw + (r0 + j * kAtOnce) * C::kRawRow;
-    c[j] = lds64(from + piece * 8);
-    scale[j] = lds8(from + kPieces * 8 + piece);
+    const int r = r0 + j * L::kRowsAtOnce;
+    c[j] = lds64(raw + r * (L::kPieces * 8) + piece * 8);
+    scale[j] = lds8(raw + C::kRows * (L::kPieces * 8) + r * 16 + piece);
   }
+  to += (piece >> 2) * C::kBlock;
 #pragma unroll
   for (int j = 0; j < kSteps; ++j) {
-    const int row = pw * C::kRows + r0 + j * kAtOnce;
+    const int row = r0 + j * L::kRowsAtOnce;
     const uint32_t sc = scale[j], e1m2 = sc >> 7;
     const uint32_t s2 = cvt_f16x2_from_e4m3x2((uint16_t)((sc & 0x7Fu) * 0x0101u));
     const uint32_t lo = kLutE2M1Lo + e1m2 * (kLutE1M2Lo - kLutE2M1Lo), hi = kLutE2M1Hi + e1m2 * (kLutE1M2Hi - kLutE2M1Hi);
@@ -356,18 +398,21 @@ __device__ __forceinline__ void decode_tile(uint32_t ring, uint32_t raw0, uint32
     decode8(c[j].x, lo, hi, s2, v[0]);
     decode8(c[j].y, lo, hi, s2, v[1]);
     const int u0 = (piece & 3) * 2;
-    sts128(to + row * 128 + ((u0 ^ (row & 7)) << 4), v[0][0], v[0][1], v[0][2], v[0][3]);
-    sts128(to + row * 128 + (((u0 + 1) ^ (row & 7)) << 4), v[1][0], v[1][1], v[1][2], v[1][3]);
+    const int x = (row + before) & 7;  // `before` rows of the tile lie ahead of the warp's
+    sts128(to + row * 128 + ((u0 ^ x) << 4), v[0][0], v[0][1], v[0][2], v[0][3]);
+    sts128(to + row * 128 + (((u0 + 1) ^ x) << 4), v[1][0], v[1][1], v[1][2], v[1][3]);
   }
 }
 
-template <int DT, int NM, bool kFp4>
-__global__ void __launch_bounds__(Cfg<DT, NM, kFp4>::kThreads, 1) tree_attention_kernel(const TreeArgs p) {
-  using C = Cfg<DT, NM, kFp4>;
+template <int DT, int MT, bool kFp4>
+__global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, 1) tree_attention_kernel(const TreeArgs p, const __grid_constant__ CUtensorMap tm_k,
+                      const __grid_constant__ CUtensorMap tm_v) {
+  using C = Cfg<DT, MT, kFp4>;
   constexpr int TN = C::kTokens, CW = C::kCw;
   extern __shared__ __align__(1024) uint8_t smem[];
-  Shared& sh = *reinterpret_cast<Shared*>(smem + C::kQ + C::kSlots * C::kSlot + C::kRaw);
+  Shared& sh = *reinterpret_cast<Shared*>(smem + C::kQ + C::kSlots * C::kSlot + C::kRaw + C::kPlaces);
   const uint32_t q_smem = smem_u32(smem), ring = q_smem + C::kQ;
+  [[maybe_unused]] const uint32_t places = ring + C::kSlots * C::kSlot + C::kRaw;  // [kAddresses][tokens] (row, scales)
   volatile int* abort_flag = &sh.abort;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int share = (int)blockIdx.x / p.together, mate = (int)blockIdx.x % p.together;
@@ -379,8 +424,12 @@ __global__ void __launch_bounds__(Cfg<DT, NM, kFp4>::kThreads, 1) tree_attention
     tmem_relinquish();
   } else if (tid == 0) {
     for (int i = 0; i < C::kSlots; ++i) {
-      mbar_init(smem_u32(&sh.full[i]), kFp4 ? C::kProducers : C::kProducers * 32);
+      mbar_init(smem_u32(&sh.full[i]), kFp4 ? C::kProducers : (p.box ? 1 : C::kProducers * 32));
       mbar_init(smem_u32(&sh.empty[i]), 1);
+    }
+    for (int i = 0; i < C::kAddresses; ++i) {
+      mbar_init(smem_u32(&sh.placed[i]), 1);
+      mbar_init(smem_u32(&sh.used[i]), C::kProducers);
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(smem_u32(&sh.s_full[i]), 1);
@@ -401,7 +450,7 @@ __global__ void __launch_bounds__(Cfg<DT, NM, kFp4>::kThreads, 1) tree_attention
   {
     const int strip = (p.B + C::kThreads - 1) / C::kThreads, lo = min(p.B, tid * strip), hi = min(p.B, lo + strip);
     int64_t mine = 0;
-    for (int i = lo; i < hi; ++i) mine += units_of<TN>(span_of(p, i));
+    for (int i = lo; i < hi; ++i) mine += units_of<TN>(span_of<TN>(p, i));
     int64_t before = mine;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
@@ -420,7 +469,7 @@ __global__ void __launch_bounds__(Cfg<DT, NM, kFp4>::kThreads, 1) tree_attention
     before -= mine;
     const int64_t all = total * rows, shares = min(all, (int64_t)p.shares);
     for (int64_t i = blockIdx.x; i < p.B; i += gridDim.x) {  // sequences that see nothing
-      if (units_of<TN>(span_of(p, (int)i)) > 0) continue;
+      if (units_of<TN>(span_of<TN>(p, (int)i)) > 0) continue;
       const int64_t heads = (int64_t)p.t * p.q_heads, words = heads * D / 2;
       for (int64_t k = tid; k < words; k += C::kThreads) reinterpret_cast<uint32_t*>(p.out)[i * words + k] = 0u;
       if (p.lse)
@@ -435,10 +484,10 @@ __global__ void __launch_bounds__(Cfg<DT, NM, kFp4>::kThreads, 1) tree_attention
         if (edge >= before * rows && edge < (before + mine) * rows) {
           int i = lo;
           int64_t at = before;
-          int u = units_of<TN>(span_of(p, i));
+          int u = units_of<TN>(span_of<TN>(p, i));
           while (i < hi - 1 && edge >= (at + u) * rows) {
             at += u;
-            u = units_of<TN>(span_of(p, ++i));
+            u = units_of<TN>(span_of<TN>(p, ++i));
           }
           const int64_t into = u > 0 ? (edge - at * rows) % u : 0;
           sh.edge[k] = into <= kRowCost ? edge - into : edge;
@@ -466,25 +515,26 @@ __global__ void __launch_bounds__(Cfg<DT, NM, kFp4>::kThreads, 1) tree_attention
   Part w;
 
   if (warp < C::kSoftmax) {
+    if constexpr (C::kSoftRegs > C::kRegs) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::kSoftRegs));
     // ================================================= softmax: a row to a thread
     const int m = warp >> 2, qd = warp & 3, tl = tid & 127;
     const uint32_t lanes = tmem + ((uint32_t)qd * 32u << 16);
     const uint32_t o_col = lanes + C::kScoreCols + m * DT;
-    uint32_t g = 0, turn = 0;
+    uint32_t g = 0, turn = 0;  // tiles and parts before this one
     while (walk.next(p, mate, w)) {
-      const int R = min(128 * NM, p.t * p.group - w.chunk * 128 * NM);
-      const int copies = NM == 2 || R > 64 ? 1 : (R > 32 ? 2 : 4), own = 128 / copies, steps = 4 / copies;
-      const int r = m * 128 + tl % own, copy = tl / own, step0 = copy * steps;
-      const int idx = w.chunk * 128 * NM + r, i = idx / p.group, h = w.head * p.group + idx - i * p.group;
+      const int R = min(128 * MT, p.t * p.group - w.chunk * 128 * MT);
+      const int copies = MT == 2 || R > 64 ? 1 : (R > 32 ? 2 : 4), own = 128 / copies, steps = 4 / copies;
+      const int r = (MT == 2 ? m * 128 : 0) + tl % own, copy = tl / own, step0 = copy * steps;
+      const int idx = w.chunk * 128 * MT + r, i = idx / p.group, h = w.head * p.group + idx - i * p.group;
       const bool held = r < R, valid = held && i < w.s.c;  // rows behind the drafts have a result too, of zeros
-      const bool idle = m * 128 + (copies == 1 ? qd * 32 : 0) >= R;
-      int* depth = sh.depth[turn & 1];
-      if (tid < kMostDrafts) depth[tid] = tid < w.s.c ? depth_of(bits_of(p, w.b, tid, w.s.c), tid) : 0;
+      const bool idle = (MT == 2 ? m * 128 : 0) + (copies == 1 ? qd * 32 : 0) >= R;
+      uint8_t* depth = sh.depth[turn & 1];
+      if (tid < kMostDrafts) depth[tid] = (uint8_t)(tid < w.s.c ? depth_of(bits_of(p, w.b, tid, w.s.c), tid) : 0);
       uint64_t sees = valid ? bits_of(p, w.b, i, w.s.c) : 0;
       const int place = w.s.first + (valid ? depth_of(sees, i) : 0);
       const float slope = p.slopes && valid ? p.slopes[h] * -kLog2e : 0.0f;
 
-      // ---- the row's queries, into the swizzled tile
+      // ---- the row's queries, into the swizzled tile (of one tile of rows, each group every other piece)
       float fs = p.scale * (kFp4 ? 0.5f * kts : 1.0f);
       {
         const uint16_t* q = p.q + (int64_t)w.b * p.q_stride + (int64_t)i * p.q_token_stride + (int64_t)h * p.q_head_stride;
@@ -503,8 +553,9 @@ __global__ void __launch_bounds__(Cfg<DT, NM, kFp4>::kThreads, 1) tree_attention
           up = __uint_as_float((uint32_t)(268 - e) << 23);
           fs *= __uint_as_float((uint32_t)(e - 14) << 23);
         }
-        const uint32_t at = q_smem + m * (128 * DT * 2) + tl * 128;
-        for (int u = 0; u < D / 8; ++u) {
+        const uint32_t at = q_smem + (MT == 2 ? m * (128 * DT * 2) : 0) + tl * 128;
+#pragma unroll 4
+        for (int u = C::kTurns ? m : 0; u < D / 8; u += C::kTurns ? 2 : 1) {
           uint4 v = make_uint4(0, 0, 0, 0);
           if (valid) v = *reinterpret_cast<const uint4*>(q + 8 * u);
           if (kFp4) {
@@ -519,7 +570,7 @@ __global__ void __launch_bounds__(Cfg<DT, NM, kFp4>::kThreads, 1) tree_attention
       fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&sh.q_full));
-      bar_sync(1, 128 * NM);  // the depths
+      bar_sync(1, C::kSoftmax * 32);  // the depths
       if (p.window > 0)
         for (int k = 0; k < w.s.c; ++k)
           if (place - w.s.first - depth[k] >= p.window) sees &= ~(1ull << k);
@@ -528,11 +579,17 @@ __global__ void __launch_bounds__(Cfg<DT, NM, kFp4>::kThreads, 1) tree_attention
 
       float mx = kNoScore, l = 0.0f, m_aside = kNoScore;  // mx: the m of the weights
       bool chained = false;
-      float4* aside = p.part + ((2 * (int64_t)blockIdx.x + (w.first ? 1 : 0)) * NM + m) * (DT / 4 * 128) + tl;
-      auto set_aside = [&] {  // O joins what was set aside before, and begins at 0
-        wait(sh.o_done[m], (g - 1) & 1, 1u);
+      uint32_t n = C::kTurns ? (g + 1 - m) >> 1 : g;  // tiles of this group before this one
+      int done = 0;                                   // and of this part
+      const int64_t slot = (2 * (int64_t)blockIdx.x + (w.first ? 1 : 0)) * C::kGroups + m;
+      float4* aside = p.part + slot * (DT / 4 * 128) + tl;
+      auto o_ready = [&](uint32_t bit) {  // O of this group's tile before this one
+        wait(sh.o_done[m], (n - 1) & 1, bit);
         __syncwarp();
         tc_fence_after();
+      };
+      auto set_aside = [&] {  // O joins what was set aside before, and begins at 0
+        o_ready(1u);
         const float f = ex2(m_aside - mx);
 #pragma unroll 1
         for (int d = 0; d < D; d += 16) {
@@ -555,16 +612,17 @@ __global__ void __launch_bounds__(Cfg<DT, NM, kFp4>::kThreads, 1) tree_attention
         m_aside = mx;
       };
 
-      for (int it = 0; it < w.tiles; ++it, ++g) {
-        const int buf = NM == 2 ? m : (int)(g & 1);
+      for (int it = C::kTurns ? (int)((g + m) & 1) : 0; it < w.tiles; it += C::kTurns ? 2 : 1, ++n, ++done) {
+        const uint32_t tile = g + it;
+        const int buf = C::kGroups == 2 ? m : (int)(tile & 1);
         const uint32_t scores = lanes + buf * TN;
-        const bool begins = it % kChain == 0;
-        if (it > 0 && begins) set_aside();
-        wait(sh.s_full[buf], NM == 2 ? g & 1 : (g >> 1) & 1, 2u);
+        const bool begins = done % kChain == 0;
+        if (done > 0 && begins) set_aside();
+        wait(sh.s_full[buf], C::kGroups == 2 ? n & 1 : (tile >> 1) & 1, 2u);
         __syncwarp();
         tc_fence_after();
         const int j0 = w.s.from + (w.tile + w.tiles - 1 - it) * TN;
-        const uint32_t* there = sh.there[g & 7];
+        const uint32_t* there = sh.there[tile % kThere];
         bool whole = there[0] == kAll && there[1] == kAll;
         if (TN == 128) whole = whole && there[2] == kAll && there[3] == kAll;
         const bool edge = p.window > 0 && j0 < w.s.first + w.s.c - p.window;  // some rows' windows begin behind j0
@@ -573,28 +631,34 @@ __global__ void __launch_bounds__(Cfg<DT, NM, kFp4>::kThreads, 1) tree_attention
         const bool general = masked || !plain;
 
         bool slow = false;
-        if (uneven) {  // a NaN or an infinity in V?
-          const uint32_t q = 2 * g + 1, slot = q % C::kSlots;
-          wait(sh.full[slot], (q / C::kSlots) & 1, 4u);
+        const bool clear = !kFp4 && p.box && !whole && (C::kTurns || m == 0);
+        if (uneven || clear) {
+          const uint32_t q = 2 * tile + 1, place_v = q % C::kSlots, at = ring + place_v * C::kSlot + tl * 128;
+          wait(sh.full[place_v], (q / C::kSlots) & 1, 4u);
           __syncwarp();
-          bool bad = false;
-          if (tl < TN) {
-            constexpr uint32_t kExp = kFp4 ? 0x7C00u : 0x7F80u;
-            const uint32_t at = ring + slot * C::kSlot + tl * 128;
+          const bool mine = tl < TN, here = mine && (there[(tl & (TN - 1)) >> 5] >> (tl & 31)) & 1u;
+          if (clear && mine && !here) {  // TMA brings whole boxes, with whatever lies between a page's tokens
 #pragma unroll 4
-            for (int u = 0; u < D / 8; ++u) {
-              const uint4 v = lds128(at + (u >> 3) * C::kBlock + (((u & 7) ^ (tl & 7)) << 4));
-              const uint32_t x[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-              for (int e = 0; e < 4; ++e)
-                bad = bad || (x[e] & kExp) == kExp || (x[e] & (kExp << 16)) == kExp << 16;
-            }
+            for (int u = 0; u < D / 8; ++u) sts128(at + (u >> 3) * C::kBlock + (((u & 7) ^ (tl & 7)) << 4), 0, 0, 0, 0);
+            fence_proxy_async_smem();
           }
-          slow = bar_or(2 + m, 128, bad);
+          if (uneven) {  // a NaN or an infinity in V?
+            bool bad = false;
+            if (here) {
+              constexpr uint32_t kExp = kFp4 ? 0x7C00u : 0x7F80u;
+#pragma unroll 4
+              for (int u = 0; u < D / 8; ++u) {
+                const uint4 v = lds128(at + (u >> 3) * C::kBlock + (((u & 7) ^ (tl & 7)) << 4));
+                const uint32_t x[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                  bad = bad || (x[e] & kExp) == kExp || (x[e] & (kExp << 16)) == kExp << 16;
+              }
+            }
+            slow = bar_or(2 + m, 128, bad);
+          }
         }
         if (!idle) {
-          // ---- the scores' maximum; scores that need more than a factor are put back as they are to be
-          float top = -INFINITY;
           // Which of a step's tokens the row sees, a bit each.
           auto seen_of = [&](int s) -> uint32_t {
             const int a = j0 + s * CW, x = w.s.first - a;
@@ -607,24 +671,25 @@ __global__ void __launch_bounds__(Cfg<DT, NM, kFp4>::kThreads, 1) tree_attention
               v |= (uint32_t)sees << x;
             return v & have;
           };
-          if (!general) {
+          // ---- the scores' maximum; scores that need more than a factor are put back as they are to be.  Where the row
+          // has one step, it stays in registers.
+          float top = -INFINITY;
+          uint32_t v[CW];
 #pragma unroll 1
-            for (int s = step0; s < step0 + steps; ++s) {
-              uint32_t v[CW];
-              tmem_load<CW>(scores + s * CW, v);
-              tmem_loaded<CW>(v);
+          for (int s = step0; s < step0 + steps; ++s) {
+            tmem_load<CW>(scores + s * CW, v);
+            tmem_loaded<CW>(v);
+            if (!general) {
+              float top2 = -INFINITY;  // two chains
 #pragma unroll
-              for (int e = 0; e < CW; e += 2) top = max3f(top, __uint_as_float(v[e]), __uint_as_float(v[e + 1]));
-            }
-            top *= fs;
-          } else {
-#pragma unroll 1
-            for (int s = step0; s < step0 + steps; ++s) {
+              for (int e = 0; e < CW; e += 4) {
+                top = max3f(top, __uint_as_float(v[e]), __uint_as_float(v[e + 1]));
+                top2 = max3f(top2, __uint_as_float(v[e + 2]), __uint_as_float(v[e + 3]));
+              }
+              top = fmaxf(top, top2);
+            } else {
               const int a = j0 + s * CW;
               const uint32_t seen = masked ? seen_of(s) : kAll;
-              uint32_t v[CW];
-              tmem_load<CW>(scores + s * CW, v);
-              tmem_loaded<CW>(v);
 #pragma unroll
               for (int e = 0; e < CW; ++e) {
                 float x = __uint_as_float(v[e]) * fs;
@@ -639,19 +704,20 @@ __global__ void __launch_bounds__(Cfg<DT, NM, kFp4>::kThreads, 1) tree_attention
                 top = fmaxf(top, x);
                 v[e] = __float_as_uint(x);
               }
-              tmem_store<CW>(scores + s * CW, v);
+              if (steps > 1 || slow) tmem_store<CW>(scores + s * CW, v);
             }
-            tmem_st_wait();
           }
+          if (general)
+            tmem_st_wait();
+          else
+            top *= fs;
           const float f = general ? 1.0f : fs;
           if (__any_sync(kAll, top > mx + kSlack)) {
             const float v = fminf(fmaxf(mx, top), kMostScore), cor = ex2(mx - v);  // 0 at the first score
             mx = v;
             l *= cor;
             if (!begins) {
-              wait(sh.o_done[m], (g - 1) & 1, 8u);
-              __syncwarp();
-              tc_fence_after();
+              o_ready(8u);
 #pragma unroll 1
               for (int d = 0; d < D; d += 16) {
                 uint32_t o[16];
@@ -667,44 +733,46 @@ __global__ void __launch_bounds__(Cfg<DT, NM, kFp4>::kThreads, 1) tree_attention
 
           // ---- the weights
           const float less = (kFp4 ? kFp4Exp : 0.0f) - mx;
-          float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
           if (!slow) {
+            constexpr int kOut = kFp4 ? CW / 2 : CW;
+            const u64 ff = pack2(f, f), ll = pack2(less, less), tiny = pack2(0x1p-30f, 0x1p-30f);
+            u64 sum[2] = {0ull, 0ull};
 #pragma unroll 1
-            for (int s = 0; s < 4; ++s) {
-              constexpr int kOut = kFp4 ? CW / 2 : CW;
-              uint32_t v[CW], out[kOut];
-              if (s < step0 || s >= step0 + steps) {  // another copy's tokens
-#pragma unroll
-                for (int e = 0; e < kOut; ++e) out[e] = 0u;
-              } else {
+            for (int s = step0; s < step0 + steps; ++s) {
+              if (steps > 1) {
                 tmem_load<CW>(scores + s * CW, v);
                 tmem_loaded<CW>(v);
+              }
+              uint32_t out[kOut];
 #pragma unroll
-                for (int e = 0; e < CW; e += 2) {
-                  const float w0 = ex2(fmaf(__uint_as_float(v[e]), f, less)), w1 = ex2(fmaf(__uint_as_float(v[e + 1]), f, less));
-                  sum[e & 2] += w0;
-                  sum[(e & 2) + 1] += w1;
-                  if (kFp4) {
-                    out[e / 2] = f16x2(w0, w1);
-                  } else {
-                    // The upper part by truncation, so that the lower is not negative, and not 0 either where the weight
-                    // is not (2^-126 then): times an infinite element of V both give its infinity.
-                    out[e / 2] = prmt(__float_as_uint(w0), __float_as_uint(w1), 0x7632u);
-                    out[CW / 2 + e / 2] = bf16x2(fmaxf(w0 - bf_hi(__float_as_uint(w0)), fminf(w0, 0x1p-126f)),
-                                                 fmaxf(w1 - bf_hi(__float_as_uint(w1)), fminf(w1, 0x1p-126f)));
-                  }
+              for (int e = 0; e < CW; e += 2) {
+                float x0, x1;
+                unpack2(fma2(bits2(v[e], v[e + 1]), ff, ll), x0, x1);
+                const float w0 = ex2(x0), w1 = ex2(x1);
+                const u64 ww = pack2(w0, w1);
+                sum[e / 2 & 1] = add2(sum[e / 2 & 1], ww);
+                if (kFp4) {
+                  out[e / 2] = f16x2(w0, w1);
+                } else {
+                  // The upper part by truncation, so that the lower is not negative; 2^-30 of the weight on top, so that
+                  // it is not 0 either: times an infinite element of V both give its infinity.
+                  const u64 up = bits2(__float_as_uint(w0) & 0xFFFF0000u, __float_as_uint(w1) & 0xFFFF0000u);
+                  float l0, l1;
+                  unpack2(fma2(ww, tiny, sub2(ww, up)), l0, l1);
+                  out[e / 2] = prmt(__float_as_uint(w0), __float_as_uint(w1), 0x7632u);
+                  out[CW / 2 + e / 2] = bf16x2(l0, l1);
                 }
               }
               tmem_store<kOut>(scores + s * CW, out);
             }
+            float s0, s1;
+            unpack2(add2(sum[0], sum[1]), s0, s1);
+            l += s0 + s1;
           } else {
             // Products of what the row sees alone.
-            const uint32_t slot = (2 * g + 1) % C::kSlots, v_smem = ring + slot * C::kSlot;
-            if (!begins) {
-              wait(sh.o_done[m], (g - 1) & 1, 16u);
-              __syncwarp();
-              tc_fence_after();
-            }
+            const uint32_t v_smem = ring + (2 * tile + 1) % C::kSlots * C::kSlot;
+            if (!begins) o_ready(16u);
+            float sum = 0.0f;
 #pragma unroll 1
             for (int d = 0; d < D; d += 16) {
               uint32_t o[16];
@@ -721,7 +789,7 @@ __global__ void __launch_bounds__(Cfg<DT, NM, kFp4>::kThreads, 1) tree_attention
                 uint32_t xs;
                 tmem_ld1(scores + col, xs);
                 const float x = fmaf(__uint_as_float(xs), f, less), wt = ex2(x);
-                if (d == 0) sum[0] += wt;
+                if (d == 0) sum += wt;
                 const bool mine = (seen_of(col / CW) >> (col % CW)) & 1u;
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
@@ -743,8 +811,8 @@ __global__ void __launch_bounds__(Cfg<DT, NM, kFp4>::kThreads, 1) tree_attention
               }
               tmem_store<16>(o_col + d, o);
             }
+            l += sum;
           }
-          l += (sum[0] + sum[2]) + (sum[1] + sum[3]);
           tmem_st_wait();
         }
         if (tl == 0) sh.skip[buf] = slow;
@@ -753,42 +821,36 @@ __global__ void __launch_bounds__(Cfg<DT, NM, kFp4>::kThreads, 1) tree_attention
         if (lane == 0) mbar_arrive(smem_u32(&sh.p_full[buf]));
       }
 
-      // ---- the part's end: O, m and l of every row, finished where the part is the whole row
-      wait(sh.o_done[m], (g - 1) & 1, 32u);
-      __syncwarp();
-      tc_fence_after();
+      // ---- the part's end: O, m and l of every row, finished where the part is the whole row.  Copies of a row, and the
+      // two groups that took turns, are added up in shared memory.
+      if (done > 0) o_ready(32u);
       const bool all = w.first && w.last;
-      const int64_t slot = (2 * (int64_t)blockIdx.x + (w.first ? 1 : 0)) * NM + m;
-      float4* part = p.part + slot * (DT / 4 * 128);
+      float4* part = p.part + (slot - (C::kTurns ? m : 0)) * (DT / 4 * 128);
       const int64_t at = ((int64_t)w.b * p.t + i) * p.q_heads + h;  // of the results
       const float old = chained ? ex2(m_aside - mx) : 0.0f;
       if (!valid) mx = kNoScore, l = 0.0f;
-      if (copies > 1) {
-        sh.ml[tl] = make_float2(mx, l);
-        bar_sync(2 + m, 128);
-      }
+      constexpr int kTurners = C::kTurns ? 2 : 1;
+      const int many = copies * kTurners;
       float M = mx, L = l;
-      if (copies > 1) {
-        for (int k = 0; k < copies; ++k) M = fmaxf(M, sh.ml[tl % own + k * own].x);
+      if (many > 1) {
+        sh.ml[m * 128 + tl] = make_float2(mx, l);
+        bar_sync(1, C::kSoftmax * 32);
+        for (int k = 0; k < many; ++k) M = fmaxf(M, sh.ml[tl % own + k * own].x);
         L = 0.0f;
-        for (int k = 0; k < copies; ++k) {
+        for (int k = 0; k < many; ++k) {
           const float2 s = sh.ml[tl % own + k * own];
           L += ex2(s.x - M) * s.y;
         }
       }
-      const float last = all ? out_factor<kFp4>(L, vts) : 1.0f, f = copies > 1 ? ex2(mx - M) : 1.0f;
-      // Columns [d, d + 8) of the row's sum, to their place.
+      const float last = all ? out_factor<kFp4>(L, vts) : 1.0f, f = many > 1 ? ex2(mx - M) : 1.0f;
+      // Columns [d, d + 4) of the row's sum, to their place.
       auto put = [&](int d, const float* x) {
         if (!held || dead || d >= D) return;
-        if (all) {
-          uint4 v;
-          v.x = bf16x2(x[0] * last, x[1] * last), v.y = bf16x2(x[2] * last, x[3] * last);
-          v.z = bf16x2(x[4] * last, x[5] * last), v.w = bf16x2(x[6] * last, x[7] * last);
-          *reinterpret_cast<uint4*>(p.out + at * D + d) = v;
-        } else {
-          part[(d / 4) * 128 + tl % own] = make_float4(x[0], x[1], x[2], x[3]);
-          part[(d / 4 + 1) * 128 + tl % own] = make_float4(x[4], x[5], x[6], x[7]);
-        }
+        if (all)
+          *reinterpret_cast<uint2*>(p.out + at * D + d) =
+              make_uint2(bf16x2(x[0] * last, x[1] * last), bf16x2(x[2] * last, x[3] * last));
+        else
+          part[(d / 4) * 128 + (MT == 2 ? tl : r)] = make_float4(x[0], x[1], x[2], x[3]);
       };
       auto take = [&](int d, float* x) {  // 16 columns of O, with what was set aside
         uint32_t v[16];
@@ -805,48 +867,56 @@ __global__ void __launch_bounds__(Cfg<DT, NM, kFp4>::kThreads, 1) tree_attention
           }
         }
 #pragma unroll
-        for (int e = 0; e < 16; ++e) x[e] = valid ? x[e] * f : 0.0f;
+        for (int e = 0; e < 16; ++e) x[e] = valid && done > 0 ? x[e] * f : 0.0f;
       };
-      if (copies == 1) {
+      if (many == 1) {
         if (!idle)
 #pragma unroll 1
           for (int d = 0; d < D; d += 16) {
             float x[16];
             take(d, x);
             put(d, x);
+            put(d + 4, x + 4);
             put(d + 8, x + 8);
+            put(d + 12, x + 12);
           }
       } else {
-        float* stage = reinterpret_cast<float*>(smem);  // [half the dimensions][128], where the queries were
-        constexpr int kHalf = DT / 2;
-        const int each = kHalf / copies;
+        float* stage = reinterpret_cast<float*>(smem);  // [group][32][128], where the queries were
+        const int each = 32 / many, who = (kTurners == 2 ? m * copies : 0) + copy;
 #pragma unroll 1
-        for (int half = 0; half < 2 && half * kHalf < D; ++half) {
+        for (int d0 = 0; d0 < D; d0 += 32) {
 #pragma unroll 1
-          for (int d = 0; d < kHalf; d += 16) {
+          for (int d = 0; d < 32; d += 16) {
             float x[16];
-            take(half * kHalf + d, x);
+            take(d0 + d, x);
 #pragma unroll
-            for (int e = 0; e < 16; ++e) stage[(d + e) * 128 + tl] = x[e];
+            for (int e = 0; e < 16; ++e) stage[(m * 32 + d + e) * 128 + tl] = x[e];
           }
-          bar_sync(2 + m, 128);
+          bar_sync(1, C::kSoftmax * 32);
 #pragma unroll 1
-          for (int d = copy * each; d < (copy + 1) * each; d += 8) {
-            float x[8];
+          for (int d = who * each; d < (who + 1) * each; d += 4) {
+            float x[4];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
+            for (int e = 0; e < 4; ++e) {
               const float* s = stage + (d + e) * 128 + tl % own;
-              x[e] = s[0] + s[own];
-              if (copies == 4) x[e] += s[2 * own] + s[3 * own];
+              x[e] = 0.0f;
+#pragma unroll
+              for (int k = 0; k < kTurners; ++k) {
+                const float* t = s + k * (32 * 128);
+                float y = t[0];
+                if (copies > 1) y += t[own];
+                if (copies == 4) y += t[2 * own] + t[3 * own];
+                x[e] += y;
+              }
             }
-            put(half * kHalf + d, x);
+            put(d0 + d, x);
           }
-          bar_sync(2 + m, 128);
+          bar_sync(1, C::kSoftmax * 32);
         }
       }
-      if (held && copy == 0 && !dead) {
+      if (held && copy == 0 && !dead && (!C::kTurns || m == 0)) {
         if (!all)
-          p.stat[slot * 128 + tl] = make_float2(M, L);
+          p.stat[(slot - (C::kTurns ? m : 0)) * 128 + tl] = make_float2(M, L);
         else if (p.lse)
           p.lse[at] = lse_of<kFp4>(M, L);
       }
@@ -855,171 +925,302 @@ __global__ void __launch_bounds__(Cfg<DT, NM, kFp4>::kThreads, 1) tree_attention
       tc_fence_before();
       __syncwarp();
       ++turn;
+      g += w.tiles;
     }
-  } else if (warp == C::kSoftmax) {
+  } else {
+    if constexpr (C::kSoftRegs > C::kRegs) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kOtherRegs));
+  if (warp == C::kSoftmax) {
     // ================================================= one thread issues the products
     if (elect_one()) {
       constexpr uint32_t kType = kFp4 ? 0u : (1u << 7) | (1u << 10);
       const uint32_t i_scores = (1u << 4) | kType | ((uint32_t)(TN >> 3) << 17) | (8u << 24);
       const uint32_t i_out = (1u << 4) | kType | (1u << 16) | ((uint32_t)(D >> 3) << 17) | (8u << 24);
       uint32_t g = 0, turn = 0;
-      auto scores = [&](uint32_t tile, int m) {  // of tile number `tile`, into its buffer
+      auto scores = [&](uint32_t tile, int m) {  // of tile number `tile` and the m-th rows, into their buffer
         const uint32_t q = 2 * tile, slot = q % C::kSlots;
         if (m == 0) {
           wait(sh.full[slot], (q / C::kSlots) & 1, 64u);
-          if (!kFp4) fence_proxy_async_smem();  // of what cp.async has written
+          if (!kFp4 && !p.box) fence_proxy_async_smem();  // of what cp.async has written
           tc_fence_after();
         }
-        const int buf = NM == 2 ? m : (int)(tile & 1);
+        const int buf = MT == 2 ? m : (int)(tile & 1);
         const uint32_t a = q_smem + m * (128 * DT * 2), b = ring + slot * C::kSlot;
 #pragma unroll 1
         for (int k = 0; k < D / 16; ++k)
           mma_f16(tmem + buf * TN, smem_desc_sw128(a + (k >> 2) * 16384 + (k & 3) * 32),
                   smem_desc_sw128(b + (k >> 2) * C::kBlock + (k & 3) * 32), i_scores, k > 0);
         mma_commit(smem_u32(&sh.s_full[buf]));
-        if (m == NM - 1) mma_commit(smem_u32(&sh.empty[slot]));
+        if (m == MT - 1) mma_commit(smem_u32(&sh.empty[slot]));
       };
       while (walk.next(p, mate, w)) {
         wait(sh.q_full, turn & 1, 128u);
         ++turn;
+        const int R = min(128 * MT, p.t * p.group - w.chunk * 128 * MT);
+        const int copies = MT == 2 || R > 64 ? 1 : (R > 32 ? 2 : 4);
         tc_fence_after();
-        for (int m = 0; m < NM; ++m) scores(g, m);
+        for (int m = 0; m < MT; ++m) scores(g, m);
         for (int it = 0; it < w.tiles; ++it, ++g) {
-          if (NM == 1 && it + 1 < w.tiles) scores(g + 1, 0);
+          if (MT == 1 && it + 1 < w.tiles) scores(g + 1, 0);
           const uint32_t q = 2 * g + 1, slot = q % C::kSlots, v = ring + slot * C::kSlot;
-          for (int m = 0; m < NM; ++m) {
-            const int buf = NM == 2 ? m : (int)(g & 1);
+          for (int m = 0; m < MT; ++m) {
+            const int buf = MT == 2 ? m : (int)(g & 1);
+            const int acc = C::kGroups == 2 ? buf : 0;                     // whose O
+            const bool begins = (C::kTurns ? it >> 1 : it) % kChain == 0;  // it is at 0
             if (m == 0) {
               wait(sh.full[slot], (q / C::kSlots) & 1, 256u);
-              if (!kFp4) fence_proxy_async_smem();
+              if (!kFp4 && !p.box) fence_proxy_async_smem();
             }
-            wait(sh.p_full[buf], NM == 2 ? g & 1 : (g >> 1) & 1, 512u);
+            wait(sh.p_full[buf], MT == 2 ? g & 1 : (g >> 1) & 1, 512u);
             tc_fence_after();
             if (!*reinterpret_cast<volatile int*>(&sh.skip[buf])) {
 #pragma unroll 1
               for (int k = 0; k < TN / 16; ++k) {
                 const uint32_t a = tmem + buf * TN + (k * 16 / CW) * CW + (k * 16 % CW) / 2;
                 const uint64_t b = smem_desc_sw128_mn(v + k * 2048, C::kBlock);
-                mma_f16_tmem_a(tmem + C::kScoreCols + m * DT, a, b, i_out, k > 0 || it % kChain != 0);
-                if (!kFp4) mma_f16_tmem_a(tmem + C::kScoreCols + m * DT, a + CW / 2, b, i_out, 1u);
+                // A copy's tokens go to its lanes of O alone; the first of them begin it.
+                const int copy = k * copies * 16 / TN;
+                const bool first = begins && k * 16 % (TN / copies) == 0;
+                auto off = [&](int quarter) { return quarter / (4 / copies) == copy ? 0u : kAll; };
+                const uint4 lanes = make_uint4(off(0), off(1), off(2), off(3));
+                mma_f16_tmem_a_lanes(tmem + C::kScoreCols + acc * DT, a, b, i_out, !first, lanes);
+                if (!kFp4) mma_f16_tmem_a_lanes(tmem + C::kScoreCols + acc * DT, a + CW / 2, b, i_out, 1u, lanes);
               }
             }
-            mma_commit(smem_u32(&sh.o_done[m]));
-            if (m == NM - 1) mma_commit(smem_u32(&sh.empty[slot]));
-            if (NM == 2 && it + 1 < w.tiles) scores(g + 1, m);
+            mma_commit(smem_u32(&sh.o_done[acc]));
+            if (m == MT - 1) mma_commit(smem_u32(&sh.empty[slot]));
+            if (MT == 2 && it + 1 < w.tiles) scores(g + 1, m);
           }
         }
       }
       mma_commit(smem_u32(&sh.end));
       mbar_wait(smem_u32(&sh.end), 0, nullptr, kWaitLimitNs);
     }
-  } else {
-    // ================================================= producers
-    const int pw = warp - C::kSoftmax - 1;
-    constexpr int kRows = C::kRows;
-    uint32_t g = 0, q = 0, sent = 0;  // tiles, copies asked for, copies handed over
-    [[maybe_unused]] const uint32_t raw0 = ring + C::kSlots * C::kSlot + pw * C::kRawDepth * C::kRawSlot;
-    // The oldest copy not decoded yet, with `later` behind it: once it has landed, for the tensor cores.
-    [[maybe_unused]] auto hand_over = [&](int later) {
-      cp_wait_at_most(later);
-      __syncwarp();
-      wait(sh.empty[sent % C::kSlots], ((sent / C::kSlots) & 1) ^ 1, 1024u);
-      __syncwarp();
-      decode_tile<C>(ring, raw0, sent, pw, lane, D);
-      fence_proxy_async_smem();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&sh.full[sent % C::kSlots]));
-      ++sent;
-    };
-    while (walk.next(p, mate, w)) {
-      const int32_t* table = p.table + (int64_t)w.b * p.table_stride;
-      auto page_of = [&](int tok) { return p.page_shift >= 0 ? tok >> p.page_shift : tok / p.c.page_size; };
-      // Page of this lane's token of the tile.
-      auto ask = [&](int it) -> int {
-        const int tok = w.s.from + (w.tile + w.tiles - 1 - it) * TN + pw * kRows + lane;
-        return it < w.tiles && lane < kRows && tok >= w.s.low && tok < w.s.end ? table[page_of(tok)] : -1;
-      };
-      int page = ask(0);
+  } else if (!kFp4 && p.box && warp < C::kSoftmax + 3) {
+    // ================================================= rows of a bf16 cache by TMA, boxes of one page, 64 dimensions
+    // each: keys by one warp, values by another
+    {
+      const int kv = warp - C::kSoftmax - 1;
+      const int boxes = TN / p.box, blocks = (D + 63) / 64;  // of a tile; at most 16 copies to its keys or values
+      const int box = lane % boxes, block = lane / boxes;
+      const bool mine = block < blocks;
+      uint32_t g = 0;
+      while (walk.next(p, mate, w)) {
+        const int32_t* table = p.table + (int64_t)w.b * p.table_stride;
+        auto page_of = [&](int tok) { return p.page_shift >= 0 ? tok >> p.page_shift : tok / p.c.page_size; };
+        // Page of this lane's box of the tile.
+        auto ask = [&](int it) -> int {
+          const int tok = w.s.from + (w.tile + w.tiles - 1 - it) * TN + box * p.box;
+          return mine && it < w.tiles && tok < w.s.end && tok + p.box > w.s.low ? table[page_of(tok)] : -1;
+        };
+        int page = ask(0);
 #pragma unroll 1
-      for (int it = 0; it < w.tiles; ++it, ++g) {
-        const int tok = w.s.from + (w.tile + w.tiles - 1 - it) * TN + pw * kRows + lane;
-        const bool ok = page >= 0 && page < p.c.pages;
-        int64_t at = 0, sat = 0;
-        if (ok) {
-          const int off = tok - page_of(tok) * p.c.page_size;
-          at = ((int64_t)page * p.c.page_stride + (int64_t)off * p.c.token_stride + (int64_t)w.head * p.c.head_stride) *
-               (kFp4 ? 1 : 2);
-          sat = (int64_t)page * p.c.scale_page_stride + (int64_t)off * p.c.scale_token_stride +
-                (int64_t)w.head * p.c.scale_head_stride;
+        for (int it = 0; it < w.tiles && !dead; ++it, ++g) {
+          const int j0 = w.s.from + (w.tile + w.tiles - 1 - it) * TN, tok = j0 + box * p.box;
+          const bool ok = page >= 0 && page < p.c.pages;
+          const int from = page, row = tok - page_of(tok) * p.c.page_size;
+          page = ask(it + 1);
+          const uint32_t good = __ballot_sync(kAll, ok);  // bit i: box i % boxes
+          if (kv == 0 && lane < TN / 32) {
+            const int a = j0 + lane * 32;
+            auto below = [](int k) -> uint32_t { return k <= 0 ? 0u : (k >= 32 ? kAll : (1u << k) - 1u); };
+            uint32_t there = below(w.s.end - a) & ~below(w.s.low - a);
+            if (!((good >> (lane * 32 / p.box)) & 1u)) there &= 0xFFFF0000u;
+            if (!((good >> ((lane * 32 + 16) / p.box)) & 1u)) there &= 0xFFFFu;
+            sh.there[g % kThere][lane] = there;
+          }
+          const uint32_t bytes = __popc(good) * p.box * 128;
+          __syncwarp();
+          const uint32_t q = 2 * g + kv, slot = q % C::kSlots, bar = smem_u32(&sh.full[slot]);
+          wait(sh.empty[slot], ((q / C::kSlots) & 1) ^ 1, 1024u);
+          dead = __any_sync(kAll, dead);
+          if (dead) break;
+          if (lane == 0) mbar_arrive_expect_tx(bar, bytes);
+          __syncwarp();
+          if (ok)
+            tma_load_4d(ring + slot * C::kSlot + block * C::kBlock + box * p.box * 128, kv ? &tm_v : &tm_k, block * 64, row,
+                        w.head, from, bar);
+          __syncwarp();
         }
-        page = ask(it + 1);
-        const uint32_t there = __ballot_sync(kAll, ok);
-        if (lane == 0) {
-          uint8_t* to = reinterpret_cast<uint8_t*>(sh.there[g & 7]) + pw * (kRows / 8);
-          if constexpr (kRows == 32)
-            *reinterpret_cast<uint32_t*>(to) = there;
-          else if constexpr (kRows == 16)
-            *reinterpret_cast<uint16_t*>(to) = (uint16_t)there;
-          else
-            *to = (uint8_t)there;
-        }
-        // Where this lane's pieces of rows begin: all asked of the other lanes at once, for keys and values alike.
-        constexpr int kPieces = kFp4 ? DT / 16 : DT / 8, kAtOnce = 32 / kPieces, kSteps = kRows / kAtOnce;
-        constexpr int kBytes = kFp4 ? 8 : 16;
-        const int piece = lane % kPieces, r0 = lane / kPieces;
-        int64_t from[kSteps];
-        uint32_t take = 0;
-#pragma unroll
-        for (int j = 0; j < kSteps; ++j) from[j] = __shfl_sync(kAll, at, r0 + j * kAtOnce) + piece * kBytes;
-#pragma unroll
-        for (int j = 0; j < kSteps; ++j) {
-          const bool t = piece * kBytes * (kFp4 ? 2 : 1) < D * (kFp4 ? 1 : 2) && ((there >> (r0 + j * kAtOnce)) & 1u);
-          take |= (uint32_t)t << j;
-          if (!t) from[j] = 0;
-        }
+      }
+      if (dead)  // the copies in flight land before the CTA ends
+        for (uint32_t n = g > C::kSlots / 2 ? g - C::kSlots / 2 : 0; n < g; ++n)
+          mbar_wait(smem_u32(&sh.full[(2 * n + kv) % C::kSlots]), ((2 * n + kv) / C::kSlots) & 1, nullptr, kWaitLimitNs);
+    }
+  } else if (!kFp4) {
+    // ================================================= or by cp.async, row by row, by two warps
+    if constexpr (!kFp4) {
+      const int pw = warp - C::kSoftmax - 2;
+      constexpr int kRows = C::kRows, kPieces = DT / 8, kRowsAtOnce = 32 / kPieces;
+      const int piece = lane % kPieces, r0 = lane / kPieces;
+      uint32_t g = 0, q = 0;
+      while (!p.box && pw >= 0 && walk.next(p, mate, w)) {
+        const int32_t* table = p.table + (int64_t)w.b * p.table_stride;
 #pragma unroll 1
-        for (int kv = 0; kv < 2; ++kv, ++q) {
-          const uint8_t* base = static_cast<const uint8_t*>(kv ? p.c.v : p.c.k);
-          if constexpr (!kFp4) {
+        for (int it = 0; it < w.tiles; ++it, ++g) {
+          const int tok0 = w.s.from + (w.tile + w.tiles - 1 - it) * TN + pw * kRows;
+          int64_t at[kRows / 32];  // of tokens lane, lane + 32; < 0: not there
+#pragma unroll
+          for (int j = 0; j < kRows / 32; ++j) {
+            const int tok = tok0 + 32 * j + lane, in_page = tok / p.c.page_size;
+            int page = -1;
+            if (tok >= w.s.low && tok < w.s.end) page = table[in_page];
+            const bool ok = page >= 0 && page < p.c.pages;
+            at[j] = -1;
+            if (ok)
+              at[j] = 2 * ((int64_t)page * p.c.page_stride + (int64_t)(tok - in_page * p.c.page_size) * p.c.token_stride +
+                           (int64_t)w.head * p.c.head_stride);
+            const uint32_t there = __ballot_sync(kAll, ok);
+            if (lane == 0) sh.there[g % kThere][pw * (kRows / 32) + j] = there;
+          }
+#pragma unroll 1
+          for (int kv = 0; kv < 2; ++kv, ++q) {
+            const uint8_t* base = static_cast<const uint8_t*>(kv ? p.c.v : p.c.k);
             const uint32_t slot = q % C::kSlots;
             wait(sh.empty[slot], ((q / C::kSlots) & 1) ^ 1, 1024u);
             __syncwarp();
             const uint32_t dst = ring + slot * C::kSlot + (piece >> 3) * C::kBlock + pw * kRows * 128;
 #pragma unroll
-            for (int j = 0; j < kSteps; ++j) {
-              const int r = r0 + j * kAtOnce;
-              cp_async<16>(dst + r * 128 + (((piece & 7) ^ (r & 7)) << 4), base + from[j], (take >> j) & 1u);
-            }
-            cp_async_arrive(smem_u32(&sh.full[slot]));  // when this lane's have landed
-          } else {
-            // ---- the codes as they lie, into this warp's own part
-            const uint32_t raw = raw0 + (q % C::kRawDepth) * C::kRawSlot;
-            const uint8_t* scales = kv ? p.c.v_scales : p.c.k_scales;
-#pragma unroll
-            for (int j = 0; j < kSteps; ++j)
-              cp_async<8>(raw + (r0 + j * kAtOnce) * C::kRawRow + piece * 8, base + from[j], (take >> j) & 1u);
-            if (lane < kRows) {
-              const uint32_t sd = raw + lane * C::kRawRow + DT / 2;
-              const uint8_t* src = scales + (ok ? sat : 0);
-              if (D == 128) {
-                cp_async<8>(sd, src, ok);
-              } else if (D == 256) {
-                cp_async<16>(sd, src, ok);
-              } else if (D % 64 == 0) {
-                for (int k = 0; k < D / 16; k += 4) cp_async<4>(sd + k, src + k, ok);
-              } else {  // rows of an odd number of scale bytes
-                for (int k = 0; k < D / 16; ++k) sts8(sd + k, ok ? src[k] : 0u);
+            for (int j = 0; j < kRows / 32; ++j)
+#pragma unroll 4
+              for (int k = 0; k < 32 / kRowsAtOnce; ++k) {
+                const int r = r0 + k * kRowsAtOnce, row = 32 * j + r;
+                const int64_t from = __shfl_sync(kAll, at[j], r);
+                const bool take = from >= 0 && piece * 8 < D;
+                cp_async<16>(dst + row * 128 + (((piece & 7) ^ (row & 7)) << 4), base + (take ? from + piece * 16 : 0), take);
               }
-            }
-            cp_commit();
-            if (q - sent >= C::kLag) hand_over(C::kLag);
+            cp_async_arrive(smem_u32(&sh.full[slot]));  // when this lane's have landed
           }
         }
       }
+      cp_async_wait_all();
     }
-    if constexpr (kFp4)
-      while (sent < q) hand_over((int)(q - sent - 1));
+  } else if (warp < C::kSoftmax + 4) {
+    // ================================================= helpers: where a MixFP4 tile's rows lie, a third of the tiles each
+    if constexpr (kFp4) {
+      const int me = warp - C::kSoftmax - 1;
+      uint32_t g = 0;
+      while (walk.next(p, mate, w)) {
+        const int32_t* table = p.table + (int64_t)w.b * p.table_stride;
+        for (int it = 0; it < w.tiles; ++it, ++g) {
+          if ((int)(g % 3) != me) continue;
+          const uint32_t at = places + (g % C::kAddresses) * (TN * 16);
+          const int tok0 = w.s.from + (w.tile + w.tiles - 1 - it) * TN + lane;
+          int page[TN / 32];
+#pragma unroll
+          for (int j = 0; j < TN / 32; ++j) {
+            const int tok = tok0 + 32 * j;
+            page[j] = -1;
+            if (tok >= w.s.low && tok < w.s.end)
+              page[j] = table[p.page_shift >= 0 ? tok >> p.page_shift : tok / p.c.page_size];
+          }
+          wait(sh.used[g % C::kAddresses], ((g / C::kAddresses) & 1) ^ 1, 2048u);
+          __syncwarp();
+#pragma unroll
+          for (int j = 0; j < TN / 32; ++j) {
+            const int tok = tok0 + 32 * j;
+            const int off = p.page_shift >= 0 ? tok & (p.c.page_size - 1) : tok % p.c.page_size;
+            const bool ok = page[j] >= 0 && page[j] < p.c.pages;
+            int64_t x = -1, y = 0;
+            if (ok) {
+              x = (int64_t)page[j] * p.c.page_stride + (int64_t)off * p.c.token_stride + (int64_t)w.head * p.c.head_stride;
+              y = (int64_t)page[j] * p.c.scale_page_stride + (int64_t)off * p.c.scale_token_stride +
+                  (int64_t)w.head * p.c.scale_head_stride;
+            }
+            sts128(at + (32 * j + lane) * 16, (uint32_t)x, (uint32_t)(x >> 32), (uint32_t)y, (uint32_t)(y >> 32));
+            const uint32_t there = __ballot_sync(kAll, ok);
+            if (lane == 0) sh.there[g % kThere][j] = there;
+          }
+          __syncwarp();
+          if (lane == 0) mbar_arrive(smem_u32(&sh.placed[g % C::kAddresses]));
+        }
+      }
+    }
+  } else if constexpr (kFp4) {
+    // ================================================= producers of a MixFP4 cache: codes in, f16 out
+    const int pw = warp - C::kSoftmax - 4;
+    using L = Lanes<DT>;
+    const int piece = L::piece(lane), r0 = L::row(lane);
+    const uint32_t raw0 = ring + C::kSlots * C::kSlot + pw * C::kRawDepth * C::kRawSlot;
+    constexpr int kRows = C::kRows, kSteps = kRows / L::kRowsAtOnce;
+    uint32_t g = 0, q = 0, sent = 0;  // tiles, copies asked for, copies decoded
+    // The oldest copy not decoded yet, with `later` behind it: once it has landed, for the tensor cores.
+    auto hand_over = [&](int later) {
+      cp_wait_at_most(later);
+      __syncwarp();
+      const uint32_t slot = sent % C::kSlots;
+      wait(sh.empty[slot], ((sent / C::kSlots) & 1) ^ 1, 1024u);
+      __syncwarp();
+      if (piece * 16 < D)
+        decode_rows<C, L, kSteps>(ring + slot * C::kSlot + pw * kRows * 128, raw0 + (sent % C::kRawDepth) * C::kRawSlot,
+                                  piece, r0, C::kRows >= 8 ? 0 : pw * kRows);
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&sh.full[slot]));
+      ++sent;
+    };
+    while (walk.next(p, mate, w)) {
+#pragma unroll 1
+      for (int it = 0; it < w.tiles; ++it, ++g) {
+        wait(sh.placed[g % C::kAddresses], (g / C::kAddresses) & 1, 4096u);
+        __syncwarp();
+        const uint32_t at = places + (g % C::kAddresses) * (TN * 16) + pw * kRows * 16;
+        int64_t from[kSteps];
+#pragma unroll
+        for (int j = 0; j < kSteps; ++j) {
+          const uint2 v = lds64(at + (r0 + j * L::kRowsAtOnce) * 16);
+          from[j] = (int64_t)((u64)v.x | (u64)v.y << 32);
+        }
+#pragma unroll 1
+        for (int kv = 0; kv < 2; ++kv, ++q) {
+          const uint8_t* base = static_cast<const uint8_t*>(kv ? p.c.v : p.c.k);
+          const uint8_t* scales = kv ? p.c.v_scales : p.c.k_scales;
+          const uint32_t raw = raw0 + (q % C::kRawDepth) * C::kRawSlot, sd = raw + kRows * (DT / 2);
+#pragma unroll
+          for (int j = 0; j < kSteps; ++j) {
+            const bool take = from[j] >= 0 && piece * 16 < D;
+            cp_async<8>(raw + (r0 + j * L::kRowsAtOnce) * (DT / 2) + piece * 8, base + (take ? from[j] + piece * 8 : 0), take);
+          }
+          if (D % 64 == 0) {
+            if (lane < kRows) {
+              const uint4 v = lds128(at + lane * 16);
+              const bool ok = (int32_t)v.y >= 0;
+              const uint8_t* src = scales + (ok ? (int64_t)((u64)v.z | (u64)v.w << 32) : 0);
+              if (D == 128) {
+                cp_async<8>(sd + lane * 16, src, ok);
+              } else if (D == 256) {
+                cp_async<16>(sd + lane * 16, src, ok);
+              } else {
+                for (int k = 0; k < D / 16; k += 4) cp_async<4>(sd + lane * 16 + k, src + k, ok);
+              }
+            }
+          } else {  // rows of an odd number of scale bytes: a lane to a byte
+            const int bytes = D / 16;
+            uint32_t b[(kRows * 15 + 31) / 32];
+#pragma unroll
+            for (int k = 0; k < (kRows * 15 + 31) / 32; ++k) {
+              const int x = lane + 32 * k, r = x / bytes;
+              b[k] = 0u;
+              if (r < kRows) {
+                const uint4 v = lds128(at + r * 16);
+                if ((int32_t)v.y >= 0) b[k] = scales[(int64_t)((u64)v.z | (u64)v.w << 32) + x - r * bytes];
+              }
+            }
+#pragma unroll
+            for (int k = 0; k < (kRows * 15 + 31) / 32; ++k) {
+              const int x = lane + 32 * k, r = x / bytes;
+              if (r < kRows) sts8(sd + r * 16 + x - r * bytes, b[k]);
+            }
+          }
+          cp_commit();
+          if (q - sent >= C::kRawDepth - 1) hand_over(C::kRawDepth - 1);
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&sh.used[g % C::kAddresses]));
+      }
+    }
+    while (sent < q) hand_over((int)(q - sent - 1));
     cp_async_wait_all();
+  }
   }
   __syncwarp();
   tc_fence_before();
@@ -1031,17 +1232,18 @@ __global__ void __launch_bounds__(Cfg<DT, NM, kFp4>::kThreads, 1) tree_attention
 }
 
 // Joins the parts of the row that CTA blockIdx.x began: a thread to four dimensions of a query row.
-template <int DT, int NM, bool kFp4>
+template <int DT, int MT, bool kFp4>
 __global__ void __launch_bounds__(kJoinThreads) tree_attention_join_kernel(const TreeArgs p) {
   griddep_wait();
   const int4 s = p.split[blockIdx.x];
   if (s.x < 0) return;
   const int mate = (int)blockIdx.x % p.together, chunk = s.y % p.chunks, head = s.y / p.chunks * p.together + mate;
-  const int R = min(128 * NM, p.t * p.group - chunk * 128 * NM), D = p.c.head_dim;
+  constexpr int kGroups = Cfg<DT, MT, kFp4>::kGroups;
+  const int R = min(128 * MT, p.t * p.group - chunk * 128 * MT), D = p.c.head_dim;
   const int x = (int)blockIdx.y * kJoinThreads + (int)threadIdx.x, r = x % R, d4 = x / R;
   if (d4 >= D / 4) return;
   auto slot = [&](int k) {
-    return (2 * ((int64_t)k * p.together + mate) + (k == s.z ? 1 : 0)) * NM + (r >> 7);
+    return (2 * ((int64_t)k * p.together + mate) + (k == s.z ? 1 : 0)) * kGroups + (r >> 7);
   };
   float M = kNoScore, L = 0.0f;
   float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
@@ -1072,7 +1274,7 @@ __global__ void __launch_bounds__(kJoinThreads) tree_attention_join_kernel(const
       o.z = fmaf(f, v[a].z, o.z), o.w = fmaf(f, v[a].w, o.w);
     }
   }
-  const int idx = chunk * 128 * NM + r, i = idx / p.group, h = head * p.group + idx - i * p.group;
+  const int idx = chunk * 128 * MT + r, i = idx / p.group, h = head * p.group + idx - i * p.group;
   const int64_t at = ((int64_t)s.x * p.t + i) * p.q_heads + h;
   const float f = out_factor<kFp4>(L, kFp4 ? *p.c.v_ts : 1.0f);
   *reinterpret_cast<uint2*>(p.out + at * D + d4 * 4) = make_uint2(bf16x2(o.x * f, o.y * f), bf16x2(o.z * f, o.w * f));
@@ -1087,6 +1289,7 @@ inline int padded_dim(int D) { return D <= 64 ? 64 : (D <= 128 ? 128 : 256); }
 inline int row_tiles(const mixfp4_kv_cache* c, int64_t t, int64_t q_heads) {
   return c->head_dim <= 128 && t * (q_heads / c->heads) > 128 ? 2 : 1;
 }
+inline int groups_of(const mixfp4_kv_cache* c) { return c->head_dim > 128 ? 1 : 2; }  // of softmax warps
 inline int tile_tokens(const mixfp4_kv_cache* c) { return c->head_dim > 128 ? 64 : 128; }
 // Key heads whose CTAs walk over the same tokens at the same time.
 inline int together_of(const mixfp4_kv_cache* c) {
@@ -1096,18 +1299,43 @@ inline int together_of(const mixfp4_kv_cache* c) {
 }
 inline int grid_of(const mixfp4_kv_cache* c) { return num_sms() / together_of(c) * together_of(c); }
 
-template <int DT, int NM, bool kFp4>
-int launch(const TreeArgs& p, int grid, cudaStream_t s) {
-  using C = Cfg<DT, NM, kFp4>;
+// Rows that one TMA copy of a bf16 cache brings: of one page, and a part of a tile; 0 where TMA's rules do not allow it
+// (pages of no multiple of 16 tokens, rows of less than 64 elements, whose copies would not fill the operand's).
+inline int box_of(const mixfp4_kv_cache& c, int tokens) {
+  if (c.page_size % 16 != 0 || c.head_dim < 64 || c.pages == 0) return 0;
+  int n = 16;
+  while (n < tokens && c.page_size % (2 * n) == 0) n *= 2;
+  return n;
+}
+inline bool make_map_rows(CUtensorMap* m, const void* base, const mixfp4_kv_cache& c, int box) {
+  auto fn = encode_fn();
+  if (!fn) return false;
+  // An axis of one element has any stride; 32 bytes will do.
+  auto bytes = [](int64_t stride, int64_t n) { return (cuuint64_t)(n > 1 ? stride * 2 : 32); };
+  cuuint64_t dims[4] = {(cuuint64_t)c.head_dim, (cuuint64_t)c.page_size, (cuuint64_t)c.heads, (cuuint64_t)c.pages};
+  cuuint64_t strides[3] = {bytes(c.token_stride, c.page_size), bytes(c.head_stride, c.heads), bytes(c.page_stride, c.pages)};
+  cuuint32_t boxes[4] = {64, (cuuint32_t)box, 1, 1};
+  cuuint32_t estr[4] = {1, 1, 1, 1};
+  return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, boxes, estr,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int DT, int MT, bool kFp4>
+int launch(TreeArgs p, int grid, cudaStream_t s) {
+  using C = Cfg<DT, MT, kFp4>;
+  CUtensorMap maps[2] = {};
+  p.box = kFp4 ? 0 : box_of(p.c, C::kTokens);
+  if (p.box && !(make_map_rows(&maps[0], p.c.k, p.c, p.box) && make_map_rows(&maps[1], p.c.v, p.c, p.box))) p.box = 0;
   static std::atomic<uint64_t> done{0};
-  auto* kernel = tree_attention_kernel<DT, NM, kFp4>;
+  auto* kernel = tree_attention_kernel<DT, MT, kFp4>;
   if (!set_dynamic_smem_once(reinterpret_cast<const void*>(kernel), C::kSmem, done)) return MIXFP4_ERR_CUDA;
-  kernel<<<grid, C::kThreads, C::kSmem, s>>>(p);
+  kernel<<<grid, C::kThreads, C::kSmem, s>>>(p, maps[0], maps[1]);
   if (int st = launch_status()) return st;
   if (!p.joined) return MIXFP4_OK;
-  const int rows = p.t * p.group < 128 * NM ? p.t * p.group : 128 * NM;
+  const int rows = p.t * p.group < 128 * MT ? p.t * p.group : 128 * MT;
   const dim3 jg((unsigned)grid, (unsigned)((rows * (p.c.head_dim / 4) + kJoinThreads - 1) / kJoinThreads));
-  return launch_pdl(tree_attention_join_kernel<DT, NM, kFp4>, jg, dim3(kJoinThreads), 0, s, p) == cudaSuccess
+  return launch_pdl(tree_attention_join_kernel<DT, MT, kFp4>, jg, dim3(kJoinThreads), 0, s, p) == cudaSuccess
              ? MIXFP4_OK
              : MIXFP4_ERR_CUDA;
 }
@@ -1134,7 +1362,7 @@ int mixfp4_tree_attention_workspace(const mixfp4_kv_cache* cache, int64_t B, int
   if (B < 0 || t < 0 || t > kMostDrafts || q_heads < 0 || q_heads % cache->heads != 0) return MIXFP4_ERR_SHAPE;
   *bytes = 0;
   if (B == 0 || t == 0 || q_heads == 0) return MIXFP4_OK;
-  const int64_t grid = grid_of(cache), rows = 128 * row_tiles(cache, t, q_heads);
+  const int64_t grid = grid_of(cache), rows = 128 * groups_of(cache);
   *bytes = (grid * 16 + 255) / 256 * 256 + 2 * grid * rows * (8 + padded_dim(cache->head_dim) * 4);
   return MIXFP4_OK;
 }
@@ -1176,9 +1404,7 @@ int mixfp4_tree_attention(const void* q, int64_t q_stride, int64_t q_token_strid
   p.chunks = (int)((rows + 128 * tiles - 1) / (128 * tiles));
   p.together = together_of(cache);
   p.shares = grid / p.together;
-  // Rows of one tile are never cut.
-  const int64_t bound = window > 0 && window + t < p.max_tokens ? window + t + 15 : p.max_tokens;
-  p.joined = bound > tile_tokens(cache);
+  p.joined = p.max_tokens > tile_tokens(cache);  // rows of one tile are never cut
   p.page_shift = -1;
   for (int i = 0; i < 31; ++i)
     if (cache->page_size == 1 << i) p.page_shift = i;
@@ -1186,7 +1412,7 @@ int mixfp4_tree_attention(const void* q, int64_t q_stride, int64_t q_token_strid
   p.split = reinterpret_cast<int4*>(w);
   w += ((int64_t)grid * 16 + 255) / 256 * 256;
   p.stat = reinterpret_cast<float2*>(w);
-  p.part = reinterpret_cast<float4*>(w + 2 * (int64_t)grid * 128 * tiles * 8);
+  p.part = reinterpret_cast<float4*>(w + 2 * (int64_t)grid * 128 * groups_of(cache) * 8);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   if (status_word && cudaMemsetAsync(status_word, 0, 4, s) != cudaSuccess) return MIXFP4_ERR_CUDA;
   return cache->dtype == MIXFP4_CACHE_MIXFP4 ? launch_dim<true>(p, grid, tiles, s) : launch_dim<false>(p, grid, tiles, s);
