@@ -117,16 +117,32 @@ struct Cfg {
   static constexpr uint32_t kScoreCols = 2 * kTokens;      // of tensor memory, O behind them
 };
 
+// What of a sequence is looked at.
+struct Span {
+  int n, c, first;  // tokens, drafts, certain tokens
+  int from, end;    // tokens [from, end) may be seen; from is a tile's first
+  int low;          // tokens below are not
+};
+// A part of a row: tiles [tile, tile + tiles) of chunk `chunk` of key head `head` of sequence b, walked from the last on.
+struct Part {
+  Span s;
+  int b, row, head, chunk, tile, tiles;
+  bool first, last;
+  int64_t behind;  // the unit behind the row's last
+};
+
 struct Shared {
-  uint64_t full[8], empty[8], placed[4], used[4], s_full[2], p_full[2], o_done[2], q_full, end;
+  uint64_t full[8], empty[8], placed[4], used[4], s_full[2], p_full[2], o_done[2], told[2], heard[2], q_full, end;
   uint32_t tmem;
   int abort;
   int skip[2];
   int edge_b;
-  int64_t before, edge[2], scan[28];
+  int64_t before, edge[2], scan[20];
   uint32_t there[kThere][4];  // of a tile, which of its tokens there are
+  // The part that softmax is at and the next, read ahead by a warp of its own: which drafts each sees, how many.
+  Part part[2];
+  uint64_t bits[2][kMostDrafts];
   uint8_t depth[2][kMostDrafts];
-  float2 ml[256];
 };
 static_assert(sizeof(Shared) <= kMisc);
 
@@ -284,12 +300,6 @@ __device__ __forceinline__ void tmem_store(uint32_t taddr, const uint32_t* v) {
   }
 }
 
-// What of a sequence is looked at.
-struct Span {
-  int n, c, first;  // tokens, drafts, certain tokens
-  int from, end;    // tokens [from, end) may be seen; from is a tile's first
-  int low;          // tokens below are not
-};
 template <int kTokens>
 __device__ __forceinline__ Span span_of(const TreeArgs& p, int b) {
   Span s;
@@ -308,13 +318,6 @@ __device__ __forceinline__ int units_of(const Span& s) {
   return s.c > 0 && s.end > s.low ? kRowCost + (s.end - s.from + kTokens - 1) / kTokens : 0;
 }
 
-// A part of a row: tiles [tile, tile + tiles) of chunk `chunk` of key head `head` of sequence b, walked from the last on.
-struct Part {
-  Span s;
-  int b, row, head, chunk, tile, tiles;
-  bool first, last;
-  int64_t behind;  // the unit behind the row's last
-};
 // Every role walks a CTA's share in the same steps.
 template <int kTokens>
 struct Walk {
@@ -436,6 +439,10 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, 1) tree_attention
       mbar_init(smem_u32(&sh.p_full[i]), 4);
       mbar_init(smem_u32(&sh.o_done[i]), 1);
     }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(smem_u32(&sh.told[i]), 1);
+      mbar_init(smem_u32(&sh.heard[i]), C::kSoftmax);
+    }
     mbar_init(smem_u32(&sh.q_full), C::kSoftmax);
     mbar_init(smem_u32(&sh.end), 1);
     sh.abort = 0;
@@ -511,6 +518,11 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, 1) tree_attention
       *abort_flag = 1;
     }
   };
+  // The same for a whole warp, whose lanes agree on it.
+  auto waits = [&](uint64_t& bar, uint32_t parity, uint32_t bit) {
+    wait(bar, parity, bit);
+    dead = __any_sync(kAll, dead);
+  };
   const float kts = kFp4 ? *p.c.k_ts : 1.0f, vts = kFp4 ? *p.c.v_ts : 1.0f;
   Part w;
 
@@ -521,17 +533,20 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, 1) tree_attention
     const uint32_t lanes = tmem + ((uint32_t)qd * 32u << 16);
     const uint32_t o_col = lanes + C::kScoreCols + m * DT;
     uint32_t g = 0, turn = 0;  // tiles and parts before this one
-    while (walk.next(p, mate, w)) {
+    for (;;) {
+      // All warps of softmax have the same parts and so meet at the same barriers, also where a wait has run out.
+      if (!__all_sync(kAll, mbar_wait(smem_u32(&sh.told[turn & 1]), (turn >> 1) & 1, nullptr, kWaitLimitNs))) break;
+      w = sh.part[turn & 1];
+      if (w.tiles == 0) break;
       const int R = min(128 * MT, p.t * p.group - w.chunk * 128 * MT);
       const int copies = MT == 2 || R > 64 ? 1 : (R > 32 ? 2 : 4), own = 128 / copies, steps = 4 / copies;
       const int r = (MT == 2 ? m * 128 : 0) + tl % own, copy = tl / own, step0 = copy * steps;
       const int idx = w.chunk * 128 * MT + r, i = idx / p.group, h = w.head * p.group + idx - i * p.group;
       const bool held = r < R, valid = held && i < w.s.c;  // rows behind the drafts have a result too, of zeros
       const bool idle = (MT == 2 ? m * 128 : 0) + (copies == 1 ? qd * 32 : 0) >= R;
-      uint8_t* depth = sh.depth[turn & 1];
-      if (tid < kMostDrafts) depth[tid] = (uint8_t)(tid < w.s.c ? depth_of(bits_of(p, w.b, tid, w.s.c), tid) : 0);
-      uint64_t sees = valid ? bits_of(p, w.b, i, w.s.c) : 0;
-      const int place = w.s.first + (valid ? depth_of(sees, i) : 0);
+      const uint8_t* depth = sh.depth[turn & 1];
+      uint64_t sees = valid ? sh.bits[turn & 1][i] : 0;
+      const int place = w.s.first + (valid ? depth[i] : 0);
       const float slope = p.slopes && valid ? p.slopes[h] * -kLog2e : 0.0f;
 
       // ---- the row's queries, into the swizzled tile (of one tile of rows, each group every other piece)
@@ -539,30 +554,49 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, 1) tree_attention
       {
         const uint16_t* q = p.q + (int64_t)w.b * p.q_stride + (int64_t)i * p.q_token_stride + (int64_t)h * p.q_head_stride;
         float up = 1.0f;
+        constexpr int kBatch = 8;  // pieces asked for at once
         if (kFp4) {  // q times 2^(14 - exponent of the row's largest) as f16
           float top = 0.0f;
-          if (valid)
-            for (int d = 0; d < D; d += 8) {
-              const uint4 v = *reinterpret_cast<const uint4*>(q + d);
-              top = max3f(top, fabsf(bf_lo(v.x)), fabsf(bf_hi(v.x)));
-              top = max3f(top, fabsf(bf_lo(v.y)), fabsf(bf_hi(v.y)));
-              top = max3f(top, fabsf(bf_lo(v.z)), fabsf(bf_hi(v.z)));
-              top = max3f(top, fabsf(bf_lo(v.w)), fabsf(bf_hi(v.w)));
+#pragma unroll 1
+          for (int u0 = 0; u0 < D / 8; u0 += kBatch) {
+            uint4 v[kBatch];
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) {
+              v[k] = make_uint4(0, 0, 0, 0);
+              if (valid && u0 + k < D / 8) v[k] = *reinterpret_cast<const uint4*>(q + 8 * (u0 + k));
             }
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) {
+              top = max3f(top, fabsf(bf_lo(v[k].x)), fabsf(bf_hi(v[k].x)));
+              top = max3f(top, fabsf(bf_lo(v[k].y)), fabsf(bf_hi(v[k].y)));
+              top = max3f(top, fabsf(bf_lo(v[k].z)), fabsf(bf_hi(v[k].z)));
+              top = max3f(top, fabsf(bf_lo(v[k].w)), fabsf(bf_hi(v[k].w)));
+            }
+          }
           const int e = min(max((int)(__float_as_uint(top) >> 23), 15), 253);
           up = __uint_as_float((uint32_t)(268 - e) << 23);
           fs *= __uint_as_float((uint32_t)(e - 14) << 23);
         }
         const uint32_t at = q_smem + (MT == 2 ? m * (128 * DT * 2) : 0) + tl * 128;
-#pragma unroll 4
-        for (int u = C::kTurns ? m : 0; u < D / 8; u += C::kTurns ? 2 : 1) {
-          uint4 v = make_uint4(0, 0, 0, 0);
-          if (valid) v = *reinterpret_cast<const uint4*>(q + 8 * u);
-          if (kFp4) {
-            v.x = f16x2(bf_lo(v.x) * up, bf_hi(v.x) * up), v.y = f16x2(bf_lo(v.y) * up, bf_hi(v.y) * up);
-            v.z = f16x2(bf_lo(v.z) * up, bf_hi(v.z) * up), v.w = f16x2(bf_lo(v.w) * up, bf_hi(v.w) * up);
+        constexpr int kEvery = C::kTurns ? 2 : 1;
+#pragma unroll 1
+        for (int u0 = C::kTurns ? m : 0; u0 < D / 8; u0 += kBatch * kEvery) {
+          uint4 v[kBatch];
+#pragma unroll
+          for (int k = 0; k < kBatch; ++k) {
+            v[k] = make_uint4(0, 0, 0, 0);
+            if (valid && u0 + k * kEvery < D / 8) v[k] = *reinterpret_cast<const uint4*>(q + 8 * (u0 + k * kEvery));
           }
-          sts128(at + (u >> 3) * 16384 + (((u & 7) ^ (tl & 7)) << 4), v.x, v.y, v.z, v.w);
+#pragma unroll
+          for (int k = 0; k < kBatch; ++k) {
+            const int u = u0 + k * kEvery;
+            if (u >= D / 8) break;
+            if (kFp4) {
+              v[k].x = f16x2(bf_lo(v[k].x) * up, bf_hi(v[k].x) * up), v[k].y = f16x2(bf_lo(v[k].y) * up, bf_hi(v[k].y) * up);
+              v[k].z = f16x2(bf_lo(v[k].z) * up, bf_hi(v[k].z) * up), v[k].w = f16x2(bf_lo(v[k].w) * up, bf_hi(v[k].w) * up);
+            }
+            sts128(at + (u >> 3) * 16384 + (((u & 7) ^ (tl & 7)) << 4), v[k].x, v[k].y, v[k].z, v[k].w);
+          }
         }
       }
       const float cap2 = p.softcap * kLog2e;
@@ -570,7 +604,6 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, 1) tree_attention
       fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&sh.q_full));
-      bar_sync(1, C::kSoftmax * 32);  // the depths
       if (p.window > 0)
         for (int k = 0; k < w.s.c; ++k)
           if (place - w.s.first - depth[k] >= p.window) sees &= ~(1ull << k);
@@ -584,8 +617,7 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, 1) tree_attention
       const int64_t slot = (2 * (int64_t)blockIdx.x + (w.first ? 1 : 0)) * C::kGroups + m;
       float4* aside = p.part + slot * (DT / 4 * 128) + tl;
       auto o_ready = [&](uint32_t bit) {  // O of this group's tile before this one
-        wait(sh.o_done[m], (n - 1) & 1, bit);
-        __syncwarp();
+        waits(sh.o_done[m], (n - 1) & 1, bit);
         tc_fence_after();
       };
       auto set_aside = [&] {  // O joins what was set aside before, and begins at 0
@@ -618,8 +650,7 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, 1) tree_attention
         const uint32_t scores = lanes + buf * TN;
         const bool begins = done % kChain == 0;
         if (done > 0 && begins) set_aside();
-        wait(sh.s_full[buf], C::kGroups == 2 ? n & 1 : (tile >> 1) & 1, 2u);
-        __syncwarp();
+        waits(sh.s_full[buf], C::kGroups == 2 ? n & 1 : (tile >> 1) & 1, 2u);
         tc_fence_after();
         const int j0 = w.s.from + (w.tile + w.tiles - 1 - it) * TN;
         const uint32_t* there = sh.there[tile % kThere];
@@ -634,26 +665,26 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, 1) tree_attention
         const bool clear = !kFp4 && p.box && !whole && (C::kTurns || m == 0);
         if (uneven || clear) {
           const uint32_t q = 2 * tile + 1, place_v = q % C::kSlots, at = ring + place_v * C::kSlot + tl * 128;
-          wait(sh.full[place_v], (q / C::kSlots) & 1, 4u);
-          __syncwarp();
+          waits(sh.full[place_v], (q / C::kSlots) & 1, 4u);
           const bool mine = tl < TN, here = mine && (there[(tl & (TN - 1)) >> 5] >> (tl & 31)) & 1u;
           if (clear && mine && !here) {  // TMA brings whole boxes, with whatever lies between a page's tokens
 #pragma unroll 4
             for (int u = 0; u < D / 8; ++u) sts128(at + (u >> 3) * C::kBlock + (((u & 7) ^ (tl & 7)) << 4), 0, 0, 0, 0);
             fence_proxy_async_smem();
           }
-          if (uneven) {  // a NaN or an infinity in V?
+          if (uneven) {  // a NaN or an infinity in V, in a row that not all see?
             bool bad = false;
-            if (here) {
-              constexpr uint32_t kExp = kFp4 ? 0x7C00u : 0x7F80u;
-#pragma unroll 4
-              for (int u = 0; u < D / 8; ++u) {
-                const uint4 v = lds128(at + (u >> 3) * C::kBlock + (((u & 7) ^ (tl & 7)) << 4));
-                const uint32_t x[4] = {v.x, v.y, v.z, v.w};
+            constexpr uint32_t kExp = kFp4 ? 0x7C00u : 0x7F80u;
+            const int row0 = edge ? 0 : max(w.s.first - j0, 0), units = D / 8;
+#pragma unroll 2
+            for (int x = tl; x < (TN - row0) * units; x += 128) {
+              const int y = x / units, u = x - y * units, row = row0 + y;
+              const uint4 v = lds128(ring + place_v * C::kSlot + row * 128 + (u >> 3) * C::kBlock + (((u & 7) ^ (row & 7)) << 4));
+              const uint32_t z[4] = {v.x, v.y, v.z, v.w};
+              bool odd = false;
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                  bad = bad || (x[e] & kExp) == kExp || (x[e] & (kExp << 16)) == kExp << 16;
-              }
+              for (int e = 0; e < 4; ++e) odd = odd || (z[e] & kExp) == kExp || (z[e] & (kExp << 16)) == kExp << 16;
+              bad = bad || (odd && ((there[row >> 5] >> (row & 31)) & 1u));
             }
             slow = bar_or(2 + m, 128, bad);
           }
@@ -689,20 +720,34 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, 1) tree_attention
               top = fmaxf(top, top2);
             } else {
               const int a = j0 + s * CW;
-              const uint32_t seen = masked ? seen_of(s) : kAll;
+              auto shaped = [&](uint32_t y) {
+                const float x = __uint_as_float(y) * fs;
+                return p.softcap > 0.0f ? cap2 * tanh_of(x) : x;
+              };
+              if (!masked) {
+                const float far0 = (float)(place - a);
 #pragma unroll
-              for (int e = 0; e < CW; ++e) {
-                float x = __uint_as_float(v[e]) * fs;
-                if (p.softcap > 0.0f) x = cap2 * tanh_of(x);
-                if (p.slopes) {
-                  const int j = a + e;
-                  int far = place - j;
-                  if (j >= w.s.first) far = place - w.s.first - depth[min(j - w.s.first, kMostDrafts - 1)];
-                  x = fmaf(slope, (float)far, x);
+                for (int e = 0; e < CW; ++e) {
+                  float x = shaped(v[e]);
+                  if (p.slopes) x = fmaf(slope, far0 - (float)e, x);
+                  top = fmaxf(top, x);
+                  v[e] = __float_as_uint(x);
                 }
-                x = (seen >> e) & 1u ? x : -INFINITY;
-                top = fmaxf(top, x);
-                v[e] = __float_as_uint(x);
+              } else {
+                const uint32_t seen = seen_of(s);
+#pragma unroll
+                for (int e = 0; e < CW; ++e) {
+                  float x = shaped(v[e]);
+                  if (p.slopes) {
+                    const int j = a + e;
+                    int far = place - j;
+                    if (j >= w.s.first) far = place - w.s.first - depth[min(j - w.s.first, kMostDrafts - 1)];
+                    x = fmaf(slope, (float)far, x);
+                  }
+                  x = (seen >> e) & 1u ? x : -INFINITY;
+                  top = fmaxf(top, x);
+                  v[e] = __float_as_uint(x);
+                }
               }
               if (steps > 1 || slow) tmem_store<CW>(scores + s * CW, v);
             }
@@ -833,14 +878,17 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, 1) tree_attention
       const int many = copies * kTurners;
       float M = mx, L = l;
       if (many > 1) {
-        sh.ml[m * 128 + tl] = make_float2(mx, l);
+        float2* ml = reinterpret_cast<float2*>(smem);  // where the queries were, once no product reads them
         bar_sync(1, C::kSoftmax * 32);
-        for (int k = 0; k < many; ++k) M = fmaxf(M, sh.ml[tl % own + k * own].x);
+        ml[m * 128 + tl] = make_float2(mx, l);
+        bar_sync(1, C::kSoftmax * 32);
+        for (int k = 0; k < many; ++k) M = fmaxf(M, ml[tl % own + k * own].x);
         L = 0.0f;
         for (int k = 0; k < many; ++k) {
-          const float2 s = sh.ml[tl % own + k * own];
+          const float2 s = ml[tl % own + k * own];
           L += ex2(s.x - M) * s.y;
         }
+        bar_sync(1, C::kSoftmax * 32);
       }
       const float last = all ? out_factor<kFp4>(L, vts) : 1.0f, f = many > 1 ? ex2(mx - M) : 1.0f;
       // Columns [d, d + 4) of the row's sum, to their place.
@@ -852,45 +900,43 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, 1) tree_attention
         else
           part[(d / 4) * 128 + (MT == 2 ? tl : r)] = make_float4(x[0], x[1], x[2], x[3]);
       };
-      auto take = [&](int d, float* x) {  // 16 columns of O, with what was set aside
-        uint32_t v[16];
-        tmem_load<16>(o_col + d, v);
-        tmem_loaded<16>(v);
+      auto take = [&](int d, float* x) {  // 32 columns of O, with what was set aside
+        uint32_t v[32];
+        tmem_load<32>(o_col + d, v);
+        tmem_loaded<32>(v);
 #pragma unroll
-        for (int e = 0; e < 16; ++e) x[e] = __uint_as_float(v[e]);
+        for (int e = 0; e < 32; ++e) x[e] = __uint_as_float(v[e]);
         if (chained) {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
+          for (int e = 0; e < 8; ++e) {
+            if (d + 4 * e >= D) break;
             const float4 y = aside[(d / 4 + e) * 128];
             x[4 * e] = fmaf(old, y.x, x[4 * e]), x[4 * e + 1] = fmaf(old, y.y, x[4 * e + 1]);
             x[4 * e + 2] = fmaf(old, y.z, x[4 * e + 2]), x[4 * e + 3] = fmaf(old, y.w, x[4 * e + 3]);
           }
         }
 #pragma unroll
-        for (int e = 0; e < 16; ++e) x[e] = valid && done > 0 ? x[e] * f : 0.0f;
+        for (int e = 0; e < 32; ++e) x[e] = valid && done > 0 ? x[e] * f : 0.0f;
       };
       if (many == 1) {
         if (!idle)
 #pragma unroll 1
-          for (int d = 0; d < D; d += 16) {
-            float x[16];
+          for (int d = 0; d < D; d += 32) {
+            float x[32];
             take(d, x);
-            put(d, x);
-            put(d + 4, x + 4);
-            put(d + 8, x + 8);
-            put(d + 12, x + 12);
+#pragma unroll
+            for (int e = 0; e < 32; e += 4) put(d + e, x + e);
           }
       } else {
         float* stage = reinterpret_cast<float*>(smem);  // [group][32][128], where the queries were
         const int each = 32 / many, who = (kTurners == 2 ? m * copies : 0) + copy;
 #pragma unroll 1
         for (int d0 = 0; d0 < D; d0 += 32) {
-#pragma unroll 1
-          for (int d = 0; d < 32; d += 16) {
-            float x[16];
-            take(d0 + d, x);
+          {
+            float x[32];
+            take(d0, x);
 #pragma unroll
-            for (int e = 0; e < 16; ++e) stage[(m * 32 + d + e) * 128 + tl] = x[e];
+            for (int e = 0; e < 32; ++e) stage[(m * 32 + e) * 128 + tl] = x[e];
           }
           bar_sync(1, C::kSoftmax * 32);
 #pragma unroll 1
@@ -924,6 +970,7 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, 1) tree_attention
         p.split[blockIdx.x] = make_int4(w.b, w.row, share, (int)((w.behind * sh.scan[1] - 1) / sh.scan[0]));
       tc_fence_before();
       __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&sh.heard[turn & 1]));
       ++turn;
       g += w.tiles;
     }
@@ -995,6 +1042,39 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, 1) tree_attention
       mma_commit(smem_u32(&sh.end));
       mbar_wait(smem_u32(&sh.end), 0, nullptr, kWaitLimitNs);
     }
+  } else if (warp == C::kSoftmax + 3) {
+    // ================================================= reads a part ahead for softmax, and asks for its queries
+    uint32_t turn = 0;
+    for (bool more = true; more; ++turn) {
+      more = walk.next(p, mate, w);
+      uint64_t bits[2] = {0, 0};
+      if (more) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+          if (lane + 32 * k < w.s.c) bits[k] = bits_of(p, w.b, lane + 32 * k, w.s.c);
+        const int R = min(128 * MT, p.t * p.group - w.chunk * 128 * MT), lines = (D * 2 + 127) / 128;
+        for (int x = lane; x < R * lines; x += 32) {
+          const int r = x / lines, idx = w.chunk * 128 * MT + r, i = idx / p.group;
+          if (i < w.s.c)
+            asm volatile("prefetch.global.L2 [%0];" ::"l"(p.q + (int64_t)w.b * p.q_stride + (int64_t)i * p.q_token_stride +
+                                                          (int64_t)(w.head * p.group + idx - i * p.group) * p.q_head_stride +
+                                                          (x - r * lines) * 64));
+        }
+      }
+      waits(sh.heard[turn & 1], ((turn >> 1) & 1) ^ 1, 1u << 14);
+      if (dead) break;  // what softmax may still read stays
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        sh.bits[turn & 1][lane + 32 * k] = bits[k];
+        sh.depth[turn & 1][lane + 32 * k] = (uint8_t)depth_of(bits[k], lane + 32 * k);
+      }
+      if (lane == 0) {
+        if (!more) w.tiles = 0;
+        sh.part[turn & 1] = w;
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&sh.told[turn & 1]));
+    }
   } else if (!kFp4 && p.box && warp < C::kSoftmax + 3) {
     // ================================================= rows of a bf16 cache by TMA, boxes of one page, 64 dimensions
     // each: keys by one warp, values by another
@@ -1049,11 +1129,11 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, 1) tree_attention
   } else if (!kFp4) {
     // ================================================= or by cp.async, row by row, by two warps
     if constexpr (!kFp4) {
-      const int pw = warp - C::kSoftmax - 2;
+      const int pw = warp - C::kSoftmax - 1;
       constexpr int kRows = C::kRows, kPieces = DT / 8, kRowsAtOnce = 32 / kPieces;
       const int piece = lane % kPieces, r0 = lane / kPieces;
       uint32_t g = 0, q = 0;
-      while (!p.box && pw >= 0 && walk.next(p, mate, w)) {
+      while (walk.next(p, mate, w)) {
         const int32_t* table = p.table + (int64_t)w.b * p.table_stride;
 #pragma unroll 1
         for (int it = 0; it < w.tiles; ++it, ++g) {
@@ -1076,8 +1156,7 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, 1) tree_attention
           for (int kv = 0; kv < 2; ++kv, ++q) {
             const uint8_t* base = static_cast<const uint8_t*>(kv ? p.c.v : p.c.k);
             const uint32_t slot = q % C::kSlots;
-            wait(sh.empty[slot], ((q / C::kSlots) & 1) ^ 1, 1024u);
-            __syncwarp();
+            waits(sh.empty[slot], ((q / C::kSlots) & 1) ^ 1, 1024u);
             const uint32_t dst = ring + slot * C::kSlot + (piece >> 3) * C::kBlock + pw * kRows * 128;
 #pragma unroll
             for (int j = 0; j < kRows / 32; ++j)
@@ -1095,14 +1174,14 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, 1) tree_attention
       cp_async_wait_all();
     }
   } else if (warp < C::kSoftmax + 4) {
-    // ================================================= helpers: where a MixFP4 tile's rows lie, a third of the tiles each
+    // ================================================= helpers: where a MixFP4 tile's rows lie, every other tile each
     if constexpr (kFp4) {
-      const int me = warp - C::kSoftmax - 1;
+      const int me = warp - C::kSoftmax - 1;  // of two
       uint32_t g = 0;
       while (walk.next(p, mate, w)) {
         const int32_t* table = p.table + (int64_t)w.b * p.table_stride;
         for (int it = 0; it < w.tiles; ++it, ++g) {
-          if ((int)(g % 3) != me) continue;
+          if ((int)(g & 1) != me) continue;
           const uint32_t at = places + (g % C::kAddresses) * (TN * 16);
           const int tok0 = w.s.from + (w.tile + w.tiles - 1 - it) * TN + lane;
           int page[TN / 32];
@@ -1113,8 +1192,7 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, 1) tree_attention
             if (tok >= w.s.low && tok < w.s.end)
               page[j] = table[p.page_shift >= 0 ? tok >> p.page_shift : tok / p.c.page_size];
           }
-          wait(sh.used[g % C::kAddresses], ((g / C::kAddresses) & 1) ^ 1, 2048u);
-          __syncwarp();
+          waits(sh.used[g % C::kAddresses], ((g / C::kAddresses) & 1) ^ 1, 2048u);
 #pragma unroll
           for (int j = 0; j < TN / 32; ++j) {
             const int tok = tok0 + 32 * j;
@@ -1148,8 +1226,7 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, 1) tree_attention
       cp_wait_at_most(later);
       __syncwarp();
       const uint32_t slot = sent % C::kSlots;
-      wait(sh.empty[slot], ((sent / C::kSlots) & 1) ^ 1, 1024u);
-      __syncwarp();
+      waits(sh.empty[slot], ((sent / C::kSlots) & 1) ^ 1, 1024u);
       if (piece * 16 < D)
         decode_rows<C, L, kSteps>(ring + slot * C::kSlot + pw * kRows * 128, raw0 + (sent % C::kRawDepth) * C::kRawSlot,
                                   piece, r0, C::kRows >= 8 ? 0 : pw * kRows);
@@ -1161,8 +1238,7 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, 1) tree_attention
     while (walk.next(p, mate, w)) {
 #pragma unroll 1
       for (int it = 0; it < w.tiles; ++it, ++g) {
-        wait(sh.placed[g % C::kAddresses], (g / C::kAddresses) & 1, 4096u);
-        __syncwarp();
+        waits(sh.placed[g % C::kAddresses], (g / C::kAddresses) & 1, 4096u);
         const uint32_t at = places + (g % C::kAddresses) * (TN * 16) + pw * kRows * 16;
         int64_t from[kSteps];
 #pragma unroll
