@@ -45,9 +45,9 @@ constexpr int kJoinThreads = 256;
 constexpr uint64_t kWaitLimitNs = 1000000000ull;
 // What beginning a row costs (its queries, the way to its first pages, its end), in tiles.
 constexpr int kRowCost = 2;
-// Tiles after which O is set aside and begins at 0: the tensor cores round a chain of sums towards zero, some 2^-25 of
-// the sum a link, and 64 tiles of 128 tokens are 512 links (1024 with two parts of the weights).
-constexpr int kChain = 64;
+// Tokens after which O is set aside and begins at 0: the tensor cores round a chain of sums towards zero, some 2^-25 of
+// the sum a link, and 8192 tokens are 512 links (1024 with two parts of the weights).
+constexpr int kChainTokens = 8192;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // How far a score may lie above the m of its weight 2^(s - m).  On a MixFP4 cache the weights are 2^7 times that:
 // at most 2^15 in f16, whose least value is then 2^-31 of the weight at m.
@@ -55,7 +55,7 @@ constexpr float kSlack = 8.0f, kFp4Exp = 7.0f;
 constexpr float kNoScore = -3e38f;  // m where no token has been seen: no difference to a score or to itself is NaN
 constexpr float kMostScore = 3.402823466e38f;  // m of a score of +inf, whose weight is then +inf instead of NaN
 constexpr unsigned kAll = 0xFFFFFFFFu;
-constexpr int kMisc = 3072;  // bytes of shared memory beside the tiles
+constexpr int kMostSlots = 12;
 constexpr int kThere = 16;   // tiles whose tokens are known at a time
 
 struct TreeArgs {
@@ -80,41 +80,10 @@ struct TreeArgs {
   uint16_t* out;
   float* lse;
   int4* split;   // [grid]: the row that a CTA begins and others end: (sequence, row, first share, last); x < 0: none
-  float2* stat;  // [2 grid][groups][128] (m, l) of parts
-  float4* part;  // [2 grid][groups][dimensions / 4][128]: O of parts, and what a row in work has set aside
+  float2* stat;  // [2 grid][row tiles][128] (m, l) of parts
+  float4* part;  // [2 grid][row tiles][dimensions / 4][128]: O of parts, and what a row in work has set aside
   uint32_t* status;
   int box;  // rows of a bf16 page that one TMA copy brings; 0: cp.async does
-};
-
-template <int DT, int MT, bool kFp4>
-struct Cfg {
-  static constexpr int kTokens = DT == 256 ? 64 : 128;     // of a tile
-  static constexpr int kCw = kTokens / 4;                  // and of its quarter, a thread's step
-  static constexpr int kBlock = kTokens * 128;             // 64 dimensions of a tile
-  static constexpr int kSlot = kBlock * (DT / 64);
-  // Groups of four softmax warps: one to each of two tiles of rows; or two that take turns at the tiles of tokens, each with
-  // an O of its own, which tensor memory holds beside both S up to 128 dimensions.
-  static constexpr int kGroups = DT == 256 ? 1 : 2;
-  static constexpr bool kTurns = MT == 1 && kGroups == 2;
-  static constexpr int kQ = MT * 128 * DT * 2 > kGroups * 16384 ? MT * 128 * DT * 2 : kGroups * 16384;
-  static constexpr int kSoftmax = 4 * kGroups;             // warps
-  static constexpr int kProducers = kFp4 ? 8 : 2;          // of a bf16 cache where TMA cannot bring its rows
-  static constexpr int kThreads = (kSoftmax + 4 + (kFp4 ? kProducers : 0)) * 32;  // the four: products, TMA or helpers
-  // Registers of a thread at launch, then of softmax and of the other threads (together no more than at launch).
-  static constexpr int kRegs = 65536 / kThreads / 8 * 8;
-  static constexpr int kOtherRegs = kFp4 ? 72 : 168;
-  static constexpr int kLeft = (kRegs * kThreads - kOtherRegs * (kThreads - kSoftmax * 32)) / (kSoftmax * 32) / 8 * 8;
-  static constexpr int kSoftRegs = kLeft < 232 ? kLeft : 232;
-  static constexpr int kRows = kTokens / kProducers;       // of a tile, to a producer warp
-  static constexpr int kRawSlot = kRows * (DT / 2 + 16);   // MixFP4 rows as they lie: codes, then scale bytes
-  static constexpr int kRawDepth = kFp4 ? 5 : 0;
-  static constexpr int kRaw = kProducers * kRawDepth * kRawSlot;
-  static constexpr int kAddresses = kFp4 ? 4 : 0;          // tiles whose rows' places are known
-  static constexpr int kPlaces = kAddresses * kTokens * 16;
-  static constexpr int kFit = (227 * 1024 - kMisc - kQ - kRaw - kPlaces) / kSlot;
-  static constexpr int kSlots = kFit < 8 ? kFit : 8;
-  static constexpr int kSmem = kQ + kSlots * kSlot + kRaw + kPlaces + kMisc;
-  static constexpr uint32_t kScoreCols = 2 * kTokens;      // of tensor memory, O behind them
 };
 
 // What of a sequence is looked at.
@@ -131,20 +100,65 @@ struct Part {
   int64_t behind;  // the unit behind the row's last
 };
 
+template <int kSlots, int kAddresses, int kWords>
 struct Shared {
-  uint64_t full[8], empty[8], placed[4], used[4], s_full[2], p_full[2], o_done[2], told[2], heard[2], q_full, end;
+  uint64_t full[kSlots], empty[kSlots], placed[kAddresses], used[kAddresses];
+  // Of a buffer of scores: they are there, their weights are, O has taken those up.  No buffer has two uses under way, so
+  // the parity of a wait tells one use from the next.
+  uint64_t s_full[2], p_full[2], o_done[2];
+  uint64_t told, heard, q_full, end;
   uint32_t tmem;
   int abort;
   int skip[2];
+  int64_t all, shares, before, edge[2];
   int edge_b;
-  int64_t before, edge[2], scan[20];
-  uint32_t there[kThere][4];  // of a tile, which of its tokens there are
-  // The part that softmax is at and the next, read ahead by a warp of its own: which drafts each sees, how many.
-  Part part[2];
-  uint64_t bits[2][kMostDrafts];
-  uint8_t depth[2][kMostDrafts];
+  uint32_t there[kThere][kWords];  // of a tile, which of its tokens there are
+  // The part that softmax is at, read ahead by a warp of its own: which drafts each draft sees, and how many.
+  uint8_t depth[kMostDrafts];
+  Part part;
+  union {
+    uint64_t bits[kMostDrafts];
+    int64_t scan[32];  // of the shares, before the first part
+  };
 };
-static_assert(sizeof(Shared) <= kMisc);
+
+template <int DT, int MT, bool kFp4>
+struct Cfg {
+  // With one tile of rows two CTAs share an SM: what one does once a row (its queries, its end) the other's tiles cover.
+  // A MixFP4 cache's decoding takes the registers and the larger tiles of one.
+  static constexpr int kCtas = !kFp4 && MT == 1 && DT <= 128 ? 2 : 1;
+  static constexpr int kTokens = DT <= 128 && (MT == 2 || kFp4) ? 128 : 64;  // of a tile
+  static constexpr int kChain = kChainTokens / kTokens;    // tiles to a chain of sums
+  static constexpr int kCw = kTokens / 4;                  // and of its quarter, a thread's step
+  static constexpr int kBlock = kTokens * 128;             // 64 dimensions of a tile
+  static constexpr int kSlot = kBlock * (DT / 64);
+  static constexpr int kSoftmax = 4 * MT;                  // warps, four to a tile of rows
+  static constexpr int kQ = MT * 128 * DT * 2;
+  static constexpr int kProducers = kFp4 ? (MT == 1 ? 16 : 8) : 2;  // of a bf16 cache where TMA cannot bring its rows
+  static constexpr int kThreads = (kSoftmax + 4 + (kFp4 ? kProducers : 0)) * 32;  // the four: products, TMA or helpers
+  // Registers of a thread at launch, then of softmax and of the other threads (together no more than at launch).
+  static constexpr int kRegs = 65536 / (kThreads * kCtas) / 8 * 8;
+  static constexpr int kOtherRegs = kFp4 ? (MT == 1 ? 64 : 72) : kRegs;
+  static constexpr int kLeft = (kRegs * kThreads - kOtherRegs * (kThreads - kSoftmax * 32)) / (kSoftmax * 32) / 8 * 8;
+  static constexpr int kSoftRegs = kLeft < 232 ? kLeft : 232;
+  static constexpr int kRows = kTokens / kProducers;       // of a tile, to a producer warp
+  static constexpr int kRawSlot = kRows * (DT / 2 + 16);   // MixFP4 rows as they lie: codes, then scale bytes
+  static constexpr int kRawDepth = kFp4 ? 5 : 0;
+  static constexpr int kRaw = kProducers * kRawDepth * kRawSlot;
+  static constexpr int kAddresses = kFp4 ? 4 : 0;          // tiles whose rows' places are known
+  static constexpr int kPlaces = kAddresses * kTokens * 16;
+  static constexpr int kWords = kTokens / 32;
+  static constexpr int kRoom = (kCtas == 2 ? 113 : 227) * 1024 - kQ - kRaw - kPlaces;
+  static constexpr int slots(int n) {  // as many as there is room for
+    return n == 1 || n * (kSlot + 16) + (int)sizeof(Shared<1, kFp4 ? 4 : 1, kWords>) <= kRoom ? n : slots(n - 1);
+  }
+  static constexpr int kSlots = slots(kMostSlots);
+  using Sh = Shared<kSlots, kFp4 ? 4 : 1, kWords>;
+  static constexpr int kSmem = kQ + kSlots * kSlot + kRaw + kPlaces + (int)sizeof(Sh);
+  static_assert(kSlots >= 3 && sizeof(Sh) % 8 == 0 && kSmem <= (kCtas == 2 ? 113 : 227) * 1024);
+  static constexpr uint32_t kScoreCols = 2 * kTokens;      // of tensor memory, O behind them
+  static constexpr uint32_t kCols = kCtas == 2 ? 256 : 512;
+};
 
 template <int kBytes>
 __device__ __forceinline__ void cp_async(uint32_t dst, const void* src, bool take) {
@@ -408,12 +422,12 @@ __device__ __forceinline__ void decode_rows(uint32_t to, uint32_t raw, int piece
 }
 
 template <int DT, int MT, bool kFp4>
-__global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, 1) tree_attention_kernel(const TreeArgs p, const __grid_constant__ CUtensorMap tm_k,
+__global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>::kCtas) tree_attention_kernel(const TreeArgs p, const __grid_constant__ CUtensorMap tm_k,
                       const __grid_constant__ CUtensorMap tm_v) {
   using C = Cfg<DT, MT, kFp4>;
   constexpr int TN = C::kTokens, CW = C::kCw;
   extern __shared__ __align__(1024) uint8_t smem[];
-  Shared& sh = *reinterpret_cast<Shared*>(smem + C::kQ + C::kSlots * C::kSlot + C::kRaw + C::kPlaces);
+  auto& sh = *reinterpret_cast<typename C::Sh*>(smem + C::kQ + C::kSlots * C::kSlot + C::kRaw + C::kPlaces);
   const uint32_t q_smem = smem_u32(smem), ring = q_smem + C::kQ;
   [[maybe_unused]] const uint32_t places = ring + C::kSlots * C::kSlot + C::kRaw;  // [kAddresses][tokens] (row, scales)
   volatile int* abort_flag = &sh.abort;
@@ -423,7 +437,7 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, 1) tree_attention
   griddep_launch_dependents();
 
   if (warp == C::kSoftmax) {
-    tmem_alloc(smem_u32(&sh.tmem), 512);
+    tmem_alloc(smem_u32(&sh.tmem), C::kCols);
     tmem_relinquish();
   } else if (tid == 0) {
     for (int i = 0; i < C::kSlots; ++i) {
@@ -439,10 +453,8 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, 1) tree_attention
       mbar_init(smem_u32(&sh.p_full[i]), 4);
       mbar_init(smem_u32(&sh.o_done[i]), 1);
     }
-    for (int i = 0; i < 2; ++i) {
-      mbar_init(smem_u32(&sh.told[i]), 1);
-      mbar_init(smem_u32(&sh.heard[i]), C::kSoftmax);
-    }
+    mbar_init(smem_u32(&sh.told), 1);
+    mbar_init(smem_u32(&sh.heard), C::kSoftmax);
     mbar_init(smem_u32(&sh.q_full), C::kSoftmax);
     mbar_init(smem_u32(&sh.end), 1);
     sh.abort = 0;
@@ -507,7 +519,7 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, 1) tree_attention
     __syncthreads();
     if (share < shares) walk.pos = sh.edge[0], walk.end = sh.edge[1], walk.b = sh.edge_b, walk.base = sh.before * rows;
     // Last share of the row that ends before unit x (see `split`).
-    if (tid == 0) sh.scan[0] = all, sh.scan[1] = shares;
+    if (tid == 0) sh.all = all, sh.shares = shares;
   }
   const uint32_t tmem = sh.tmem;
   bool dead = false;  // a wait has run out: no more waits and no more results, but every step, so that all warps meet
@@ -535,21 +547,21 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, 1) tree_attention
     uint32_t g = 0, turn = 0;  // tiles and parts before this one
     for (;;) {
       // All warps of softmax have the same parts and so meet at the same barriers, also where a wait has run out.
-      if (!__all_sync(kAll, mbar_wait(smem_u32(&sh.told[turn & 1]), (turn >> 1) & 1, nullptr, kWaitLimitNs))) break;
-      w = sh.part[turn & 1];
+      if (!__all_sync(kAll, mbar_wait(smem_u32(&sh.told), turn & 1, nullptr, kWaitLimitNs))) break;
+      w = sh.part;
       if (w.tiles == 0) break;
       const int R = min(128 * MT, p.t * p.group - w.chunk * 128 * MT);
       const int copies = MT == 2 || R > 64 ? 1 : (R > 32 ? 2 : 4), own = 128 / copies, steps = 4 / copies;
-      const int r = (MT == 2 ? m * 128 : 0) + tl % own, copy = tl / own, step0 = copy * steps;
+      const int r = m * 128 + tl % own, copy = tl / own, step0 = copy * steps;
       const int idx = w.chunk * 128 * MT + r, i = idx / p.group, h = w.head * p.group + idx - i * p.group;
       const bool held = r < R, valid = held && i < w.s.c;  // rows behind the drafts have a result too, of zeros
-      const bool idle = (MT == 2 ? m * 128 : 0) + (copies == 1 ? qd * 32 : 0) >= R;
-      const uint8_t* depth = sh.depth[turn & 1];
-      uint64_t sees = valid ? sh.bits[turn & 1][i] : 0;
+      const bool idle = m * 128 + (copies == 1 ? qd * 32 : 0) >= R;
+      const uint8_t* depth = sh.depth;
+      uint64_t sees = valid ? sh.bits[i] : 0;
       const int place = w.s.first + (valid ? depth[i] : 0);
       const float slope = p.slopes && valid ? p.slopes[h] * -kLog2e : 0.0f;
 
-      // ---- the row's queries, into the swizzled tile (of one tile of rows, each group every other piece)
+      // ---- the row's queries, into the swizzled tile
       float fs = p.scale * (kFp4 ? 0.5f * kts : 1.0f);
       {
         const uint16_t* q = p.q + (int64_t)w.b * p.q_stride + (int64_t)i * p.q_token_stride + (int64_t)h * p.q_head_stride;
@@ -577,19 +589,18 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, 1) tree_attention
           up = __uint_as_float((uint32_t)(268 - e) << 23);
           fs *= __uint_as_float((uint32_t)(e - 14) << 23);
         }
-        const uint32_t at = q_smem + (MT == 2 ? m * (128 * DT * 2) : 0) + tl * 128;
-        constexpr int kEvery = C::kTurns ? 2 : 1;
+        const uint32_t at = q_smem + m * (128 * DT * 2) + tl * 128;
 #pragma unroll 1
-        for (int u0 = C::kTurns ? m : 0; u0 < D / 8; u0 += kBatch * kEvery) {
+        for (int u0 = 0; u0 < D / 8; u0 += kBatch) {
           uint4 v[kBatch];
 #pragma unroll
           for (int k = 0; k < kBatch; ++k) {
             v[k] = make_uint4(0, 0, 0, 0);
-            if (valid && u0 + k * kEvery < D / 8) v[k] = *reinterpret_cast<const uint4*>(q + 8 * (u0 + k * kEvery));
+            if (valid && u0 + k < D / 8) v[k] = *reinterpret_cast<const uint4*>(q + 8 * (u0 + k));
           }
 #pragma unroll
           for (int k = 0; k < kBatch; ++k) {
-            const int u = u0 + k * kEvery;
+            const int u = u0 + k;
             if (u >= D / 8) break;
             if (kFp4) {
               v[k].x = f16x2(bf_lo(v[k].x) * up, bf_hi(v[k].x) * up), v[k].y = f16x2(bf_lo(v[k].y) * up, bf_hi(v[k].y) * up);
@@ -612,12 +623,10 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, 1) tree_attention
 
       float mx = kNoScore, l = 0.0f, m_aside = kNoScore;  // mx: the m of the weights
       bool chained = false;
-      uint32_t n = C::kTurns ? (g + 1 - m) >> 1 : g;  // tiles of this group before this one
-      int done = 0;                                   // and of this part
-      const int64_t slot = (2 * (int64_t)blockIdx.x + (w.first ? 1 : 0)) * C::kGroups + m;
+      const int64_t slot = (2 * (int64_t)blockIdx.x + (w.first ? 1 : 0)) * MT + m;
       float4* aside = p.part + slot * (DT / 4 * 128) + tl;
-      auto o_ready = [&](uint32_t bit) {  // O of this group's tile before this one
-        waits(sh.o_done[m], (n - 1) & 1, bit);
+      auto o_ready = [&](uint32_t bit) {  // O of the tile before this one
+        waits(sh.o_done[MT == 2 ? m : (g - 1) & 1], (MT == 2 ? g - 1 : (g - 1) >> 1) & 1, bit);
         tc_fence_after();
       };
       auto set_aside = [&] {  // O joins what was set aside before, and begins at 0
@@ -644,27 +653,27 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, 1) tree_attention
         m_aside = mx;
       };
 
-      for (int it = C::kTurns ? (int)((g + m) & 1) : 0; it < w.tiles; it += C::kTurns ? 2 : 1, ++n, ++done) {
-        const uint32_t tile = g + it;
-        const int buf = C::kGroups == 2 ? m : (int)(tile & 1);
+      for (int it = 0; it < w.tiles; ++it, ++g) {
+        const int buf = MT == 2 ? m : (int)(g & 1);
         const uint32_t scores = lanes + buf * TN;
-        const bool begins = done % kChain == 0;
-        if (done > 0 && begins) set_aside();
-        waits(sh.s_full[buf], C::kGroups == 2 ? n & 1 : (tile >> 1) & 1, 2u);
+        const bool begins = it % C::kChain == 0;
+        if (it > 0 && begins) set_aside();
+        waits(sh.s_full[buf], MT == 2 ? g & 1 : (g >> 1) & 1, 2u);
         tc_fence_after();
         const int j0 = w.s.from + (w.tile + w.tiles - 1 - it) * TN;
-        const uint32_t* there = sh.there[tile % kThere];
-        bool whole = there[0] == kAll && there[1] == kAll;
-        if (TN == 128) whole = whole && there[2] == kAll && there[3] == kAll;
+        const uint32_t* there = sh.there[g % kThere];
+        bool whole = true;
+#pragma unroll
+        for (int k = 0; k < C::kWords; ++k) whole = whole && there[k] == kAll;
         const bool edge = p.window > 0 && j0 < w.s.first + w.s.c - p.window;  // some rows' windows begin behind j0
         const bool uneven = w.s.c > 1 && (edge || j0 + TN > w.s.first);       // rows may see different tokens
         const bool masked = !whole || edge || j0 + TN > w.s.first;
         const bool general = masked || !plain;
 
         bool slow = false;
-        const bool clear = !kFp4 && p.box && !whole && (C::kTurns || m == 0);
+        const bool clear = !kFp4 && p.box && !whole && m == 0;
         if (uneven || clear) {
-          const uint32_t q = 2 * tile + 1, place_v = q % C::kSlots, at = ring + place_v * C::kSlot + tl * 128;
+          const uint32_t q = 2 * g + 1, place_v = q % C::kSlots, at = ring + place_v * C::kSlot + tl * 128;
           waits(sh.full[place_v], (q / C::kSlots) & 1, 4u);
           const bool mine = tl < TN, here = mine && (there[(tl & (TN - 1)) >> 5] >> (tl & 31)) & 1u;
           if (clear && mine && !here) {  // TMA brings whole boxes, with whatever lies between a page's tokens
@@ -815,7 +824,7 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, 1) tree_attention
             l += s0 + s1;
           } else {
             // Products of what the row sees alone.
-            const uint32_t v_smem = ring + (2 * tile + 1) % C::kSlots * C::kSlot;
+            const uint32_t v_smem = ring + (2 * g + 1) % C::kSlots * C::kSlot;
             if (!begins) o_ready(16u);
             float sum = 0.0f;
 #pragma unroll 1
@@ -866,31 +875,29 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, 1) tree_attention
         if (lane == 0) mbar_arrive(smem_u32(&sh.p_full[buf]));
       }
 
-      // ---- the part's end: O, m and l of every row, finished where the part is the whole row.  Copies of a row, and the
-      // two groups that took turns, are added up in shared memory.
-      if (done > 0) o_ready(32u);
+      // ---- the part's end: O, m and l of every row, finished where the part is the whole row.  Copies of a row are added
+      // up in shared memory.
+      o_ready(32u);
       const bool all = w.first && w.last;
-      float4* part = p.part + (slot - (C::kTurns ? m : 0)) * (DT / 4 * 128);
+      float4* part = p.part + slot * (DT / 4 * 128);
       const int64_t at = ((int64_t)w.b * p.t + i) * p.q_heads + h;  // of the results
       const float old = chained ? ex2(m_aside - mx) : 0.0f;
       if (!valid) mx = kNoScore, l = 0.0f;
-      constexpr int kTurners = C::kTurns ? 2 : 1;
-      const int many = copies * kTurners;
       float M = mx, L = l;
-      if (many > 1) {
-        float2* ml = reinterpret_cast<float2*>(smem);  // where the queries were, once no product reads them
-        bar_sync(1, C::kSoftmax * 32);
-        ml[m * 128 + tl] = make_float2(mx, l);
-        bar_sync(1, C::kSoftmax * 32);
-        for (int k = 0; k < many; ++k) M = fmaxf(M, ml[tl % own + k * own].x);
+      if (copies > 1) {  // of one tile of rows
+        float2* ml = reinterpret_cast<float2*>(smem);  // where the queries were: no product reads them any more
+        bar_sync(1, 128);
+        ml[tl] = make_float2(mx, l);
+        bar_sync(1, 128);
+        for (int k = 0; k < copies; ++k) M = fmaxf(M, ml[tl % own + k * own].x);
         L = 0.0f;
-        for (int k = 0; k < many; ++k) {
+        for (int k = 0; k < copies; ++k) {
           const float2 s = ml[tl % own + k * own];
           L += ex2(s.x - M) * s.y;
         }
-        bar_sync(1, C::kSoftmax * 32);
+        bar_sync(1, 128);
       }
-      const float last = all ? out_factor<kFp4>(L, vts) : 1.0f, f = many > 1 ? ex2(mx - M) : 1.0f;
+      const float last = all ? out_factor<kFp4>(L, vts) : 1.0f, f = copies > 1 ? ex2(mx - M) : 1.0f;
       // Columns [d, d + 4) of the row's sum, to their place.
       auto put = [&](int d, const float* x) {
         if (!held || dead || d >= D) return;
@@ -898,7 +905,7 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, 1) tree_attention
           *reinterpret_cast<uint2*>(p.out + at * D + d) =
               make_uint2(bf16x2(x[0] * last, x[1] * last), bf16x2(x[2] * last, x[3] * last));
         else
-          part[(d / 4) * 128 + (MT == 2 ? tl : r)] = make_float4(x[0], x[1], x[2], x[3]);
+          part[(d / 4) * 128 + tl % own] = make_float4(x[0], x[1], x[2], x[3]);
       };
       auto take = [&](int d, float* x) {  // 32 columns of O, with what was set aside
         uint32_t v[32];
@@ -916,9 +923,9 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, 1) tree_attention
           }
         }
 #pragma unroll
-        for (int e = 0; e < 32; ++e) x[e] = valid && done > 0 ? x[e] * f : 0.0f;
+        for (int e = 0; e < 32; ++e) x[e] = valid ? x[e] * f : 0.0f;
       };
-      if (many == 1) {
+      if (copies == 1) {
         if (!idle)
 #pragma unroll 1
           for (int d = 0; d < D; d += 32) {
@@ -928,51 +935,43 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, 1) tree_attention
             for (int e = 0; e < 32; e += 4) put(d + e, x + e);
           }
       } else {
-        float* stage = reinterpret_cast<float*>(smem);  // [group][32][128], where the queries were
-        const int each = 32 / many, who = (kTurners == 2 ? m * copies : 0) + copy;
+        float* stage = reinterpret_cast<float*>(smem);  // [32][128]
+        const int each = 32 / copies;
 #pragma unroll 1
         for (int d0 = 0; d0 < D; d0 += 32) {
           {
             float x[32];
             take(d0, x);
 #pragma unroll
-            for (int e = 0; e < 32; ++e) stage[(m * 32 + e) * 128 + tl] = x[e];
+            for (int e = 0; e < 32; ++e) stage[e * 128 + tl] = x[e];
           }
-          bar_sync(1, C::kSoftmax * 32);
+          bar_sync(1, 128);
 #pragma unroll 1
-          for (int d = who * each; d < (who + 1) * each; d += 4) {
+          for (int d = copy * each; d < (copy + 1) * each; d += 4) {
             float x[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               const float* s = stage + (d + e) * 128 + tl % own;
-              x[e] = 0.0f;
-#pragma unroll
-              for (int k = 0; k < kTurners; ++k) {
-                const float* t = s + k * (32 * 128);
-                float y = t[0];
-                if (copies > 1) y += t[own];
-                if (copies == 4) y += t[2 * own] + t[3 * own];
-                x[e] += y;
-              }
+              x[e] = s[0] + s[own];
+              if (copies == 4) x[e] += s[2 * own] + s[3 * own];
             }
             put(d0 + d, x);
           }
-          bar_sync(1, C::kSoftmax * 32);
+          bar_sync(1, 128);
         }
       }
-      if (held && copy == 0 && !dead && (!C::kTurns || m == 0)) {
+      if (held && copy == 0 && !dead) {
         if (!all)
-          p.stat[(slot - (C::kTurns ? m : 0)) * 128 + tl] = make_float2(M, L);
+          p.stat[slot * 128 + tl] = make_float2(M, L);
         else if (p.lse)
           p.lse[at] = lse_of<kFp4>(M, L);
       }
       if (tid == 0 && w.first && !w.last)
-        p.split[blockIdx.x] = make_int4(w.b, w.row, share, (int)((w.behind * sh.scan[1] - 1) / sh.scan[0]));
+        p.split[blockIdx.x] = make_int4(w.b, w.row, share, (int)((w.behind * sh.shares - 1) / sh.all));
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&sh.heard[turn & 1]));
+      if (lane == 0) mbar_arrive(smem_u32(&sh.heard));
       ++turn;
-      g += w.tiles;
     }
   } else {
     if constexpr (C::kSoftRegs > C::kRegs) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kOtherRegs));
@@ -1005,37 +1004,60 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, 1) tree_attention
         const int R = min(128 * MT, p.t * p.group - w.chunk * 128 * MT);
         const int copies = MT == 2 || R > 64 ? 1 : (R > 32 ? 2 : 4);
         tc_fence_after();
-        for (int m = 0; m < MT; ++m) scores(g, m);
-        for (int it = 0; it < w.tiles; ++it, ++g) {
-          if (MT == 1 && it + 1 < w.tiles) scores(g + 1, 0);
+        const int tiles = w.tiles;
+        // O_m += P V of tile g.
+        auto weigh = [&](int it, int m) {
           const uint32_t q = 2 * g + 1, slot = q % C::kSlots, v = ring + slot * C::kSlot;
-          for (int m = 0; m < MT; ++m) {
-            const int buf = MT == 2 ? m : (int)(g & 1);
-            const int acc = C::kGroups == 2 ? buf : 0;                     // whose O
-            const bool begins = (C::kTurns ? it >> 1 : it) % kChain == 0;  // it is at 0
-            if (m == 0) {
-              wait(sh.full[slot], (q / C::kSlots) & 1, 256u);
-              if (!kFp4 && !p.box) fence_proxy_async_smem();
-            }
-            wait(sh.p_full[buf], MT == 2 ? g & 1 : (g >> 1) & 1, 512u);
-            tc_fence_after();
-            if (!*reinterpret_cast<volatile int*>(&sh.skip[buf])) {
+          const int buf = MT == 2 ? m : (int)(g & 1);
+          const bool begins = it % C::kChain == 0;  // O is at 0
+          if (m == 0) {
+            wait(sh.full[slot], (q / C::kSlots) & 1, 256u);
+            if (!kFp4 && !p.box) fence_proxy_async_smem();
+          }
+          wait(sh.p_full[buf], MT == 2 ? g & 1 : (g >> 1) & 1, 512u);
+          tc_fence_after();
+          if (!*reinterpret_cast<volatile int*>(&sh.skip[buf])) {
 #pragma unroll 1
-              for (int k = 0; k < TN / 16; ++k) {
-                const uint32_t a = tmem + buf * TN + (k * 16 / CW) * CW + (k * 16 % CW) / 2;
-                const uint64_t b = smem_desc_sw128_mn(v + k * 2048, C::kBlock);
-                // A copy's tokens go to its lanes of O alone; the first of them begin it.
-                const int copy = k * copies * 16 / TN;
-                const bool first = begins && k * 16 % (TN / copies) == 0;
-                auto off = [&](int quarter) { return quarter / (4 / copies) == copy ? 0u : kAll; };
-                const uint4 lanes = make_uint4(off(0), off(1), off(2), off(3));
-                mma_f16_tmem_a_lanes(tmem + C::kScoreCols + acc * DT, a, b, i_out, !first, lanes);
-                if (!kFp4) mma_f16_tmem_a_lanes(tmem + C::kScoreCols + acc * DT, a + CW / 2, b, i_out, 1u, lanes);
-              }
+            for (int k = 0; k < TN / 16; ++k) {
+              const uint32_t a = tmem + buf * TN + (k * 16 / CW) * CW + (k * 16 % CW) / 2;
+              const uint64_t b = smem_desc_sw128_mn(v + k * 2048, C::kBlock);
+              // A copy's tokens go to its lanes of O alone; the first of them begin it.
+              const int copy = k * copies * 16 / TN;
+              const bool first = begins && k * 16 % (TN / copies) == 0;
+              auto off = [&](int quarter) { return quarter / (4 / copies) == copy ? 0u : kAll; };
+              const uint4 lanes = make_uint4(off(0), off(1), off(2), off(3));
+              mma_f16_tmem_a_lanes(tmem + C::kScoreCols + m * DT, a, b, i_out, !first, lanes);
+              if (!kFp4) mma_f16_tmem_a_lanes(tmem + C::kScoreCols + m * DT, a + CW / 2, b, i_out, 1u, lanes);
             }
-            mma_commit(smem_u32(&sh.o_done[acc]));
-            if (m == MT - 1) mma_commit(smem_u32(&sh.empty[slot]));
-            if (MT == 2 && it + 1 < w.tiles) scores(g + 1, m);
+          }
+          mma_commit(smem_u32(&sh.o_done[buf]));
+          if (m == MT - 1) mma_commit(smem_u32(&sh.empty[slot]));
+        };
+        // Products of different shapes have no order among themselves: scores wait until the weights whose place they
+        // take have been used.
+        auto used_up = [&](uint32_t tile, int m) {
+          wait(sh.o_done[MT == 2 ? m : tile & 1], (MT == 2 ? tile : tile >> 1) & 1, 1u << 17);
+        };
+        scores(g, 0);
+        if (MT == 2) scores(g, 1);
+        for (int it = 0; it < tiles; ++it, ++g) {
+          if (MT == 1) {
+            if (it + 1 < tiles) {
+              if (it > 0) used_up(g - 1, 0);
+              scores(g + 1, 0);
+            }
+            weigh(it, 0);
+          } else {
+            weigh(it, 0);
+            if (it > 0) {
+              used_up(g - 1, 1);
+              scores(g, 1);
+            }
+            if (it + 1 < tiles) {
+              used_up(g, 0);
+              scores(g + 1, 0);
+            }
+            weigh(it, 1);
           }
         }
       }
@@ -1061,19 +1083,19 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, 1) tree_attention
                                                           (x - r * lines) * 64));
         }
       }
-      waits(sh.heard[turn & 1], ((turn >> 1) & 1) ^ 1, 1u << 14);
+      waits(sh.heard, (turn & 1) ^ 1, 1u << 14);
       if (dead) break;  // what softmax may still read stays
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
-        sh.bits[turn & 1][lane + 32 * k] = bits[k];
-        sh.depth[turn & 1][lane + 32 * k] = (uint8_t)depth_of(bits[k], lane + 32 * k);
+        sh.bits[lane + 32 * k] = bits[k];
+        sh.depth[lane + 32 * k] = (uint8_t)depth_of(bits[k], lane + 32 * k);
       }
       if (lane == 0) {
         if (!more) w.tiles = 0;
-        sh.part[turn & 1] = w;
+        sh.part = w;
       }
       __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&sh.told[turn & 1]));
+      if (lane == 0) mbar_arrive(smem_u32(&sh.told));
     }
   } else if (!kFp4 && p.box && warp < C::kSoftmax + 3) {
     // ================================================= rows of a bf16 cache by TMA, boxes of one page, 64 dimensions
@@ -1303,7 +1325,7 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, 1) tree_attention
   __syncthreads();
   if (warp == C::kSoftmax) {
     tc_fence_after();
-    tmem_dealloc(tmem, 512);
+    tmem_dealloc(tmem, C::kCols);
   }
 }
 
@@ -1314,12 +1336,11 @@ __global__ void __launch_bounds__(kJoinThreads) tree_attention_join_kernel(const
   const int4 s = p.split[blockIdx.x];
   if (s.x < 0) return;
   const int mate = (int)blockIdx.x % p.together, chunk = s.y % p.chunks, head = s.y / p.chunks * p.together + mate;
-  constexpr int kGroups = Cfg<DT, MT, kFp4>::kGroups;
   const int R = min(128 * MT, p.t * p.group - chunk * 128 * MT), D = p.c.head_dim;
   const int x = (int)blockIdx.y * kJoinThreads + (int)threadIdx.x, r = x % R, d4 = x / R;
   if (d4 >= D / 4) return;
   auto slot = [&](int k) {
-    return (2 * ((int64_t)k * p.together + mate) + (k == s.z ? 1 : 0)) * kGroups + (r >> 7);
+    return (2 * ((int64_t)k * p.together + mate) + (k == s.z ? 1 : 0)) * MT + (r >> 7);
   };
   float M = kNoScore, L = 0.0f;
   float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
@@ -1365,15 +1386,19 @@ inline int padded_dim(int D) { return D <= 64 ? 64 : (D <= 128 ? 128 : 256); }
 inline int row_tiles(const mixfp4_kv_cache* c, int64_t t, int64_t q_heads) {
   return c->head_dim <= 128 && t * (q_heads / c->heads) > 128 ? 2 : 1;
 }
-inline int groups_of(const mixfp4_kv_cache* c) { return c->head_dim > 128 ? 1 : 2; }  // of softmax warps
-inline int tile_tokens(const mixfp4_kv_cache* c) { return c->head_dim > 128 ? 64 : 128; }
+inline int tile_tokens(const mixfp4_kv_cache* c, int tiles) {
+  return c->head_dim <= 128 && (tiles == 2 || c->dtype == MIXFP4_CACHE_MIXFP4) ? 128 : 64;
+}
 // Key heads whose CTAs walk over the same tokens at the same time.
 inline int together_of(const mixfp4_kv_cache* c) {
   for (int n = 8; n > 1; n /= 2)
     if (c->heads % n == 0) return n;
   return 1;
 }
-inline int grid_of(const mixfp4_kv_cache* c) { return num_sms() / together_of(c) * together_of(c); }
+inline int grid_of(const mixfp4_kv_cache* c, int tiles) {
+  const int ctas = num_sms() * (tiles == 1 && c->head_dim <= 128 && c->dtype == MIXFP4_CACHE_BF16 ? 2 : 1);
+  return ctas / together_of(c) * together_of(c);
+}
 
 // Rows that one TMA copy of a bf16 cache brings: of one page, and a part of a tile; 0 where TMA's rules do not allow it
 // (pages of no multiple of 16 tokens, rows of less than 64 elements, whose copies would not fill the operand's).
@@ -1438,7 +1463,8 @@ int mixfp4_tree_attention_workspace(const mixfp4_kv_cache* cache, int64_t B, int
   if (B < 0 || t < 0 || t > kMostDrafts || q_heads < 0 || q_heads % cache->heads != 0) return MIXFP4_ERR_SHAPE;
   *bytes = 0;
   if (B == 0 || t == 0 || q_heads == 0) return MIXFP4_OK;
-  const int64_t grid = grid_of(cache), rows = 128 * groups_of(cache);
+  const int tiles = row_tiles(cache, t, q_heads);
+  const int64_t grid = grid_of(cache, tiles), rows = 128 * tiles;
   *bytes = (grid * 16 + 255) / 256 * 256 + 2 * grid * rows * (8 + padded_dim(cache->head_dim) * 4);
   return MIXFP4_OK;
 }
@@ -1474,13 +1500,13 @@ int mixfp4_tree_attention(const void* q, int64_t q_stride, int64_t q_token_strid
   p.scale = scale, p.softcap = softcap, p.window = window, p.slopes = slopes;
   p.out = static_cast<uint16_t*>(out), p.lse = lse;
   p.status = status_word;
-  const int grid = grid_of(cache), tiles = row_tiles(cache, t, q_heads);
+  const int tiles = row_tiles(cache, t, q_heads), grid = grid_of(cache, tiles);
   const int64_t rows = t * p.group;
   if (rows > INT32_MAX - 256) return MIXFP4_ERR_SHAPE;
   p.chunks = (int)((rows + 128 * tiles - 1) / (128 * tiles));
   p.together = together_of(cache);
   p.shares = grid / p.together;
-  p.joined = p.max_tokens > tile_tokens(cache);  // rows of one tile are never cut
+  p.joined = p.max_tokens > tile_tokens(cache, tiles);  // rows of one tile are never cut
   p.page_shift = -1;
   for (int i = 0; i < 31; ++i)
     if (cache->page_size == 1 << i) p.page_shift = i;
@@ -1488,7 +1514,7 @@ int mixfp4_tree_attention(const void* q, int64_t q_stride, int64_t q_token_strid
   p.split = reinterpret_cast<int4*>(w);
   w += ((int64_t)grid * 16 + 255) / 256 * 256;
   p.stat = reinterpret_cast<float2*>(w);
-  p.part = reinterpret_cast<float4*>(w + 2 * (int64_t)grid * 128 * groups_of(cache) * 8);
+  p.part = reinterpret_cast<float4*>(w + 2 * (int64_t)grid * 128 * tiles * 8);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   if (status_word && cudaMemsetAsync(status_word, 0, 4, s) != cudaSuccess) return MIXFP4_ERR_CUDA;
   return cache->dtype == MIXFP4_CACHE_MIXFP4 ? launch_dim<true>(p, grid, tiles, s) : launch_dim<false>(p, grid, tiles, s);
