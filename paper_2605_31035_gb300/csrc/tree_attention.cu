@@ -100,16 +100,16 @@ struct Part {
   int64_t behind;  // the unit behind the row's last
 };
 
-template <int kSlots, int kAddresses, int kWords>
+template <int kSlots, int kAddresses, int kWords, int MT>
 struct Shared {
   uint64_t full[kSlots], empty[kSlots], placed[kAddresses], used[kAddresses];
   // Of a buffer of scores: they are there, their weights are, O has taken those up.  No buffer has two uses under way, so
   // the parity of a wait tells one use from the next.
-  uint64_t s_full[2], p_full[2], o_done[2];
+  uint64_t s_full[2 * MT], p_full[2 * MT], o_done[2 * MT];
   uint64_t told, heard, q_full, end;
   uint32_t tmem;
   int abort;
-  int skip[2];
+  int skip[2 * MT];
   int64_t all, shares, before, edge[2];
   int edge_b;
   uint32_t there[kThere][kWords];  // of a tile, which of its tokens there are
@@ -127,36 +127,37 @@ struct Cfg {
   // With one tile of rows two CTAs share an SM: what one does once a row (its queries, its end) the other's tiles cover.
   // A MixFP4 cache's decoding takes the registers and the larger tiles of one.
   static constexpr int kCtas = !kFp4 && MT == 1 && DT <= 128 ? 2 : 1;
-  static constexpr int kTokens = DT <= 128 && (MT == 2 || kFp4) ? 128 : 64;  // of a tile
+  static constexpr int kTokens = kFp4 && MT == 1 && DT <= 128 ? 128 : 64;  // of a tile
   static constexpr int kChain = kChainTokens / kTokens;    // tiles to a chain of sums
   static constexpr int kCw = kTokens / 4;                  // and of its quarter, a thread's step
   static constexpr int kBlock = kTokens * 128;             // 64 dimensions of a tile
+  static constexpr int kStep = kTokens == 128 || MT == 2 ? 32 : 16;  // columns of scores that a thread has in registers
   static constexpr int kSlot = kBlock * (DT / 64);
   static constexpr int kSoftmax = 4 * MT;                  // warps, four to a tile of rows
   static constexpr int kQ = MT * 128 * DT * 2;
-  static constexpr int kProducers = kFp4 ? (MT == 1 ? 16 : 8) : 2;  // of a bf16 cache where TMA cannot bring its rows
+  static constexpr int kProducers = kFp4 ? 8 : 2;  // of a bf16 cache where TMA cannot bring its rows
   static constexpr int kThreads = (kSoftmax + 4 + (kFp4 ? kProducers : 0)) * 32;  // the four: products, TMA or helpers
   // Registers of a thread at launch, then of softmax and of the other threads (together no more than at launch).
   static constexpr int kRegs = 65536 / (kThreads * kCtas) / 8 * 8;
-  static constexpr int kOtherRegs = kFp4 ? (MT == 1 ? 64 : 72) : kRegs;
+  static constexpr int kOtherRegs = kFp4 && MT == 2 ? 72 : kRegs;
   static constexpr int kLeft = (kRegs * kThreads - kOtherRegs * (kThreads - kSoftmax * 32)) / (kSoftmax * 32) / 8 * 8;
   static constexpr int kSoftRegs = kLeft < 232 ? kLeft : 232;
   static constexpr int kRows = kTokens / kProducers;       // of a tile, to a producer warp
   static constexpr int kRawSlot = kRows * (DT / 2 + 16);   // MixFP4 rows as they lie: codes, then scale bytes
-  static constexpr int kRawDepth = kFp4 ? 5 : 0;
-  static constexpr int kRaw = kProducers * kRawDepth * kRawSlot;
-  static constexpr int kAddresses = kFp4 ? 4 : 0;          // tiles whose rows' places are known
+  static constexpr int kRawDepth = kFp4 ? 3 : 0;           // tiles
+  static constexpr int kRaw = kProducers * kRawDepth * 2 * kRawSlot;
+  static constexpr int kAddresses = kFp4 ? 2 : 0;          // tiles whose rows' places are known
   static constexpr int kPlaces = kAddresses * kTokens * 16;
   static constexpr int kWords = kTokens / 32;
   static constexpr int kRoom = (kCtas == 2 ? 113 : 227) * 1024 - kQ - kRaw - kPlaces;
   static constexpr int slots(int n) {  // as many as there is room for
-    return n == 1 || n * (kSlot + 16) + (int)sizeof(Shared<1, kFp4 ? 4 : 1, kWords>) <= kRoom ? n : slots(n - 1);
+    return n == 1 || n * (kSlot + 16) + (int)sizeof(Shared<1, kFp4 ? 2 : 1, kWords, MT>) <= kRoom ? n : slots(n - 1);
   }
   static constexpr int kSlots = slots(kMostSlots);
-  using Sh = Shared<kSlots, kFp4 ? 4 : 1, kWords>;
+  using Sh = Shared<kSlots, kFp4 ? 2 : 1, kWords, MT>;
   static constexpr int kSmem = kQ + kSlots * kSlot + kRaw + kPlaces + (int)sizeof(Sh);
   static_assert(kSlots >= 3 && sizeof(Sh) % 8 == 0 && kSmem <= (kCtas == 2 ? 113 : 227) * 1024);
-  static constexpr uint32_t kScoreCols = 2 * kTokens;      // of tensor memory, O behind them
+  static constexpr uint32_t kScoreCols = 2 * MT * kTokens; // of tensor memory, O behind them
   static constexpr uint32_t kCols = kCtas == 2 ? 256 : 512;
 };
 
@@ -392,40 +393,42 @@ struct Lanes {
   static __device__ __forceinline__ int row(int lane) { return (lane >> 2 & 1) | (lane >> kShift << 1); }
 };
 
-// A warp's rows of a MixFP4 tile decoded to f16 at the operand's swizzled places: twice their values under the block
-// scale alone.
-template <typename C, typename L, int kSteps>
-__device__ __forceinline__ void decode_rows(uint32_t to, uint32_t raw, int piece, int r0, int before) {
+// A lane's pieces of a MixFP4 tile, 16 elements of each of kSteps rows: all asked for at once, then decoded to f16 (twice
+// their values under the block scale alone) at the operand's swizzled places.
+template <int kSteps>
+struct Codes {
   uint2 c[kSteps];
   uint32_t scale[kSteps];
+  __device__ __forceinline__ void load(uint32_t codes, int step, uint32_t scales, int scale_step) {
 #pragma unroll
-  for (int j = 0; j < kSteps; ++j) {  // all asked for before the first is used
-    const int r = r0 + j * L::kRowsAtOnce;
-    c[j] = lds64(raw + r * (L::kPieces * 8) + piece * 8);
-    scale[j] = lds8(raw + C::kRows * (L::kPieces * 8) + r * 16 + piece);
+    for (int j = 0; j < kSteps; ++j) {
+      c[j] = lds64(codes + j * step);
+      scale[j] = lds8(scales + j * scale_step);
+    }
   }
-  to += (piece >> 2) * C::kBlock;
+  // Rows row0, row0 + step ... of the block of 64 dimensions at `to`, 16-byte units u0 and u0 + 1.
+  __device__ __forceinline__ void decode(uint32_t to, int row0, int step, int u0) const {
 #pragma unroll
-  for (int j = 0; j < kSteps; ++j) {
-    const int row = r0 + j * L::kRowsAtOnce;
-    const uint32_t sc = scale[j], e1m2 = sc >> 7;
-    const uint32_t s2 = cvt_f16x2_from_e4m3x2((uint16_t)((sc & 0x7Fu) * 0x0101u));
-    const uint32_t lo = kLutE2M1Lo + e1m2 * (kLutE1M2Lo - kLutE2M1Lo), hi = kLutE2M1Hi + e1m2 * (kLutE1M2Hi - kLutE2M1Hi);
-    uint32_t v[2][4];
-    decode8(c[j].x, lo, hi, s2, v[0]);
-    decode8(c[j].y, lo, hi, s2, v[1]);
-    const int u0 = (piece & 3) * 2;
-    const int x = (row + before) & 7;  // `before` rows of the tile lie ahead of the warp's
-    sts128(to + row * 128 + ((u0 ^ x) << 4), v[0][0], v[0][1], v[0][2], v[0][3]);
-    sts128(to + row * 128 + (((u0 + 1) ^ x) << 4), v[1][0], v[1][1], v[1][2], v[1][3]);
+    for (int j = 0; j < kSteps; ++j) {
+      const int row = row0 + j * step, x = row & 7;
+      const uint32_t sc = scale[j], e1m2 = sc >> 7;
+      const uint32_t s2 = cvt_f16x2_from_e4m3x2((uint16_t)((sc & 0x7Fu) * 0x0101u));
+      const uint32_t lo = kLutE2M1Lo + e1m2 * (kLutE1M2Lo - kLutE2M1Lo);
+      const uint32_t hi = kLutE2M1Hi + e1m2 * (kLutE1M2Hi - kLutE2M1Hi);
+      uint32_t v[2][4];
+      decode8(c[j].x, lo, hi, s2, v[0]);
+      decode8(c[j].y, lo, hi, s2, v[1]);
+      sts128(to + row * 128 + ((u0 ^ x) << 4), v[0][0], v[0][1], v[0][2], v[0][3]);
+      sts128(to + row * 128 + (((u0 + 1) ^ x) << 4), v[1][0], v[1][1], v[1][2], v[1][3]);
+    }
   }
-}
+};
 
 template <int DT, int MT, bool kFp4>
 __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>::kCtas) tree_attention_kernel(const TreeArgs p, const __grid_constant__ CUtensorMap tm_k,
                       const __grid_constant__ CUtensorMap tm_v) {
   using C = Cfg<DT, MT, kFp4>;
-  constexpr int TN = C::kTokens, CW = C::kCw;
+  constexpr int TN = C::kTokens, CW = C::kCw, PW = C::kStep;
   extern __shared__ __align__(1024) uint8_t smem[];
   auto& sh = *reinterpret_cast<typename C::Sh*>(smem + C::kQ + C::kSlots * C::kSlot + C::kRaw + C::kPlaces);
   const uint32_t q_smem = smem_u32(smem), ring = q_smem + C::kQ;
@@ -448,7 +451,7 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
       mbar_init(smem_u32(&sh.placed[i]), 1);
       mbar_init(smem_u32(&sh.used[i]), C::kProducers);
     }
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < 2 * MT; ++i) {
       mbar_init(smem_u32(&sh.s_full[i]), 1);
       mbar_init(smem_u32(&sh.p_full[i]), 4);
       mbar_init(smem_u32(&sh.o_done[i]), 1);
@@ -626,7 +629,7 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
       const int64_t slot = (2 * (int64_t)blockIdx.x + (w.first ? 1 : 0)) * MT + m;
       float4* aside = p.part + slot * (DT / 4 * 128) + tl;
       auto o_ready = [&](uint32_t bit) {  // O of the tile before this one
-        waits(sh.o_done[MT == 2 ? m : (g - 1) & 1], (MT == 2 ? g - 1 : (g - 1) >> 1) & 1, bit);
+        waits(sh.o_done[2 * m + ((g - 1) & 1)], ((g - 1) >> 1) & 1, bit);
         tc_fence_after();
       };
       auto set_aside = [&] {  // O joins what was set aside before, and begins at 0
@@ -654,11 +657,11 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
       };
 
       for (int it = 0; it < w.tiles; ++it, ++g) {
-        const int buf = MT == 2 ? m : (int)(g & 1);
+        const int buf = 2 * m + (int)(g & 1);
         const uint32_t scores = lanes + buf * TN;
         const bool begins = it % C::kChain == 0;
         if (it > 0 && begins) set_aside();
-        waits(sh.s_full[buf], MT == 2 ? g & 1 : (g >> 1) & 1, 2u);
+        waits(sh.s_full[buf], (g >> 1) & 1, 2u);
         tc_fence_after();
         const int j0 = w.s.from + (w.tile + w.tiles - 1 - it) * TN;
         const uint32_t* there = sh.there[g % kThere];
@@ -699,10 +702,10 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
           }
         }
         if (!idle) {
-          // Which of a step's tokens the row sees, a bit each.
-          auto seen_of = [&](int s) -> uint32_t {
-            const int a = j0 + s * CW, x = w.s.first - a;
-            const uint32_t have = CW == 32 ? there[s] : (there[s >> 1] >> (16 * (s & 1))) & 0xFFFFu;
+          // Which of the 32 tokens from column `col` on the row sees, a bit each (of the tile's: the rest is 0).
+          auto seen_of = [&](int col) -> uint32_t {
+            const int a = j0 + col, x = w.s.first - a;
+            const uint32_t have = there[col >> 5] >> (col & 31);
             auto below = [](int k) -> uint32_t { return k <= 0 ? 0u : (k >= 32 ? kAll : (1u << k) - 1u); };
             uint32_t v = valid ? below(x) & ~below(low - a) : 0u;
             if (x <= 0)
@@ -714,21 +717,30 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
           // ---- the scores' maximum; scores that need more than a factor are put back as they are to be.  Where the row
           // has one step, it stays in registers.
           float top = -INFINITY;
-          uint32_t v[CW];
+          uint32_t v[PW];
+          const int c_end = (step0 + steps) * CW;
+          const bool narrow = PW > CW && steps == 1;  // half a step
+          auto load = [&](int c) {
+            if (narrow)
+              tmem_load<16>(scores + c, v);
+            else
+              tmem_load<PW>(scores + c, v);
+            tmem_loaded<PW>(v);
+          };
 #pragma unroll 1
-          for (int s = step0; s < step0 + steps; ++s) {
-            tmem_load<CW>(scores + s * CW, v);
-            tmem_loaded<CW>(v);
+          for (int c = step0 * CW; c < c_end; c += PW) {
+            load(c);
             if (!general) {
               float top2 = -INFINITY;  // two chains
 #pragma unroll
-              for (int e = 0; e < CW; e += 4) {
+              for (int e = 0; e < PW; e += 4) {
+                if (e == 16 && narrow) break;
                 top = max3f(top, __uint_as_float(v[e]), __uint_as_float(v[e + 1]));
                 top2 = max3f(top2, __uint_as_float(v[e + 2]), __uint_as_float(v[e + 3]));
               }
               top = fmaxf(top, top2);
             } else {
-              const int a = j0 + s * CW;
+              const int a = j0 + c;
               auto shaped = [&](uint32_t y) {
                 const float x = __uint_as_float(y) * fs;
                 return p.softcap > 0.0f ? cap2 * tanh_of(x) : x;
@@ -736,16 +748,18 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
               if (!masked) {
                 const float far0 = (float)(place - a);
 #pragma unroll
-                for (int e = 0; e < CW; ++e) {
+                for (int e = 0; e < 32; ++e) {
+                  if (e == 16 && narrow) break;
                   float x = shaped(v[e]);
                   if (p.slopes) x = fmaf(slope, far0 - (float)e, x);
                   top = fmaxf(top, x);
                   v[e] = __float_as_uint(x);
                 }
               } else {
-                const uint32_t seen = seen_of(s);
+                const uint32_t seen = seen_of(c);
 #pragma unroll
-                for (int e = 0; e < CW; ++e) {
+                for (int e = 0; e < 32; ++e) {
+                  if (e == 16 && narrow) break;
                   float x = shaped(v[e]);
                   if (p.slopes) {
                     const int j = a + e;
@@ -758,7 +772,12 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
                   v[e] = __float_as_uint(x);
                 }
               }
-              if (steps > 1 || slow) tmem_store<CW>(scores + s * CW, v);
+              if (c_end - step0 * CW > PW || slow) {
+                if (narrow)
+                  tmem_store<16>(scores + c, v);
+                else
+                  tmem_store<PW>(scores + c, v);
+              }
             }
           }
           if (general)
@@ -788,18 +807,15 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
           // ---- the weights
           const float less = (kFp4 ? kFp4Exp : 0.0f) - mx;
           if (!slow) {
-            constexpr int kOut = kFp4 ? CW / 2 : CW;
             const u64 ff = pack2(f, f), ll = pack2(less, less), tiny = pack2(0x1p-30f, 0x1p-30f);
             u64 sum[2] = {0ull, 0ull};
 #pragma unroll 1
-            for (int s = step0; s < step0 + steps; ++s) {
-              if (steps > 1) {
-                tmem_load<CW>(scores + s * CW, v);
-                tmem_loaded<CW>(v);
-              }
-              uint32_t out[kOut];
+            for (int c = step0 * CW; c < c_end; c += PW) {
+              if (c_end - step0 * CW > PW) load(c);
+              uint32_t out[kFp4 ? PW / 2 : PW];
 #pragma unroll
-              for (int e = 0; e < CW; e += 2) {
+              for (int e = 0; e < PW; e += 2) {
+                if (e == 16 && narrow) break;
                 float x0, x1;
                 unpack2(fma2(bits2(v[e], v[e + 1]), ff, ll), x0, x1);
                 const float w0 = ex2(x0), w1 = ex2(x1);
@@ -813,11 +829,20 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
                   const u64 up = bits2(__float_as_uint(w0) & 0xFFFF0000u, __float_as_uint(w1) & 0xFFFF0000u);
                   float l0, l1;
                   unpack2(fma2(ww, tiny, sub2(ww, up)), l0, l1);
-                  out[e / 2] = prmt(__float_as_uint(w0), __float_as_uint(w1), 0x7632u);
-                  out[CW / 2 + e / 2] = bf16x2(l0, l1);
+                  const int at = e / CW * CW + e % CW / 2;  // the upper parts of a quarter, then its lower ones
+                  out[at] = prmt(__float_as_uint(w0), __float_as_uint(w1), 0x7632u);
+                  out[at + CW / 2] = bf16x2(l0, l1);
                 }
               }
-              tmem_store<kOut>(scores + s * CW, out);
+              if constexpr (kFp4) {
+                tmem_store<CW / 2>(scores + c, out);
+                if constexpr (PW > CW)
+                  if (!narrow) tmem_store<CW / 2>(scores + c + CW, out + CW / 2);
+              } else if (narrow) {
+                tmem_store<CW>(scores + c, out);
+              } else {
+                tmem_store<PW>(scores + c, out);
+              }
             }
             float s0, s1;
             unpack2(add2(sum[0], sum[1]), s0, s1);
@@ -844,7 +869,7 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
                 tmem_ld1(scores + col, xs);
                 const float x = fmaf(__uint_as_float(xs), f, less), wt = ex2(x);
                 if (d == 0) sum += wt;
-                const bool mine = (seen_of(col / CW) >> (col % CW)) & 1u;
+                const bool mine = seen_of(col) & 1u;
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
                   const uint4 v = lds128(v_smem + (d >> 6) * C::kBlock + col * 128 +
@@ -982,19 +1007,22 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
       const uint32_t i_scores = (1u << 4) | kType | ((uint32_t)(TN >> 3) << 17) | (8u << 24);
       const uint32_t i_out = (1u << 4) | kType | (1u << 16) | ((uint32_t)(D >> 3) << 17) | (8u << 24);
       uint32_t g = 0, turn = 0;
-      auto scores = [&](uint32_t tile, int m) {  // of tile number `tile` and the m-th rows, into their buffer
+      // S_m of tile number `tile`, into its buffer.
+      auto scores = [&](uint32_t tile, int m) {
         const uint32_t q = 2 * tile, slot = q % C::kSlots;
         if (m == 0) {
           wait(sh.full[slot], (q / C::kSlots) & 1, 64u);
           if (!kFp4 && !p.box) fence_proxy_async_smem();  // of what cp.async has written
           tc_fence_after();
         }
-        const int buf = MT == 2 ? m : (int)(tile & 1);
-        const uint32_t a = q_smem + m * (128 * DT * 2), b = ring + slot * C::kSlot;
-#pragma unroll 1
-        for (int k = 0; k < D / 16; ++k)
-          mma_f16(tmem + buf * TN, smem_desc_sw128(a + (k >> 2) * 16384 + (k & 3) * 32),
-                  smem_desc_sw128(b + (k >> 2) * C::kBlock + (k & 3) * 32), i_scores, k > 0);
+        const int buf = 2 * m + (int)(tile & 1);
+        const uint64_t a = smem_desc_sw128(q_smem + m * (128 * DT * 2)), b = smem_desc_sw128(ring + slot * C::kSlot);
+#pragma unroll
+        for (int k = 0; k < DT / 16; ++k) {
+          if (16 * k >= D) break;
+          mma_f16(tmem + buf * TN, a + ((k >> 2) * 16384 + (k & 3) * 32) / 16, b + ((k >> 2) * C::kBlock + (k & 3) * 32) / 16,
+                  i_scores, k > 0);
+        }
         mma_commit(smem_u32(&sh.s_full[buf]));
         if (m == MT - 1) mma_commit(smem_u32(&sh.empty[slot]));
       };
@@ -1004,42 +1032,43 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
         const int R = min(128 * MT, p.t * p.group - w.chunk * 128 * MT);
         const int copies = MT == 2 || R > 64 ? 1 : (R > 32 ? 2 : 4);
         tc_fence_after();
-        const int tiles = w.tiles;
-        // O_m += P V of tile g.
+        // O_m += P_m V of tile g.
         auto weigh = [&](int it, int m) {
-          const uint32_t q = 2 * g + 1, slot = q % C::kSlots, v = ring + slot * C::kSlot;
-          const int buf = MT == 2 ? m : (int)(g & 1);
+          const uint32_t q = 2 * g + 1, slot = q % C::kSlots;
+          const int buf = 2 * m + (int)(g & 1);
           const bool begins = it % C::kChain == 0;  // O is at 0
           if (m == 0) {
             wait(sh.full[slot], (q / C::kSlots) & 1, 256u);
             if (!kFp4 && !p.box) fence_proxy_async_smem();
           }
-          wait(sh.p_full[buf], MT == 2 ? g & 1 : (g >> 1) & 1, 512u);
+          wait(sh.p_full[buf], (g >> 1) & 1, 512u);
           tc_fence_after();
           if (!*reinterpret_cast<volatile int*>(&sh.skip[buf])) {
-#pragma unroll 1
+            const uint64_t v = smem_desc_sw128_mn(ring + slot * C::kSlot, C::kBlock);
+            const uint32_t o = tmem + C::kScoreCols + m * DT;
+#pragma unroll
             for (int k = 0; k < TN / 16; ++k) {
               const uint32_t a = tmem + buf * TN + (k * 16 / CW) * CW + (k * 16 % CW) / 2;
-              const uint64_t b = smem_desc_sw128_mn(v + k * 2048, C::kBlock);
               // A copy's tokens go to its lanes of O alone; the first of them begin it.
               const int copy = k * copies * 16 / TN;
               const bool first = begins && k * 16 % (TN / copies) == 0;
               auto off = [&](int quarter) { return quarter / (4 / copies) == copy ? 0u : kAll; };
               const uint4 lanes = make_uint4(off(0), off(1), off(2), off(3));
-              mma_f16_tmem_a_lanes(tmem + C::kScoreCols + m * DT, a, b, i_out, !first, lanes);
-              if (!kFp4) mma_f16_tmem_a_lanes(tmem + C::kScoreCols + m * DT, a + CW / 2, b, i_out, 1u, lanes);
+              mma_f16_tmem_a_lanes(o, a, v + k * 128, i_out, !first, lanes);
+              if (!kFp4) mma_f16_tmem_a_lanes(o, a + CW / 2, v + k * 128, i_out, 1u, lanes);
             }
           }
           mma_commit(smem_u32(&sh.o_done[buf]));
           if (m == MT - 1) mma_commit(smem_u32(&sh.empty[slot]));
         };
         // Products of different shapes have no order among themselves: scores wait until the weights whose place they
-        // take have been used.
-        auto used_up = [&](uint32_t tile, int m) {
-          wait(sh.o_done[MT == 2 ? m : tile & 1], (MT == 2 ? tile : tile >> 1) & 1, 1u << 17);
-        };
+        // take have been used up, which with two tiles of rows in turn is while the other's products run.
+        auto used_up = [&](uint32_t tile, int m) { wait(sh.o_done[2 * m + (tile & 1)], (tile >> 1) & 1, 1u << 17); };
+        const int tiles = w.tiles;
         scores(g, 0);
-        if (MT == 2) scores(g, 1);
+        if (MT == 2) {
+          scores(g, 1);
+        }
         for (int it = 0; it < tiles; ++it, ++g) {
           if (MT == 1) {
             if (it + 1 < tiles) {
@@ -1048,15 +1077,13 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
             }
             weigh(it, 0);
           } else {
-            weigh(it, 0);
-            if (it > 0) {
-              used_up(g - 1, 1);
-              scores(g, 1);
-            }
             if (it + 1 < tiles) {
-              used_up(g, 0);
+              if (it > 0) used_up(g - 1, 0);
               scores(g + 1, 0);
+              if (it > 0) used_up(g - 1, 1);
+              scores(g + 1, 1);
             }
+            weigh(it, 0);
             weigh(it, 1);
           }
         }
@@ -1240,21 +1267,29 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
     const int pw = warp - C::kSoftmax - 4;
     using L = Lanes<DT>;
     const int piece = L::piece(lane), r0 = L::row(lane);
-    const uint32_t raw0 = ring + C::kSlots * C::kSlot + pw * C::kRawDepth * C::kRawSlot;
-    constexpr int kRows = C::kRows, kSteps = kRows / L::kRowsAtOnce;
-    uint32_t g = 0, q = 0, sent = 0;  // tiles, copies asked for, copies decoded
-    // The oldest copy not decoded yet, with `later` behind it: once it has landed, for the tensor cores.
+    const uint32_t raw0 = ring + C::kSlots * C::kSlot + pw * C::kRawDepth * 2 * C::kRawSlot;
+    constexpr int kRows = C::kRows, kSteps = kRows / L::kRowsAtOnce, kCodes = kRows * (DT / 2);
+    uint32_t g = 0, sent = 0;  // tiles asked for, tiles decoded
+    // The oldest tile not decoded yet, with `later` behind it: once it has landed, for the tensor cores.
     auto hand_over = [&](int later) {
       cp_wait_at_most(later);
       __syncwarp();
-      const uint32_t slot = sent % C::kSlots;
-      waits(sh.empty[slot], ((sent / C::kSlots) & 1) ^ 1, 1024u);
-      if (piece * 16 < D)
-        decode_rows<C, L, kSteps>(ring + slot * C::kSlot + pw * kRows * 128, raw0 + (sent % C::kRawDepth) * C::kRawSlot,
-                                  piece, r0, C::kRows >= 8 ? 0 : pw * kRows);
-      fence_proxy_async_smem();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&sh.full[slot]));
+      const uint32_t raw = raw0 + (sent % C::kRawDepth) * 2 * C::kRawSlot;
+      Codes<kSteps> c[2];
+#pragma unroll
+      for (int kv = 0; kv < 2; ++kv)
+        if (piece * 16 < D) c[kv].load(raw + kv * C::kRawSlot + r0 * (DT / 2) + piece * 8, L::kRowsAtOnce * (DT / 2),
+                                       raw + kv * C::kRawSlot + kCodes + r0 * 16 + piece, L::kRowsAtOnce * 16);
+#pragma unroll
+      for (int kv = 0; kv < 2; ++kv) {
+        const uint32_t q = 2 * sent + kv, slot = q % C::kSlots;
+        waits(sh.empty[slot], ((q / C::kSlots) & 1) ^ 1, 1024u);
+        if (piece * 16 < D)
+          c[kv].decode(ring + slot * C::kSlot + (piece >> 2) * C::kBlock, pw * kRows + r0, L::kRowsAtOnce, (piece & 3) * 2);
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&sh.full[slot]));
+      }
       ++sent;
     };
     while (walk.next(p, mate, w)) {
@@ -1262,61 +1297,59 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
       for (int it = 0; it < w.tiles; ++it, ++g) {
         waits(sh.placed[g % C::kAddresses], (g / C::kAddresses) & 1, 4096u);
         const uint32_t at = places + (g % C::kAddresses) * (TN * 16) + pw * kRows * 16;
-        int64_t from[kSteps];
+        const uint32_t raw = raw0 + (g % C::kRawDepth) * 2 * C::kRawSlot;
 #pragma unroll
         for (int j = 0; j < kSteps; ++j) {
-          const uint2 v = lds64(at + (r0 + j * L::kRowsAtOnce) * 16);
-          from[j] = (int64_t)((u64)v.x | (u64)v.y << 32);
+          const int r = r0 + j * L::kRowsAtOnce;
+          const uint2 x = lds64(at + r * 16);
+          const bool take = (int32_t)x.y >= 0 && piece * 16 < D;
+          const int64_t from = take ? (int64_t)((u64)x.x | (u64)x.y << 32) + piece * 8 : 0;
+          const uint32_t to = raw + r * (DT / 2) + piece * 8;
+          cp_async<8>(to, static_cast<const uint8_t*>(p.c.k) + from, take);
+          cp_async<8>(to + C::kRawSlot, static_cast<const uint8_t*>(p.c.v) + from, take);
         }
-#pragma unroll 1
-        for (int kv = 0; kv < 2; ++kv, ++q) {
-          const uint8_t* base = static_cast<const uint8_t*>(kv ? p.c.v : p.c.k);
-          const uint8_t* scales = kv ? p.c.v_scales : p.c.k_scales;
-          const uint32_t raw = raw0 + (q % C::kRawDepth) * C::kRawSlot, sd = raw + kRows * (DT / 2);
-#pragma unroll
-          for (int j = 0; j < kSteps; ++j) {
-            const bool take = from[j] >= 0 && piece * 16 < D;
-            cp_async<8>(raw + (r0 + j * L::kRowsAtOnce) * (DT / 2) + piece * 8, base + (take ? from[j] + piece * 8 : 0), take);
-          }
-          if (D % 64 == 0) {
-            if (lane < kRows) {
-              const uint4 v = lds128(at + lane * 16);
-              const bool ok = (int32_t)v.y >= 0;
-              const uint8_t* src = scales + (ok ? (int64_t)((u64)v.z | (u64)v.w << 32) : 0);
-              if (D == 128) {
-                cp_async<8>(sd + lane * 16, src, ok);
-              } else if (D == 256) {
-                cp_async<16>(sd + lane * 16, src, ok);
-              } else {
-                for (int k = 0; k < D / 16; k += 4) cp_async<4>(sd + lane * 16 + k, src + k, ok);
-              }
-            }
-          } else {  // rows of an odd number of scale bytes: a lane to a byte
-            const int bytes = D / 16;
-            uint32_t b[(kRows * 15 + 31) / 32];
-#pragma unroll
-            for (int k = 0; k < (kRows * 15 + 31) / 32; ++k) {
-              const int x = lane + 32 * k, r = x / bytes;
-              b[k] = 0u;
-              if (r < kRows) {
-                const uint4 v = lds128(at + r * 16);
-                if ((int32_t)v.y >= 0) b[k] = scales[(int64_t)((u64)v.z | (u64)v.w << 32) + x - r * bytes];
-              }
-            }
-#pragma unroll
-            for (int k = 0; k < (kRows * 15 + 31) / 32; ++k) {
-              const int x = lane + 32 * k, r = x / bytes;
-              if (r < kRows) sts8(sd + r * 16 + x - r * bytes, b[k]);
+        if (D % 64 == 0) {  // scale bytes: half the lanes the keys' rows, half the values'
+          const int r = lane & (kRows - 1), kv = lane / kRows;
+          if (kv < 2) {
+            const uint4 x = lds128(at + r * 16);
+            const bool ok = (int32_t)x.y >= 0;
+            const uint8_t* src = (kv ? p.c.v_scales : p.c.k_scales) + (ok ? (int64_t)((u64)x.z | (u64)x.w << 32) : 0);
+            const uint32_t sd = raw + kv * C::kRawSlot + kCodes + r * 16;
+            if (D == 128) {
+              cp_async<8>(sd, src, ok);
+            } else if (D == 256) {
+              cp_async<16>(sd, src, ok);
+            } else {
+              for (int k = 0; k < D / 16; k += 4) cp_async<4>(sd + k, src + k, ok);
             }
           }
-          cp_commit();
-          if (q - sent >= C::kRawDepth - 1) hand_over(C::kRawDepth - 1);
+        } else {  // rows of an odd number of scale bytes: a lane to a byte
+          const int bytes = D / 16;
+          constexpr int kMost = (2 * kRows * 15 + 31) / 32;
+          uint32_t b[kMost];
+#pragma unroll
+          for (int k = 0; k < kMost; ++k) {
+            const int x = lane + 32 * k, y = x / bytes, r = y & (kRows - 1), kv = y / kRows;
+            b[k] = 0u;
+            if (kv < 2) {
+              const uint4 z = lds128(at + r * 16);
+              if ((int32_t)z.y >= 0)
+                b[k] = (kv ? p.c.v_scales : p.c.k_scales)[(int64_t)((u64)z.z | (u64)z.w << 32) + x - y * bytes];
+            }
+          }
+#pragma unroll
+          for (int k = 0; k < kMost; ++k) {
+            const int x = lane + 32 * k, y = x / bytes, r = y & (kRows - 1), kv = y / kRows;
+            if (kv < 2) sts8(raw + kv * C::kRawSlot + kCodes + r * 16 + x - y * bytes, b[k]);
+          }
         }
+        cp_commit();
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&sh.used[g % C::kAddresses]));
+        if (g - sent >= C::kRawDepth - 1) hand_over(C::kRawDepth - 1);
       }
     }
-    while (sent < q) hand_over((int)(q - sent - 1));
+    while (sent < g) hand_over((int)(g - sent - 1));
     cp_async_wait_all();
   }
   }
@@ -1387,7 +1420,7 @@ inline int row_tiles(const mixfp4_kv_cache* c, int64_t t, int64_t q_heads) {
   return c->head_dim <= 128 && t * (q_heads / c->heads) > 128 ? 2 : 1;
 }
 inline int tile_tokens(const mixfp4_kv_cache* c, int tiles) {
-  return c->head_dim <= 128 && (tiles == 2 || c->dtype == MIXFP4_CACHE_MIXFP4) ? 128 : 64;
+  return c->head_dim <= 128 && tiles == 1 && c->dtype == MIXFP4_CACHE_MIXFP4 ? 128 : 64;
 }
 // Key heads whose CTAs walk over the same tokens at the same time.
 inline int together_of(const mixfp4_kv_cache* c) {
