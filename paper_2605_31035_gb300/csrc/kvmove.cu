@@ -19,7 +19,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kInFlight = 4;
-constexpr int kMoveThreads = 128;  // of mixfp4_kv_accept, whose rows lie in shared memory between reading and writing
+constexpr int kMoveThreads = 128;  // of mixfp4_kv_accept
 constexpr int kMostDepth = 64;
 
 // One of a cache's arrays (keys, values, their scales), in bytes.
@@ -159,41 +159,57 @@ struct AcceptArgs {
   int32_t* lengths_out;
 };
 
-// A thread's column, the same bytes of every row: all its rows into shared memory, then out again.
+// A thread's column, the same bytes of every row.  Where the path rises, as one from a root to a leaf does whose drafts
+// come after their ancestors, no row is written before it has been read if rows go in order: draft path[k] >= k.  Eight at
+// a time then wait for memory together.  Any other path is read as a whole first, into the thread's own memory.
 template <int kBytes>
-__device__ __forceinline__ void move_column(uint8_t* col, const int64_t* from, const int64_t* to, int n, uint4* mine) {
+__device__ __forceinline__ void move_column(uint8_t* col, const int64_t* from, const int64_t* to, int n, bool rises) {
   typedef typename Piece<kBytes>::type T;
-#pragma unroll 8
-  for (int k = 0; k < n; ++k)
-    if (from[k] >= 0) *reinterpret_cast<T*>(mine + k * kMoveThreads) = Piece<kBytes>::load(col + from[k]);
-#pragma unroll 8
-  for (int k = 0; k < n; ++k)
-    if (from[k] >= 0) Piece<kBytes>::store(col + to[k], *reinterpret_cast<T*>(mine + k * kMoveThreads));
+  if (rises) {
+    constexpr int kBatch = 8;
+#pragma unroll 1
+    for (int k0 = 0; k0 < n; k0 += kBatch) {
+      T v[kBatch];
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k)
+        if (k0 + k < n && from[k0 + k] >= 0) v[k] = Piece<kBytes>::load(col + from[k0 + k]);
+#pragma unroll
+      for (int k = 0; k < kBatch; ++k)
+        if (k0 + k < n && from[k0 + k] >= 0) Piece<kBytes>::store(col + to[k0 + k], v[k]);
+    }
+  } else {
+    T v[kMostDepth];
+#pragma unroll 1
+    for (int k = 0; k < n; ++k)
+      if (from[k] >= 0) v[k] = Piece<kBytes>::load(col + from[k]);
+#pragma unroll 1
+    for (int k = 0; k < n; ++k)
+      if (from[k] >= 0) Piece<kBytes>::store(col + to[k], v[k]);
+  }
 }
 __device__ __forceinline__ void move_column(int bytes, uint8_t* col, const int64_t* from, const int64_t* to, int n,
-                                            uint4* mine) {
+                                            bool rises) {
   switch (bytes) {
-    case 16: return move_column<16>(col, from, to, n, mine);
-    case 8: return move_column<8>(col, from, to, n, mine);
-    case 4: return move_column<4>(col, from, to, n, mine);
-    default: return move_column<1>(col, from, to, n, mine);
+    case 16: return move_column<16>(col, from, to, n, rises);
+    case 8: return move_column<8>(col, from, to, n, rises);
+    case 4: return move_column<4>(col, from, to, n, rises);
+    default: return move_column<1>(col, from, to, n, rises);
   }
 }
 
 // A cluster of CTAs to a sequence; each thread moves whole columns, so no thread writes what another reads.
 __global__ void __launch_bounds__(kMoveThreads) kv_accept_kernel(const AcceptArgs a) {
-  extern __shared__ __align__(16) uint4 stage[];
   // Offsets of the moved rows in the arrays and in the scales; from < 0: the row stays.
   __shared__ int64_t from[2][kMostDepth], to[2][kMostDepth];
   __shared__ int sh_path[kMostDepth];
-  __shared__ int accepted;
+  __shared__ int accepted, falls;  // the path's length; whether some entry is no more than the one before it
   uint32_t rank, ranks;
   asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
   asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(ranks));
   const int64_t b = blockIdx.x / ranks;
   const int tid = threadIdx.x;
   const int n = max(a.lengths[b], 0), c = min(max(a.counts[b], 0), n), first = n - c;
-  if (tid == 0) accepted = a.depth;
+  if (tid == 0) accepted = a.depth, falls = 0;
   __syncthreads();
   if (tid < a.depth) {
     const int v = a.path[b * a.path_stride + tid];
@@ -220,6 +236,7 @@ __global__ void __launch_bounds__(kMoveThreads) kv_accept_kernel(const AcceptArg
     }
 #pragma unroll
     for (int s = 0; s < 2; ++s) from[s][tid] = ok ? off[0][s] : -1, to[s][tid] = off[1][s];
+    if (tid > 0 && sh_path[tid] <= sh_path[tid - 1]) falls = 1;
   }
   __syncthreads();
   const int row = a.pieces + a.spieces, columns = 2 * a.c.heads * row;
@@ -227,10 +244,10 @@ __global__ void __launch_bounds__(kMoveThreads) kv_accept_kernel(const AcceptArg
     const int hv = x / row, piece = x - hv * row, h = hv >> 1;
     if (piece < a.pieces) {
       uint8_t* col = static_cast<uint8_t*>(hv & 1 ? a.c.v : a.c.k) + h * a.c.head_stride * a.esize + piece * a.piece;
-      move_column(a.piece, col, from[0], to[0], moved, stage + tid);
+      move_column(a.piece, col, from[0], to[0], moved, !falls);
     } else {
       uint8_t* col = (hv & 1 ? a.c.v_scales : a.c.k_scales) + h * a.c.scale_head_stride + (piece - a.pieces) * a.spiece;
-      move_column(a.spiece, col, from[1], to[1], moved, stage + tid);
+      move_column(a.spiece, col, from[1], to[1], moved, !falls);
     }
   }
   // lengths_out may be lengths: written when every CTA of the cluster has read it.
@@ -392,16 +409,12 @@ int mixfp4_kv_accept(const mixfp4_kv_cache* cache, const int32_t* block_table, i
   int cluster = 1;
   while (cluster < 8 && cluster * kMoveThreads < columns) cluster *= 2;
   if (B * cluster > INT32_MAX) return MIXFP4_ERR_SHAPE;
-  static std::atomic<uint64_t> done{0};
-  if (!set_dynamic_smem_once(reinterpret_cast<const void*>(kv_accept_kernel), kMostDepth * kMoveThreads * 16, done))
-    return MIXFP4_ERR_CUDA;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = (unsigned)cluster, attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(B * cluster));
   cfg.blockDim = dim3(kMoveThreads);
-  cfg.dynamicSmemBytes = (size_t)depth * kMoveThreads * 16;
   cfg.stream = static_cast<cudaStream_t>(stream);
   cfg.attrs = attr;
   cfg.numAttrs = 1;

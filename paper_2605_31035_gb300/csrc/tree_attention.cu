@@ -49,9 +49,10 @@ constexpr int kRowCost = 2;
 // the sum a link, and 8192 tokens are 512 links (1024 with two parts of the weights).
 constexpr int kChainTokens = 8192;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-// How far a score may lie above the m of its weight 2^(s - m).  On a MixFP4 cache the weights are 2^7 times that:
-// at most 2^15 in f16, whose least value is then 2^-31 of the weight at m.
-constexpr float kSlack = 8.0f, kFp4Exp = 7.0f;
+// How far a score may lie above the m of its weight 2^(s - m), which follows the maximum from afar: bf16 parts and fp32
+// sums have the room.  On a MixFP4 cache the weights are 2^7 times that: at most 2^15 in f16, whose least value is then
+// 2^-31 of the weight at m.
+constexpr float kSlack = 16.0f, kFp4Slack = 8.0f, kFp4Exp = 7.0f;
 constexpr float kNoScore = -3e38f;  // m where no token has been seen: no difference to a score or to itself is NaN
 constexpr float kMostScore = 3.402823466e38f;  // m of a score of +inf, whose weight is then +inf instead of NaN
 constexpr unsigned kAll = 0xFFFFFFFFu;
@@ -83,7 +84,10 @@ struct TreeArgs {
   float2* stat;  // [2 grid][row tiles][128] (m, l) of parts
   float4* part;  // [2 grid][row tiles][dimensions / 4][128]: O of parts, and what a row in work has set aside
   uint32_t* status;
-  int box;  // rows of a bf16 page that one TMA copy brings; 0: cp.async does
+  int box;  // rows of a page that one TMA copy brings; 0: cp.async does
+  // A MixFP4 cache's scale bytes by TMA: bytes from one row's to the next in shared memory, and whether a copy brings
+  // those of neighbouring heads of a token (16 bytes) or of neighbouring tokens of a head.
+  int scale_pitch, scale_by_head;
 };
 
 // What of a sequence is looked at.
@@ -103,6 +107,7 @@ struct Part {
 template <int kSlots, int kAddresses, int kWords, int MT>
 struct Shared {
   uint64_t full[kSlots], empty[kSlots], placed[kAddresses], used[kAddresses];
+  uint64_t raw_full[3], raw_empty[3];
   // Of a buffer of scores: they are there, their weights are, O has taken those up.  No buffer has two uses under way, so
   // the parity of a wait tells one use from the next.
   uint64_t s_full[2 * MT], p_full[2 * MT], o_done[2 * MT];
@@ -120,6 +125,11 @@ struct Shared {
     uint64_t bits[kMostDrafts];
     int64_t scan[32];  // of the shares, before the first part
   };
+};
+
+// Tensor maps of keys and values, and of their scale bytes.
+struct Maps {
+  CUtensorMap rows[2], scales[2];
 };
 
 template <int DT, int MT, bool kFp4>
@@ -143,9 +153,10 @@ struct Cfg {
   static constexpr int kLeft = (kRegs * kThreads - kOtherRegs * (kThreads - kSoftmax * 32)) / (kSoftmax * 32) / 8 * 8;
   static constexpr int kSoftRegs = kLeft < 232 ? kLeft : 232;
   static constexpr int kRows = kTokens / kProducers;       // of a tile, to a producer warp
-  static constexpr int kRawSlot = kRows * (DT / 2 + 16);   // MixFP4 rows as they lie: codes, then scale bytes
+  static constexpr int kCodes = kTokens * (DT / 2);        // bytes of a MixFP4 tile's keys as they lie
+  static constexpr int kRawTile = 2 * kCodes + 2 * kTokens * 16;  // keys, values, their scale bytes (16 bytes to a row)
   static constexpr int kRawDepth = kFp4 ? 3 : 0;           // tiles
-  static constexpr int kRaw = kProducers * kRawDepth * 2 * kRawSlot;
+  static constexpr int kRaw = kRawDepth * kRawTile;
   static constexpr int kAddresses = kFp4 ? 2 : 0;          // tiles whose rows' places are known
   static constexpr int kPlaces = kAddresses * kTokens * 16;
   static constexpr int kWords = kTokens / 32;
@@ -376,6 +387,16 @@ __device__ __forceinline__ float lse_of(float m, float l) {
   return l == 0.0f ? -INFINITY : (m + log2f(l) - (kFp4 ? kFp4Exp : 0.0f)) * kLn2;
 }
 
+// The lowest k bits.
+__device__ __forceinline__ uint32_t below(int k) { return k <= 0 ? 0u : (k >= 32 ? kAll : (1u << k) - 1u); }
+// Which of the 32 tokens from a on, at column `col` of a tile, there are, a bit each; bit i of `good`: box i has a page.
+__device__ __forceinline__ uint32_t there_of(const TreeArgs& p, const Span& s, int a, int col, uint32_t good) {
+  uint32_t v = below(s.end - a) & ~below(s.low - a);
+  if (!((good >> (col / p.box)) & 1u)) v &= 0xFFFF0000u;
+  if (!((good >> ((col + 16) / p.box)) & 1u)) v &= 0xFFFFu;
+  return v;
+}
+
 // Which drafts draft k of sequence b sees, of its c.
 __device__ __forceinline__ uint64_t bits_of(const TreeArgs& p, int b, int k, int c) {
   const uint64_t all = c >= 64 ? ~0ull : (1ull << c) - 1;
@@ -399,11 +420,11 @@ template <int kSteps>
 struct Codes {
   uint2 c[kSteps];
   uint32_t scale[kSteps];
-  __device__ __forceinline__ void load(uint32_t codes, int step, uint32_t scales, int scale_step) {
+  __device__ __forceinline__ void load(uint32_t codes, int step, const uint32_t* scales, int behind) {
 #pragma unroll
     for (int j = 0; j < kSteps; ++j) {
       c[j] = lds64(codes + j * step);
-      scale[j] = lds8(scales + j * scale_step);
+      scale[j] = lds8(scales[j] + behind);
     }
   }
   // Rows row0, row0 + step ... of the block of 64 dimensions at `to`, 16-byte units u0 and u0 + 1.
@@ -425,14 +446,14 @@ struct Codes {
 };
 
 template <int DT, int MT, bool kFp4>
-__global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>::kCtas) tree_attention_kernel(const TreeArgs p, const __grid_constant__ CUtensorMap tm_k,
-                      const __grid_constant__ CUtensorMap tm_v) {
+__global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>::kCtas) tree_attention_kernel(const TreeArgs p, const __grid_constant__ Maps tm) {
   using C = Cfg<DT, MT, kFp4>;
   constexpr int TN = C::kTokens, CW = C::kCw, PW = C::kStep;
   extern __shared__ __align__(1024) uint8_t smem[];
   auto& sh = *reinterpret_cast<typename C::Sh*>(smem + C::kQ + C::kSlots * C::kSlot + C::kRaw + C::kPlaces);
   const uint32_t q_smem = smem_u32(smem), ring = q_smem + C::kQ;
-  [[maybe_unused]] const uint32_t places = ring + C::kSlots * C::kSlot + C::kRaw;  // [kAddresses][tokens] (row, scales)
+  [[maybe_unused]] const uint32_t raw_tiles = ring + C::kSlots * C::kSlot;  // [kRawDepth]
+  [[maybe_unused]] const uint32_t places = raw_tiles + C::kRaw;  // [kAddresses][tokens] (row, scales)
   volatile int* abort_flag = &sh.abort;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int share = (int)blockIdx.x / p.together, mate = (int)blockIdx.x % p.together;
@@ -446,6 +467,10 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
     for (int i = 0; i < C::kSlots; ++i) {
       mbar_init(smem_u32(&sh.full[i]), kFp4 ? C::kProducers : (p.box ? 1 : C::kProducers * 32));
       mbar_init(smem_u32(&sh.empty[i]), 1);
+    }
+    for (int i = 0; i < C::kRawDepth; ++i) {
+      mbar_init(smem_u32(&sh.raw_full[i]), 1);
+      mbar_init(smem_u32(&sh.raw_empty[i]), C::kProducers);
     }
     for (int i = 0; i < C::kAddresses; ++i) {
       mbar_init(smem_u32(&sh.placed[i]), 1);
@@ -674,7 +699,7 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
         const bool general = masked || !plain;
 
         bool slow = false;
-        const bool clear = !kFp4 && p.box && !whole && m == 0;
+        const bool clear = p.box && !whole && m == 0;
         if (uneven || clear) {
           const uint32_t q = 2 * g + 1, place_v = q % C::kSlots, at = ring + place_v * C::kSlot + tl * 128;
           waits(sh.full[place_v], (q / C::kSlots) & 1, 4u);
@@ -706,7 +731,6 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
           auto seen_of = [&](int col) -> uint32_t {
             const int a = j0 + col, x = w.s.first - a;
             const uint32_t have = there[col >> 5] >> (col & 31);
-            auto below = [](int k) -> uint32_t { return k <= 0 ? 0u : (k >= 32 ? kAll : (1u << k) - 1u); };
             uint32_t v = valid ? below(x) & ~below(low - a) : 0u;
             if (x <= 0)
               v |= x > -64 ? (uint32_t)(sees >> -x) : 0u;
@@ -785,20 +809,20 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
           else
             top *= fs;
           const float f = general ? 1.0f : fs;
-          if (__any_sync(kAll, top > mx + kSlack)) {
+          if (__any_sync(kAll, top > mx + (kFp4 ? kFp4Slack : kSlack))) {
             const float v = fminf(fmaxf(mx, top), kMostScore), cor = ex2(mx - v);  // 0 at the first score
             mx = v;
             l *= cor;
             if (!begins) {
               o_ready(8u);
 #pragma unroll 1
-              for (int d = 0; d < D; d += 16) {
-                uint32_t o[16];
-                tmem_load<16>(o_col + d, o);
-                tmem_loaded<16>(o);
+              for (int d = 0; d < D; d += 32) {  // columns behind D are nobody's
+                uint32_t o[32];
+                tmem_load<32>(o_col + d, o);
+                tmem_loaded<32>(o);
 #pragma unroll
-                for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * cor);
-                tmem_store<16>(o_col + d, o);
+                for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * cor);
+                tmem_store<32>(o_col + d, o);
               }
               tmem_st_wait();
             }
@@ -1150,12 +1174,7 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
           page = ask(it + 1);
           const uint32_t good = __ballot_sync(kAll, ok);  // bit i: box i % boxes
           if (kv == 0 && lane < TN / 32) {
-            const int a = j0 + lane * 32;
-            auto below = [](int k) -> uint32_t { return k <= 0 ? 0u : (k >= 32 ? kAll : (1u << k) - 1u); };
-            uint32_t there = below(w.s.end - a) & ~below(w.s.low - a);
-            if (!((good >> (lane * 32 / p.box)) & 1u)) there &= 0xFFFF0000u;
-            if (!((good >> ((lane * 32 + 16) / p.box)) & 1u)) there &= 0xFFFFu;
-            sh.there[g % kThere][lane] = there;
+            sh.there[g % kThere][lane] = there_of(p, w.s, j0 + lane * 32, lane * 32, good);
           }
           const uint32_t bytes = __popc(good) * p.box * 128;
           __syncwarp();
@@ -1166,7 +1185,7 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
           if (lane == 0) mbar_arrive_expect_tx(bar, bytes);
           __syncwarp();
           if (ok)
-            tma_load_4d(ring + slot * C::kSlot + block * C::kBlock + box * p.box * 128, kv ? &tm_v : &tm_k, block * 64, row,
+            tma_load_4d(ring + slot * C::kSlot + block * C::kBlock + box * p.box * 128, &tm.rows[kv], block * 64, row,
                         w.head, from, bar);
           __syncwarp();
         }
@@ -1223,69 +1242,117 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
       cp_async_wait_all();
     }
   } else if (warp < C::kSoftmax + 4) {
-    // ================================================= helpers: where a MixFP4 tile's rows lie, every other tile each
+    // ================================================= helpers of a MixFP4 cache's producers, every other tile each
     if constexpr (kFp4) {
-      const int me = warp - C::kSoftmax - 1;  // of two
-      uint32_t g = 0;
-      while (walk.next(p, mate, w)) {
+      const int me = warp - C::kSoftmax - 1;
+      uint32_t g = 0, asked = 0;  // tiles, and behind the last that this warp has asked for by TMA
+      // Boxes of this lane: keys' and values' codes, then their scale bytes.
+      const int boxes = p.box ? TN / p.box : 1, box = lane % boxes, what = lane / boxes;
+      const int box_pitch = (p.box * p.scale_pitch + 127) / 128 * 128;
+      while (!dead && walk.next(p, mate, w)) {
         const int32_t* table = p.table + (int64_t)w.b * p.table_stride;
+        auto page_of = [&](int tok) { return p.page_shift >= 0 ? tok >> p.page_shift : tok / p.c.page_size; };
+#pragma unroll 1
         for (int it = 0; it < w.tiles; ++it, ++g) {
           if ((int)(g & 1) != me) continue;
-          const uint32_t at = places + (g % C::kAddresses) * (TN * 16);
-          const int tok0 = w.s.from + (w.tile + w.tiles - 1 - it) * TN + lane;
-          int page[TN / 32];
-#pragma unroll
-          for (int j = 0; j < TN / 32; ++j) {
-            const int tok = tok0 + 32 * j;
-            page[j] = -1;
-            if (tok >= w.s.low && tok < w.s.end)
-              page[j] = table[p.page_shift >= 0 ? tok >> p.page_shift : tok / p.c.page_size];
-          }
-          waits(sh.used[g % C::kAddresses], ((g / C::kAddresses) & 1) ^ 1, 2048u);
-#pragma unroll
-          for (int j = 0; j < TN / 32; ++j) {
-            const int tok = tok0 + 32 * j;
-            const int off = p.page_shift >= 0 ? tok & (p.c.page_size - 1) : tok % p.c.page_size;
-            const bool ok = page[j] >= 0 && page[j] < p.c.pages;
-            int64_t x = -1, y = 0;
+          const int j0 = w.s.from + (w.tile + w.tiles - 1 - it) * TN;
+          if (p.box) {
+            const int tok = j0 + box * p.box, in_table = page_of(tok);
+            const int page = tok < w.s.end && tok + p.box > w.s.low ? table[in_table] : -1;
+            const bool here = page >= 0 && page < p.c.pages, ok = here && what < 4;
+            const uint32_t good = __ballot_sync(kAll, here), n = g % C::kRawDepth, bar = smem_u32(&sh.raw_full[n]);
+            if (lane < TN / 32) sh.there[g % kThere][lane] = there_of(p, w.s, j0 + lane * 32, lane * 32, good);
+            __syncwarp();
+            waits(sh.raw_empty[n], ((g / C::kRawDepth) & 1) ^ 1, 1u << 18);
+            if (dead) break;
+            const int bytes = what < 2 ? p.box * (D / 2) : (p.scale_by_head ? p.box * 16 : p.box * (D / 16));
+            const int all = __reduce_add_sync(kAll, ok ? bytes : 0);
+            if (lane == 0) mbar_arrive_expect_tx(bar, (uint32_t)all);
+            __syncwarp();
             if (ok) {
-              x = (int64_t)page[j] * p.c.page_stride + (int64_t)off * p.c.token_stride + (int64_t)w.head * p.c.head_stride;
-              y = (int64_t)page[j] * p.c.scale_page_stride + (int64_t)off * p.c.scale_token_stride +
-                  (int64_t)w.head * p.c.scale_head_stride;
+              const int row = tok - in_table * p.c.page_size, kv = what & 1;
+              const uint32_t to = raw_tiles + n * C::kRawTile;
+              if (what < 2)
+                tma_load_4d(to + kv * C::kCodes + box * p.box * (D / 2), &tm.rows[kv], 0, row, w.head, page, bar);
+              else if (p.scale_by_head)
+                tma_load_4d(to + 2 * C::kCodes + kv * TN * 16 + box * box_pitch, &tm.scales[kv], w.head * (D / 16) & ~15, row, 0,
+                            page, bar);
+              else
+                tma_load_4d(to + 2 * C::kCodes + kv * TN * 16 + box * box_pitch, &tm.scales[kv], D == 256 ? 2 * row : row, 0, w.head,
+                            page, bar);
             }
-            sts128(at + (32 * j + lane) * 16, (uint32_t)x, (uint32_t)(x >> 32), (uint32_t)y, (uint32_t)(y >> 32));
-            const uint32_t there = __ballot_sync(kAll, ok);
-            if (lane == 0) sh.there[g % kThere][j] = there;
+            __syncwarp();
+            asked = g + 1;
+          } else {  // where each row lies
+            const uint32_t at = places + (g % C::kAddresses) * (TN * 16);
+            int page[TN / 32];
+#pragma unroll
+            for (int j = 0; j < TN / 32; ++j) {
+              const int tok = j0 + 32 * j + lane;
+              page[j] = tok >= w.s.low && tok < w.s.end ? table[page_of(tok)] : -1;
+            }
+            waits(sh.used[g % C::kAddresses], ((g / C::kAddresses) & 1) ^ 1, 2048u);
+#pragma unroll
+            for (int j = 0; j < TN / 32; ++j) {
+              const int tok = j0 + 32 * j + lane, off = tok - page_of(tok) * p.c.page_size;
+              const bool ok = page[j] >= 0 && page[j] < p.c.pages;
+              int64_t x = -1, y = 0;
+              if (ok) {
+                x = (int64_t)page[j] * p.c.page_stride + (int64_t)off * p.c.token_stride + (int64_t)w.head * p.c.head_stride;
+                y = (int64_t)page[j] * p.c.scale_page_stride + (int64_t)off * p.c.scale_token_stride +
+                    (int64_t)w.head * p.c.scale_head_stride;
+              }
+              sts128(at + (32 * j + lane) * 16, (uint32_t)x, (uint32_t)(x >> 32), (uint32_t)y, (uint32_t)(y >> 32));
+              const uint32_t there = __ballot_sync(kAll, ok);
+              if (lane == 0) sh.there[g % kThere][j] = there;
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&sh.placed[g % C::kAddresses]));
           }
-          __syncwarp();
-          if (lane == 0) mbar_arrive(smem_u32(&sh.placed[g % C::kAddresses]));
         }
       }
+      if (dead && asked > 0)  // the copies in flight land before the CTA ends
+        mbar_wait(smem_u32(&sh.raw_full[(asked - 1) % C::kRawDepth]), ((asked - 1) / C::kRawDepth) & 1, nullptr, kWaitLimitNs);
     }
   } else if constexpr (kFp4) {
     // ================================================= producers of a MixFP4 cache: codes in, f16 out
     const int pw = warp - C::kSoftmax - 4;
     using L = Lanes<DT>;
     const int piece = L::piece(lane), r0 = L::row(lane);
-    const uint32_t raw0 = ring + C::kSlots * C::kSlot + pw * C::kRawDepth * 2 * C::kRawSlot;
-    constexpr int kRows = C::kRows, kSteps = kRows / L::kRowsAtOnce, kCodes = kRows * (DT / 2);
+    constexpr int kRows = C::kRows, kSteps = kRows / L::kRowsAtOnce;
+    const int row0 = pw * kRows, pitch = p.box ? D / 2 : DT / 2;  // rows of codes lie as TMA puts them, or apart
     uint32_t g = 0, sent = 0;  // tiles asked for, tiles decoded
     // The oldest tile not decoded yet, with `later` behind it: once it has landed, for the tensor cores.
+    const int box_shift = p.box ? __ffs(p.box) - 1 : 31, box_pitch = (p.box * p.scale_pitch + 127) / 128 * 128;
     auto hand_over = [&](int later) {
-      cp_wait_at_most(later);
-      __syncwarp();
-      const uint32_t raw = raw0 + (sent % C::kRawDepth) * 2 * C::kRawSlot;
+      const uint32_t n = sent % C::kRawDepth, raw = raw_tiles + n * C::kRawTile;
+      if (p.box)
+        wait(sh.raw_full[n], (sent / C::kRawDepth) & 1, 1u << 19);
+      else
+        cp_wait_at_most(later);
+      dead = __any_sync(kAll, dead);
       Codes<kSteps> c[2];
+      uint32_t scales[kSteps];  // where a row's scale byte lies
+#pragma unroll
+      for (int j = 0; j < kSteps; ++j) {
+        const int r = row0 + r0 + j * L::kRowsAtOnce;
+        scales[j] = raw + 2 * C::kCodes + piece +
+                    (p.box ? (r >> box_shift) * box_pitch + (r & (p.box - 1)) * p.scale_pitch +
+                                 (p.scale_by_head ? w.head * (D / 16) & 15 : 0)
+                           : r * 16);
+      }
 #pragma unroll
       for (int kv = 0; kv < 2; ++kv)
-        if (piece * 16 < D) c[kv].load(raw + kv * C::kRawSlot + r0 * (DT / 2) + piece * 8, L::kRowsAtOnce * (DT / 2),
-                                       raw + kv * C::kRawSlot + kCodes + r0 * 16 + piece, L::kRowsAtOnce * 16);
+        if (piece * 16 < D)
+          c[kv].load(raw + kv * C::kCodes + (row0 + r0) * pitch + piece * 8, L::kRowsAtOnce * pitch, scales, kv * TN * 16);
+      __syncwarp();
+      if (p.box && lane == 0) mbar_arrive(smem_u32(&sh.raw_empty[n]));
 #pragma unroll
       for (int kv = 0; kv < 2; ++kv) {
         const uint32_t q = 2 * sent + kv, slot = q % C::kSlots;
         waits(sh.empty[slot], ((q / C::kSlots) & 1) ^ 1, 1024u);
         if (piece * 16 < D)
-          c[kv].decode(ring + slot * C::kSlot + (piece >> 2) * C::kBlock, pw * kRows + r0, L::kRowsAtOnce, (piece & 3) * 2);
+          c[kv].decode(ring + slot * C::kSlot + (piece >> 2) * C::kBlock, row0 + r0, L::kRowsAtOnce, (piece & 3) * 2);
         fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&sh.full[slot]));
@@ -1295,26 +1362,30 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
     while (walk.next(p, mate, w)) {
 #pragma unroll 1
       for (int it = 0; it < w.tiles; ++it, ++g) {
+        if (p.box) {
+          hand_over(0);
+          continue;
+        }
         waits(sh.placed[g % C::kAddresses], (g / C::kAddresses) & 1, 4096u);
-        const uint32_t at = places + (g % C::kAddresses) * (TN * 16) + pw * kRows * 16;
-        const uint32_t raw = raw0 + (g % C::kRawDepth) * 2 * C::kRawSlot;
+        const uint32_t at = places + (g % C::kAddresses) * (TN * 16) + row0 * 16;
+        const uint32_t raw = raw_tiles + (g % C::kRawDepth) * C::kRawTile, scales = raw + 2 * C::kCodes + row0 * 16;
 #pragma unroll
         for (int j = 0; j < kSteps; ++j) {
           const int r = r0 + j * L::kRowsAtOnce;
           const uint2 x = lds64(at + r * 16);
           const bool take = (int32_t)x.y >= 0 && piece * 16 < D;
           const int64_t from = take ? (int64_t)((u64)x.x | (u64)x.y << 32) + piece * 8 : 0;
-          const uint32_t to = raw + r * (DT / 2) + piece * 8;
+          const uint32_t to = raw + (row0 + r) * pitch + piece * 8;
           cp_async<8>(to, static_cast<const uint8_t*>(p.c.k) + from, take);
-          cp_async<8>(to + C::kRawSlot, static_cast<const uint8_t*>(p.c.v) + from, take);
+          cp_async<8>(to + C::kCodes, static_cast<const uint8_t*>(p.c.v) + from, take);
         }
-        if (D % 64 == 0) {  // scale bytes: half the lanes the keys' rows, half the values'
+        if (D % 64 == 0) {  // scale bytes: some lanes the keys' rows, as many the values'
           const int r = lane & (kRows - 1), kv = lane / kRows;
           if (kv < 2) {
             const uint4 x = lds128(at + r * 16);
             const bool ok = (int32_t)x.y >= 0;
             const uint8_t* src = (kv ? p.c.v_scales : p.c.k_scales) + (ok ? (int64_t)((u64)x.z | (u64)x.w << 32) : 0);
-            const uint32_t sd = raw + kv * C::kRawSlot + kCodes + r * 16;
+            const uint32_t sd = scales + (kv * TN + r) * 16;
             if (D == 128) {
               cp_async<8>(sd, src, ok);
             } else if (D == 256) {
@@ -1340,7 +1411,7 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
 #pragma unroll
           for (int k = 0; k < kMost; ++k) {
             const int x = lane + 32 * k, y = x / bytes, r = y & (kRows - 1), kv = y / kRows;
-            if (kv < 2) sts8(raw + kv * C::kRawSlot + kCodes + r * 16 + x - y * bytes, b[k]);
+            if (kv < 2) sts8(scales + (kv * TN + r) * 16 + x - y * bytes, b[k]);
           }
         }
         cp_commit();
@@ -1433,38 +1504,83 @@ inline int grid_of(const mixfp4_kv_cache* c, int tiles) {
   return ctas / together_of(c) * together_of(c);
 }
 
-// Rows that one TMA copy of a bf16 cache brings: of one page, and a part of a tile; 0 where TMA's rules do not allow it
-// (pages of no multiple of 16 tokens, rows of less than 64 elements, whose copies would not fill the operand's).
+// Whether scale bytes of neighbouring heads, or of a head's neighbouring tokens, lie together and at multiples of 16
+// bytes: TMA brings no less than 16, from such an address on.
+inline bool scales_by_head(const mixfp4_kv_cache& c) {
+  const int64_t n = c.head_dim / 16;
+  return 16 % n == 0 && c.heads * n % 16 == 0 && (c.scale_head_stride == n || c.heads == 1) &&
+         (c.scale_token_stride | c.scale_page_stride) % 16 == 0 && aligned(c.k_scales, 16) && aligned(c.v_scales, 16);
+}
+inline bool scales_by_token(const mixfp4_kv_cache& c) {
+  const int64_t n = c.head_dim / 16;
+  return 16 % n == 0 && c.scale_token_stride == n && (c.scale_head_stride | c.scale_page_stride) % 16 == 0 &&
+         aligned(c.k_scales, 16) && aligned(c.v_scales, 16);
+}
+// Rows that one TMA copy brings: of one page, and a part of a tile; 0 where TMA's rules do not allow it (pages of no
+// multiple of 16 tokens, rows of codes that are no multiple of 16 bytes or lie on none) or bf16 rows of less than 64
+// elements would not fill the operand's.
 inline int box_of(const mixfp4_kv_cache& c, int tokens) {
-  if (c.page_size % 16 != 0 || c.head_dim < 64 || c.pages == 0) return 0;
+  const bool fp4 = c.dtype == MIXFP4_CACHE_MIXFP4;
+  if (c.page_size % 16 != 0 || c.pages == 0 || (fp4 ? c.head_dim % 32 != 0 : c.head_dim < 64)) return 0;
+  if (fp4 && (!aligned(c.k, 16) || !aligned(c.v, 16) || (c.token_stride | c.head_stride | c.page_stride) % 16 ||
+              (!scales_by_head(c) && !scales_by_token(c))))
+    return 0;
   int n = 16;
   while (n < tokens && c.page_size % (2 * n) == 0) n *= 2;
   return n;
 }
+// Boxes of 64 elements of bf16 rows, swizzled as the operands are, or whole rows of codes as they lie.
 inline bool make_map_rows(CUtensorMap* m, const void* base, const mixfp4_kv_cache& c, int box) {
   auto fn = encode_fn();
   if (!fn) return false;
+  const bool fp4 = c.dtype == MIXFP4_CACHE_MIXFP4;
+  const int row = fp4 ? c.head_dim / 2 : c.head_dim, esize = fp4 ? 1 : 2;
   // An axis of one element has any stride; 32 bytes will do.
-  auto bytes = [](int64_t stride, int64_t n) { return (cuuint64_t)(n > 1 ? stride * 2 : 32); };
-  cuuint64_t dims[4] = {(cuuint64_t)c.head_dim, (cuuint64_t)c.page_size, (cuuint64_t)c.heads, (cuuint64_t)c.pages};
+  auto bytes = [&](int64_t stride, int64_t n) { return (cuuint64_t)(n > 1 ? stride * esize : 32); };
+  cuuint64_t dims[4] = {(cuuint64_t)row, (cuuint64_t)c.page_size, (cuuint64_t)c.heads, (cuuint64_t)c.pages};
   cuuint64_t strides[3] = {bytes(c.token_stride, c.page_size), bytes(c.head_stride, c.heads), bytes(c.page_stride, c.pages)};
-  cuuint32_t boxes[4] = {64, (cuuint32_t)box, 1, 1};
+  cuuint32_t boxes[4] = {(cuuint32_t)(fp4 ? row : 64), (cuuint32_t)box, 1, 1};
   cuuint32_t estr[4] = {1, 1, 1, 1};
-  return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, boxes, estr,
-            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+  return fn(m, fp4 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims,
+            strides, boxes, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            fp4 ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Boxes of 16 bytes of a token's scale bytes, or of `box` tokens' of a head.
+inline bool make_map_scales(CUtensorMap* m, const void* base, const mixfp4_kv_cache& c, int box) {
+  auto fn = encode_fn();
+  if (!fn) return false;
+  const int n = c.head_dim / 16;
+  const bool by_head = scales_by_head(c);
+  // Of a head's tokens, elements of 4 or 8 bytes: a box has at most 256 of them along an axis.
+  const int per_token = by_head ? n : (n == 16 ? 2 : 1);
+  const auto type = by_head ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : (n == 4 ? CU_TENSOR_MAP_DATA_TYPE_INT32 : CU_TENSOR_MAP_DATA_TYPE_INT64);
+  auto bytes = [](int64_t stride, int64_t count) { return (cuuint64_t)(count > 1 ? stride : 32); };
+  cuuint64_t dims[4] = {(cuuint64_t)(by_head ? c.heads : c.page_size) * per_token, (cuuint64_t)(by_head ? c.page_size : 1),
+                        (cuuint64_t)(by_head ? 1 : c.heads), (cuuint64_t)c.pages};
+  cuuint64_t strides[3] = {bytes(c.scale_token_stride, (int64_t)dims[1]), bytes(c.scale_head_stride, (int64_t)dims[2]),
+                           bytes(c.scale_page_stride, c.pages)};
+  cuuint32_t boxes[4] = {(cuuint32_t)(by_head ? 16 : box * per_token), (cuuint32_t)(by_head ? box : 1), 1, 1};
+  cuuint32_t estr[4] = {1, 1, 1, 1};
+  return fn(m, type, 4, const_cast<void*>(base), dims, strides, boxes, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 template <int DT, int MT, bool kFp4>
 int launch(TreeArgs p, int grid, cudaStream_t s) {
   using C = Cfg<DT, MT, kFp4>;
-  CUtensorMap maps[2] = {};
-  p.box = kFp4 ? 0 : box_of(p.c, C::kTokens);
-  if (p.box && !(make_map_rows(&maps[0], p.c.k, p.c, p.box) && make_map_rows(&maps[1], p.c.v, p.c, p.box))) p.box = 0;
+  Maps maps = {};
+  p.box = box_of(p.c, C::kTokens);
+  if (p.box && kFp4) p.scale_by_head = scales_by_head(p.c), p.scale_pitch = p.scale_by_head ? 16 : p.c.head_dim / 16;
+  if (p.box && !(make_map_rows(&maps.rows[0], p.c.k, p.c, p.box) && make_map_rows(&maps.rows[1], p.c.v, p.c, p.box) &&
+                 (!kFp4 || (make_map_scales(&maps.scales[0], p.c.k_scales, p.c, p.box) &&
+                            make_map_scales(&maps.scales[1], p.c.v_scales, p.c, p.box)))))
+    p.box = 0;
   static std::atomic<uint64_t> done{0};
   auto* kernel = tree_attention_kernel<DT, MT, kFp4>;
   if (!set_dynamic_smem_once(reinterpret_cast<const void*>(kernel), C::kSmem, done)) return MIXFP4_ERR_CUDA;
-  kernel<<<grid, C::kThreads, C::kSmem, s>>>(p, maps[0], maps[1]);
+  kernel<<<grid, C::kThreads, C::kSmem, s>>>(p, maps);
   if (int st = launch_status()) return st;
   if (!p.joined) return MIXFP4_OK;
   const int rows = p.t * p.group < 128 * MT ? p.t * p.group : 128 * MT;
