@@ -772,7 +772,7 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
               if (!masked) {
                 const float far0 = (float)(place - a);
 #pragma unroll
-                for (int e = 0; e < 32; ++e) {
+                for (int e = 0; e < PW; ++e) {
                   if (e == 16 && narrow) break;
                   float x = shaped(v[e]);
                   if (p.slopes) x = fmaf(slope, far0 - (float)e, x);
@@ -782,7 +782,7 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
               } else {
                 const uint32_t seen = seen_of(c);
 #pragma unroll
-                for (int e = 0; e < 32; ++e) {
+                for (int e = 0; e < PW; ++e) {
                   if (e == 16 && narrow) break;
                   float x = shaped(v[e]);
                   if (p.slopes) {
@@ -1553,9 +1553,12 @@ inline bool make_map_scales(CUtensorMap* m, const void* base, const mixfp4_kv_ca
   if (!fn) return false;
   const int n = c.head_dim / 16;
   const bool by_head = scales_by_head(c);
-  // Of a head's tokens, elements of 4 or 8 bytes: a box has at most 256 of them along an axis.
+  // Of a head's tokens, elements of 2 to 8 bytes: a box has at most 256 of them along an axis.
   const int per_token = by_head ? n : (n == 16 ? 2 : 1);
-  const auto type = by_head ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : (n == 4 ? CU_TENSOR_MAP_DATA_TYPE_INT32 : CU_TENSOR_MAP_DATA_TYPE_INT64);
+  const auto type = by_head  ? CU_TENSOR_MAP_DATA_TYPE_UINT8
+                    : n == 2 ? CU_TENSOR_MAP_DATA_TYPE_UINT16
+                    : n == 4 ? CU_TENSOR_MAP_DATA_TYPE_INT32
+                             : CU_TENSOR_MAP_DATA_TYPE_INT64;
   auto bytes = [](int64_t stride, int64_t count) { return (cuuint64_t)(count > 1 ? stride : 32); };
   cuuint64_t dims[4] = {(cuuint64_t)(by_head ? c.heads : c.page_size) * per_token, (cuuint64_t)(by_head ? c.page_size : 1),
                         (cuuint64_t)(by_head ? 1 : c.heads), (cuuint64_t)c.pages};

@@ -176,6 +176,70 @@ def test_every_number_of_rows(fp4, rows):
 
 
 @pytest.mark.parametrize("fp4", [False, True])
+@pytest.mark.parametrize("Hkv,D,page,layout", [(8, 128, 16, "nhd"), (8, 128, 128, "hnd"), (1, 128, 64, "nhd"),
+                                               (3, 128, 32, "kv"), (4, 64, 16, "nhd"), (4, 64, 256, "hnd"), (8, 32, 16, "nhd"),
+                                               (2, 32, 48, "hnd"), (1, 256, 16, "nhd"), (3, 256, 128, "hnd"),
+                                               (2, 96, 64, "hnd"), (5, 160, 16, "nhd"), (2, 64, 24, "nhd")])
+def test_layouts(fp4, Hkv, D, page, layout):
+    """Rows and scale bytes as the copies of each way into shared memory find them: whole pages, parts, heads together or
+    apart, pages that are not a multiple of 16."""
+    run(fp4, [300, 1000, 5, 129], None, 5, 2 * Hkv, Hkv, D, page, layout=layout, window=0, seed=D + page)
+    run(fp4, [300, 1000, 5, 129], [5, 2, 5, 1], 5, 2 * Hkv, Hkv, D, page, layout=layout, window=150, seed=D + page + 1)
+
+
+@pytest.mark.parametrize("fp4", [False, True])
+@pytest.mark.parametrize("B,longest,t,D,Hq,Hkv", [(3, 9000, 24, 128, 8, 2), (3, 9000, 8, 128, 8, 2), (3, 9000, 16, 128, 8, 2),
+                                                  (20, 3000, 24, 128, 32, 8), (3, 9000, 64, 128, 8, 2),
+                                                  (5, 2000, 7, 256, 4, 1), (30, 500, 3, 64, 8, 2)])
+def test_same_results_every_time(fp4, B, longest, t, D, Hq, Hkv):
+    """No result depends on which warp, copy or product comes first."""
+    o = ops()
+    g = random.Random(B)
+    lengths = [g.randint(1, longest) for _ in range(B)]
+    counts = [g.randint(0, t) for _ in range(B)]
+    cache, table, _, _ = pa.build(fp4, lengths, Hkv, D, 16, seed=B)
+    q = (randn(B, t, Hq, D, seed=5) * 1.5).to(torch.bfloat16)
+    mask = ints([signed(m) for m in tree(t, B)], torch.int64)
+    first, lse = o.mixfp4_tree_attention(q, cache, table, ints(lengths), mask=mask, counts=ints(counts), return_lse=True)
+    for _ in range(40):
+        out, l2 = o.mixfp4_tree_attention(q, cache, table, ints(lengths), mask=mask, counts=ints(counts), return_lse=True)
+        assert torch.equal(out, first) and torch.equal(l2, lse)
+
+
+@pytest.mark.parametrize("fp4", [False, True])
+@pytest.mark.parametrize("t,n,B", [(2, 140000, 20), (33, 150000, 10)])
+def test_parts_of_many_tiles(fp4, t, n, B):
+    """Parts of rows of more than 8192 tokens to a CTA, whose sums are set aside on the way; page numbers are in
+    any order."""
+    o = ops()
+    D, page, Hq = 64, 16, 4
+    pages = B * (n // page)
+    g = torch.Generator(DEV).manual_seed(t)
+    if fp4:
+        parts = [torch.randint(0, 256, (pages, page, 1, D // 2), generator=g, device=DEV, dtype=torch.uint8) for _ in range(2)]
+        parts += [torch.randint(0x30, 0x38, (pages, page, 1, D // 16), generator=g, device=DEV, dtype=torch.uint8)
+                  for _ in range(2)]
+        one = torch.ones(1, device=DEV)
+        cache = o.KVCache(*parts, one * 0.25, one)
+    else:
+        cache = o.KVCache(*(torch.randn(pages, page, 1, D, generator=g, device=DEV).to(torch.bfloat16) for _ in range(2)))
+    table = torch.randperm(pages, generator=g, device=DEV).to(torch.int32).view(B, -1)
+    q = (randn(B, t, Hq, D, seed=5) * 1.5).to(torch.bfloat16)
+    out, lse = o.mixfp4_tree_attention(q, cache, table, ints([n] * B), return_lse=True)
+    for b in (0, B // 2, B - 1):
+        slots = (table[b].long()[:, None] * page + torch.arange(page, device=DEV)).reshape(-1)
+        k, v = (x.double() for x in o.mixfp4_kv_gather(cache, slots, torch.float32))
+        for i in (0, t - 1):
+            m = n - t + 1 + i
+            s = torch.einsum("hd,nd->hn", q[b, i].double(), k[:m, 0]) * D ** -0.5
+            p = s.softmax(-1)
+            A = p @ v[:m, 0].abs()
+            bound = 2.0 ** -10.5 * A + 2.0 ** -32 * v[:m, 0].abs().sum(0) if fp4 else 2.0 ** -13 * A
+            pa.within(out[b, i], p @ v[:m, 0], bound)
+            assert torch.all((lse[b, i].double() - torch.logsumexp(s, -1)).abs() <= 2.0 ** -17 * (1 + s.abs().amax(-1)))
+
+
+@pytest.mark.parametrize("fp4", [False, True])
 @pytest.mark.parametrize("B,longest,t,D", [(1, 30000, 3, 64), (3, 9000, 24, 128), (150, 300, 2, 64), (700, 40, 1, 128),
                                            (1500, 20, 3, 16)])
 def test_many_shares(fp4, B, longest, t, D):
@@ -395,6 +459,9 @@ def test_strides_workspace_and_stream(fp4):
     torch.testing.assert_close(got, ref[2:], rtol=2.0 ** -7, atol=2.0 ** -9)
     with pytest.raises(o.MixFP4Error, match="invalid shape"):
         o.mixfp4_tree_attention(q, cache, table, n, workspace=ws[:need - 1])
+    status = torch.full((1,), 7, dtype=torch.int32, device=DEV)
+    got = o.mixfp4_tree_attention(q, cache, table, n, mask=mask, status_word=status)
+    assert torch.equal(got, ref) and int(status) == 0
 
 
 def test_two_calls_at_once():
