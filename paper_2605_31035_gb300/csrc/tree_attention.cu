@@ -53,6 +53,8 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // sums have the room.  On a MixFP4 cache the weights are 2^7 times that: at most 2^15 in f16, whose least value is then
 // 2^-31 of the weight at m.
 constexpr float kSlack = 16.0f, kFp4Slack = 8.0f, kFp4Exp = 7.0f;
+// A MixFP4 operand's elements are their values under the block scale over this (fp4_to_f16).
+constexpr float kFp4Unit = 512.0f;
 constexpr float kNoScore = -3e38f;  // m where no token has been seen: no difference to a score or to itself is NaN
 constexpr float kMostScore = 3.402823466e38f;  // m of a score of +inf, whose weight is then +inf instead of NaN
 constexpr unsigned kAll = 0xFFFFFFFFu;
@@ -104,7 +106,7 @@ struct Part {
   int64_t behind;  // the unit behind the row's last
 };
 
-template <int kSlots, int kAddresses, int kWords, int MT>
+template <int kSlots, int kAddresses, int kWords, int MT, bool kFp4>
 struct Shared {
   uint64_t full[kSlots], empty[kSlots], placed[kAddresses], used[kAddresses];
   uint64_t raw_full[3], raw_empty[3];
@@ -120,6 +122,7 @@ struct Shared {
   uint32_t there[kThere][kWords];  // of a tile, which of its tokens there are
   // The part that softmax is at, read ahead by a warp of its own: which drafts each draft sees, and how many.
   uint8_t depth[kMostDrafts];
+  uint8_t exponent[kFp4 ? MT * 128 : 8];  // of a row's largest query element
   Part part;
   union {
     uint64_t bits[kMostDrafts];
@@ -162,10 +165,10 @@ struct Cfg {
   static constexpr int kWords = kTokens / 32;
   static constexpr int kRoom = (kCtas == 2 ? 113 : 227) * 1024 - kQ - kRaw - kPlaces;
   static constexpr int slots(int n) {  // as many as there is room for
-    return n == 1 || n * (kSlot + 16) + (int)sizeof(Shared<1, kFp4 ? 2 : 1, kWords, MT>) <= kRoom ? n : slots(n - 1);
+    return n == 1 || n * (kSlot + 16) + (int)sizeof(Shared<1, kFp4 ? 2 : 1, kWords, MT, kFp4>) <= kRoom ? n : slots(n - 1);
   }
   static constexpr int kSlots = slots(kMostSlots);
-  using Sh = Shared<kSlots, kFp4 ? 2 : 1, kWords, MT>;
+  using Sh = Shared<kSlots, kFp4 ? 2 : 1, kWords, MT, kFp4>;
   static constexpr int kSmem = kQ + kSlots * kSlot + kRaw + kPlaces + (int)sizeof(Sh);
   static_assert(kSlots >= 3 && sizeof(Sh) % 8 == 0 && kSmem <= (kCtas == 2 ? 113 : 227) * 1024);
   static constexpr uint32_t kScoreCols = 2 * MT * kTokens; // of tensor memory, O behind them
@@ -238,16 +241,24 @@ __device__ __forceinline__ float rcp(float x) {
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-// tanh within 2^-21 of itself: x P(x^2) / Q(x^2) for |x| <= 9, beyond which it is 1 in fp32.  The coefficients are a
-// weighted least-squares fit of tanh(x) / x that evens out the relative error (2e-8 before rounding).
-__device__ __forceinline__ float tanh_of(float x) {
-  const float z = fminf(fmaxf(x, -9.0f), 9.0f), y = z * z;
-  float a = fmaf(y, 1.335449179e-08f, 2.060896267e-05f), b = fmaf(y, 7.776489695e-07f, 3.285623034e-04f);
-  a = fmaf(y, a, 3.495580968e-03f), b = fmaf(y, b, 2.587695507e-02f);
-  a = fmaf(y, a, 1.338101964e-01f), b = fmaf(y, b, 4.671433524e-01f);
-  a = fmaf(y, a, 1.0f), b = fmaf(y, b, 1.0f);
-  const float r = fminf(fmaxf(z * a * rcp(b), -1.0f), 1.0f);
-  return x != x ? x : r;
+// tanh of two numbers, within 2^-21 of itself: x P(x^2) / Q(x^2) for |x| <= 9, beyond which it is 1 in fp32.  The
+// coefficients are a weighted least-squares fit of tanh(x) / x that evens out the relative error (2e-8 before rounding).
+// Written out for pairs, on which fp32 products and sums work at once: 11 instructions to a number instead of 17.
+__device__ __forceinline__ void tanh2(float& x0, float& x1) {
+  auto held = [](float x) {  // NaN stays
+    float y;
+    asm("{ .reg .f32 t; max.NaN.f32 t, %1, 0fC1100000; min.NaN.f32 %0, t, 0f41100000; }" : "=f"(y) : "f"(x));
+    return y;
+  };
+  auto both = [](float c) { return pack2(c, c); };
+  const u64 z = pack2(held(x0), held(x1)), y = mul2(z, z);
+  u64 a = fma2(y, both(1.335449179e-08f), both(2.060896267e-05f)), b = fma2(y, both(7.776489695e-07f), both(3.285623034e-04f));
+  a = fma2(y, a, both(3.495580968e-03f)), b = fma2(y, b, both(2.587695507e-02f));
+  a = fma2(y, a, both(1.338101964e-01f)), b = fma2(y, b, both(4.671433524e-01f));
+  a = fma2(y, a, both(1.0f)), b = fma2(y, b, both(1.0f));
+  float b0, b1;
+  unpack2(b, b0, b1);
+  unpack2(mul2(mul2(z, a), pack2(rcp(b0), rcp(b1))), x0, x1);
 }
 // As mma_f16_tmem_a, lanes of D whose bit is set in the four words left as they are.
 __device__ __forceinline__ void mma_f16_tmem_a_lanes(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc,
@@ -380,7 +391,7 @@ struct Walk {
 // are -inf); NaN goes through, and so does the +inf of a score of +inf.
 template <bool kFp4>
 __device__ __forceinline__ float out_factor(float l, float vts) {
-  return l == 0.0f ? 0.0f : (kFp4 ? 0.5f * vts : 1.0f) / l;
+  return l == 0.0f ? 0.0f : (kFp4 ? kFp4Unit * vts : 1.0f) / l;
 }
 template <bool kFp4>
 __device__ __forceinline__ float lse_of(float m, float l) {
@@ -414,33 +425,46 @@ struct Lanes {
   static __device__ __forceinline__ int row(int lane) { return (lane >> 2 & 1) | (lane >> kShift << 1); }
 };
 
-// A lane's pieces of a MixFP4 tile, 16 elements of each of kSteps rows: all asked for at once, then decoded to f16 (twice
-// their values under the block scale alone) at the operand's swizzled places.
+// A MixFP4 tile's elements in f16, at 2^-9 of their values under the block scale alone: a payload's three bits are those
+// of an f16 below its sign, and hold E2M1's value times 2^-14 at bits 11 to 9, E1M2's times 2^-16 at 10 to 8, subnormals
+// included; a factor of the scale times 2^5 (2^7) makes both exact multiples of 2^-19 below 8.
+// The order that eight elements then have, and the operands with them: nibbles of even places first, i and i + 4 to a
+// word.  It is its own inverse.
+__device__ __forceinline__ constexpr int fp4_order(int i) { return (i & 1) << 2 | (i & 2) | (i >> 2 & 1); }
+__device__ __forceinline__ void fp4_to_f16(uint32_t w, uint32_t e1m2, uint32_t s2, uint32_t* out) {
+  const uint32_t even = ((w << 4) & 0x80808080u) | (w & 0x07070707u) * (2u - e1m2);
+  const uint32_t odd = (w & 0x80808080u) | ((w & 0x70707070u) >> (3u + e1m2));
+  out[0] = hmul2(prmt(even, 0u, 0x2404u), s2);
+  out[1] = hmul2(even & 0xFF00FF00u, s2);
+  out[2] = hmul2(prmt(odd, 0u, 0x2404u), s2);
+  out[3] = hmul2(odd & 0xFF00FF00u, s2);
+}
+
+// A lane's pieces of a MixFP4 tile, 16 elements of each of kSteps rows: all asked for at once, then decoded to the
+// operand's swizzled places.
 template <int kSteps>
 struct Codes {
   uint2 c[kSteps];
   uint32_t scale[kSteps];
-  __device__ __forceinline__ void load(uint32_t codes, int step, const uint32_t* scales, int behind) {
+  __device__ __forceinline__ void load(uint32_t codes, int step, uint32_t scales, const int* at) {
 #pragma unroll
     for (int j = 0; j < kSteps; ++j) {
       c[j] = lds64(codes + j * step);
-      scale[j] = lds8(scales[j] + behind);
+      scale[j] = lds8(scales + at[j]);
     }
   }
-  // Rows row0, row0 + step ... of the block of 64 dimensions at `to`, 16-byte units u0 and u0 + 1.
-  __device__ __forceinline__ void decode(uint32_t to, int row0, int step, int u0) const {
+  // `at`: the first 16 bytes of row j's 32 in the slot `to`; the others are in its other half.
+  __device__ __forceinline__ void decode(uint32_t to, const int* at) const {
 #pragma unroll
     for (int j = 0; j < kSteps; ++j) {
-      const int row = row0 + j * step, x = row & 7;
-      const uint32_t sc = scale[j], e1m2 = sc >> 7;
-      const uint32_t s2 = cvt_f16x2_from_e4m3x2((uint16_t)((sc & 0x7Fu) * 0x0101u));
-      const uint32_t lo = kLutE2M1Lo + e1m2 * (kLutE1M2Lo - kLutE2M1Lo);
-      const uint32_t hi = kLutE2M1Hi + e1m2 * (kLutE1M2Hi - kLutE2M1Hi);
+      const uint32_t e1m2 = scale[j] >> 7;
+      const uint32_t s2 = hmul2(cvt_f16x2_from_e4m3x2((uint16_t)((scale[j] & 0x7Fu) * 0x0101u)),
+                                0x50005000u + e1m2 * 0x08000800u);
       uint32_t v[2][4];
-      decode8(c[j].x, lo, hi, s2, v[0]);
-      decode8(c[j].y, lo, hi, s2, v[1]);
-      sts128(to + row * 128 + ((u0 ^ x) << 4), v[0][0], v[0][1], v[0][2], v[0][3]);
-      sts128(to + row * 128 + (((u0 + 1) ^ x) << 4), v[1][0], v[1][1], v[1][2], v[1][3]);
+      fp4_to_f16(c[j].x, e1m2, s2, v[0]);
+      fp4_to_f16(c[j].y, e1m2, s2, v[1]);
+      sts128(to + at[j], v[0][0], v[0][1], v[0][2], v[0][3]);
+      sts128(to + (at[j] ^ 16), v[1][0], v[1][1], v[1][2], v[1][3]);
     }
   }
 };
@@ -575,7 +599,7 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
     uint32_t g = 0, turn = 0;  // tiles and parts before this one
     for (;;) {
       // All warps of softmax have the same parts and so meet at the same barriers, also where a wait has run out.
-      if (!__all_sync(kAll, mbar_wait(smem_u32(&sh.told), turn & 1, nullptr, kWaitLimitNs))) break;
+      if (bar_or(1, C::kSoftmax * 32, !mbar_wait(smem_u32(&sh.told), turn & 1, nullptr, kWaitLimitNs))) break;
       w = sh.part;
       if (w.tiles == 0) break;
       const int R = min(128 * MT, p.t * p.group - w.chunk * 128 * MT);
@@ -590,59 +614,57 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
       const float slope = p.slopes && valid ? p.slopes[h] * -kLog2e : 0.0f;
 
       // ---- the row's queries, into the swizzled tile
-      float fs = p.scale * (kFp4 ? 0.5f * kts : 1.0f);
+      // A warp brings its rows' (those of which it has copies with the warps that have the others), a row by DT / 8
+      // neighbouring lanes, to each copy's place.
+      float fs = p.scale * (kFp4 ? kFp4Unit * kts : 1.0f);
       {
-        const uint16_t* q = p.q + (int64_t)w.b * p.q_stride + (int64_t)i * p.q_token_stride + (int64_t)h * p.q_head_stride;
-        float up = 1.0f;
-        constexpr int kBatch = 8;  // pieces asked for at once
-        if (kFp4) {  // q times 2^(14 - exponent of the row's largest) as f16
-          float top = 0.0f;
+        constexpr int kLanes = DT / 8, kRowsAtOnce = 32 / kLanes, kBatch = 8;  // steps asked for at once
+        const int steps_q = kLanes / copies, u = lane % kLanes, base = copy * (32 / copies) + lane / kLanes;
+        const int64_t from = valid ? (int64_t)w.b * p.q_stride + (int64_t)i * p.q_token_stride + (int64_t)h * p.q_head_stride
+                                   : -1;
+        const uint32_t tile = q_smem + m * (128 * DT * 2) + (tl % own & 96) * 128 + (u >> 3) * 16384;
 #pragma unroll 1
-          for (int u0 = 0; u0 < D / 8; u0 += kBatch) {
-            uint4 v[kBatch];
-#pragma unroll
-            for (int k = 0; k < kBatch; ++k) {
-              v[k] = make_uint4(0, 0, 0, 0);
-              if (valid && u0 + k < D / 8) v[k] = *reinterpret_cast<const uint4*>(q + 8 * (u0 + k));
-            }
-#pragma unroll
-            for (int k = 0; k < kBatch; ++k) {
-              top = max3f(top, fabsf(bf_lo(v[k].x)), fabsf(bf_hi(v[k].x)));
-              top = max3f(top, fabsf(bf_lo(v[k].y)), fabsf(bf_hi(v[k].y)));
-              top = max3f(top, fabsf(bf_lo(v[k].z)), fabsf(bf_hi(v[k].z)));
-              top = max3f(top, fabsf(bf_lo(v[k].w)), fabsf(bf_hi(v[k].w)));
-            }
-          }
-          const int e = min(max((int)(__float_as_uint(top) >> 23), 15), 253);
-          up = __uint_as_float((uint32_t)(268 - e) << 23);
-          fs *= __uint_as_float((uint32_t)(e - 14) << 23);
-        }
-        const uint32_t at = q_smem + m * (128 * DT * 2) + tl * 128;
-#pragma unroll 1
-        for (int u0 = 0; u0 < D / 8; u0 += kBatch) {
+        for (int k0 = 0; k0 < steps_q; k0 += kBatch) {
           uint4 v[kBatch];
 #pragma unroll
           for (int k = 0; k < kBatch; ++k) {
             v[k] = make_uint4(0, 0, 0, 0);
-            if (valid && u0 + k < D / 8) v[k] = *reinterpret_cast<const uint4*>(q + 8 * (u0 + k));
+            const int64_t x = __shfl_sync(kAll, from, base + (k0 + k) * kRowsAtOnce);
+            if (x >= 0 && u * 8 < D && k0 + k < steps_q) v[k] = *reinterpret_cast<const uint4*>(p.q + x + u * 8);
           }
 #pragma unroll
           for (int k = 0; k < kBatch; ++k) {
-            const int u = u0 + k;
-            if (u >= D / 8) break;
-            if (kFp4) {
-              v[k].x = f16x2(bf_lo(v[k].x) * up, bf_hi(v[k].x) * up), v[k].y = f16x2(bf_lo(v[k].y) * up, bf_hi(v[k].y) * up);
-              v[k].z = f16x2(bf_lo(v[k].z) * up, bf_hi(v[k].z) * up), v[k].w = f16x2(bf_lo(v[k].w) * up, bf_hi(v[k].w) * up);
+            if (k0 + k >= steps_q) break;
+            const int row = base + (k0 + k) * kRowsAtOnce;
+            if (kFp4) {  // q times 2^(14 - exponent of the row's largest) as f16, in the keys' order
+              float top = max3f(fabsf(bf_lo(v[k].x)), fabsf(bf_hi(v[k].x)), fabsf(bf_lo(v[k].y)));
+              top = max3f(top, fabsf(bf_hi(v[k].y)), fabsf(bf_lo(v[k].z)));
+              top = max3f(top, fabsf(bf_hi(v[k].z)), fabsf(bf_lo(v[k].w)));
+              top = fmaxf(top, fabsf(bf_hi(v[k].w)));
+#pragma unroll
+              for (int d = 1; d < kLanes; d *= 2) top = fmaxf(top, __shfl_xor_sync(kAll, top, d));
+              const int e = min(max((int)(__float_as_uint(top) >> 23), 15), 253);
+              const float up = __uint_as_float((uint32_t)(268 - e) << 23);
+              if (u == 0)
+                for (int c = 0; c < copies; ++c) sh.exponent[m * 128 + c * own + (tl % own & 96) + row] = (uint8_t)e;
+              const uint4 x = v[k];
+              v[k].x = f16x2(bf_lo(x.x) * up, bf_lo(x.z) * up), v[k].y = f16x2(bf_lo(x.y) * up, bf_lo(x.w) * up);
+              v[k].z = f16x2(bf_hi(x.x) * up, bf_hi(x.z) * up), v[k].w = f16x2(bf_hi(x.y) * up, bf_hi(x.w) * up);
             }
-            sts128(at + (u >> 3) * 16384 + (((u & 7) ^ (tl & 7)) << 4), v[k].x, v[k].y, v[k].z, v[k].w);
+            for (int c = 0; c < copies; ++c)
+              sts128(tile + (c * own + row) * 128 + (((u & 7) ^ (row & 7)) << 4), v[k].x, v[k].y, v[k].z, v[k].w);
           }
         }
       }
-      const float cap2 = p.softcap * kLog2e;
-      fs *= p.softcap > 0.0f ? 1.0f / p.softcap : kLog2e;
       fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&sh.q_full));
+      if (kFp4) {
+        bar_sync(4 + m, 128);
+        fs *= __uint_as_float((uint32_t)(sh.exponent[m * 128 + tl] - 14) << 23);
+      }
+      const float cap2 = p.softcap * kLog2e;
+      fs *= p.softcap > 0.0f ? 1.0f / p.softcap : kLog2e;
       if (p.window > 0)
         for (int k = 0; k < w.s.c; ++k)
           if (place - w.s.first - depth[k] >= p.window) sees &= ~(1ull << k);
@@ -765,37 +787,58 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
               top = fmaxf(top, top2);
             } else {
               const int a = j0 + c;
-              auto shaped = [&](uint32_t y) {
-                const float x = __uint_as_float(y) * fs;
-                return p.softcap > 0.0f ? cap2 * tanh_of(x) : x;
-              };
-              if (!masked) {
-                const float far0 = (float)(place - a);
+              const u64 ff = pack2(fs, fs);
 #pragma unroll
-                for (int e = 0; e < PW; ++e) {
+              for (int e = 0; e < PW; e += 2) {
+                if (e == 16 && narrow) break;
+                float x0, x1;
+                unpack2(mul2(bits2(v[e], v[e + 1]), ff), x0, x1);
+                v[e] = __float_as_uint(x0), v[e + 1] = __float_as_uint(x1);
+              }
+              if (p.softcap > 0.0f) {
+#pragma unroll
+                for (int e = 0; e < PW; e += 2) {
                   if (e == 16 && narrow) break;
-                  float x = shaped(v[e]);
-                  if (p.slopes) x = fmaf(slope, far0 - (float)e, x);
-                  top = fmaxf(top, x);
-                  v[e] = __float_as_uint(x);
+                  float x0 = __uint_as_float(v[e]), x1 = __uint_as_float(v[e + 1]);
+                  tanh2(x0, x1);
+                  v[e] = __float_as_uint(cap2 * x0), v[e + 1] = __float_as_uint(cap2 * x1);
                 }
-              } else {
+              }
+              if (p.slopes) {
+                if (a + PW <= w.s.first) {
+                  const float far0 = (float)(place - a);
+#pragma unroll
+                  for (int e = 0; e < PW; ++e) {
+                    if (e == 16 && narrow) break;
+                    v[e] = __float_as_uint(fmaf(slope, far0 - (float)e, __uint_as_float(v[e])));
+                  }
+                } else {
+#pragma unroll
+                  for (int e = 0; e < PW; ++e) {
+                    if (e == 16 && narrow) break;
+                    const int j = a + e;
+                    int far = place - j;
+                    if (j >= w.s.first) far = place - w.s.first - depth[min(j - w.s.first, kMostDrafts - 1)];
+                    v[e] = __float_as_uint(fmaf(slope, (float)far, __uint_as_float(v[e])));
+                  }
+                }
+              }
+              if (masked) {
                 const uint32_t seen = seen_of(c);
 #pragma unroll
                 for (int e = 0; e < PW; ++e) {
                   if (e == 16 && narrow) break;
-                  float x = shaped(v[e]);
-                  if (p.slopes) {
-                    const int j = a + e;
-                    int far = place - j;
-                    if (j >= w.s.first) far = place - w.s.first - depth[min(j - w.s.first, kMostDrafts - 1)];
-                    x = fmaf(slope, (float)far, x);
-                  }
-                  x = (seen >> e) & 1u ? x : -INFINITY;
-                  top = fmaxf(top, x);
-                  v[e] = __float_as_uint(x);
+                  v[e] = (seen >> e) & 1u ? v[e] : __float_as_uint(-INFINITY);
                 }
               }
+              float top2 = -INFINITY;
+#pragma unroll
+              for (int e = 0; e < PW; e += 4) {
+                if (e == 16 && narrow) break;
+                top = max3f(top, __uint_as_float(v[e]), __uint_as_float(v[e + 1]));
+                top2 = max3f(top2, __uint_as_float(v[e + 2]), __uint_as_float(v[e + 3]));
+              }
+              top = fmaxf(top, top2);
               if (c_end - step0 * CW > PW || slow) {
                 if (narrow)
                   tmem_store<16>(scores + c, v);
@@ -932,81 +975,96 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
       const int64_t at = ((int64_t)w.b * p.t + i) * p.q_heads + h;  // of the results
       const float old = chained ? ex2(m_aside - mx) : 0.0f;
       if (!valid) mx = kNoScore, l = 0.0f;
-      float M = mx, L = l;
+      float M = mx, L = l, part_of[4];  // what a copy's O counts
       if (copies > 1) {  // of one tile of rows
         float2* ml = reinterpret_cast<float2*>(smem);  // where the queries were: no product reads them any more
-        bar_sync(1, 128);
         ml[tl] = make_float2(mx, l);
         bar_sync(1, 128);
-        for (int k = 0; k < copies; ++k) M = fmaxf(M, ml[tl % own + k * own].x);
-        L = 0.0f;
-        for (int k = 0; k < copies; ++k) {
-          const float2 s = ml[tl % own + k * own];
-          L += ex2(s.x - M) * s.y;
+        float2 x[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          x[k] = k < copies ? ml[tl % own + k * own] : make_float2(kNoScore, 0.0f);
+          M = fmaxf(M, x[k].x);
         }
-        bar_sync(1, 128);
+        L = 0.0f;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          part_of[k] = ex2(x[k].x - M);
+          L += part_of[k] * x[k].y;
+        }
       }
-      const float last = all ? out_factor<kFp4>(L, vts) : 1.0f, f = copies > 1 ? ex2(mx - M) : 1.0f;
-      // Columns [d, d + 4) of the row's sum, to their place.
-      auto put = [&](int d, const float* x) {
+      const float last = all ? out_factor<kFp4>(L, vts) : 1.0f;
+      // Columns [d, d + 8) of the row's sum, in their own order from here on, to their place.
+      auto put = [&](int d, const float* y) {
         if (!held || dead || d >= D) return;
-        if (all)
-          *reinterpret_cast<uint2*>(p.out + at * D + d) =
-              make_uint2(bf16x2(x[0] * last, x[1] * last), bf16x2(x[2] * last, x[3] * last));
-        else
-          part[(d / 4) * 128 + tl % own] = make_float4(x[0], x[1], x[2], x[3]);
+        float x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[kFp4 ? fp4_order(e) : e] = valid ? y[e] * last : 0.0f;
+        if (all) {
+          *reinterpret_cast<uint4*>(p.out + at * D + d) =
+              make_uint4(bf16x2(x[0], x[1]), bf16x2(x[2], x[3]), bf16x2(x[4], x[5]), bf16x2(x[6], x[7]));
+        } else {
+          float4* to = part + (d / 4) * 128 + tl % own;
+          to[0] = make_float4(x[0], x[1], x[2], x[3]), to[128] = make_float4(x[4], x[5], x[6], x[7]);
+        }
       };
-      auto take = [&](int d, float* x) {  // 32 columns of O, with what was set aside
-        uint32_t v[32];
+      auto take = [&](int d, uint32_t* v) {  // 32 columns of O, with what was set aside
         tmem_load<32>(o_col + d, v);
         tmem_loaded<32>(v);
-#pragma unroll
-        for (int e = 0; e < 32; ++e) x[e] = __uint_as_float(v[e]);
         if (chained) {
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            if (d + 4 * e >= D) break;
-            const float4 y = aside[(d / 4 + e) * 128];
-            x[4 * e] = fmaf(old, y.x, x[4 * e]), x[4 * e + 1] = fmaf(old, y.y, x[4 * e + 1]);
-            x[4 * e + 2] = fmaf(old, y.z, x[4 * e + 2]), x[4 * e + 3] = fmaf(old, y.w, x[4 * e + 3]);
+          for (int e = 0; e < 32; e += 4) {
+            if (d + e >= D) break;
+            const float4 y = aside[(d + e) * 32];
+            auto more = [&](int k, float z) { v[e + k] = __float_as_uint(fmaf(old, z, __uint_as_float(v[e + k]))); };
+            more(0, y.x), more(1, y.y), more(2, y.z), more(3, y.w);
           }
         }
-#pragma unroll
-        for (int e = 0; e < 32; ++e) x[e] = valid ? x[e] * f : 0.0f;
       };
       if (copies == 1) {
         if (!idle)
 #pragma unroll 1
           for (int d = 0; d < D; d += 32) {
-            float x[32];
-            take(d, x);
+            uint32_t v[32];
+            take(d, v);
 #pragma unroll
-            for (int e = 0; e < 32; e += 4) put(d + e, x + e);
+            for (int e = 0; e < 32; e += 8) put(d + e, reinterpret_cast<const float*>(v) + e);
           }
       } else {
-        float* stage = reinterpret_cast<float*>(smem);  // [32][128]
+        // 32 columns of all rows at a time, [row][8 pieces of 16 bytes] swizzled as the operands are, in two places in
+        // turn (m and l were in the second's) where the queries' room allows.
+        constexpr bool kTwo = C::kQ >= 32768;
         const int each = 32 / copies;
+        if (!kTwo) bar_sync(1, 128);
 #pragma unroll 1
         for (int d0 = 0; d0 < D; d0 += 32) {
+          const uint32_t stage = q_smem + (kTwo && !(d0 & 32) ? 16384 : 0);
           {
-            float x[32];
-            take(d0, x);
+            uint32_t v[32];
+            take(d0, v);
 #pragma unroll
-            for (int e = 0; e < 32; ++e) stage[e * 128 + tl] = x[e];
+            for (int e = 0; e < 8; ++e)
+              sts128(stage + tl * 128 + ((e ^ (tl & 7)) << 4), v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]);
           }
           bar_sync(1, 128);
 #pragma unroll 1
-          for (int d = copy * each; d < (copy + 1) * each; d += 4) {
-            float x[4];
+          for (int d = copy * each; d < (copy + 1) * each; d += 8) {
+            float x[8] = {};
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const float* s = stage + (d + e) * 128 + tl % own;
-              x[e] = s[0] + s[own];
-              if (copies == 4) x[e] += s[2 * own] + s[3 * own];
+            for (int k = 0; k < 4; ++k) {
+              if (k >= copies) break;
+#pragma unroll
+              for (int u = 0; u < 2; ++u) {
+                const uint4 v = lds128(stage + (tl % own + k * own) * 128 + (((d / 4 + u) ^ (tl & 7)) << 4));
+                x[4 * u] = fmaf(part_of[k], __uint_as_float(v.x), x[4 * u]);
+                x[4 * u + 1] = fmaf(part_of[k], __uint_as_float(v.y), x[4 * u + 1]);
+                x[4 * u + 2] = fmaf(part_of[k], __uint_as_float(v.z), x[4 * u + 2]);
+                x[4 * u + 3] = fmaf(part_of[k], __uint_as_float(v.w), x[4 * u + 3]);
+              }
             }
             put(d0 + d, x);
           }
-          bar_sync(1, 128);
+          if (!kTwo) bar_sync(1, 128);
         }
       }
       if (held && copy == 0 && !dead) {
@@ -1324,6 +1382,13 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
     uint32_t g = 0, sent = 0;  // tiles asked for, tiles decoded
     // The oldest tile not decoded yet, with `later` behind it: once it has landed, for the tensor cores.
     const int box_shift = p.box ? __ffs(p.box) - 1 : 31, box_pitch = (p.box * p.scale_pitch + 127) / 128 * 128;
+    int scales[kSteps], at_slot[kSteps];  // where a row's scale byte lies, and its elements
+#pragma unroll
+    for (int j = 0; j < kSteps; ++j) {
+      const int r = row0 + r0 + j * L::kRowsAtOnce;
+      scales[j] = p.box ? (r >> box_shift) * box_pitch + (r & (p.box - 1)) * p.scale_pitch : r * 16;
+      at_slot[j] = (piece >> 2) * C::kBlock + r * 128 + ((((piece & 3) * 2) ^ (r & 7)) << 4);
+    }
     auto hand_over = [&](int later) {
       const uint32_t n = sent % C::kRawDepth, raw = raw_tiles + n * C::kRawTile;
       if (p.box)
@@ -1332,19 +1397,11 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
         cp_wait_at_most(later);
       dead = __any_sync(kAll, dead);
       Codes<kSteps> c[2];
-      uint32_t scales[kSteps];  // where a row's scale byte lies
-#pragma unroll
-      for (int j = 0; j < kSteps; ++j) {
-        const int r = row0 + r0 + j * L::kRowsAtOnce;
-        scales[j] = raw + 2 * C::kCodes + piece +
-                    (p.box ? (r >> box_shift) * box_pitch + (r & (p.box - 1)) * p.scale_pitch +
-                                 (p.scale_by_head ? w.head * (D / 16) & 15 : 0)
-                           : r * 16);
-      }
+      const uint32_t bytes = raw + 2 * C::kCodes + piece + (p.scale_by_head ? w.head * (D / 16) & 15 : 0);
 #pragma unroll
       for (int kv = 0; kv < 2; ++kv)
         if (piece * 16 < D)
-          c[kv].load(raw + kv * C::kCodes + (row0 + r0) * pitch + piece * 8, L::kRowsAtOnce * pitch, scales, kv * TN * 16);
+          c[kv].load(raw + kv * C::kCodes + (row0 + r0) * pitch + piece * 8, L::kRowsAtOnce * pitch, bytes + kv * TN * 16, scales);
       __syncwarp();
       if (p.box && lane == 0) mbar_arrive(smem_u32(&sh.raw_empty[n]));
 #pragma unroll
@@ -1352,7 +1409,7 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
         const uint32_t q = 2 * sent + kv, slot = q % C::kSlots;
         waits(sh.empty[slot], ((q / C::kSlots) & 1) ^ 1, 1024u);
         if (piece * 16 < D)
-          c[kv].decode(ring + slot * C::kSlot + (piece >> 2) * C::kBlock, row0 + r0, L::kRowsAtOnce, (piece & 3) * 2);
+          c[kv].decode(ring + slot * C::kSlot, at_slot);
         fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&sh.full[slot]));
@@ -1368,7 +1425,7 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
         }
         waits(sh.placed[g % C::kAddresses], (g / C::kAddresses) & 1, 4096u);
         const uint32_t at = places + (g % C::kAddresses) * (TN * 16) + row0 * 16;
-        const uint32_t raw = raw_tiles + (g % C::kRawDepth) * C::kRawTile, scales = raw + 2 * C::kCodes + row0 * 16;
+        const uint32_t raw = raw_tiles + (g % C::kRawDepth) * C::kRawTile, bytes_at = raw + 2 * C::kCodes + row0 * 16;
 #pragma unroll
         for (int j = 0; j < kSteps; ++j) {
           const int r = r0 + j * L::kRowsAtOnce;
@@ -1385,7 +1442,7 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
             const uint4 x = lds128(at + r * 16);
             const bool ok = (int32_t)x.y >= 0;
             const uint8_t* src = (kv ? p.c.v_scales : p.c.k_scales) + (ok ? (int64_t)((u64)x.z | (u64)x.w << 32) : 0);
-            const uint32_t sd = scales + (kv * TN + r) * 16;
+            const uint32_t sd = bytes_at + (kv * TN + r) * 16;
             if (D == 128) {
               cp_async<8>(sd, src, ok);
             } else if (D == 256) {
@@ -1411,7 +1468,7 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
 #pragma unroll
           for (int k = 0; k < kMost; ++k) {
             const int x = lane + 32 * k, y = x / bytes, r = y & (kRows - 1), kv = y / kRows;
-            if (kv < 2) sts8(scales + (kv * TN + r) * 16 + x - y * bytes, b[k]);
+            if (kv < 2) sts8(bytes_at + (kv * TN + r) * 16 + x - y * bytes, b[k]);
           }
         }
         cp_commit();
