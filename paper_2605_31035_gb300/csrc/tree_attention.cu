@@ -1396,24 +1396,20 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
       else
         cp_wait_at_most(later);
       dead = __any_sync(kAll, dead);
-      Codes<kSteps> c[2];
-      const uint32_t bytes = raw + 2 * C::kCodes + piece + (p.scale_by_head ? w.head * (D / 16) & 15 : 0);
-#pragma unroll
-      for (int kv = 0; kv < 2; ++kv)
-        if (piece * 16 < D)
-          c[kv].load(raw + kv * C::kCodes + (row0 + r0) * pitch + piece * 8, L::kRowsAtOnce * pitch, bytes + kv * TN * 16, scales);
-      __syncwarp();
-      if (p.box && lane == 0) mbar_arrive(smem_u32(&sh.raw_empty[n]));
-#pragma unroll
+      const uint32_t bytes = raw + 2 * C::kCodes + piece + (p.box && p.scale_by_head ? w.head * (D / 16) & 15 : 0);
+#pragma unroll 1
       for (int kv = 0; kv < 2; ++kv) {
         const uint32_t q = 2 * sent + kv, slot = q % C::kSlots;
-        waits(sh.empty[slot], ((q / C::kSlots) & 1) ^ 1, 1024u);
+        Codes<kSteps> c;
         if (piece * 16 < D)
-          c[kv].decode(ring + slot * C::kSlot, at_slot);
+          c.load(raw + kv * C::kCodes + (row0 + r0) * pitch + piece * 8, L::kRowsAtOnce * pitch, bytes + kv * TN * 16, scales);
+        waits(sh.empty[slot], ((q / C::kSlots) & 1) ^ 1, 1024u);
+        if (piece * 16 < D) c.decode(ring + slot * C::kSlot, at_slot);
         fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&sh.full[slot]));
       }
+      if (p.box && lane == 0) mbar_arrive(smem_u32(&sh.raw_empty[n]));
       ++sent;
     };
     while (walk.next(p, mate, w)) {
