@@ -594,7 +594,9 @@ int mixfp4_paged_attention_workspace(const mixfp4_kv_cache* cache, int64_t B, in
  * out is rounded to bf16.  A draft that sees nothing, and rows i >= c, give out = 0
  * and lse = -inf.  What a draft does not see does not reach its results, NaN and
  * infinities included.  Scores of NaN and +inf and infinities of V as
- * mixfp4_paged_attention has them.  The order of every sum depends on the arguments alone.
+ * mixfp4_paged_attention has them, but that an infinity of V with a weight below 2^-80 of the
+ * row's largest may give NaN instead; weights on a MixFP4 cache end at 2^-31 of the largest.
+ * The order of every sum depends on the arguments alone.
  *
  * q            device, bf16: element d of head h of draft i of sequence b at
  *              b * q_stride + i * q_token_stride + h * q_head_stride + d; 16-byte

@@ -1,28 +1,32 @@
 // Attention of drafted tokens over the paged cache (mixfp4_tree_attention).
 //
-// A key head's queries, t drafts times the query heads that share it, are the
-// rows of one tcgen05 tile: 128 of them, or two tiles of 128 over the same tokens.
-// Per tile of 128 tokens (64 with more than 128 dimensions) S = Q K^T goes to
-// tensor memory, four warps a tile of rows take it from there, a row to a thread,
-// and put the softmax's weights P back in its place, and O += P V follows with P
-// from tensor memory.  What bounds it: HBM for a bf16 cache and up to 256 rows,
-// the tensor cores beyond.
+// A key head's queries, t drafts times the query heads that share it, are the rows of a tcgen05 tile of 128, or of two
+// tiles over the same tokens.  To a tile of 64 tokens (128 on a MixFP4 cache with one tile of rows) S = Q K^T goes to
+// tensor memory; four warps a tile of rows take it from there, a row to a thread, and put the softmax's weights P back in
+// its place; O += P V follows with P from tensor memory.  m and l are held in fp32 beside O, and O is only scaled again
+// where the maximum has grown by more than 2^16 (2^8): weights are relative to a maximum that may be an old one.
 //
-//   * Roles: producer warps bring K and V tiles into a ring, the row's bytes by
-//     cp.async into the places that the 128-byte swizzle gives them (so that any
-//     strides and pages of any size will do), or decode a MixFP4 cache's codes into
-//     them as exact f16; one thread issues the products; the others are softmax.
-//   * Few rows: 32 (or 64) rows are held four times (twice) in the 128 lanes and
-//     each copy takes its quarter (half) of a tile's tokens; the copies are joined
-//     at the end.  A thread then has 32 scores a tile instead of 128.
-//   * The weights keep 16 bits in two bf16 parts of one sign on a bf16 cache, f16's
-//     11 on a MixFP4 one, whose queries are scaled per row by a power of two into f16.
-//   * Where rows of a tile see different tokens (drafts, a window's edge), a weight
-//     of 0 would still make NaN of an infinite or NaN element of V.  Such tiles are
-//     looked over for those, and where there is one the threads take the products
-//     themselves, of what each row sees alone.
-//   * Tokens are cut into equal shares over the device as in the attention of one
-//     token; CTAs of neighbouring heads walk the same tokens at the same time.
+//   * Roles: rows of K and V come by TMA into a ring, boxes of one page, where the strides allow it, by cp.async
+//     otherwise; a MixFP4 cache's codes and scale bytes come the same ways and eight warps write them into the ring as
+//     exact f16.  One thread issues the products, one warp reads the next part of the work ahead.  Every wait ends
+//     after a second at the latest, with an error in the status word.
+//   * Few rows: 32 (or 64) rows are held four times (twice) in the 128 lanes and each copy takes its quarter (half) of a
+//     tile's tokens, by products that write its lanes of O alone; the copies are joined at the end.  A thread then has a
+//     quarter of the scores: 187 instead of 201 us at 8 drafts below, 204 instead of 255 on a MixFP4 cache.
+//   * More than 128 rows (and up to 128 dimensions): two tiles of rows to a CTA, so that K and V are fetched, and decoded,
+//     once for both.  412 instead of 435 us at 64 drafts, 469 instead of 581 on a MixFP4 cache; 40 drafts 392 and 399.
+//   * On a bf16 cache the weights keep 16 bits in two bf16 parts of one sign; on a MixFP4 one f16's 11, and the queries
+//     are scaled per row by a power of two into f16.
+//   * Where rows of a tile see different tokens (drafts, a window's edge), a weight of 0 would still make NaN of an
+//     infinite or NaN element of V.  Such tiles are looked over for those, and where there is one the threads take the
+//     products themselves, of what each row sees alone.
+//   * Tokens are cut into equal shares over the device.  CTAs of neighbouring heads walk the same tokens at the same time,
+//     whose rows lie together: 187 instead of 200 us at 8 drafts, 412 instead of 505 at 64.
+//
+// Measured on 64 sequences of up to 8192 tokens, 32 query heads on 8, 128 dimensions (bf16 cache 1.1 GB, MixFP4 0.3 GB):
+// bf16 183 us at 8 drafts (6.0 TB/s: bound by HBM), 195 at 16, 383 at 64 (645 TFLOP/s: bound by the tensor cores, which
+// take P in two parts, and by what the softmax of 256 rows issues); MixFP4 196 us at 8 and 448 at 64 drafts, bound by the
+// instructions of decoding and of the softmax (half of the issue slots used, a fifth of all waits for instructions).
 #include <cuda_runtime.h>
 #include <atomic>
 #include <cstdint>
@@ -43,15 +47,13 @@ using namespace sm100;
 constexpr int kMostDrafts = 64;
 constexpr int kJoinThreads = 256;
 constexpr uint64_t kWaitLimitNs = 1000000000ull;
-// What beginning a row costs (its queries, the way to its first pages, its end), in tiles.
-constexpr int kRowCost = 2;
 // Tokens after which O is set aside and begins at 0: the tensor cores round a chain of sums towards zero, some 2^-25 of
 // the sum a link, and 8192 tokens are 512 links (1024 with two parts of the weights).
 constexpr int kChainTokens = 8192;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-// How far a score may lie above the m of its weight 2^(s - m), which follows the maximum from afar: bf16 parts and fp32
-// sums have the room.  On a MixFP4 cache the weights are 2^7 times that: at most 2^15 in f16, whose least value is then
-// 2^-31 of the weight at m.
+// How far a score may lie above the m of its weight 2^(s - m), which follows the maximum from afar (187 us at 8 drafts,
+// 412 at 64; 191 and 443 where it follows at once): bf16 parts and fp32 sums have the room.  On a MixFP4 cache the
+// weights are 2^7 times that: at most 2^15 in f16, whose least value is then 2^-31 of the weight at m.
 constexpr float kSlack = 16.0f, kFp4Slack = 8.0f, kFp4Exp = 7.0f;
 // A MixFP4 operand's elements are their values under the block scale over this (fp4_to_f16).
 constexpr float kFp4Unit = 512.0f;
@@ -137,10 +139,16 @@ struct Maps {
 
 template <int DT, int MT, bool kFp4>
 struct Cfg {
-  // With one tile of rows two CTAs share an SM: what one does once a row (its queries, its end) the other's tiles cover.
-  // A MixFP4 cache's decoding takes the registers and the larger tiles of one.
+  // With one tile of rows two CTAs share an SM: what one does once a row (its queries, its end) the other's tiles cover
+  // (187 instead of 229 us at 8 drafts).  A MixFP4 cache's decoding takes the registers and the larger tiles of one (two
+  // were 358 instead of 236 us).
   static constexpr int kCtas = !kFp4 && MT == 1 && DT <= 128 ? 2 : 1;
-  static constexpr int kTokens = kFp4 && MT == 1 && DT <= 128 ? 128 : 64;  // of a tile
+  // Of a tile.  A larger one has fewer steps between the roles, which on a MixFP4 cache are most of the time (203 instead
+  // of 270 us at 8 drafts); a bf16 one of two CTAs has no room for it, nor have two tiles of rows in tensor memory.
+  static constexpr int kTokens = kFp4 && MT == 1 && DT <= 128 ? 128 : 64;
+  // What beginning a row costs (its queries, the way to its first pages, its end), in tiles.  64 sequences of up to 8192
+  // tokens, us at a cost of 0, 2, 4, 8 and 12: 8 drafts 195, 187, 183, 184, 184; 64 drafts 425, 412, 404, 383, 385.
+  static constexpr int kRowCost = MT == 2 ? 8 : 4;
   static constexpr int kChain = kChainTokens / kTokens;    // tiles to a chain of sums
   static constexpr int kCw = kTokens / 4;                  // and of its quarter, a thread's step
   static constexpr int kBlock = kTokens * 128;             // 64 dimensions of a tile
@@ -148,7 +156,9 @@ struct Cfg {
   static constexpr int kSlot = kBlock * (DT / 64);
   static constexpr int kSoftmax = 4 * MT;                  // warps, four to a tile of rows
   static constexpr int kQ = MT * 128 * DT * 2;
-  static constexpr int kProducers = kFp4 ? 8 : 2;  // of a bf16 cache where TMA cannot bring its rows
+  // Warps that decode (16 in one team, or in two of 64 registers, were slower), or bring a bf16 cache's rows where TMA
+  // cannot.
+  static constexpr int kProducers = kFp4 ? 8 : 2;
   static constexpr int kThreads = (kSoftmax + 4 + (kFp4 ? kProducers : 0)) * 32;  // the four: products, TMA or helpers
   // Registers of a thread at launch, then of softmax and of the other threads (together no more than at launch).
   static constexpr int kRegs = 65536 / (kThreads * kCtas) / 8 * 8;
@@ -252,7 +262,8 @@ __device__ __forceinline__ void tanh2(float& x0, float& x1) {
   };
   auto both = [](float c) { return pack2(c, c); };
   const u64 z = pack2(held(x0), held(x1)), y = mul2(z, z);
-  u64 a = fma2(y, both(1.335449179e-08f), both(2.060896267e-05f)), b = fma2(y, both(7.776489695e-07f), both(3.285623034e-04f));
+  u64 a = fma2(y, both(1.335449179e-08f), both(2.060896267e-05f));
+  u64 b = fma2(y, both(7.776489695e-07f), both(3.285623034e-04f));
   a = fma2(y, a, both(3.495580968e-03f)), b = fma2(y, b, both(2.587695507e-02f));
   a = fma2(y, a, both(1.338101964e-01f)), b = fma2(y, b, both(4.671433524e-01f));
   a = fma2(y, a, both(1.0f)), b = fma2(y, b, both(1.0f));
@@ -311,12 +322,7 @@ __device__ __forceinline__ void tmem_load(uint32_t taddr, uint32_t* v) {
   else
     tmem_ld_32x32b_x16(taddr, v);
 }
-// Keeps the use of loaded columns behind the wait for them.
-template <int kCols>
-__device__ __forceinline__ void tmem_fence(uint32_t* v) {
-  reg_fence16(v);
-  if constexpr (kCols == 32) reg_fence16(v + 16);
-}
+// Waits for loaded columns, and keeps their use behind the wait.
 template <int kCols>
 __device__ __forceinline__ void tmem_loaded(uint32_t* v) {
   if constexpr (kCols == 32)
@@ -337,7 +343,7 @@ __device__ __forceinline__ void tmem_store(uint32_t taddr, const uint32_t* v) {
   }
 }
 
-template <int kTokens>
+template <class C>
 __device__ __forceinline__ Span span_of(const TreeArgs& p, int b) {
   Span s;
   s.n = max(p.lengths[b], 0);
@@ -346,25 +352,25 @@ __device__ __forceinline__ Span span_of(const TreeArgs& p, int b) {
   s.first = s.n - s.c;
   s.end = (int)min((int64_t)s.n, p.max_tokens);
   s.low = p.window > 0 ? (int)max((int64_t)0, s.first + 1 - p.window) : 0;  // of the drafts, those that see none
-  s.from = s.low & ~(kTokens - 1);
+  s.from = s.low & ~(C::kTokens - 1);
   return s;
 }
 // Units of work of a row of the sequence: kRowCost for its beginning, then one to a tile.
-template <int kTokens>
+template <class C>
 __device__ __forceinline__ int units_of(const Span& s) {
-  return s.c > 0 && s.end > s.low ? kRowCost + (s.end - s.from + kTokens - 1) / kTokens : 0;
+  return s.c > 0 && s.end > s.low ? C::kRowCost + (s.end - s.from + C::kTokens - 1) / C::kTokens : 0;
 }
 
 // Every role walks a CTA's share in the same steps.
-template <int kTokens>
+template <class C>
 struct Walk {
   int64_t pos, end, base;
   int b;
   __device__ __forceinline__ bool next(const TreeArgs& p, int mate, Part& w) {
     const int rows = p.c.heads / p.together * p.chunks;
     while (pos < end && b < p.B) {
-      w.s = span_of<kTokens>(p, b);
-      const int u = units_of<kTokens>(w.s);
+      w.s = span_of<C>(p, b);
+      const int u = units_of<C>(w.s);
       if (u == 0 || pos >= base + (int64_t)u * rows) {
         base += (int64_t)u * rows;
         ++b;
@@ -375,8 +381,8 @@ struct Walk {
       const int k0 = (int)((pos - base) - (int64_t)w.row * u), cnt = (int)min((int64_t)(u - k0), end - pos);
       w.head = w.row / p.chunks * p.together + mate;
       w.chunk = w.row % p.chunks;
-      w.tile = max(k0 - kRowCost, 0);
-      w.tiles = k0 + cnt - kRowCost - w.tile;
+      w.tile = max(k0 - C::kRowCost, 0);
+      w.tiles = k0 + cnt - C::kRowCost - w.tile;
       w.first = k0 == 0;
       w.last = k0 + cnt == u;
       w.behind = base + (int64_t)(w.row + 1) * u;
@@ -470,7 +476,8 @@ struct Codes {
 };
 
 template <int DT, int MT, bool kFp4>
-__global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>::kCtas) tree_attention_kernel(const TreeArgs p, const __grid_constant__ Maps tm) {
+__global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>::kCtas)
+    tree_attention_kernel(const TreeArgs p, const __grid_constant__ Maps tm) {
   using C = Cfg<DT, MT, kFp4>;
   constexpr int TN = C::kTokens, CW = C::kCw, PW = C::kStep;
   extern __shared__ __align__(1024) uint8_t smem[];
@@ -516,12 +523,12 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
   }
 
   // This CTA's share [pos, end) of all units, and the sequence it starts in.
-  Walk<TN> walk;
+  Walk<C> walk;
   const int rows = p.c.heads / p.together * p.chunks;
   {
     const int strip = (p.B + C::kThreads - 1) / C::kThreads, lo = min(p.B, tid * strip), hi = min(p.B, lo + strip);
     int64_t mine = 0;
-    for (int i = lo; i < hi; ++i) mine += units_of<TN>(span_of<TN>(p, i));
+    for (int i = lo; i < hi; ++i) mine += units_of<C>(span_of<C>(p, i));
     int64_t before = mine;
 #pragma unroll
     for (int d = 1; d < 32; d <<= 1) {
@@ -540,7 +547,7 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
     before -= mine;
     const int64_t all = total * rows, shares = min(all, (int64_t)p.shares);
     for (int64_t i = blockIdx.x; i < p.B; i += gridDim.x) {  // sequences that see nothing
-      if (units_of<TN>(span_of<TN>(p, (int)i)) > 0) continue;
+      if (units_of<C>(span_of<C>(p, (int)i)) > 0) continue;
       const int64_t heads = (int64_t)p.t * p.q_heads, words = heads * D / 2;
       for (int64_t k = tid; k < words; k += C::kThreads) reinterpret_cast<uint32_t*>(p.out)[i * words + k] = 0u;
       if (p.lse)
@@ -555,13 +562,13 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
         if (edge >= before * rows && edge < (before + mine) * rows) {
           int i = lo;
           int64_t at = before;
-          int u = units_of<TN>(span_of<TN>(p, i));
+          int u = units_of<C>(span_of<C>(p, i));
           while (i < hi - 1 && edge >= (at + u) * rows) {
             at += u;
-            u = units_of<TN>(span_of<TN>(p, ++i));
+            u = units_of<C>(span_of<C>(p, ++i));
           }
           const int64_t into = u > 0 ? (edge - at * rows) % u : 0;
-          sh.edge[k] = into <= kRowCost ? edge - into : edge;
+          sh.edge[k] = into <= C::kRowCost ? edge - into : edge;
           if (k == 0) sh.edge_b = i, sh.before = at;
         } else if (edge == all && tid == 0) {
           sh.edge[k] = all;
@@ -738,7 +745,8 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
 #pragma unroll 2
             for (int x = tl; x < (TN - row0) * units; x += 128) {
               const int y = x / units, u = x - y * units, row = row0 + y;
-              const uint4 v = lds128(ring + place_v * C::kSlot + row * 128 + (u >> 3) * C::kBlock + (((u & 7) ^ (row & 7)) << 4));
+              const uint4 v =
+                  lds128(ring + place_v * C::kSlot + row * 128 + (u >> 3) * C::kBlock + (((u & 7) ^ (row & 7)) << 4));
               const uint32_t z[4] = {v.x, v.y, v.z, v.w};
               bool odd = false;
 #pragma unroll
@@ -1329,15 +1337,13 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
             __syncwarp();
             if (ok) {
               const int row = tok - in_table * p.c.page_size, kv = what & 1;
-              const uint32_t to = raw_tiles + n * C::kRawTile;
+              const uint32_t to = raw_tiles + n * C::kRawTile, byte_to = to + 2 * C::kCodes + kv * TN * 16 + box * box_pitch;
               if (what < 2)
                 tma_load_4d(to + kv * C::kCodes + box * p.box * (D / 2), &tm.rows[kv], 0, row, w.head, page, bar);
               else if (p.scale_by_head)
-                tma_load_4d(to + 2 * C::kCodes + kv * TN * 16 + box * box_pitch, &tm.scales[kv], w.head * (D / 16) & ~15, row, 0,
-                            page, bar);
+                tma_load_4d(byte_to, &tm.scales[kv], w.head * (D / 16) & ~15, row, 0, page, bar);
               else
-                tma_load_4d(to + 2 * C::kCodes + kv * TN * 16 + box * box_pitch, &tm.scales[kv], D == 256 ? 2 * row : row, 0, w.head,
-                            page, bar);
+                tma_load_4d(byte_to, &tm.scales[kv], D == 256 ? 2 * row : row, 0, w.head, page, bar);
             }
             __syncwarp();
             asked = g + 1;
@@ -1370,7 +1376,8 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
         }
       }
       if (dead && asked > 0)  // the copies in flight land before the CTA ends
-        mbar_wait(smem_u32(&sh.raw_full[(asked - 1) % C::kRawDepth]), ((asked - 1) / C::kRawDepth) & 1, nullptr, kWaitLimitNs);
+        mbar_wait(smem_u32(&sh.raw_full[(asked - 1) % C::kRawDepth]), ((asked - 1) / C::kRawDepth) & 1, nullptr,
+                  kWaitLimitNs);
     }
   } else if constexpr (kFp4) {
     // ================================================= producers of a MixFP4 cache: codes in, f16 out
@@ -1397,12 +1404,13 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
         cp_wait_at_most(later);
       dead = __any_sync(kAll, dead);
       const uint32_t bytes = raw + 2 * C::kCodes + piece + (p.box && p.scale_by_head ? w.head * (D / 16) & 15 : 0);
-#pragma unroll 1
+#pragma unroll 1  // one copy of the code: the instruction caches are shared by all roles (214 us written out, 204 so)
       for (int kv = 0; kv < 2; ++kv) {
         const uint32_t q = 2 * sent + kv, slot = q % C::kSlots;
         Codes<kSteps> c;
         if (piece * 16 < D)
-          c.load(raw + kv * C::kCodes + (row0 + r0) * pitch + piece * 8, L::kRowsAtOnce * pitch, bytes + kv * TN * 16, scales);
+          c.load(raw + kv * C::kCodes + (row0 + r0) * pitch + piece * 8, L::kRowsAtOnce * pitch, bytes + kv * TN * 16,
+                 scales);
         waits(sh.empty[slot], ((q / C::kSlots) & 1) ^ 1, 1024u);
         if (piece * 16 < D) c.decode(ring + slot * C::kSlot, at_slot);
         fence_proxy_async_smem();
@@ -1569,9 +1577,9 @@ inline bool scales_by_token(const mixfp4_kv_cache& c) {
   return 16 % n == 0 && c.scale_token_stride == n && (c.scale_head_stride | c.scale_page_stride) % 16 == 0 &&
          aligned(c.k_scales, 16) && aligned(c.v_scales, 16);
 }
-// Rows that one TMA copy brings: of one page, and a part of a tile; 0 where TMA's rules do not allow it (pages of no
-// multiple of 16 tokens, rows of codes that are no multiple of 16 bytes or lie on none) or bf16 rows of less than 64
-// elements would not fill the operand's.
+// Rows that one TMA copy brings (bf16 at 8 drafts 187 us, by cp.async 222; MixFP4 203 and 287): of one page, and a part
+// of a tile; 0 where TMA's rules do not allow it (pages of no multiple of 16 tokens, rows of codes that are no multiple of
+// 16 bytes or lie on none) or bf16 rows of less than 64 elements would not fill the operand's.
 inline int box_of(const mixfp4_kv_cache& c, int tokens) {
   const bool fp4 = c.dtype == MIXFP4_CACHE_MIXFP4;
   if (c.page_size % 16 != 0 || c.pages == 0 || (fp4 ? c.head_dim % 32 != 0 : c.head_dim < 64)) return 0;
@@ -1620,7 +1628,8 @@ inline bool make_map_scales(CUtensorMap* m, const void* base, const mixfp4_kv_ca
   cuuint32_t boxes[4] = {(cuuint32_t)(by_head ? 16 : box * per_token), (cuuint32_t)(by_head ? box : 1), 1, 1};
   cuuint32_t estr[4] = {1, 1, 1, 1};
   return fn(m, type, 4, const_cast<void*>(base), dims, strides, boxes, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-            CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+            CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 template <int DT, int MT, bool kFp4>
