@@ -579,7 +579,7 @@ int mixfp4_paged_attention_workspace(const mixfp4_kv_cache* cache, int64_t B, in
 /*
  * mixfp4_tree_attention -- attention of up to 64 drafted tokens per sequence
  * over a mixfp4_kv_cache that holds them already (mixfp4_kv_append) behind the
- * tokens that are certain.  Sequence b has n = lengths[b] tokens in the cache,
+ * tokens that are certain (no counterpart in the paper).  Sequence b has n = lengths[b] tokens in the cache,
  * the last c = min(counts[b], t, n) of them drafts, the first p = n - c certain.
  * Bit k of mask[b][i] says whether draft i sees draft k (its own bit is asked for
  * like any other); without masks a draft sees those up to itself.  Draft i stands
@@ -670,7 +670,8 @@ int mixfp4_kv_fork(const mixfp4_kv_cache* cache, const int32_t* block_table, int
 
 /*
  * mixfp4_kv_copy_pages -- page src[i] of the cache copied to page dst[i], keys and
- * values (and scales), bit for bit.  The pages in dst differ, and are none of those
+ * values (and scales), bit for bit, as mixfp4_kv_fork copies a part of one: for
+ * pools that are compacted, and tables that a caller keeps.  The pages in dst differ, and are none of those
  * in src but their own: else what they hold afterwards is undefined.  A pair with a
  * page outside the cache is left out.
  *
