@@ -950,8 +950,8 @@ def mixfp4_tree_attention(q: torch.Tensor, cache: KVCache, block_table: torch.Te
         if workspace is None and _elsewhere(stream, cache.device) and H % cache.heads == 0 and t <= 64:
             workspace = _empty(tree_attention_workspace_bytes(cache, B, t, H), torch.uint8, cache.device, stream, True)
     r = _native().tree_attention(cache._address, cache._index, q, block_table, lengths, mask, counts, scale, window,
-                                 softcap, slopes, out, lse, return_lse, workspace, _ptr(status_word) if status_word is not None else None,
-                                 _stream(stream))
+                                 softcap, slopes, out, lse, return_lse, workspace,
+                                 _ptr(status_word) if status_word is not None else None, _stream(stream))
     if r.__class__ is int:
         _check("mixfp4_tree_attention", r)
     return r

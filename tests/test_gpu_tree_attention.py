@@ -239,6 +239,46 @@ def test_parts_of_many_tiles(fp4, t, n, B):
             assert torch.all((lse[b, i].double() - torch.logsumexp(s, -1)).abs() <= 2.0 ** -17 * (1 + s.abs().amax(-1)))
 
 
+@pytest.mark.parametrize("page", [16, 24])
+@pytest.mark.parametrize("fp4", [False, True])
+def test_pages_far_into_the_pool(fp4, page):
+    """Pages more than 2^32 bytes behind the first, by TMA and row by row, and moved there."""
+    o = ops()
+    Hkv, D, Hq, t, n = 4, 128, 8, 5, 900
+    row = D // 2 if fp4 else 2 * D
+    pages = (2 ** 32 + 2 ** 26) // (page * Hkv * row)
+    ts = dict(k_ts=torch.full((1,), 0.25, device=DEV), v_ts=torch.full((1,), 1.0, device=DEV)) if fp4 else {}
+    cache = o.empty_kv_cache(pages, page, Hkv, D, DEV, **ts)
+    held = -(-n // page) + 1
+    far = pages - 1 - torch.randperm(2 * held, device=DEV).to(torch.int32)
+    table = far[:held].view(1, -1)
+    at = torch.arange(n, device=DEV)
+    slots = table[0, at // page].long() * page + at % page
+    o.mixfp4_kv_append(randn(n, Hkv, D, seed=1), randn(n, Hkv, D, seed=2), cache, slots)
+    q = (randn(1, t, Hq, D, seed=5) * 1.5).to(torch.bfloat16)
+
+    def look(table, n):
+        at = torch.arange(n, device=DEV)
+        rows = o.mixfp4_kv_gather(cache, table[0, at // page].long() * page + at % page, torch.float32)
+        k, v = (x.double() for x in rows)
+        out, lse = o.mixfp4_tree_attention(q, cache, table, ints([n]), return_lse=True)
+        check(out, lse, q, k, v, [n], [t], [chain(t)], D ** -0.5, fp4)
+        return out
+    first = look(table, n)
+    o.mixfp4_kv_copy_pages(cache, far[:held], far[held:])
+    assert torch.equal(look(far[held:].view(1, -1), n), first)
+    path = ints([[0, 2, 3, -1]])
+    before = [x.clone() for x in o.mixfp4_kv_gather(cache, slots, torch.float32)]
+    length = o.mixfp4_kv_accept(cache, table, ints([n]), path, ints([t]))
+    assert length.tolist() == [n - t + 3]
+    after = o.mixfp4_kv_gather(cache, slots, torch.float32)
+    kept = [*range(n - t), n - t, n - t + 2, n - t + 3]
+    assert all(torch.equal(y[:n - t + 3], x[kept]) for x, y in zip(before, after))
+    tables, lengths = o.mixfp4_kv_fork(cache, table, length, ints([0, 0]), torch.stack([far[held], ints([-1])[0]]))
+    assert lengths.tolist() == length.tolist() * 2
+    assert torch.equal(look(tables[:1].contiguous(), n - t + 3), look(tables[1:].contiguous(), n - t + 3))
+
+
 @pytest.mark.parametrize("fp4", [False, True])
 @pytest.mark.parametrize("B,longest,t,D", [(1, 30000, 3, 64), (3, 9000, 24, 128), (150, 300, 2, 64), (700, 40, 1, 128),
                                            (1500, 20, 3, 16)])
