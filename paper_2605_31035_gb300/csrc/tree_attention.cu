@@ -156,8 +156,7 @@ struct Cfg {
   static constexpr int kSlot = kBlock * (DT / 64);
   static constexpr int kSoftmax = 4 * MT;                  // warps, four to a tile of rows
   static constexpr int kQ = MT * 128 * DT * 2;
-  // Warps that decode (16 in one team, or in two of 64 registers, were slower), or bring a bf16 cache's rows where TMA
-  // cannot.
+  // Warps that decode (196 us at 8 drafts; 16 of them 216), or bring a bf16 cache's rows where TMA cannot.
   static constexpr int kProducers = kFp4 ? 8 : 2;
   static constexpr int kThreads = (kSoftmax + 4 + (kFp4 ? kProducers : 0)) * 32;  // the four: products, TMA or helpers
   // Registers of a thread at launch, then of softmax and of the other threads (together no more than at launch).
