@@ -1255,9 +1255,11 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
           __syncwarp();
         }
       }
-      if (dead)  // the copies in flight land before the CTA ends
-        for (uint32_t n = g > C::kSlots / 2 ? g - C::kSlots / 2 : 0; n < g; ++n)
-          mbar_wait(smem_u32(&sh.full[(2 * n + kv) % C::kSlots]), ((2 * n + kv) / C::kSlots) & 1, nullptr, kWaitLimitNs);
+      // The copies in flight land before the CTA ends, also where those who would have waited for them have given up: the
+      // last use of each slot.
+      for (uint32_t q = 2 * g > C::kSlots ? 2 * g - C::kSlots : 0; q < 2 * g; ++q)
+        if ((int)(q & 1) == kv)
+          mbar_wait(smem_u32(&sh.full[q % C::kSlots]), (q / C::kSlots) & 1, nullptr, kWaitLimitNs);
     }
   } else if (!kFp4) {
     // ================================================= or by cp.async, row by row, by two warps
@@ -1374,9 +1376,11 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
           }
         }
       }
-      if (dead && asked > 0)  // the copies in flight land before the CTA ends
-        mbar_wait(smem_u32(&sh.raw_full[(asked - 1) % C::kRawDepth]), ((asked - 1) / C::kRawDepth) & 1, nullptr,
-                  kWaitLimitNs);
+      // The copies in flight land before the CTA ends, as above.
+      const uint32_t end = !p.box ? 0 : (dead ? asked : g);
+      for (uint32_t n = end > C::kRawDepth ? end - C::kRawDepth : 0; n < end; ++n)
+        if ((int)(n & 1) == me)
+          mbar_wait(smem_u32(&sh.raw_full[n % C::kRawDepth]), (n / C::kRawDepth) & 1, nullptr, kWaitLimitNs);
     }
   } else if constexpr (kFp4) {
     // ================================================= producers of a MixFP4 cache: codes in, f16 out
