@@ -24,9 +24,11 @@
 //     whose rows lie together: 187 instead of 200 us at 8 drafts, 412 instead of 505 at 64.
 //
 // Measured on 64 sequences of up to 8192 tokens, 32 query heads on 8, 128 dimensions (bf16 cache 1.1 GB, MixFP4 0.3 GB):
-// bf16 183 us at 8 drafts (6.0 TB/s: bound by HBM), 195 at 16, 383 at 64 (645 TFLOP/s: bound by the tensor cores, which
-// take P in two parts, and by what the softmax of 256 rows issues); MixFP4 196 us at 8 and 448 at 64 drafts, bound by the
-// instructions of decoding and of the softmax (half of the issue slots used, a fifth of all waits for instructions).
+// bf16 182 us at 8 drafts (6.0 TB/s: bound by HBM), 195 at 16, 378 at 64 (653 TFLOP/s: bound by the tensor cores, which
+// take P in two parts, and by what the softmax of 256 rows issues); MixFP4 194 us at 8 and 446 at 64 drafts, bound by the
+// instructions of decoding and of the softmax (half of the issue slots used).  Short rows are bound by their beginning
+// and end, some 7 us each: 142 sequences of 2 tokens with 32 key heads, 30 rows to an SM, 112 us, MixFP4 224.
+// The rules below give both sides as they were measured when the rule was made.
 #include <cuda_runtime.h>
 #include <atomic>
 #include <cstdint>
@@ -740,9 +742,11 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
           if (uneven) {  // a NaN or an infinity in V, in a row that not all see?
             bool bad = false;
             constexpr uint32_t kExp = kFp4 ? 0x7C00u : 0x7F80u;
-            const int row0 = edge ? 0 : max(w.s.first - j0, 0), units = D / 8;
+            // From the first row that not all see to the last that there is (of short rows few: 142 sequences of 2 tokens
+            // with 32 key heads 291 us with the tile's other rows, 224 without).
+            const int row0 = edge ? 0 : max(w.s.first - j0, 0), rows_v = min(TN, w.s.end - j0) - row0, units = D / 8;
 #pragma unroll 2
-            for (int x = tl; x < (TN - row0) * units; x += 128) {
+            for (int x = tl; x < rows_v * units; x += 128) {
               const int y = x / units, u = x - y * units, row = row0 + y;
               const uint4 v =
                   lds128(ring + place_v * C::kSlot + row * 128 + (u >> 3) * C::kBlock + (((u & 7) ^ (row & 7)) << 4));
