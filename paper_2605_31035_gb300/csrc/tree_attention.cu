@@ -25,7 +25,7 @@
 //
 // Measured on 64 sequences of up to 8192 tokens, 32 query heads on 8, 128 dimensions (bf16 cache 1.1 GB, MixFP4 0.3 GB):
 // bf16 182 us at 8 drafts (6.0 TB/s: bound by HBM), 195 at 16, 378 at 64 (653 TFLOP/s: bound by the tensor cores, which
-// take P in two parts, and by what the softmax of 256 rows issues); MixFP4 194 us at 8 and 446 at 64 drafts, bound by the
+// take P in two parts, and by what the softmax of 256 rows issues); MixFP4 182 us at 8 and 457 at 64 drafts, bound by the
 // instructions of decoding and of the softmax (half of the issue slots used).  Short rows are bound by their beginning
 // and end, some 7 us each: 142 sequences of 2 tokens with 32 key heads, 30 rows to an SM, 112 us, MixFP4 224.
 // The rules below give both sides as they were measured when the rule was made.
@@ -1408,7 +1408,7 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
       if (p.box)
         wait(sh.raw_full[n], (sent / C::kRawDepth) & 1, 1u << 19);
       else
-        cp_wait_at_most(later);
+        cp_wait_at_most(later), __syncwarp();
       dead = __any_sync(kAll, dead);
       const uint32_t bytes = raw + 2 * C::kCodes + piece + (p.box && p.scale_by_head ? w.head * (D / 16) & 15 : 0);
 #pragma unroll 1  // one copy of the code: the instruction caches are shared by all roles (214 us written out, 204 so)
@@ -1426,6 +1426,25 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
       }
       if (p.box && lane == 0) mbar_arrive(smem_u32(&sh.raw_empty[n]));
       ++sent;
+    };
+    // Rows of an odd number of scale bytes (or of pairs): a lane to a byte, asked for with a tile's codes and put in place
+    // before the next tile's are, so that no warp waits for them (80 dimensions 922 us where they did, 708 so).
+    constexpr int kMost = (2 * kRows * 15 + 31) / 32;
+    uint32_t odd[kMost], odd_at = 0;  // of a tile, and where its rows' bytes go; 0: none
+    auto each_byte = [&](auto&& f) {  // f(k, row, keys or values, byte)
+      const int bytes = D / 16, rows_on = 32 / bytes, bytes_on = 32 - rows_on * bytes;
+      int y = lane / bytes, e = lane - y * bytes;
+#pragma unroll
+      for (int k = 0; k < kMost; ++k) {
+        if (32 * k >= 2 * kRows * bytes) break;
+        if (y < 2 * kRows) f(k, y & (kRows - 1), y / kRows, e);
+        y += rows_on, e += bytes_on;
+        if (e >= bytes) e -= bytes, ++y;
+      }
+    };
+    auto put_bytes = [&] {
+      if (odd_at) each_byte([&](int k, int r, int kv, int e) { sts8(odd_at + (kv * TN + r) * 16 + e, odd[k]); });
+      odd_at = 0;
     };
     while (walk.next(p, mate, w)) {
 #pragma unroll 1
@@ -1462,25 +1481,14 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
               for (int k = 0; k < D / 16; k += 4) cp_async<4>(sd + k, src + k, ok);
             }
           }
-        } else {  // rows of an odd number of scale bytes: a lane to a byte
-          const int bytes = D / 16;
-          constexpr int kMost = (2 * kRows * 15 + 31) / 32;
-          uint32_t b[kMost];
-#pragma unroll
-          for (int k = 0; k < kMost; ++k) {
-            const int x = lane + 32 * k, y = x / bytes, r = y & (kRows - 1), kv = y / kRows;
-            b[k] = 0u;
-            if (kv < 2) {
-              const uint4 z = lds128(at + r * 16);
-              if ((int32_t)z.y >= 0)
-                b[k] = (kv ? p.c.v_scales : p.c.k_scales)[(int64_t)((u64)z.z | (u64)z.w << 32) + x - y * bytes];
-            }
-          }
-#pragma unroll
-          for (int k = 0; k < kMost; ++k) {
-            const int x = lane + 32 * k, y = x / bytes, r = y & (kRows - 1), kv = y / kRows;
-            if (kv < 2) sts8(bytes_at + (kv * TN + r) * 16 + x - y * bytes, b[k]);
-          }
+        } else {
+          put_bytes();
+          each_byte([&](int k, int r, int kv, int e) {
+            const uint4 z = lds128(at + r * 16);
+            odd[k] = 0u;
+            if ((int32_t)z.y >= 0) odd[k] = (kv ? p.c.v_scales : p.c.k_scales)[(int64_t)((u64)z.z | (u64)z.w << 32) + e];
+          });
+          odd_at = bytes_at;
         }
         cp_commit();
         __syncwarp();
@@ -1488,6 +1496,7 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
         if (g - sent >= C::kRawDepth - 1) hand_over(C::kRawDepth - 1);
       }
     }
+    put_bytes();
     while (sent < g) hand_over((int)(g - sent - 1));
     cp_async_wait_all();
   }
