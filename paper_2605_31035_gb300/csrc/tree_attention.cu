@@ -24,10 +24,10 @@
 //     whose rows lie together: 187 instead of 200 us at 8 drafts, 412 instead of 505 at 64.
 //
 // Measured on 64 sequences of up to 8192 tokens, 32 query heads on 8, 128 dimensions (bf16 cache 1.1 GB, MixFP4 0.3 GB):
-// bf16 182 us at 8 drafts (6.0 TB/s: bound by HBM), 195 at 16, 378 at 64 (653 TFLOP/s: bound by the tensor cores, which
-// take P in two parts, and by what the softmax of 256 rows issues); MixFP4 182 us at 8 and 457 at 64 drafts, bound by the
+// bf16 182 us at 8 drafts (6.0 TB/s: bound by HBM), 197 at 16, 381 at 64 (648 TFLOP/s: bound by the tensor cores, which
+// take P in two parts, and by what the softmax of 256 rows issues); MixFP4 180 us at 8 and 418 at 64 drafts, bound by the
 // instructions of decoding and of the softmax (half of the issue slots used).  Short rows are bound by their beginning
-// and end, some 7 us each: 142 sequences of 2 tokens with 32 key heads, 30 rows to an SM, 112 us, MixFP4 224.
+// and end, some 7 us each: 142 sequences of 2 tokens with 32 key heads, 30 rows to an SM, 108 us, MixFP4 219.
 // The rules below give both sides as they were measured when the rule was made.
 #include <cuda_runtime.h>
 #include <atomic>
@@ -626,7 +626,8 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
       // neighbouring lanes, to each copy's place.
       float fs = p.scale * (kFp4 ? kFp4Unit * kts : 1.0f);
       {
-        constexpr int kLanes = DT / 8, kRowsAtOnce = 32 / kLanes, kBatch = 8;  // steps asked for at once
+        constexpr int kLanes = DT / 8, kRowsAtOnce = 32 / kLanes;
+        constexpr int kBatch = 4;  // steps asked for at once (2: 399 us at 64 drafts, 4: 380, 8: 382)
         const int steps_q = kLanes / copies, u = lane % kLanes, base = copy * (32 / copies) + lane / kLanes;
         const int64_t from = valid ? (int64_t)w.b * p.q_stride + (int64_t)i * p.q_token_stride + (int64_t)h * p.q_head_stride
                                    : -1;
@@ -1139,7 +1140,10 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
           if (!*reinterpret_cast<volatile int*>(&sh.skip[buf])) {
             const uint64_t v = smem_desc_sw128_mn(ring + slot * C::kSlot, C::kBlock);
             const uint32_t o = tmem + C::kScoreCols + m * DT;
-#pragma unroll
+            // Not written out, as the softmax's queries are not, for the instruction caches' sake: MixFP4 at 8 drafts 182 us
+            // with all of it unrolled, 180 so (and 186 one by one); at 64 drafts 457, 435 and 417.
+            constexpr int kAtOnce = kFp4 && MT == 2 ? 1 : 2;
+#pragma unroll kAtOnce
             for (int k = 0; k < TN / 16; ++k) {
               const uint32_t a = tmem + buf * TN + (k * 16 / CW) * CW + (k * 16 % CW) / 2;
               // A copy's tokens go to its lanes of O alone; the first of them begin it.
@@ -1430,7 +1434,7 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
     // Rows of an odd number of scale bytes (or of pairs): a lane to a byte, asked for with a tile's codes and put in place
     // before the next tile's are, so that no warp waits for them (80 dimensions 922 us where they did, 708 so).
     constexpr int kMost = (2 * kRows * 15 + 31) / 32;
-    uint32_t odd[kMost], odd_at = 0;  // of a tile, and where its rows' bytes go; 0: none
+    uint32_t odd[kMost] = {}, odd_at = 0;  // of a tile, and where its rows' bytes go; 0: none
     auto each_byte = [&](auto&& f) {  // f(k, row, keys or values, byte)
       const int bytes = D / 16, rows_on = 32 / bytes, bytes_on = 32 - rows_on * bytes;
       int y = lane / bytes, e = lane - y * bytes;
