@@ -17,9 +17,9 @@
 //     once for both.  412 instead of 435 us at 64 drafts, 469 instead of 581 on a MixFP4 cache; 40 drafts 392 and 399.
 //   * On a bf16 cache the weights keep 16 bits in two bf16 parts of one sign; on a MixFP4 one f16's 11, and the queries
 //     are scaled per row by a power of two into f16.
-//   * Where rows of a tile see different tokens (drafts, a window's edge), a weight of 0 would still make NaN of an
-//     infinite or NaN element of V.  Such tiles are looked over for those, and where there is one the threads take the
-//     products themselves, of what each row sees alone.
+//   * Where rows of a tile see different tokens (drafts, a window's edge; one draft alone whose own bit is off sees less
+//     than there is), a weight of 0 would still make NaN of an infinite or NaN element of V.  Such tiles are looked over
+//     for those, and where there is one the threads take the products themselves, of what each row sees alone.
 //   * Tokens are cut into equal shares over the device.  CTAs of neighbouring heads walk the same tokens at the same time,
 //     whose rows lie together: 187 instead of 200 us at 8 drafts, 412 instead of 505 at 64.
 //
@@ -725,7 +725,8 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
 #pragma unroll
         for (int k = 0; k < C::kWords; ++k) whole = whole && there[k] == kAll;
         const bool edge = p.window > 0 && j0 < w.s.first + w.s.c - p.window;  // some rows' windows begin behind j0
-        const bool uneven = w.s.c > 1 && (edge || j0 + TN > w.s.first);       // rows may see different tokens
+        // Rows may see different tokens, or none may see the only draft.
+        const bool uneven = (w.s.c > 1 && edge) || (j0 + TN > w.s.first && (w.s.c > 1 || !(sh.bits[0] & 1)));
         const bool masked = !whole || edge || j0 + TN > w.s.first;
         const bool general = masked || !plain;
 
