@@ -725,8 +725,8 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
 #pragma unroll
         for (int k = 0; k < C::kWords; ++k) whole = whole && there[k] == kAll;
         const bool edge = p.window > 0 && j0 < w.s.first + w.s.c - p.window;  // some rows' windows begin behind j0
-        // Rows may see different tokens, or none may see the only draft.
-        const bool uneven = (w.s.c > 1 && edge) || (j0 + TN > w.s.first && (w.s.c > 1 || !(sh.bits[0] & 1)));
+        // Rows may see different tokens, or, by a mask, none the only draft.
+        const bool uneven = (w.s.c > 1 || p.mask) && (edge || j0 + TN > w.s.first);
         const bool masked = !whole || edge || j0 + TN > w.s.first;
         const bool general = masked || !plain;
 
