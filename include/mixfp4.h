@@ -773,6 +773,26 @@ int mixfp4_selftest_gemm_missed_stage(const uint8_t* a_codes, const uint8_t* a_s
                                       int64_t N, int64_t K, float* C, int64_t ldc, uint32_t* status_word,
                                       uint64_t limit_ns, void* stream);
 
+/*
+ * mixfp4_selftest_tree_attention_missed_rows -- check of the failure path of
+ * mixfp4_tree_attention's kernel: a chain of t drafts a sequence, dense q and
+ * table, scale 1/8, with every wait limited to limit_ns and with the keys (of a
+ * MixFP4 cache: the codes, or their addresses) of every CTA's first tile never
+ * sent.  The waits on them run out; whoever gives up first sets its bit in
+ * *status_word, and every role then stops, lets what it has in flight land, and
+ * exits.  What out holds afterwards is undefined.  Nothing faults or hangs, and the
+ * device stays usable.
+ *
+ * Arguments as mixfp4_tree_attention (B, t, q_heads >= 1; head dimensions of 80 to 128).
+ * status_word  device, one uint32, 4-byte aligned, required (zeroed first).
+ * limit_ns     1 .. 2e9 (else MIXFP4_ERR_ARG); the call takes a few limit_ns.
+ */
+int mixfp4_selftest_tree_attention_missed_rows(const void* q, int64_t B, int64_t t, int64_t q_heads,
+                                               const mixfp4_kv_cache* cache, const int32_t* block_table,
+                                               int64_t table_pages, const int32_t* lengths, void* out, void* workspace,
+                                               int64_t workspace_bytes, uint32_t* status_word, uint64_t limit_ns,
+                                               void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -9,7 +9,8 @@
 //   * Roles: rows of K and V come by TMA into a ring, boxes of one page, where the strides allow it, by cp.async
 //     otherwise; a MixFP4 cache's codes and scale bytes come the same ways and eight warps write them into the ring as
 //     exact f16.  One thread issues the products, one warp reads the next part of the work ahead.  Every wait ends
-//     after a second at the latest, with an error in the status word.
+//     after a second at the latest, with an error in the status word; what is in flight then still lands before
+//     the CTA ends.
 //   * Few rows: 32 (or 64) rows are held four times (twice) in the 128 lanes and each copy takes its quarter (half) of a
 //     tile's tokens, by products that write its lanes of O alone; the copies are joined at the end.  A thread then has a
 //     quarter of the scores: 187 instead of 201 us at 8 drafts below, 204 instead of 255 on a MixFP4 cache.
@@ -90,6 +91,7 @@ struct TreeArgs {
   float2* stat;  // [2 grid][row tiles][128] (m, l) of parts
   float4* part;  // [2 grid][row tiles][dimensions / 4][128]: O of parts, and what a row in work has set aside
   uint32_t* status;
+  uint64_t wait_ns;  // of the self-test: the limit of every wait
   int box;  // rows of a page that one TMA copy brings; 0: cp.async does
   // A MixFP4 cache's scale bytes by TMA: bytes from one row's to the next in shared memory, and whether a copy brings
   // those of neighbouring heads of a token (16 bytes) or of neighbouring tokens of a head.
@@ -476,7 +478,9 @@ struct Codes {
   }
 };
 
-template <int DT, int MT, bool kFp4>
+// kWithheld: the self-test of the failure path, in which rows of a CTA's first tile are never sent (an argument instead of
+// a variant cost 2 to 4 % on a MixFP4 cache).
+template <int DT, int MT, bool kFp4, bool kWithheld>
 __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>::kCtas)
     tree_attention_kernel(const TreeArgs p, const __grid_constant__ Maps tm) {
   using C = Cfg<DT, MT, kFp4>;
@@ -582,9 +586,13 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
     if (tid == 0) sh.all = all, sh.shares = shares;
   }
   const uint32_t tmem = sh.tmem;
-  bool dead = false;  // a wait has run out: no more waits and no more results, but every step, so that all warps meet
+  // A wait has run out: no more waits and no more results, but every step, so that all warps meet.  Slots are then freed too
+  // early and places not written: whoever asks for copies looks at the flag as well before each, and whoever reads places
+  // stops.
+  bool dead = false;
+  const uint64_t limit = kWithheld ? p.wait_ns : kWaitLimitNs;
   auto wait = [&](uint64_t& bar, uint32_t parity, uint32_t bit) {
-    if (!dead && !mbar_wait(smem_u32(&bar), parity, abort_flag, kWaitLimitNs)) {
+    if (!dead && !mbar_wait(smem_u32(&bar), parity, abort_flag, limit)) {
       dead = true;
       if (p.status && !*abort_flag) atomicOr(p.status, bit);
       *abort_flag = 1;
@@ -607,7 +615,7 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
     uint32_t g = 0, turn = 0;  // tiles and parts before this one
     for (;;) {
       // All warps of softmax have the same parts and so meet at the same barriers, also where a wait has run out.
-      if (bar_or(1, C::kSoftmax * 32, !mbar_wait(smem_u32(&sh.told), turn & 1, nullptr, kWaitLimitNs))) break;
+      if (bar_or(1, C::kSoftmax * 32, !mbar_wait(smem_u32(&sh.told), turn & 1, nullptr, limit))) break;
       w = sh.part;
       if (w.tiles == 0) break;
       const int R = min(128 * MT, p.t * p.group - w.chunk * 128 * MT);
@@ -1187,7 +1195,7 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
         }
       }
       mma_commit(smem_u32(&sh.end));
-      mbar_wait(smem_u32(&sh.end), 0, nullptr, kWaitLimitNs);
+      mbar_wait(smem_u32(&sh.end), 0, nullptr, limit);
     }
   } else if (warp == C::kSoftmax + 3) {
     // ================================================= reads a part ahead for softmax, and asks for its queries
@@ -1231,7 +1239,7 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
       const int box = lane % boxes, block = lane / boxes;
       const bool mine = block < blocks;
       uint32_t g = 0;
-      while (walk.next(p, mate, w)) {
+      while (!dead && walk.next(p, mate, w)) {
         const int32_t* table = p.table + (int64_t)w.b * p.table_stride;
         auto page_of = [&](int tok) { return p.page_shift >= 0 ? tok >> p.page_shift : tok / p.c.page_size; };
         // Page of this lane's box of the tile.
@@ -1254,8 +1262,9 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
           __syncwarp();
           const uint32_t q = 2 * g + kv, slot = q % C::kSlots, bar = smem_u32(&sh.full[slot]);
           wait(sh.empty[slot], ((q / C::kSlots) & 1) ^ 1, 1024u);
-          dead = __any_sync(kAll, dead);
+          dead = __any_sync(kAll, dead || *abort_flag);
           if (dead) break;
+          if (kWithheld && q == 0) continue;
           if (lane == 0) mbar_arrive_expect_tx(bar, bytes);
           __syncwarp();
           if (ok)
@@ -1268,7 +1277,7 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
       // last use of each slot.
       for (uint32_t q = 2 * g > C::kSlots ? 2 * g - C::kSlots : 0; q < 2 * g; ++q)
         if ((int)(q & 1) == kv)
-          mbar_wait(smem_u32(&sh.full[q % C::kSlots]), (q / C::kSlots) & 1, nullptr, kWaitLimitNs);
+          mbar_wait(smem_u32(&sh.full[q % C::kSlots]), (q / C::kSlots) & 1, nullptr, limit);
     }
   } else if (!kFp4) {
     // ================================================= or by cp.async, row by row, by two warps
@@ -1277,10 +1286,10 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
       constexpr int kRows = C::kRows, kPieces = DT / 8, kRowsAtOnce = 32 / kPieces;
       const int piece = lane % kPieces, r0 = lane / kPieces;
       uint32_t g = 0, q = 0;
-      while (walk.next(p, mate, w)) {
+      while (!dead && walk.next(p, mate, w)) {
         const int32_t* table = p.table + (int64_t)w.b * p.table_stride;
 #pragma unroll 1
-        for (int it = 0; it < w.tiles; ++it, ++g) {
+        for (int it = 0; it < w.tiles && !dead; ++it, ++g) {
           const int tok0 = w.s.from + (w.tile + w.tiles - 1 - it) * TN + pw * kRows;
           int64_t at[kRows / 32];  // of tokens lane, lane + 32; < 0: not there
 #pragma unroll
@@ -1301,6 +1310,8 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
             const uint8_t* base = static_cast<const uint8_t*>(kv ? p.c.v : p.c.k);
             const uint32_t slot = q % C::kSlots;
             waits(sh.empty[slot], ((q / C::kSlots) & 1) ^ 1, 1024u);
+            if (dead) break;
+            if (kWithheld && q == 0) continue;
             const uint32_t dst = ring + slot * C::kSlot + (piece >> 3) * C::kBlock + pw * kRows * 128;
 #pragma unroll
             for (int j = 0; j < kRows / 32; ++j)
@@ -1339,8 +1350,11 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
             const uint32_t good = __ballot_sync(kAll, here), n = g % C::kRawDepth, bar = smem_u32(&sh.raw_full[n]);
             if (lane < TN / 32) sh.there[g % kThere][lane] = there_of(p, w.s, j0 + lane * 32, lane * 32, good);
             __syncwarp();
-            waits(sh.raw_empty[n], ((g / C::kRawDepth) & 1) ^ 1, 1u << 18);
+            wait(sh.raw_empty[n], ((g / C::kRawDepth) & 1) ^ 1, 1u << 18);
+            dead = __any_sync(kAll, dead || *abort_flag);
             if (dead) break;
+            asked = g + 1;
+            if (kWithheld && g == 0) continue;
             const int bytes = what < 2 ? p.box * (D / 2) : (p.scale_by_head ? p.box * 16 : p.box * (D / 16));
             const int all = __reduce_add_sync(kAll, ok ? bytes : 0);
             if (lane == 0) mbar_arrive_expect_tx(bar, (uint32_t)all);
@@ -1356,7 +1370,6 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
                 tma_load_4d(byte_to, &tm.scales[kv], D == 256 ? 2 * row : row, 0, w.head, page, bar);
             }
             __syncwarp();
-            asked = g + 1;
           } else {  // where each row lies
             const uint32_t at = places + (g % C::kAddresses) * (TN * 16);
             int page[TN / 32];
@@ -1366,6 +1379,8 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
               page[j] = tok >= w.s.low && tok < w.s.end ? table[page_of(tok)] : -1;
             }
             waits(sh.used[g % C::kAddresses], ((g / C::kAddresses) & 1) ^ 1, 2048u);
+            if (dead) break;
+            if (kWithheld && g == 0) continue;
 #pragma unroll
             for (int j = 0; j < TN / 32; ++j) {
               const int tok = j0 + 32 * j + lane, off = tok - page_of(tok) * p.c.page_size;
@@ -1389,7 +1404,7 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
       const uint32_t end = !p.box ? 0 : (dead ? asked : g);
       for (uint32_t n = end > C::kRawDepth ? end - C::kRawDepth : 0; n < end; ++n)
         if ((int)(n & 1) == me)
-          mbar_wait(smem_u32(&sh.raw_full[n % C::kRawDepth]), (n / C::kRawDepth) & 1, nullptr, kWaitLimitNs);
+          mbar_wait(smem_u32(&sh.raw_full[n % C::kRawDepth]), (n / C::kRawDepth) & 1, nullptr, limit);
     }
   } else if constexpr (kFp4) {
     // ================================================= producers of a MixFP4 cache: codes in, f16 out
@@ -1459,6 +1474,7 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
           continue;
         }
         waits(sh.placed[g % C::kAddresses], (g / C::kAddresses) & 1, 4096u);
+        if (dead) break;
         const uint32_t at = places + (g % C::kAddresses) * (TN * 16) + row0 * 16;
         const uint32_t raw = raw_tiles + (g % C::kRawDepth) * C::kRawTile, bytes_at = raw + 2 * C::kCodes + row0 * 16;
 #pragma unroll
@@ -1653,7 +1669,7 @@ inline bool make_map_scales(CUtensorMap* m, const void* base, const mixfp4_kv_ca
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int DT, int MT, bool kFp4>
+template <int DT, int MT, bool kFp4, bool kWithheld = false>
 int launch(TreeArgs p, int grid, cudaStream_t s) {
   using C = Cfg<DT, MT, kFp4>;
   Maps maps = {};
@@ -1664,7 +1680,7 @@ int launch(TreeArgs p, int grid, cudaStream_t s) {
                             make_map_scales(&maps.scales[1], p.c.v_scales, p.c, p.box)))))
     p.box = 0;
   static std::atomic<uint64_t> done{0};
-  auto* kernel = tree_attention_kernel<DT, MT, kFp4>;
+  auto* kernel = tree_attention_kernel<DT, MT, kFp4, kWithheld>;
   if (!set_dynamic_smem_once(reinterpret_cast<const void*>(kernel), C::kSmem, done)) return MIXFP4_ERR_CUDA;
   kernel<<<grid, C::kThreads, C::kSmem, s>>>(p, maps);
   if (int st = launch_status()) return st;
@@ -1678,11 +1694,63 @@ int launch(TreeArgs p, int grid, cudaStream_t s) {
 
 template <bool kFp4>
 int launch_dim(const TreeArgs& p, int grid, int tiles, cudaStream_t s) {
+  if (p.wait_ns) return tiles == 2 ? launch<128, 2, kFp4, true>(p, grid, s) : launch<128, 1, kFp4, true>(p, grid, s);
   switch (padded_dim(p.c.head_dim)) {
     case 64: return tiles == 2 ? launch<64, 2, kFp4>(p, grid, s) : launch<64, 1, kFp4>(p, grid, s);
     case 128: return tiles == 2 ? launch<128, 2, kFp4>(p, grid, s) : launch<128, 1, kFp4>(p, grid, s);
     default: return launch<256, 1, kFp4>(p, grid, s);
   }
+}
+
+int tree_attention(const void* q, int64_t q_stride, int64_t q_token_stride, int64_t q_head_stride, int64_t B, int64_t t,
+                   int64_t q_heads, const mixfp4_kv_cache* cache, const int32_t* block_table, int64_t table_stride,
+                   int64_t table_pages, const int32_t* lengths, const int64_t* mask, int64_t mask_stride,
+                   const int32_t* counts, float scale, int64_t window, float softcap, const float* slopes, void* out,
+                   float* lse, void* workspace, int64_t workspace_bytes, uint32_t* status_word, uint64_t wait_ns,
+                   void* stream) {
+  int64_t need = 0;
+  if (int st = mixfp4_tree_attention_workspace(cache, B, t, q_heads, &need)) return st;
+  if (!(softcap == 0.0f || (softcap >= 1e-6f && softcap <= 1e6f))) return MIXFP4_ERR_ARG;
+  if (B > INT32_MAX || q_heads > INT32_MAX || q_stride < 0 || q_token_stride < 0 || q_head_stride < 0 ||
+      table_stride < 0 || table_pages < 0 || table_stride < table_pages ||
+      table_pages > (INT32_MAX - 4096) / cache->page_size || window < 0 || mask_stride < 0 ||
+      (mask_stride != 0 && mask_stride < t) || workspace_bytes < need)
+    return MIXFP4_ERR_SHAPE;
+  if (need == 0) return MIXFP4_OK;
+  if (!q || !out || !lengths || !workspace || (table_pages > 0 && !block_table)) return MIXFP4_ERR_NULL;
+  if (!aligned(q, 16) || q_stride % 8 || q_token_stride % 8 || q_head_stride % 8 || !aligned(block_table, 4) ||
+      !aligned(lengths, 4) || !aligned(mask, 8) || !aligned(counts, 4) || !aligned(slopes, 4) || !aligned(out, 16) ||
+      !aligned(lse, 4) || !aligned(workspace, 256) || !aligned(status_word, 4))
+    return MIXFP4_ERR_ALIGN;
+  TreeArgs p = {};
+  p.q = static_cast<const uint16_t*>(q);
+  p.q_stride = q_stride, p.q_token_stride = q_token_stride, p.q_head_stride = q_head_stride;
+  p.B = (int)B, p.t = (int)t, p.q_heads = (int)q_heads, p.group = (int)(q_heads / cache->heads);
+  p.c = *cache;
+  p.table = block_table, p.table_stride = table_stride, p.max_tokens = table_pages * cache->page_size;
+  p.lengths = lengths, p.mask = mask, p.mask_stride = mask_stride, p.counts = counts;
+  p.scale = scale, p.softcap = softcap, p.window = window, p.slopes = slopes;
+  p.out = static_cast<uint16_t*>(out), p.lse = lse;
+  p.status = status_word;
+  p.wait_ns = wait_ns;
+  const int tiles = row_tiles(cache, t, q_heads), grid = grid_of(cache, tiles);
+  const int64_t rows = t * p.group;
+  if (rows > INT32_MAX - 256) return MIXFP4_ERR_SHAPE;
+  p.chunks = (int)((rows + 128 * tiles - 1) / (128 * tiles));
+  p.together = together_of(cache);
+  p.shares = grid / p.together;
+  p.joined = p.max_tokens > tile_tokens(cache, tiles);  // rows of one tile are never cut
+  p.page_shift = -1;
+  for (int i = 0; i < 31; ++i)
+    if (cache->page_size == 1 << i) p.page_shift = i;
+  uint8_t* w = static_cast<uint8_t*>(workspace);
+  p.split = reinterpret_cast<int4*>(w);
+  w += ((int64_t)grid * 16 + 255) / 256 * 256;
+  p.stat = reinterpret_cast<float2*>(w);
+  p.part = reinterpret_cast<float4*>(w + 2 * (int64_t)grid * 128 * tiles * 8);
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (status_word && cudaMemsetAsync(status_word, 0, 4, s) != cudaSuccess) return MIXFP4_ERR_CUDA;
+  return cache->dtype == MIXFP4_CACHE_MIXFP4 ? launch_dim<true>(p, grid, tiles, s) : launch_dim<false>(p, grid, tiles, s);
 }
 
 }  // namespace
@@ -1710,49 +1778,24 @@ int mixfp4_tree_attention(const void* q, int64_t q_stride, int64_t q_token_strid
                           int64_t mask_stride, const int32_t* counts, float scale, int64_t window, float softcap,
                           const float* slopes, void* out, float* lse, void* workspace, int64_t workspace_bytes,
                           uint32_t* status_word, void* stream) {
-  using namespace mixfp4;
-  int64_t need = 0;
-  if (int st = mixfp4_tree_attention_workspace(cache, B, t, q_heads, &need)) return st;
-  if (!(softcap == 0.0f || (softcap >= 1e-6f && softcap <= 1e6f))) return MIXFP4_ERR_ARG;
-  if (B > INT32_MAX || q_heads > INT32_MAX || q_stride < 0 || q_token_stride < 0 || q_head_stride < 0 ||
-      table_stride < 0 || table_pages < 0 || table_stride < table_pages ||
-      table_pages > (INT32_MAX - 4096) / cache->page_size || window < 0 || mask_stride < 0 ||
-      (mask_stride != 0 && mask_stride < t) || workspace_bytes < need)
-    return MIXFP4_ERR_SHAPE;
-  if (need == 0) return MIXFP4_OK;
-  if (!q || !out || !lengths || !workspace || (table_pages > 0 && !block_table)) return MIXFP4_ERR_NULL;
-  if (!aligned(q, 16) || q_stride % 8 || q_token_stride % 8 || q_head_stride % 8 || !aligned(block_table, 4) ||
-      !aligned(lengths, 4) || !aligned(mask, 8) || !aligned(counts, 4) || !aligned(slopes, 4) || !aligned(out, 16) ||
-      !aligned(lse, 4) || !aligned(workspace, 256) || !aligned(status_word, 4))
-    return MIXFP4_ERR_ALIGN;
-  TreeArgs p = {};
-  p.q = static_cast<const uint16_t*>(q);
-  p.q_stride = q_stride, p.q_token_stride = q_token_stride, p.q_head_stride = q_head_stride;
-  p.B = (int)B, p.t = (int)t, p.q_heads = (int)q_heads, p.group = (int)(q_heads / cache->heads);
-  p.c = *cache;
-  p.table = block_table, p.table_stride = table_stride, p.max_tokens = table_pages * cache->page_size;
-  p.lengths = lengths, p.mask = mask, p.mask_stride = mask_stride, p.counts = counts;
-  p.scale = scale, p.softcap = softcap, p.window = window, p.slopes = slopes;
-  p.out = static_cast<uint16_t*>(out), p.lse = lse;
-  p.status = status_word;
-  const int tiles = row_tiles(cache, t, q_heads), grid = grid_of(cache, tiles);
-  const int64_t rows = t * p.group;
-  if (rows > INT32_MAX - 256) return MIXFP4_ERR_SHAPE;
-  p.chunks = (int)((rows + 128 * tiles - 1) / (128 * tiles));
-  p.together = together_of(cache);
-  p.shares = grid / p.together;
-  p.joined = p.max_tokens > tile_tokens(cache, tiles);  // rows of one tile are never cut
-  p.page_shift = -1;
-  for (int i = 0; i < 31; ++i)
-    if (cache->page_size == 1 << i) p.page_shift = i;
-  uint8_t* w = static_cast<uint8_t*>(workspace);
-  p.split = reinterpret_cast<int4*>(w);
-  w += ((int64_t)grid * 16 + 255) / 256 * 256;
-  p.stat = reinterpret_cast<float2*>(w);
-  p.part = reinterpret_cast<float4*>(w + 2 * (int64_t)grid * 128 * tiles * 8);
-  cudaStream_t s = static_cast<cudaStream_t>(stream);
-  if (status_word && cudaMemsetAsync(status_word, 0, 4, s) != cudaSuccess) return MIXFP4_ERR_CUDA;
-  return cache->dtype == MIXFP4_CACHE_MIXFP4 ? launch_dim<true>(p, grid, tiles, s) : launch_dim<false>(p, grid, tiles, s);
+  return mixfp4::tree_attention(q, q_stride, q_token_stride, q_head_stride, B, t, q_heads, cache, block_table,
+                                table_stride, table_pages, lengths, mask, mask_stride, counts, scale, window, softcap,
+                                slopes, out, lse, workspace, workspace_bytes, status_word, 0, stream);
+}
+
+int mixfp4_selftest_tree_attention_missed_rows(const void* q, int64_t B, int64_t t, int64_t q_heads,
+                                               const mixfp4_kv_cache* cache, const int32_t* block_table,
+                                               int64_t table_pages, const int32_t* lengths, void* out, void* workspace,
+                                               int64_t workspace_bytes, uint32_t* status_word, uint64_t limit_ns,
+                                               void* stream) {
+  if (B < 1 || t < 1 || q_heads < 1) return MIXFP4_ERR_SHAPE;
+  if (limit_ns == 0 || limit_ns > 2000000000ull) return MIXFP4_ERR_ARG;
+  if (!cache || !status_word) return MIXFP4_ERR_NULL;
+  if (cache->head_dim <= 64 || cache->head_dim > 128) return MIXFP4_ERR_SHAPE;
+  const int64_t row = q_heads * (int64_t)cache->head_dim;
+  return mixfp4::tree_attention(q, t * row, row, cache->head_dim, B, t, q_heads, cache, block_table, table_pages,
+                                table_pages, lengths, nullptr, 0, nullptr, 0.125f, 0, 0.0f, nullptr, out, nullptr,
+                                workspace, workspace_bytes, status_word, limit_ns, stream);
 }
 
 }  // extern "C"

@@ -104,6 +104,9 @@ def lib() -> ctypes.CDLL:
         L.mixfp4_paged_attention_workspace.argtypes = [ctypes.POINTER(_CKVCache), I64, I64, ctypes.POINTER(I64)]
         L.mixfp4_tree_attention_workspace.restype = I
         L.mixfp4_tree_attention_workspace.argtypes = [ctypes.POINTER(_CKVCache), I64, I64, I64, ctypes.POINTER(I64)]
+        L.mixfp4_selftest_tree_attention_missed_rows.restype = I
+        L.mixfp4_selftest_tree_attention_missed_rows.argtypes = [P, I64, I64, I64, ctypes.POINTER(_CKVCache), P, I64, P, P, P,
+                                                                 I64, P, ctypes.c_uint64, P]
         L.mixfp4_status_string.restype = ctypes.c_char_p
         L.mixfp4_status_string.argtypes = [I]
         L.mixfp4_version.restype = I
@@ -955,6 +958,31 @@ def mixfp4_tree_attention(q: torch.Tensor, cache: KVCache, block_table: torch.Te
     if r.__class__ is int:
         _check("mixfp4_tree_attention", r)
     return r
+
+
+def selftest_tree_attention_missed_rows(q: torch.Tensor, cache: KVCache, block_table: torch.Tensor,
+                                        lengths: torch.Tensor, limit_ns: int = 5_000_000, stream=None) -> int:
+    """Run mixfp4_tree_attention's kernel with the keys of every CTA's first tile withheld and short wait limits (q,
+    block_table and lengths as there, dense; head dimensions of 80 to 128); returns the status bits it reported (nonzero when the failure path
+    worked)."""
+    _check_cache(cache)
+    B, t, H, D = _shape(q, 4)
+    for x, dtype, shape, what in ((q, torch.bfloat16, (B, t, H, cache.head_dim), "q"),
+                                  (block_table, torch.int32, (B, *_shape(block_table, 2)[1:]), "block_table"),
+                                  (lengths, torch.int32, (B,), "lengths")):
+        _check_dev(x, cache.device, what)
+        _require(x.dtype is dtype and x.shape == shape and x.is_contiguous(), f"{what} must be a dense {dtype} tensor {shape}")
+    need = tree_attention_workspace_bytes(cache, B, t, H)
+    with _on(stream, cache.device):
+        status = torch.zeros(1, dtype=torch.int32, device=cache.device)
+        out, workspace = torch.empty_like(q), torch.empty(need, dtype=torch.uint8, device=cache.device)
+    _check("mixfp4_selftest_tree_attention_missed_rows",
+           lib().mixfp4_selftest_tree_attention_missed_rows(_ptr(q), B, t, H, ctypes.byref(cache._c), _ptr(block_table),
+                                                            block_table.shape[1], _ptr(lengths), _ptr(out),
+                                                            _ptr(workspace), need, _ptr(status), int(limit_ns),
+                                                            _stream(stream)))
+    torch.cuda.synchronize(cache.device)
+    return int(status.item())
 
 
 def mixfp4_kv_accept(cache: KVCache, block_table: torch.Tensor, lengths: torch.Tensor, path: torch.Tensor,
