@@ -539,8 +539,9 @@ int mixfp4_kv_gather(const mixfp4_kv_cache* cache, const int64_t* slots, int64_t
  * h / (q_heads / heads) and j over the sequence's tokens that are seen,
  *   s_j = scale * q . k_j,   out = sum_j exp(s_j - lse) v_j,   lse = log sum_j exp(s_j).
  * Products are exact, sums and the softmax in fp32 (the weights enter the
- * second product as two bf16 parts, or for a MixFP4 cache as f16 of 11 bits),
- * and out is rounded to bf16.  A sequence that sees no token gives out = 0 and
+ * second product as two bf16 parts, or for a MixFP4 cache as f16 of 11 bits; over
+ * one, elements of q below 2^-31 of their head's largest are off by up to 2^-39 of
+ * it), and out is rounded to bf16.  A sequence that sees no token gives out = 0 and
  * lse = -inf.  A score of NaN makes its head's out and lse NaN; one of +inf out
  * NaN and lse +inf; an infinite element of V makes out infinite (NaN if its
  * weight is below fp32's normal range).  The tokens' axis is cut over the GPU and
@@ -590,8 +591,9 @@ int mixfp4_paged_attention_workspace(const mixfp4_kv_cache* cache, int64_t B, in
  *   s = s - slopes[h] (x_i - x_j) with slopes;  window > 0: only where x_i - x_j < window,
  *   out = sum_j exp(s_j - lse) v_j,   lse = log sum_j exp(s_j).
  * Products are exact, sums and the softmax in fp32 (the weights enter the
- * second product as two bf16 parts, or for a MixFP4 cache as f16 of 11 bits), and
- * out is rounded to bf16.  A draft that sees nothing, and rows i >= c, give out = 0
+ * second product as two bf16 parts, or for a MixFP4 cache as f16 of 11 bits; over
+ * one, elements of q below 2^-31 of the largest of their draft and head are off by up
+ * to 2^-39 of it), and out is rounded to bf16.  A draft that sees nothing, and rows i >= c, give out = 0
  * and lse = -inf.  What a draft does not see does not reach its results, NaN and
  * infinities included.  Scores of NaN and +inf and infinities of V as
  * mixfp4_paged_attention has them, but that an infinity of V with a weight below 2^-80 of the

@@ -28,7 +28,8 @@
 //   * The weights P keep 16 bits of mantissa in two bf16 parts of one sign (one
 //     product each) on a bf16 cache.  On a MixFP4 cache a row's values times its block
 //     scales are exact in f16, Q is scaled per head by a power of two into f16
-//     (exact but for elements 2^-29 below the largest), and P takes 11 bits: the
+//     (exact but for elements below 2^-31 of the largest, which are off by up to
+//     2^-39 of it: half of f16's least step), and P takes 11 bits: the
 //     4-bit rows themselves hold 3.
 //   * Sequences differ in length, so the axis (sequence, key head, token) is cut
 //     into equal shares of 64-token units, one per CTA; where a CTA's share ends

@@ -17,7 +17,8 @@
 //   * More than 128 rows (and up to 128 dimensions): two tiles of rows to a CTA, so that K and V are fetched, and decoded,
 //     once for both.  412 instead of 435 us at 64 drafts, 469 instead of 581 on a MixFP4 cache; 40 drafts 392 and 399.
 //   * On a bf16 cache the weights keep 16 bits in two bf16 parts of one sign; on a MixFP4 one f16's 11, and the queries
-//     are scaled per row by a power of two into f16.
+//     are scaled per row by a power of two into f16: exact but for elements below 2^-31 of the row's largest, which are
+//     off by up to 2^-39 of it, half of f16's least step.
 //   * Where rows of a tile see different tokens (drafts, a window's edge; one draft alone whose own bit is off sees less
 //     than there is), a weight of 0 would still make NaN of an infinite or NaN element of V.  Such tiles are looked over
 //     for those, and where there is one the threads take the products themselves, of what each row sees alone.
