@@ -237,6 +237,21 @@ PyObject* kv_gather(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+const Tensor& table_of(PyObject* o, int64_t B, int64_t index) {
+  const Tensor* table = tensor(o);
+  if (!on(table, index) || table->scalar_type() != ScalarType::Int || table->dim() != 2 ||
+      (B >= 0 && table->size(0) != B) || (table->stride(1) != 1 && table->size(1) > 1))
+    refuse("%s must be an int32 CUDA tensor [%lld, pages] on device %lld with unit column stride", "block_table", B,
+           index);
+  return *table;
+}
+// A table's stride from row to row, at least its width.
+int64_t table_step(const Tensor& table) {
+  const int64_t pages = table.size(1);
+  if (table.size(0) > 1 && table.stride(0) < pages) refuse("%s must not have overlapping rows", "block_table");
+  return std::max(step(table, 0), pages);
+}
+
 // (cache, index, q, block_table, lengths, scale, window, out, lse, want_lse, workspace, stream)
 PyObject* paged_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (!counted(n, 12)) return nullptr;
@@ -246,11 +261,8 @@ PyObject* paged_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const Tensor& q = heads(a[2], ScalarType::BFloat16, -1, D, index, "q");
     const int64_t B = q.size(0), H = q.size(1);
     if (H % c->heads != 0) refuse("%s must be a multiple of the cache's heads", "q_heads");
-    const Tensor* table = tensor(a[3]);
-    if (!on(table, index) || table->scalar_type() != ScalarType::Int || table->dim() != 2 || table->size(0) != B ||
-        (table->stride(1) != 1 && table->size(1) > 1))
-      refuse("%s must be an int32 CUDA tensor [%lld, pages] on device %lld with unit column stride", "block_table", B,
-             index);
+    const Tensor& table = table_of(a[3], B, index);
+    const int64_t ts = table_step(table);
     const Tensor& lengths = vector(a[4], ScalarType::Int, B, index, "lengths");
     float scale = (float)std::pow((double)D, -0.5);
     if (given(a[5])) {
@@ -287,12 +299,11 @@ PyObject* paged_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (!out.defined()) out = fresh({B, H, D}, ScalarType::BFloat16, q);
     if (!lse.defined() && truth(a[9])) lse = fresh({B, H}, ScalarType::Float, q);
     void* stream = stream_of(a[11]);
-    const int64_t pages = table->size(1);
     int st;
     {
       Unlocked unlocked;
       st = mixfp4_paged_attention(q.const_data_ptr(), step(q, 0), step(q, 1), B, H, c,
-                                  table->const_data_ptr<int32_t>(), std::max(step(*table, 0), pages), pages,
+                                  table.const_data_ptr<int32_t>(), ts, table.size(1),
                                   lengths.const_data_ptr<int32_t>(), scale, window, out.mutable_data_ptr(),
                                   lse.defined() ? lse.mutable_data_ptr<float>() : nullptr,
                                   workspace.mutable_data_ptr(), need, stream);
@@ -315,21 +326,6 @@ const int64_t* masks(PyObject* o, int64_t B, int64_t t, int64_t index, int64_t* 
   if (d == 2 && B > 1) *stride = m->stride(0);
   if (*stride != 0 && *stride < t) refuse("%s must not have overlapping rows", "mask");
   return m->const_data_ptr<int64_t>();
-}
-
-const Tensor& table_of(PyObject* o, int64_t B, int64_t index) {
-  const Tensor* table = tensor(o);
-  if (!on(table, index) || table->scalar_type() != ScalarType::Int || table->dim() != 2 ||
-      (B >= 0 && table->size(0) != B) || (table->stride(1) != 1 && table->size(1) > 1))
-    refuse("%s must be an int32 CUDA tensor [%lld, pages] on device %lld with unit column stride", "block_table", B,
-           index);
-  return *table;
-}
-// A table's stride from row to row, at least its width.
-int64_t table_step(const Tensor& table) {
-  const int64_t pages = table.size(1);
-  if (table.size(0) > 1 && table.stride(0) < pages) refuse("%s must not have overlapping rows", "block_table");
-  return std::max(step(table, 0), pages);
 }
 
 int64_t length_of(PyObject* o, const char* what) {
