@@ -40,6 +40,15 @@ def random_trees(batch, t, g):
     return parents, mask
 
 
+def branch_pages(own, lengths, parents, page):
+    """Of children with pages own[i] (int32 [n, width]) and parents' lengths: the page that takes the parent's last one if
+    that is filled in part (-1: none is), and the first of the child's columns that are its own."""
+    length = lengths[parents.long()].long()
+    part = length // page  # the table's width where the parent has filled it
+    fresh = own.gather(1, part.clamp(max=own.shape[1] - 1)[:, None]).squeeze(1)
+    return torch.where(length % page > 0, fresh, -1).to(torch.int32), part
+
+
 class Layer:
     """Weights and paged cache of one attention layer, and the requests in it."""
 
@@ -109,8 +118,7 @@ class Layer:
         if self.spare.numel() < n * width:
             raise ValueError(f"{n} branches want {n * width} pages, {self.spare.numel()} are left")
         own, self.spare = self.spare[:n * width].view(n, width), self.spare[n * width:]
-        part = (self.lengths // self.page)[parents.long()].long()
-        fresh = own.gather(1, part[:, None]).squeeze(1).contiguous()
+        fresh, part = branch_pages(own, self.lengths, parents, self.page)
         table, self.lengths = ops.mixfp4_kv_fork(self.cache, self.table, self.lengths, parents, fresh)
         later = torch.arange(width, device=table.device) >= part[:, None]
         self.table = torch.where(later, own, table)
