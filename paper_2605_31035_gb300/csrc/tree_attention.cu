@@ -157,7 +157,9 @@ struct Cfg {
   static constexpr int kChain = kChainTokens / kTokens;    // tiles to a chain of sums
   static constexpr int kCw = kTokens / 4;                  // and of its quarter, a thread's step
   static constexpr int kBlock = kTokens * 128;             // 64 dimensions of a tile
-  static constexpr int kStep = kTokens == 128 || MT == 2 ? 32 : 16;  // columns of scores that a thread has in registers
+  // Columns of scores that a thread has in registers; with one tile of rows its copy's share of a tile, or a part of it.
+  static constexpr int kStep = kTokens == 128 || MT == 2 ? 32 : 16;
+  static_assert(kStep == kCw || MT == 2);
   static constexpr int kSlot = kBlock * (DT / 64);
   static constexpr int kSoftmax = 4 * MT;                  // warps, four to a tile of rows
   static constexpr int kQ = MT * 128 * DT * 2;
@@ -787,12 +789,8 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
           float top = -INFINITY;
           uint32_t v[PW];
           const int c_end = (step0 + steps) * CW;
-          const bool narrow = PW > CW && steps == 1;  // half a step
           auto load = [&](int c) {
-            if (narrow)
-              tmem_load<16>(scores + c, v);
-            else
-              tmem_load<PW>(scores + c, v);
+            tmem_load<PW>(scores + c, v);
             tmem_loaded<PW>(v);
           };
 #pragma unroll 1
@@ -802,7 +800,6 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
               float top2 = -INFINITY;  // two chains
 #pragma unroll
               for (int e = 0; e < PW; e += 4) {
-                if (e == 16 && narrow) break;
                 top = max3f(top, __uint_as_float(v[e]), __uint_as_float(v[e + 1]));
                 top2 = max3f(top2, __uint_as_float(v[e + 2]), __uint_as_float(v[e + 3]));
               }
@@ -812,7 +809,6 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
               const u64 ff = pack2(fs, fs);
 #pragma unroll
               for (int e = 0; e < PW; e += 2) {
-                if (e == 16 && narrow) break;
                 float x0, x1;
                 unpack2(mul2(bits2(v[e], v[e + 1]), ff), x0, x1);
                 v[e] = __float_as_uint(x0), v[e + 1] = __float_as_uint(x1);
@@ -820,7 +816,6 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
               if (p.softcap > 0.0f) {
 #pragma unroll
                 for (int e = 0; e < PW; e += 2) {
-                  if (e == 16 && narrow) break;
                   float x0 = __uint_as_float(v[e]), x1 = __uint_as_float(v[e + 1]);
                   tanh2(x0, x1);
                   v[e] = __float_as_uint(cap2 * x0), v[e + 1] = __float_as_uint(cap2 * x1);
@@ -831,13 +826,11 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
                   const float far0 = (float)(place - a);
 #pragma unroll
                   for (int e = 0; e < PW; ++e) {
-                    if (e == 16 && narrow) break;
                     v[e] = __float_as_uint(fmaf(slope, far0 - (float)e, __uint_as_float(v[e])));
                   }
                 } else {
 #pragma unroll
                   for (int e = 0; e < PW; ++e) {
-                    if (e == 16 && narrow) break;
                     const int j = a + e;
                     int far = place - j;
                     if (j >= w.s.first) far = place - w.s.first - depth[min(j - w.s.first, kMostDrafts - 1)];
@@ -849,24 +842,17 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
                 const uint32_t seen = seen_of(c);
 #pragma unroll
                 for (int e = 0; e < PW; ++e) {
-                  if (e == 16 && narrow) break;
                   v[e] = (seen >> e) & 1u ? v[e] : __float_as_uint(-INFINITY);
                 }
               }
               float top2 = -INFINITY;
 #pragma unroll
               for (int e = 0; e < PW; e += 4) {
-                if (e == 16 && narrow) break;
                 top = max3f(top, __uint_as_float(v[e]), __uint_as_float(v[e + 1]));
                 top2 = max3f(top2, __uint_as_float(v[e + 2]), __uint_as_float(v[e + 3]));
               }
               top = fmaxf(top, top2);
-              if (c_end - step0 * CW > PW || slow) {
-                if (narrow)
-                  tmem_store<16>(scores + c, v);
-                else
-                  tmem_store<PW>(scores + c, v);
-              }
+              if (c_end - step0 * CW > PW || slow) tmem_store<PW>(scores + c, v);
             }
           }
           if (general)
@@ -904,7 +890,6 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
               uint32_t out[kFp4 ? PW / 2 : PW];
 #pragma unroll
               for (int e = 0; e < PW; e += 2) {
-                if (e == 16 && narrow) break;
                 float x0, x1;
                 unpack2(fma2(bits2(v[e], v[e + 1]), ff, ll), x0, x1);
                 const float w0 = ex2(x0), w1 = ex2(x1);
@@ -925,10 +910,7 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
               }
               if constexpr (kFp4) {
                 tmem_store<CW / 2>(scores + c, out);
-                if constexpr (PW > CW)
-                  if (!narrow) tmem_store<CW / 2>(scores + c + CW, out + CW / 2);
-              } else if (narrow) {
-                tmem_store<CW>(scores + c, out);
+                if constexpr (PW > CW) tmem_store<CW / 2>(scores + c + CW, out + CW / 2);
               } else {
                 tmem_store<PW>(scores + c, out);
               }
