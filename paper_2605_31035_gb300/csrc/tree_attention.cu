@@ -737,7 +737,7 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
         for (int k = 0; k < C::kWords; ++k) whole = whole && there[k] == kAll;
         const bool edge = p.window > 0 && j0 < w.s.first + w.s.c - p.window;  // some rows' windows begin behind j0
         // Rows may see different tokens, or, by a mask, none the only draft.
-        const bool uneven = (w.s.c > 1 || p.mask) && (edge || j0 + TN > w.s.first);
+        const bool uneven = (edge || j0 + TN > w.s.first) && (w.s.c > 1 || (p.mask && !(sh.bits[0] & 1)));
         const bool masked = !whole || edge || j0 + TN > w.s.first;
         const bool general = masked || !plain;
 
