@@ -13,9 +13,10 @@
 //     the CTA ends.
 //   * Few rows: 32 (or 64) rows are held four times (twice) in the 128 lanes and each copy takes its quarter (half) of a
 //     tile's tokens, by products that write its lanes of O alone; the copies are joined at the end.  A thread then has a
-//     quarter of the scores: 187 instead of 201 us at 8 drafts below, 204 instead of 255 on a MixFP4 cache.
+//     quarter of the scores: 179 instead of 192 us at 8 drafts below, 185 instead of 239 on a MixFP4 cache.
 //   * More than 128 rows (and up to 128 dimensions): two tiles of rows to a CTA, so that K and V are fetched, and decoded,
-//     once for both.  412 instead of 435 us at 64 drafts, 469 instead of 581 on a MixFP4 cache; 40 drafts 392 and 399.
+//     once for both.  375 instead of 420 us at 64 drafts, 428 instead of 532 on a MixFP4 cache; at 40 drafts 363 and 380,
+//     401 and 443.
 //   * On a bf16 cache the weights keep 16 bits in two bf16 parts of one sign; on a MixFP4 one f16's 11, and the queries
 //     are scaled per row by a power of two into f16: exact but for elements below 2^-31 of the row's largest, which are
 //     off by up to 2^-39 of it, half of f16's least step.
@@ -23,14 +24,15 @@
 //     than there is), a weight of 0 would still make NaN of an infinite or NaN element of V.  Such tiles are looked over
 //     for those, and where there is one the threads take the products themselves, of what each row sees alone.
 //   * Tokens are cut into equal shares over the device.  CTAs of neighbouring heads walk the same tokens at the same time,
-//     whose rows lie together: 187 instead of 200 us at 8 drafts, 412 instead of 505 at 64.
+//     whose rows lie together: 179 instead of 181 us at 8 drafts, 375 instead of 383 at 64, on a MixFP4 cache
+//     185 instead of 206 and 428 instead of 467.
 //
 // Measured on 64 sequences of up to 8192 tokens, 32 query heads on 8, 128 dimensions (bf16 cache 1.1 GB, MixFP4 0.3 GB):
-// bf16 182 us at 8 drafts (6.0 TB/s: bound by HBM), 197 at 16, 381 at 64 (648 TFLOP/s: bound by the tensor cores, which
-// take P in two parts, and by what the softmax of 256 rows issues); MixFP4 180 us at 8 and 418 at 64 drafts, bound by the
+// bf16 179 us at 8 drafts (6.1 TB/s: bound by HBM), 193 at 16, 375 at 64 (658 TFLOP/s: bound by the tensor cores, which
+// take P in two parts, and by what the softmax of 256 rows issues); MixFP4 185 us at 8 and 428 at 64 drafts, bound by the
 // instructions of decoding and of the softmax (half of the issue slots used).  Short rows are bound by their beginning
-// and end, some 7 us each: 142 sequences of 2 tokens with 32 key heads, 30 rows to an SM, 108 us, MixFP4 219.
-// The rules below give both sides as they were measured when the rule was made.
+// and end, some 7 us each: 142 sequences of 2 tokens with 32 key heads, 30 rows to an SM, 106 us, MixFP4 215.
+// The rules here and below give both sides, the other one measured with all else as it is.
 #include <cuda_runtime.h>
 #include <atomic>
 #include <cstdint>
@@ -55,9 +57,10 @@ constexpr uint64_t kWaitLimitNs = 1000000000ull;
 // the sum a link, and 8192 tokens are 512 links (1024 with two parts of the weights).
 constexpr int kChainTokens = 8192;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-// How far a score may lie above the m of its weight 2^(s - m), which follows the maximum from afar (187 us at 8 drafts,
-// 412 at 64; 191 and 443 where it follows at once): bf16 parts and fp32 sums have the room.  On a MixFP4 cache the
-// weights are 2^7 times that: at most 2^15 in f16, whose least value is then 2^-31 of the weight at m.
+// How far a score may lie above the m of its weight 2^(s - m), which follows the maximum from afar (179 us at 8 drafts,
+// 375 at 64, MixFP4 185 and 428; 182 and 407, 191 and 478 where it follows at once): bf16 parts and fp32 sums have the
+// room.  On a MixFP4 cache the weights are 2^7 times that: at most 2^15 in f16, whose least value is then 2^-31 of the
+// weight at m.
 constexpr float kSlack = 16.0f, kFp4Slack = 8.0f, kFp4Exp = 7.0f;
 // A MixFP4 operand's elements are their values under the block scale over this (fp4_to_f16).
 constexpr float kFp4Unit = 512.0f;
@@ -145,30 +148,33 @@ struct Maps {
 template <int DT, int MT, bool kFp4>
 struct Cfg {
   // With one tile of rows two CTAs share an SM: what one does once a row (its queries, its end) the other's tiles cover
-  // (187 instead of 229 us at 8 drafts).  A MixFP4 cache's decoding takes the registers and the larger tiles of one (two
-  // were 358 instead of 236 us).
+  // (179 instead of 204 us at 8 drafts).  A MixFP4 cache's decoding takes the registers and the shared memory of one.
   static constexpr int kCtas = !kFp4 && MT == 1 && DT <= 128 ? 2 : 1;
-  // Of a tile.  A larger one has fewer steps between the roles, which on a MixFP4 cache are most of the time (203 instead
-  // of 270 us at 8 drafts); a bf16 one of two CTAs has no room for it, nor have two tiles of rows in tensor memory.
+  // Of a tile.  A larger one has fewer steps between the roles, which on a MixFP4 cache are most of the time (185 instead
+  // of 263 us at 8 drafts); a bf16 one of two CTAs has no room for it, nor have two tiles of rows in tensor memory.
   static constexpr int kTokens = kFp4 && MT == 1 && DT <= 128 ? 128 : 64;
   // What beginning a row costs (its queries, the way to its first pages, its end), in tiles.  64 sequences of up to 8192
-  // tokens, us at a cost of 0, 2, 4, 8 and 12: 8 drafts 195, 187, 183, 184, 184; 64 drafts 425, 412, 404, 383, 385.
+  // tokens, us at a cost of 0, 2, 4, 8 and 12: 8 drafts 190, 181, 179, 180, 180, MixFP4 193, 188, 185, 189, 195; 64 drafts
+  // 419, 399, 390, 375, 377.
   static constexpr int kRowCost = MT == 2 ? 8 : 4;
   static constexpr int kChain = kChainTokens / kTokens;    // tiles to a chain of sums
   static constexpr int kCw = kTokens / 4;                  // and of its quarter, a thread's step
   static constexpr int kBlock = kTokens * 128;             // 64 dimensions of a tile
-  // Columns of scores that a thread has in registers; with one tile of rows its copy's share of a tile, or a part of it.
+  // Columns of scores that a thread has in registers; with one tile of rows its copy's share of a tile, or a part of it;
+  // with two 32 (at 40 and 64 drafts 363 and 375 us; with 16 370 and 378, MixFP4 401 and 428, 424 and 438).
   static constexpr int kStep = kTokens == 128 || MT == 2 ? 32 : 16;
   static_assert(kStep == kCw || MT == 2);
   static constexpr int kSlot = kBlock * (DT / 64);
   static constexpr int kSoftmax = 4 * MT;                  // warps, four to a tile of rows
   static constexpr int kQ = MT * 128 * DT * 2;
-  // Warps that decode (196 us at 8 drafts; 16 of them 216), or bring a bf16 cache's rows where TMA cannot.
+  // Warps that decode (185 us at 8 drafts; 16 of them, with 80 registers to a thread, 268), or bring a bf16 cache's rows
+  // where TMA cannot.
   static constexpr int kProducers = kFp4 ? 8 : 2;
   static constexpr int kThreads = (kSoftmax + 4 + (kFp4 ? kProducers : 0)) * 32;  // the four: products, TMA or helpers
-  // Registers of a thread at launch, then of softmax and of the other threads (together no more than at launch).
+  // Registers of a thread at launch, then of softmax and of the other threads (together no more than at launch).  MixFP4
+  // at 64 drafts 428 us; with no split, or with 72 for the others, 436, with 88 432.
   static constexpr int kRegs = 65536 / (kThreads * kCtas) / 8 * 8;
-  static constexpr int kOtherRegs = kFp4 && MT == 2 ? 72 : kRegs;
+  static constexpr int kOtherRegs = kFp4 && MT == 2 ? 80 : kRegs;
   static constexpr int kLeft = (kRegs * kThreads - kOtherRegs * (kThreads - kSoftmax * 32)) / (kSoftmax * 32) / 8 * 8;
   static constexpr int kSoftRegs = kLeft < 232 ? kLeft : 232;
   static constexpr int kRows = kTokens / kProducers;       // of a tile, to a producer warp
@@ -638,7 +644,7 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
       float fs = p.scale * (kFp4 ? kFp4Unit * kts : 1.0f);
       {
         constexpr int kLanes = DT / 8, kRowsAtOnce = 32 / kLanes;
-        constexpr int kBatch = 4;  // steps asked for at once (2: 399 us at 64 drafts, 4: 380, 8: 382)
+        constexpr int kBatch = 4;  // steps asked for at once (2: 396 us at 64 drafts, 4: 375, 8: 373; MixFP4 442, 428, 438)
         const int steps_q = kLanes / copies, u = lane % kLanes, base = copy * (32 / copies) + lane / kLanes;
         const int64_t from = valid ? (int64_t)w.b * p.q_stride + (int64_t)i * p.q_token_stride + (int64_t)h * p.q_head_stride
                                    : -1;
@@ -756,7 +762,7 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
             bool bad = false;
             constexpr uint32_t kExp = kFp4 ? 0x7C00u : 0x7F80u;
             // From the first row that not all see to the last that there is (of short rows few: 142 sequences of 2 tokens
-            // with 32 key heads 291 us with the tile's other rows, 224 without).
+            // with 32 key heads 122 us with the tile's other rows, 106 without; MixFP4 283 and 215).
             const int row0 = edge ? 0 : max(w.s.first - j0, 0), rows_v = min(TN, w.s.end - j0) - row0, units = D / 8;
 #pragma unroll 2
             for (int x = tl; x < rows_v * units; x += 128) {
@@ -1132,8 +1138,8 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
           if (!*reinterpret_cast<volatile int*>(&sh.skip[buf])) {
             const uint64_t v = smem_desc_sw128_mn(ring + slot * C::kSlot, C::kBlock);
             const uint32_t o = tmem + C::kScoreCols + m * DT;
-            // Not written out, as the softmax's queries are not, for the instruction caches' sake: MixFP4 at 8 drafts 182 us
-            // with all of it unrolled, 180 so (and 186 one by one); at 64 drafts 457, 435 and 417.
+            // Not written out, as the softmax's queries are not, for the instruction caches' sake: MixFP4 at 8 drafts 187 us
+            // with all of it unrolled, 185 so (and 192 one by one); at 64 drafts 454, 441 and 428.
             constexpr int kAtOnce = kFp4 && MT == 2 ? 1 : 2;
 #pragma unroll kAtOnce
             for (int k = 0; k < TN / 16; ++k) {
@@ -1414,7 +1420,7 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
         cp_wait_at_most(later), __syncwarp();
       dead = __any_sync(kAll, dead);
       const uint32_t bytes = raw + 2 * C::kCodes + piece + (p.box && p.scale_by_head ? w.head * (D / 16) & 15 : 0);
-#pragma unroll 1  // one copy of the code: the instruction caches are shared by all roles (214 us written out, 204 so)
+#pragma unroll 1  // one copy of the code: the instruction caches are shared by all roles (215 us written out, 185 so)
       for (int kv = 0; kv < 2; ++kv) {
         const uint32_t q = 2 * sent + kv, slot = q % C::kSlots;
         Codes<kSteps> c;
@@ -1431,7 +1437,8 @@ __global__ void __launch_bounds__(Cfg<DT, MT, kFp4>::kThreads, Cfg<DT, MT, kFp4>
       ++sent;
     };
     // Rows of an odd number of scale bytes (or of pairs): a lane to a byte, asked for with a tile's codes and put in place
-    // before the next tile's are, so that no warp waits for them (80 dimensions 922 us where they did, 708 so).
+    // before the next tile's are, so that no warp waits for them (80 dimensions 744 us, and 740 where they do: the other
+    // warps cover that; 128 dimensions, whose loop this is too, 185 and 188).
     constexpr int kMost = (2 * kRows * 15 + 31) / 32;
     uint32_t odd[kMost] = {}, odd_at = 0;  // of a tile, and where its rows' bytes go; 0: none
     auto each_byte = [&](auto&& f) {  // f(k, row, keys or values, byte)
@@ -1597,7 +1604,7 @@ inline bool scales_by_token(const mixfp4_kv_cache& c) {
   return 16 % n == 0 && c.scale_token_stride == n && (c.scale_head_stride | c.scale_page_stride) % 16 == 0 &&
          aligned(c.k_scales, 16) && aligned(c.v_scales, 16);
 }
-// Rows that one TMA copy brings (bf16 at 8 drafts 187 us, by cp.async 222; MixFP4 203 and 287): of one page, and a part
+// Rows that one TMA copy brings (bf16 at 8 drafts 179 us, by cp.async 216; MixFP4 185 and 268): of one page, and a part
 // of a tile; 0 where TMA's rules do not allow it (pages of no multiple of 16 tokens, rows of codes that are no multiple of
 // 16 bytes or lie on none) or bf16 rows of less than 64 elements would not fill the operand's.
 inline int box_of(const mixfp4_kv_cache& c, int tokens) {
