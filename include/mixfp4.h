@@ -616,7 +616,8 @@ int mixfp4_paged_attention_workspace(const mixfp4_kv_cache* cache, int64_t B, in
  *              mixfp4_tree_attention_workspace reports; free for reuse once the
  *              call's work on `stream` is done.
  * status_word  as mixfp4_gemm's: 0 unless a wait of the kernel ran out, in
- *              which case the results are not to be used.
+ *              which case the results are not to be used.  A call without rows
+ *              (B, t or q_heads 0) does not write it.
  */
 int mixfp4_tree_attention(const void* q, int64_t q_stride, int64_t q_token_stride, int64_t q_head_stride, int64_t B,
                           int64_t t, int64_t q_heads, const mixfp4_kv_cache* cache, const int32_t* block_table,

@@ -2,10 +2,12 @@
 // drafts (mixfp4_kv_accept), branching sequences (mixfp4_kv_fork) and whole
 // pages (mixfp4_kv_copy_pages).
 //
-// Bytes are read once and written once: 4099 pages of 64 KB move in 79 us, 1.00 of the
-// rate of a plain copy.  What is small is a wait for lengths and table, then one for the
-// rows: 512 children of 256 sequences 14 us, 256 sequences' accepted drafts 7 us, 5 pages
-// or 8 sequences 3 us.  A page is a set of runs of bytes that
+// Bytes are read once and written once: 4099 pages of 64 KB move in 82 us, 0.96 of the
+// rate of a plain copy; of 18 KB (MixFP4) in 54, 0.41: a CTA's share of one is a single
+// piece a thread, and its scale bytes take a CTA of their own.  What is small is a wait for
+// lengths and table, then one for the rows: 512 children of 256 sequences 10 us (MixFP4), 200
+// sequences' accepted drafts 4.7 us, 256 sequences' 6.9 (512 CTAs of 150 registers, of which
+// 456 run at once: a second round), 5 pages or 8 sequences 3 to 4 us.  A page is a set of runs of bytes that
 // lie together: the whole page where it is dense in either order of tokens and
 // heads, a token's heads or a head's tokens where only those are, else single head
 // rows.  A CTA takes a share of one page's keys or values (or their scales), four
